@@ -1,0 +1,107 @@
+/*
+ * im2win_seq.h -- operators over sequences of tokens: the short causal
+ * convolution of state space layers (a depthwise convolution along time),
+ * the selective state space scan that reads its output, and the
+ * root-mean-square norm with the residual's addition in front of both.
+ * Exported by libim2win beside the im2win entry points of im2win.h (same
+ * error codes, error messages and conventions about streams and ownership;
+ * see there).  Where this header differs:
+ *
+ *  - Tokens are rows.  A tensor of T tokens and D channels is T x D with its
+ *    channels contiguous; inputs may have a row stride of their own (ld_*, in
+ *    elements, at least the row's width), so that slices of a wider row can
+ *    be read in place.  Outputs are dense.
+ *  - Sequences lie one behind the other in the rows.  seq_starts (device,
+ *    sequences + 1 int32, not decreasing) gives their first rows: sequence b
+ *    is [seq_starts[b], seq_starts[b+1]), possibly empty.  NULL means
+ *    sequences of tokens / sequences rows each.  Rows before the first start
+ *    and behind the last are neither read nor written.  Values outside of
+ *    [0, tokens] are taken as the nearest of the two.
+ *  - Pointers need the alignment of their element type only (wide loads are
+ *    used where pointers, strides and sizes allow them); workspaces need 16
+ *    bytes.
+ *  - Arrays of T rows may be NULL when tokens is 0.  Outputs must not overlap
+ *    inputs or each other, except where an entry point says so.
+ *  - "dtype" arrays hold im2win_dtype elements; every sum, state, statistic
+ *    and gradient of a parameter is fp32.  Results are rounded once, when
+ *    they are written, and every sum has a fixed order: a call gives the same
+ *    bits each time.
+ */
+#ifndef IM2WIN_SEQ_H
+#define IM2WIN_SEQ_H
+
+#include "im2win.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ------------------------------------------------------------------------ */
+/* Short causal convolution                                                  */
+/* ------------------------------------------------------------------------ */
+
+typedef struct {
+    int64_t tokens;      /* T, rows of x (requests, for the step) */
+    int64_t channels;    /* D */
+    int64_t width;       /* W, taps, 1 to 8 */
+    int64_t sequences;   /* B >= 1 (not used by the step) */
+    int64_t ld_x;        /* row stride of x */
+    int32_t dtype;       /* of x, w, bias, y, the states and their gradients */
+    int32_t silu;        /* nonzero: y = s * sigmoid(s) of the sum s */
+} im2win_conv1d_desc;
+
+/*
+ * y[t][c] = act(bias[c] + sum_{k<W} w[c][k] * x[t - (W-1) + k][c])
+ * where the inputs before a sequence's first row are its initial state's
+ * rows (initial_state[b][j] lies W-1-j tokens before the first), or zero.
+ *   x              device, T x D, row stride ld_x
+ *   w              device, D x W;  bias  device, D, or NULL
+ *   initial_state  device, B x (W-1) x D, or NULL (zeros)
+ *   y              device, T x D
+ *   final_state    device, B x (W-1) x D, or NULL: the last W-1 inputs of
+ *                  each sequence (of its initial state too, where it is
+ *                  shorter), as the next call's initial state
+ * Errors: EINVAL, ENULL, EALIGN, EOVERFLOW, EHIP.
+ */
+int im2win_causal_conv1d(const im2win_conv1d_desc* d, const void* x, const void* w,
+                         const void* bias, const int32_t* seq_starts, const void* initial_state,
+                         void* y, void* final_state, void* stream);
+
+/* Bytes of workspace that im2win_causal_conv1d_backward takes.  Host only. */
+int im2win_causal_conv1d_backward_workspace_bytes(const im2win_conv1d_desc* d, size_t* bytes);
+
+/*
+ * Gradients of im2win_causal_conv1d for the gradient dy of y (T x D) and,
+ * where d_final_state (B x (W-1) x D) is given, of the final state.
+ *   dx               device, T x D
+ *   dw, dbias        device, D x W and D, fp32 (dbias may be NULL)
+ *   d_initial_state  device, B x (W-1) x D, or NULL
+ *   workspace        device, 16-byte aligned, at least the bytes above
+ * Errors: EINVAL, ENULL, EALIGN, EWORKSPACE, EOVERFLOW, EHIP.
+ */
+int im2win_causal_conv1d_backward(const im2win_conv1d_desc* d, const void* dy, const void* x,
+                                  const void* w, const void* bias, const int32_t* seq_starts,
+                                  const void* initial_state, const void* d_final_state, void* dx,
+                                  float* dw, float* dbias, void* d_initial_state, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/*
+ * One token for each of d->tokens requests.  Request i's last W-1 inputs are
+ * state[slots[i]] of a pool of state_slots states (W-1 x D each); the call
+ * moves them on by one token in place.  slots NULL means slot i.  A request
+ * whose slot is outside of [0, state_slots) gets y = 0 and leaves the pool as
+ * it is.  No two requests may name the same slot.
+ *   x, y   device, T x D (x with row stride ld_x);  w, bias as above
+ *   state  device, state_slots x (W-1) x D (read and written; may be NULL
+ *          when W is 1)
+ * Errors: EINVAL, ENULL, EALIGN, EOVERFLOW, EHIP.
+ */
+int im2win_causal_conv1d_step(const im2win_conv1d_desc* d, const void* x, const void* w,
+                              const void* bias, const int32_t* slots, void* state,
+                              int64_t state_slots, void* y, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* IM2WIN_SEQ_H */

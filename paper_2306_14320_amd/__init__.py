@@ -6,7 +6,9 @@ marshal arguments; every step of the computation runs in the HIP kernels.
 The tensor helpers below them (``desc_for``, ``transform``, ``conv2d``,
 ``conv2d_fused``) check that the tensors match the descriptor and use PyTorch
 only to allocate device memory (window tensor, filter scratch, output) on the
-call's HIP stream.
+call's HIP stream.  The operators over sequences of tokens
+(``include/im2win_seq.h``) are bound the same way in ``sequence.py`` and
+exported here.
 
 There is no fallback: if the library is missing or was built for another
 target, loading fails with an error.  Build it with
@@ -88,6 +90,7 @@ def load_library():
         "im2win_selftest": [],
         "im2win_check_plan": [D],
     }
+    sigs.update(sequence.SIGNATURES)
     for name, args in sigs.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -346,3 +349,7 @@ def direct_conv2d(x: torch.Tensor, w: torch.Tensor, desc: im2win_desc, y: torch.
     y, yp = _output(y, desc, x.device, stream)
     im2win_direct_conv2d(desc, xp, wp, yp, _stream(stream))
     return y
+
+
+from . import sequence  # noqa: E402  (needs the names above)
+from .sequence import *  # noqa: E402,F401,F403

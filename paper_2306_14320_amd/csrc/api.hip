@@ -13,6 +13,7 @@
 #include "common.h"
 #include "conv_common.h"
 #include "direct.h"
+#include "error.h"
 
 // Filter scratch of im2win_conv2d_fused_noalloc: a static device array, so
 // that the call allocates nothing.  Each device holds its own copy; its
@@ -20,9 +21,9 @@
 // and kept.  Host code uses only that address, never the array's name.
 static __device__ __align__(256) unsigned char scratch[IM2WIN_NOALLOC_SCRATCH_BYTES];
 
-namespace {
+static thread_local char g_err[512] = "";
 
-thread_local char g_err[512] = "";
+namespace im2win {
 
 int fail(int code, const char* fmt, ...) {
     va_list ap;
@@ -36,6 +37,13 @@ int ok() {
     g_err[0] = '\0';
     return IM2WIN_OK;
 }
+
+}  // namespace im2win
+
+using im2win::fail;
+using im2win::ok;
+
+namespace {
 
 constexpr int64_t kI31 = (int64_t(1) << 31) - 1;   // kernels index with 32-bit ints
 constexpr int64_t kI62 = int64_t(1) << 62;

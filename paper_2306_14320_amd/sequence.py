@@ -1,0 +1,235 @@
+"""Binding of the sequence operators of ``libim2win.so``
+(``include/im2win_seq.h``): the short causal convolution, its gradients and
+its form for single tokens.
+
+The ``im2win_*`` functions mirror the C entry points and take device pointers;
+the tensor helpers below them check every tensor against the descriptor and
+allocate outputs and workspaces with ``torch.empty`` on the call's stream.
+Tokens are rows: x is T x D with contiguous channels and a row stride of its
+own; ``seq_starts`` (int32, sequences + 1 values on the device) gives the
+sequences' first rows, and without it the sequences are of equal length.
+Rows that no sequence holds are neither read nor written, so the outputs'
+rows there hold what the memory held.
+"""
+import ctypes
+from typing import NamedTuple, Optional
+
+import torch
+
+from . import (_DTYPES, _check, _empty, _stream, IM2WIN_F32, load_library)
+
+__all__ = [
+    "im2win_conv1d_desc", "im2win_causal_conv1d", "im2win_causal_conv1d_backward_workspace_bytes",
+    "im2win_causal_conv1d_backward", "im2win_causal_conv1d_step",
+    "causal_conv1d_desc_for", "causal_conv1d", "causal_conv1d_backward", "causal_conv1d_step", "Conv1dGradients",
+]
+
+_P, _SZ, _I64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64
+
+
+class _Desc(ctypes.Structure):
+    def __repr__(self):
+        return "%s(%s)" % (type(self).__name__, ", ".join("%s=%s" % (f[0], getattr(self, f[0])) for f in self._fields_))
+
+
+class im2win_conv1d_desc(_Desc):
+    """Mirror of the C ``im2win_conv1d_desc``."""
+    _fields_ = [("tokens", _I64), ("channels", _I64), ("width", _I64), ("sequences", _I64), ("ld_x", _I64),
+                ("dtype", ctypes.c_int32), ("silu", ctypes.c_int32)]
+
+
+_CONV = ctypes.POINTER(im2win_conv1d_desc)
+
+SIGNATURES = {
+    "im2win_causal_conv1d": [_CONV] + [_P] * 8,
+    "im2win_causal_conv1d_backward_workspace_bytes": [_CONV, ctypes.POINTER(_SZ)],
+    "im2win_causal_conv1d_backward": [_CONV] + [_P] * 12 + [_SZ, _P],
+    "im2win_causal_conv1d_step": [_CONV] + [_P] * 5 + [_I64, _P, _P],
+}
+
+
+def _bytes(name, desc):
+    out = _SZ()
+    _check(getattr(load_library(), name)(ctypes.byref(desc), ctypes.byref(out)))
+    return out.value
+
+
+# ---------------------------------------------------------------------------
+# C entry points, same names and arguments (raising Im2winError on failure)
+# ---------------------------------------------------------------------------
+
+def im2win_causal_conv1d(desc, x, w, bias, seq_starts, initial_state, y, final_state, stream) -> None:
+    _check(load_library().im2win_causal_conv1d(ctypes.byref(desc), x, w, bias, seq_starts, initial_state, y,
+                                               final_state, stream))
+
+
+def im2win_causal_conv1d_backward_workspace_bytes(desc) -> int:
+    return _bytes("im2win_causal_conv1d_backward_workspace_bytes", desc)
+
+
+def im2win_causal_conv1d_backward(desc, dy, x, w, bias, seq_starts, initial_state, d_final_state, dx, dw, dbias,
+                                  d_initial_state, workspace, workspace_bytes, stream) -> None:
+    _check(load_library().im2win_causal_conv1d_backward(
+        ctypes.byref(desc), dy, x, w, bias, seq_starts, initial_state, d_final_state, dx, dw, dbias, d_initial_state,
+        workspace, workspace_bytes, stream))
+
+
+def im2win_causal_conv1d_step(desc, x, w, bias, slots, state, state_slots, y, stream) -> None:
+    _check(load_library().im2win_causal_conv1d_step(ctypes.byref(desc), x, w, bias, slots, state, state_slots, y,
+                                                    stream))
+
+
+# ---------------------------------------------------------------------------
+# Tensor helpers
+# ---------------------------------------------------------------------------
+
+def _torch_dtype(desc):
+    return torch.float32 if desc.dtype == IM2WIN_F32 else torch.bfloat16
+
+
+def _dtype_code(dtype):
+    if dtype not in _DTYPES:
+        raise ValueError(f"unsupported dtype {dtype} (float32 or bfloat16)")
+    return _DTYPES[dtype]
+
+
+def _row_stride(t, name):
+    """Elements from one row to the next of a tensor whose rows are contiguous
+    (its trailing dimensions, without gaps)."""
+    if not isinstance(t, torch.Tensor) or t.dim() < 2:
+        raise ValueError(f"{name} must be a tensor of rows")
+    width = 1
+    for size, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if size != 1 and stride != width:
+            raise ValueError(f"{name}: the elements of a row must lie one behind the other")
+        width *= size
+    return t.stride(0) if t.shape[0] > 1 else width
+
+
+def _device_of(t, name):
+    """The index of t's device, which has to be the current one (the call
+    launches there)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    dev = t.get_device()
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"{name} is on device {dev}, the current device is {torch.cuda.current_device()}")
+    return dev
+
+
+def _rows(t, name, shape, dtype, ld, dev):
+    """Pointer of a T x ... input whose rows are ld elements apart."""
+    if not isinstance(t, torch.Tensor) or t.get_device() != dev:
+        raise ValueError(f"{name} must be a tensor on device {dev}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs {shape}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, the call needs {dtype}")
+    if shape[0] > 1 and _row_stride(t, name) != ld:
+        raise ValueError(f"{name} has rows {t.stride(0)} elements apart, the descriptor says {ld}")
+    if shape[0] == 1:
+        _row_stride(t, name)
+    return t.data_ptr()
+
+
+def _dense(t, name, shape, dtype, dev):
+    """Pointer of a contiguous tensor; None stays None."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor on device {dev}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs {shape}")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} has dtype {t.dtype}, the call needs {dtype}")
+    return t.data_ptr()
+
+
+def _out(t, name, shape, dtype, like, dev, stream):
+    """An output and its pointer: t, or a new tensor."""
+    if t is None:
+        t = _empty(shape, dtype, like.device, stream)
+    return t, _dense(t, name, shape, dtype, dev)
+
+
+def _workspace(ws, need, like, stream):
+    """A workspace of at least `need` bytes, its pointer and size."""
+    if ws is None:
+        ws = _empty((max(need, 16),), torch.uint8, like.device, stream)
+    elif not isinstance(ws, torch.Tensor) or ws.get_device() != like.get_device() or not ws.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the inputs' device")
+    return ws, ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def causal_conv1d_desc_for(x, w, sequences=1, silu=True) -> im2win_conv1d_desc:
+    """Descriptor of the short causal convolution of x (T x D, rows of any
+    stride) with the taps w (D x W): `sequences` packed sequences, SiLU on the
+    sum unless silu is false."""
+    ld = _row_stride(x, "x")
+    if x.dim() != 2 or w.dim() != 2 or w.shape[0] != x.shape[1]:
+        raise ValueError(f"x must be T x D and w D x W (got {tuple(x.shape)} and {tuple(w.shape)})")
+    return im2win_conv1d_desc(x.shape[0], x.shape[1], w.shape[1], sequences, ld, _dtype_code(x.dtype), int(bool(silu)))
+
+
+def _conv_inputs(x, w, bias, seq_starts, initial_state, d):
+    dt, dev = _torch_dtype(d), _device_of(x, "x")
+    return dev, dt, (
+        _rows(x, "x", (d.tokens, d.channels), dt, d.ld_x, dev),
+        _dense(w, "w", (d.channels, d.width), dt, dev),
+        _dense(bias, "bias", (d.channels,), dt, dev),
+        _dense(seq_starts, "seq_starts", (d.sequences + 1,), torch.int32, dev),
+        _dense(initial_state, "initial_state", (d.sequences, d.width - 1, d.channels), dt, dev))
+
+
+def causal_conv1d(x, w, desc, bias=None, seq_starts=None, initial_state=None, y=None, final_state=None, stream=None):
+    """y[t] = act(bias + sum_k w[:, k] x[t - W + 1 + k]), T x D in x's dtype.
+    The inputs before a sequence are initial_state's (sequences x W-1 x D) or
+    zero; final_state, if given, receives each sequence's last W-1 inputs."""
+    dev, dt, (xp, wp, bp, sp, ip) = _conv_inputs(x, w, bias, seq_starts, initial_state, desc)
+    y, yp = _out(y, "y", (desc.tokens, desc.channels), dt, x, dev, stream)
+    fp = _dense(final_state, "final_state", (desc.sequences, desc.width - 1, desc.channels), dt, dev)
+    im2win_causal_conv1d(desc, xp, wp, bp, sp, ip, yp, fp, _stream(stream))
+    return y
+
+
+class Conv1dGradients(NamedTuple):
+    dx: torch.Tensor                # T x D, x's dtype
+    dw: torch.Tensor                # D x W, fp32
+    dbias: Optional[torch.Tensor]   # D, fp32; None without a bias
+    d_initial_state: Optional[torch.Tensor]
+
+
+def causal_conv1d_backward(dy, x, w, desc, bias=None, seq_starts=None, initial_state=None, d_final_state=None,
+                           workspace=None, stream=None) -> Conv1dGradients:
+    """Gradients of causal_conv1d for dy (T x D, dense) and, where it is given,
+    d_final_state.  d_initial_state is returned where initial_state is given."""
+    d = desc
+    dev, dt, (xp, wp, bp, sp, ip) = _conv_inputs(x, w, bias, seq_starts, initial_state, d)
+    state = (d.sequences, d.width - 1, d.channels)
+    dyp = _dense(dy, "dy", (d.tokens, d.channels), dt, dev)
+    dfp = _dense(d_final_state, "d_final_state", state, dt, dev)
+    dx, dxp = _out(None, "dx", (d.tokens, d.channels), dt, x, dev, stream)
+    dw, dwp = _out(None, "dw", (d.channels, d.width), torch.float32, x, dev, stream)
+    dbias, dbp = (None, None) if bias is None else _out(None, "dbias", (d.channels,), torch.float32, x, dev, stream)
+    di, dip = (None, None) if initial_state is None else _out(None, "d_initial_state", state, dt, x, dev, stream)
+    workspace, wsp, wsb = _workspace(workspace, im2win_causal_conv1d_backward_workspace_bytes(d), x, stream)
+    im2win_causal_conv1d_backward(d, dyp, xp, wp, bp, sp, ip, dfp, dxp, dwp, dbp, dip, wsp, wsb, _stream(stream))
+    return Conv1dGradients(dx, dw, dbias, di)
+
+
+def causal_conv1d_step(x, w, state, desc, bias=None, slots=None, y=None, stream=None):
+    """One token of each request: x is requests x D, state a pool of slots x
+    W-1 x D that moves on in place, slots (int32) the request's place in it
+    (its own index when None; outside of the pool: y = 0, nothing moves)."""
+    dt, dev = _torch_dtype(desc), _device_of(x, "x")
+    xp = _rows(x, "x", (desc.tokens, desc.channels), dt, desc.ld_x, dev)
+    wp = _dense(w, "w", (desc.channels, desc.width), dt, dev)
+    bp = _dense(bias, "bias", (desc.channels,), dt, dev)
+    if not isinstance(state, torch.Tensor):
+        raise ValueError("state must be a tensor")
+    pool = state.shape[0]
+    stp = _dense(state, "state", (pool, desc.width - 1, desc.channels), dt, dev)
+    slp = _dense(slots, "slots", (desc.tokens,), torch.int32, dev)
+    y, yp = _out(y, "y", (desc.tokens, desc.channels), dt, x, dev, stream)
+    im2win_causal_conv1d_step(desc, xp, wp, bp, slp, stp, pool, yp, _stream(stream))
+    return y
