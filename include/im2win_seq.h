@@ -100,6 +100,68 @@ int im2win_causal_conv1d_step(const im2win_conv1d_desc* d, const void* x, const 
                               const void* bias, const int32_t* slots, void* state,
                               int64_t state_slots, void* y, void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* Root-mean-square norm with the residual's addition                        */
+/* ------------------------------------------------------------------------ */
+
+typedef struct {
+    int64_t tokens;          /* T */
+    int64_t channels;        /* D, at most 16384 */
+    int64_t ld_x;            /* row stride of x */
+    int64_t block;           /* channels that share a scale of the 8-bit output: 0 (the row), or a
+                                power of two from 16 to 512 that divides D */
+    int32_t dtype;           /* of x, y and dy */
+    int32_t residual_dtype;  /* of the residual, h and their gradients */
+    float eps;               /* >= 0 */
+} im2win_norm_desc;
+
+/*
+ * h[t] = x[t] + residual[t], rounded to residual_dtype (h = x so rounded
+ * where residual is NULL);
+ * y[t][c] = h[t][c] * rsqrt(mean_c(h[t][c]^2) + eps) * w[c], of the rounded h.
+ *   x         device, T x D, row stride ld_x
+ *   residual  device, T x D, or NULL
+ *   w         device, D, fp32
+ *   y         device, T x D
+ *   h         device, T x D; may be residual itself (the sum in place), and
+ *             may be NULL where residual is NULL
+ * Errors: EINVAL, ENULL, EALIGN, EOVERFLOW, EHIP.
+ */
+int im2win_add_rms_norm(const im2win_norm_desc* d, const void* x, const void* residual, const float* w,
+                        void* y, void* h, void* stream);
+
+/*
+ * The same with y in 8 bits (OCP e4m3: 4 bits of exponent, 3 of mantissa,
+ * largest value 448): for each row, or each `block` channels of it,
+ *   scale = max |y| / 448 (1 where the block is all zeros or holds a NaN),
+ *   q = y / scale, rounded to nearest even.  y is not rounded before.  Beside
+ *   a NaN in its block a y beyond 448 has no value in q.
+ *   q       device, T x D, one byte each
+ *   scales  device, T x (D / block) (T x 1 for block 0), fp32
+ * Errors: EINVAL, ENULL, EALIGN, EOVERFLOW, EHIP.
+ */
+int im2win_add_rms_norm_fp8(const im2win_norm_desc* d, const void* x, const void* residual, const float* w,
+                            void* q, float* scales, void* h, void* stream);
+
+/* Bytes of workspace that im2win_add_rms_norm_backward takes.  Host only. */
+int im2win_add_rms_norm_backward_workspace_bytes(const im2win_norm_desc* d, size_t* bytes);
+
+/*
+ * Gradients for dy (T x D) and, where it is given, d_residual (T x D, the
+ * gradient that h receives from elsewhere): with r = rsqrt(mean(h^2) + eps)
+ * and g = dy w,
+ *   dx = r (g - h r^2 mean(g h)) + d_residual,  the gradient of x and of residual,
+ *   dw[c] = sum_t dy[t][c] h[t][c] r[t].
+ *   h   device, T x D, as the forward call wrote it
+ *   dx  device, T x D, residual_dtype; may be d_residual itself
+ *   dw  device, D, fp32
+ *   workspace  device, 16-byte aligned, at least the bytes above
+ * Errors: EINVAL, ENULL, EALIGN, EWORKSPACE, EOVERFLOW, EHIP.
+ */
+int im2win_add_rms_norm_backward(const im2win_norm_desc* d, const void* dy, const void* h, const float* w,
+                                 const void* d_residual, void* dx, float* dw, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

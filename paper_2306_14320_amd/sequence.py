@@ -1,6 +1,7 @@
 """Binding of the sequence operators of ``libim2win.so``
 (``include/im2win_seq.h``): the short causal convolution, its gradients and
-its form for single tokens.
+its form for single tokens, and the root-mean-square norm with the residual's
+addition.
 
 The ``im2win_*`` functions mirror the C entry points and take device pointers;
 the tensor helpers below them check every tensor against the descriptor and
@@ -22,6 +23,9 @@ __all__ = [
     "im2win_conv1d_desc", "im2win_causal_conv1d", "im2win_causal_conv1d_backward_workspace_bytes",
     "im2win_causal_conv1d_backward", "im2win_causal_conv1d_step",
     "causal_conv1d_desc_for", "causal_conv1d", "causal_conv1d_backward", "causal_conv1d_step", "Conv1dGradients",
+    "im2win_norm_desc", "im2win_add_rms_norm", "im2win_add_rms_norm_fp8",
+    "im2win_add_rms_norm_backward_workspace_bytes", "im2win_add_rms_norm_backward",
+    "rms_norm_desc_for", "add_rms_norm", "add_rms_norm_fp8", "add_rms_norm_backward",
 ]
 
 _P, _SZ, _I64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64
@@ -38,13 +42,24 @@ class im2win_conv1d_desc(_Desc):
                 ("dtype", ctypes.c_int32), ("silu", ctypes.c_int32)]
 
 
+class im2win_norm_desc(_Desc):
+    """Mirror of the C ``im2win_norm_desc``."""
+    _fields_ = [("tokens", _I64), ("channels", _I64), ("ld_x", _I64), ("block", _I64),
+                ("dtype", ctypes.c_int32), ("residual_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
 _CONV = ctypes.POINTER(im2win_conv1d_desc)
+_NORM = ctypes.POINTER(im2win_norm_desc)
 
 SIGNATURES = {
     "im2win_causal_conv1d": [_CONV] + [_P] * 8,
     "im2win_causal_conv1d_backward_workspace_bytes": [_CONV, ctypes.POINTER(_SZ)],
     "im2win_causal_conv1d_backward": [_CONV] + [_P] * 12 + [_SZ, _P],
     "im2win_causal_conv1d_step": [_CONV] + [_P] * 5 + [_I64, _P, _P],
+    "im2win_add_rms_norm": [_NORM] + [_P] * 6,
+    "im2win_add_rms_norm_fp8": [_NORM] + [_P] * 7,
+    "im2win_add_rms_norm_backward_workspace_bytes": [_NORM, ctypes.POINTER(_SZ)],
+    "im2win_add_rms_norm_backward": [_NORM] + [_P] * 7 + [_SZ, _P],
 }
 
 
@@ -77,6 +92,23 @@ def im2win_causal_conv1d_backward(desc, dy, x, w, bias, seq_starts, initial_stat
 def im2win_causal_conv1d_step(desc, x, w, bias, slots, state, state_slots, y, stream) -> None:
     _check(load_library().im2win_causal_conv1d_step(ctypes.byref(desc), x, w, bias, slots, state, state_slots, y,
                                                     stream))
+
+
+def im2win_add_rms_norm(desc, x, residual, w, y, h, stream) -> None:
+    _check(load_library().im2win_add_rms_norm(ctypes.byref(desc), x, residual, w, y, h, stream))
+
+
+def im2win_add_rms_norm_fp8(desc, x, residual, w, q, scales, h, stream) -> None:
+    _check(load_library().im2win_add_rms_norm_fp8(ctypes.byref(desc), x, residual, w, q, scales, h, stream))
+
+
+def im2win_add_rms_norm_backward_workspace_bytes(desc) -> int:
+    return _bytes("im2win_add_rms_norm_backward_workspace_bytes", desc)
+
+
+def im2win_add_rms_norm_backward(desc, dy, h, w, d_residual, dx, dw, workspace, workspace_bytes, stream) -> None:
+    _check(load_library().im2win_add_rms_norm_backward(ctypes.byref(desc), dy, h, w, d_residual, dx, dw, workspace,
+                                                       workspace_bytes, stream))
 
 
 # ---------------------------------------------------------------------------
@@ -233,3 +265,65 @@ def causal_conv1d_step(x, w, state, desc, bias=None, slots=None, y=None, stream=
     y, yp = _out(y, "y", (desc.tokens, desc.channels), dt, x, dev, stream)
     im2win_causal_conv1d_step(desc, xp, wp, bp, slp, stp, pool, yp, _stream(stream))
     return y
+
+
+def rms_norm_desc_for(tokens, channels, dtype, residual_dtype=None, eps=1e-5, block=0, ld_x=None) -> im2win_norm_desc:
+    """Descriptor of the norm of `tokens` rows: x and y of dtype, the residual
+    and h of residual_dtype (dtype when None); block: channels per scale of
+    the 8-bit output (0: one scale a row); ld_x: row stride of x."""
+    return im2win_norm_desc(tokens, channels, channels if ld_x is None else ld_x, block, _dtype_code(dtype),
+                            _dtype_code(residual_dtype or dtype), eps)
+
+
+def _residual_dtype(desc):
+    return torch.float32 if desc.residual_dtype == IM2WIN_F32 else torch.bfloat16
+
+
+def _norm_inputs(x, w, residual, h, d, stream):
+    """x, w, residual, h and their pointers; h is x itself where there is no
+    residual, and no other type, to add."""
+    dev, shape, rd = _device_of(x, "x"), (d.tokens, d.channels), _residual_dtype(d)
+    xp = _rows(x, "x", shape, _torch_dtype(d), d.ld_x, dev)
+    wp = _dense(w, "w", (d.channels,), torch.float32, dev)
+    rp = _dense(residual, "residual", shape, rd, dev)
+    if h is None and residual is None and d.residual_dtype == d.dtype:
+        return dev, xp, wp, rp, x, None
+    h, hp = _out(h, "h", shape, rd, x, dev, stream)
+    return dev, xp, wp, rp, h, hp
+
+
+def add_rms_norm(x, w, desc, residual=None, y=None, h=None, stream=None):
+    """(y, h): h = x + residual in the residual's type, y = h / rms(h) * w in
+    x's.  h may be the residual itself (the sum in place); without a residual
+    of another type h is x."""
+    dev, xp, wp, rp, h, hp = _norm_inputs(x, w, residual, h, desc, stream)
+    y, yp = _out(y, "y", (desc.tokens, desc.channels), _torch_dtype(desc), x, dev, stream)
+    im2win_add_rms_norm(desc, xp, rp, wp, yp, hp, _stream(stream))
+    return y, h
+
+
+def add_rms_norm_fp8(x, w, desc, residual=None, q=None, scales=None, h=None, stream=None):
+    """(q, scales, h): y = h / rms(h) * w as float8_e4m3fn values q times one
+    fp32 scale for each row or block (T x D/block)."""
+    dev, xp, wp, rp, h, hp = _norm_inputs(x, w, residual, h, desc, stream)
+    t, d = desc.tokens, desc.channels
+    q, qp = _out(q, "q", (t, d), torch.float8_e4m3fn, x, dev, stream)
+    scales, sp = _out(scales, "scales", (t, d // (desc.block or d)), torch.float32, x, dev, stream)
+    im2win_add_rms_norm_fp8(desc, xp, rp, wp, qp, sp, hp, _stream(stream))
+    return q, scales, h
+
+
+def add_rms_norm_backward(dy, h, w, desc, d_residual=None, dx=None, workspace=None, stream=None):
+    """(dx, dw) for dy and the gradient d_residual that h has from elsewhere:
+    dx (the residual's type; may be d_residual itself) is the gradient of both
+    x and the residual, dw is fp32."""
+    dev, shape, rd = _device_of(dy, "dy"), (desc.tokens, desc.channels), _residual_dtype(desc)
+    dyp = _dense(dy, "dy", shape, _torch_dtype(desc), dev)
+    hp = _dense(h, "h", shape, rd, dev)
+    wp = _dense(w, "w", (desc.channels,), torch.float32, dev)
+    drp = _dense(d_residual, "d_residual", shape, rd, dev)
+    dx, dxp = _out(dx, "dx", shape, rd, dy, dev, stream)
+    dw, dwp = _out(None, "dw", (desc.channels,), torch.float32, dy, dev, stream)
+    workspace, wsp, wsb = _workspace(workspace, im2win_add_rms_norm_backward_workspace_bytes(desc), dy, stream)
+    im2win_add_rms_norm_backward(desc, dyp, hp, wp, drp, dxp, dwp, wsp, wsb, _stream(stream))
+    return dx, dw

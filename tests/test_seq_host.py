@@ -80,3 +80,43 @@ def test_conv1d_helpers_refuse():
     assert (d.tokens, d.channels, d.width, d.sequences, d.ld_x, d.dtype, d.silu) == (12, 8, 4, 3, 20, P.IM2WIN_F32, 0)
     with pytest.raises(ValueError):
         P.causal_conv1d(x, w, P.causal_conv1d_desc_for(x, w))      # not a device tensor
+
+
+def norm_desc(**kw):
+    d = dict(tokens=4, channels=256, ld_x=256, block=0, dtype=P.IM2WIN_BF16, residual_dtype=P.IM2WIN_F32, eps=1e-5)
+    d.update(kw)
+    return P.im2win_norm_desc(**d)
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("tokens", -1, "EINVAL"), ("channels", 0, "EINVAL"), ("ld_x", 255, "EINVAL"), ("dtype", 2, "EINVAL"), ("residual_dtype", 2, "EINVAL"),
+    ("eps", -1.0, "EINVAL"), ("eps", float("nan"), "EINVAL"), ("block", 8, "EINVAL"), ("block", 48, "EINVAL"), ("block", 1024, "EINVAL"),
+    ("block", -64, "EINVAL"), ("tokens", 1 << 31, "EOVERFLOW"), ("channels", 16385, "EOVERFLOW"),
+])
+def test_norm_bad_descriptor(field, value, code):
+    d = norm_desc(**{field: value})
+    for call in (lambda: P.im2win_add_rms_norm(d, FAKE, FAKE, FAKE, FAKE, FAKE, 0),
+                 lambda: P.im2win_add_rms_norm_fp8(d, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 0),
+                 lambda: P.im2win_add_rms_norm_backward(d, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 40, 0)):
+        assert _code(call) == getattr(P, "IM2WIN_" + code)
+
+
+def test_norm_null_misaligned_and_short_workspace():
+    d = norm_desc()
+    assert _code(P.im2win_add_rms_norm, norm_desc(block=128), FAKE, FAKE, FAKE, FAKE, FAKE, 0) == P.IM2WIN_EINVAL
+    assert _code(P.im2win_add_rms_norm_fp8, norm_desc(channels=320, ld_x=320, block=128), FAKE, FAKE, FAKE, FAKE, FAKE, FAKE, 0) == P.IM2WIN_EINVAL
+    for i in (0, 2, 3, 4):     # h is needed beside a residual
+        assert _code(P.im2win_add_rms_norm, d, *[0 if j == i else FAKE for j in range(5)], 0) == P.IM2WIN_ENULL
+    for i in (0, 2, 3, 4, 5):
+        assert _code(P.im2win_add_rms_norm_fp8, d, *[0 if j == i else FAKE for j in range(6)], 0) == P.IM2WIN_ENULL
+    for i in range(5):
+        assert _code(P.im2win_add_rms_norm, d, *[FAKE + 1 if j == i else FAKE for j in range(5)], 0) == P.IM2WIN_EALIGN
+    need = P.im2win_add_rms_norm_backward_workspace_bytes(d)
+    assert need == 4 * 256 * 4
+    for i in (0, 1, 2, 4, 5, 6):
+        assert _code(P.im2win_add_rms_norm_backward, d, *[0 if j == i else FAKE for j in range(7)], need, 0) == P.IM2WIN_ENULL
+    assert _code(P.im2win_add_rms_norm_backward, d, *[FAKE] * 7, need - 1, 0) == P.IM2WIN_EWORKSPACE
+    with pytest.raises(ValueError):
+        P.rms_norm_desc_for(4, 8, torch.float16)
+    with pytest.raises(ValueError):
+        P.add_rms_norm(torch.zeros(4, 8), torch.zeros(8), P.rms_norm_desc_for(4, 8, torch.float32))
