@@ -162,6 +162,56 @@ int im2win_add_rms_norm_backward(const im2win_norm_desc* d, const void* dy, cons
                                  const void* d_residual, void* dx, float* dw, void* workspace,
                                  size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------ */
+/* Selective state space scan                                                */
+/* ------------------------------------------------------------------------ */
+
+typedef struct {
+    int64_t tokens;      /* T (requests, for the step) */
+    int64_t channels;    /* D */
+    int64_t states;      /* N, states of a channel, 1 to 128 */
+    int64_t groups;      /* G: channel c reads B and C of group c / (D / G); divides D */
+    int64_t sequences;   /* S >= 1 (not used by the step) */
+    int64_t ld_x, ld_dt, ld_z;   /* row strides of x, dt and z */
+    int64_t ld_b, ld_c;          /* row strides of B and C (rows of G x N) */
+    int32_t dtype;       /* of x, dt, B, C, z, y and their gradients */
+    int32_t softplus;    /* nonzero: the step size is log(1 + exp(dt + dt_bias)) */
+} im2win_scan_desc;
+
+/*
+ * For each channel c and state n, along each sequence,
+ *   s[t][c]    = act(dt[t][c] + dt_bias[c])
+ *   h[t][c][n] = exp(s[t][c] A[c][n]) h[t-1][c][n] + s[t][c] x[t][c] B[t][g(c)][n]
+ *   y[t][c]    = (sum_n C[t][g(c)][n] h[t][c][n] + D[c] x[t][c]) * z[t][c] sigmoid(z[t][c])
+ * where the state before a sequence is its initial state, or zero.
+ *   x, dt     device, T x D;  z  device, T x D, or NULL (no gate)
+ *   A         device, D x N, fp32;  D, dt_bias  device, D, fp32, or NULL
+ *   B, C      device, T x G x N
+ *   initial_state  device, S x D x N, fp32, or NULL (zeros)
+ *   y         device, T x D
+ *   final_state    device, S x D x N, fp32, or NULL
+ *   workspace      device, 16-byte aligned, at least the bytes that
+ *                  im2win_selective_scan_workspace_bytes gives (NULL when 0)
+ * Errors: EINVAL, ENULL, EALIGN, EWORKSPACE, EOVERFLOW, EHIP.
+ */
+int im2win_selective_scan_workspace_bytes(const im2win_scan_desc* d, size_t* bytes);
+int im2win_selective_scan(const im2win_scan_desc* d, const void* x, const void* dt, const float* A,
+                          const void* B, const void* C, const float* D, const void* z,
+                          const float* dt_bias, const int32_t* seq_starts, const float* initial_state,
+                          void* y, float* final_state, void* workspace, size_t workspace_bytes,
+                          void* stream);
+
+/*
+ * One token for each of d->tokens requests: the state of request i is
+ * state[slots[i]] of a pool of state_slots states (D x N each, fp32), moved
+ * on in place; slots as for im2win_causal_conv1d_step.
+ * Errors: EINVAL, ENULL, EALIGN, EOVERFLOW, EHIP.
+ */
+int im2win_selective_scan_step(const im2win_scan_desc* d, const void* x, const void* dt, const float* A,
+                               const void* B, const void* C, const float* D, const void* z,
+                               const float* dt_bias, const int32_t* slots, float* state,
+                               int64_t state_slots, void* y, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,513 @@
+// Selective state space scan (im2win_selective_scan, _step,
+// include/im2win_seq.h).
+//
+// The recurrence h_t = a_t h_{t-1} + b_t runs along the rows, so a long
+// sequence with few channels would leave most of the chip idle.  The rows are
+// cut into chunks, whatever sequences lie in them:
+//   1. scan_kernel<SUMMARY>: for each chunk whose last sequence goes on behind
+//      it, the state at its end from a zero (or initial) state, and the sum S
+//      of the step sizes that a state from before the chunk passes, which is
+//      its decay exp(A S);
+//   2. scan_carry_kernel: the states behind the chunks, one after the other;
+//   3. scan_kernel: each chunk from the state before it, with the outputs.
+// With one chunk, or chunks of whole sequences, only step 3 runs.
+#include <algorithm>
+
+#include "seq_scan.h"
+
+namespace im2win {
+namespace {
+
+// Values of four rows and the lane's channels, one row per lane of the quad
+template <typename T, int CH>
+struct Rows {
+    Raw<T, CH> x, dt, z;
+
+    template <bool GATE>
+    __device__ __forceinline__ void load(const ScanArgs& a, const Lane<CH>& l, int t, int last) {
+        const int64_t row = min(t + l.q, last);
+        x.load(static_cast<const T*>(a.x) + row * a.ld_x, l.c, a.wide);
+        dt.load(static_cast<const T*>(a.dt) + row * a.ld_dt, l.c, a.wide);
+        if constexpr (GATE)
+            if (a.z) z.load(static_cast<const T*>(a.z) + row * a.ld_z, l.c, a.wide);
+    }
+};
+
+template <typename T, int NS, int CH, bool SUMMARY>
+__global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
+    constexpr int NP = kQuad * NS;
+    __shared__ __align__(16) float sb[kScanTile * NP];
+    __shared__ __align__(16) float sc[SUMMARY ? 4 : kScanTile * NP];
+    const int block = blockIdx.x % a.blocks, chunk = blockIdx.x / a.blocks;
+    const int wave = uniform(threadIdx.x / kWave);
+
+    if (chunk >= a.chunks) {
+        // workgroups behind the chunks': the final states of sequences without rows
+        if constexpr (!SUMMARY) {
+            const int64_t each = (int64_t)a.channels * a.states;
+            const int extra = (int)gridDim.x - a.blocks * a.chunks;
+            for (int b = blockIdx.x - a.blocks * a.chunks; b < a.seq.count; b += extra) {
+                if (a.seq.first(b + 1) > a.seq.first(b)) continue;
+                for (int64_t i = threadIdx.x; i < each; i += blockDim.x)
+                    a.final_state[b * each + i] = a.init ? a.init[b * each + i] : 0.0f;
+            }
+        }
+        return;
+    }
+
+    int lo = max(a.seq.first(0), chunk * a.chunk);
+    const int hi = min(a.seq.first(a.seq.count), min(chunk * a.chunk, a.seq.tokens - a.chunk) + a.chunk);
+    if (lo >= hi) {
+        if (SUMMARY && block == 0 && threadIdx.x == 0) a.flags[chunk] = 0;
+        return;
+    }
+    int b = a.seq.find(SUMMARY ? hi - 1 : lo);
+    int first = a.seq.first(b), end = a.seq.first(b + 1);
+    if constexpr (SUMMARY) {
+        if (block == 0 && threadIdx.x == 0)
+            a.flags[chunk] = (end > hi ? kGoesOn : 0) | (first >= lo ? kBegan : 0);
+        if (end <= hi) return;
+        lo = max(lo, first);
+    }
+
+    Lane<CH> l;
+    l.init(a, block, wave);
+    const int group_offset = block / a.group_blocks * a.states;
+    const float* init = a.init;
+    float a2[CH][NS], h[CH][NS], bias[CH], skip[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        bias[i] = a.dt_bias ? a.dt_bias[l.c[i]] : 0.0f;
+        skip[i] = !SUMMARY && a.D ? a.D[l.c[i]] : 0.0f;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int n = l.q * NS + s;
+            a2[i][s] = n < a.states ? kLog2e * a.A[(int64_t)l.c[i] * a.states + n] : 0.0f;
+        }
+    }
+    auto begin = [&]() {     // the state before the first row of sequence b
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const int n = l.q * NS + s;
+                h[i][s] = init && n < a.states ? init[((int64_t)b * a.channels + l.c[i]) * a.states + n] : 0.0f;
+            }
+    };
+    if (lo == first) {
+        begin();
+    } else {
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+                h[i][s] = SUMMARY ? 0.0f : a.carry[((int64_t)(chunk - 1) * a.channels + l.c[i]) * NP + l.q * NS + s];
+    }
+
+    float span[CH] = {};
+    Rows<T, CH> next;
+    next.template load<!SUMMARY>(a, l, lo, hi - 1);
+    for (int tile = lo; tile < hi; tile += kScanTile) {
+        const int rows = min(kScanTile, hi - tile);
+        __syncthreads();
+        stage<T, NS>(sb, static_cast<const T*>(a.B), a.ld_b, group_offset, a.states, tile, rows);
+        if constexpr (!SUMMARY)
+            stage<T, NS>(sc, static_cast<const T*>(a.C), a.ld_c, group_offset, a.states, tile, rows);
+        __syncthreads();
+        for (int r = 0; r < rows; r += kQuad) {
+            const int t = tile + r;
+            const Rows<T, CH> now = next;
+            if (t + kQuad < hi) next.template load<!SUMMARY>(a, l, t + kQuad, hi - 1);
+            float step[CH], in[CH], x[CH], sum[CH] = {};
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                x[i] = now.x.get(i, a.wide);
+                step[i] = now.dt.get(i, a.wide) + bias[i];
+                if (a.softplus) step[i] = softplus(step[i]);
+                in[i] = step[i] * x[i];
+                if (SUMMARY && t + l.q < hi) span[i] += step[i];
+            }
+            auto token = [&](auto j) {
+                constexpr int J = decltype(j)::value;
+                float bm[NS], cm[NS];
+                lds_row<NS>(sb + (r + J) * NP + l.q * NS, bm);
+                if constexpr (!SUMMARY) lds_row<NS>(sc + (r + J) * NP + l.q * NS, cm);
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const float sj = quad_get<J>(step[i]), ij = quad_get<J>(in[i]);
+                    float acc = 0.0f;
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        h[i][s] = fmaf(__builtin_amdgcn_exp2f(sj * a2[i][s]), h[i][s], ij * bm[s]);
+                        if constexpr (!SUMMARY) acc = fmaf(cm[s], h[i][s], acc);
+                    }
+                    if constexpr (!SUMMARY) {
+                        acc = quad_sum(acc);
+                        if (l.q == J) sum[i] = acc;
+                    }
+                }
+            };
+            auto finish = [&]() {     // the state behind the last row of sequence b
+                if (SUMMARY || !a.final_state) return;
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        const int n = l.q * NS + s;
+                        if (l.live[i] && n < a.states)
+                            a.final_state[((int64_t)b * a.channels + l.c[i]) * a.states + n] = h[i][s];
+                    }
+            };
+            auto advance = [&](int row) {
+                b = a.seq.find(row);
+                end = a.seq.first(b + 1);
+                begin();
+            };
+            using std::integral_constant;
+            if (SUMMARY ? t + kQuad <= hi : t < end && t + kQuad <= min(end, hi)) {
+                token(integral_constant<int, 0>{});
+                token(integral_constant<int, 1>{});
+                token(integral_constant<int, 2>{});
+                token(integral_constant<int, 3>{});
+                if (t + kQuad == end) finish();
+            } else {
+                auto one = [&](auto j) {
+                    const int row = t + decltype(j)::value;
+                    if (row >= hi) return;
+                    if (!SUMMARY && row >= end) advance(row);
+                    token(j);
+                    if (row + 1 == end) finish();
+                };
+                one(integral_constant<int, 0>{});
+                one(integral_constant<int, 1>{});
+                one(integral_constant<int, 2>{});
+                one(integral_constant<int, 3>{});
+            }
+            if constexpr (!SUMMARY) {
+                if (t + l.q < hi) {
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) {
+                        sum[i] = fmaf(skip[i], x[i], sum[i]);
+                        if (a.z) {
+                            const float z = now.z.get(i, a.wide);
+                            sum[i] *= z * sigmoid(z);
+                        }
+                    }
+                    store_channels<CH>(static_cast<T*>(a.y) + (int64_t)(t + l.q) * a.channels, l.c0, l.live, sum, a.wide);
+                }
+            }
+        }
+    }
+    if constexpr (SUMMARY) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            span[i] = quad_sum(span[i]);
+            if (!l.live[i]) continue;
+            const int64_t at = (int64_t)chunk * a.channels + l.c[i];
+            if (l.q == 0) a.span[at] = span[i];
+#pragma unroll
+            for (int s = 0; s < NS; ++s) a.carry[at * NP + l.q * NS + s] = h[i][s];
+        }
+    }
+}
+
+// The states behind the chunks from the chunks' own: one thread per channel
+// and state walks the chunks.  The loads of eight chunks do not wait for one
+// another.
+__global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a, int padded) {
+    const int64_t each = (int64_t)a.channels * padded;
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= each) return;
+    const int c = (int)(e / padded), n = (int)(e % padded);
+    const float a2 = n < a.states ? kLog2e * a.A[(int64_t)c * a.states + n] : 0.0f;
+    constexpr int U = 8;
+    float h = 0.0f;
+    for (int k = 0; k < a.chunks - 1; k += U) {
+        const int m = min(U, a.chunks - 1 - k);
+        float own[U], decay[U];
+        int f[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = k + min(u, m - 1);
+            f[u] = a.flags[at];
+            own[u] = f[u] & kGoesOn ? a.carry[at * each + e] : 0.0f;
+            decay[u] = f[u] == kGoesOn ? __builtin_amdgcn_exp2f(a2 * a.span[at * a.channels + c]) : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (u >= m || !(f[u] & kGoesOn)) continue;
+            h = f[u] & kBegan ? own[u] : fmaf(decay[u], h, own[u]);
+            a.carry[(k + u) * each + e] = h;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// One token of each request: a quad per channel, a quarter of its states each
+// ---------------------------------------------------------------------------
+struct ScanStepArgs {
+    ScanArgs a;
+    const int32_t* slots;
+    float* state;
+    int64_t state_slots;
+    int whole;          // states are NS whole floats for every lane, on their boundaries
+};
+
+template <typename T, int NS>
+__global__ __launch_bounds__(kScanWaves * kWave) void scan_step_kernel(ScanStepArgs p) {
+    const ScanArgs& a = p.a;
+    const int64_t row = blockIdx.x;
+    const int q = threadIdx.x % kQuad;
+    const int c_own = ((int)blockIdx.y * kScanWaves * kWave + (int)threadIdx.x) / kQuad;
+    const bool live = c_own < a.channels;
+    const int c = live ? c_own : 0;
+    T* y = static_cast<T*>(a.y) + row * a.channels + c;
+    const int64_t slot = p.slots ? (int64_t)p.slots[row] : row;
+    if (slot < 0 || slot >= p.state_slots) {
+        if (live && q == 0) *y = (T)0.0f;
+        return;
+    }
+    float* state = p.state + (slot * a.channels + c) * a.states + q * NS;
+    const float* arow = a.A + (int64_t)c * a.states + q * NS;
+    const int g = c / a.group_channels * a.states + q * NS;
+    const T* bm = static_cast<const T*>(a.B) + row * a.ld_b + g;
+    const T* cm = static_cast<const T*>(a.C) + row * a.ld_c + g;
+    float h[NS], a2[NS];
+    if (p.whole) {
+        lds_row<NS>(state, h);
+        lds_row<NS>(arow, a2);
+    } else {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const bool in = q * NS + s < a.states;
+            h[s] = in ? state[s] : 0.0f;
+            a2[s] = in ? arow[s] : 0.0f;
+        }
+    }
+    const float x = (float)(static_cast<const T*>(a.x) + row * a.ld_x)[c];
+    float step = (float)(static_cast<const T*>(a.dt) + row * a.ld_dt)[c] + (a.dt_bias ? a.dt_bias[c] : 0.0f);
+    if (a.softplus) step = softplus(step);
+    const float in = step * x;
+    float sum = 0.0f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+        const bool exists = p.whole || q * NS + s < a.states;
+        const float bv = exists ? (float)bm[s] : 0.0f, cv = exists ? (float)cm[s] : 0.0f;
+        h[s] = fmaf(__builtin_amdgcn_exp2f(step * (kLog2e * a2[s])), h[s], in * bv);
+        sum = fmaf(cv, h[s], sum);
+    }
+    sum = quad_sum(sum);
+    if (!live) return;
+    if (p.whole) {
+        if constexpr (NS % 4 == 0) {
+            store_f32<NS>(state, h);
+        } else {
+#pragma unroll
+            for (int s = 0; s < NS; s += 2) *reinterpret_cast<float2*>(state + s) = make_float2(h[s], h[s + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+            if (q * NS + s < a.states) state[s] = h[s];
+    }
+    if (q == 0) {
+        if (a.D) sum = fmaf(a.D[c], x, sum);
+        if (a.z) {
+            const float z = (float)(static_cast<const T*>(a.z) + row * a.ld_z)[c];
+            sum *= z * sigmoid(z);
+        }
+        *y = (T)sum;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+struct ScanPlan {
+    int64_t chunk = 0, chunks = 0, blocks = 0;
+    int ns = 0, ch = 0;
+    size_t carry_bytes = 0, span_bytes = 0, bytes = 0;
+};
+
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+
+// The chunk: as long as leaves about three waves for each of the chip's 1024
+// SIMDs, but no shorter than two tiles; equal sequences are cut into equal
+// parts, or taken whole where they are shorter.
+ScanPlan plan_scan(const im2win_scan_desc* d) {
+    ScanPlan p;
+    with_states(d->states, [&](auto ns, auto ch) {
+        p.ns = decltype(ns)::value;
+        p.ch = decltype(ch)::value;
+    });
+    const int64_t per_block = kScanWaves * (kWave / kQuad) * p.ch;
+    const int64_t group = d->channels / d->groups;
+    p.blocks = d->groups * ((group + per_block - 1) / per_block);
+    if (d->tokens == 0) return p;
+    const int64_t want = (3072 + p.blocks * kScanWaves - 1) / (p.blocks * kScanWaves);
+    p.chunk = std::max<int64_t>((d->tokens + want - 1) / want, 2 * kScanTile);
+    const int64_t len = d->tokens / d->sequences;
+    if (d->tokens % d->sequences == 0 && d->sequences > 1) {
+        if (len <= p.chunk) {
+            p.chunk = p.chunk / len * len;
+        } else {
+            for (int64_t m = (len + p.chunk - 1) / p.chunk; m <= 2 * (len / p.chunk) + 1; ++m)
+                if (len % m == 0) {
+                    p.chunk = len / m;
+                    break;
+                }
+        }
+    }
+    p.chunk = std::min(p.chunk, d->tokens);
+    p.chunks = (d->tokens + p.chunk - 1) / p.chunk;
+    if (p.chunks > 1) {
+        p.carry_bytes = round16((size_t)(p.chunks * d->channels * kQuad * p.ns) * 4);
+        p.span_bytes = round16((size_t)(p.chunks * d->channels) * 4);
+        p.bytes = p.carry_bytes + p.span_bytes + round16((size_t)p.chunks * 4);
+    }
+    return p;
+}
+
+constexpr int kEmptyBlocks = 32;     // workgroups that look for sequences without rows
+
+template <typename F>
+void with_type(int32_t dtype, F f) {
+    if (dtype == IM2WIN_F32) f(float{});
+    else f(bf16{});
+}
+
+}  // namespace
+
+int check_scan(const im2win_scan_desc* d, bool sequences, const int32_t* starts, bool have_starts) {
+    if (!d) return fail(IM2WIN_ENULL, "descriptor is NULL");
+    int rc = check_rows(d->tokens, d->channels, d->dtype);
+    if (rc) return rc;
+    if (d->states < 1 || d->states > 128) return fail(IM2WIN_EINVAL, "states must be 1 to 128 (got %lld)", (long long)d->states);
+    if (d->groups < 1 || d->channels % d->groups)
+        return fail(IM2WIN_EINVAL, "groups (%lld) must divide the %lld channels", (long long)d->groups, (long long)d->channels);
+    if ((rc = check_ld(d->ld_x, d->channels, "ld_x")) || (rc = check_ld(d->ld_dt, d->channels, "ld_dt")) ||
+        (rc = check_ld(d->ld_z, d->channels, "ld_z")) || (rc = check_ld(d->ld_b, d->groups * d->states, "ld_b")) ||
+        (rc = check_ld(d->ld_c, d->groups * d->states, "ld_c")))
+        return rc;
+    return sequences ? check_sequences(d->tokens, d->sequences, starts, have_starts) : IM2WIN_OK;
+}
+
+int check_scan_inputs(const im2win_scan_desc* d, const void* x, const void* dt, const float* A, const void* B,
+                      const void* C, const float* D, const void* z, const float* dt_bias) {
+    const size_t e = d->dtype == IM2WIN_F32 ? 4 : 2;
+    int rc;
+    if ((rc = need_ptr(A, 4, "A")) || (rc = may_ptr(D, 4, "D")) || (rc = may_ptr(dt_bias, 4, "dt_bias"))) return rc;
+    if (d->tokens == 0) return IM2WIN_OK;
+    if ((rc = need_ptr(x, e, "x")) || (rc = need_ptr(dt, e, "dt")) || (rc = need_ptr(B, e, "B")) ||
+        (rc = need_ptr(C, e, "C")) || (rc = may_ptr(z, e, "z")))
+        return rc;
+    return IM2WIN_OK;
+}
+
+ScanArgs scan_args(const im2win_scan_desc* d, const void* x, const void* dt, const float* A, const void* B,
+                   const void* C, const float* D, const void* z, const float* dt_bias, int ch) {
+    ScanArgs a{};
+    a.x = x; a.dt = dt; a.A = A; a.B = B; a.C = C; a.D = D; a.z = z; a.dt_bias = dt_bias;
+    a.ld_x = d->ld_x; a.ld_dt = d->ld_dt; a.ld_z = d->ld_z; a.ld_b = d->ld_b; a.ld_c = d->ld_c;
+    a.channels = (int)d->channels; a.states = (int)d->states;
+    a.group_channels = (int)(d->channels / d->groups);
+    const int per_block = kScanWaves * (kWave / kQuad) * ch;
+    a.group_blocks = (a.group_channels + per_block - 1) / per_block;
+    a.blocks = (int)d->groups * a.group_blocks;
+    a.softplus = d->softplus != 0;
+    const size_t pair = d->dtype == IM2WIN_F32 ? 8 : 4;
+    a.wide = a.group_channels % 2 == 0 && d->ld_x % 2 == 0 && d->ld_dt % 2 == 0 && (!z || d->ld_z % 2 == 0) &&
+             aligned_to(x, pair) && aligned_to(dt, pair) && aligned_to(z, pair);
+    return a;
+}
+
+}  // namespace im2win
+
+using namespace im2win;
+
+extern "C" {
+
+int im2win_selective_scan_workspace_bytes(const im2win_scan_desc* d, size_t* bytes) {
+    int rc = check_scan(d, true, nullptr, false);
+    if (rc) return rc;
+    if (!bytes) return fail(IM2WIN_ENULL, "bytes is NULL");
+    *bytes = plan_scan(d).bytes;
+    return ok();
+}
+
+int im2win_selective_scan(const im2win_scan_desc* d, const void* x, const void* dt, const float* A, const void* B,
+                          const void* C, const float* D, const void* z, const float* dt_bias,
+                          const int32_t* seq_starts, const float* initial_state, void* y, float* final_state,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_scan(d, true, seq_starts, true);
+    if (rc || (rc = check_scan_inputs(d, x, dt, A, B, C, D, z, dt_bias))) return rc;
+    if ((d->tokens && (rc = need_ptr(y, d->dtype == IM2WIN_F32 ? 4 : 2, "y"))) ||
+        (rc = may_ptr(initial_state, 4, "initial_state")) || (rc = may_ptr(final_state, 4, "final_state")))
+        return rc;
+    const ScanPlan p = plan_scan(d);
+    if (p.bytes && (rc = need_ptr(workspace, 16, "workspace"))) return rc;
+    if (workspace_bytes < p.bytes)
+        return fail(IM2WIN_EWORKSPACE, "workspace holds %zu bytes, the scan needs %zu", workspace_bytes, p.bytes);
+    ScanArgs a = scan_args(d, x, dt, A, B, C, D, z, dt_bias, p.ch);
+    a.init = initial_state; a.y = y; a.final_state = final_state;
+    a.seq = make_seq_map(d->tokens, d->sequences, seq_starts);
+    a.chunk = (int)p.chunk; a.chunks = (int)p.chunks;
+    a.wide = a.wide && aligned_to(y, d->dtype == IM2WIN_F32 ? 8 : 4);
+    char* ws = static_cast<char*>(workspace);
+    if (p.bytes) {
+        a.carry = reinterpret_cast<float*>(ws);
+        a.span = reinterpret_cast<float*>(ws + p.carry_bytes);
+        a.flags = reinterpret_cast<int*>(ws + p.carry_bytes + p.span_bytes);
+    }
+    const int64_t grid = p.blocks * p.chunks;
+    const int64_t extra = final_state && (seq_starts || d->tokens == 0) ? std::min<int64_t>(d->sequences, kEmptyBlocks) : 0;
+    if (grid + extra == 0) return ok();
+    if (grid + extra > (int64_t(1) << 31) - 1) return fail(IM2WIN_EOVERFLOW, "too many channels and tokens");
+    // chunks that no sequence crosses need no states from before them
+    const bool whole = !seq_starts && p.chunks && p.chunk % (d->tokens / d->sequences) == 0;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    with_type(d->dtype, [&](auto t) {
+        with_states(d->states, [&](auto ns, auto ch) {
+            using T = decltype(t);
+            constexpr int NS = decltype(ns)::value, CH = decltype(ch)::value;
+            const dim3 threads(kScanWaves * kWave);
+            if (p.chunks > 1 && !whole) {
+                hipLaunchKernelGGL((scan_kernel<T, NS, CH, true>), dim3((unsigned)(p.blocks * (p.chunks - 1))), threads, 0, s, a);
+                const int64_t each = (int64_t)a.channels * kQuad * NS;
+                hipLaunchKernelGGL(scan_carry_kernel, dim3((unsigned)((each + 255) / 256)), dim3(256), 0, s, a, kQuad * NS);
+            }
+            hipLaunchKernelGGL((scan_kernel<T, NS, CH, false>), dim3((unsigned)(grid + extra)), threads, 0, s, a);
+        });
+    });
+    return launched("selective_scan");
+}
+
+int im2win_selective_scan_step(const im2win_scan_desc* d, const void* x, const void* dt, const float* A, const void* B,
+                               const void* C, const float* D, const void* z, const float* dt_bias,
+                               const int32_t* slots, float* state, int64_t state_slots, void* y, void* stream) {
+    int rc = check_scan(d, false, nullptr, false);
+    if (rc) return rc;
+    if (state_slots < 0) return fail(IM2WIN_EINVAL, "state_slots is negative (%lld)", (long long)state_slots);
+    if ((rc = check_scan_inputs(d, x, dt, A, B, C, D, z, dt_bias))) return rc;
+    if (d->tokens == 0) return ok();
+    if ((rc = may_ptr(slots, 4, "slots")) || (rc = need_ptr(y, d->dtype == IM2WIN_F32 ? 4 : 2, "y")) ||
+        (state_slots && (rc = need_ptr(state, 4, "state"))))
+        return rc;
+    ScanStepArgs p{};
+    p.a = scan_args(d, x, dt, A, B, C, D, z, dt_bias, 1);
+    p.a.y = y;
+    p.slots = slots; p.state = state; p.state_slots = state_slots;
+    const unsigned cover = (unsigned)((d->channels * kQuad + kScanWaves * kWave - 1) / (kScanWaves * kWave));
+    with_type(d->dtype, [&](auto t) {
+        with_states(d->states, [&](auto ns, auto) {
+            using T = decltype(t);
+            constexpr int NS = decltype(ns)::value;
+            p.whole = d->states == kQuad * NS && aligned_to(A, 16) && aligned_to(state, 16);
+            hipLaunchKernelGGL((scan_step_kernel<T, NS>), dim3((unsigned)d->tokens, cover), dim3(kScanWaves * kWave), 0,
+                               static_cast<hipStream_t>(stream), p);
+        });
+    });
+    return launched("selective_scan_step");
+}
+
+}  // extern "C"

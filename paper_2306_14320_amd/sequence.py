@@ -1,7 +1,7 @@
 """Binding of the sequence operators of ``libim2win.so``
 (``include/im2win_seq.h``): the short causal convolution, its gradients and
-its form for single tokens, and the root-mean-square norm with the residual's
-addition.
+its form for single tokens, the root-mean-square norm with the residual's
+addition, and the selective state space scan with its form for single tokens.
 
 The ``im2win_*`` functions mirror the C entry points and take device pointers;
 the tensor helpers below them check every tensor against the descriptor and
@@ -26,6 +26,8 @@ __all__ = [
     "im2win_norm_desc", "im2win_add_rms_norm", "im2win_add_rms_norm_fp8",
     "im2win_add_rms_norm_backward_workspace_bytes", "im2win_add_rms_norm_backward",
     "rms_norm_desc_for", "add_rms_norm", "add_rms_norm_fp8", "add_rms_norm_backward",
+    "im2win_scan_desc", "im2win_selective_scan_workspace_bytes", "im2win_selective_scan", "im2win_selective_scan_step",
+    "selective_scan_desc_for", "selective_scan", "selective_scan_step",
 ]
 
 _P, _SZ, _I64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64
@@ -48,7 +50,15 @@ class im2win_norm_desc(_Desc):
                 ("dtype", ctypes.c_int32), ("residual_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
+class im2win_scan_desc(_Desc):
+    """Mirror of the C ``im2win_scan_desc``."""
+    _fields_ = [("tokens", _I64), ("channels", _I64), ("states", _I64), ("groups", _I64), ("sequences", _I64),
+                ("ld_x", _I64), ("ld_dt", _I64), ("ld_z", _I64), ("ld_b", _I64), ("ld_c", _I64),
+                ("dtype", ctypes.c_int32), ("softplus", ctypes.c_int32)]
+
+
 _CONV = ctypes.POINTER(im2win_conv1d_desc)
+_SCAN = ctypes.POINTER(im2win_scan_desc)
 _NORM = ctypes.POINTER(im2win_norm_desc)
 
 SIGNATURES = {
@@ -56,6 +66,9 @@ SIGNATURES = {
     "im2win_causal_conv1d_backward_workspace_bytes": [_CONV, ctypes.POINTER(_SZ)],
     "im2win_causal_conv1d_backward": [_CONV] + [_P] * 12 + [_SZ, _P],
     "im2win_causal_conv1d_step": [_CONV] + [_P] * 5 + [_I64, _P, _P],
+    "im2win_selective_scan_workspace_bytes": [_SCAN, ctypes.POINTER(_SZ)],
+    "im2win_selective_scan": [_SCAN] + [_P] * 13 + [_SZ, _P],
+    "im2win_selective_scan_step": [_SCAN] + [_P] * 10 + [_I64, _P, _P],
     "im2win_add_rms_norm": [_NORM] + [_P] * 6,
     "im2win_add_rms_norm_fp8": [_NORM] + [_P] * 7,
     "im2win_add_rms_norm_backward_workspace_bytes": [_NORM, ctypes.POINTER(_SZ)],
@@ -109,6 +122,21 @@ def im2win_add_rms_norm_backward_workspace_bytes(desc) -> int:
 def im2win_add_rms_norm_backward(desc, dy, h, w, d_residual, dx, dw, workspace, workspace_bytes, stream) -> None:
     _check(load_library().im2win_add_rms_norm_backward(ctypes.byref(desc), dy, h, w, d_residual, dx, dw, workspace,
                                                        workspace_bytes, stream))
+
+
+def im2win_selective_scan_workspace_bytes(desc) -> int:
+    return _bytes("im2win_selective_scan_workspace_bytes", desc)
+
+
+def im2win_selective_scan(desc, x, dt, A, B, C, D, z, dt_bias, seq_starts, initial_state, y, final_state, workspace,
+                          workspace_bytes, stream) -> None:
+    _check(load_library().im2win_selective_scan(ctypes.byref(desc), x, dt, A, B, C, D, z, dt_bias, seq_starts,
+                                                initial_state, y, final_state, workspace, workspace_bytes, stream))
+
+
+def im2win_selective_scan_step(desc, x, dt, A, B, C, D, z, dt_bias, slots, state, state_slots, y, stream) -> None:
+    _check(load_library().im2win_selective_scan_step(ctypes.byref(desc), x, dt, A, B, C, D, z, dt_bias, slots, state,
+                                                     state_slots, y, stream))
 
 
 # ---------------------------------------------------------------------------
@@ -327,3 +355,64 @@ def add_rms_norm_backward(dy, h, w, desc, d_residual=None, dx=None, workspace=No
     workspace, wsp, wsb = _workspace(workspace, im2win_add_rms_norm_backward_workspace_bytes(desc), dy, stream)
     im2win_add_rms_norm_backward(desc, dyp, hp, wp, drp, dxp, dwp, wsp, wsb, _stream(stream))
     return dx, dw
+
+
+def selective_scan_desc_for(x, dt, A, B, C, z=None, sequences=1, softplus=True) -> im2win_scan_desc:
+    """Descriptor of the selective scan of x and dt (T x D), A (D x N), B and
+    C (T x G x N) and the gate z (T x D or None); rows may have any stride."""
+    if x.dim() != 2 or A.dim() != 2 or B.dim() != 3 or A.shape[0] != x.shape[1] or B.shape[2] != A.shape[1]:
+        raise ValueError("x must be T x D, A D x N and B T x G x N (got %s, %s and %s)"
+                         % (tuple(x.shape), tuple(A.shape), tuple(B.shape)))
+    t, d = x.shape
+    return im2win_scan_desc(t, d, A.shape[1], B.shape[1], sequences, _row_stride(x, "x"), _row_stride(dt, "dt"),
+                            d if z is None else _row_stride(z, "z"), _row_stride(B, "B"), _row_stride(C, "C"),
+                            _dtype_code(x.dtype), int(bool(softplus)))
+
+
+def _scan_inputs(x, dt, A, B, C, D, z, dt_bias, d):
+    """The device, the element type and the pointers of the scan's inputs."""
+    dev, ty = _device_of(x, "x"), _torch_dtype(d)
+    rows, proj = (d.tokens, d.channels), (d.tokens, d.groups, d.states)
+    return dev, ty, (
+        _rows(x, "x", rows, ty, d.ld_x, dev),
+        _rows(dt, "dt", rows, ty, d.ld_dt, dev),
+        _dense(A, "A", (d.channels, d.states), torch.float32, dev),
+        _rows(B, "B", proj, ty, d.ld_b, dev),
+        _rows(C, "C", proj, ty, d.ld_c, dev),
+        _dense(D, "D", (d.channels,), torch.float32, dev),
+        None if z is None else _rows(z, "z", rows, ty, d.ld_z, dev),
+        _dense(dt_bias, "dt_bias", (d.channels,), torch.float32, dev))
+
+
+def selective_scan(x, dt, A, B, C, desc, D=None, z=None, dt_bias=None, seq_starts=None, initial_state=None, y=None,
+                   final_state=None, workspace=None, stream=None):
+    """y of the scan h_t = exp(s_t A) h_{t-1} + s_t x_t B_t, s = softplus(dt +
+    dt_bias), y = (C h + D x) silu(z), T x D in x's dtype.  The state before a
+    sequence is initial_state's (sequences x D x N, fp32) or zero; final_state,
+    if given, receives the state behind each sequence."""
+    d = desc
+    dev, ty, (xp, dtp, ap, bp, cp, dp, zp, tbp) = _scan_inputs(x, dt, A, B, C, D, z, dt_bias, d)
+    state = (d.sequences, d.channels, d.states)
+    sp = _dense(seq_starts, "seq_starts", (d.sequences + 1,), torch.int32, dev)
+    ip = _dense(initial_state, "initial_state", state, torch.float32, dev)
+    fp = _dense(final_state, "final_state", state, torch.float32, dev)
+    y, yp = _out(y, "y", (d.tokens, d.channels), ty, x, dev, stream)
+    workspace, wsp, wsb = _workspace(workspace, im2win_selective_scan_workspace_bytes(d), x, stream)
+    im2win_selective_scan(d, xp, dtp, ap, bp, cp, dp, zp, tbp, sp, ip, yp, fp, wsp, wsb, _stream(stream))
+    return y
+
+
+def selective_scan_step(x, dt, A, B, C, state, desc, D=None, z=None, dt_bias=None, slots=None, y=None, stream=None):
+    """One token of each request: inputs have a row for each, state is a pool
+    of slots x D x N (fp32) that moves on in place, slots (int32) the
+    request's place in it (its own index when None; outside of the pool: y =
+    0, nothing moves)."""
+    dev, ty, (xp, dtp, ap, bp, cp, dp, zp, tbp) = _scan_inputs(x, dt, A, B, C, D, z, dt_bias, desc)
+    if not isinstance(state, torch.Tensor):
+        raise ValueError("state must be a tensor")
+    pool = state.shape[0]
+    stp = _dense(state, "state", (pool, desc.channels, desc.states), torch.float32, dev)
+    slp = _dense(slots, "slots", (desc.tokens,), torch.int32, dev)
+    y, yp = _out(y, "y", (desc.tokens, desc.channels), ty, x, dev, stream)
+    im2win_selective_scan_step(desc, xp, dtp, ap, bp, cp, dp, zp, tbp, slp, stp, pool, yp, _stream(stream))
+    return y

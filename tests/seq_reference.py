@@ -42,3 +42,25 @@ def gradients(fn, inputs, weights):
     total = sum((o * w).sum() for o, w in zip(outs, weights) if w is not None)
     got = iter(torch.autograd.grad(total, [v for v in leaves if v is not None], allow_unused=True))
     return [None if v is None else next(got) for v in leaves]
+
+
+def scan(x, dt, A, B, C, D, z, dt_bias, starts, init=None, softplus=True):
+    """y and the final states of the selective scan.  B and C are T x G x N."""
+    t, d = x.shape
+    per = d // B.shape[1]
+    s = dt if dt_bias is None else dt + dt_bias
+    s = torch.logaddexp(s, torch.zeros_like(s)) if softplus else s
+    rows, finals = [None] * t, []
+    for b, (lo, hi) in enumerate(zip(starts, starts[1:])):
+        h = init[b] if init is not None else x.new_zeros(d, A.shape[1])
+        for i in range(lo, hi):
+            bm, cm = B[i].repeat_interleave(per, 0), C[i].repeat_interleave(per, 0)
+            h = torch.exp(s[i][:, None] * A) * h + (s[i] * x[i])[:, None] * bm
+            rows[i] = (h * cm).sum(1)
+        finals.append(h)
+    y = torch.stack([r if r is not None else x.new_zeros(d) for r in rows]) if t else x
+    if D is not None:
+        y = y + D * x
+    if z is not None:
+        y = y * z * torch.sigmoid(z)
+    return y, torch.stack(finals)

@@ -120,3 +120,59 @@ def test_norm_null_misaligned_and_short_workspace():
         P.rms_norm_desc_for(4, 8, torch.float16)
     with pytest.raises(ValueError):
         P.add_rms_norm(torch.zeros(4, 8), torch.zeros(8), P.rms_norm_desc_for(4, 8, torch.float32))
+
+
+def scan_desc(**kw):
+    d = dict(tokens=12, channels=8, states=16, groups=2, sequences=3, ld_x=8, ld_dt=8, ld_z=8, ld_b=32, ld_c=32, dtype=P.IM2WIN_F32, softplus=1)
+    d.update(kw)
+    return P.im2win_scan_desc(**d)
+
+
+def scan_calls(d):
+    ok = 1 << 50
+    return [lambda: P.im2win_selective_scan(d, *[FAKE] * 8, 0, FAKE, FAKE, FAKE, FAKE, ok, 0),
+            lambda: P.im2win_selective_scan_step(d, *[FAKE] * 8, 0, FAKE, 4, FAKE, 0)]
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("tokens", -1, "EINVAL"), ("channels", 0, "EINVAL"), ("states", 0, "EINVAL"), ("states", 129, "EINVAL"), ("groups", 0, "EINVAL"),
+    ("groups", 3, "EINVAL"), ("ld_x", 7, "EINVAL"), ("ld_dt", 7, "EINVAL"), ("ld_z", 0, "EINVAL"), ("ld_b", 31, "EINVAL"), ("ld_c", 16, "EINVAL"),
+    ("dtype", 3, "EINVAL"), ("tokens", 1 << 31, "EOVERFLOW"), ("channels", 1 << 21, "EOVERFLOW"), ("ld_b", 1 << 31, "EOVERFLOW"),
+])
+def test_scan_bad_descriptor(field, value, code):
+    d = scan_desc(**{field: value})
+    for call in scan_calls(d):
+        assert _code(call) == getattr(P, "IM2WIN_" + code)
+    assert _code(P.im2win_selective_scan_workspace_bytes, d) == getattr(P, "IM2WIN_" + code)
+
+
+def test_scan_null_misaligned_and_short_workspace():
+    d = scan_desc(tokens=600, channels=16)
+    d.ld_x = d.ld_dt = d.ld_z = 16
+    need = P.im2win_selective_scan_workspace_bytes(d)
+    assert need > 0
+    good = [FAKE] * 8 + [0, FAKE, FAKE, FAKE, FAKE]
+    for i in (0, 1, 2, 3, 4, 10, 12):
+        assert _code(P.im2win_selective_scan, d, *[0 if j == i else v for j, v in enumerate(good)], need, 0) == P.IM2WIN_ENULL
+    for i in (0, 1, 2, 3, 4, 5, 6, 7, 9, 10, 11, 12):
+        assert _code(P.im2win_selective_scan, d, *[v + 2 if j == i else v for j, v in enumerate(good)], need, 0) == P.IM2WIN_EALIGN
+    assert _code(P.im2win_selective_scan, d, *good, need - 1, 0) == P.IM2WIN_EWORKSPACE
+    for bad in (0, -2, 7):
+        d.sequences = bad
+        assert _code(P.im2win_selective_scan, d, *good, need, 0) == P.IM2WIN_EINVAL
+    step = [FAKE] * 8 + [0, FAKE, 4, FAKE]
+    for i in (0, 1, 2, 3, 4, 9, 11):
+        assert _code(P.im2win_selective_scan_step, d, *[0 if j == i else v for j, v in enumerate(step)], 0) == P.IM2WIN_ENULL
+    assert _code(P.im2win_selective_scan_step, d, *step[:10], -1, FAKE, 0) == P.IM2WIN_EINVAL
+    with pytest.raises(ValueError):
+        P.selective_scan_desc_for(torch.zeros(4, 8), torch.zeros(4, 8), torch.zeros(8, 3), torch.zeros(4, 1, 4), torch.zeros(4, 1, 4))
+
+
+def test_scan_workspace_covers_every_plan():
+    """No workspace where one chunk holds all rows; otherwise a state for each
+    chunk, channel and padded state, at chunks of 32 rows or more."""
+    for tokens, seqs, channels, n, groups in [(64, 1, 2048, 16, 1), (1, 1, 1, 1, 1), (8192, 1, 2048, 16, 1), (16384, 8, 2048, 16, 1), (3001, 17, 777, 24, 3), (100000, 7, 33, 128, 1)]:
+        d = scan_desc(tokens=tokens, channels=channels, states=n, groups=groups, sequences=seqs, ld_x=channels, ld_dt=channels, ld_z=channels, ld_b=groups * n, ld_c=groups * n)
+        need = P.im2win_selective_scan_workspace_bytes(d)
+        assert (need == 0) == (tokens <= 64)
+        assert need <= (tokens / 32 + 1) * channels * (4 * 132) + tokens + 4096
