@@ -212,6 +212,29 @@ int im2win_selective_scan_step(const im2win_scan_desc* d, const void* x, const v
                                const float* dt_bias, const int32_t* slots, float* state,
                                int64_t state_slots, void* y, void* stream);
 
+/* Bytes of workspace that im2win_selective_scan_backward takes.  Host only. */
+int im2win_selective_scan_backward_workspace_bytes(const im2win_scan_desc* d, size_t* bytes);
+
+/*
+ * Gradients of im2win_selective_scan for the gradient dy of y (T x D, dense)
+ * and, where d_final_state (S x D x N, fp32) is given, of the final states.
+ * The states are computed again; nothing of the forward call is needed.
+ *   dx, ddt, dz   device, T x D (dz only where z is given, and then needed)
+ *   dB, dC        device, T x G x N
+ *   dA            device, D x N, fp32
+ *   dD, ddt_bias  device, D, fp32, or NULL
+ *   d_initial_state  device, S x D x N, fp32, or NULL
+ *   workspace     device, 16-byte aligned, at least the bytes above
+ * Errors: EINVAL, ENULL, EALIGN, EWORKSPACE, EOVERFLOW, EHIP.
+ */
+int im2win_selective_scan_backward(const im2win_scan_desc* d, const void* dy, const void* x, const void* dt,
+                                   const float* A, const void* B, const void* C, const float* D,
+                                   const void* z, const float* dt_bias, const int32_t* seq_starts,
+                                   const float* initial_state, const float* d_final_state, void* dx,
+                                   void* ddt, float* dA, void* dB, void* dC, float* dD, void* dz,
+                                   float* ddt_bias, float* d_initial_state, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

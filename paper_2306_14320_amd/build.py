@@ -13,7 +13,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libim2win.so")
 SOURCES = ["api.hip", "transform.hip", "conv_f32.hip", "conv_bf16.hip", "conv_bf16_image.hip", "conv_f32_band.hip", "conv_plain.hip", "check.hip", "direct.hip",
-           "seq_conv1d.hip", "seq_norm.hip", "seq_scan.hip"]
+           "seq_conv1d.hip", "seq_norm.hip", "seq_scan.hip", "seq_scan_bwd.hip"]
 ARCH = "gfx950"
 
 

@@ -101,7 +101,7 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int s = 0; s < NS; ++s)
-                h[i][s] = SUMMARY ? 0.0f : a.carry[((int64_t)(chunk - 1) * a.channels + l.c[i]) * NP + l.q * NS + s];
+                h[i][s] = SUMMARY || chunk == 0 ? 0.0f : a.carry[((int64_t)(chunk - 1) * a.channels + l.c[i]) * NP + l.q * NS + s];
     }
 
     float span[CH] = {};

@@ -1,0 +1,836 @@
+// Gradients of the selective scan (im2win_selective_scan_backward,
+// include/im2win_seq.h).
+//
+// With s the step size, a = exp(s A), u = s x and p = dy silu(z) the gradient
+// of the sum in front of the gate, the gradient g_t of the state h_t obeys
+//   g_t = C_t p_t + a_{t+1} g_{t+1}          (along a sequence, from its end),
+// and   dC_t = sum_c p h,        dB_t = sum_c g u   (over the group's channels),
+//       q_t  = g a h_{t-1},      dA = sum_t q s,
+//       du   = sum_n g B,        dx = du s + D p,   ds = du x + sum_n q A.
+// Chunks of rows as in the forward scan, in four kernels:
+//   1. each chunk's state from zero and, in the same walk, the gradient that
+//      its rows send to the state before it: sum_t (prod_{r<=t} a_r) C_t p_t;
+//   2. both carried over the chunks, forwards and backwards;
+//   3. each chunk: a walk forwards that leaves the state before every tile of
+//      rows in LDS, then the tiles from the last to the first: the tile's
+//      states again into registers, then its rows backwards;
+//   4. the sums over chunks (dA, dD, ddt_bias) and over workgroups (dB, dC).
+// The sums over channels of dB and dC run over a wave's 16 quads: four values
+// at a time fold into one register by swapping halves and rows of lanes, so
+// that a value costs two instructions instead of four exchanges.
+#include <algorithm>
+
+#include "seq_scan.h"
+
+namespace im2win {
+namespace {
+
+struct ScanBwdArgs {
+    ScanArgs s;
+    const void* dy;
+    const float* d_final;
+    void* dx;
+    void* ddt;
+    float* dA;
+    void* dB;
+    void* dC;
+    float* dD;
+    void* dz;
+    float* ddt_bias;
+    float* d_init;
+    float* back;      // [chunks][channels][4*NS]: the gradient of the state before each chunk
+    float* dbc;       // [group_blocks][tokens][G][2][4*NS]
+    float* da_part;   // [chunks][channels][4*NS]
+    float* dd_part;   // [chunks][channels][2]: dD and ddt_bias
+    int groups;
+};
+
+// flags beside kGoesOn and kBegan: the chunk's first sequence began before it /
+// and goes on behind it, so that the chunk is inside one sequence
+constexpr int kFromBefore = 4, kThrough = 8;
+
+// Rows of a tile whose states are in registers, and of a chunk (whose tiles'
+// first states, B and C lie in LDS)
+template <int NS> constexpr int kTileRows = NS >= 16 || NS == 6 ? 4 : 8;
+template <int NS> constexpr int kChunkRows = NS == 32 ? 12 : NS == 16 || NS == 6 ? 24 : 64;
+
+template <int NS, int CH>
+struct BwdLds {
+    static constexpr int NP = kQuad * NS, Q = kChunkRows<NS>, TB = kTileRows<NS>;
+    float b[Q * NP], c[Q * NP];
+    float part[kScanWaves][TB][2 * NP];
+    float state[kScanWaves][Q / TB][CH * NS][kWave];
+};
+
+// The chunk's rows and the sequence of one of them
+struct ChunkRows {
+    int lo, hi;
+    __device__ __forceinline__ ChunkRows(const ScanArgs& a, int chunk) {
+        lo = max(a.seq.first(0), chunk * a.chunk);
+        hi = min(a.seq.first(a.seq.count), min(chunk * a.chunk, a.seq.tokens - a.chunk) + a.chunk);
+    }
+};
+
+template <int NS, int CH>
+__device__ __forceinline__ void load_state(const float* m, const ScanArgs& a, const Lane<CH>& l, int b, float (&h)[CH][NS]) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int n = l.q * NS + s;
+            h[i][s] = m && n < a.states ? m[((int64_t)b * a.channels + l.c[i]) * a.states + n] : 0.0f;
+        }
+}
+
+template <int NS, int CH>
+__device__ __forceinline__ void load_decay(const ScanArgs& a, const Lane<CH>& l, float (&a2)[CH][NS]) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            const int n = l.q * NS + s;
+            a2[i][s] = n < a.states ? kLog2e * a.A[(int64_t)l.c[i] * a.states + n] : 0.0f;
+        }
+}
+
+// What four rows (one per lane of the quad) need in the walks
+template <typename T, int CH>
+struct BwdRows {
+    Raw<T, CH> x, dt, z, dy;
+
+    __device__ __forceinline__ void load_in(const ScanArgs& a, const Lane<CH>& l, int64_t row) {
+        x.load(static_cast<const T*>(a.x) + row * a.ld_x, l.c, a.wide);
+        dt.load(static_cast<const T*>(a.dt) + row * a.ld_dt, l.c, a.wide);
+    }
+    __device__ __forceinline__ void load_grad(const ScanBwdArgs& p, const Lane<CH>& l, int64_t row) {
+        if (p.s.z) z.load(static_cast<const T*>(p.s.z) + row * p.s.ld_z, l.c, p.s.wide);
+        dy.load(static_cast<const T*>(p.dy) + row * p.s.channels, l.c, p.s.wide);
+    }
+    __device__ __forceinline__ float step(const ScanArgs& a, int i, float bias) const {
+        const float v = dt.get(i, a.wide) + bias;
+        return a.softplus ? softplus(v) : v;
+    }
+    // the gradient of the sum in front of the gate
+    __device__ __forceinline__ float grad(const ScanArgs& a, int i) const {
+        const float g = dy.get(i, a.wide);
+        if (!a.z) return g;
+        const float v = z.get(i, a.wide);
+        return g * v * sigmoid(v);
+    }
+};
+
+// ---------------------------------------------------------------------------
+// 1. What a chunk does to the states: forwards for its last sequence, where
+// that goes on, and backwards for its first, where that began before.
+// ---------------------------------------------------------------------------
+template <typename T, int NS, int CH>
+__global__ __launch_bounds__(kScanWaves * kWave) void scan_bwd_summary_kernel(ScanBwdArgs p) {
+    constexpr int NP = kQuad * NS;
+    const ScanArgs& a = p.s;
+    __shared__ __align__(16) float sb[kScanTile * NP];
+    __shared__ __align__(16) float sc[kScanTile * NP];
+    const int block = blockIdx.x % a.blocks, chunk = blockIdx.x / a.blocks;
+    const int wave = uniform(threadIdx.x / kWave);
+    const ChunkRows rows(a, chunk);
+    int flags = 0, b0 = 0, end0 = 0, b1 = 0, first1 = 0;
+    if (rows.lo < rows.hi) {
+        b0 = a.seq.find(rows.lo);
+        b1 = a.seq.find(rows.hi - 1);
+        end0 = a.seq.first(b0 + 1);
+        first1 = a.seq.first(b1);
+        const int first0 = a.seq.first(b0), end1 = a.seq.first(b1 + 1);
+        flags = (end1 > rows.hi ? kGoesOn : 0) | (first1 >= rows.lo ? kBegan : 0) | (first0 < rows.lo ? kFromBefore : 0);
+        if (first0 < rows.lo && end0 > rows.hi) flags |= kThrough;
+    }
+    if (block == 0 && threadIdx.x == 0) a.flags[chunk] = flags;
+    if (!(flags & (kGoesOn | kFromBefore))) return;
+
+    Lane<CH> l;
+    l.init(a, block, wave);
+    const int group_offset = block / a.group_blocks * a.states;
+    float a2[CH][NS], bias[CH];
+    load_decay<NS, CH>(a, l, a2);
+#pragma unroll
+    for (int i = 0; i < CH; ++i) bias[i] = a.dt_bias ? a.dt_bias[l.c[i]] : 0.0f;
+
+    // rows [from, to) of one sequence: h from its value before, the sum of steps, and the gradient sent back
+    float h[CH][NS], back[CH][NS], pass[CH][NS], span[CH];
+    auto walk = [&](int from, int to) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            span[i] = 0.0f;
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                back[i][s] = 0.0f;
+                pass[i][s] = 1.0f;
+            }
+        }
+        BwdRows<T, CH> next;
+        int64_t row = min(from + l.q, to - 1);
+        next.load_in(a, l, row);
+        next.load_grad(p, l, row);
+        for (int tile = from; tile < to; tile += kScanTile) {
+            const int n = min(kScanTile, to - tile);
+            __syncthreads();
+            stage<T, NS>(sb, static_cast<const T*>(a.B), a.ld_b, group_offset, a.states, tile, n);
+            stage<T, NS>(sc, static_cast<const T*>(a.C), a.ld_c, group_offset, a.states, tile, n);
+            __syncthreads();
+            for (int r = 0; r < n; r += kQuad) {
+                const int t = tile + r;
+                const BwdRows<T, CH> now = next;
+                if (t + kQuad < to) {
+                    row = min(t + kQuad + l.q, to - 1);
+                    next.load_in(a, l, row);
+                    next.load_grad(p, l, row);
+                }
+                float step[CH], in[CH], grad[CH];
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    step[i] = now.step(a, i, bias[i]);
+                    in[i] = step[i] * now.x.get(i, a.wide);
+                    grad[i] = now.grad(a, i);
+                    if (t + l.q < to) span[i] += step[i];
+                }
+                auto token = [&](auto j) {
+                    constexpr int J = decltype(j)::value;
+                    if (t + J >= to) return;
+                    float bm[NS], cm[NS];
+                    lds_row<NS>(sb + (r + J) * NP + l.q * NS, bm);
+                    lds_row<NS>(sc + (r + J) * NP + l.q * NS, cm);
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) {
+                        const float sj = quad_get<J>(step[i]), ij = quad_get<J>(in[i]), gj = quad_get<J>(grad[i]);
+#pragma unroll
+                        for (int s = 0; s < NS; ++s) {
+                            const float decay = __builtin_amdgcn_exp2f(sj * a2[i][s]);
+                            h[i][s] = fmaf(decay, h[i][s], ij * bm[s]);
+                            pass[i][s] *= decay;
+                            back[i][s] = fmaf(pass[i][s], gj * cm[s], back[i][s]);
+                        }
+                    }
+                };
+                using std::integral_constant;
+                token(integral_constant<int, 0>{});
+                token(integral_constant<int, 1>{});
+                token(integral_constant<int, 2>{});
+                token(integral_constant<int, 3>{});
+            }
+        }
+    };
+    auto put = [&](float* m, const float (&v)[CH][NS]) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+                if (l.live[i]) m[((int64_t)chunk * a.channels + l.c[i]) * NP + l.q * NS + s] = v[i][s];
+    };
+    auto put_forward = [&]() {
+        put(a.carry, h);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            span[i] = quad_sum(span[i]);
+            if (l.live[i] && l.q == 0) a.span[(int64_t)chunk * a.channels + l.c[i]] = span[i];
+        }
+    };
+    if (flags & kFromBefore) {
+        load_state<NS, CH>(nullptr, a, l, 0, h);
+        walk(rows.lo, min(end0, rows.hi));
+        if (p.d_final && end0 <= rows.hi) {
+            // the sequence ends here: its final state's gradient comes back through all of its rows
+            float d[CH][NS];
+            load_state<NS, CH>(p.d_final, a, l, b0, d);
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int s = 0; s < NS; ++s) back[i][s] = fmaf(pass[i][s], d[i][s], back[i][s]);
+        }
+        put(p.back, back);
+        if (flags & kThrough) put_forward();
+    }
+    if ((flags & kGoesOn) && !(flags & kThrough)) {
+        load_state<NS, CH>(first1 >= rows.lo ? a.init : nullptr, a, l, b1, h);
+        walk(max(rows.lo, first1), rows.hi);
+        put_forward();
+    }
+}
+
+// ---------------------------------------------------------------------------
+// 2. The states behind the chunks (blockIdx.y 0) and the gradients of the
+// states before them (1): one thread per channel and state.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void scan_bwd_carry_kernel(ScanBwdArgs p, int padded) {
+    const ScanArgs& a = p.s;
+    const int64_t each = (int64_t)a.channels * padded;
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (e >= each) return;
+    const int c = (int)(e / padded), n = (int)(e % padded);
+    const float a2 = n < a.states ? kLog2e * a.A[(int64_t)c * a.states + n] : 0.0f;
+    constexpr int U = 8;
+    const bool forward = blockIdx.y == 0;
+    float* m = forward ? a.carry : p.back;
+    const int reads = forward ? kGoesOn : kFromBefore;
+    float v = 0.0f;
+    for (int k = 0; k < a.chunks; k += U) {
+        float own[U], decay[U];
+        int f[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = min(k + u, a.chunks - 1);
+            const int64_t at = forward ? i : a.chunks - 1 - i;
+            f[u] = a.flags[at];
+            own[u] = f[u] & reads ? m[at * each + e] : 0.0f;
+            decay[u] = f[u] & kThrough ? __builtin_amdgcn_exp2f(a2 * a.span[at * a.channels + c]) : 0.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (k + u >= a.chunks || !(f[u] & reads)) continue;
+            const int64_t at = forward ? k + u : a.chunks - 1 - (k + u);
+            v = f[u] & kThrough ? fmaf(decay[u], v, own[u]) : own[u];
+            m[at * each + e] = v;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// 3. The rows' gradients
+// ---------------------------------------------------------------------------
+
+// Four values summed over the wave's lanes of the same place in their quad:
+// every lane of row r of 16 holds the sum of v[kFoldOrder[r]].
+__device__ __forceinline__ float fold4(float v0, float v1, float v2, float v3) {
+    auto halves = [](float x, float y) {     // lanes 0-31: x over both halves; 32-63: y
+        auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+        return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    };
+    const float w0 = halves(v0, v1), w1 = halves(v2, v3);
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(w0), __float_as_uint(w1), false, false);
+    float u = __uint_as_float(r[0]) + __uint_as_float(r[1]);     // rows of 16 lanes: v0, v2, v1, v3
+    u += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(u), 0x124, 0xf, 0xf, true));   // rotated by 4 lanes
+    u += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(u), 0x128, 0xf, 0xf, true));   // and by 8
+    return u;
+}
+// the value that row r of 16 lanes holds: 0, 2, 1, 3
+__device__ __forceinline__ int fold_place(int lane) { return (lane >> 5 & 1) | (lane >> 3 & 2); }
+
+template <typename T, int NS, int CH>
+__global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd_kernel(ScanBwdArgs p) {
+    constexpr int NP = kQuad * NS, TB = kTileRows<NS>, GROUPS = TB / kQuad;
+    extern __shared__ __align__(16) char raw_lds[];
+    BwdLds<NS, CH>& lds = *reinterpret_cast<BwdLds<NS, CH>*>(raw_lds);
+    const ScanArgs& a = p.s;
+    const int block = blockIdx.x % a.blocks, chunk = blockIdx.x / a.blocks;
+    const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+
+    if (chunk >= a.chunks) {
+        // workgroups behind the chunks': the states of sequences without rows pass from one end to the other
+        const int64_t each = (int64_t)a.channels * a.states;
+        const int extra = (int)gridDim.x - a.blocks * a.chunks;
+        for (int b = blockIdx.x - a.blocks * a.chunks; b < a.seq.count; b += extra) {
+            if (a.seq.first(b + 1) > a.seq.first(b)) continue;
+            for (int64_t i = threadIdx.x; i < each; i += blockDim.x)
+                p.d_init[b * each + i] = p.d_final ? p.d_final[b * each + i] : 0.0f;
+        }
+        return;
+    }
+
+    Lane<CH> l;
+    l.init(a, block, wave);
+    const int group = block / a.group_blocks, group_block = block % a.group_blocks;
+    const ChunkRows rows(a, chunk);
+    float da[CH][NS] = {}, dd[CH] = {}, dbias[CH] = {};
+
+    if (rows.lo < rows.hi) {
+        float a2[CH][NS], bias[CH], skip[CH];
+        load_decay<NS, CH>(a, l, a2);
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+            bias[i] = a.dt_bias ? a.dt_bias[l.c[i]] : 0.0f;
+            skip[i] = a.D ? a.D[l.c[i]] : 0.0f;
+        }
+        const int n_rows = rows.hi - rows.lo, tiles = (n_rows + TB - 1) / TB;
+        for (int i = threadIdx.x; i < n_rows * NP; i += kScanWaves * kWave) {
+            const int r = i / NP, s = i % NP;
+            const bool in = s < a.states;
+            const int64_t at = (int64_t)group * a.states + s;
+            lds.b[i] = in ? (float)(static_cast<const T*>(a.B) + (int64_t)(rows.lo + r) * a.ld_b)[at] : 0.0f;
+            lds.c[i] = in ? (float)(static_cast<const T*>(a.C) + (int64_t)(rows.lo + r) * a.ld_c)[at] : 0.0f;
+        }
+        __syncthreads();
+
+        // forwards: the state before each tile
+        {
+            float h[CH][NS];
+            int b = a.seq.find(rows.lo), end = a.seq.first(b + 1);
+            const int first = a.seq.first(b);
+            if (rows.lo == first) {
+                load_state<NS, CH>(a.init, a, l, b, h);
+            } else {
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int s = 0; s < NS; ++s)
+                        h[i][s] = chunk ? a.carry[((int64_t)(chunk - 1) * a.channels + l.c[i]) * NP + l.q * NS + s] : 0.0f;
+            }
+            BwdRows<T, CH> next;
+            next.load_in(a, l, min(rows.lo + l.q, rows.hi - 1));
+            for (int k = 0; k < tiles; ++k) {
+#pragma unroll
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) lds.state[wave][k][i * NS + s][lane] = h[i][s];
+                if (k == tiles - 1) break;
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) {
+                    const int r = k * TB + g * kQuad, t = rows.lo + r;
+                    const BwdRows<T, CH> now = next;
+                    next.load_in(a, l, min(t + kQuad + l.q, rows.hi - 1));
+                    float step[CH], in[CH];
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) {
+                        step[i] = now.step(a, i, bias[i]);
+                        in[i] = step[i] * now.x.get(i, a.wide);
+                    }
+                    auto token = [&](auto j) {
+                        constexpr int J = decltype(j)::value;
+                        if (t + J >= end) {
+                            b = a.seq.find(t + J);
+                            end = a.seq.first(b + 1);
+                            load_state<NS, CH>(a.init, a, l, b, h);
+                        }
+                        float bm[NS];
+                        lds_row<NS>(lds.b + (r + J) * NP + l.q * NS, bm);
+#pragma unroll
+                        for (int i = 0; i < CH; ++i) {
+                            const float sj = quad_get<J>(step[i]), ij = quad_get<J>(in[i]);
+#pragma unroll
+                            for (int s = 0; s < NS; ++s)
+                                h[i][s] = fmaf(__builtin_amdgcn_exp2f(sj * a2[i][s]), h[i][s], ij * bm[s]);
+                        }
+                    };
+                    using std::integral_constant;
+                    token(integral_constant<int, 0>{});
+                    token(integral_constant<int, 1>{});
+                    token(integral_constant<int, 2>{});
+                    token(integral_constant<int, 3>{});
+                }
+            }
+        }
+
+        // backwards
+        int b = a.seq.find(rows.hi - 1), first = a.seq.first(b), end = a.seq.first(b + 1);
+        float r[CH][NS];     // a g of the row behind: what the state's gradient receives from there
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int s = 0; s < NS; ++s)
+                r[i][s] = end > rows.hi && l.live[i] && chunk + 1 < a.chunks
+                              ? p.back[((int64_t)(chunk + 1) * a.channels + l.c[i]) * NP + l.q * NS + s] : 0.0f;
+        for (int k = tiles - 1; k >= 0; --k) {
+            const int r0 = k * TB, t0 = rows.lo + r0, t1 = min(t0 + TB, rows.hi);
+            if (t1 - 1 < first) {
+                b = a.seq.find(t1 - 1);
+                first = a.seq.first(b);
+                end = a.seq.first(b + 1);
+            }
+            // a tile inside one sequence, none of whose rows is the sequence's first or last
+            const bool inside = first < t0 && end > t0 + TB && t0 + TB <= rows.hi;
+
+            BwdRows<T, CH> now[GROUPS];
+            float step[GROUPS][CH], in[GROUPS][CH], grad[GROUPS][CH];
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const int64_t row = min(t0 + g * kQuad + l.q, rows.hi - 1);
+                now[g].load_in(a, l, row);
+                now[g].load_grad(p, l, row);
+            }
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    step[g][i] = now[g].step(a, i, bias[i]);
+                    in[g][i] = l.live[i] ? step[g][i] * now[g].x.get(i, a.wide) : 0.0f;
+                    grad[g][i] = l.live[i] ? now[g].grad(a, i) : 0.0f;
+                }
+            float h0[CH][NS], h[TB][CH][NS];
+#pragma unroll
+            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                for (int s = 0; s < NS; ++s) h0[i][s] = lds.state[wave][k][i * NS + s][lane];
+
+            float du[GROUPS][CH] = {}, ds[GROUPS][CH] = {}, sum[GROUPS][CH] = {};
+            auto tile = [&](auto edge) {
+                constexpr bool EDGE = decltype(edge)::value;
+                unsigned starts = 0, ends = 0;      // rows that begin or end a sequence
+                int bb = 0, bend = 0;
+                if constexpr (EDGE) {
+                    bb = a.seq.find(t0);
+                    bend = a.seq.first(bb + 1);
+                    if (a.seq.first(bb) == t0) starts = 1;
+                }
+                auto forward = [&](auto j) {
+                    constexpr int J = decltype(j)::value, G = J / kQuad;
+                    if constexpr (EDGE) {
+                        if (t0 + J >= rows.hi) return;
+                        if (t0 + J >= bend) {
+                            bb = a.seq.find(t0 + J);
+                            bend = a.seq.first(bb + 1);
+                            starts |= 1u << J;
+                        }
+                        if (t0 + J + 1 == bend) ends |= 1u << J;
+                    }
+                    float bm[NS];
+                    lds_row<NS>(lds.b + (r0 + J) * NP + l.q * NS, bm);
+                    float hp[CH][NS];
+#pragma unroll
+                    for (int i = 0; i < CH; ++i)
+#pragma unroll
+                        for (int s = 0; s < NS; ++s) hp[i][s] = J == 0 ? h0[i][s] : h[J > 0 ? J - 1 : 0][i][s];
+                    if constexpr (EDGE)
+                        if (starts >> J & 1) load_state<NS, CH>(a.init, a, l, bb, hp);
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) {
+                        const float sj = quad_get<J % kQuad>(step[G][i]), ij = quad_get<J % kQuad>(in[G][i]);
+#pragma unroll
+                        for (int s = 0; s < NS; ++s)
+                            h[J][i][s] = fmaf(__builtin_amdgcn_exp2f(sj * a2[i][s]), hp[i][s], ij * bm[s]);
+                    }
+                };
+                auto backward = [&](auto j) {
+                    constexpr int J = decltype(j)::value, G = J / kQuad;
+                    float hp[CH][NS];
+#pragma unroll
+                    for (int i = 0; i < CH; ++i)
+#pragma unroll
+                        for (int s = 0; s < NS; ++s) hp[i][s] = J == 0 ? h0[i][s] : h[J > 0 ? J - 1 : 0][i][s];
+                    if constexpr (EDGE) {
+                        if (t0 + J >= rows.hi) return;
+                        if ((starts | ends) >> J & 1) {
+                            bb = a.seq.find(t0 + J);
+                            if (starts >> J & 1) load_state<NS, CH>(a.init, a, l, bb, hp);
+                            if (ends >> J & 1) {
+                                load_state<NS, CH>(p.d_final, a, l, bb, r);
+#pragma unroll
+                                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                                    for (int s = 0; s < NS; ++s)
+                                        if (!l.live[i]) r[i][s] = 0.0f;
+                            }
+                        }
+                    }
+                    float bm[NS], cm[NS], v[2 * NS];
+                    lds_row<NS>(lds.b + (r0 + J) * NP + l.q * NS, bm);
+                    lds_row<NS>(lds.c + (r0 + J) * NP + l.q * NS, cm);
+#pragma unroll
+                    for (int s = 0; s < 2 * NS; ++s) v[s] = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) {
+                        const float sj = quad_get<J % kQuad>(step[G][i]), ij = quad_get<J % kQuad>(in[G][i]),
+                                    gj = quad_get<J % kQuad>(grad[G][i]);
+                        float u = 0.0f, w = 0.0f, y = 0.0f;
+#pragma unroll
+                        for (int s = 0; s < NS; ++s) {
+                            const float g = fmaf(cm[s], gj, r[i][s]);
+                            v[s] = fmaf(g, ij, v[s]);
+                            v[NS + s] = fmaf(h[J][i][s], gj, v[NS + s]);
+                            u = fmaf(g, bm[s], u);
+                            y = fmaf(cm[s], h[J][i][s], y);
+                            r[i][s] = __builtin_amdgcn_exp2f(sj * a2[i][s]) * g;
+                            const float q = r[i][s] * hp[i][s];
+                            w = fmaf(q, a2[i][s], w);
+                            da[i][s] = fmaf(q, sj, da[i][s]);
+                        }
+                        u = quad_sum(u);
+                        w = quad_sum(w);
+                        y = quad_sum(y);
+                        if (l.q == J % kQuad) {
+                            du[G][i] = u;
+                            ds[G][i] = w;
+                            sum[G][i] = y;
+                        }
+                    }
+#pragma unroll
+                    for (int f = 0; f < 2 * NS; f += 4) {
+                        const float folded = fold4(v[f], v[f + 1], v[f + 2], v[f + 3]);
+                        if ((lane & 12) == 0) {
+                            const int at = f + fold_place(lane);
+                            lds.part[wave][J][at < NS ? l.q * NS + at : NP + l.q * NS + at - NS] = folded;
+                        }
+                    }
+                    if constexpr (EDGE) {
+                        if ((starts >> J & 1) && p.d_init) {
+#pragma unroll
+                            for (int i = 0; i < CH; ++i)
+#pragma unroll
+                                for (int s = 0; s < NS; ++s) {
+                                    const int n = l.q * NS + s;
+                                    if (l.live[i] && n < a.states)
+                                        p.d_init[((int64_t)bb * a.channels + l.c[i]) * a.states + n] = r[i][s];
+                                }
+                        }
+                    }
+                };
+                using std::integral_constant;
+                forward(integral_constant<int, 0>{});
+                forward(integral_constant<int, 1>{});
+                forward(integral_constant<int, 2>{});
+                forward(integral_constant<int, 3>{});
+                if constexpr (TB == 8) {
+                    forward(integral_constant<int, 4>{});
+                    forward(integral_constant<int, 5>{});
+                    forward(integral_constant<int, 6>{});
+                    forward(integral_constant<int, 7>{});
+                    backward(integral_constant<int, 7>{});
+                    backward(integral_constant<int, 6>{});
+                    backward(integral_constant<int, 5>{});
+                    backward(integral_constant<int, 4>{});
+                }
+                backward(integral_constant<int, 3>{});
+                backward(integral_constant<int, 2>{});
+                backward(integral_constant<int, 1>{});
+                backward(integral_constant<int, 0>{});
+            };
+            if (inside) tile(std::false_type{});
+            else tile(std::true_type{});
+
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) {
+                const int64_t row = t0 + g * kQuad + l.q;
+                if (row >= t1) continue;
+                float dx[CH], ddt[CH], dz[CH];
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const float x = now[g].x.get(i, a.wide);
+                    dx[i] = fmaf(du[g][i], step[g][i], skip[i] * grad[g][i]);
+                    ddt[i] = fmaf(du[g][i], x, ds[g][i] * (1.0f / kLog2e));
+                    if (a.softplus) ddt[i] *= sigmoid(now[g].dt.get(i, a.wide) + bias[i]);
+                    if (a.z) {
+                        const float z = now[g].z.get(i, a.wide), sig = sigmoid(z);
+                        dz[i] = now[g].dy.get(i, a.wide) * fmaf(skip[i], x, sum[g][i]) * sig * fmaf(z, 1.0f - sig, 1.0f);
+                    }
+                    dd[i] = fmaf(grad[g][i], x, dd[i]);
+                    dbias[i] += ddt[i];
+                }
+                store_channels<CH>(static_cast<T*>(p.dx) + row * a.channels, l.c0, l.live, dx, a.wide);
+                store_channels<CH>(static_cast<T*>(p.ddt) + row * a.channels, l.c0, l.live, ddt, a.wide);
+                if (a.z) store_channels<CH>(static_cast<T*>(p.dz) + row * a.channels, l.c0, l.live, dz, a.wide);
+            }
+
+            // the waves' sums of dB and dC
+            __syncthreads();
+            for (int i = threadIdx.x; i < (t1 - t0) * 2 * NP; i += kScanWaves * kWave) {
+                const int j = i / (2 * NP), n = i % (2 * NP);
+                float v = lds.part[0][j][n];
+#pragma unroll
+                for (int w = 1; w < kScanWaves; ++w) v += lds.part[w][j][n];
+                p.dbc[(((int64_t)group_block * a.seq.tokens + t0 + j) * p.groups + group) * (2 * NP) + n] = v;
+            }
+            __syncthreads();
+        }
+    }
+
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+        dd[i] = quad_sum(dd[i]);
+        dbias[i] = quad_sum(dbias[i]);
+        if (!l.live[i]) continue;
+        const int64_t at = (int64_t)chunk * a.channels + l.c[i];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) p.da_part[at * NP + l.q * NS + s] = da[i][s];
+        if (l.q == 0) {
+            p.dd_part[2 * at] = dd[i];
+            p.dd_part[2 * at + 1] = dbias[i];
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// 4. Sums.  Workgroups 0 to param_blocks - 1: 64 channels' states (or
+// channels) each, a wave for every fourth chunk; the others dB and dC.
+// ---------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(kScanWaves * kWave) void scan_bwd_sum_kernel(ScanBwdArgs p, int padded, int state_blocks, int param_blocks) {
+    const ScanArgs& a = p.s;
+    __shared__ float part[kScanWaves][kWave];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    if ((int)blockIdx.x < param_blocks) {
+        const bool states = (int)blockIdx.x < state_blocks;
+        const int64_t each = (int64_t)a.channels * (states ? padded : 2);
+        const float* m = states ? p.da_part : p.dd_part;
+        const int64_t e = ((int64_t)blockIdx.x - (states ? 0 : state_blocks)) * kWave + lane;
+        float v = 0.0f;
+        if (e < each)
+            for (int k = wave; k < a.chunks; k += kScanWaves) v += m[k * each + e];
+        part[wave][lane] = v;
+        __syncthreads();
+        if (wave != 0 || e >= each) return;
+#pragma unroll
+        for (int w = 1; w < kScanWaves; ++w) v += part[w][lane];
+        if (states) {
+            const int64_t c = e / padded, n = e % padded;
+            if (n < a.states) p.dA[c * a.states + n] = v;
+        } else {
+            float* out = e % 2 ? p.ddt_bias : p.dD;
+            if (out) out[e / 2] = v;
+        }
+        return;
+    }
+    // dB and dC of the rows that sequences hold
+    const int64_t per_row = (int64_t)p.groups * a.states;
+    const int64_t lo = (int64_t)a.seq.first(0) * per_row, hi = (int64_t)a.seq.first(a.seq.count) * per_row;
+    const int64_t e = ((int64_t)blockIdx.x - param_blocks) * blockDim.x + threadIdx.x;
+    if (e < lo || e >= hi) return;
+    const int64_t rg = e / a.states, n = e % a.states;      // row and group
+    const float* m = p.dbc + rg * (2 * padded) + n;
+    const int64_t next = (int64_t)a.seq.tokens * p.groups * (2 * padded);
+    float b = 0.0f, c = 0.0f;
+    for (int k = 0; k < a.group_blocks; ++k, m += next) {
+        b += m[0];
+        c += m[padded];
+    }
+    static_cast<T*>(p.dB)[e] = (T)b;
+    static_cast<T*>(p.dC)[e] = (T)c;
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+struct BwdPlan {
+    int64_t chunk = 0, chunks = 0, blocks = 0, group_blocks = 0;
+    int ns = 0, ch = 0;
+    size_t carry = 0, span = 0, flags = 0, dbc = 0, da = 0, dd = 0, bytes = 0;
+};
+
+size_t round16(size_t n) { return (n + 15) / 16 * 16; }
+
+BwdPlan plan_bwd(const im2win_scan_desc* d) {
+    BwdPlan p;
+    int64_t tile = 8;
+    with_states(d->states, [&](auto ns, auto ch) {
+        p.ns = decltype(ns)::value;
+        p.ch = decltype(ch)::value;
+        p.chunk = kChunkRows<decltype(ns)::value>;
+        tile = kTileRows<decltype(ns)::value>;
+    });
+    const int64_t per_block = kScanWaves * (kWave / kQuad) * p.ch;
+    p.group_blocks = (d->channels / d->groups + per_block - 1) / per_block;
+    p.blocks = d->groups * p.group_blocks;
+    if (d->tokens == 0) return p;
+    // the longest chunk the LDS holds, halved while that leaves fewer than two workgroups for each CU
+    while (p.chunk > 2 * tile && p.blocks * ((d->tokens + p.chunk - 1) / p.chunk) < 512)
+        p.chunk = std::max(p.chunk / 2 / tile, int64_t(2)) * tile;
+    p.chunk = std::min(p.chunk, d->tokens);
+    p.chunks = (d->tokens + p.chunk - 1) / p.chunk;
+    const int64_t np = kQuad * p.ns;
+    p.carry = round16((size_t)(p.chunks * d->channels * np) * 4);
+    p.span = round16((size_t)(p.chunks * d->channels) * 4);
+    p.flags = round16((size_t)p.chunks * 4);
+    p.dbc = round16((size_t)(p.group_blocks * d->tokens * d->groups * 2 * np) * 4);
+    p.da = p.carry;
+    p.dd = 2 * p.span;
+    p.bytes = 2 * p.carry + p.span + p.flags + p.dbc + p.da + p.dd;
+    return p;
+}
+
+constexpr int kEmptyBlocks = 32;
+
+template <typename F>
+void with_type(int32_t dtype, F f) {
+    if (dtype == IM2WIN_F32) f(float{});
+    else f(bf16{});
+}
+
+}  // namespace
+}  // namespace im2win
+
+using namespace im2win;
+
+extern "C" {
+
+int im2win_selective_scan_backward_workspace_bytes(const im2win_scan_desc* d, size_t* bytes) {
+    int rc = check_scan(d, true, nullptr, false);
+    if (rc) return rc;
+    if (!bytes) return fail(IM2WIN_ENULL, "bytes is NULL");
+    *bytes = plan_bwd(d).bytes;
+    return ok();
+}
+
+int im2win_selective_scan_backward(const im2win_scan_desc* d, const void* dy, const void* x, const void* dt,
+                                   const float* A, const void* B, const void* C, const float* D, const void* z,
+                                   const float* dt_bias, const int32_t* seq_starts, const float* initial_state,
+                                   const float* d_final_state, void* dx, void* ddt, float* dA, void* dB, void* dC,
+                                   float* dD, void* dz, float* ddt_bias, float* d_initial_state, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+    int rc = check_scan(d, true, seq_starts, true);
+    if (rc || (rc = check_scan_inputs(d, x, dt, A, B, C, D, z, dt_bias))) return rc;
+    const size_t e = d->dtype == IM2WIN_F32 ? 4 : 2;
+    if (d->tokens && ((rc = need_ptr(dy, e, "dy")) || (rc = need_ptr(dx, e, "dx")) || (rc = need_ptr(ddt, e, "ddt")) ||
+                      (rc = need_ptr(dB, e, "dB")) || (rc = need_ptr(dC, e, "dC")) ||
+                      (z && (rc = need_ptr(dz, e, "dz")))))
+        return rc;
+    if ((rc = need_ptr(dA, 4, "dA")) || (rc = may_ptr(dD, 4, "dD")) || (rc = may_ptr(ddt_bias, 4, "ddt_bias")) ||
+        (rc = may_ptr(initial_state, 4, "initial_state")) || (rc = may_ptr(d_final_state, 4, "d_final_state")) ||
+        (rc = may_ptr(d_initial_state, 4, "d_initial_state")))
+        return rc;
+    const BwdPlan p = plan_bwd(d);
+    if (p.bytes && (rc = need_ptr(workspace, 16, "workspace"))) return rc;
+    if (workspace_bytes < p.bytes)
+        return fail(IM2WIN_EWORKSPACE, "workspace holds %zu bytes, the gradients need %zu", workspace_bytes, p.bytes);
+    ScanBwdArgs b{};
+    b.s = scan_args(d, x, dt, A, B, C, D, z, dt_bias, p.ch);
+    b.s.init = initial_state;
+    b.s.seq = make_seq_map(d->tokens, d->sequences, seq_starts);
+    b.s.chunk = (int)p.chunk; b.s.chunks = (int)p.chunks;
+    const size_t pair = 2 * e;
+    b.s.wide = b.s.wide && aligned_to(dy, pair) && aligned_to(dx, pair) && aligned_to(ddt, pair) && aligned_to(dz, pair);
+    b.dy = dy; b.d_final = d_final_state; b.dx = dx; b.ddt = ddt; b.dA = dA; b.dB = dB; b.dC = dC; b.dD = dD;
+    b.dz = dz; b.ddt_bias = ddt_bias; b.d_init = d_initial_state;
+    b.groups = (int)d->groups;
+    char* ws = static_cast<char*>(workspace);
+    auto take = [&](size_t n) { char* q = ws; ws += n; return q; };
+    if (p.bytes) {
+        b.s.carry = reinterpret_cast<float*>(take(p.carry));
+        b.back = reinterpret_cast<float*>(take(p.carry));
+        b.s.span = reinterpret_cast<float*>(take(p.span));
+        b.s.flags = reinterpret_cast<int*>(take(p.flags));
+        b.dbc = reinterpret_cast<float*>(take(p.dbc));
+        b.da_part = reinterpret_cast<float*>(take(p.da));
+        b.dd_part = reinterpret_cast<float*>(take(p.dd));
+    }
+    const int64_t grid = p.blocks * p.chunks;
+    const int64_t extra = d_initial_state && (seq_starts || d->tokens == 0) ? std::min<int64_t>(d->sequences, kEmptyBlocks) : 0;
+    const int64_t np = kQuad * p.ns;
+    const int64_t state_blocks = (d->channels * np + kWave - 1) / kWave;
+    const int64_t param_blocks = state_blocks + (2 * d->channels + kWave - 1) / kWave;
+    const int64_t sums = param_blocks + (d->tokens * d->groups * d->states + kScanWaves * kWave - 1) / (kScanWaves * kWave);
+    if (grid + extra > (int64_t(1) << 31) - 1 || sums > (int64_t(1) << 31) - 1)
+        return fail(IM2WIN_EOVERFLOW, "too many channels and tokens");
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    int hip = 0;
+    with_type(d->dtype, [&](auto t) {
+        using T = decltype(t);
+        with_states(d->states, [&](auto ns, auto ch) {
+            constexpr int NS = decltype(ns)::value, CH = decltype(ch)::value;
+            const dim3 threads(kScanWaves * kWave);
+            if (p.chunks > 1) {
+                hipLaunchKernelGGL((scan_bwd_summary_kernel<T, NS, CH>), dim3((unsigned)grid), threads, 0, s, b);
+                hipLaunchKernelGGL(scan_bwd_carry_kernel, dim3((unsigned)((d->channels * np + 255) / 256), 2), dim3(256), 0, s,
+                                   b, (int)np);
+            }
+            if (grid + extra) {
+                constexpr int bytes = (int)sizeof(BwdLds<NS, CH>);
+                static_assert(bytes <= 160 * 1024, "LDS of a CU");
+                if (bytes > 64 * 1024)
+                    hip = (int)hipFuncSetAttribute(reinterpret_cast<const void*>(&scan_bwd_kernel<T, NS, CH>),
+                                                   hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+                if (!hip) hipLaunchKernelGGL((scan_bwd_kernel<T, NS, CH>), dim3((unsigned)(grid + extra)), threads, bytes, s, b);
+            }
+        });
+        if (!hip)
+            hipLaunchKernelGGL((scan_bwd_sum_kernel<T>), dim3((unsigned)sums), dim3(kScanWaves * kWave), 0, s, b, (int)np,
+                               (int)state_blocks, (int)param_blocks);
+    });
+    if (hip) return fail(IM2WIN_EHIP, "LDS size: %s", hipGetErrorString((hipError_t)hip));
+    return launched("selective_scan_backward");
+}
+
+}  // extern "C"

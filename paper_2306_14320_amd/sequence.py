@@ -1,7 +1,8 @@
 """Binding of the sequence operators of ``libim2win.so``
 (``include/im2win_seq.h``): the short causal convolution, its gradients and
 its form for single tokens, the root-mean-square norm with the residual's
-addition, and the selective state space scan with its form for single tokens.
+addition, and the selective state space scan, its gradients and its form for
+single tokens.
 
 The ``im2win_*`` functions mirror the C entry points and take device pointers;
 the tensor helpers below them check every tensor against the descriptor and
@@ -27,7 +28,8 @@ __all__ = [
     "im2win_add_rms_norm_backward_workspace_bytes", "im2win_add_rms_norm_backward",
     "rms_norm_desc_for", "add_rms_norm", "add_rms_norm_fp8", "add_rms_norm_backward",
     "im2win_scan_desc", "im2win_selective_scan_workspace_bytes", "im2win_selective_scan", "im2win_selective_scan_step",
-    "selective_scan_desc_for", "selective_scan", "selective_scan_step",
+    "im2win_selective_scan_backward_workspace_bytes", "im2win_selective_scan_backward",
+    "selective_scan_desc_for", "selective_scan", "selective_scan_backward", "selective_scan_step", "ScanGradients",
 ]
 
 _P, _SZ, _I64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int64
@@ -68,6 +70,8 @@ SIGNATURES = {
     "im2win_causal_conv1d_step": [_CONV] + [_P] * 5 + [_I64, _P, _P],
     "im2win_selective_scan_workspace_bytes": [_SCAN, ctypes.POINTER(_SZ)],
     "im2win_selective_scan": [_SCAN] + [_P] * 13 + [_SZ, _P],
+    "im2win_selective_scan_backward_workspace_bytes": [_SCAN, ctypes.POINTER(_SZ)],
+    "im2win_selective_scan_backward": [_SCAN] + [_P] * 22 + [_SZ, _P],
     "im2win_selective_scan_step": [_SCAN] + [_P] * 10 + [_I64, _P, _P],
     "im2win_add_rms_norm": [_NORM] + [_P] * 6,
     "im2win_add_rms_norm_fp8": [_NORM] + [_P] * 7,
@@ -132,6 +136,18 @@ def im2win_selective_scan(desc, x, dt, A, B, C, D, z, dt_bias, seq_starts, initi
                           workspace_bytes, stream) -> None:
     _check(load_library().im2win_selective_scan(ctypes.byref(desc), x, dt, A, B, C, D, z, dt_bias, seq_starts,
                                                 initial_state, y, final_state, workspace, workspace_bytes, stream))
+
+
+def im2win_selective_scan_backward_workspace_bytes(desc) -> int:
+    return _bytes("im2win_selective_scan_backward_workspace_bytes", desc)
+
+
+def im2win_selective_scan_backward(desc, dy, x, dt, A, B, C, D, z, dt_bias, seq_starts, initial_state, d_final_state,
+                                   dx, ddt, dA, dB, dC, dD, dz, ddt_bias, d_initial_state, workspace, workspace_bytes,
+                                   stream) -> None:
+    _check(load_library().im2win_selective_scan_backward(
+        ctypes.byref(desc), dy, x, dt, A, B, C, D, z, dt_bias, seq_starts, initial_state, d_final_state, dx, ddt, dA,
+        dB, dC, dD, dz, ddt_bias, d_initial_state, workspace, workspace_bytes, stream))
 
 
 def im2win_selective_scan_step(desc, x, dt, A, B, C, D, z, dt_bias, slots, state, state_slots, y, stream) -> None:
@@ -400,6 +416,43 @@ def selective_scan(x, dt, A, B, C, desc, D=None, z=None, dt_bias=None, seq_start
     workspace, wsp, wsb = _workspace(workspace, im2win_selective_scan_workspace_bytes(d), x, stream)
     im2win_selective_scan(d, xp, dtp, ap, bp, cp, dp, zp, tbp, sp, ip, yp, fp, wsp, wsb, _stream(stream))
     return y
+
+
+class ScanGradients(NamedTuple):
+    dx: torch.Tensor                # T x D, x's dtype
+    ddt: torch.Tensor               # T x D, x's dtype
+    dA: torch.Tensor                # D x N, fp32
+    dB: torch.Tensor                # T x G x N, x's dtype
+    dC: torch.Tensor                # T x G x N, x's dtype
+    dD: Optional[torch.Tensor]      # D, fp32; None without D
+    dz: Optional[torch.Tensor]      # T x D, x's dtype; None without a gate
+    ddt_bias: Optional[torch.Tensor]          # D, fp32; None without a bias
+    d_initial_state: Optional[torch.Tensor]   # sequences x D x N, fp32; None without an initial state
+
+
+def selective_scan_backward(dy, x, dt, A, B, C, desc, D=None, z=None, dt_bias=None, seq_starts=None,
+                            initial_state=None, d_final_state=None, workspace=None, stream=None) -> ScanGradients:
+    """Gradients of selective_scan for dy (T x D, dense) and, where it is given,
+    d_final_state."""
+    d = desc
+    dev, ty, (xp, dtp, ap, bp, cp, dp, zp, tbp) = _scan_inputs(x, dt, A, B, C, D, z, dt_bias, d)
+    rows, proj, state = (d.tokens, d.channels), (d.tokens, d.groups, d.states), (d.sequences, d.channels, d.states)
+    sp = _dense(seq_starts, "seq_starts", (d.sequences + 1,), torch.int32, dev)
+    ip = _dense(initial_state, "initial_state", state, torch.float32, dev)
+    dyp = _dense(dy, "dy", rows, ty, dev)
+    dfp = _dense(d_final_state, "d_final_state", state, torch.float32, dev)
+
+    def new(shape, dtype, wanted=True):
+        return _empty(shape, dtype, x.device, stream) if wanted else None
+
+    f32 = torch.float32
+    g = ScanGradients(new(rows, ty), new(rows, ty), new((d.channels, d.states), f32), new(proj, ty), new(proj, ty),
+                      new((d.channels,), f32, D is not None), new(rows, ty, z is not None),
+                      new((d.channels,), f32, dt_bias is not None), new(state, f32, initial_state is not None))
+    workspace, wsp, wsb = _workspace(workspace, im2win_selective_scan_backward_workspace_bytes(d), x, stream)
+    im2win_selective_scan_backward(d, dyp, xp, dtp, ap, bp, cp, dp, zp, tbp, sp, ip, dfp,
+                                   *[None if v is None else v.data_ptr() for v in g], wsp, wsb, _stream(stream))
+    return g
 
 
 def selective_scan_step(x, dt, A, B, C, state, desc, D=None, z=None, dt_bias=None, slots=None, y=None, stream=None):

@@ -176,3 +176,21 @@ def test_scan_workspace_covers_every_plan():
         need = P.im2win_selective_scan_workspace_bytes(d)
         assert (need == 0) == (tokens <= 64)
         assert need <= (tokens / 32 + 1) * channels * (4 * 132) + tokens + 4096
+
+
+def test_scan_backward_refuses():
+    d = scan_desc(tokens=600, channels=16, ld_x=16, ld_dt=16, ld_z=16)
+    need = P.im2win_selective_scan_backward_workspace_bytes(d)
+    # dy x dt A B C D z dt_bias starts init d_final dx ddt dA dB dC dD dz ddt_bias d_init workspace
+    good = [FAKE] * 9 + [0] + [FAKE] * 12
+    for i in (0, 1, 2, 3, 4, 5, 12, 13, 14, 15, 16, 18, 21):
+        assert _code(P.im2win_selective_scan_backward, d, *[0 if j == i else v for j, v in enumerate(good)], need, 0) == P.IM2WIN_ENULL
+    for i in set(range(22)) - {9}:
+        assert _code(P.im2win_selective_scan_backward, d, *[v + 2 if j == i else v for j, v in enumerate(good)], need, 0) == P.IM2WIN_EALIGN
+    assert _code(P.im2win_selective_scan_backward, d, *good, need - 1, 0) == P.IM2WIN_EWORKSPACE
+    for field, value in (("states", 129), ("groups", 5), ("sequences", 7), ("dtype", 9), ("tokens", -4)):
+        bad = scan_desc(tokens=600, channels=16, ld_x=16, ld_dt=16, ld_z=16)
+        setattr(bad, field, value)
+        assert _code(P.im2win_selective_scan_backward, bad, *good, need, 0) == P.IM2WIN_EINVAL
+        if field != "sequences":     # with seq_starts 7 sequences may share 600 rows
+            assert _code(P.im2win_selective_scan_backward_workspace_bytes, bad) == P.IM2WIN_EINVAL
