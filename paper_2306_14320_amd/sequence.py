@@ -193,18 +193,23 @@ def _device_of(t, name):
     return dev
 
 
-def _rows(t, name, shape, dtype, ld, dev):
-    """Pointer of a T x ... input whose rows are ld elements apart."""
+def _matches(t, name, shape, dtype, dev):
+    """Raises unless t is a tensor of this shape and dtype on the device."""
     if not isinstance(t, torch.Tensor) or t.get_device() != dev:
         raise ValueError(f"{name} must be a tensor on device {dev}")
-    if tuple(t.shape) != shape:
+    if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs {shape}")
     if t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, the call needs {dtype}")
-    if shape[0] > 1 and _row_stride(t, name) != ld:
-        raise ValueError(f"{name} has rows {t.stride(0)} elements apart, the descriptor says {ld}")
-    if shape[0] == 1:
-        _row_stride(t, name)
+
+
+def _rows(t, name, shape, dtype, ld, dev):
+    """Pointer of a T x ... input whose rows are ld elements apart."""
+    _matches(t, name, shape, dtype, dev)
+    strides = t.stride()
+    if strides[-1] != 1 or strides[0] != ld or len(shape) > 2:     # the common case is settled
+        if _row_stride(t, name) != ld and shape[0] > 1:
+            raise ValueError(f"{name} has rows {strides[0]} elements apart, the descriptor says {ld}")
     return t.data_ptr()
 
 
@@ -212,29 +217,41 @@ def _dense(t, name, shape, dtype, dev):
     """Pointer of a contiguous tensor; None stays None."""
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.get_device() != dev or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous tensor on device {dev}")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs {shape}")
-    if t.dtype != dtype:
-        raise ValueError(f"{name} has dtype {t.dtype}, the call needs {dtype}")
+    _matches(t, name, shape, dtype, dev)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
+
+
+def _new(shape, dtype, like, stream):
+    """An output on the call's stream."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    return _empty(shape, dtype, like.device, stream)
 
 
 def _out(t, name, shape, dtype, like, dev, stream):
     """An output and its pointer: t, or a new tensor."""
     if t is None:
-        t = _empty(shape, dtype, like.device, stream)
+        t = _new(shape, dtype, like, stream)
+        return t, t.data_ptr()
     return t, _dense(t, name, shape, dtype, dev)
 
 
 def _workspace(ws, need, like, stream):
     """A workspace of at least `need` bytes, its pointer and size."""
     if ws is None:
-        ws = _empty((max(need, 16),), torch.uint8, like.device, stream)
+        if need == 0:
+            return None, None, 0
+        ws = _new((need,), torch.uint8, like, stream)
     elif not isinstance(ws, torch.Tensor) or ws.get_device() != like.get_device() or not ws.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the inputs' device")
     return ws, ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def _stream_on(stream, dev):
+    """The call's HIP stream: the device's current one unless one is given."""
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
 
 
 def causal_conv1d_desc_for(x, w, sequences=1, silu=True) -> im2win_conv1d_desc:
@@ -264,7 +281,7 @@ def causal_conv1d(x, w, desc, bias=None, seq_starts=None, initial_state=None, y=
     dev, dt, (xp, wp, bp, sp, ip) = _conv_inputs(x, w, bias, seq_starts, initial_state, desc)
     y, yp = _out(y, "y", (desc.tokens, desc.channels), dt, x, dev, stream)
     fp = _dense(final_state, "final_state", (desc.sequences, desc.width - 1, desc.channels), dt, dev)
-    im2win_causal_conv1d(desc, xp, wp, bp, sp, ip, yp, fp, _stream(stream))
+    im2win_causal_conv1d(desc, xp, wp, bp, sp, ip, yp, fp, _stream_on(stream, dev))
     return y
 
 
@@ -289,7 +306,7 @@ def causal_conv1d_backward(dy, x, w, desc, bias=None, seq_starts=None, initial_s
     dbias, dbp = (None, None) if bias is None else _out(None, "dbias", (d.channels,), torch.float32, x, dev, stream)
     di, dip = (None, None) if initial_state is None else _out(None, "d_initial_state", state, dt, x, dev, stream)
     workspace, wsp, wsb = _workspace(workspace, im2win_causal_conv1d_backward_workspace_bytes(d), x, stream)
-    im2win_causal_conv1d_backward(d, dyp, xp, wp, bp, sp, ip, dfp, dxp, dwp, dbp, dip, wsp, wsb, _stream(stream))
+    im2win_causal_conv1d_backward(d, dyp, xp, wp, bp, sp, ip, dfp, dxp, dwp, dbp, dip, wsp, wsb, _stream_on(stream, dev))
     return Conv1dGradients(dx, dw, dbias, di)
 
 
@@ -307,7 +324,7 @@ def causal_conv1d_step(x, w, state, desc, bias=None, slots=None, y=None, stream=
     stp = _dense(state, "state", (pool, desc.width - 1, desc.channels), dt, dev)
     slp = _dense(slots, "slots", (desc.tokens,), torch.int32, dev)
     y, yp = _out(y, "y", (desc.tokens, desc.channels), dt, x, dev, stream)
-    im2win_causal_conv1d_step(desc, xp, wp, bp, slp, stp, pool, yp, _stream(stream))
+    im2win_causal_conv1d_step(desc, xp, wp, bp, slp, stp, pool, yp, _stream_on(stream, dev))
     return y
 
 
@@ -342,7 +359,7 @@ def add_rms_norm(x, w, desc, residual=None, y=None, h=None, stream=None):
     of another type h is x."""
     dev, xp, wp, rp, h, hp = _norm_inputs(x, w, residual, h, desc, stream)
     y, yp = _out(y, "y", (desc.tokens, desc.channels), _torch_dtype(desc), x, dev, stream)
-    im2win_add_rms_norm(desc, xp, rp, wp, yp, hp, _stream(stream))
+    im2win_add_rms_norm(desc, xp, rp, wp, yp, hp, _stream_on(stream, dev))
     return y, h
 
 
@@ -353,7 +370,7 @@ def add_rms_norm_fp8(x, w, desc, residual=None, q=None, scales=None, h=None, str
     t, d = desc.tokens, desc.channels
     q, qp = _out(q, "q", (t, d), torch.float8_e4m3fn, x, dev, stream)
     scales, sp = _out(scales, "scales", (t, d // (desc.block or d)), torch.float32, x, dev, stream)
-    im2win_add_rms_norm_fp8(desc, xp, rp, wp, qp, sp, hp, _stream(stream))
+    im2win_add_rms_norm_fp8(desc, xp, rp, wp, qp, sp, hp, _stream_on(stream, dev))
     return q, scales, h
 
 
@@ -369,7 +386,7 @@ def add_rms_norm_backward(dy, h, w, desc, d_residual=None, dx=None, workspace=No
     dx, dxp = _out(dx, "dx", shape, rd, dy, dev, stream)
     dw, dwp = _out(None, "dw", (desc.channels,), torch.float32, dy, dev, stream)
     workspace, wsp, wsb = _workspace(workspace, im2win_add_rms_norm_backward_workspace_bytes(desc), dy, stream)
-    im2win_add_rms_norm_backward(desc, dyp, hp, wp, drp, dxp, dwp, wsp, wsb, _stream(stream))
+    im2win_add_rms_norm_backward(desc, dyp, hp, wp, drp, dxp, dwp, wsp, wsb, _stream_on(stream, dev))
     return dx, dw
 
 
@@ -414,7 +431,7 @@ def selective_scan(x, dt, A, B, C, desc, D=None, z=None, dt_bias=None, seq_start
     fp = _dense(final_state, "final_state", state, torch.float32, dev)
     y, yp = _out(y, "y", (d.tokens, d.channels), ty, x, dev, stream)
     workspace, wsp, wsb = _workspace(workspace, im2win_selective_scan_workspace_bytes(d), x, stream)
-    im2win_selective_scan(d, xp, dtp, ap, bp, cp, dp, zp, tbp, sp, ip, yp, fp, wsp, wsb, _stream(stream))
+    im2win_selective_scan(d, xp, dtp, ap, bp, cp, dp, zp, tbp, sp, ip, yp, fp, wsp, wsb, _stream_on(stream, dev))
     return y
 
 
@@ -443,7 +460,7 @@ def selective_scan_backward(dy, x, dt, A, B, C, desc, D=None, z=None, dt_bias=No
     dfp = _dense(d_final_state, "d_final_state", state, torch.float32, dev)
 
     def new(shape, dtype, wanted=True):
-        return _empty(shape, dtype, x.device, stream) if wanted else None
+        return _new(shape, dtype, x, stream) if wanted else None
 
     f32 = torch.float32
     g = ScanGradients(new(rows, ty), new(rows, ty), new((d.channels, d.states), f32), new(proj, ty), new(proj, ty),
@@ -451,7 +468,7 @@ def selective_scan_backward(dy, x, dt, A, B, C, desc, D=None, z=None, dt_bias=No
                       new((d.channels,), f32, dt_bias is not None), new(state, f32, initial_state is not None))
     workspace, wsp, wsb = _workspace(workspace, im2win_selective_scan_backward_workspace_bytes(d), x, stream)
     im2win_selective_scan_backward(d, dyp, xp, dtp, ap, bp, cp, dp, zp, tbp, sp, ip, dfp,
-                                   *[None if v is None else v.data_ptr() for v in g], wsp, wsb, _stream(stream))
+                                   *[None if v is None else v.data_ptr() for v in g], wsp, wsb, _stream_on(stream, dev))
     return g
 
 
@@ -467,5 +484,5 @@ def selective_scan_step(x, dt, A, B, C, state, desc, D=None, z=None, dt_bias=Non
     stp = _dense(state, "state", (pool, desc.channels, desc.states), torch.float32, dev)
     slp = _dense(slots, "slots", (desc.tokens,), torch.int32, dev)
     y, yp = _out(y, "y", (desc.tokens, desc.channels), ty, x, dev, stream)
-    im2win_selective_scan_step(desc, xp, dtp, ap, bp, cp, dp, zp, tbp, slp, stp, pool, yp, _stream(stream))
+    im2win_selective_scan_step(desc, xp, dtp, ap, bp, cp, dp, zp, tbp, slp, stp, pool, yp, _stream_on(stream, dev))
     return y
