@@ -17,9 +17,8 @@
  *    sequences of tokens / sequences rows each.  Rows before the first start
  *    and behind the last are neither read nor written.  Values outside of
  *    [0, tokens] are taken as the nearest of the two.
- *  - Pointers need the alignment of their element type only (wide loads are
- *    used where pointers, strides and sizes allow them); workspaces need 16
- *    bytes.
+ *  - Pointers need the alignment of their element type only; workspaces need
+ *    16 bytes.  Row strides stay below 2^28 elements.
  *  - Arrays of T rows may be NULL when tokens is 0.  Outputs must not overlap
  *    inputs or each other, except where an entry point says so.
  *  - "dtype" arrays hold im2win_dtype elements; every sum, state, statistic

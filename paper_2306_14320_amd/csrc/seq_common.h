@@ -54,46 +54,40 @@ inline SeqMap make_seq_map(int64_t tokens, int64_t sequences, const int32_t* sta
 }
 
 // ---------------------------------------------------------------------------
-// V consecutive elements, as fp32.  V > 1 means 16 bytes at a 16-byte aligned
-// address (4 floats, 8 bfloat16).
+// V consecutive elements: one, or 16 bytes of them (4 floats, 8 bfloat16) in
+// one access.  Addresses need the alignment of an element only: the hardware
+// takes 16 bytes from any address, and rows of an odd number of channels cost
+// 1.1 times the aligned ones instead of V accesses each.
 // ---------------------------------------------------------------------------
 template <typename T> constexpr int kVec = 16 / sizeof(T);
 
-template <int V>
-__device__ __forceinline__ void load_vec(const float* p, float (&v)[V]) {
-    if constexpr (V == 1) {
-        v[0] = p[0];
-    } else {
-        static_assert(V == 4, "16 bytes");
-        const float4 r = *reinterpret_cast<const float4*>(p);
-        v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w;
+// V elements as they lie in memory; get() converts, so that a load can stay
+// in flight until its value is used.
+template <typename T, int V>
+struct Bits {
+    static_assert(V == kVec<T>, "16 bytes");
+    uint32_t u[4];
+    __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(u, p, 16); }
+    __device__ __forceinline__ void zero() { u[0] = u[1] = u[2] = u[3] = 0; }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(u[i]);
+        else return __uint_as_float(i % 2 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
     }
-}
+};
+template <typename T>
+struct Bits<T, 1> {
+    T u;
+    __device__ __forceinline__ void load(const T* p) { u = *p; }
+    __device__ __forceinline__ void zero() { u = (T)0.0f; }
+    __device__ __forceinline__ float get(int) const { return (float)u; }
+};
 
-template <int V>
-__device__ __forceinline__ void load_vec(const bf16* p, float (&v)[V]) {
-    if constexpr (V == 1) {
-        v[0] = (float)p[0];
-    } else {
-        static_assert(V == 8, "16 bytes");
-        const uint4 r = *reinterpret_cast<const uint4*>(p);
-        const uint32_t u[4] = {r.x, r.y, r.z, r.w};
+template <int V, typename T>
+__device__ __forceinline__ void load_vec(const T* p, float (&v)[V]) {
+    Bits<T, V> r;
+    r.load(p);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            v[2 * i] = __uint_as_float(u[i] << 16);
-            v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
-        }
-    }
-}
-
-template <int V>
-__device__ __forceinline__ void store_vec(float* p, const float (&v)[V]) {
-    if constexpr (V == 1) {
-        p[0] = v[0];
-    } else {
-        static_assert(V == 4, "16 bytes");
-        *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    }
+    for (int i = 0; i < V; ++i) v[i] = r.get(i);
 }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
@@ -102,26 +96,30 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 }
 
 template <int V>
+__device__ __forceinline__ void store_vec(float* p, const float (&v)[V]) {
+    __builtin_memcpy(p, v, V * sizeof(float));
+}
+
+template <int V>
 __device__ __forceinline__ void store_vec(bf16* p, const float (&v)[V]) {
     if constexpr (V == 1) {
         p[0] = (bf16)v[0];
     } else {
-        static_assert(V == 8, "16 bytes");
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]),
-                                                  pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+        const uint32_t u[4] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        __builtin_memcpy(p, u, 16);
     }
 }
 
-// fp32 arrays of a multiple of four, on 16-byte boundaries when V > 1
-template <int V>
-__device__ __forceinline__ void store_f32(float* p, const float (&v)[V]) {
-    if constexpr (V % 4 == 0) {
+// N consecutive values, a multiple of the vector width
+template <int N, typename T>
+__device__ __forceinline__ void store_run(T* p, const float (&v)[N]) {
+    static_assert(N % kVec<T> == 0, "whole vectors");
 #pragma unroll
-        for (int i = 0; i < V; i += 4)
-            *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
-    } else {
+    for (int i = 0; i < N; i += kVec<T>) {
+        float w[kVec<T>];
 #pragma unroll
-        for (int i = 0; i < V; ++i) p[i] = v[i];
+        for (int j = 0; j < kVec<T>; ++j) w[j] = v[i + j];
+        store_vec<kVec<T>>(p + i, w);
     }
 }
 
@@ -169,11 +167,13 @@ inline int check_sequences(int64_t tokens, int64_t sequences, const int32_t* sta
     return may_ptr(starts, 4, "seq_starts");
 }
 
-// Row strides stay below 2^31 elements, so that a row times its stride, in bytes, fits 64 bits.
+// Row strides: four rows' bytes fit 32 bits, as the kernels' offsets inside such a group do.
+constexpr int64_t kMaxStride = int64_t(1) << 28;
+
 inline int check_ld(int64_t ld, int64_t width, const char* name) {
     if (ld < width)
         return fail(IM2WIN_EINVAL, "%s is %lld, less than the row's %lld elements", name, (long long)ld, (long long)width);
-    if (ld > (int64_t(1) << 31) - 1) return fail(IM2WIN_EOVERFLOW, "%s (%lld) exceeds 2^31 - 1", name, (long long)ld);
+    if (ld > kMaxStride - 1) return fail(IM2WIN_EOVERFLOW, "%s (%lld) reaches 2^28", name, (long long)ld);
     return IM2WIN_OK;
 }
 

@@ -17,7 +17,8 @@ struct Conv1dArgs {
     SeqMap seq;
     int64_t ld_x;
     int channels;
-    int tiles;          // token tiles; rows of grid.x behind them write final states
+    int tiles;          // token tiles; tiles behind them write final states
+    int groups;         // workgroups beside one another that cover a row
     int silu;
 };
 
@@ -32,10 +33,7 @@ struct Taps {
     __device__ void load(const T* wp, const T* bp, int c) {
         float flat[W][V];
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if constexpr (V > 1) load_vec<V>(wp + (int64_t)c * W + i * V, flat[i]);
-            else flat[i][0] = (float)wp[(int64_t)c * W + i];
-        }
+        for (int i = 0; i < W; ++i) load_vec<V>(wp + (int64_t)c * W + i * V, flat[i]);
 #pragma unroll
         for (int k = 0; k < W; ++k)
 #pragma unroll
@@ -63,15 +61,25 @@ __device__ __forceinline__ void load_input(const T* x, const T* init, int64_t ld
     }
 }
 
-// One wave: kConvTile rows of 64*V channels.
+// The first of a lane's V channels.  Lanes past the last V channels take those
+// (several lanes then compute and store the same values) or none.
+template <int V>
+__device__ __forceinline__ bool lane_channels(int group, int lane, int channels, int* c) {
+    const int own = (group * kWave + lane) * V;
+    *c = min(own, channels - V);
+    return own < channels;
+}
+
+// One wave: kConvTile rows of 64*V channels.  Bound by memory: each wave has
+// all its rows' loads in flight before it uses the first.
 template <typename T, int V, int W>
 __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_kernel(Conv1dArgs a) {
     const T* x = static_cast<const T*>(a.x);
     const T* init = static_cast<const T*>(a.init);
     T* y = static_cast<T*>(a.y);
-    const int64_t tile = (int64_t)blockIdx.x * kConvWaves + uniform(threadIdx.x / kWave);
-    const int c = ((int)blockIdx.y * kWave + (int)(threadIdx.x % kWave)) * V;
-    if (c >= a.channels) return;
+    const int64_t tile = (int64_t)(blockIdx.x / a.groups) * kConvWaves + uniform(threadIdx.x / kWave);
+    int c;
+    if (!lane_channels<V>(blockIdx.x % a.groups, threadIdx.x % kWave, a.channels, &c)) return;
 
     if (tile >= a.tiles) {
         // one row of a final state: input e of the sequence with its W-1 earlier ones in front
@@ -104,24 +112,19 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_kernel(Conv1dArgs a
 
     if (lo == t0 && hi == t0 + kConvTile && end >= hi && lo - first >= W - 1) {
         // the tile and the rows before it lie in one sequence
-        float win[W][V];
+        Bits<T, V> in[kConvTile + W - 1];
         const T* p = x + (int64_t)(t0 - (W - 1)) * a.ld_x + c;
 #pragma unroll
-        for (int j = 0; j < W - 1; ++j, p += a.ld_x) load_vec<V>(p, win[j]);
+        for (int i = 0; i < kConvTile + W - 1; ++i, p += a.ld_x) in[i].load(p);
 #pragma unroll
-        for (int i = 0; i < kConvTile; ++i, p += a.ld_x) {
-            load_vec<V>(p, win[W - 1]);
+        for (int i = 0; i < kConvTile; ++i) {
             float acc[V];
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 acc[v] = taps.bias[v];
 #pragma unroll
-                for (int k = 0; k < W; ++k) acc[v] = fmaf(taps.w[k][v], win[k][v], acc[v]);
+                for (int k = 0; k < W; ++k) acc[v] = fmaf(taps.w[k][v], in[i + k].get(v), acc[v]);
             }
-#pragma unroll
-            for (int k = 0; k + 1 < W; ++k)
-#pragma unroll
-                for (int v = 0; v < V; ++v) win[k][v] = win[k + 1][v];
             finish(t0 + i, acc);
         }
         return;
@@ -164,12 +167,13 @@ struct Conv1dBwdArgs {
     const void* d_final;
     void* dx;
     void* d_init;
-    float* part;        // [gridDim.x][W + 1][channels]
+    float* part;        // [parts][W + 1][channels]
     float* dw;
     float* dbias;
     SeqMap seq;
     int64_t ld_x;
     int channels;
+    int groups;
     int silu;
     int parts;
 };
@@ -195,15 +199,15 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_bwd_kernel(Conv1dBw
     const T* d_final = static_cast<const T*>(a.d_final);
     T* dx = static_cast<T*>(a.dx);
     const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-    const int c_own = ((int)blockIdx.y * kWave + lane) * V;
-    const bool live = c_own < a.channels;
-    const int c = live ? c_own : 0;          // lanes past the last channel compute the first and store nothing
+    int c;
+    const bool live = lane_channels<V>(blockIdx.x % a.groups, lane, a.channels, &c);
+    const int part = blockIdx.x / a.groups;
 
     Taps<T, V, W> taps;
     taps.load(static_cast<const T*>(a.w), static_cast<const T*>(a.bias), c);
     float dw[W + 1][V] = {};                 // the last row is dbias
 
-    const int64_t s0 = ((int64_t)blockIdx.x * kConvWaves + wave) * kConvStripe;
+    const int64_t s0 = ((int64_t)part * kConvWaves + wave) * kConvStripe;
     const int lo = (int)max<int64_t>(a.seq.first(0), s0);
     const int hi = (int)min<int64_t>(a.seq.first(a.seq.count), s0 + kConvStripe);
     for (int t = lo; t < hi;) {
@@ -214,49 +218,92 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_bwd_kernel(Conv1dBw
 #pragma unroll
         for (int j = 0; j < W - 1; ++j)
             load_input<T, V, W>(x, init, a.ld_x, a.channels, b, first, t, W - 1 - j, c, win[j]);
-        for (int r = t; r < own + W - 1; ++r) {
+
+        // g of row r, with its window; r's own sums where `mine`
+        auto row = [&](const Bits<T, V>& xr, const Bits<T, V>& dyr, bool mine) {
+            float s[V];
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                win[W - 1][v] = xr.get(v);
+                g[W - 1][v] = dyr.get(v);
+                s[v] = taps.bias[v];
+#pragma unroll
+                for (int k = 0; k < W; ++k) s[v] = fmaf(taps.w[k][v], win[k][v], s[v]);
+            }
+            times_slope<V>(g[W - 1], s, a.silu);
+            if (mine) {
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    dw[W][v] += g[W - 1][v];
+#pragma unroll
+                    for (int k = 0; k < W; ++k) dw[k][v] = fmaf(g[W - 1][v], win[k][v], dw[k][v]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k + 1 < W; ++k)
+#pragma unroll
+                for (int v = 0; v < V; ++v) win[k][v] = win[k + 1][v];
+        };
+        auto shift = [&]() {
 #pragma unroll
             for (int k = 0; k + 1 < W; ++k)
 #pragma unroll
                 for (int v = 0; v < V; ++v) g[k][v] = g[k + 1][v];
+        };
+        // dx of row u, whose gradient and the W-1 behind it are in g
+        auto put = [&](int u) {
+            if (u < t) return;
+            float d[V] = {};
+            if (d_final && u >= end - (W - 1))
+                load_vec<V>(d_final + ((int64_t)b * (W - 1) + (u - (end - (W - 1)))) * a.channels + c, d);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int k = 0; k < W; ++k) d[v] = fmaf(taps.w[k][v], g[W - 1 - k][v], d[v]);
+            if (live) store_vec<V>(dx + (int64_t)u * a.channels + c, d);
+        };
+
+        // the stripe's rows, kBatch of them loaded while the ones before are worked on
+        constexpr int kBatch = 4;
+        Bits<T, V> nx[kBatch], ng[kBatch];
+        auto fetch = [&](int r) {
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int64_t at = min(r + i, own - 1);
+                nx[i].load(x + at * a.ld_x + c);
+                ng[i].load(dy + at * a.channels + c);
+            }
+        };
+        fetch(t);
+        for (int r = t; r < own; r += kBatch) {
+            Bits<T, V> cx[kBatch], cg[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                cx[i] = nx[i];
+                cg[i] = ng[i];
+            }
+            if (r + kBatch < own) fetch(r + kBatch);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                if (r + i >= own) break;
+                shift();
+                row(cx[i], cg[i], true);
+                put(r + i - (W - 1));
+            }
+        }
+        // the rows behind, which the last W-1 of the stripe reach
+        for (int r = own; r < own + W - 1; ++r) {
+            shift();
             if (r < end) {
-                load_vec<V>(x + (int64_t)r * a.ld_x + c, win[W - 1]);
-                load_vec<V>(dy + (int64_t)r * a.channels + c, g[W - 1]);
-                float s[V];
-#pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    s[v] = taps.bias[v];
-#pragma unroll
-                    for (int k = 0; k < W; ++k) s[v] = fmaf(taps.w[k][v], win[k][v], s[v]);
-                }
-                times_slope<V>(g[W - 1], s, a.silu);
-                if (r < own) {
-#pragma unroll
-                    for (int v = 0; v < V; ++v) {
-                        dw[W][v] += g[W - 1][v];
-#pragma unroll
-                        for (int k = 0; k < W; ++k) dw[k][v] = fmaf(g[W - 1][v], win[k][v], dw[k][v]);
-                    }
-                }
-#pragma unroll
-                for (int k = 0; k + 1 < W; ++k)
-#pragma unroll
-                    for (int v = 0; v < V; ++v) win[k][v] = win[k + 1][v];
+                Bits<T, V> xr, gr;
+                xr.load(x + (int64_t)r * a.ld_x + c);
+                gr.load(dy + (int64_t)r * a.channels + c);
+                row(xr, gr, false);
             } else {
 #pragma unroll
                 for (int v = 0; v < V; ++v) g[W - 1][v] = 0.0f;
             }
-            const int u = r - (W - 1);       // g[m] is the gradient of row u + m
-            if (u >= t) {
-                float d[V] = {};
-                if (d_final && u >= end - (W - 1))
-                    load_vec<V>(d_final + ((int64_t)b * (W - 1) + (u - (end - (W - 1)))) * a.channels + c, d);
-#pragma unroll
-                for (int v = 0; v < V; ++v)
-#pragma unroll
-                    for (int k = 0; k < W; ++k) d[v] = fmaf(taps.w[k][v], g[W - 1 - k][v], d[v]);
-                if (live) store_vec<V>(dx + (int64_t)u * a.channels + c, d);
-            }
+            put(r - (W - 1));
         }
         t = own;
     }
@@ -276,24 +323,29 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_bwd_kernel(Conv1dBw
 #pragma unroll
                 for (int i = 1; i < kConvWaves; ++i) s[v] += sum[i][lane][v];
             }
-            store_f32<V>(a.part + ((int64_t)blockIdx.x * (W + 1) + k) * a.channels + c, s);
+            store_vec<V>(a.part + ((int64_t)part * (W + 1) + k) * a.channels + c, s);
         }
     }
 }
 
-// dw and dbias from the workgroups' sums: a wave for 64 channels of one tap
-__global__ __launch_bounds__(kConvWaves * kWave) void conv1d_bwd_sum_kernel(Conv1dBwdArgs a, int width) {
-    __shared__ float sum[kConvWaves][kWave];
+constexpr int kSumWaves = 8;
+
+// dw and dbias from the workgroups' sums: 64 channels of one tap per workgroup,
+// every eighth sum per wave, eight loads in flight
+__global__ __launch_bounds__(kSumWaves * kWave) void conv1d_bwd_sum_kernel(Conv1dBwdArgs a, int width) {
+    __shared__ float sum[kSumWaves][kWave];
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int c = (int)blockIdx.x * kWave + lane, k = blockIdx.y;
     float s = 0.0f;
-    if (c < a.channels)
-        for (int i = wave; i < a.parts; i += kConvWaves)
+    if (c < a.channels) {
+#pragma unroll 8
+        for (int i = wave; i < a.parts; i += kSumWaves)
             s += a.part[((int64_t)i * (width + 1) + k) * a.channels + c];
+    }
     sum[wave][lane] = s;
     __syncthreads();
     if (wave == 0 && c < a.channels) {
-        for (int i = 1; i < kConvWaves; ++i) s += sum[i][lane];
+        for (int i = 1; i < kSumWaves; ++i) s += sum[i][lane];
         if (k < width) a.dw[(int64_t)c * width + k] = s;
         else if (a.dbias) a.dbias[c] = s;
     }
@@ -391,15 +443,10 @@ int check_desc(const im2win_conv1d_desc* d) {
 
 size_t elem_of(const im2win_conv1d_desc* d) { return d->dtype == IM2WIN_F32 ? 4 : 2; }
 
-// Whether rows of 16-byte vectors can be read and written: every base, row
-// stride and the row itself is whole vectors.
-bool whole_vectors(const im2win_conv1d_desc* d, std::initializer_list<const void*> ptrs) {
-    const size_t e = elem_of(d);
-    if (d->channels * e % 16 || d->ld_x * e % 16) return false;
-    for (const void* p : ptrs)
-        if (!aligned_to(p, 16)) return false;
-    return true;
-}
+// Lanes of 16 bytes each need as many channels; the step, which reads and
+// writes its state in place, also that no two lanes share a channel.
+bool vectors(const im2win_conv1d_desc* d) { return d->channels * elem_of(d) >= 16; }
+bool whole_vectors(const im2win_conv1d_desc* d) { return d->channels * elem_of(d) % 16 == 0; }
 
 int64_t channel_groups(int64_t channels, int v) { return (channels + kWave * v - 1) / (kWave * v); }
 
@@ -421,7 +468,7 @@ void with_width(int64_t w, F f) {
     }
 }
 
-// f(type, vector width, taps) for the call's element type, alignment and width
+// f(type, vector width, taps) for the call's element type, channels and width
 template <typename F>
 void with_kernel(const im2win_conv1d_desc* d, bool vec, F f) {
     with_width(d->width, [&](auto w) {
@@ -460,13 +507,16 @@ int im2win_causal_conv1d(const im2win_conv1d_desc* d, const void* x, const void*
     const int64_t rows = a.tiles + (final_state ? d->sequences * (d->width - 1) : 0);
     if (rows == 0) return ok();
     const int64_t blocks = (rows + kConvWaves - 1) / kConvWaves;
-    if (blocks > (int64_t(1) << 31) - 1) return fail(IM2WIN_EOVERFLOW, "too many sequences (%lld)", (long long)d->sequences);
-    const bool vec = whole_vectors(d, {x, w, bias, initial_state, y, final_state});
+    const bool vec = vectors(d);
+    a.groups = (int)channel_groups(d->channels, vec ? (int)(16 / e) : 1);
+    if (blocks * a.groups > (int64_t(1) << 31) - 1)
+        return fail(IM2WIN_EOVERFLOW, "too many tokens, sequences and channels (%lld, %lld, %lld)", (long long)d->tokens,
+                    (long long)d->sequences, (long long)d->channels);
     with_kernel(d, vec, [&](auto t, auto v, auto taps) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value, W = decltype(taps)::value;
-        hipLaunchKernelGGL((conv1d_kernel<T, V, W>), dim3((unsigned)blocks, (unsigned)channel_groups(d->channels, V)),
-                           dim3(kConvWaves * kWave), 0, static_cast<hipStream_t>(stream), a);
+        hipLaunchKernelGGL((conv1d_kernel<T, V, W>), dim3((unsigned)(blocks * a.groups)), dim3(kConvWaves * kWave), 0,
+                           static_cast<hipStream_t>(stream), a);
     });
     return launched("causal_conv1d");
 }
@@ -506,13 +556,15 @@ int im2win_causal_conv1d_backward(const im2win_conv1d_desc* d, const void* dy, c
     a.seq = make_seq_map(d->tokens, d->sequences, seq_starts);
     a.ld_x = d->ld_x; a.channels = (int)d->channels; a.silu = d->silu != 0; a.parts = (int)blocks;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool vec = whole_vectors(d, {dy, x, w, bias, initial_state, d_final_state, dx});
+    const bool vec = vectors(d);
+    a.groups = (int)channel_groups(d->channels, vec ? (int)(16 / e) : 1);
+    if (blocks * a.groups > (int64_t(1) << 31) - 1)
+        return fail(IM2WIN_EOVERFLOW, "too many tokens and channels (%lld, %lld)", (long long)d->tokens, (long long)d->channels);
     with_kernel(d, vec, [&](auto t, auto v, auto taps) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value, W = decltype(taps)::value;
         if (blocks)
-            hipLaunchKernelGGL((conv1d_bwd_kernel<T, V, W>),
-                               dim3((unsigned)blocks, (unsigned)channel_groups(d->channels, V)),
+            hipLaunchKernelGGL((conv1d_bwd_kernel<T, V, W>), dim3((unsigned)(blocks * a.groups)),
                                dim3(kConvWaves * kWave), 0, s, a);
     });
     if (states)
@@ -526,7 +578,7 @@ int im2win_causal_conv1d_backward(const im2win_conv1d_desc* d, const void* dy, c
         });
     hipLaunchKernelGGL(conv1d_bwd_sum_kernel,
                        dim3((unsigned)((d->channels + kWave - 1) / kWave), (unsigned)(d->width + 1)),
-                       dim3(kConvWaves * kWave), 0, s, a, (int)d->width);
+                       dim3(kSumWaves * kWave), 0, s, a, (int)d->width);
     return launched("causal_conv1d_backward");
 }
 
@@ -544,7 +596,7 @@ int im2win_causal_conv1d_step(const im2win_conv1d_desc* d, const void* x, const 
     Conv1dStepArgs a{};
     a.x = x; a.w = w; a.bias = bias; a.slots = slots; a.state = state; a.y = y; a.state_slots = state_slots;
     a.ld_x = d->ld_x; a.channels = (int)d->channels; a.silu = d->silu != 0;
-    const bool vec = whole_vectors(d, {x, w, bias, state, y});
+    const bool vec = whole_vectors(d);
     with_kernel(d, vec, [&](auto t, auto v, auto taps) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value, W = decltype(taps)::value;

@@ -23,41 +23,58 @@ struct NormArgs {
     float inv_d;
 };
 
-// Eight consecutive elements of which the first `n` exist; VEC: all eight do,
-// and p is a multiple of 16 bytes.
-template <bool VEC>
-__device__ __forceinline__ void load8(const float* p, int n, float (&v)[kPer]) {
-    if constexpr (VEC) {
-        const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-        v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
+// Eight consecutive elements of which the first `n` exist, as they lie in
+// memory: one or two 16-byte loads at any address, and element by element for
+// the last thread of a row whose channels are no multiple of eight.  get()
+// converts, so that the loads of several arrays are in flight together.
+template <typename T>
+struct Eight {
+    Bits<T, kVec<T>> r[kPer / kVec<T>];
+
+    __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) v[i] = i < n ? p[i] : 0.0f;
+        for (int i = 0; i < kPer / kVec<T>; ++i) r[i].load(p + i * kVec<T>);
+    }
+    __device__ __forceinline__ void load(const T* p, int n) {
+        T e[kPer];
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) e[i] = i < n ? p[i] : (T)0.0f;
+#pragma unroll
+        for (int i = 0; i < kPer / kVec<T>; ++i) __builtin_memcpy(r[i].u, e + i * kVec<T>, 16);
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < kPer / kVec<T>; ++i) r[i].zero();
+    }
+    __device__ __forceinline__ float get(int i) const { return r[i / kVec<T>].get(i % kVec<T>); }
+};
+
+// The same eight channels of up to three arrays
+template <typename A, typename B, typename C>
+__device__ __forceinline__ void load8(int n, Eight<A>& a, const A* pa, Eight<B>& b, const B* pb, Eight<C>& c, const C* pc, bool have_c) {
+    a.zero();
+    b.zero();
+    c.zero();
+    if (n >= kPer) {
+        a.load(pa);
+        b.load(pb);
+        if (have_c) c.load(pc);
+    } else if (n > 0) {
+        a.load(pa, n);
+        b.load(pb, n);
+        if (have_c) c.load(pc, n);
     }
 }
-template <bool VEC>
-__device__ __forceinline__ void load8(const bf16* p, int n, float (&v)[kPer]) {
-    if constexpr (VEC) load_vec<kPer>(p, v);
-    else
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
-}
-template <bool VEC>
-__device__ __forceinline__ void store8(float* p, int n, const float (&v)[kPer]) {
-    if constexpr (VEC) store_f32<kPer>(p, v);
-    else
+
+template <typename T>
+__device__ __forceinline__ void store8(T* p, int n, const float (&v)[kPer]) {
+    if (n >= kPer) {
+        store_run<kPer>(p, v);
+    } else {
 #pragma unroll
         for (int i = 0; i < kPer; ++i)
-            if (i < n) p[i] = v[i];
-}
-template <bool VEC>
-__device__ __forceinline__ void store8(bf16* p, int n, const float (&v)[kPer]) {
-    if constexpr (VEC) store_vec<kPer>(p, v);
-    else
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (i < n) p[i] = (bf16)v[i];
+            if (i < n) p[i] = (T)v[i];
+    }
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
@@ -107,7 +124,7 @@ __device__ __forceinline__ uint32_t pack_fp8(float a, float b, float c, float d)
 
 // TX: x and y.  TR: residual and h.  NT threads, NV steps of eight channels
 // per thread (NT * NV * 8 >= channels).
-template <typename TX, typename TR, int NT, int NV, bool VEC, bool FP8>
+template <typename TX, typename TR, int NT, int NV, bool FP8>
 __global__ __launch_bounds__(NT) void add_rms_norm_kernel(NormArgs a) {
     __shared__ float part[NT / kWave];
     __shared__ uint32_t top_part[NT / kWave];
@@ -115,41 +132,39 @@ __global__ __launch_bounds__(NT) void add_rms_norm_kernel(NormArgs a) {
     const TX* x = static_cast<const TX*>(a.x) + row * a.ld_x;
     const TR* res = static_cast<const TR*>(a.res) + row * a.channels;
     TR* h = static_cast<TR*>(a.h) + row * a.channels;
-    float v[NV][kPer], w[NV][kPer];
+    Eight<TX> xr[NV];
+    Eight<float> w[NV];
+    Eight<TR> rr[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        const int c = (j * NT + (int)threadIdx.x) * kPer;
+        load8(a.channels - c, xr[j], x + c, w[j], a.w + c, rr[j], res + c, a.res != nullptr);
+    }
+    float v[NV][kPer];
     float ss = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int c = (j * NT + (int)threadIdx.x) * kPer, n = a.channels - c;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) v[j][i] = w[j][i] = 0.0f;
-        if (n <= 0) continue;
-        load8<VEC>(x + c, n, v[j]);
-        load8<VEC>(a.w + c, n, w[j]);
-        if (a.res) {
-            float r[kPer];
-            load8<VEC>(res + c, n, r);
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) v[j][i] += r[i];
+        for (int i = 0; i < kPer; ++i) {
+            v[j][i] = xr[j].get(i) + rr[j].get(i);
+            if constexpr (sizeof(TR) == 2) v[j][i] = (float)(TR)v[j][i];   // the norm is that of h as it is kept
+            ss = fmaf(v[j][i], v[j][i], ss);
         }
-        if constexpr (sizeof(TR) == 2)   // the norm is that of h as it is kept
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) v[j][i] = (float)(TR)v[j][i];
-        if (a.h) store8<VEC>(h + c, n, v[j]);
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) ss = fmaf(v[j][i], v[j][i], ss);
+        if (a.h && n > 0) store8(h + c, n, v[j]);
     }
     const float r = 1.0f / sqrtf(fmaf(block_sum<NT>(ss, part), a.inv_d, a.eps));
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) v[j][i] = v[j][i] * r * w[j][i];
+        for (int i = 0; i < kPer; ++i) v[j][i] = v[j][i] * r * w[j].get(i);
 
     if constexpr (!FP8) {
         TX* y = static_cast<TX*>(a.y) + row * a.channels;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * NT + (int)threadIdx.x) * kPer, n = a.channels - c;
-            if (n > 0) store8<VEC>(y + c, n, v[j]);
+            if (n > 0) store8(y + c, n, v[j]);
         }
     } else {
         uint8_t* q = static_cast<uint8_t*>(a.y) + row * a.channels;
@@ -189,8 +204,9 @@ __global__ __launch_bounds__(NT) void add_rms_norm_kernel(NormArgs a) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) s[i] = v[j][i] / scale;
             const uint32_t lo = pack_fp8(s[0], s[1], s[2], s[3]), hi = pack_fp8(s[4], s[5], s[6], s[7]);
-            if constexpr (VEC) {
-                *reinterpret_cast<uint2*>(q + c) = make_uint2(lo, hi);
+            if (n >= kPer) {
+                const uint32_t both[2] = {lo, hi};
+                __builtin_memcpy(q + c, both, 8);
             } else {
 #pragma unroll
                 for (int i = 0; i < kPer; ++i)
@@ -220,35 +236,37 @@ struct NormBwdArgs {
     float inv_d;
 };
 
-template <typename TX, typename TR, int NT, int NV, bool VEC>
+template <typename TX, typename TR, int NT, int NV>
 __global__ __launch_bounds__(NT) void add_rms_norm_bwd_kernel(NormBwdArgs a) {
     __shared__ float part[2][2][NT / kWave];
-    float dw[NV][kPer] = {}, w[NV][kPer] = {};
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-        const int c = (j * NT + (int)threadIdx.x) * kPer, n = a.channels - c;
-        if (n > 0) load8<VEC>(a.w + c, n, w[j]);
-    }
+    float dw[NV][kPer] = {};
     int turn = 0;
     for (int64_t row = blockIdx.x; row < a.tokens; row += gridDim.x, turn ^= 1) {
         const TX* dy = static_cast<const TX*>(a.dy) + row * a.channels;
         const TR* h = static_cast<const TR*>(a.h) + row * a.channels;
-        float g[NV][kPer], v[NV][kPer];
+        const TR* dres = static_cast<const TR*>(a.dres) + row * a.channels;
+        Eight<TX> g[NV];
+        Eight<float> w[NV];
+        Eight<TR> v[NV], d0[NV];
         float ss = 0.0f, gh = 0.0f;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            const int c = (j * NT + (int)threadIdx.x) * kPer, n = a.channels - c;
+            const int c = (j * NT + (int)threadIdx.x) * kPer;
+            load8(a.channels - c, g[j], dy + c, v[j], h + c, d0[j], dres + c, a.dres != nullptr);
+        }
 #pragma unroll
-            for (int i = 0; i < kPer; ++i) g[j][i] = v[j][i] = 0.0f;
-            if (n <= 0) continue;
-            load8<VEC>(dy + c, n, g[j]);
-            load8<VEC>(h + c, n, v[j]);
+        for (int j = 0; j < NV; ++j) {
+            const int c = (j * NT + (int)threadIdx.x) * kPer;
+            Eight<float> none;
+            load8(a.channels - c, w[j], a.w + c, none, a.w + c, none, a.w, false);
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                ss = fmaf(v[j][i], v[j][i], ss);
-                gh = fmaf(g[j][i] * w[j][i], v[j][i], gh);
+                ss = fmaf(v[j].get(i), v[j].get(i), ss);
+                gh = fmaf(g[j].get(i) * w[j].get(i), v[j].get(i), gh);
             }
-        }
         // two arrays of partial sums in turn: a wave that is a row ahead writes the other one, and
         // it cannot be two ahead, as every row has a barrier
         ss = wave_sum(ss);
@@ -269,39 +287,40 @@ __global__ __launch_bounds__(NT) void add_rms_norm_bwd_kernel(NormBwdArgs a) {
         }
         const float r = 1.0f / sqrtf(fmaf(ss, a.inv_d, a.eps));
         const float k = r * r * gh * a.inv_d;
-        const TR* dres = static_cast<const TR*>(a.dres) + row * a.channels;
         TR* dx = static_cast<TR*>(a.dx) + row * a.channels;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const int c = (j * NT + (int)threadIdx.x) * kPer, n = a.channels - c;
-            if (n <= 0) continue;
-            float d[kPer] = {};
-            if (a.dres) load8<VEC>(dres + c, n, d);
+            float d[kPer];
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                d[i] = fmaf(r, fmaf(-k, v[j][i], g[j][i] * w[j][i]), d[i]);
-                dw[j][i] = fmaf(g[j][i] * r, v[j][i], dw[j][i]);
+                const float gi = g[j].get(i), hi = v[j].get(i);
+                d[i] = fmaf(r, fmaf(-k, hi, gi * w[j].get(i)), d0[j].get(i));
+                dw[j][i] = fmaf(gi * r, hi, dw[j][i]);
             }
-            store8<VEC>(dx + c, n, d);
+            if (n > 0) store8(dx + c, n, d);
         }
     }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
         const int c = (j * NT + (int)threadIdx.x) * kPer, n = a.channels - c;
-        if (n > 0) store8<VEC>(a.part + (int64_t)blockIdx.x * a.channels + c, n, dw[j]);
+        if (n > 0) store8(a.part + (int64_t)blockIdx.x * a.channels + c, n, dw[j]);
     }
 }
 
-constexpr int kSumWaves = 4;
+constexpr int kSumWaves = 16;
 
-// dw from the workgroups' sums: 64 channels per workgroup, each wave a run of rows
+// dw from the workgroups' sums: 64 channels per workgroup, every 16th row per
+// wave, eight rows' loads in flight
 __global__ __launch_bounds__(kSumWaves * kWave) void add_rms_norm_bwd_sum_kernel(NormBwdArgs a) {
     __shared__ float sum[kSumWaves][kWave];
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int c = (int)blockIdx.x * kWave + lane;
     float s = 0.0f;
-    if (c < a.channels)
+    if (c < a.channels) {
+#pragma unroll 8
         for (int i = wave; i < a.blocks; i += kSumWaves) s += a.part[(int64_t)i * a.channels + c];
+    }
     sum[wave][lane] = s;
     __syncthreads();
     if (wave == 0 && c < a.channels) {
@@ -337,12 +356,6 @@ int check_desc(const im2win_norm_desc* d) {
 
 size_t size_of(int32_t dtype) { return dtype == IM2WIN_F32 ? 4 : 2; }
 
-bool all_aligned(std::initializer_list<const void*> ptrs) {
-    for (const void* p : ptrs)
-        if (!aligned_to(p, 16)) return false;
-    return true;
-}
-
 // f(threads, steps): the smallest workgroup that holds the row.  A wave per
 // row up to 512 channels, then 256 threads of one to four steps, then 1024
 // of two (16384 channels, what their registers hold beside dw).
@@ -357,17 +370,13 @@ void with_shape(int64_t channels, F f) {
 }
 
 template <typename F>
-void with_types(const im2win_norm_desc* d, bool vec, F f) {
-    auto with_vec = [&](auto tx, auto tr) {
-        if (vec) f(tx, tr, std::true_type{});
-        else f(tx, tr, std::false_type{});
-    };
+void with_types(const im2win_norm_desc* d, F f) {
     if (d->dtype == IM2WIN_F32) {
-        if (d->residual_dtype == IM2WIN_F32) with_vec(float{}, float{});
-        else with_vec(float{}, bf16{});
+        if (d->residual_dtype == IM2WIN_F32) f(float{}, float{});
+        else f(float{}, bf16{});
     } else {
-        if (d->residual_dtype == IM2WIN_F32) with_vec(bf16{}, float{});
-        else with_vec(bf16{}, bf16{});
+        if (d->residual_dtype == IM2WIN_F32) f(bf16{}, float{});
+        else f(bf16{}, bf16{});
     }
 }
 
@@ -389,14 +398,12 @@ int forward(const im2win_norm_desc* d, const void* x, const void* residual, cons
     a.x = x; a.res = residual; a.w = w; a.y = y; a.scales = scales; a.h = h;
     a.ld_x = d->ld_x; a.channels = (int)d->channels; a.block = (int)d->block;
     a.eps = d->eps; a.inv_d = 1.0f / (float)d->channels;
-    // every thread's eight channels exist, and lie on 16-byte boundaries (8 for the bytes of q)
-    const bool vec = d->channels % kPer == 0 && d->ld_x % kPer == 0 && all_aligned({x, residual, w, y, h});
-    with_types(d, vec, [&](auto tx, auto tr, auto v) {
+    with_types(d, [&](auto tx, auto tr) {
         with_shape(d->channels, [&](auto nt, auto nv) {
             using TX = decltype(tx);
             using TR = decltype(tr);
             constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-            hipLaunchKernelGGL((add_rms_norm_kernel<TX, TR, NT, NV, decltype(v)::value, FP8>),
+            hipLaunchKernelGGL((add_rms_norm_kernel<TX, TR, NT, NV, FP8>),
                                dim3((unsigned)d->tokens), dim3(NT), 0, static_cast<hipStream_t>(stream), a);
         });
     });
@@ -446,14 +453,13 @@ int im2win_add_rms_norm_backward(const im2win_norm_desc* d, const void* dy, cons
     a.tokens = (int)d->tokens; a.channels = (int)d->channels; a.blocks = (int)blocks;
     a.eps = d->eps; a.inv_d = 1.0f / (float)d->channels;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool vec = d->channels % kPer == 0 && all_aligned({dy, h, w, d_residual, dx});
     if (blocks)
-        with_types(d, vec, [&](auto tx, auto tr, auto v) {
+        with_types(d, [&](auto tx, auto tr) {
             with_shape(d->channels, [&](auto nt, auto nv) {
                 using TX = decltype(tx);
                 using TR = decltype(tr);
                 constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-                hipLaunchKernelGGL((add_rms_norm_bwd_kernel<TX, TR, NT, NV, decltype(v)::value>),
+                hipLaunchKernelGGL((add_rms_norm_bwd_kernel<TX, TR, NT, NV>),
                                    dim3((unsigned)blocks), dim3(NT), 0, s, a);
             });
         });

@@ -300,7 +300,7 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_step_kernel(ScanStepA
     if (!live) return;
     if (p.whole) {
         if constexpr (NS % 4 == 0) {
-            store_f32<NS>(state, h);
+            store_run<NS>(state, h);
         } else {
 #pragma unroll
             for (int s = 0; s < NS; s += 2) *reinterpret_cast<float2*>(state + s) = make_float2(h[s], h[s + 1]);
