@@ -22,7 +22,10 @@ struct Conv1dArgs {
     int silu;
 };
 
-constexpr int kConvTile = 16;    // tokens per wave
+// Tokens per wave.  Short tiles read their W-1 rows of overlap from L2 again
+// but fill the chip: 16384 x 4096 bf16 (4 taps) takes 62 us with 16 rows, 50
+// with 8, 51 with 4, and 512 x 512 takes 14.7, 8.5 and 8.4.
+constexpr int kConvTile = 4;
 constexpr int kConvWaves = 4;    // waves per workgroup, each with its own tile
 
 template <typename T, int V, int W>
@@ -175,10 +178,22 @@ struct Conv1dBwdArgs {
     int channels;
     int groups;
     int silu;
+    int stripe;         // rows per wave
     int parts;
 };
 
-constexpr int kConvStripe = 32;   // rows per wave
+constexpr int kConvBatch = 4;     // rows in flight
+
+// Rows per wave: a walk of a stripe is serial, so a short problem takes short
+// stripes, and a large one long ones, whose sums are fewer: the longest that
+// leaves a wave for each of the chip's 1024 SIMDs.  16384 x 4096 bf16 takes 91
+// us with 64 rows, 98 with 32 and 110 with 16; 512 x 512 takes 44, 26 and 17.5
+// with 64, 32 and 8; 8000 x 2001 fp32 takes 63, 56 and 62 with 64, 32 and 16.
+int64_t stripe_of(int64_t tokens, int64_t groups) {
+    int64_t stripe = 64;
+    while (stripe > 8 && groups * ((tokens + stripe - 1) / stripe) < 1024) stripe /= 2;
+    return stripe;
+}
 
 template <int V>
 __device__ __forceinline__ void times_slope(float (&g)[V], const float (&s)[V], int silu) {
@@ -207,9 +222,9 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_bwd_kernel(Conv1dBw
     taps.load(static_cast<const T*>(a.w), static_cast<const T*>(a.bias), c);
     float dw[W + 1][V] = {};                 // the last row is dbias
 
-    const int64_t s0 = ((int64_t)part * kConvWaves + wave) * kConvStripe;
+    const int64_t s0 = ((int64_t)part * kConvWaves + wave) * a.stripe;
     const int lo = (int)max<int64_t>(a.seq.first(0), s0);
-    const int hi = (int)min<int64_t>(a.seq.first(a.seq.count), s0 + kConvStripe);
+    const int hi = (int)min<int64_t>(a.seq.first(a.seq.count), s0 + a.stripe);
     for (int t = lo; t < hi;) {
         const int b = a.seq.find(t);
         const int first = a.seq.first(b), end = max(a.seq.first(b + 1), t + 1);
@@ -263,46 +278,40 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_bwd_kernel(Conv1dBw
             if (live) store_vec<V>(dx + (int64_t)u * a.channels + c, d);
         };
 
-        // the stripe's rows, kBatch of them loaded while the ones before are worked on
-        constexpr int kBatch = 4;
-        Bits<T, V> nx[kBatch], ng[kBatch];
+        // the stripe's rows and the W-1 behind, which its last ones reach: kBatch rows are loaded while
+        // the ones before them are worked on
+        const int reach = min(own + W - 1, end);
+        Bits<T, V> nx[kConvBatch], ng[kConvBatch];
         auto fetch = [&](int r) {
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                const int64_t at = min(r + i, own - 1);
+            for (int i = 0; i < kConvBatch; ++i) {
+                const int64_t at = min(r + i, reach - 1);
                 nx[i].load(x + at * a.ld_x + c);
                 ng[i].load(dy + at * a.channels + c);
             }
         };
         fetch(t);
-        for (int r = t; r < own; r += kBatch) {
-            Bits<T, V> cx[kBatch], cg[kBatch];
+        for (int r = t; r < reach; r += kConvBatch) {
+            Bits<T, V> cx[kConvBatch], cg[kConvBatch];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
+            for (int i = 0; i < kConvBatch; ++i) {
                 cx[i] = nx[i];
                 cg[i] = ng[i];
             }
-            if (r + kBatch < own) fetch(r + kBatch);
+            if (r + kConvBatch < reach) fetch(r + kConvBatch);
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                if (r + i >= own) break;
+            for (int i = 0; i < kConvBatch; ++i) {
+                if (r + i >= reach) break;
                 shift();
-                row(cx[i], cg[i], true);
+                row(cx[i], cg[i], r + i < own);
                 put(r + i - (W - 1));
             }
         }
-        // the rows behind, which the last W-1 of the stripe reach
-        for (int r = own; r < own + W - 1; ++r) {
+        // behind the sequence's end there is no gradient
+        for (int r = reach; r < own + W - 1; ++r) {
             shift();
-            if (r < end) {
-                Bits<T, V> xr, gr;
-                xr.load(x + (int64_t)r * a.ld_x + c);
-                gr.load(dy + (int64_t)r * a.channels + c);
-                row(xr, gr, false);
-            } else {
 #pragma unroll
-                for (int v = 0; v < V; ++v) g[W - 1][v] = 0.0f;
-            }
+            for (int v = 0; v < V; ++v) g[W - 1][v] = 0.0f;
             put(r - (W - 1));
         }
         t = own;
@@ -330,57 +339,64 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_bwd_kernel(Conv1dBw
 
 constexpr int kSumWaves = 8;
 
-// dw and dbias from the workgroups' sums: 64 channels of one tap per workgroup,
-// every eighth sum per wave, eight loads in flight
-__global__ __launch_bounds__(kSumWaves * kWave) void conv1d_bwd_sum_kernel(Conv1dBwdArgs a, int width) {
+// What is left after the walks, one workgroup for each row of 512 channels
+// that a state's gradient has, and before them one for each 64 channels of a
+// tap (or of the bias): its workgroups' sums, every eighth per wave, eight
+// loads in flight.
+template <typename T, int W>
+__global__ __launch_bounds__(kSumWaves * kWave) void conv1d_bwd_finish_kernel(Conv1dBwdArgs a) {
     __shared__ float sum[kSumWaves][kWave];
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-    const int c = (int)blockIdx.x * kWave + lane, k = blockIdx.y;
-    float s = 0.0f;
-    if (c < a.channels) {
+    const int across = (a.channels + kWave - 1) / kWave;
+    if ((int64_t)blockIdx.x < (int64_t)across * (W + 1)) {
+        const int c = (int)(blockIdx.x % across) * kWave + lane, k = blockIdx.x / across;
+        float s = 0.0f;
+        if (c < a.channels) {
 #pragma unroll 8
-        for (int i = wave; i < a.parts; i += kSumWaves)
-            s += a.part[((int64_t)i * (width + 1) + k) * a.channels + c];
-    }
-    sum[wave][lane] = s;
-    __syncthreads();
-    if (wave == 0 && c < a.channels) {
-        for (int i = 1; i < kSumWaves; ++i) s += sum[i][lane];
-        if (k < width) a.dw[(int64_t)c * width + k] = s;
-        else if (a.dbias) a.dbias[c] = s;
-    }
-}
-
-// Gradient of the initial states: row e of a sequence's W-1 earlier inputs
-template <typename T, int W>
-__global__ __launch_bounds__(256) void conv1d_bwd_init_kernel(Conv1dBwdArgs a) {
-    const T* x = static_cast<const T*>(a.x);
-    const T* init = static_cast<const T*>(a.init);
-    const T* d_final = static_cast<const T*>(a.d_final);
-    const int64_t row = blockIdx.x;
-    const int b = (int)(row / (W - 1)), e = (int)(row % (W - 1));
-    const int first = a.seq.first(b), end = max(a.seq.first(b + 1), first), len = end - first;
-    const int c = (int)blockIdx.y * 256 + threadIdx.x;
-    if (c >= a.channels) return;
-    Taps<T, 1, W> taps;
-    taps.load(static_cast<const T*>(a.w), static_cast<const T*>(a.bias), c);
-    float d = 0.0f;
-    if (d_final && e >= len) d = (float)d_final[((int64_t)b * (W - 1) + (e - len)) * a.channels + c];
-#pragma unroll
-    for (int k = 0; k < W; ++k) {
-        const int p = e - k;                 // the row of the sequence that reads input e with tap k
-        if (p < 0 || p >= len) continue;
-        float s[1] = {taps.bias[0]}, g[1] = {(float)static_cast<const T*>(a.dy)[(int64_t)(first + p) * a.channels + c]};
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-            float in[1];
-            load_input<T, 1, W>(x, init, a.ld_x, a.channels, b, first, first + p, W - 1 - j, c, in);
-            s[0] = fmaf(taps.w[j][0], in[0], s[0]);
+            for (int i = wave; i < a.parts; i += kSumWaves)
+                s += a.part[((int64_t)i * (W + 1) + k) * a.channels + c];
         }
-        times_slope<1>(g, s, a.silu);
-        d = fmaf(taps.w[k][0], g[0], d);
+        sum[wave][lane] = s;
+        __syncthreads();
+        if (wave == 0 && c < a.channels) {
+#pragma unroll
+            for (int i = 1; i < kSumWaves; ++i) s += sum[i][lane];
+            if (k < W) a.dw[(int64_t)c * W + k] = s;
+            else if (a.dbias) a.dbias[c] = s;
+        }
+        return;
     }
-    static_cast<T*>(a.d_init)[row * a.channels + c] = (T)d;
+    if constexpr (W > 1) {
+        // row e of a sequence's W-1 earlier inputs
+        const T* x = static_cast<const T*>(a.x);
+        const T* init = static_cast<const T*>(a.init);
+        const T* d_final = static_cast<const T*>(a.d_final);
+        const int wide = (a.channels + kSumWaves * kWave - 1) / (kSumWaves * kWave);
+        const int64_t block = (int64_t)blockIdx.x - (int64_t)across * (W + 1), row = block / wide;
+        const int b = (int)(row / (W - 1)), e = (int)(row % (W - 1));
+        const int first = a.seq.first(b), end = max(a.seq.first(b + 1), first), len = end - first;
+        const int c = (int)(block % wide) * kSumWaves * kWave + threadIdx.x;
+        if (c >= a.channels) return;
+        Taps<T, 1, W> taps;
+        taps.load(static_cast<const T*>(a.w), static_cast<const T*>(a.bias), c);
+        float d = 0.0f;
+        if (d_final && e >= len) d = (float)d_final[((int64_t)b * (W - 1) + (e - len)) * a.channels + c];
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            const int p = e - k;             // the row of the sequence that reads input e with tap k
+            if (p < 0 || p >= len) continue;
+            float s[1] = {taps.bias[0]}, g[1] = {(float)static_cast<const T*>(a.dy)[(int64_t)(first + p) * a.channels + c]};
+#pragma unroll
+            for (int j = 0; j < W; ++j) {
+                float in[1];
+                load_input<T, 1, W>(x, init, a.ld_x, a.channels, b, first, first + p, W - 1 - j, c, in);
+                s[0] = fmaf(taps.w[j][0], in[0], s[0]);
+            }
+            times_slope<1>(g, s, a.silu);
+            d = fmaf(taps.w[k][0], g[0], d);
+        }
+        static_cast<T*>(a.d_init)[row * a.channels + c] = (T)d;
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -450,8 +466,18 @@ bool whole_vectors(const im2win_conv1d_desc* d) { return d->channels * elem_of(d
 
 int64_t channel_groups(int64_t channels, int v) { return (channels + kWave * v - 1) / (kWave * v); }
 
-int64_t bwd_blocks(int64_t tokens) {
-    return (tokens + kConvStripe * kConvWaves - 1) / (kConvStripe * kConvWaves);
+struct BwdPlan {
+    int64_t groups, stripe, parts;
+    size_t bytes;
+};
+
+BwdPlan plan_bwd(const im2win_conv1d_desc* d) {
+    BwdPlan p;
+    p.groups = channel_groups(d->channels, vectors(d) ? (int)(16 / elem_of(d)) : 1);
+    p.stripe = stripe_of(d->tokens, p.groups);
+    p.parts = (d->tokens + p.stripe * kConvWaves - 1) / (p.stripe * kConvWaves);
+    p.bytes = (size_t)(p.parts * (d->width + 1) * d->channels * 4);
+    return p;
 }
 
 template <typename F>
@@ -525,7 +551,7 @@ int im2win_causal_conv1d_backward_workspace_bytes(const im2win_conv1d_desc* d, s
     int rc = check_desc(d);
     if (rc || (rc = check_sequences(d->tokens, d->sequences, nullptr, false))) return rc;
     if (!bytes) return fail(IM2WIN_ENULL, "bytes is NULL");
-    *bytes = (size_t)(bwd_blocks(d->tokens) * (d->width + 1) * d->channels * 4);
+    *bytes = plan_bwd(d).bytes;
     return ok();
 }
 
@@ -543,42 +569,34 @@ int im2win_causal_conv1d_backward(const im2win_conv1d_desc* d, const void* dy, c
         (rc = may_ptr(dbias, 4, "dbias")) || (rc = may_ptr(initial_state, e, "initial_state")) ||
         (rc = may_ptr(d_final_state, e, "d_final_state")) || (rc = may_ptr(d_initial_state, e, "d_initial_state")))
         return rc;
-    const int64_t blocks = bwd_blocks(d->tokens);
-    const size_t need = (size_t)(blocks * (d->width + 1) * d->channels * 4);
-    if (workspace_bytes < need)
-        return fail(IM2WIN_EWORKSPACE, "workspace holds %zu bytes, the gradients need %zu", workspace_bytes, need);
-    const bool states = d_initial_state && d->width > 1;
-    if (states && d->sequences * (d->width - 1) > (int64_t(1) << 31) - 1)
-        return fail(IM2WIN_EOVERFLOW, "too many sequences (%lld)", (long long)d->sequences);
+    const BwdPlan p = plan_bwd(d);
+    if (workspace_bytes < p.bytes)
+        return fail(IM2WIN_EWORKSPACE, "workspace holds %zu bytes, the gradients need %zu", workspace_bytes, p.bytes);
+    const int64_t sums = (d->channels + kWave - 1) / kWave * (d->width + 1);
+    const int64_t states = d_initial_state ? d->sequences * (d->width - 1) * ((d->channels + kSumWaves * kWave - 1) / (kSumWaves * kWave)) : 0;
+    if (sums + states > (int64_t(1) << 31) - 1)
+        return fail(IM2WIN_EOVERFLOW, "too many sequences and channels (%lld, %lld)", (long long)d->sequences, (long long)d->channels);
     Conv1dBwdArgs a{};
     a.dy = dy; a.x = x; a.w = w; a.bias = bias; a.init = initial_state; a.d_final = d_final_state;
     a.dx = dx; a.d_init = d_initial_state; a.part = static_cast<float*>(workspace); a.dw = dw; a.dbias = dbias;
     a.seq = make_seq_map(d->tokens, d->sequences, seq_starts);
-    a.ld_x = d->ld_x; a.channels = (int)d->channels; a.silu = d->silu != 0; a.parts = (int)blocks;
+    a.ld_x = d->ld_x; a.channels = (int)d->channels; a.silu = d->silu != 0; a.parts = (int)p.parts;
+    a.groups = (int)p.groups; a.stripe = (int)p.stripe;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool vec = vectors(d);
-    a.groups = (int)channel_groups(d->channels, vec ? (int)(16 / e) : 1);
-    if (blocks * a.groups > (int64_t(1) << 31) - 1)
+    if (p.parts * p.groups > (int64_t(1) << 31) - 1)
         return fail(IM2WIN_EOVERFLOW, "too many tokens and channels (%lld, %lld)", (long long)d->tokens, (long long)d->channels);
     with_kernel(d, vec, [&](auto t, auto v, auto taps) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value, W = decltype(taps)::value;
-        if (blocks)
-            hipLaunchKernelGGL((conv1d_bwd_kernel<T, V, W>), dim3((unsigned)(blocks * a.groups)),
+        if (p.parts)
+            hipLaunchKernelGGL((conv1d_bwd_kernel<T, V, W>), dim3((unsigned)(p.parts * p.groups)),
                                dim3(kConvWaves * kWave), 0, s, a);
     });
-    if (states)
-        with_kernel(d, false, [&](auto t, auto, auto taps) {
-            using T = decltype(t);
-            constexpr int W = decltype(taps)::value;
-            if constexpr (W > 1)
-                hipLaunchKernelGGL((conv1d_bwd_init_kernel<T, W>),
-                                   dim3((unsigned)(d->sequences * (W - 1)), (unsigned)((d->channels + 255) / 256)),
-                                   dim3(256), 0, s, a);
-        });
-    hipLaunchKernelGGL(conv1d_bwd_sum_kernel,
-                       dim3((unsigned)((d->channels + kWave - 1) / kWave), (unsigned)(d->width + 1)),
-                       dim3(kSumWaves * kWave), 0, s, a, (int)d->width);
+    with_kernel(d, false, [&](auto t, auto, auto taps) {
+        hipLaunchKernelGGL((conv1d_bwd_finish_kernel<decltype(t), decltype(taps)::value>), dim3((unsigned)(sums + states)),
+                           dim3(kSumWaves * kWave), 0, s, a);
+    });
     return launched("causal_conv1d_backward");
 }
 
