@@ -17,9 +17,12 @@ constexpr int kWave = 64;
 constexpr int64_t kMaxTokens = (int64_t(1) << 31) - (int64_t(1) << 20);
 constexpr int64_t kMaxChannels = int64_t(1) << 20;
 
+// A value that is the same in every lane of the wave, held in a scalar register.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
 // ---------------------------------------------------------------------------
 // Sequences in the rows.  Every bound a kernel uses comes from first(), which
-// lies in [0, tokens] whatever seq_starts holds.
+// lies in [0, tokens] whatever seq_starts holds.  Arguments are wave-uniform.
 // ---------------------------------------------------------------------------
 struct SeqMap {
     const int32_t* starts;   // NULL: sequences of `len` rows each
@@ -29,7 +32,7 @@ struct SeqMap {
 
     __device__ int first(int b) const {
         if (!starts) return b * len;   // b <= count, count * len == tokens
-        const int s = starts[b];
+        const int s = uniform(starts[b]);
         return s < 0 ? 0 : s > tokens ? tokens : s;
     }
     // The sequence that holds row t, for first(0) <= t < first(count).
@@ -128,8 +131,6 @@ __device__ __forceinline__ void store_run(T* p, const float (&v)[N]) {
 __device__ __forceinline__ float sigmoid(float v) {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896f * v));
 }
-
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // ---------------------------------------------------------------------------
 // Host side

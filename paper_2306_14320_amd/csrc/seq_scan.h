@@ -41,7 +41,6 @@ struct ScanArgs {
     int chunk;             // rows per chunk
     int chunks;
     int softplus;
-    int wide;              // rows of pairs of channels can be read and written in one access
     float* carry;          // [chunks][channels][4*NS]: the state behind each chunk
     float* span;           // [chunks][channels]: the sum of step sizes that the state passes
     int* flags;            // [chunks]
@@ -60,6 +59,18 @@ __device__ __forceinline__ float quad_sum(float v) {   // in every lane of the q
     return v;
 }
 
+// Four rows' values, each spread over the quad's lanes, summed: lane J gets row J's.
+__device__ __forceinline__ float quad_sums(float r0, float r1, float r2, float r3, int q) {
+    auto cross = [](float own, float other, auto lanes) {
+        return own + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(other), decltype(lanes)::value, 0xf, 0xf, true));
+    };
+    using std::integral_constant;
+    const bool odd = q & 1, high = q & 2;
+    const float low = cross(odd ? r1 : r0, odd ? r0 : r1, integral_constant<int, 0xB1>{});
+    const float top = cross(odd ? r3 : r2, odd ? r2 : r3, integral_constant<int, 0xB1>{});
+    return cross(high ? top : low, high ? low : top, integral_constant<int, 0x4E>{});
+}
+
 // log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|), and log1p(e) =
 // 2 atanh(s) with s = e / (2 + e) <= 1/3 by its power series, whose first
 // term left out is s^17 / 17 < 1e-9: small steps keep their relative accuracy.
@@ -76,69 +87,43 @@ __device__ __forceinline__ float softplus(float v) {
     return fmaxf(v, 0.0f) + fmaf(2.0f * s * q, p, 2.0f * s);
 }
 
-// CH neighbouring channels of a row as they lie in memory; the conversion is
-// left to get(), so that a load can stay in flight.  `wide`: one access.
-template <typename T, int CH> struct Raw;
-
-template <> struct Raw<float, 1> {
-    float v;
-    __device__ __forceinline__ void load(const float* row, const int (&c)[1], bool) { v = row[c[0]]; }
-    __device__ __forceinline__ float get(int, bool) const { return v; }
-};
-template <> struct Raw<float, 2> {
-    float2 v;
-    __device__ __forceinline__ void load(const float* row, const int (&c)[2], bool wide) {
-        if (wide) v = *reinterpret_cast<const float2*>(row + c[0]);
-        else v = make_float2(row[c[0]], row[c[1]]);
-    }
-    __device__ __forceinline__ float get(int i, bool) const { return i ? v.y : v.x; }
-};
-template <> struct Raw<bf16, 1> {
-    uint16_t v;
-    __device__ __forceinline__ void load(const bf16* row, const int (&c)[1], bool) {
-        v = reinterpret_cast<const uint16_t*>(row)[c[0]];
-    }
-    __device__ __forceinline__ float get(int, bool) const { return __uint_as_float((uint32_t)v << 16); }
-};
-template <> struct Raw<bf16, 2> {
-    uint32_t a, b;     // both channels in a where wide, one in each otherwise
-    __device__ __forceinline__ void load(const bf16* row, const int (&c)[2], bool wide) {
-        const uint16_t* p = reinterpret_cast<const uint16_t*>(row);
-        if (wide) {
-            a = *reinterpret_cast<const uint32_t*>(p + c[0]);
+// CH neighbouring channels of a row as they lie in memory, one access at any
+// address; the conversion is left to get(), so that a load can stay in flight.
+template <typename T, int CH>
+struct Raw {
+    static_assert(CH == 1 || CH == 2, "one channel or two");
+    static constexpr int kWords = (CH * (int)sizeof(T) + 3) / 4;
+    uint32_t u[kWords];
+    __device__ __forceinline__ void load(const char* p) {
+        if constexpr (CH * sizeof(T) < 4) {
+            uint16_t v;
+            __builtin_memcpy(&v, p, 2);
+            u[0] = v;
         } else {
-            a = p[c[0]];
-            b = p[c[1]];
+            __builtin_memcpy(u, p, CH * sizeof(T));
         }
     }
-    __device__ __forceinline__ float get(int i, bool wide) const {
-        return __uint_as_float(i == 0 ? a << 16 : wide ? a & 0xffff0000u : b << 16);
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(u[i]);
+        else return __uint_as_float(i ? u[0] & 0xffff0000u : u[0] << 16);
     }
 };
 
-template <int CH>
-__device__ __forceinline__ void store_channels(float* row, int c, const bool (&live)[CH], const float (&v)[CH], bool wide) {
+// The channels of a row that a lane owns
+template <typename T, int CH>
+__device__ __forceinline__ void store_channels(char* p, const bool (&live)[CH], const float (&v)[CH]) {
+    T e[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) e[i] = (T)v[i];
     if constexpr (CH == 2) {
-        if (wide) {
-            if (live[0]) *reinterpret_cast<float2*>(row + c) = make_float2(v[0], v[1]);
+        if (live[0] && live[1]) {
+            __builtin_memcpy(p, e, sizeof e);
             return;
         }
     }
 #pragma unroll
     for (int i = 0; i < CH; ++i)
-        if (live[i]) row[c + i] = v[i];
-}
-template <int CH>
-__device__ __forceinline__ void store_channels(bf16* row, int c, const bool (&live)[CH], const float (&v)[CH], bool wide) {
-    if constexpr (CH == 2) {
-        if (wide) {
-            if (live[0]) *reinterpret_cast<uint32_t*>(row + c) = pack_bf16(v[0], v[1]);
-            return;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < CH; ++i)
-        if (live[i]) row[c + i] = (bf16)v[i];
+        if (live[i]) __builtin_memcpy(p + i * sizeof(T), e + i, sizeof(T));
 }
 
 // NS consecutive floats of LDS on a boundary of their largest power of two
@@ -162,12 +147,14 @@ __device__ __forceinline__ void lds_row(const float* p, float (&v)[NS]) {
     }
 }
 
-// The channels of a lane
+// The channels of a lane: c to c + CH - 1.  A lane past its group, and the
+// second place of a group's odd last channel, hold other channels of the row
+// (whose memory exists) and are not live; the last channel of a row of them is
+// the second place of the pair in front of it.
 template <int CH>
 struct Lane {
     int q;              // lane of the quad: its quarter of the states, and its row of four
-    int c0;             // first channel (may lie past the group)
-    int c[CH];          // channels to read from: past the group, its first one
+    int c;
     bool live[CH];
 
     __device__ __forceinline__ void init(const ScanArgs& a, int block, int wave) {
@@ -175,12 +162,26 @@ struct Lane {
         q = lane % kQuad;
         const int group = block / a.group_blocks;
         const int from = group * a.group_channels, to = from + a.group_channels;
-        c0 = from + ((block % a.group_blocks) * kScanWaves + wave) * (kWave / kQuad) * CH + lane / kQuad * CH;
+        const int own = from + ((block % a.group_blocks) * kScanWaves + wave) * (kWave / kQuad) * CH + lane / kQuad * CH;
+        c = min(own, a.channels - CH);
 #pragma unroll
-        for (int i = 0; i < CH; ++i) {
-            live[i] = c0 + i < to;
-            c[i] = live[i] ? c0 + i : from + (a.wide ? i : 0);
-        }
+        for (int i = 0; i < CH; ++i) live[i] = c + i >= own && c + i < to;
+    }
+};
+
+// A T x D array: the rows of a group of four, one for each lane of the quad.
+// The group's first row is a scalar address and a lane's place beside it a
+// 32-bit offset, so that a group costs no vector instruction for addresses.
+template <typename T>
+struct RowPlace {
+    uint32_t offset;
+    template <int CH>
+    __device__ __forceinline__ RowPlace(int64_t ld, const Lane<CH>& l, int row) : offset((uint32_t)((row * ld + l.c) * (int64_t)sizeof(T))) {}
+    __device__ __forceinline__ const char* at(const void* m, int64_t ld, int t) const {
+        return static_cast<const char*>(m) + t * ld * (int64_t)sizeof(T) + offset;
+    }
+    __device__ __forceinline__ char* at(void* m, int64_t ld, int t) const {
+        return static_cast<char*>(m) + t * ld * (int64_t)sizeof(T) + offset;
     }
 };
 
@@ -194,11 +195,13 @@ __device__ __forceinline__ void stage(float* lds, const T* m, int64_t ld, int gr
     }
 }
 
-// Compiled shapes: f(NS, CH) for N states
+// Compiled shapes: f(NS, CH) for N states of D channels.  Up to 24 states a lane
+// holds a pair of channels; a single channel has no neighbour to read.
 template <typename F>
-void with_states(int64_t n, F f) {
+void with_states(int64_t n, int64_t channels, F f) {
     using std::integral_constant;
-    if (n <= 8) f(integral_constant<int, 2>{}, integral_constant<int, 2>{});
+    if (channels == 1 && n <= 32) f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
+    else if (n <= 8) f(integral_constant<int, 2>{}, integral_constant<int, 2>{});
     else if (n <= 16) f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
     else if (n <= 24) f(integral_constant<int, 6>{}, integral_constant<int, 2>{});
     else if (n <= 32) f(integral_constant<int, 8>{}, integral_constant<int, 1>{});

@@ -22,14 +22,17 @@ namespace {
 template <typename T, int CH>
 struct Rows {
     Raw<T, CH> x, dt, z;
-
+};
+template <typename T, int CH>
+struct Places {
+    RowPlace<T> x, dt, z;
+    __device__ __forceinline__ Places(const ScanArgs& a, const Lane<CH>& l, int row) : x(a.ld_x, l, row), dt(a.ld_dt, l, row), z(a.ld_z, l, row) {}
     template <bool GATE>
-    __device__ __forceinline__ void load(const ScanArgs& a, const Lane<CH>& l, int t, int last) {
-        const int64_t row = min(t + l.q, last);
-        x.load(static_cast<const T*>(a.x) + row * a.ld_x, l.c, a.wide);
-        dt.load(static_cast<const T*>(a.dt) + row * a.ld_dt, l.c, a.wide);
+    __device__ __forceinline__ void load(const ScanArgs& a, int t, Rows<T, CH>& r) const {
+        r.x.load(x.at(a.x, a.ld_x, t));
+        r.dt.load(dt.at(a.dt, a.ld_dt, t));
         if constexpr (GATE)
-            if (a.z) z.load(static_cast<const T*>(a.z) + row * a.ld_z, l.c, a.wide);
+            if (a.z) r.z.load(z.at(a.z, a.ld_z, t));
     }
 };
 
@@ -77,12 +80,12 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
     float a2[CH][NS], h[CH][NS], bias[CH], skip[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        bias[i] = a.dt_bias ? a.dt_bias[l.c[i]] : 0.0f;
-        skip[i] = !SUMMARY && a.D ? a.D[l.c[i]] : 0.0f;
+        bias[i] = a.dt_bias ? a.dt_bias[l.c + i] : 0.0f;
+        skip[i] = !SUMMARY && a.D ? a.D[l.c + i] : 0.0f;
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const int n = l.q * NS + s;
-            a2[i][s] = n < a.states ? kLog2e * a.A[(int64_t)l.c[i] * a.states + n] : 0.0f;
+            a2[i][s] = n < a.states ? kLog2e * a.A[(int64_t)(l.c + i) * a.states + n] : 0.0f;
         }
     }
     auto begin = [&]() {     // the state before the first row of sequence b
@@ -91,7 +94,7 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
 #pragma unroll
             for (int s = 0; s < NS; ++s) {
                 const int n = l.q * NS + s;
-                h[i][s] = init && n < a.states ? init[((int64_t)b * a.channels + l.c[i]) * a.states + n] : 0.0f;
+                h[i][s] = init && n < a.states ? init[((int64_t)b * a.channels + (l.c + i)) * a.states + n] : 0.0f;
             }
     };
     if (lo == first) {
@@ -101,12 +104,19 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int s = 0; s < NS; ++s)
-                h[i][s] = SUMMARY || chunk == 0 ? 0.0f : a.carry[((int64_t)(chunk - 1) * a.channels + l.c[i]) * NP + l.q * NS + s];
+                h[i][s] = SUMMARY || chunk == 0 ? 0.0f : a.carry[((int64_t)(chunk - 1) * a.channels + (l.c + i)) * NP + l.q * NS + s];
     }
 
     float span[CH] = {};
+    // the last group may have fewer than four rows: the lanes past them take its last one
+    const Places<T, CH> whole(a, l, l.q), part(a, l, min(l.q, (hi - lo - 1) % kQuad));
+    const RowPlace<T> out(a.channels, l, l.q);
+    auto load = [&](int t, Rows<T, CH>& r) {
+        if (t + kQuad <= hi) whole.template load<!SUMMARY>(a, t, r);
+        else part.template load<!SUMMARY>(a, t, r);
+    };
     Rows<T, CH> next;
-    next.template load<!SUMMARY>(a, l, lo, hi - 1);
+    load(lo, next);
     for (int tile = lo; tile < hi; tile += kScanTile) {
         const int rows = min(kScanTile, hi - tile);
         __syncthreads();
@@ -117,12 +127,12 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
         for (int r = 0; r < rows; r += kQuad) {
             const int t = tile + r;
             const Rows<T, CH> now = next;
-            if (t + kQuad < hi) next.template load<!SUMMARY>(a, l, t + kQuad, hi - 1);
-            float step[CH], in[CH], x[CH], sum[CH] = {};
+            if (t + kQuad < hi) load(t + kQuad, next);
+            float step[CH], in[CH], x[CH], sums[kQuad][CH] = {};
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                x[i] = now.x.get(i, a.wide);
-                step[i] = now.dt.get(i, a.wide) + bias[i];
+                x[i] = now.x.get(i);
+                step[i] = now.dt.get(i) + bias[i];
                 if (a.softplus) step[i] = softplus(step[i]);
                 in[i] = step[i] * x[i];
                 if (SUMMARY && t + l.q < hi) span[i] += step[i];
@@ -141,10 +151,7 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
                         h[i][s] = fmaf(__builtin_amdgcn_exp2f(sj * a2[i][s]), h[i][s], ij * bm[s]);
                         if constexpr (!SUMMARY) acc = fmaf(cm[s], h[i][s], acc);
                     }
-                    if constexpr (!SUMMARY) {
-                        acc = quad_sum(acc);
-                        if (l.q == J) sum[i] = acc;
-                    }
+                    if constexpr (!SUMMARY) sums[J][i] = acc;
                 }
             };
             auto finish = [&]() {     // the state behind the last row of sequence b
@@ -155,7 +162,7 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
                     for (int s = 0; s < NS; ++s) {
                         const int n = l.q * NS + s;
                         if (l.live[i] && n < a.states)
-                            a.final_state[((int64_t)b * a.channels + l.c[i]) * a.states + n] = h[i][s];
+                            a.final_state[((int64_t)b * a.channels + (l.c + i)) * a.states + n] = h[i][s];
                     }
             };
             auto advance = [&](int row) {
@@ -184,17 +191,16 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
                 one(integral_constant<int, 3>{});
             }
             if constexpr (!SUMMARY) {
-                if (t + l.q < hi) {
+                float sum[CH];
 #pragma unroll
-                    for (int i = 0; i < CH; ++i) {
-                        sum[i] = fmaf(skip[i], x[i], sum[i]);
-                        if (a.z) {
-                            const float z = now.z.get(i, a.wide);
-                            sum[i] *= z * sigmoid(z);
-                        }
+                for (int i = 0; i < CH; ++i) {
+                    sum[i] = fmaf(skip[i], x[i], quad_sums(sums[0][i], sums[1][i], sums[2][i], sums[3][i], l.q));
+                    if (a.z) {
+                        const float z = now.z.get(i);
+                        sum[i] *= z * sigmoid(z);
                     }
-                    store_channels<CH>(static_cast<T*>(a.y) + (int64_t)(t + l.q) * a.channels, l.c0, l.live, sum, a.wide);
                 }
+                if (t + l.q < hi) store_channels<T, CH>(out.at(a.y, a.channels, t), l.live, sum);
             }
         }
     }
@@ -203,7 +209,7 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
         for (int i = 0; i < CH; ++i) {
             span[i] = quad_sum(span[i]);
             if (!l.live[i]) continue;
-            const int64_t at = (int64_t)chunk * a.channels + l.c[i];
+            const int64_t at = (int64_t)chunk * a.channels + (l.c + i);
             if (l.q == 0) a.span[at] = span[i];
 #pragma unroll
             for (int s = 0; s < NS; ++s) a.carry[at * NP + l.q * NS + s] = h[i][s];
@@ -336,7 +342,7 @@ size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 // parts, or taken whole where they are shorter.
 ScanPlan plan_scan(const im2win_scan_desc* d) {
     ScanPlan p;
-    with_states(d->states, [&](auto ns, auto ch) {
+    with_states(d->states, d->channels, [&](auto ns, auto ch) {
         p.ns = decltype(ns)::value;
         p.ch = decltype(ch)::value;
     });
@@ -415,9 +421,6 @@ ScanArgs scan_args(const im2win_scan_desc* d, const void* x, const void* dt, con
     a.group_blocks = (a.group_channels + per_block - 1) / per_block;
     a.blocks = (int)d->groups * a.group_blocks;
     a.softplus = d->softplus != 0;
-    const size_t pair = d->dtype == IM2WIN_F32 ? 8 : 4;
-    a.wide = a.group_channels % 2 == 0 && d->ld_x % 2 == 0 && d->ld_dt % 2 == 0 && (!z || d->ld_z % 2 == 0) &&
-             aligned_to(x, pair) && aligned_to(dt, pair) && aligned_to(z, pair);
     return a;
 }
 
@@ -452,7 +455,6 @@ int im2win_selective_scan(const im2win_scan_desc* d, const void* x, const void* 
     a.init = initial_state; a.y = y; a.final_state = final_state;
     a.seq = make_seq_map(d->tokens, d->sequences, seq_starts);
     a.chunk = (int)p.chunk; a.chunks = (int)p.chunks;
-    a.wide = a.wide && aligned_to(y, d->dtype == IM2WIN_F32 ? 8 : 4);
     char* ws = static_cast<char*>(workspace);
     if (p.bytes) {
         a.carry = reinterpret_cast<float*>(ws);
@@ -467,7 +469,7 @@ int im2win_selective_scan(const im2win_scan_desc* d, const void* x, const void* 
     const bool whole = !seq_starts && p.chunks && p.chunk % (d->tokens / d->sequences) == 0;
     hipStream_t s = static_cast<hipStream_t>(stream);
     with_type(d->dtype, [&](auto t) {
-        with_states(d->states, [&](auto ns, auto ch) {
+        with_states(d->states, d->channels, [&](auto ns, auto ch) {
             using T = decltype(t);
             constexpr int NS = decltype(ns)::value, CH = decltype(ch)::value;
             const dim3 threads(kScanWaves * kWave);
@@ -499,7 +501,7 @@ int im2win_selective_scan_step(const im2win_scan_desc* d, const void* x, const v
     p.slots = slots; p.state = state; p.state_slots = state_slots;
     const unsigned cover = (unsigned)((d->channels * kQuad + kScanWaves * kWave - 1) / (kScanWaves * kWave));
     with_type(d->dtype, [&](auto t) {
-        with_states(d->states, [&](auto ns, auto) {
+        with_states(d->states, d->channels, [&](auto ns, auto) {
             using T = decltype(t);
             constexpr int NS = decltype(ns)::value;
             p.whole = d->states == kQuad * NS && aligned_to(A, 16) && aligned_to(state, 16);

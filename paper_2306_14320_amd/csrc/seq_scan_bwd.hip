@@ -71,6 +71,8 @@ struct ChunkRows {
     }
 };
 
+// A state of sequence b (zero where m is NULL).  Places that are not live hold zeros throughout,
+// so that they add nothing to sums over channels.
 template <int NS, int CH>
 __device__ __forceinline__ void load_state(const float* m, const ScanArgs& a, const Lane<CH>& l, int b, float (&h)[CH][NS]) {
 #pragma unroll
@@ -78,7 +80,7 @@ __device__ __forceinline__ void load_state(const float* m, const ScanArgs& a, co
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const int n = l.q * NS + s;
-            h[i][s] = m && n < a.states ? m[((int64_t)b * a.channels + l.c[i]) * a.states + n] : 0.0f;
+            h[i][s] = m && l.live[i] && n < a.states ? m[((int64_t)b * a.channels + (l.c + i)) * a.states + n] : 0.0f;
         }
 }
 
@@ -89,7 +91,7 @@ __device__ __forceinline__ void load_decay(const ScanArgs& a, const Lane<CH>& l,
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
             const int n = l.q * NS + s;
-            a2[i][s] = n < a.states ? kLog2e * a.A[(int64_t)l.c[i] * a.states + n] : 0.0f;
+            a2[i][s] = l.live[i] && n < a.states ? kLog2e * a.A[(int64_t)(l.c + i) * a.states + n] : 0.0f;
         }
 }
 
@@ -98,24 +100,30 @@ template <typename T, int CH>
 struct BwdRows {
     Raw<T, CH> x, dt, z, dy;
 
-    __device__ __forceinline__ void load_in(const ScanArgs& a, const Lane<CH>& l, int64_t row) {
-        x.load(static_cast<const T*>(a.x) + row * a.ld_x, l.c, a.wide);
-        dt.load(static_cast<const T*>(a.dt) + row * a.ld_dt, l.c, a.wide);
-    }
-    __device__ __forceinline__ void load_grad(const ScanBwdArgs& p, const Lane<CH>& l, int64_t row) {
-        if (p.s.z) z.load(static_cast<const T*>(p.s.z) + row * p.s.ld_z, l.c, p.s.wide);
-        dy.load(static_cast<const T*>(p.dy) + row * p.s.channels, l.c, p.s.wide);
-    }
     __device__ __forceinline__ float step(const ScanArgs& a, int i, float bias) const {
-        const float v = dt.get(i, a.wide) + bias;
+        const float v = dt.get(i) + bias;
         return a.softplus ? softplus(v) : v;
     }
     // the gradient of the sum in front of the gate
     __device__ __forceinline__ float grad(const ScanArgs& a, int i) const {
-        const float g = dy.get(i, a.wide);
+        const float g = dy.get(i);
         if (!a.z) return g;
-        const float v = z.get(i, a.wide);
+        const float v = z.get(i);
         return g * v * sigmoid(v);
+    }
+};
+template <typename T, int CH>
+struct BwdPlaces {
+    RowPlace<T> x, dt, z, dense;
+    __device__ __forceinline__ BwdPlaces(const ScanArgs& a, const Lane<CH>& l, int row)
+        : x(a.ld_x, l, row), dt(a.ld_dt, l, row), z(a.ld_z, l, row), dense(a.channels, l, row) {}
+    __device__ __forceinline__ void load_in(const ScanArgs& a, int t, BwdRows<T, CH>& r) const {
+        r.x.load(x.at(a.x, a.ld_x, t));
+        r.dt.load(dt.at(a.dt, a.ld_dt, t));
+    }
+    __device__ __forceinline__ void load_grad(const ScanBwdArgs& p, int t, BwdRows<T, CH>& r) const {
+        if (p.s.z) r.z.load(z.at(p.s.z, p.s.ld_z, t));
+        r.dy.load(dense.at(p.dy, p.s.channels, t));
     }
 };
 
@@ -151,7 +159,7 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_bwd_summary_kernel(Sc
     float a2[CH][NS], bias[CH];
     load_decay<NS, CH>(a, l, a2);
 #pragma unroll
-    for (int i = 0; i < CH; ++i) bias[i] = a.dt_bias ? a.dt_bias[l.c[i]] : 0.0f;
+    for (int i = 0; i < CH; ++i) bias[i] = a.dt_bias ? a.dt_bias[l.c + i] : 0.0f;
 
     // rows [from, to) of one sequence: h from its value before, the sum of steps, and the gradient sent back
     float h[CH][NS], back[CH][NS], pass[CH][NS], span[CH];
@@ -165,10 +173,14 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_bwd_summary_kernel(Sc
                 pass[i][s] = 1.0f;
             }
         }
+        const BwdPlaces<T, CH> whole(a, l, l.q), part(a, l, min(l.q, (to - from - 1) % kQuad));
+        auto load = [&](int t, BwdRows<T, CH>& r) {
+            const BwdPlaces<T, CH>& w = t + kQuad <= to ? whole : part;
+            w.load_in(a, t, r);
+            w.load_grad(p, t, r);
+        };
         BwdRows<T, CH> next;
-        int64_t row = min(from + l.q, to - 1);
-        next.load_in(a, l, row);
-        next.load_grad(p, l, row);
+        load(from, next);
         for (int tile = from; tile < to; tile += kScanTile) {
             const int n = min(kScanTile, to - tile);
             __syncthreads();
@@ -178,16 +190,12 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_bwd_summary_kernel(Sc
             for (int r = 0; r < n; r += kQuad) {
                 const int t = tile + r;
                 const BwdRows<T, CH> now = next;
-                if (t + kQuad < to) {
-                    row = min(t + kQuad + l.q, to - 1);
-                    next.load_in(a, l, row);
-                    next.load_grad(p, l, row);
-                }
+                if (t + kQuad < to) load(t + kQuad, next);
                 float step[CH], in[CH], grad[CH];
 #pragma unroll
                 for (int i = 0; i < CH; ++i) {
                     step[i] = now.step(a, i, bias[i]);
-                    in[i] = step[i] * now.x.get(i, a.wide);
+                    in[i] = step[i] * now.x.get(i);
                     grad[i] = now.grad(a, i);
                     if (t + l.q < to) span[i] += step[i];
                 }
@@ -222,14 +230,14 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_bwd_summary_kernel(Sc
         for (int i = 0; i < CH; ++i)
 #pragma unroll
             for (int s = 0; s < NS; ++s)
-                if (l.live[i]) m[((int64_t)chunk * a.channels + l.c[i]) * NP + l.q * NS + s] = v[i][s];
+                if (l.live[i]) m[((int64_t)chunk * a.channels + (l.c + i)) * NP + l.q * NS + s] = v[i][s];
     };
     auto put_forward = [&]() {
         put(a.carry, h);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
             span[i] = quad_sum(span[i]);
-            if (l.live[i] && l.q == 0) a.span[(int64_t)chunk * a.channels + l.c[i]] = span[i];
+            if (l.live[i] && l.q == 0) a.span[(int64_t)chunk * a.channels + l.c + i] = span[i];
         }
     };
     if (flags & kFromBefore) {
@@ -344,11 +352,10 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
         load_decay<NS, CH>(a, l, a2);
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            bias[i] = a.dt_bias ? a.dt_bias[l.c[i]] : 0.0f;
-            skip[i] = a.D ? a.D[l.c[i]] : 0.0f;
+            bias[i] = a.dt_bias ? a.dt_bias[l.c + i] : 0.0f;
+            skip[i] = a.D ? a.D[l.c + i] : 0.0f;
         }
-        const int n_rows = rows.hi - rows.lo, tiles = (n_rows + TB - 1) / TB;
-        for (int i = threadIdx.x; i < n_rows * NP; i += kScanWaves * kWave) {
+        for (int i = threadIdx.x; i < (rows.hi - rows.lo) * NP; i += kScanWaves * kWave) {
             const int r = i / NP, s = i % NP;
             const bool in = s < a.states;
             const int64_t at = (int64_t)group * a.states + s;
@@ -357,48 +364,44 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
         }
         __syncthreads();
 
-        // forwards: the state before each tile
-        {
-            float h[CH][NS];
-            int b = a.seq.find(rows.lo), end = a.seq.first(b + 1);
-            const int first = a.seq.first(b);
-            if (rows.lo == first) {
+        const BwdPlaces<T, CH> whole(a, l, l.q);
+        // one row of a sequence's part of the chunk: a chunk or a sequence before it left the state
+        auto start = [&](int b, bool begins, float (&h)[CH][NS]) {
+            if (begins) {
                 load_state<NS, CH>(a.init, a, l, b, h);
-            } else {
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int s = 0; s < NS; ++s)
-                        h[i][s] = chunk ? a.carry[((int64_t)(chunk - 1) * a.channels + l.c[i]) * NP + l.q * NS + s] : 0.0f;
+                return;
             }
-            BwdRows<T, CH> next;
-            next.load_in(a, l, min(rows.lo + l.q, rows.hi - 1));
-            for (int k = 0; k < tiles; ++k) {
 #pragma unroll
-                for (int i = 0; i < CH; ++i)
+            for (int i = 0; i < CH; ++i)
 #pragma unroll
-                    for (int s = 0; s < NS; ++s) lds.state[wave][k][i * NS + s][lane] = h[i][s];
-                if (k == tiles - 1) break;
-#pragma unroll
-                for (int g = 0; g < GROUPS; ++g) {
-                    const int r = k * TB + g * kQuad, t = rows.lo + r;
+                for (int s = 0; s < NS; ++s)
+                    h[i][s] = chunk && l.live[i] ? a.carry[((int64_t)(chunk - 1) * a.channels + (l.c + i)) * NP + l.q * NS + s] : 0.0f;
+        };
+
+        // Forwards: the state before every tile of a sequence but its first, which start() gives.  Each
+        // follows TB rows of its own, so there are at most Q / TB.
+        int slot = 0;
+        for (int t = rows.lo; t < rows.hi;) {
+            const int b = a.seq.find(t), first = a.seq.first(b), stop = min(max(a.seq.first(b + 1), t + 1), rows.hi);
+            const int walk = (stop - t - 1) / TB * TB;      // rows of all tiles but the last
+            if (walk) {
+                float h[CH][NS];
+                start(b, t == first, h);
+                BwdRows<T, CH> next;
+                whole.load_in(a, t, next);
+                for (int r = 0; r < walk; r += kQuad) {
                     const BwdRows<T, CH> now = next;
-                    next.load_in(a, l, min(t + kQuad + l.q, rows.hi - 1));
+                    if (r + kQuad < walk) whole.load_in(a, t + r + kQuad, next);
                     float step[CH], in[CH];
 #pragma unroll
                     for (int i = 0; i < CH; ++i) {
-                        step[i] = now.step(a, i, bias[i]);
-                        in[i] = step[i] * now.x.get(i, a.wide);
+                        step[i] = l.live[i] ? now.step(a, i, bias[i]) : 0.0f;
+                        in[i] = l.live[i] ? step[i] * now.x.get(i) : 0.0f;
                     }
                     auto token = [&](auto j) {
                         constexpr int J = decltype(j)::value;
-                        if (t + J >= end) {
-                            b = a.seq.find(t + J);
-                            end = a.seq.first(b + 1);
-                            load_state<NS, CH>(a.init, a, l, b, h);
-                        }
                         float bm[NS];
-                        lds_row<NS>(lds.b + (r + J) * NP + l.q * NS, bm);
+                        lds_row<NS>(lds.b + (t - rows.lo + r + J) * NP + l.q * NS, bm);
 #pragma unroll
                         for (int i = 0; i < CH; ++i) {
                             const float sj = quad_get<J>(step[i]), ij = quad_get<J>(in[i]);
@@ -412,111 +415,105 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
                     token(integral_constant<int, 1>{});
                     token(integral_constant<int, 2>{});
                     token(integral_constant<int, 3>{});
+                    if ((r + kQuad) % TB == 0) {
+#pragma unroll
+                        for (int i = 0; i < CH; ++i)
+#pragma unroll
+                            for (int s = 0; s < NS; ++s) lds.state[wave][slot][i * NS + s][lane] = h[i][s];
+                        ++slot;
+                    }
                 }
             }
+            t = stop;
         }
 
-        // backwards
-        int b = a.seq.find(rows.hi - 1), first = a.seq.first(b), end = a.seq.first(b + 1);
-        float r[CH][NS];     // a g of the row behind: what the state's gradient receives from there
+        // Backwards, sequence by sequence, tile by tile
+        for (int stop = rows.hi; stop > rows.lo;) {
+            const int b = a.seq.find(stop - 1), first = a.seq.first(b), end = a.seq.first(b + 1);
+            const int from = max(min(first, stop - 1), rows.lo);
+            float r[CH][NS];     // a g of the row behind: what the state's gradient receives from there
+            if (end > stop) {
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+                for (int i = 0; i < CH; ++i)
 #pragma unroll
-            for (int s = 0; s < NS; ++s)
-                r[i][s] = end > rows.hi && l.live[i] && chunk + 1 < a.chunks
-                              ? p.back[((int64_t)(chunk + 1) * a.channels + l.c[i]) * NP + l.q * NS + s] : 0.0f;
-        for (int k = tiles - 1; k >= 0; --k) {
-            const int r0 = k * TB, t0 = rows.lo + r0, t1 = min(t0 + TB, rows.hi);
-            if (t1 - 1 < first) {
-                b = a.seq.find(t1 - 1);
-                first = a.seq.first(b);
-                end = a.seq.first(b + 1);
+                    for (int s = 0; s < NS; ++s)
+                        r[i][s] = l.live[i] && chunk + 1 < a.chunks
+                                      ? p.back[((int64_t)(chunk + 1) * a.channels + (l.c + i)) * NP + l.q * NS + s] : 0.0f;
+            } else {
+                load_state<NS, CH>(p.d_final, a, l, b, r);
             }
-            // a tile inside one sequence, none of whose rows is the sequence's first or last
-            const bool inside = first < t0 && end > t0 + TB && t0 + TB <= rows.hi;
-
-            BwdRows<T, CH> now[GROUPS];
-            float step[GROUPS][CH], in[GROUPS][CH], grad[GROUPS][CH];
+            const int tiles = (stop - from + TB - 1) / TB;
+            BwdRows<T, CH> next[GROUPS];
+            {
+                const int t0 = from + (tiles - 1) * TB;
+                const BwdPlaces<T, CH> part(a, l, min(l.q, (stop - t0 - 1) % kQuad));
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                const int64_t row = min(t0 + g * kQuad + l.q, rows.hi - 1);
-                now[g].load_in(a, l, row);
-                now[g].load_grad(p, l, row);
-            }
-#pragma unroll
-            for (int g = 0; g < GROUPS; ++g)
-#pragma unroll
-                for (int i = 0; i < CH; ++i) {
-                    step[g][i] = now[g].step(a, i, bias[i]);
-                    in[g][i] = l.live[i] ? step[g][i] * now[g].x.get(i, a.wide) : 0.0f;
-                    grad[g][i] = l.live[i] ? now[g].grad(a, i) : 0.0f;
-                }
-            float h0[CH][NS], h[TB][CH][NS];
-#pragma unroll
-            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                for (int s = 0; s < NS; ++s) h0[i][s] = lds.state[wave][k][i * NS + s][lane];
-
-            float du[GROUPS][CH] = {}, ds[GROUPS][CH] = {}, sum[GROUPS][CH] = {};
-            auto tile = [&](auto edge) {
-                constexpr bool EDGE = decltype(edge)::value;
-                unsigned starts = 0, ends = 0;      // rows that begin or end a sequence
-                int bb = 0, bend = 0;
-                if constexpr (EDGE) {
-                    bb = a.seq.find(t0);
-                    bend = a.seq.first(bb + 1);
-                    if (a.seq.first(bb) == t0) starts = 1;
-                }
-                auto forward = [&](auto j) {
-                    constexpr int J = decltype(j)::value, G = J / kQuad;
-                    if constexpr (EDGE) {
-                        if (t0 + J >= rows.hi) return;
-                        if (t0 + J >= bend) {
-                            bb = a.seq.find(t0 + J);
-                            bend = a.seq.first(bb + 1);
-                            starts |= 1u << J;
-                        }
-                        if (t0 + J + 1 == bend) ends |= 1u << J;
+                for (int g = 0; g < GROUPS; ++g) {
+                    const int t = t0 + g * kQuad;
+                    if (t >= stop) {
+                        next[g] = next[0];      // not used
+                        continue;
                     }
-                    float bm[NS];
-                    lds_row<NS>(lds.b + (r0 + J) * NP + l.q * NS, bm);
-                    float hp[CH][NS];
+                    const BwdPlaces<T, CH>& w = t + kQuad <= stop ? whole : part;
+                    w.load_in(a, t, next[g]);
+                    w.load_grad(p, t, next[g]);
+                }
+            }
+            for (int k = tiles - 1; k >= 0; --k) {
+                const int t0 = from + k * TB, n = min(TB, stop - t0), r0 = t0 - rows.lo;
+                BwdRows<T, CH> now[GROUPS];
+                float step[GROUPS][CH], in[GROUPS][CH], grad[GROUPS][CH];
+#pragma unroll
+                for (int g = 0; g < GROUPS; ++g) {
+                    now[g] = next[g];
+                    if (k > 0) {
+                        whole.load_in(a, t0 - TB + g * kQuad, next[g]);
+                        whole.load_grad(p, t0 - TB + g * kQuad, next[g]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) {
+                        step[g][i] = l.live[i] ? now[g].step(a, i, bias[i]) : 0.0f;
+                        in[g][i] = l.live[i] ? step[g][i] * now[g].x.get(i) : 0.0f;
+                        grad[g][i] = l.live[i] ? now[g].grad(a, i) : 0.0f;
+                    }
+                }
+                float h0[CH][NS], h[TB][CH][NS];
+                if (k > 0) {
+                    slot = max(slot - 1, 0);
 #pragma unroll
                     for (int i = 0; i < CH; ++i)
 #pragma unroll
-                        for (int s = 0; s < NS; ++s) hp[i][s] = J == 0 ? h0[i][s] : h[J > 0 ? J - 1 : 0][i][s];
-                    if constexpr (EDGE)
-                        if (starts >> J & 1) load_state<NS, CH>(a.init, a, l, bb, hp);
+                        for (int s = 0; s < NS; ++s) h0[i][s] = lds.state[wave][slot][i * NS + s][lane];
+                } else {
+                    start(b, from == first, h0);
+                }
+
+                auto forward = [&](auto j) {
+                    constexpr int J = decltype(j)::value, G = J / kQuad;
+                    __builtin_amdgcn_sched_barrier(0);     // rows side by side would not fit the registers
+                    if (J >= n) return;
+                    float bm[NS];
+                    lds_row<NS>(lds.b + (r0 + J) * NP + l.q * NS, bm);
 #pragma unroll
                     for (int i = 0; i < CH; ++i) {
                         const float sj = quad_get<J % kQuad>(step[G][i]), ij = quad_get<J % kQuad>(in[G][i]);
 #pragma unroll
                         for (int s = 0; s < NS; ++s)
-                            h[J][i][s] = fmaf(__builtin_amdgcn_exp2f(sj * a2[i][s]), hp[i][s], ij * bm[s]);
+                            h[J][i][s] = fmaf(__builtin_amdgcn_exp2f(sj * a2[i][s]), J == 0 ? h0[i][s] : h[J > 0 ? J - 1 : 0][i][s], ij * bm[s]);
                     }
+                };
+                // a group's sums over the states, in each lane of the quad its part: of g B, q A and C h
+                float du[kQuad][CH], ds[kQuad][CH], sum[kQuad][CH];
+                auto clear = [&]() {
+#pragma unroll
+                    for (int j = 0; j < kQuad; ++j)
+#pragma unroll
+                        for (int i = 0; i < CH; ++i) du[j][i] = ds[j][i] = sum[j][i] = 0.0f;
                 };
                 auto backward = [&](auto j) {
                     constexpr int J = decltype(j)::value, G = J / kQuad;
-                    float hp[CH][NS];
-#pragma unroll
-                    for (int i = 0; i < CH; ++i)
-#pragma unroll
-                        for (int s = 0; s < NS; ++s) hp[i][s] = J == 0 ? h0[i][s] : h[J > 0 ? J - 1 : 0][i][s];
-                    if constexpr (EDGE) {
-                        if (t0 + J >= rows.hi) return;
-                        if ((starts | ends) >> J & 1) {
-                            bb = a.seq.find(t0 + J);
-                            if (starts >> J & 1) load_state<NS, CH>(a.init, a, l, bb, hp);
-                            if (ends >> J & 1) {
-                                load_state<NS, CH>(p.d_final, a, l, bb, r);
-#pragma unroll
-                                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                                    for (int s = 0; s < NS; ++s)
-                                        if (!l.live[i]) r[i][s] = 0.0f;
-                            }
-                        }
-                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (J >= n) return;
                     float bm[NS], cm[NS], v[2 * NS];
                     lds_row<NS>(lds.b + (r0 + J) * NP + l.q * NS, bm);
                     lds_row<NS>(lds.c + (r0 + J) * NP + l.q * NS, cm);
@@ -535,18 +532,13 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
                             u = fmaf(g, bm[s], u);
                             y = fmaf(cm[s], h[J][i][s], y);
                             r[i][s] = __builtin_amdgcn_exp2f(sj * a2[i][s]) * g;
-                            const float q = r[i][s] * hp[i][s];
+                            const float q = r[i][s] * (J == 0 ? h0[i][s] : h[J > 0 ? J - 1 : 0][i][s]);
                             w = fmaf(q, a2[i][s], w);
                             da[i][s] = fmaf(q, sj, da[i][s]);
                         }
-                        u = quad_sum(u);
-                        w = quad_sum(w);
-                        y = quad_sum(y);
-                        if (l.q == J % kQuad) {
-                            du[G][i] = u;
-                            ds[G][i] = w;
-                            sum[G][i] = y;
-                        }
+                        du[J % kQuad][i] = u;
+                        ds[J % kQuad][i] = w;
+                        sum[J % kQuad][i] = y;
                     }
 #pragma unroll
                     for (int f = 0; f < 2 * NS; f += 4) {
@@ -556,17 +548,33 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
                             lds.part[wave][J][at < NS ? l.q * NS + at : NP + l.q * NS + at - NS] = folded;
                         }
                     }
-                    if constexpr (EDGE) {
-                        if ((starts >> J & 1) && p.d_init) {
+                };
+                auto finish = [&](auto group_of_rows) {
+                    constexpr int G = decltype(group_of_rows)::value;
+                    const int t = t0 + G * kQuad;
+                    if (G * kQuad >= n) return;
+                    auto over_quad = [&](const float (&v)[kQuad][CH], int i) { return quad_sums(v[0][i], v[1][i], v[2][i], v[3][i], l.q); };
+                    float dx[CH], ddt[CH], dz[CH];
+                    const bool mine = G * kQuad + l.q < n;
 #pragma unroll
-                            for (int i = 0; i < CH; ++i)
-#pragma unroll
-                                for (int s = 0; s < NS; ++s) {
-                                    const int n = l.q * NS + s;
-                                    if (l.live[i] && n < a.states)
-                                        p.d_init[((int64_t)bb * a.channels + l.c[i]) * a.states + n] = r[i][s];
-                                }
+                    for (int i = 0; i < CH; ++i) {
+                        const float x = now[G].x.get(i), u = over_quad(du, i), w = over_quad(ds, i);
+                        dx[i] = fmaf(u, step[G][i], skip[i] * grad[G][i]);
+                        ddt[i] = fmaf(u, x, w * (1.0f / kLog2e));
+                        if (a.softplus) ddt[i] *= sigmoid(now[G].dt.get(i) + bias[i]);
+                        if (a.z) {
+                            const float z = now[G].z.get(i), sig = sigmoid(z);
+                            dz[i] = now[G].dy.get(i) * fmaf(skip[i], x, over_quad(sum, i)) * sig * fmaf(z, 1.0f - sig, 1.0f);
                         }
+                        if (mine) {
+                            dd[i] = fmaf(grad[G][i], x, dd[i]);
+                            dbias[i] += ddt[i];
+                        }
+                    }
+                    if (mine) {
+                        store_channels<T, CH>(whole.dense.at(p.dx, a.channels, t), l.live, dx);
+                        store_channels<T, CH>(whole.dense.at(p.ddt, a.channels, t), l.live, ddt);
+                        if (a.z) store_channels<T, CH>(whole.dense.at(p.dz, a.channels, t), l.live, dz);
                     }
                 };
                 using std::integral_constant;
@@ -579,52 +587,41 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
                     forward(integral_constant<int, 5>{});
                     forward(integral_constant<int, 6>{});
                     forward(integral_constant<int, 7>{});
+                    clear();
                     backward(integral_constant<int, 7>{});
                     backward(integral_constant<int, 6>{});
                     backward(integral_constant<int, 5>{});
                     backward(integral_constant<int, 4>{});
+                    finish(integral_constant<int, 1>{});
                 }
+                clear();
                 backward(integral_constant<int, 3>{});
                 backward(integral_constant<int, 2>{});
                 backward(integral_constant<int, 1>{});
                 backward(integral_constant<int, 0>{});
-            };
-            if (inside) tile(std::false_type{});
-            else tile(std::true_type{});
+                finish(integral_constant<int, 0>{});
 
+                // the waves' sums of dB and dC
+                __syncthreads();
+                for (int i = threadIdx.x; i < n * 2 * NP; i += kScanWaves * kWave) {
+                    const int j = i / (2 * NP), m = i % (2 * NP);
+                    float v = lds.part[0][j][m];
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                const int64_t row = t0 + g * kQuad + l.q;
-                if (row >= t1) continue;
-                float dx[CH], ddt[CH], dz[CH];
-#pragma unroll
-                for (int i = 0; i < CH; ++i) {
-                    const float x = now[g].x.get(i, a.wide);
-                    dx[i] = fmaf(du[g][i], step[g][i], skip[i] * grad[g][i]);
-                    ddt[i] = fmaf(du[g][i], x, ds[g][i] * (1.0f / kLog2e));
-                    if (a.softplus) ddt[i] *= sigmoid(now[g].dt.get(i, a.wide) + bias[i]);
-                    if (a.z) {
-                        const float z = now[g].z.get(i, a.wide), sig = sigmoid(z);
-                        dz[i] = now[g].dy.get(i, a.wide) * fmaf(skip[i], x, sum[g][i]) * sig * fmaf(z, 1.0f - sig, 1.0f);
-                    }
-                    dd[i] = fmaf(grad[g][i], x, dd[i]);
-                    dbias[i] += ddt[i];
+                    for (int w = 1; w < kScanWaves; ++w) v += lds.part[w][j][m];
+                    p.dbc[(((int64_t)group_block * a.seq.tokens + t0 + j) * p.groups + group) * (2 * NP) + m] = v;
                 }
-                store_channels<CH>(static_cast<T*>(p.dx) + row * a.channels, l.c0, l.live, dx, a.wide);
-                store_channels<CH>(static_cast<T*>(p.ddt) + row * a.channels, l.c0, l.live, ddt, a.wide);
-                if (a.z) store_channels<CH>(static_cast<T*>(p.dz) + row * a.channels, l.c0, l.live, dz, a.wide);
+                __syncthreads();
             }
-
-            // the waves' sums of dB and dC
-            __syncthreads();
-            for (int i = threadIdx.x; i < (t1 - t0) * 2 * NP; i += kScanWaves * kWave) {
-                const int j = i / (2 * NP), n = i % (2 * NP);
-                float v = lds.part[0][j][n];
+            if (p.d_init && from == first) {
 #pragma unroll
-                for (int w = 1; w < kScanWaves; ++w) v += lds.part[w][j][n];
-                p.dbc[(((int64_t)group_block * a.seq.tokens + t0 + j) * p.groups + group) * (2 * NP) + n] = v;
+                for (int i = 0; i < CH; ++i)
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        const int m = l.q * NS + s;
+                        if (l.live[i] && m < a.states) p.d_init[((int64_t)b * a.channels + (l.c + i)) * a.states + m] = r[i][s];
+                    }
             }
-            __syncthreads();
+            stop = from;
         }
     }
 
@@ -633,7 +630,7 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
         dd[i] = quad_sum(dd[i]);
         dbias[i] = quad_sum(dbias[i]);
         if (!l.live[i]) continue;
-        const int64_t at = (int64_t)chunk * a.channels + l.c[i];
+        const int64_t at = (int64_t)chunk * a.channels + (l.c + i);
 #pragma unroll
         for (int s = 0; s < NS; ++s) p.da_part[at * NP + l.q * NS + s] = da[i][s];
         if (l.q == 0) {
@@ -705,7 +702,7 @@ size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 BwdPlan plan_bwd(const im2win_scan_desc* d) {
     BwdPlan p;
     int64_t tile = 8;
-    with_states(d->states, [&](auto ns, auto ch) {
+    with_states(d->states, d->channels, [&](auto ns, auto ch) {
         p.ns = decltype(ns)::value;
         p.ch = decltype(ch)::value;
         p.chunk = kChunkRows<decltype(ns)::value>;
@@ -780,8 +777,6 @@ int im2win_selective_scan_backward(const im2win_scan_desc* d, const void* dy, co
     b.s.init = initial_state;
     b.s.seq = make_seq_map(d->tokens, d->sequences, seq_starts);
     b.s.chunk = (int)p.chunk; b.s.chunks = (int)p.chunks;
-    const size_t pair = 2 * e;
-    b.s.wide = b.s.wide && aligned_to(dy, pair) && aligned_to(dx, pair) && aligned_to(ddt, pair) && aligned_to(dz, pair);
     b.dy = dy; b.d_final = d_final_state; b.dx = dx; b.ddt = ddt; b.dA = dA; b.dB = dB; b.dC = dC; b.dD = dD;
     b.dz = dz; b.ddt_bias = ddt_bias; b.d_init = d_initial_state;
     b.groups = (int)d->groups;
@@ -808,7 +803,7 @@ int im2win_selective_scan_backward(const im2win_scan_desc* d, const void* dy, co
     int hip = 0;
     with_type(d->dtype, [&](auto t) {
         using T = decltype(t);
-        with_states(d->states, [&](auto ns, auto ch) {
+        with_states(d->states, d->channels, [&](auto ns, auto ch) {
             constexpr int NS = decltype(ns)::value, CH = decltype(ch)::value;
             const dim3 threads(kScanWaves * kWave);
             if (p.chunks > 1) {
