@@ -46,8 +46,9 @@ struct ScanArgs {
     int* flags;            // [chunks]
 };
 
-// flags: the chunk's last sequence goes on behind it / began inside it
-constexpr int kGoesOn = 1, kBegan = 2;
+// flags of a chunk: its last sequence goes on behind it / its first sequence
+// began before it / both of one sequence that fills the chunk
+constexpr int kGoesOn = 1, kFromBefore = 2, kThrough = 4;
 
 template <int J>
 __device__ __forceinline__ float quad_get(float v) {   // the value of the quad's lane J
@@ -194,6 +195,68 @@ __device__ __forceinline__ void stage(float* lds, const T* m, int64_t ld, int gr
         lds[i] = r < n && s < states ? (float)m[(int64_t)(t + r) * ld + group_offset + s] : 0.0f;
     }
 }
+
+// What the chunks leave to one another, for one channel and state: walks the
+// `chunks` values m[i * each + e] from the first to the last (or the other way)
+// and turns each one that `reads` marks into own + exp(A S) * (the one before),
+// where one sequence passes through the chunk, and own otherwise.  The walk is
+// cut into gridDim.y pieces; each begins at the first chunk of its own that
+// takes nothing from the one before, and goes on to the next piece's beginning.
+// It waits for memory, not for arithmetic: kCarryBatch chunks are loaded while
+// the ones before them are worked on.  Threads that are not live take part in
+// the search for the beginning and write nothing: what they read may be written
+// by the thread whose value it is.
+constexpr int kCarryBatch = 16;
+
+__device__ __forceinline__ void carry_walk(float* m, const ScanArgs& a, int64_t each, int64_t e, int c, float a2, bool live, bool forward, int reads) {
+    const int n = a.chunks, piece = blockIdx.y, pieces = gridDim.y;
+    auto place = [&](int i) { return forward ? i : n - 1 - i; };
+    const int from = (int)((int64_t)n * piece / pieces), to = (int)((int64_t)n * (piece + 1) / pieces);
+    int begin = to;
+    for (int i = from; i < to; i += kWave) {
+        const int k = i + (int)(threadIdx.x % kWave);
+        const uint64_t fresh = __ballot(k < to && !(a.flags[place(min(k, to - 1))] & kThrough));
+        if (fresh) {
+            begin = i + __builtin_ctzll(fresh);
+            break;
+        }
+    }
+    if (begin >= to) return;
+    constexpr int U = kCarryBatch;
+    float own[U], span[U], next_own[U], next_span[U];
+    int f[U], next_f[U];
+    auto load = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t at = place(min(i0 + u, n - 1));
+            next_f[u] = uniform(a.flags[at]);
+            next_own[u] = m[at * each + e];      // of any value where nothing reads it
+            next_span[u] = a.span[at * a.channels + c];
+        }
+    };
+    float v = 0.0f;
+    load(begin);
+    for (int i0 = begin; i0 < n; i0 += U) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            f[u] = next_f[u];
+            own[u] = next_own[u];
+            span[u] = next_span[u];
+        }
+        if (i0 + U < n) load(i0 + U);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = i0 + u;
+            if (i >= n || (i >= to && !(f[u] & kThrough))) return;
+            if (!(f[u] & reads)) continue;
+            v = f[u] & kThrough ? fmaf(__builtin_amdgcn_exp2f(a2 * span[u]), v, own[u]) : own[u];
+            if (live) m[place(i) * each + e] = v;
+        }
+    }
+}
+
+// Pieces of that walk: short ones find their beginning soon, where sequences end often
+inline unsigned carry_pieces(int64_t chunks) { return (unsigned)(chunks < 16 ? 1 : chunks / 8 < 32 ? chunks / 8 : 32); }
 
 // Compiled shapes: f(NS, CH) for N states of D channels.  Up to 24 states a lane
 // holds a pair of channels; a single channel has no neighbour to read.

@@ -68,7 +68,7 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
     int first = a.seq.first(b), end = a.seq.first(b + 1);
     if constexpr (SUMMARY) {
         if (block == 0 && threadIdx.x == 0)
-            a.flags[chunk] = (end > hi ? kGoesOn : 0) | (first >= lo ? kBegan : 0);
+            a.flags[chunk] = end <= hi ? 0 : first < lo ? kGoesOn | kThrough : kGoesOn;
         if (end <= hi) return;
         lo = max(lo, first);
     }
@@ -217,35 +217,13 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
     }
 }
 
-// The states behind the chunks from the chunks' own: one thread per channel
-// and state walks the chunks.  The loads of eight chunks do not wait for one
-// another.
+// The states behind the chunks from the chunks' own: a thread per channel and state
 __global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a, int padded) {
     const int64_t each = (int64_t)a.channels * padded;
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= each) return;
+    const int64_t own = (int64_t)blockIdx.x * 256 + threadIdx.x, e = min(own, each - 1);
     const int c = (int)(e / padded), n = (int)(e % padded);
     const float a2 = n < a.states ? kLog2e * a.A[(int64_t)c * a.states + n] : 0.0f;
-    constexpr int U = 8;
-    float h = 0.0f;
-    for (int k = 0; k < a.chunks - 1; k += U) {
-        const int m = min(U, a.chunks - 1 - k);
-        float own[U], decay[U];
-        int f[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t at = k + min(u, m - 1);
-            f[u] = a.flags[at];
-            own[u] = f[u] & kGoesOn ? a.carry[at * each + e] : 0.0f;
-            decay[u] = f[u] == kGoesOn ? __builtin_amdgcn_exp2f(a2 * a.span[at * a.channels + c]) : 0.0f;
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (u >= m || !(f[u] & kGoesOn)) continue;
-            h = f[u] & kBegan ? own[u] : fmaf(decay[u], h, own[u]);
-            a.carry[(k + u) * each + e] = h;
-        }
-    }
+    carry_walk(a.carry, a, each, e, c, a2, own < each, true, kGoesOn);
 }
 
 // ---------------------------------------------------------------------------
@@ -256,73 +234,74 @@ struct ScanStepArgs {
     const int32_t* slots;
     float* state;
     int64_t state_slots;
-    int whole;          // states are NS whole floats for every lane, on their boundaries
 };
 
-template <typename T, int NS>
+// R requests per workgroup.  Bound by the states' traffic: every load is made
+// before the first wait, so absent arrays and slots read memory that is there
+// (x for z, A for the vectors of channels, the pool's first state) and drop it.
+// WHOLE: the states are NS for every lane of the quad.
+template <typename T, int NS, int R, bool WHOLE>
 __global__ __launch_bounds__(kScanWaves * kWave) void scan_step_kernel(ScanStepArgs p) {
     const ScanArgs& a = p.a;
-    const int64_t row = blockIdx.x;
     const int q = threadIdx.x % kQuad;
     const int c_own = ((int)blockIdx.y * kScanWaves * kWave + (int)threadIdx.x) / kQuad;
     const bool live = c_own < a.channels;
     const int c = live ? c_own : 0;
-    T* y = static_cast<T*>(a.y) + row * a.channels + c;
-    const int64_t slot = p.slots ? (int64_t)p.slots[row] : row;
-    if (slot < 0 || slot >= p.state_slots) {
-        if (live && q == 0) *y = (T)0.0f;
-        return;
-    }
-    float* state = p.state + (slot * a.channels + c) * a.states + q * NS;
-    const float* arow = a.A + (int64_t)c * a.states + q * NS;
-    const int g = c / a.group_channels * a.states + q * NS;
-    const T* bm = static_cast<const T*>(a.B) + row * a.ld_b + g;
-    const T* cm = static_cast<const T*>(a.C) + row * a.ld_c + g;
-    float h[NS], a2[NS];
-    if (p.whole) {
-        lds_row<NS>(state, h);
-        lds_row<NS>(arow, a2);
-    } else {
-#pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const bool in = q * NS + s < a.states;
-            h[s] = in ? state[s] : 0.0f;
-            a2[s] = in ? arow[s] : 0.0f;
-        }
-    }
-    const float x = (float)(static_cast<const T*>(a.x) + row * a.ld_x)[c];
-    float step = (float)(static_cast<const T*>(a.dt) + row * a.ld_dt)[c] + (a.dt_bias ? a.dt_bias[c] : 0.0f);
-    if (a.softplus) step = softplus(step);
-    const float in = step * x;
-    float sum = 0.0f;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-        const bool exists = p.whole || q * NS + s < a.states;
-        const float bv = exists ? (float)bm[s] : 0.0f, cv = exists ? (float)cm[s] : 0.0f;
-        h[s] = fmaf(__builtin_amdgcn_exp2f(step * (kLog2e * a2[s])), h[s], in * bv);
-        sum = fmaf(cv, h[s], sum);
-    }
-    sum = quad_sum(sum);
-    if (!live) return;
-    if (p.whole) {
-        if constexpr (NS % 4 == 0) {
-            store_run<NS>(state, h);
+    const int64_t g = (int64_t)(c / a.group_channels) * a.states + q * NS;
+    auto load = [&](const auto* m, auto (&v)[NS]) {
+        if constexpr (WHOLE) {
+            __builtin_memcpy(v, m, sizeof v);
         } else {
 #pragma unroll
-            for (int s = 0; s < NS; s += 2) *reinterpret_cast<float2*>(state + s) = make_float2(h[s], h[s + 1]);
+            for (int s = 0; s < NS; ++s) v[s] = q * NS + s < a.states ? m[s] : 0;
         }
-    } else {
+    };
+    int64_t place[R];
+    bool there[R];
+    float h[R][NS], a2[NS];
+    T x[R], dt[R], z[R], bm[R][NS], cm[R][NS];
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
-            if (q * NS + s < a.states) state[s] = h[s];
+    for (int k = 0; k < R; ++k) {
+        const int64_t row = min((int64_t)blockIdx.x * R + k, (int64_t)a.seq.tokens - 1);
+        const int64_t slot = p.slots ? (int64_t)p.slots[row] : row;
+        there[k] = slot >= 0 && slot < p.state_slots;
+        place[k] = ((there[k] ? slot : 0) * a.channels + c) * a.states + q * NS;
+        x[k] = (static_cast<const T*>(a.x) + row * a.ld_x)[c];
+        dt[k] = (static_cast<const T*>(a.dt) + row * a.ld_dt)[c];
+        z[k] = (a.z ? static_cast<const T*>(a.z) + row * a.ld_z : static_cast<const T*>(a.x) + row * a.ld_x)[c];
+        load(static_cast<const T*>(a.B) + row * a.ld_b + g, bm[k]);
+        load(static_cast<const T*>(a.C) + row * a.ld_c + g, cm[k]);
     }
-    if (q == 0) {
-        if (a.D) sum = fmaf(a.D[c], x, sum);
-        if (a.z) {
-            const float z = (float)(static_cast<const T*>(a.z) + row * a.ld_z)[c];
-            sum *= z * sigmoid(z);
+    load(a.A + (int64_t)c * a.states + q * NS, a2);
+    const float bias = (a.dt_bias ? a.dt_bias : a.A)[c], skip = (a.D ? a.D : a.A)[c];
+#pragma unroll
+    for (int k = 0; k < R; ++k) load(p.state + place[k], h[k]);
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+        const int64_t row = (int64_t)blockIdx.x * R + k;
+        float step = (float)dt[k] + (a.dt_bias ? bias : 0.0f);
+        if (a.softplus) step = softplus(step);
+        const float in = step * (float)x[k];
+        float sum = 0.0f;
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+            h[k][s] = fmaf(__builtin_amdgcn_exp2f(step * (kLog2e * a2[s])), h[k][s], in * (float)bm[k][s]);
+            sum = fmaf((float)cm[k][s], h[k][s], sum);
         }
-        *y = (T)sum;
+        sum = quad_sum(sum);
+        if (a.D) sum = fmaf(skip, (float)x[k], sum);
+        if (a.z) sum *= (float)z[k] * sigmoid((float)z[k]);
+        if (!live || row >= a.seq.tokens) continue;
+        if (there[k]) {
+            if constexpr (WHOLE) {
+                __builtin_memcpy(p.state + place[k], h[k], sizeof h[k]);
+            } else {
+#pragma unroll
+                for (int s = 0; s < NS; ++s)
+                    if (q * NS + s < a.states) p.state[place[k] + s] = h[k][s];
+            }
+        }
+        if (q == 0) static_cast<T*>(a.y)[row * a.channels + c] = (T)(there[k] ? sum : 0.0f);
     }
 }
 
@@ -476,7 +455,10 @@ int im2win_selective_scan(const im2win_scan_desc* d, const void* x, const void* 
             if (p.chunks > 1 && !whole) {
                 hipLaunchKernelGGL((scan_kernel<T, NS, CH, true>), dim3((unsigned)(p.blocks * (p.chunks - 1))), threads, 0, s, a);
                 const int64_t each = (int64_t)a.channels * kQuad * NS;
-                hipLaunchKernelGGL(scan_carry_kernel, dim3((unsigned)((each + 255) / 256)), dim3(256), 0, s, a, kQuad * NS);
+                ScanArgs before = a;      // the last chunk leaves nothing to another
+                --before.chunks;
+                hipLaunchKernelGGL(scan_carry_kernel, dim3((unsigned)((each + 255) / 256), carry_pieces(before.chunks)), dim3(256), 0, s,
+                                   before, kQuad * NS);
             }
             hipLaunchKernelGGL((scan_kernel<T, NS, CH, false>), dim3((unsigned)(grid + extra)), threads, 0, s, a);
         });
@@ -498,15 +480,26 @@ int im2win_selective_scan_step(const im2win_scan_desc* d, const void* x, const v
     ScanStepArgs p{};
     p.a = scan_args(d, x, dt, A, B, C, D, z, dt_bias, 1);
     p.a.y = y;
-    p.slots = slots; p.state = state; p.state_slots = state_slots;
+    p.a.seq.tokens = (int)d->tokens;
+    p.slots = slots; p.state_slots = state_slots;
+    p.state = state_slots ? state : const_cast<float*>(A);     // as large as one state; read, and not written without slots
     const unsigned cover = (unsigned)((d->channels * kQuad + kScanWaves * kWave - 1) / (kScanWaves * kWave));
+    const hipStream_t s = static_cast<hipStream_t>(stream);
     with_type(d->dtype, [&](auto t) {
         with_states(d->states, d->channels, [&](auto ns, auto) {
             using T = decltype(t);
             constexpr int NS = decltype(ns)::value;
-            p.whole = d->states == kQuad * NS && aligned_to(A, 16) && aligned_to(state, 16);
-            hipLaunchKernelGGL((scan_step_kernel<T, NS>), dim3((unsigned)d->tokens, cover), dim3(kScanWaves * kWave), 0,
-                               static_cast<hipStream_t>(stream), p);
+            auto launch = [&](auto r, auto whole) {
+                constexpr int R = decltype(r)::value;
+                hipLaunchKernelGGL((scan_step_kernel<T, NS, R, decltype(whole)::value>),
+                                   dim3((unsigned)((d->tokens + R - 1) / R), cover), dim3(kScanWaves * kWave), 0, s, p);
+            };
+            auto with_whole = [&](auto r) {
+                if (d->states == kQuad * NS) launch(r, std::true_type{});
+                else launch(r, std::false_type{});
+            };
+            if (NS <= 8 && d->tokens / 2 * cover >= 2048) with_whole(std::integral_constant<int, NS <= 8 ? 2 : 1>{});
+            else with_whole(std::integral_constant<int, 1>{});
         });
     });
     return launched("selective_scan_step");

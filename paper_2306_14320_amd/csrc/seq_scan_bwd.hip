@@ -45,10 +45,6 @@ struct ScanBwdArgs {
     int groups;
 };
 
-// flags beside kGoesOn and kBegan: the chunk's first sequence began before it /
-// and goes on behind it, so that the chunk is inside one sequence
-constexpr int kFromBefore = 4, kThrough = 8;
-
 // Rows of a tile whose states are in registers, and of a chunk (whose tiles'
 // first states, B and C lie in LDS)
 template <int NS> constexpr int kTileRows = NS >= 16 || NS == 6 ? 4 : 8;
@@ -147,7 +143,7 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_bwd_summary_kernel(Sc
         end0 = a.seq.first(b0 + 1);
         first1 = a.seq.first(b1);
         const int first0 = a.seq.first(b0), end1 = a.seq.first(b1 + 1);
-        flags = (end1 > rows.hi ? kGoesOn : 0) | (first1 >= rows.lo ? kBegan : 0) | (first0 < rows.lo ? kFromBefore : 0);
+        flags = (end1 > rows.hi ? kGoesOn : 0) | (first0 < rows.lo ? kFromBefore : 0);
         if (first0 < rows.lo && end0 > rows.hi) flags |= kThrough;
     }
     if (block == 0 && threadIdx.x == 0) a.flags[chunk] = flags;
@@ -263,40 +259,17 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_bwd_summary_kernel(Sc
 }
 
 // ---------------------------------------------------------------------------
-// 2. The states behind the chunks (blockIdx.y 0) and the gradients of the
+// 2. The states behind the chunks (blockIdx.z 0) and the gradients of the
 // states before them (1): one thread per channel and state.
 // ---------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void scan_bwd_carry_kernel(ScanBwdArgs p, int padded) {
     const ScanArgs& a = p.s;
     const int64_t each = (int64_t)a.channels * padded;
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= each) return;
+    const int64_t own = (int64_t)blockIdx.x * 256 + threadIdx.x, e = min(own, each - 1);
     const int c = (int)(e / padded), n = (int)(e % padded);
     const float a2 = n < a.states ? kLog2e * a.A[(int64_t)c * a.states + n] : 0.0f;
-    constexpr int U = 8;
-    const bool forward = blockIdx.y == 0;
-    float* m = forward ? a.carry : p.back;
-    const int reads = forward ? kGoesOn : kFromBefore;
-    float v = 0.0f;
-    for (int k = 0; k < a.chunks; k += U) {
-        float own[U], decay[U];
-        int f[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = min(k + u, a.chunks - 1);
-            const int64_t at = forward ? i : a.chunks - 1 - i;
-            f[u] = a.flags[at];
-            own[u] = f[u] & reads ? m[at * each + e] : 0.0f;
-            decay[u] = f[u] & kThrough ? __builtin_amdgcn_exp2f(a2 * a.span[at * a.channels + c]) : 0.0f;
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (k + u >= a.chunks || !(f[u] & reads)) continue;
-            const int64_t at = forward ? k + u : a.chunks - 1 - (k + u);
-            v = f[u] & kThrough ? fmaf(decay[u], v, own[u]) : own[u];
-            m[at * each + e] = v;
-        }
-    }
+    if (blockIdx.z == 0) carry_walk(a.carry, a, each, e, c, a2, own < each, true, kGoesOn);
+    else carry_walk(p.back, a, each, e, c, a2, own < each, false, kFromBefore);
 }
 
 // ---------------------------------------------------------------------------
@@ -808,7 +781,7 @@ int im2win_selective_scan_backward(const im2win_scan_desc* d, const void* dy, co
             const dim3 threads(kScanWaves * kWave);
             if (p.chunks > 1) {
                 hipLaunchKernelGGL((scan_bwd_summary_kernel<T, NS, CH>), dim3((unsigned)grid), threads, 0, s, b);
-                hipLaunchKernelGGL(scan_bwd_carry_kernel, dim3((unsigned)((d->channels * np + 255) / 256), 2), dim3(256), 0, s,
+                hipLaunchKernelGGL(scan_bwd_carry_kernel, dim3((unsigned)((d->channels * np + 255) / 256), carry_pieces(p.chunks), 2), dim3(256), 0, s,
                                    b, (int)np);
             }
             if (grid + extra) {
