@@ -188,39 +188,40 @@ def _device_of(t, name):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     dev = t.get_device()
-    if dev != torch.cuda.current_device():
+    if dev != torch._C._cuda_getDevice():
         raise ValueError(f"{name} is on device {dev}, the current device is {torch.cuda.current_device()}")
     return dev
 
 
-def _matches(t, name, shape, dtype, dev):
-    """Raises unless t is a tensor of this shape and dtype on the device."""
+def _refuse(t, name, shape, dtype, dev, layout):
+    """Says what is wrong with t, which no fast check accepted."""
     if not isinstance(t, torch.Tensor) or t.get_device() != dev:
         raise ValueError(f"{name} must be a tensor on device {dev}")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, the call needs {shape}")
     if t.dtype != dtype:
         raise ValueError(f"{name} has dtype {t.dtype}, the call needs {dtype}")
+    raise ValueError(f"{name} {layout}")
 
 
 def _rows(t, name, shape, dtype, ld, dev):
     """Pointer of a T x ... input whose rows are ld elements apart."""
-    _matches(t, name, shape, dtype, dev)
-    strides = t.stride()
-    if strides[-1] != 1 or strides[0] != ld or len(shape) > 2:     # the common case is settled
-        if _row_stride(t, name) != ld and shape[0] > 1:
-            raise ValueError(f"{name} has rows {strides[0]} elements apart, the descriptor says {ld}")
-    return t.data_ptr()
+    if isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == dev:
+        strides = t.stride()
+        if strides[0] == ld and strides[-1] == 1 and len(strides) == 2:     # the common case
+            return t.data_ptr()
+        if _row_stride(t, name) == ld or shape[0] <= 1:
+            return t.data_ptr()
+    return _refuse(t, name, shape, dtype, dev, f"has rows that are not {ld} elements apart, as the descriptor says")
 
 
 def _dense(t, name, shape, dtype, dev):
     """Pointer of a contiguous tensor; None stays None."""
     if t is None:
         return None
-    _matches(t, name, shape, dtype, dev)
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    if isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.is_contiguous() and t.get_device() == dev:
+        return t.data_ptr()
+    return _refuse(t, name, shape, dtype, dev, "must be contiguous")
 
 
 def _new(shape, dtype, like, stream):
