@@ -35,15 +35,38 @@ struct SeqMap {
         const int s = uniform(starts[b]);
         return s < 0 ? 0 : s > tokens ? tokens : s;
     }
-    // The sequence that holds row t, for first(0) <= t < first(count).
-    __device__ int find(int t) const {
-        if (!starts) return t / len;
-        int lo = 0, hi = count;        // starts[lo] <= t < starts[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (first(mid) <= t) lo = mid; else hi = mid;
+    // The sequence that holds row t, for first(0) <= t < first(count), and its
+    // rows.  The wave's lanes, all of them active, look at 64 starts at a time,
+    // so that up to 63 sequences take one load's latency and 4000 two.
+    struct Found {
+        int b, first, end;
+    };
+    __device__ Found at(int t) const {
+        Found f;
+        if (!starts) {
+            f.b = t / len;
+            f.first = f.b * len;
+            f.end = f.first + len;
+            return f;
         }
-        return lo;
+        const int lane = threadIdx.x % kWave;
+        auto look = [&](int i) {
+            const int s = starts[i < count ? i : count];
+            return s < 0 ? 0 : s > tokens ? tokens : s;
+        };
+        int lo = 0, n = count;         // one of the sequences [lo, lo + n); starts[lo] <= t
+        while (n > kWave - 1) {
+            const int step = (n + kWave - 2) / (kWave - 1);
+            const uint64_t before = __ballot(look(lo + lane * step) <= t) | 1;
+            lo += (63 - __builtin_clzll(before)) * step;
+            n = count - lo < step ? count - lo : step;
+        }
+        const int s = look(lo + lane);
+        const int k = 63 - __builtin_clzll(__ballot(lane < n && s <= t) | 1);
+        f.b = lo + k;
+        f.first = __builtin_amdgcn_readlane(s, k);
+        f.end = __builtin_amdgcn_readlane(s, k + 1);
+        return f;
     }
 };
 

@@ -64,8 +64,9 @@ __device__ __forceinline__ void load_input(const T* x, const T* init, int64_t ld
     }
 }
 
-// The first of a lane's V channels.  Lanes past the last V channels take those
-// (several lanes then compute and store the same values) or none.
+// The first of a lane's V channels, and whether the lane stores anything.  A
+// last lane with fewer than V channels of its own takes the row's last V (two
+// lanes then compute and store the same values); lanes past it read them only.
 template <int V>
 __device__ __forceinline__ bool lane_channels(int group, int lane, int channels, int* c) {
     const int own = (group * kWave + lane) * V;
@@ -82,7 +83,7 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_kernel(Conv1dArgs a
     T* y = static_cast<T*>(a.y);
     const int64_t tile = (int64_t)(blockIdx.x / a.groups) * kConvWaves + uniform(threadIdx.x / kWave);
     int c;
-    if (!lane_channels<V>(blockIdx.x % a.groups, threadIdx.x % kWave, a.channels, &c)) return;
+    const bool live = lane_channels<V>(blockIdx.x % a.groups, threadIdx.x % kWave, a.channels, &c);
 
     if (tile >= a.tiles) {
         // one row of a final state: input e of the sequence with its W-1 earlier ones in front
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_kernel(Conv1dArgs a
             const int first = a.seq.first(b), end = max(a.seq.first(b + 1), first);
             float v[V];
             load_input<T, V, W>(x, init, a.ld_x, a.channels, b, first, end, W - 1 - j, c, v);
-            store_vec<V>(static_cast<T*>(a.final_state) + row * a.channels + c, v);
+            if (live) store_vec<V>(static_cast<T*>(a.final_state) + row * a.channels + c, v);
         }
         return;
     }
@@ -103,17 +104,16 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_kernel(Conv1dArgs a
     if (lo >= hi) return;
     Taps<T, V, W> taps;
     taps.load(static_cast<const T*>(a.w), static_cast<const T*>(a.bias), c);
-    int b = a.seq.find(lo);
-    int first = a.seq.first(b), end = a.seq.first(b + 1);
+    SeqMap::Found in_seq = a.seq.at(lo);
 
     auto finish = [&](int t, float (&acc)[V]) {
         if (a.silu)
 #pragma unroll
             for (int v = 0; v < V; ++v) acc[v] *= sigmoid(acc[v]);
-        store_vec<V>(y + (int64_t)t * a.channels + c, acc);
+        if (live) store_vec<V>(y + (int64_t)t * a.channels + c, acc);
     };
 
-    if (lo == t0 && hi == t0 + kConvTile && end >= hi && lo - first >= W - 1) {
+    if (lo == t0 && hi == t0 + kConvTile && in_seq.end >= hi && lo - in_seq.first >= W - 1) {
         // the tile and the rows before it lie in one sequence
         Bits<T, V> in[kConvTile + W - 1];
         const T* p = x + (int64_t)(t0 - (W - 1)) * a.ld_x + c;
@@ -133,18 +133,14 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_kernel(Conv1dArgs a
         return;
     }
     for (int t = lo; t < hi; ++t) {
-        if (t >= end) {
-            b = a.seq.find(t);
-            first = a.seq.first(b);
-            end = a.seq.first(b + 1);
-        }
+        if (t >= in_seq.end) in_seq = a.seq.at(t);
         float acc[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) acc[v] = taps.bias[v];
 #pragma unroll
         for (int k = 0; k < W; ++k) {
             float in[V];
-            load_input<T, V, W>(x, init, a.ld_x, a.channels, b, first, t, W - 1 - k, c, in);
+            load_input<T, V, W>(x, init, a.ld_x, a.channels, in_seq.b, in_seq.first, t, W - 1 - k, c, in);
 #pragma unroll
             for (int v = 0; v < V; ++v) acc[v] = fmaf(taps.w[k][v], in[v], acc[v]);
         }
@@ -226,8 +222,8 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_bwd_kernel(Conv1dBw
     const int lo = (int)max<int64_t>(a.seq.first(0), s0);
     const int hi = (int)min<int64_t>(a.seq.first(a.seq.count), s0 + a.stripe);
     for (int t = lo; t < hi;) {
-        const int b = a.seq.find(t);
-        const int first = a.seq.first(b), end = max(a.seq.first(b + 1), t + 1);
+        const SeqMap::Found in_seq = a.seq.at(t);
+        const int b = in_seq.b, first = in_seq.first, end = max(in_seq.end, t + 1);
         const int own = min(end, hi);        // rows [t, own) of this sequence are the stripe's
         float win[W][V], g[W][V] = {};
 #pragma unroll

@@ -186,6 +186,19 @@ struct RowPlace {
     }
 };
 
+// A lane's quarter of the N floats at m; states past N are zero
+template <int NS>
+__device__ __forceinline__ void load_states(const float* m, int q, int states, float (&v)[NS]) {
+    if (states == kQuad * NS) {
+        __builtin_memcpy(v, m + q * NS, sizeof v);
+    } else {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) v[s] = m[min(q * NS + s, states - 1)];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) v[s] = q * NS + s < states ? v[s] : 0.0f;
+    }
+}
+
 // B or C of rows [t, t + n), n <= kScanTile, as fp32; states past N and rows past n are zero
 template <typename T, int NS>
 __device__ __forceinline__ void stage(float* lds, const T* m, int64_t ld, int group_offset, int states, int t, int n) {
@@ -229,7 +242,7 @@ __device__ __forceinline__ void carry_walk(float* m, const ScanArgs& a, int64_t 
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t at = place(min(i0 + u, n - 1));
-            next_f[u] = uniform(a.flags[at]);
+            next_f[u] = a.flags[at];
             next_own[u] = m[at * each + e];      // of any value where nothing reads it
             next_span[u] = a.span[at * a.channels + c];
         }
@@ -247,9 +260,10 @@ __device__ __forceinline__ void carry_walk(float* m, const ScanArgs& a, int64_t 
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int i = i0 + u;
-            if (i >= n || (i >= to && !(f[u] & kThrough))) return;
-            if (!(f[u] & reads)) continue;
-            v = f[u] & kThrough ? fmaf(__builtin_amdgcn_exp2f(a2 * span[u]), v, own[u]) : own[u];
+            const int flags = uniform(f[u]);
+            if (i >= n || (i >= to && !(flags & kThrough))) return;
+            if (!(flags & reads)) continue;
+            v = flags & kThrough ? fmaf(__builtin_amdgcn_exp2f(a2 * span[u]), v, own[u]) : own[u];
             if (live) m[place(i) * each + e] = v;
         }
     }

@@ -64,8 +64,9 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
         if (SUMMARY && block == 0 && threadIdx.x == 0) a.flags[chunk] = 0;
         return;
     }
-    int b = a.seq.find(SUMMARY ? hi - 1 : lo);
-    int first = a.seq.first(b), end = a.seq.first(b + 1);
+    const SeqMap::Found found = a.seq.at(SUMMARY ? hi - 1 : lo);
+    const int first = found.first;
+    int b = found.b, end = found.end;
     if constexpr (SUMMARY) {
         if (block == 0 && threadIdx.x == 0)
             a.flags[chunk] = end <= hi ? 0 : first < lo ? kGoesOn | kThrough : kGoesOn;
@@ -82,20 +83,20 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
     for (int i = 0; i < CH; ++i) {
         bias[i] = a.dt_bias ? a.dt_bias[l.c + i] : 0.0f;
         skip[i] = !SUMMARY && a.D ? a.D[l.c + i] : 0.0f;
+        load_states<NS>(a.A + (int64_t)(l.c + i) * a.states, l.q, a.states, a2[i]);
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const int n = l.q * NS + s;
-            a2[i][s] = n < a.states ? kLog2e * a.A[(int64_t)(l.c + i) * a.states + n] : 0.0f;
-        }
+        for (int s = 0; s < NS; ++s) a2[i][s] *= kLog2e;
     }
     auto begin = [&]() {     // the state before the first row of sequence b
 #pragma unroll
-        for (int i = 0; i < CH; ++i)
+        for (int i = 0; i < CH; ++i) {
+            if (init) {
+                load_states<NS>(init + ((int64_t)b * a.channels + l.c + i) * a.states, l.q, a.states, h[i]);
+            } else {
 #pragma unroll
-            for (int s = 0; s < NS; ++s) {
-                const int n = l.q * NS + s;
-                h[i][s] = init && n < a.states ? init[((int64_t)b * a.channels + (l.c + i)) * a.states + n] : 0.0f;
+                for (int s = 0; s < NS; ++s) h[i][s] = 0.0f;
             }
+        }
     };
     if (lo == first) {
         begin();
@@ -166,8 +167,9 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
                     }
             };
             auto advance = [&](int row) {
-                b = a.seq.find(row);
-                end = a.seq.first(b + 1);
+                const SeqMap::Found next_seq = a.seq.at(row);
+                b = next_seq.b;
+                end = next_seq.end;
                 begin();
             };
             using std::integral_constant;
@@ -316,9 +318,11 @@ struct ScanPlan {
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-// The chunk: as long as leaves about three waves for each of the chip's 1024
-// SIMDs, but no shorter than two tiles; equal sequences are cut into equal
-// parts, or taken whole where they are shorter.
+// The chunk: as long as leaves about four waves for each of the chip's 1024
+// SIMDs (8192 x 2048 x 16: 182 us with two, 167 with three, 163 with four), but
+// no shorter than 16 rows (160 x 512 x 16: 42 us with 64 rows, 28 with 32, 22
+// with 16); up to 64 rows one chunk is as fast as three kernels.  Equal
+// sequences are cut into equal parts, or taken whole where they are shorter.
 ScanPlan plan_scan(const im2win_scan_desc* d) {
     ScanPlan p;
     with_states(d->states, d->channels, [&](auto ns, auto ch) {
@@ -329,8 +333,8 @@ ScanPlan plan_scan(const im2win_scan_desc* d) {
     const int64_t group = d->channels / d->groups;
     p.blocks = d->groups * ((group + per_block - 1) / per_block);
     if (d->tokens == 0) return p;
-    const int64_t want = (3072 + p.blocks * kScanWaves - 1) / (p.blocks * kScanWaves);
-    p.chunk = std::max<int64_t>((d->tokens + want - 1) / want, 2 * kScanTile);
+    const int64_t want = (4096 + p.blocks * kScanWaves - 1) / (p.blocks * kScanWaves);
+    p.chunk = d->tokens <= 64 ? d->tokens : std::max<int64_t>((d->tokens + want - 1) / want, 16);
     const int64_t len = d->tokens / d->sequences;
     if (d->tokens % d->sequences == 0 && d->sequences > 1) {
         if (len <= p.chunk) {

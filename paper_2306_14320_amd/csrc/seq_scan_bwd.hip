@@ -72,23 +72,21 @@ struct ChunkRows {
 template <int NS, int CH>
 __device__ __forceinline__ void load_state(const float* m, const ScanArgs& a, const Lane<CH>& l, int b, float (&h)[CH][NS]) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
+    for (int i = 0; i < CH; ++i) {
+        if (m) load_states<NS>(m + ((int64_t)b * a.channels + l.c + i) * a.states, l.q, a.states, h[i]);
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const int n = l.q * NS + s;
-            h[i][s] = m && l.live[i] && n < a.states ? m[((int64_t)b * a.channels + (l.c + i)) * a.states + n] : 0.0f;
-        }
+        for (int s = 0; s < NS; ++s) h[i][s] = m && l.live[i] ? h[i][s] : 0.0f;
+    }
 }
 
 template <int NS, int CH>
 __device__ __forceinline__ void load_decay(const ScanArgs& a, const Lane<CH>& l, float (&a2)[CH][NS]) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i)
+    for (int i = 0; i < CH; ++i) {
+        load_states<NS>(a.A + (int64_t)(l.c + i) * a.states, l.q, a.states, a2[i]);
 #pragma unroll
-        for (int s = 0; s < NS; ++s) {
-            const int n = l.q * NS + s;
-            a2[i][s] = l.live[i] && n < a.states ? kLog2e * a.A[(int64_t)(l.c + i) * a.states + n] : 0.0f;
-        }
+        for (int s = 0; s < NS; ++s) a2[i][s] = l.live[i] ? kLog2e * a2[i][s] : 0.0f;
+    }
 }
 
 // What four rows (one per lane of the quad) need in the walks
@@ -138,11 +136,12 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_bwd_summary_kernel(Sc
     const ChunkRows rows(a, chunk);
     int flags = 0, b0 = 0, end0 = 0, b1 = 0, first1 = 0;
     if (rows.lo < rows.hi) {
-        b0 = a.seq.find(rows.lo);
-        b1 = a.seq.find(rows.hi - 1);
-        end0 = a.seq.first(b0 + 1);
-        first1 = a.seq.first(b1);
-        const int first0 = a.seq.first(b0), end1 = a.seq.first(b1 + 1);
+        const SeqMap::Found f0 = a.seq.at(rows.lo), f1 = a.seq.at(rows.hi - 1);
+        b0 = f0.b;
+        b1 = f1.b;
+        end0 = f0.end;
+        first1 = f1.first;
+        const int first0 = f0.first, end1 = f1.end;
         flags = (end1 > rows.hi ? kGoesOn : 0) | (first0 < rows.lo ? kFromBefore : 0);
         if (first0 < rows.lo && end0 > rows.hi) flags |= kThrough;
     }
@@ -355,7 +354,8 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
         // follows TB rows of its own, so there are at most Q / TB.
         int slot = 0;
         for (int t = rows.lo; t < rows.hi;) {
-            const int b = a.seq.find(t), first = a.seq.first(b), stop = min(max(a.seq.first(b + 1), t + 1), rows.hi);
+            const SeqMap::Found f = a.seq.at(t);
+            const int b = f.b, first = f.first, stop = min(max(f.end, t + 1), rows.hi);
             const int walk = (stop - t - 1) / TB * TB;      // rows of all tiles but the last
             if (walk) {
                 float h[CH][NS];
@@ -402,7 +402,8 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
 
         // Backwards, sequence by sequence, tile by tile
         for (int stop = rows.hi; stop > rows.lo;) {
-            const int b = a.seq.find(stop - 1), first = a.seq.first(b), end = a.seq.first(b + 1);
+            const SeqMap::Found f = a.seq.at(stop - 1);
+            const int b = f.b, first = f.first, end = f.end;
             const int from = max(min(first, stop - 1), rows.lo);
             float r[CH][NS];     // a g of the row behind: what the state's gradient receives from there
             if (end > stop) {

@@ -170,12 +170,12 @@ def test_scan_null_misaligned_and_short_workspace():
 
 def test_scan_workspace_covers_every_plan():
     """No workspace where one chunk holds all rows; otherwise a state for each
-    chunk, channel and padded state, at chunks of 32 rows or more."""
+    chunk, channel and padded state, at chunks of 16 rows or more."""
     for tokens, seqs, channels, n, groups in [(64, 1, 2048, 16, 1), (1, 1, 1, 1, 1), (8192, 1, 2048, 16, 1), (16384, 8, 2048, 16, 1), (3001, 17, 777, 24, 3), (100000, 7, 33, 128, 1)]:
         d = scan_desc(tokens=tokens, channels=channels, states=n, groups=groups, sequences=seqs, ld_x=channels, ld_dt=channels, ld_z=channels, ld_b=groups * n, ld_c=groups * n)
         need = P.im2win_selective_scan_workspace_bytes(d)
         assert (need == 0) == (tokens <= 64)
-        assert need <= (tokens / 32 + 1) * channels * (4 * 132) + tokens + 4096
+        assert need <= (tokens / 16 + 1) * channels * (4 * 132) + tokens + 4096
 
 
 def test_scan_backward_refuses():
