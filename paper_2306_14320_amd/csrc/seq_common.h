@@ -20,6 +20,12 @@ constexpr int64_t kMaxChannels = int64_t(1) << 20;
 // A value that is the same in every lane of the wave, held in a scalar register.
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
+// Waits for a load whose result is v, here and not where v is used.  Loads and
+// stores come back in one order, so a wait for a prefetched value that stands
+// behind stores waits for those too: it is put in front of them.
+__device__ __forceinline__ void arrive(uint32_t& v) { asm volatile("" : "+v"(v)); }
+__device__ __forceinline__ void arrive(float& v) { asm volatile("" : "+v"(v)); }
+
 // ---------------------------------------------------------------------------
 // Sequences in the rows.  Every bound a kernel uses comes from first(), which
 // lies in [0, tokens] whatever seq_starts holds.  Arguments are wave-uniform.
@@ -95,6 +101,10 @@ struct Bits {
     uint32_t u[4];
     __device__ __forceinline__ void load(const T* p) { __builtin_memcpy(u, p, 16); }
     __device__ __forceinline__ void zero() { u[0] = u[1] = u[2] = u[3] = 0; }
+    __device__ __forceinline__ void wait() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) arrive(u[i]);
+    }
     __device__ __forceinline__ float get(int i) const {
         if constexpr (sizeof(T) == 4) return __uint_as_float(u[i]);
         else return __uint_as_float(i % 2 ? u[i / 2] & 0xffff0000u : u[i / 2] << 16);
@@ -105,6 +115,7 @@ struct Bits<T, 1> {
     T u;
     __device__ __forceinline__ void load(const T* p) { u = *p; }
     __device__ __forceinline__ void zero() { u = (T)0.0f; }
+    __device__ __forceinline__ void wait() {}
     __device__ __forceinline__ float get(int) const { return (float)u; }
 };
 

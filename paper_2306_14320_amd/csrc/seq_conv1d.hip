@@ -262,16 +262,18 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_bwd_kernel(Conv1dBw
                 for (int v = 0; v < V; ++v) g[k][v] = g[k + 1][v];
         };
         // dx of row u, whose gradient and the W-1 behind it are in g
-        auto put = [&](int u) {
-            if (u < t) return;
-            float d[V] = {};
-            if (d_final && u >= end - (W - 1))
+        auto input_grad = [&](int u, float (&d)[V]) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) d[v] = 0.0f;
+            if (d_final && u >= t && u >= end - (W - 1))
                 load_vec<V>(d_final + ((int64_t)b * (W - 1) + (u - (end - (W - 1)))) * a.channels + c, d);
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
                 for (int k = 0; k < W; ++k) d[v] = fmaf(taps.w[k][v], g[W - 1 - k][v], d[v]);
-            if (live) store_vec<V>(dx + (int64_t)u * a.channels + c, d);
+        };
+        auto put = [&](int u, const float (&d)[V]) {
+            if (u >= t && live) store_vec<V>(dx + (int64_t)u * a.channels + c, d);
         };
 
         // the stripe's rows and the W-1 behind, which its last ones reach: kBatch rows are loaded while
@@ -295,20 +297,31 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_bwd_kernel(Conv1dBw
                 cg[i] = ng[i];
             }
             if (r + kConvBatch < reach) fetch(r + kConvBatch);
+            float d[kConvBatch][V];
 #pragma unroll
             for (int i = 0; i < kConvBatch; ++i) {
                 if (r + i >= reach) break;
                 shift();
                 row(cx[i], cg[i], r + i < own);
-                put(r + i - (W - 1));
+                input_grad(r + i - (W - 1), d[i]);
             }
+#pragma unroll
+            for (int i = 0; i < kConvBatch; ++i) {
+                nx[i].wait();
+                ng[i].wait();
+            }
+#pragma unroll
+            for (int i = 0; i < kConvBatch; ++i)
+                if (r + i < reach) put(r + i - (W - 1), d[i]);
         }
         // behind the sequence's end there is no gradient
         for (int r = reach; r < own + W - 1; ++r) {
             shift();
 #pragma unroll
             for (int v = 0; v < V; ++v) g[W - 1][v] = 0.0f;
-            put(r - (W - 1));
+            float d[V];
+            input_grad(r - (W - 1), d);
+            put(r - (W - 1), d);
         }
         t = own;
     }

@@ -108,6 +108,10 @@ struct Raw {
         if constexpr (sizeof(T) == 4) return __uint_as_float(u[i]);
         else return __uint_as_float(i ? u[0] & 0xffff0000u : u[0] << 16);
     }
+    __device__ __forceinline__ void wait() {
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) arrive(u[i]);
+    }
 };
 
 // The channels of a row that a lane owns
@@ -211,8 +215,8 @@ __device__ __forceinline__ void stage(float* lds, const T* m, int64_t ld, int gr
 
 // What the chunks leave to one another, for one channel and state: walks the
 // `chunks` values m[i * each + e] from the first to the last (or the other way)
-// and turns each one that `reads` marks into own + exp(A S) * (the one before),
-// where one sequence passes through the chunk, and own otherwise.  The walk is
+// and turns each into own + exp(A S) * (the one before), where one sequence
+// passes through the chunk, and leaves it otherwise (read or not).  The walk is
 // cut into gridDim.y pieces; each begins at the first chunk of its own that
 // takes nothing from the one before, and goes on to the next piece's beginning.
 // It waits for memory, not for arithmetic: kCarryBatch chunks are loaded while
@@ -221,7 +225,7 @@ __device__ __forceinline__ void stage(float* lds, const T* m, int64_t ld, int gr
 // by the thread whose value it is.
 constexpr int kCarryBatch = 16;
 
-__device__ __forceinline__ void carry_walk(float* m, const ScanArgs& a, int64_t each, int64_t e, int c, float a2, bool live, bool forward, int reads) {
+__device__ __forceinline__ void carry_walk(float* m, const ScanArgs& a, int64_t each, int64_t e, int c, float a2, bool live, bool forward) {
     const int n = a.chunks, piece = blockIdx.y, pieces = gridDim.y;
     auto place = [&](int i) { return forward ? i : n - 1 - i; };
     const int from = (int)((int64_t)n * piece / pieces), to = (int)((int64_t)n * (piece + 1) / pieces);
@@ -234,15 +238,15 @@ __device__ __forceinline__ void carry_walk(float* m, const ScanArgs& a, int64_t 
             break;
         }
     }
-    if (begin >= to) return;
+    if (begin >= to || !live) return;
     constexpr int U = kCarryBatch;
     float own[U], span[U], next_own[U], next_span[U];
-    int f[U], next_f[U];
+    uint32_t next_f[U];
     auto load = [&](int i0) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t at = place(min(i0 + u, n - 1));
-            next_f[u] = a.flags[at];
+            next_f[u] = (uint32_t)a.flags[at];
             next_own[u] = m[at * each + e];      // of any value where nothing reads it
             next_span[u] = a.span[at * a.channels + c];
         }
@@ -250,21 +254,38 @@ __device__ __forceinline__ void carry_walk(float* m, const ScanArgs& a, int64_t 
     float v = 0.0f;
     load(begin);
     for (int i0 = begin; i0 < n; i0 += U) {
+        int f[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            f[u] = next_f[u];
+            f[u] = uniform((int)next_f[u]);
             own[u] = next_own[u];
             span[u] = next_span[u];
         }
         if (i0 + U < n) load(i0 + U);
+        // the batch's chunks of this walk: up to the end, or to where the next piece begins
+        int count = min(U, n - i0);
+#pragma unroll
+        for (int u = U - 1; u >= 0; --u)
+            if (i0 + u >= to && !(f[u] & kThrough)) count = min(count, u);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int i = i0 + u;
-            const int flags = uniform(f[u]);
-            if (i >= n || (i >= to && !(flags & kThrough))) return;
-            if (!(flags & reads)) continue;
-            v = flags & kThrough ? fmaf(__builtin_amdgcn_exp2f(a2 * span[u]), v, own[u]) : own[u];
-            if (live) m[place(i) * each + e] = v;
+            v = f[u] & kThrough ? fmaf(__builtin_amdgcn_exp2f(a2 * span[u]), v, own[u]) : own[u];
+            own[u] = v;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            arrive(next_f[u]);
+            arrive(next_own[u]);
+            arrive(next_span[u]);
+        }
+        if (count == U) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) m[place(i0 + u) * each + e] = own[u];
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (u < count) m[place(i0 + u) * each + e] = own[u];
+            return;
         }
     }
 }

@@ -22,6 +22,11 @@ namespace {
 template <typename T, int CH>
 struct Rows {
     Raw<T, CH> x, dt, z;
+    __device__ __forceinline__ void wait() {
+        x.wait();
+        dt.wait();
+        z.wait();
+    }
 };
 template <typename T, int CH>
 struct Places {
@@ -202,6 +207,7 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
                         sum[i] *= z * sigmoid(z);
                     }
                 }
+                next.wait();
                 if (t + l.q < hi) store_channels<T, CH>(out.at(a.y, a.channels, t), l.live, sum);
             }
         }
@@ -225,7 +231,7 @@ __global__ __launch_bounds__(256) void scan_carry_kernel(ScanArgs a, int padded)
     const int64_t own = (int64_t)blockIdx.x * 256 + threadIdx.x, e = min(own, each - 1);
     const int c = (int)(e / padded), n = (int)(e % padded);
     const float a2 = n < a.states ? kLog2e * a.A[(int64_t)c * a.states + n] : 0.0f;
-    carry_walk(a.carry, a, each, e, c, a2, own < each, true, kGoesOn);
+    carry_walk(a.carry, a, each, e, c, a2, own < each, true);
 }
 
 // ---------------------------------------------------------------------------

@@ -94,6 +94,12 @@ template <typename T, int CH>
 struct BwdRows {
     Raw<T, CH> x, dt, z, dy;
 
+    __device__ __forceinline__ void wait() {
+        x.wait();
+        dt.wait();
+        z.wait();
+        dy.wait();
+    }
     __device__ __forceinline__ float step(const ScanArgs& a, int i, float bias) const {
         const float v = dt.get(i) + bias;
         return a.softplus ? softplus(v) : v;
@@ -267,8 +273,8 @@ __global__ __launch_bounds__(256) void scan_bwd_carry_kernel(ScanBwdArgs p, int 
     const int64_t own = (int64_t)blockIdx.x * 256 + threadIdx.x, e = min(own, each - 1);
     const int c = (int)(e / padded), n = (int)(e % padded);
     const float a2 = n < a.states ? kLog2e * a.A[(int64_t)c * a.states + n] : 0.0f;
-    if (blockIdx.z == 0) carry_walk(a.carry, a, each, e, c, a2, own < each, true, kGoesOn);
-    else carry_walk(p.back, a, each, e, c, a2, own < each, false, kFromBefore);
+    if (blockIdx.z == 0) carry_walk(a.carry, a, each, e, c, a2, own < each, true);
+    else carry_walk(p.back, a, each, e, c, a2, own < each, false);
 }
 
 // ---------------------------------------------------------------------------
@@ -440,10 +446,6 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
 #pragma unroll
                 for (int g = 0; g < GROUPS; ++g) {
                     now[g] = next[g];
-                    if (k > 0) {
-                        whole.load_in(a, t0 - TB + g * kQuad, next[g]);
-                        whole.load_grad(p, t0 - TB + g * kQuad, next[g]);
-                    }
 #pragma unroll
                     for (int i = 0; i < CH; ++i) {
                         step[g][i] = l.live[i] ? now[g].step(a, i, bias[i]) : 0.0f;
@@ -523,6 +525,16 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
                         }
                     }
                 };
+                // The next tile's rows are loaded behind the stores of this tile's upper group, and arrive
+                // before those of its lower one.
+                auto fetch = [&]() {
+                    if (k == 0) return;
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g) {
+                        whole.load_in(a, t0 - TB + g * kQuad, next[g]);
+                        whole.load_grad(p, t0 - TB + g * kQuad, next[g]);
+                    }
+                };
                 auto finish = [&](auto group_of_rows) {
                     constexpr int G = decltype(group_of_rows)::value;
                     const int t = t0 + G * kQuad;
@@ -545,6 +557,9 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
                             dbias[i] += ddt[i];
                         }
                     }
+                    if constexpr (G == 0)
+#pragma unroll
+                        for (int g = 0; g < GROUPS; ++g) next[g].wait();
                     if (mine) {
                         store_channels<T, CH>(whole.dense.at(p.dx, a.channels, t), l.live, dx);
                         store_channels<T, CH>(whole.dense.at(p.ddt, a.channels, t), l.live, ddt);
@@ -569,6 +584,7 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
                     finish(integral_constant<int, 1>{});
                 }
                 clear();
+                fetch();
                 backward(integral_constant<int, 3>{});
                 backward(integral_constant<int, 2>{});
                 backward(integral_constant<int, 1>{});
