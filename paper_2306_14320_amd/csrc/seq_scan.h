@@ -293,18 +293,31 @@ __device__ __forceinline__ void carry_walk(float* m, const ScanArgs& a, int64_t 
 // Pieces of that walk: short ones find their beginning soon, where sequences end often
 inline unsigned carry_pieces(int64_t chunks) { return (unsigned)(chunks < 16 ? 1 : chunks / 8 < 32 ? chunks / 8 : 32); }
 
-// Compiled shapes: f(NS, CH) for N states of D channels.  Up to 24 states a lane
-// holds a pair of channels; a single channel has no neighbour to read.
+// Whether a lane holds one channel instead of a pair: a single channel has no
+// neighbour to read, and few channels and rows fill the chip better with waves
+// of half the work (2500 ragged rows of 1000 channels: 42 us with one, 48 with
+// pairs; 16384 x 2048 is faster with pairs, which share B, C and their loads).
+inline bool narrow(const im2win_scan_desc* d) {
+    return d->channels == 1 || d->channels * d->tokens < (int64_t(1) << 22);
+}
+
+// Compiled shapes: f(NS, CH) for N states; from 32 states a lane's registers
+// hold one channel's
 template <typename F>
-void with_states(int64_t n, int64_t channels, F f) {
+void with_states(int64_t n, bool one, F f) {
     using std::integral_constant;
-    if (channels == 1 && n <= 32) f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    else if (n <= 8) f(integral_constant<int, 2>{}, integral_constant<int, 2>{});
-    else if (n <= 16) f(integral_constant<int, 4>{}, integral_constant<int, 2>{});
-    else if (n <= 24) f(integral_constant<int, 6>{}, integral_constant<int, 2>{});
-    else if (n <= 32) f(integral_constant<int, 8>{}, integral_constant<int, 1>{});
-    else if (n <= 64) f(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    else f(integral_constant<int, 32>{}, integral_constant<int, 1>{});
+    using One = integral_constant<int, 1>;
+    using Two = integral_constant<int, 2>;
+    auto shape = [&](auto ns) {
+        if (one) f(ns, One{});
+        else f(ns, Two{});
+    };
+    if (n <= 8) shape(integral_constant<int, 2>{});
+    else if (n <= 16) shape(integral_constant<int, 4>{});
+    else if (n <= 24) shape(integral_constant<int, 6>{});
+    else if (n <= 32) f(integral_constant<int, 8>{}, One{});
+    else if (n <= 64) f(integral_constant<int, 16>{}, One{});
+    else f(integral_constant<int, 32>{}, One{});
 }
 
 // Checks and geometry that the entry points share (seq_scan.hip)

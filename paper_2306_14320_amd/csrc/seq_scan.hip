@@ -331,7 +331,7 @@ size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 // sequences are cut into equal parts, or taken whole where they are shorter.
 ScanPlan plan_scan(const im2win_scan_desc* d) {
     ScanPlan p;
-    with_states(d->states, d->channels, [&](auto ns, auto ch) {
+    with_states(d->states, narrow(d), [&](auto ns, auto ch) {
         p.ns = decltype(ns)::value;
         p.ch = decltype(ch)::value;
     });
@@ -458,7 +458,7 @@ int im2win_selective_scan(const im2win_scan_desc* d, const void* x, const void* 
     const bool whole = !seq_starts && p.chunks && p.chunk % (d->tokens / d->sequences) == 0;
     hipStream_t s = static_cast<hipStream_t>(stream);
     with_type(d->dtype, [&](auto t) {
-        with_states(d->states, d->channels, [&](auto ns, auto ch) {
+        with_states(d->states, narrow(d), [&](auto ns, auto ch) {
             using T = decltype(t);
             constexpr int NS = decltype(ns)::value, CH = decltype(ch)::value;
             const dim3 threads(kScanWaves * kWave);
@@ -496,7 +496,7 @@ int im2win_selective_scan_step(const im2win_scan_desc* d, const void* x, const v
     const unsigned cover = (unsigned)((d->channels * kQuad + kScanWaves * kWave - 1) / (kScanWaves * kWave));
     const hipStream_t s = static_cast<hipStream_t>(stream);
     with_type(d->dtype, [&](auto t) {
-        with_states(d->states, d->channels, [&](auto ns, auto) {
+        with_states(d->states, true, [&](auto ns, auto) {
             using T = decltype(t);
             constexpr int NS = decltype(ns)::value;
             auto launch = [&](auto r, auto whole) {

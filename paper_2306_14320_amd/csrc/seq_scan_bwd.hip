@@ -692,7 +692,7 @@ size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 BwdPlan plan_bwd(const im2win_scan_desc* d) {
     BwdPlan p;
     int64_t tile = 8;
-    with_states(d->states, d->channels, [&](auto ns, auto ch) {
+    with_states(d->states, narrow(d), [&](auto ns, auto ch) {
         p.ns = decltype(ns)::value;
         p.ch = decltype(ch)::value;
         p.chunk = kChunkRows<decltype(ns)::value>;
@@ -793,7 +793,7 @@ int im2win_selective_scan_backward(const im2win_scan_desc* d, const void* dy, co
     int hip = 0;
     with_type(d->dtype, [&](auto t) {
         using T = decltype(t);
-        with_states(d->states, d->channels, [&](auto ns, auto ch) {
+        with_states(d->states, narrow(d), [&](auto ns, auto ch) {
             constexpr int NS = decltype(ns)::value, CH = decltype(ch)::value;
             const dim3 threads(kScanWaves * kWave);
             if (p.chunks > 1) {
