@@ -50,7 +50,7 @@ struct SeqMap {
     __device__ Found at(int t) const {
         Found f;
         if (!starts) {
-            f.b = t / len;
+            f.b = uniform(t / len);
             f.first = f.b * len;
             f.end = f.first + len;
             return f;
@@ -69,7 +69,7 @@ struct SeqMap {
         }
         const int s = look(lo + lane);
         const int k = 63 - __builtin_clzll(__ballot(lane < n && s <= t) | 1);
-        f.b = lo + k;
+        f.b = uniform(lo + k);
         f.first = __builtin_amdgcn_readlane(s, k);
         f.end = __builtin_amdgcn_readlane(s, k + 1);
         return f;

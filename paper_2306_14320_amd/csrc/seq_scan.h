@@ -73,35 +73,44 @@ __device__ __forceinline__ float quad_sums(float r0, float r1, float r2, float r
 }
 
 // log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|), and log1p(e) =
-// 2 atanh(s) with s = e / (2 + e) <= 1/3 by its power series, whose first
-// term left out is s^17 / 17 < 1e-9: small steps keep their relative accuracy.
+// 2 atanh(s) with s = e / (2 + e) <= 1/3.  atanh(s) / s is a polynomial in q =
+// s^2 <= 1/9, interpolated at the Chebyshev nodes of that interval to 4e-9:
+// small steps keep their relative accuracy.
 __device__ __forceinline__ float softplus(float v) {
     const float e = __builtin_amdgcn_exp2f(-kLog2e * fabsf(v));
     const float s = e * __builtin_amdgcn_rcpf(2.0f + e), q = s * s;
-    float p = 1.0f / 15.0f;
-    p = fmaf(p, q, 1.0f / 13.0f);
-    p = fmaf(p, q, 1.0f / 11.0f);
-    p = fmaf(p, q, 1.0f / 9.0f);
-    p = fmaf(p, q, 1.0f / 7.0f);
-    p = fmaf(p, q, 1.0f / 5.0f);
-    p = fmaf(p, q, 1.0f / 3.0f);
+    float p = 0.140873286f;
+    p = fmaf(p, q, 0.139807094f);
+    p = fmaf(p, q, 0.200124269f);
+    p = fmaf(p, q, 0.33333158f);
     return fmaxf(v, 0.0f) + fmaf(2.0f * s * q, p, 2.0f * s);
 }
+
+// Device memory by its address space, which a pointer pinned to registers keeps
+// only where its type says so; the words' types have an element's alignment.
+#define IM2WIN_GLOBAL __attribute__((address_space(1)))
+using GlobalIn = const IM2WIN_GLOBAL char*;
+using GlobalOut = IM2WIN_GLOBAL char*;
+typedef uint16_t Word16;
+typedef uint32_t Word32 __attribute__((aligned(2)));
+typedef uint32_t Word64 __attribute__((ext_vector_type(2), aligned(4)));
 
 // CH neighbouring channels of a row as they lie in memory, one access at any
 // address; the conversion is left to get(), so that a load can stay in flight.
 template <typename T, int CH>
 struct Raw {
     static_assert(CH == 1 || CH == 2, "one channel or two");
-    static constexpr int kWords = (CH * (int)sizeof(T) + 3) / 4;
+    static constexpr int kBytes = CH * (int)sizeof(T), kWords = (kBytes + 3) / 4;
     uint32_t u[kWords];
-    __device__ __forceinline__ void load(const char* p) {
-        if constexpr (CH * sizeof(T) < 4) {
-            uint16_t v;
-            __builtin_memcpy(&v, p, 2);
-            u[0] = v;
+    __device__ __forceinline__ void load(GlobalIn p) {
+        if constexpr (kBytes == 2) {
+            u[0] = *reinterpret_cast<const IM2WIN_GLOBAL Word16*>(p);
+        } else if constexpr (kBytes == 4) {
+            u[0] = *reinterpret_cast<const IM2WIN_GLOBAL Word32*>(p);
         } else {
-            __builtin_memcpy(u, p, CH * sizeof(T));
+            const Word64 v = *reinterpret_cast<const IM2WIN_GLOBAL Word64*>(p);
+            u[0] = v.x;
+            u[kWords - 1] = v.y;
         }
     }
     __device__ __forceinline__ float get(int i) const {
@@ -115,20 +124,26 @@ struct Raw {
 };
 
 // The channels of a row that a lane owns
+__device__ __forceinline__ void store_one(GlobalOut p, float v, float) { *reinterpret_cast<IM2WIN_GLOBAL float*>(p) = v; }
+__device__ __forceinline__ void store_one(GlobalOut p, float v, bf16) {
+    *reinterpret_cast<IM2WIN_GLOBAL Word16*>(p) = __builtin_bit_cast(uint16_t, (bf16)v);
+}
 template <typename T, int CH>
-__device__ __forceinline__ void store_channels(char* p, const bool (&live)[CH], const float (&v)[CH]) {
-    T e[CH];
-#pragma unroll
-    for (int i = 0; i < CH; ++i) e[i] = (T)v[i];
+__device__ __forceinline__ void store_channels(GlobalOut p, const bool (&live)[CH], const float (&v)[CH]) {
     if constexpr (CH == 2) {
         if (live[0] && live[1]) {
-            __builtin_memcpy(p, e, sizeof e);
+            if constexpr (sizeof(T) == 4) {
+                const Word64 w = {__float_as_uint(v[0]), __float_as_uint(v[1])};
+                *reinterpret_cast<IM2WIN_GLOBAL Word64*>(p) = w;
+            } else {
+                *reinterpret_cast<IM2WIN_GLOBAL Word32*>(p) = pack_bf16(v[0], v[1]);
+            }
             return;
         }
     }
 #pragma unroll
     for (int i = 0; i < CH; ++i)
-        if (live[i]) __builtin_memcpy(p + i * sizeof(T), e + i, sizeof(T));
+        if (live[i]) store_one(p + i * (int)sizeof(T), v[i], T{});
 }
 
 // NS consecutive floats of LDS on a boundary of their largest power of two
@@ -175,18 +190,23 @@ struct Lane {
 };
 
 // A T x D array: the rows of a group of four, one for each lane of the quad.
-// The group's first row is a scalar address and a lane's place beside it a
-// 32-bit offset, so that a group costs no vector instruction for addresses.
+// The group's first row is a scalar address (pinned to scalar registers) and a
+// lane's place beside it a 32-bit offset, so that a group costs no vector
+// instruction for addresses.
 template <typename T>
 struct RowPlace {
     uint32_t offset;
     template <int CH>
     __device__ __forceinline__ RowPlace(int64_t ld, const Lane<CH>& l, int row) : offset((uint32_t)((row * ld + l.c) * (int64_t)sizeof(T))) {}
-    __device__ __forceinline__ const char* at(const void* m, int64_t ld, int t) const {
-        return static_cast<const char*>(m) + t * ld * (int64_t)sizeof(T) + offset;
+    __device__ __forceinline__ GlobalIn at(const void* m, int64_t ld, int t) const {
+        GlobalIn base = (GlobalIn)m + t * ld * (int64_t)sizeof(T);
+        asm("" : "+s"(base));
+        return base + offset;
     }
-    __device__ __forceinline__ char* at(void* m, int64_t ld, int t) const {
-        return static_cast<char*>(m) + t * ld * (int64_t)sizeof(T) + offset;
+    __device__ __forceinline__ GlobalOut at(void* m, int64_t ld, int t) const {
+        GlobalOut base = (GlobalOut)m + t * ld * (int64_t)sizeof(T);
+        asm("" : "+s"(base));
+        return base + offset;
     }
 };
 

@@ -113,13 +113,25 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
                 h[i][s] = SUMMARY || chunk == 0 ? 0.0f : a.carry[((int64_t)(chunk - 1) * a.channels + (l.c + i)) * NP + l.q * NS + s];
     }
 
+    auto finish = [&]() {     // the state behind the last row of sequence b
+        if (SUMMARY || !a.final_state) return;
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                const int n = l.q * NS + s;
+                if (l.live[i] && n < a.states)
+                    a.final_state[((int64_t)b * a.channels + l.c + i) * a.states + n] = h[i][s];
+            }
+    };
+
     float span[CH] = {};
-    // the last group may have fewer than four rows: the lanes past them take its last one
-    const Places<T, CH> whole(a, l, l.q), part(a, l, min(l.q, (hi - lo - 1) % kQuad));
+    Places<T, CH> places(a, l, l.q);
     const RowPlace<T> out(a.channels, l, l.q);
     auto load = [&](int t, Rows<T, CH>& r) {
-        if (t + kQuad <= hi) whole.template load<!SUMMARY>(a, t, r);
-        else part.template load<!SUMMARY>(a, t, r);
+        // the last group may have fewer than four rows: the lanes past them take its last one
+        if (t + kQuad > hi) places = Places<T, CH>(a, l, min(l.q, hi - 1 - t));
+        places.template load<!SUMMARY>(a, t, r);
     };
     Rows<T, CH> next;
     load(lo, next);
@@ -134,84 +146,93 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_kernel(ScanArgs a) {
             const int t = tile + r;
             const Rows<T, CH> now = next;
             if (t + kQuad < hi) load(t + kQuad, next);
-            float step[CH], in[CH], x[CH], sums[kQuad][CH] = {};
+            // the first row's B and C are on their way while the steps are computed
+            float bm0[NS], cm0[NS];
+            lds_row<NS>(sb + r * NP + l.q * NS, bm0);
+            if constexpr (!SUMMARY) lds_row<NS>(sc + r * NP + l.q * NS, cm0);
+            float step[CH], in[CH], x[CH], sum[CH];
+#pragma unroll
+            for (int i = 0; i < CH; ++i) step[i] = now.dt.get(i) + bias[i];
+            if (a.softplus)
+#pragma unroll
+                for (int i = 0; i < CH; ++i) step[i] = softplus(step[i]);
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
                 x[i] = now.x.get(i);
-                step[i] = now.dt.get(i) + bias[i];
-                if (a.softplus) step[i] = softplus(step[i]);
                 in[i] = step[i] * x[i];
                 if (SUMMARY && t + l.q < hi) span[i] += step[i];
+                sum[i] = 0.0f;
             }
-            auto token = [&](auto j) {
-                constexpr int J = decltype(j)::value;
-                float bm[NS], cm[NS];
-                lds_row<NS>(sb + (r + J) * NP + l.q * NS, bm);
-                if constexpr (!SUMMARY) lds_row<NS>(sc + (r + J) * NP + l.q * NS, cm);
+            // one row, whose step and input every lane of the quad has: the lane's part of C h
+            auto advance_row = [&](int i, float sj, float ij, const float (&bm)[NS], const float (&cm)[NS]) {
+                float acc = 0.0f;
 #pragma unroll
-                for (int i = 0; i < CH; ++i) {
-                    const float sj = quad_get<J>(step[i]), ij = quad_get<J>(in[i]);
-                    float acc = 0.0f;
-#pragma unroll
-                    for (int s = 0; s < NS; ++s) {
-                        h[i][s] = fmaf(__builtin_amdgcn_exp2f(sj * a2[i][s]), h[i][s], ij * bm[s]);
-                        if constexpr (!SUMMARY) acc = fmaf(cm[s], h[i][s], acc);
-                    }
-                    if constexpr (!SUMMARY) sums[J][i] = acc;
+                for (int s = 0; s < NS; ++s) {
+                    h[i][s] = fmaf(__builtin_amdgcn_exp2f(sj * a2[i][s]), h[i][s], ij * bm[s]);
+                    if constexpr (!SUMMARY) acc = fmaf(cm[s], h[i][s], acc);
                 }
+                return acc;
             };
-            auto finish = [&]() {     // the state behind the last row of sequence b
-                if (SUMMARY || !a.final_state) return;
-#pragma unroll
-                for (int i = 0; i < CH; ++i)
-#pragma unroll
-                    for (int s = 0; s < NS; ++s) {
-                        const int n = l.q * NS + s;
-                        if (l.live[i] && n < a.states)
-                            a.final_state[((int64_t)b * a.channels + (l.c + i)) * a.states + n] = h[i][s];
-                    }
-            };
-            auto advance = [&](int row) {
-                const SeqMap::Found next_seq = a.seq.at(row);
-                b = next_seq.b;
-                end = next_seq.end;
-                begin();
-            };
-            using std::integral_constant;
             if (SUMMARY ? t + kQuad <= hi : t < end && t + kQuad <= min(end, hi)) {
+                float sums[kQuad][CH];
+                auto token = [&](auto j) {
+                    constexpr int J = decltype(j)::value;
+                    float bm[NS], cm[NS];
+                    if constexpr (J > 0) {
+                        lds_row<NS>(sb + (r + J) * NP + l.q * NS, bm);
+                        if constexpr (!SUMMARY) lds_row<NS>(sc + (r + J) * NP + l.q * NS, cm);
+                    } else {
+#pragma unroll
+                        for (int s = 0; s < NS; ++s) {
+                            bm[s] = bm0[s];
+                            cm[s] = cm0[s];
+                        }
+                    }
+#pragma unroll
+                    for (int i = 0; i < CH; ++i)
+                        sums[J][i] = advance_row(i, quad_get<J>(step[i]), quad_get<J>(in[i]), bm, cm);
+                };
+                using std::integral_constant;
                 token(integral_constant<int, 0>{});
                 token(integral_constant<int, 1>{});
                 token(integral_constant<int, 2>{});
                 token(integral_constant<int, 3>{});
-                if (t + kQuad == end) finish();
-            } else {
-                auto one = [&](auto j) {
-                    const int row = t + decltype(j)::value;
-                    if (row >= hi) return;
-                    if (!SUMMARY && row >= end) advance(row);
-                    token(j);
-                    if (row + 1 == end) finish();
-                };
-                one(integral_constant<int, 0>{});
-                one(integral_constant<int, 1>{});
-                one(integral_constant<int, 2>{});
-                one(integral_constant<int, 3>{});
-            }
-            if constexpr (!SUMMARY) {
-                float sum[CH];
+                if constexpr (!SUMMARY)
 #pragma unroll
-                for (int i = 0; i < CH; ++i) {
-                    sum[i] = fmaf(skip[i], x[i], quad_sums(sums[0][i], sums[1][i], sums[2][i], sums[3][i], l.q));
-                    if (a.z) {
-                        const float z = now.z.get(i);
-                        sum[i] *= z * sigmoid(z);
+                    for (int i = 0; i < CH; ++i) sum[i] = quad_sums(sums[0][i], sums[1][i], sums[2][i], sums[3][i], l.q);
+            } else {
+                // a group where a sequence begins or ends, or of fewer than four rows
+                for (int j = 0; j < kQuad && t + j < hi; ++j) {
+                    if (!SUMMARY && t + j >= end) {
+                        if (t + j == end) finish();
+                        const SeqMap::Found next_seq = a.seq.at(t + j);
+                        b = next_seq.b;
+                        end = next_seq.end;
+                        begin();
+                    }
+                    float bm[NS], cm[NS];
+                    lds_row<NS>(sb + (r + j) * NP + l.q * NS, bm);
+                    if constexpr (!SUMMARY) lds_row<NS>(sc + (r + j) * NP + l.q * NS, cm);
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) {
+                        const int from = (int)(threadIdx.x % kWave) / kQuad * kQuad + j;
+                        const float part = quad_sum(advance_row(i, __shfl(step[i], from), __shfl(in[i], from), bm, cm));
+                        if (l.q == j) sum[i] = part;
                     }
                 }
+            }
+            if constexpr (!SUMMARY) {
+#pragma unroll
+                for (int i = 0; i < CH; ++i) sum[i] = fmaf(skip[i], x[i], sum[i]);
+                if (a.z)
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) sum[i] *= now.z.get(i) * sigmoid(now.z.get(i));
                 next.wait();
                 if (t + l.q < hi) store_channels<T, CH>(out.at(a.y, a.channels, t), l.live, sum);
             }
         }
     }
+    if (!SUMMARY && end == hi) finish();     // the chunk's last sequence ends with it
     if constexpr (SUMMARY) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {

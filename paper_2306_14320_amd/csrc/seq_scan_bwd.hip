@@ -174,11 +174,11 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_bwd_summary_kernel(Sc
                 pass[i][s] = 1.0f;
             }
         }
-        const BwdPlaces<T, CH> whole(a, l, l.q), part(a, l, min(l.q, (to - from - 1) % kQuad));
+        BwdPlaces<T, CH> places(a, l, l.q);
         auto load = [&](int t, BwdRows<T, CH>& r) {
-            const BwdPlaces<T, CH>& w = t + kQuad <= to ? whole : part;
-            w.load_in(a, t, r);
-            w.load_grad(p, t, r);
+            if (t + kQuad > to) places = BwdPlaces<T, CH>(a, l, min(l.q, to - 1 - t));     // the last group
+            places.load_in(a, t, r);
+            places.load_grad(p, t, r);
         };
         BwdRows<T, CH> next;
         load(from, next);
@@ -426,7 +426,6 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
             BwdRows<T, CH> next[GROUPS];
             {
                 const int t0 = from + (tiles - 1) * TB;
-                const BwdPlaces<T, CH> part(a, l, min(l.q, (stop - t0 - 1) % kQuad));
 #pragma unroll
                 for (int g = 0; g < GROUPS; ++g) {
                     const int t = t0 + g * kQuad;
@@ -434,9 +433,9 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
                         next[g] = next[0];      // not used
                         continue;
                     }
-                    const BwdPlaces<T, CH>& w = t + kQuad <= stop ? whole : part;
-                    w.load_in(a, t, next[g]);
-                    w.load_grad(p, t, next[g]);
+                    const BwdPlaces<T, CH> last(a, l, min(l.q, stop - 1 - t));
+                    last.load_in(a, t, next[g]);
+                    last.load_grad(p, t, next[g]);
                 }
             }
             for (int k = tiles - 1; k >= 0; --k) {
@@ -448,9 +447,20 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
                     now[g] = next[g];
 #pragma unroll
                     for (int i = 0; i < CH; ++i) {
-                        step[g][i] = l.live[i] ? now[g].step(a, i, bias[i]) : 0.0f;
+                        step[g][i] = now[g].dt.get(i) + bias[i];
+                        grad[g][i] = now[g].dy.get(i);
+                    }
+                    if (a.softplus)
+#pragma unroll
+                        for (int i = 0; i < CH; ++i) step[g][i] = softplus(step[g][i]);
+                    if (a.z)
+#pragma unroll
+                        for (int i = 0; i < CH; ++i) grad[g][i] *= now[g].z.get(i) * sigmoid(now[g].z.get(i));
+#pragma unroll
+                    for (int i = 0; i < CH; ++i) {
+                        step[g][i] = l.live[i] ? step[g][i] : 0.0f;
                         in[g][i] = l.live[i] ? step[g][i] * now[g].x.get(i) : 0.0f;
-                        grad[g][i] = l.live[i] ? now[g].grad(a, i) : 0.0f;
+                        grad[g][i] = l.live[i] ? grad[g][i] : 0.0f;
                     }
                 }
                 float h0[CH][NS], h[TB][CH][NS];
