@@ -151,7 +151,7 @@ def main():
     x = torch.randn(4 * 512, 1024, generator=g, device="cuda").to(block.dtype)
     h = torch.randn(4 * 512, 1024, generator=g, device="cuda")
     target = torch.roll(x.float(), 1, 0)
-    losses = [float(block.train(x, h, target, 4, 2.0)) for _ in range(8)]
+    losses = [float(block.train(x, h, target, 4, 0.5)) for _ in range(8)]
     print("loss " + " ".join("%.4f" % v for v in losses))
 
 
