@@ -345,8 +345,10 @@ struct ScanPlan {
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-// The chunk: as long as leaves about four waves for each of the chip's 1024
-// SIMDs (8192 x 2048 x 16: 182 us with two, 167 with three, 163 with four), but
+// The chunk: as long as leaves the waves that fit each of the chip's 1024 SIMDs
+// at once, four (8192 x 2048 x 16: 167 us with two, 154 with three, 149 with
+// four, 151 with six) or, for pairs of channels of more than 16 states, three
+// (4001 x 2111 x 24 fp32: 151 us with two, 157 with three, 180 with four), but
 // no shorter than 16 rows (160 x 512 x 16: 42 us with 64 rows, 28 with 32, 22
 // with 16); up to 64 rows one chunk is as fast as three kernels.  Equal
 // sequences are cut into equal parts, or taken whole where they are shorter.
@@ -360,7 +362,8 @@ ScanPlan plan_scan(const im2win_scan_desc* d) {
     const int64_t group = d->channels / d->groups;
     p.blocks = d->groups * ((group + per_block - 1) / per_block);
     if (d->tokens == 0) return p;
-    const int64_t want = (4096 + p.blocks * kScanWaves - 1) / (p.blocks * kScanWaves);
+    const int64_t waves = 1024 * (p.ch == 2 && p.ns > 4 ? 3 : 4);
+    const int64_t want = (waves + p.blocks * kScanWaves - 1) / (p.blocks * kScanWaves);
     p.chunk = d->tokens <= 64 ? d->tokens : std::max<int64_t>((d->tokens + want - 1) / want, 16);
     const int64_t len = d->tokens / d->sequences;
     if (d->tokens % d->sequences == 0 && d->sequences > 1) {
