@@ -18,6 +18,12 @@
 // The sums over channels of dB and dC run over a wave's 16 quads: four values
 // at a time fold into one register by swapping halves and rows of lanes, so
 // that a value costs two instructions instead of four exchanges.
+//
+// Bound by issue slots: per row, channel and state kernel 1 takes eight, the
+// walk forwards of kernel 3 five, the states again five, the row backwards
+// twelve and the folds two.  8 x 2048 rows of 2048 x 16 bf16 take 770 us: 165 in
+// kernel 1, 45 in 2, 535 in 3 (89% of its slots taken), 27 in 4; chunks of 64
+// rows write and read 0.3 GB of states, shorter ones more.
 #include <algorithm>
 
 #include "seq_scan.h"
