@@ -44,6 +44,7 @@ struct ScanArgs {
     float* carry;          // [chunks][channels][4*NS]: the state behind each chunk
     float* span;           // [chunks][channels]: the sum of step sizes that the state passes
     int* flags;            // [chunks]
+    int look;              // no carry kernel runs: carry holds the chunks' own states (see carried)
 };
 
 // flags of a chunk: its last sequence goes on behind it / its first sequence
@@ -308,6 +309,52 @@ __device__ __forceinline__ void carry_walk(float* m, const ScanArgs& a, int64_t 
             return;
         }
     }
+}
+
+// What comes to a chunk from its neighbour `from` and the ones that lie `step`
+// behind it, m[k] decayed over the chunks between.  After a carry kernel the
+// neighbour holds all of it.  Without one (look) the values are the chunks'
+// own, and this goes on as far as the sequence does; the loads of U chunks do
+// not wait for one another.
+template <int NS, int CH>
+__device__ __forceinline__ void carried(const float* m, const ScanArgs& a, const Lane<CH>& l, const float (&a2)[CH][NS], int from, int step, bool look, float (&h)[CH][NS]) {
+    constexpr int NP = kQuad * NS, U = NS * CH <= 4 ? 8 : NS * CH <= 8 ? 4 : NS * CH <= 16 ? 2 : 1;
+    auto own = [&](int k, float (&v)[CH][NS]) {
+#pragma unroll
+        for (int i = 0; i < CH; ++i) __builtin_memcpy(v[i], m + ((int64_t)k * a.channels + (l.c + i)) * NP + l.q * NS, sizeof v[i]);
+    };
+    own(from, h);
+    if (!look) return;
+    float span[CH] = {};
+    for (int k = from;; k += U * step) {
+        int f[U];
+        float d[U][CH], v[U][CH][NS];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int between = min(max(k + u * step, 0), a.chunks - 1);
+            f[u] = a.flags[between];
+#pragma unroll
+            for (int i = 0; i < CH; ++i) d[u][i] = a.span[(int64_t)between * a.channels + (l.c + i)];
+            own(min(max(k + (u + 1) * step, 0), a.chunks - 1), v[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int next = k + (u + 1) * step;
+            if (!(uniform(f[u]) & kThrough) || next < 0 || next >= a.chunks) return;
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                span[i] += d[u][i];
+#pragma unroll
+                for (int s = 0; s < NS; ++s) h[i][s] = fmaf(__builtin_amdgcn_exp2f(a2[i][s] * span[i]), v[u][i][s], h[i][s]);
+            }
+        }
+    }
+}
+
+// Whether chunks look for themselves, which saves a launch: where sequences are
+// up to `depth` chunks long on average and ragged ones four times that at most.
+inline bool look_back(int64_t chunks, int64_t sequences, bool ragged, int64_t depth) {
+    return chunks <= depth * sequences && (!ragged || chunks <= 4 * depth);
 }
 
 // Pieces of that walk: short ones find their beginning soon, where sequences end often

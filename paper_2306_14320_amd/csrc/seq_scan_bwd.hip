@@ -10,7 +10,8 @@
 // Chunks of rows as in the forward scan, in four kernels:
 //   1. each chunk's state from zero and, in the same walk, the gradient that
 //      its rows send to the state before it: sum_t (prod_{r<=t} a_r) C_t p_t;
-//   2. both carried over the chunks, forwards and backwards;
+//   2. both carried over the chunks, forwards and backwards (left to kernel 3
+//      where sequences are few chunks long);
 //   3. each chunk: a walk forwards that leaves the state before every tile of
 //      rows in LDS, then the tiles from the last to the first: the tile's
 //      states again into registers, then its rows backwards;
@@ -304,7 +305,7 @@ __device__ __forceinline__ float fold4(float v0, float v1, float v2, float v3) {
 // the value that row r of 16 lanes holds: 0, 2, 1, 3
 __device__ __forceinline__ int fold_place(int lane) { return (lane >> 5 & 1) | (lane >> 3 & 2); }
 
-template <typename T, int NS, int CH>
+template <typename T, int NS, int CH, bool LOOK>
 __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd_kernel(ScanBwdArgs p) {
     constexpr int NP = kQuad * NS, TB = kTileRows<NS>, GROUPS = TB / kQuad;
     extern __shared__ __align__(16) char raw_lds[];
@@ -355,11 +356,11 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
                 load_state<NS, CH>(a.init, a, l, b, h);
                 return;
             }
+            if (chunk) carried<NS, CH>(a.carry, a, l, a2, chunk - 1, -1, LOOK, h);
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
-                for (int s = 0; s < NS; ++s)
-                    h[i][s] = chunk && l.live[i] ? a.carry[((int64_t)(chunk - 1) * a.channels + (l.c + i)) * NP + l.q * NS + s] : 0.0f;
+                for (int s = 0; s < NS; ++s) h[i][s] = chunk && l.live[i] ? h[i][s] : 0.0f;
         };
 
         // Forwards: the state before every tile of a sequence but its first, which start() gives.  Each
@@ -419,12 +420,11 @@ __global__ __launch_bounds__(kScanWaves * kWave, NS >= 16 ? 1 : 2) void scan_bwd
             const int from = max(min(first, stop - 1), rows.lo);
             float r[CH][NS];     // a g of the row behind: what the state's gradient receives from there
             if (end > stop) {
+                if (chunk + 1 < a.chunks) carried<NS, CH>(p.back, a, l, a2, chunk + 1, 1, LOOK, r);
 #pragma unroll
                 for (int i = 0; i < CH; ++i)
 #pragma unroll
-                    for (int s = 0; s < NS; ++s)
-                        r[i][s] = l.live[i] && chunk + 1 < a.chunks
-                                      ? p.back[((int64_t)(chunk + 1) * a.channels + (l.c + i)) * NP + l.q * NS + s] : 0.0f;
+                    for (int s = 0; s < NS; ++s) r[i][s] = chunk + 1 < a.chunks && l.live[i] ? r[i][s] : 0.0f;
             } else {
                 load_state<NS, CH>(p.d_final, a, l, b, r);
             }
@@ -734,6 +734,12 @@ BwdPlan plan_bwd(const im2win_scan_desc* d) {
     return p;
 }
 
+// States of a lane up to which chunks may look for themselves instead of a
+// carry kernel, in three walks each: 16 chunks a sequence 130 us with the kernel
+// and 126 without, 32 chunks 214 and 229; of 64 states, 63 chunks in 9 ragged
+// sequences 104 and 134.
+constexpr int kLookStates = 8;
+
 constexpr int kEmptyBlocks = 32;
 
 template <typename F>
@@ -806,6 +812,7 @@ int im2win_selective_scan_backward(const im2win_scan_desc* d, const void* dy, co
     if (grid + extra > (int64_t(1) << 31) - 1 || sums > (int64_t(1) << 31) - 1)
         return fail(IM2WIN_EOVERFLOW, "too many channels and tokens");
     hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool look = p.ns <= kLookStates && look_back(p.chunks, d->sequences, seq_starts != nullptr, 16);
     int hip = 0;
     with_type(d->dtype, [&](auto t) {
         using T = decltype(t);
@@ -814,16 +821,24 @@ int im2win_selective_scan_backward(const im2win_scan_desc* d, const void* dy, co
             const dim3 threads(kScanWaves * kWave);
             if (p.chunks > 1) {
                 hipLaunchKernelGGL((scan_bwd_summary_kernel<T, NS, CH>), dim3((unsigned)grid), threads, 0, s, b);
-                hipLaunchKernelGGL(scan_bwd_carry_kernel, dim3((unsigned)((d->channels * np + 255) / 256), carry_pieces(p.chunks), 2), dim3(256), 0, s,
-                                   b, (int)np);
+                if (!look)
+                    hipLaunchKernelGGL(scan_bwd_carry_kernel, dim3((unsigned)((d->channels * np + 255) / 256), carry_pieces(p.chunks), 2), dim3(256), 0, s,
+                                       b, (int)np);
             }
             if (grid + extra) {
                 constexpr int bytes = (int)sizeof(BwdLds<NS, CH>);
                 static_assert(bytes <= 160 * 1024, "LDS of a CU");
-                if (bytes > 64 * 1024)
-                    hip = (int)hipFuncSetAttribute(reinterpret_cast<const void*>(&scan_bwd_kernel<T, NS, CH>),
-                                                   hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-                if (!hip) hipLaunchKernelGGL((scan_bwd_kernel<T, NS, CH>), dim3((unsigned)(grid + extra)), threads, bytes, s, b);
+                auto launch = [&](auto kernel) {
+                    if (bytes > 64 * 1024)
+                        hip = (int)hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+                    if (!hip) hipLaunchKernelGGL(kernel, dim3((unsigned)(grid + extra)), threads, bytes, s, b);
+                };
+                if constexpr (NS <= kLookStates) {
+                    if (look) launch(&scan_bwd_kernel<T, NS, CH, true>);
+                    else launch(&scan_bwd_kernel<T, NS, CH, false>);
+                } else {
+                    launch(&scan_bwd_kernel<T, NS, CH, false>);
+                }
             }
         });
         if (!hip)
