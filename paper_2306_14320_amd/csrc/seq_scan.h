@@ -311,6 +311,9 @@ __device__ __forceinline__ void carry_walk(float* m, const ScanArgs& a, int64_t 
     }
 }
 
+// Pieces of that walk: short ones find their beginning soon, where sequences end often
+inline unsigned carry_pieces(int64_t chunks) { return (unsigned)(chunks < 16 ? 1 : chunks / 8 < 32 ? chunks / 8 : 32); }
+
 // What comes to a chunk from its neighbour `from` and the ones that lie `step`
 // behind it, m[k] decayed over the chunks between.  After a carry kernel the
 // neighbour holds all of it.  Without one (look) the values are the chunks'
@@ -356,9 +359,6 @@ __device__ __forceinline__ void carried(const float* m, const ScanArgs& a, const
 inline bool look_back(int64_t chunks, int64_t sequences, bool ragged, int64_t depth) {
     return chunks <= depth * sequences && (!ragged || chunks <= 4 * depth);
 }
-
-// Pieces of that walk: short ones find their beginning soon, where sequences end often
-inline unsigned carry_pieces(int64_t chunks) { return (unsigned)(chunks < 16 ? 1 : chunks / 8 < 32 ? chunks / 8 : 32); }
 
 // Whether a lane holds one channel instead of a pair: a single channel has no
 // neighbour to read, and few channels and rows fill the chip better with waves
