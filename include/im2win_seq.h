@@ -132,9 +132,11 @@ int im2win_add_rms_norm(const im2win_norm_desc* d, const void* x, const void* re
 /*
  * The same with y in 8 bits (OCP e4m3: 4 bits of exponent, 3 of mantissa,
  * largest value 448): for each row, or each `block` channels of it,
- *   scale = max |y| / 448 (1 where the block is all zeros or holds a NaN),
- *   q = y / scale, rounded to nearest even.  y is not rounded before.  Beside
- *   a NaN in its block a y beyond 448 has no value in q.
+ *   scale = max |y| / 448 (1 where that is 0 in fp32, as in a block of zeros,
+ *   or where the block holds a NaN),
+ *   q = y / scale, rounded to nearest even.  y is not rounded before.  Where
+ *   the scale is subnormal, and so rounded coarsely, quotients beyond 448 are
+ *   taken as 448.  Beside a NaN in its block a y beyond 448 has no value in q.
  *   q       device, T x D, one byte each
  *   scales  device, T x (D / block) (T x 1 for block 0), fp32
  * Errors: EINVAL, ENULL, EALIGN, EOVERFLOW, EHIP.

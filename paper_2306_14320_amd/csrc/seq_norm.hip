@@ -134,12 +134,15 @@ __device__ __forceinline__ uint32_t block_max(uint32_t v, uint32_t* part) {
     return v;
 }
 
-// Four fp32 values as e4m3 bytes, rounded to nearest even.  |v| stays below
-// 448 plus one rounding of the division, which rounds to 448.
+// Four fp32 values as e4m3 bytes, rounded to nearest even: |v| is at most 448
+// and one rounding of the division, which rounds to 448.  Anything farther
+// beyond 448 becomes NaN.
 __device__ __forceinline__ uint32_t pack_fp8(float a, float b, float c, float d) {
     int r = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, r, true);
 }
+
+constexpr float kSmallestNormal = 0x1p-126f;
 
 // TX: x and y.  TR: residual and h.  NT threads, STEPS times eight channels
 // per thread (NT * STEPS * 8 >= channels).
@@ -214,7 +217,8 @@ __global__ __launch_bounds__(NT) void add_rms_norm_kernel(NormArgs a) {
             const int c = (j * NT + (int)threadIdx.x) * N, n = a.channels - c;
             if (n <= 0) continue;
             const float most = __uint_as_float(top[j]);
-            const float scale = most > 0.0f ? most / 448.0f : 1.0f;
+            const float share = most / 448.0f;
+            const float scale = share > 0.0f ? share : 1.0f;     // it may round to 0, and is NaN beside a NaN
             if (a.block == 0) {
                 if (c == 0) a.scales[row] = scale;
             } else if (c % a.block == 0) {
@@ -223,6 +227,10 @@ __global__ __launch_bounds__(NT) void add_rms_norm_kernel(NormArgs a) {
             float s[N];
 #pragma unroll
             for (int i = 0; i < N; ++i) s[i] = v[j][i] / scale;
+            // a subnormal scale has few bits, so that it may be too small for its block by up to a third
+            if (scale < kSmallestNormal)
+#pragma unroll
+                for (int i = 0; i < N; ++i) s[i] = fminf(fmaxf(s[i], -448.0f), 448.0f);
             const uint32_t lo = pack_fp8(s[0], s[1], s[2], s[3]), hi = pack_fp8(s[4], s[5], s[6], s[7]);
             if (n >= N) {
                 const uint32_t both[2] = {lo, hi};
