@@ -234,6 +234,18 @@ __device__ __forceinline__ void stage(float* lds, const T* m, int64_t ld, int gr
     }
 }
 
+// own + h 2^x for the x of a whole chunk or more, given half of it.  Where the
+// decay grows (A and the step of the same sign) 2^x alone may pass fp32's range
+// while the sum, as row by row, does not: up to 2^254, which takes every h that
+// is no subnormal past that range, the root of 2^x holds it.  Beyond, the root
+// is the largest number, so that a state of zero stays zero.  (A NaN that
+// fminf drops came from a step or an A, and so is in own too.)
+constexpr float kLargest = 0x1.fffffep127f;
+__device__ __forceinline__ float carry_on(float own, float h, float half) {
+    const float root = fminf(__builtin_amdgcn_exp2f(half), kLargest);
+    return fmaf(h * root, root, own);
+}
+
 // What the chunks leave to one another, for one channel and state: walks the
 // `chunks` values m[i * each + e] from the first to the last (or the other way)
 // and turns each into own + exp(A S) * (the one before), where one sequence
@@ -290,7 +302,7 @@ __device__ __forceinline__ void carry_walk(float* m, const ScanArgs& a, int64_t 
             if (i0 + u >= to && !(f[u] & kThrough)) count = min(count, u);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            v = f[u] & kThrough ? fmaf(__builtin_amdgcn_exp2f(a2 * span[u]), v, own[u]) : own[u];
+            v = f[u] & kThrough ? carry_on(own[u], v, 0.5f * a2 * span[u]) : own[u];
             own[u] = v;
         }
 #pragma unroll
@@ -346,9 +358,9 @@ __device__ __forceinline__ void carried(const float* m, const ScanArgs& a, const
             if (!(uniform(f[u]) & kThrough) || next < 0 || next >= a.chunks) return;
 #pragma unroll
             for (int i = 0; i < CH; ++i) {
-                span[i] += d[u][i];
+                span[i] += 0.5f * d[u][i];
 #pragma unroll
-                for (int s = 0; s < NS; ++s) h[i][s] = fmaf(__builtin_amdgcn_exp2f(a2[i][s] * span[i]), v[u][i][s], h[i][s]);
+                for (int s = 0; s < NS; ++s) h[i][s] = carry_on(h[i][s], v[u][i][s], a2[i][s] * span[i]);
             }
         }
     }

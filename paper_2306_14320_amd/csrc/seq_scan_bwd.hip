@@ -249,16 +249,44 @@ __global__ __launch_bounds__(kScanWaves * kWave) void scan_bwd_summary_kernel(Sc
         }
     };
     if (flags & kFromBefore) {
+        const int stop = min(end0, rows.hi);
+        const bool ends = p.d_final && end0 <= rows.hi;
         load_state<NS, CH>(nullptr, a, l, 0, h);
-        walk(rows.lo, min(end0, rows.hi));
-        if (p.d_final && end0 <= rows.hi) {
-            // the sequence ends here: its final state's gradient comes back through all of its rows
-            float d[CH][NS];
-            load_state<NS, CH>(p.d_final, a, l, b0, d);
+        walk(rows.lo, stop);
+        float d[CH][NS];      // where the sequence ends here, its final state's gradient comes back through all of its rows
+        load_state<NS, CH>(ends ? p.d_final : nullptr, a, l, b0, d);
+        // A growing decay's product over the rows may pass fp32's range where what it multiplies is zero or small:
+        // the gradient of such a state (marked by a NaN) is taken back row by row.
+        bool over = false;
+#pragma unroll
+        for (int i = 0; i < CH; ++i)
+#pragma unroll
+            for (int s = 0; s < NS; ++s) {
+                if (ends) back[i][s] = fmaf(pass[i][s], d[i][s], back[i][s]);
+                back[i][s] = pass[i][s] <= kLargest ? back[i][s] : __builtin_nanf("");
+                over |= back[i][s] != back[i][s];
+            }
+        if (__any(over)) {
+            const BwdPlaces<T, CH> place(a, l, 0);
+            for (int t = stop - 1; t >= rows.lo; --t) {
+                BwdRows<T, CH> row;
+                place.load_in(a, t, row);
+                place.load_grad(p, t, row);
+                const T* c = static_cast<const T*>(a.C) + (int64_t)t * a.ld_c + group_offset;
+#pragma unroll
+                for (int i = 0; i < CH; ++i) {
+                    const float step = row.step(a, i, bias[i]), grad = row.grad(a, i);
+#pragma unroll
+                    for (int s = 0; s < NS; ++s) {
+                        const float cm = l.q * NS + s < a.states ? (float)c[l.q * NS + s] : 0.0f;
+                        d[i][s] = __builtin_amdgcn_exp2f(step * a2[i][s]) * fmaf(cm, grad, d[i][s]);
+                    }
+                }
+            }
 #pragma unroll
             for (int i = 0; i < CH; ++i)
 #pragma unroll
-                for (int s = 0; s < NS; ++s) back[i][s] = fmaf(pass[i][s], d[i][s], back[i][s]);
+                for (int s = 0; s < NS; ++s) back[i][s] = back[i][s] == back[i][s] ? back[i][s] : d[i][s];
         }
         put(p.back, back);
         if (flags & kThrough) put_forward();
