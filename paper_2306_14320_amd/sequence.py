@@ -18,7 +18,7 @@ from typing import NamedTuple, Optional
 
 import torch
 
-from . import (_DTYPES, _check, _empty, _stream, IM2WIN_F32, load_library)
+from . import (_DTYPES, _check, _empty, _stream, _torch_stream, IM2WIN_F32, load_library)
 
 __all__ = [
     "im2win_conv1d_desc", "im2win_causal_conv1d", "im2win_causal_conv1d_backward_workspace_bytes",
@@ -378,9 +378,17 @@ def add_rms_norm_fp8(x, w, desc, residual=None, q=None, scales=None, h=None, str
 def add_rms_norm_backward(dy, h, w, desc, d_residual=None, dx=None, workspace=None, stream=None):
     """(dx, dw) for dy and the gradient d_residual that h has from elsewhere:
     dx (the residual's type; may be d_residual itself) is the gradient of both
-    x and the residual, dw is fp32."""
+    x and the residual, dw is fp32.  An h whose rows have gaps (x itself, as
+    add_rms_norm returns it without a residual) is copied to a dense one."""
     dev, shape, rd = _device_of(dy, "dy"), (desc.tokens, desc.channels), _residual_dtype(desc)
     dyp = _dense(dy, "dy", shape, _torch_dtype(desc), dev)
+    if isinstance(h, torch.Tensor) and h.shape == shape and not h.is_contiguous():
+        _rows(h, "h", shape, rd, _row_stride(h, "h"), dev)
+        if stream is None:
+            h = h.contiguous()
+        else:
+            with torch.cuda.stream(_torch_stream(stream)):
+                h = h.contiguous()
     hp = _dense(h, "h", shape, rd, dev)
     wp = _dense(w, "w", (desc.channels,), torch.float32, dev)
     drp = _dense(d_residual, "d_residual", shape, rd, dev)
