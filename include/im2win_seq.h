@@ -18,7 +18,9 @@
  *    and behind the last are neither read nor written.  Values outside of
  *    [0, tokens] are taken as the nearest of the two.
  *  - Pointers need the alignment of their element type only; workspaces need
- *    16 bytes.  Row strides stay below 2^28 elements.
+ *    16 bytes.  Row strides stay below 2^28 elements.  Sizes whose launch would
+ *    hold 2^32 threads (some 2^24 rows and more, of few channels) are refused
+ *    with EOVERFLOW before anything is launched; the norm takes them.
  *  - Arrays of T rows may be NULL when tokens is 0.  Outputs must not overlap
  *    inputs or each other, except where an entry point says so.
  *  - "dtype" arrays hold im2win_dtype elements; every sum, state, statistic

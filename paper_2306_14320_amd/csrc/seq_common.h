@@ -212,6 +212,17 @@ inline int check_ld(int64_t ld, int64_t width, const char* name) {
     return IM2WIN_OK;
 }
 
+// The runtime takes fewer than 2^32 threads a launch (and dimension): checked
+// before the first launch of a call, so that a refused call has written nothing.
+constexpr int64_t kMaxThreads = (int64_t(1) << 32) - 1;
+
+inline int check_launch(int64_t blocks, int threads, const char* what) {
+    if (blocks > kMaxThreads / threads)
+        return fail(IM2WIN_EOVERFLOW, "%s: %lld workgroups of %d threads are more than a launch holds (rows, sequences or channels are too many)",
+                    what, (long long)blocks, threads);
+    return IM2WIN_OK;
+}
+
 inline int launched(const char* what) {
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return fail(IM2WIN_EHIP, "%s launch failed: %s", what, hipGetErrorString(e));

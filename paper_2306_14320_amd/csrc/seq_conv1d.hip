@@ -548,9 +548,7 @@ int im2win_causal_conv1d(const im2win_conv1d_desc* d, const void* x, const void*
     const int64_t blocks = (rows + kConvWaves - 1) / kConvWaves;
     const bool vec = vectors(d);
     a.groups = (int)channel_groups(d->channels, vec ? (int)(16 / e) : 1);
-    if (blocks * a.groups > (int64_t(1) << 31) - 1)
-        return fail(IM2WIN_EOVERFLOW, "too many tokens, sequences and channels (%lld, %lld, %lld)", (long long)d->tokens,
-                    (long long)d->sequences, (long long)d->channels);
+    if ((rc = check_launch(blocks * a.groups, kConvWaves * kWave, "causal_conv1d"))) return rc;
     with_kernel(d, vec, [&](auto t, auto v, auto taps) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value, W = decltype(taps)::value;
@@ -587,8 +585,9 @@ int im2win_causal_conv1d_backward(const im2win_conv1d_desc* d, const void* dy, c
         return fail(IM2WIN_EWORKSPACE, "workspace holds %zu bytes, the gradients need %zu", workspace_bytes, p.bytes);
     const int64_t sums = (d->channels + kWave - 1) / kWave * (d->width + 1);
     const int64_t states = d_initial_state ? d->sequences * (d->width - 1) * ((d->channels + kSumWaves * kWave - 1) / (kSumWaves * kWave)) : 0;
-    if (sums + states > (int64_t(1) << 31) - 1)
-        return fail(IM2WIN_EOVERFLOW, "too many sequences and channels (%lld, %lld)", (long long)d->sequences, (long long)d->channels);
+    if ((rc = check_launch(p.parts * p.groups, kConvWaves * kWave, "causal_conv1d_backward")) ||
+        (rc = check_launch(sums + states, kSumWaves * kWave, "causal_conv1d_backward")))
+        return rc;
     Conv1dBwdArgs a{};
     a.dy = dy; a.x = x; a.w = w; a.bias = bias; a.init = initial_state; a.d_final = d_final_state;
     a.dx = dx; a.d_init = d_initial_state; a.part = static_cast<float*>(workspace); a.dw = dw; a.dbias = dbias;
@@ -597,8 +596,6 @@ int im2win_causal_conv1d_backward(const im2win_conv1d_desc* d, const void* dy, c
     a.groups = (int)p.groups; a.stripe = (int)p.stripe;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool vec = vectors(d);
-    if (p.parts * p.groups > (int64_t(1) << 31) - 1)
-        return fail(IM2WIN_EOVERFLOW, "too many tokens and channels (%lld, %lld)", (long long)d->tokens, (long long)d->channels);
     with_kernel(d, vec, [&](auto t, auto v, auto taps) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value, W = decltype(taps)::value;
@@ -624,6 +621,7 @@ int im2win_causal_conv1d_step(const im2win_conv1d_desc* d, const void* x, const 
         (rc = may_ptr(slots, 4, "slots")) || (rc = need_ptr(y, e, "y")))
         return rc;
     if (d->width > 1 && state_slots && (rc = need_ptr(state, e, "state"))) return rc;
+    if ((rc = check_launch(d->tokens, kWave, "causal_conv1d_step"))) return rc;
     Conv1dStepArgs a{};
     a.x = x; a.w = w; a.bias = bias; a.slots = slots; a.state = state; a.y = y; a.state_slots = state_slots;
     a.ld_x = d->ld_x; a.channels = (int)d->channels; a.silu = d->silu != 0;

@@ -5,6 +5,8 @@
 // Bound by memory: 16384 x 4096 bf16 to 8 bits with a scale for each 128
 // channels takes 87 us, 5.4 TB/s.  Workgroups of 256 threads and two steps beat
 // one step of twice the threads (98 us) and four of half (97).
+#include <algorithm>
+
 #include "seq_common.h"
 
 namespace im2win {
@@ -425,7 +427,7 @@ int forward(const im2win_norm_desc* d, const void* x, const void* residual, cons
     if (FP8 && (rc = need_ptr(scales, 4, "scales"))) return rc;
     if (residual && !h) return fail(IM2WIN_ENULL, "h is NULL (it may be the residual itself)");
     NormArgs a{};
-    a.x = x; a.res = residual; a.w = w; a.y = y; a.scales = scales; a.h = h;
+    a.w = w;
     a.ld_x = d->ld_x; a.channels = (int)d->channels; a.block = (int)d->block;
     a.eps = d->eps; a.inv_d = 1.0f / (float)d->channels;
     with_types(d, [&](auto tx, auto tr) {
@@ -433,8 +435,22 @@ int forward(const im2win_norm_desc* d, const void* x, const void* residual, cons
             using TX = decltype(tx);
             using TR = decltype(tr);
             constexpr int NT = decltype(nt)::value, NV = decltype(nv)::value;
-            hipLaunchKernelGGL((add_rms_norm_kernel<TX, TR, NT, NV, FP8>),
-                               dim3((unsigned)d->tokens), dim3(NT), 0, static_cast<hipStream_t>(stream), a);
+            // a workgroup a row: from 2^22 rows (of 1024 threads) to 2^26 (of 64) a launch holds no more
+            constexpr int64_t kMost = kMaxThreads / NT;
+            for (int64_t first = 0; first < d->tokens; first += kMost) {
+                const int64_t rows = std::min(kMost, d->tokens - first), at = first * d->channels;
+                a.x = static_cast<const TX*>(x) + first * d->ld_x;
+                a.res = residual ? static_cast<const TR*>(residual) + at : nullptr;
+                a.h = h ? static_cast<TR*>(h) + at : nullptr;
+                if constexpr (FP8) {
+                    a.y = static_cast<uint8_t*>(y) + at;
+                    a.scales = scales + (d->block ? at / d->block : first);
+                } else {
+                    a.y = static_cast<TX*>(y) + at;
+                }
+                hipLaunchKernelGGL((add_rms_norm_kernel<TX, TR, NT, NV, FP8>), dim3((unsigned)rows), dim3(NT), 0,
+                                   static_cast<hipStream_t>(stream), a);
+            }
         });
     });
     return launched(FP8 ? "add_rms_norm_fp8" : "add_rms_norm");

@@ -494,7 +494,7 @@ int im2win_selective_scan(const im2win_scan_desc* d, const void* x, const void* 
     const int64_t grid = p.blocks * p.chunks;
     const int64_t extra = final_state && (seq_starts || d->tokens == 0) ? std::min<int64_t>(d->sequences, kEmptyBlocks) : 0;
     if (grid + extra == 0) return ok();
-    if (grid + extra > (int64_t(1) << 31) - 1) return fail(IM2WIN_EOVERFLOW, "too many channels and tokens");
+    if ((rc = check_launch(grid + extra, kScanWaves * kWave, "selective_scan"))) return rc;
     // chunks that no sequence crosses need no states from before them
     const bool whole = !seq_starts && p.chunks && p.chunk % (d->tokens / d->sequences) == 0;
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -536,6 +536,7 @@ int im2win_selective_scan_step(const im2win_scan_desc* d, const void* x, const v
     p.a.seq.tokens = (int)d->tokens;
     p.slots = slots; p.state_slots = state_slots;
     p.state = state_slots ? state : const_cast<float*>(A);     // as large as one state; read, and not written without slots
+    if ((rc = check_launch(d->tokens, kScanWaves * kWave, "selective_scan_step"))) return rc;
     const unsigned cover = (unsigned)((d->channels * kQuad + kScanWaves * kWave - 1) / (kScanWaves * kWave));
     const hipStream_t s = static_cast<hipStream_t>(stream);
     with_type(d->dtype, [&](auto t) {

@@ -837,8 +837,7 @@ int im2win_selective_scan_backward(const im2win_scan_desc* d, const void* dy, co
     const int64_t state_blocks = (d->channels * np + kWave - 1) / kWave;
     const int64_t param_blocks = state_blocks + (2 * d->channels + kWave - 1) / kWave;
     const int64_t sums = param_blocks + (d->tokens * d->groups * d->states + kScanWaves * kWave - 1) / (kScanWaves * kWave);
-    if (grid + extra > (int64_t(1) << 31) - 1 || sums > (int64_t(1) << 31) - 1)
-        return fail(IM2WIN_EOVERFLOW, "too many channels and tokens");
+    if ((rc = check_launch(std::max(grid + extra, sums), kScanWaves * kWave, "selective_scan_backward"))) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool look = p.ns <= kLookStates && look_back(p.chunks, d->sequences, seq_starts != nullptr, 16);
     int hip = 0;
