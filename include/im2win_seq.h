@@ -186,7 +186,9 @@ typedef struct {
  *   s[t][c]    = act(dt[t][c] + dt_bias[c])
  *   h[t][c][n] = exp(s[t][c] A[c][n]) h[t-1][c][n] + s[t][c] x[t][c] B[t][g(c)][n]
  *   y[t][c]    = (sum_n C[t][g(c)][n] h[t][c][n] + D[c] x[t][c]) * z[t][c] sigmoid(z[t][c])
- * where the state before a sequence is its initial state, or zero.
+ * where the state before a sequence is its initial state, or zero.  Behind an
+ * infinite or NaN x or step its channel has no finite values up to the
+ * sequence's end (where the formula gives infinities, NaN may stand).
  *   x, dt     device, T x D;  z  device, T x D, or NULL (no gate)
  *   A         device, D x N, fp32;  D, dt_bias  device, D, fp32, or NULL
  *   B, C      device, T x G x N

@@ -76,7 +76,7 @@ __device__ __forceinline__ bool lane_channels(int group, int lane, int channels,
 
 // One wave: kConvTile rows of 64*V channels.  Bound by memory: each wave has
 // all its rows' loads in flight before it uses the first.  16384 x 4096 bf16
-// of four taps: 51 us, 5.2 TB/s for x read and y written once.
+// of four taps: 52 us, 5.2 TB/s for x read and y written once.
 template <typename T, int V, int W>
 __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_kernel(Conv1dArgs a) {
     const T* x = static_cast<const T*>(a.x);
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_kernel(Conv1dArgs a
 // inputs and gradients in registers; the stripes' sums of dw and dbias go to
 // the workspace, one row of (W+1) x D for each workgroup, and a second kernel
 // adds them in order.  16384 x 4096 bf16 of four taps: 91 us, 4.4 TB/s for x,
-// dy and dx; 83% of the issue slots are taken (s again, its sigmoid, and three
+// dy and dx; 80% of the issue slots are taken (s again, its sigmoid, and three
 // sums of W products an element).
 // ---------------------------------------------------------------------------
 struct Conv1dBwdArgs {
@@ -279,8 +279,8 @@ __global__ __launch_bounds__(kConvWaves * kWave) void conv1d_bwd_kernel(Conv1dBw
             if (u >= t && live) store_vec<V>(dx + (int64_t)u * a.channels + c, d);
         };
 
-        // the stripe's rows and the W-1 behind, which its last ones reach: kBatch rows are loaded while
-        // the ones before them are worked on
+        // the stripe's rows and the W-1 behind, which its last ones reach: kConvBatch rows are loaded
+        // while the ones before them are worked on
         const int reach = min(own + W - 1, end);
         Bits<T, V> nx[kConvBatch], ng[kConvBatch];
         auto fetch = [&](int r) {

@@ -250,7 +250,7 @@ __global__ __launch_bounds__(NT) void add_rms_norm_kernel(NormArgs a) {
 // Gradients: each workgroup walks rows row0, row0 + gridDim.x, ... with its
 // part of dw in registers, and leaves one row of partial sums; a second
 // kernel adds those in order.  Bound by memory: 16384 x 4096 bf16 takes 107 us,
-// 5.0 TB/s; 8191 x 2049 with a residual in fp32 56 us, 4.2 TB/s.
+// 5.0 TB/s; 8191 x 2049 with a residual in fp32 58 us, 4.1 TB/s.
 // ---------------------------------------------------------------------------
 struct NormBwdArgs {
     const void* dy;
@@ -390,7 +390,8 @@ size_t size_of(int32_t dtype) { return dtype == IM2WIN_F32 ? 4 : 2; }
 
 // f(threads, steps): the smallest workgroup that holds the row.  A wave per
 // row up to 512 channels, then 256 threads of one to four steps, then 1024
-// of two (16384 channels, what their registers hold beside dw).
+// of two: 16384 channels, which their 128 registers just hold beside dw (the
+// gradients spill one of them in fp32, five with a bf16 dy and fp32 rows).
 template <typename F>
 void with_shape(int64_t channels, F f) {
     using std::integral_constant;

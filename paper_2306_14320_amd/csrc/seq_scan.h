@@ -368,14 +368,21 @@ __device__ __forceinline__ void carried(const float* m, const ScanArgs& a, const
 
 // Whether chunks look for themselves, which saves a launch: where sequences are
 // up to `depth` chunks long on average and ragged ones four times that at most.
+// The host does not know the lengths of ragged ones, and the rule is a bet on
+// even ones: 17 sequences of 8003 x 500 x 16 take 48 us so and 54 with the carry
+// kernel, of 3001 x 777 x 24 43 and 51, of 4001 x 1000 x 64 132 and 148; one
+// sequence beside three short ones 73 and 63, 68 and 54, 161 and 139.
 inline bool look_back(int64_t chunks, int64_t sequences, bool ragged, int64_t depth) {
     return chunks <= depth * sequences && (!ragged || chunks <= 4 * depth);
 }
 
 // Whether a lane holds one channel instead of a pair: a single channel has no
 // neighbour to read, and few channels and rows fill the chip better with waves
-// of half the work (2500 ragged rows of 1000 channels: 42 us with one, 48 with
-// pairs; 16384 x 2048 is faster with pairs, which share B, C and their loads).
+// of half the work; pairs share B, C and their loads.  Of 16 states, one
+// sequence, singly and in pairs: 2500 x 1000 42 and 48 us, gradients 106 and 109;
+// 3001 x 1111 50 and 55, 131 and 132; 2048 x 2048 49 and 52, 135 and 123; 8192 x
+// 1024 89 and 91, 236 and 226; 16384 x 2048 307 and 275.  The gradients change
+// sides near 2^22 channels and rows, the scan alone only behind 2^23.
 inline bool narrow(const im2win_scan_desc* d) {
     return d->channels == 1 || d->channels * d->tokens < (int64_t(1) << 22);
 }

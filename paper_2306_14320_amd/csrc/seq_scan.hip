@@ -11,16 +11,16 @@
 //   2. scan_carry_kernel: the states behind the chunks, one after the other;
 //   3. scan_kernel: each chunk from the state before it, with the outputs.
 // Where sequences are few chunks long, step 3 adds up what comes to a chunk
-// itself and step 2 does not run (3001 ragged rows of 777 x 24 fp32: 56 us with
-// it, 50 without).
+// itself and step 2 does not run (3001 ragged rows of 777 x 24 fp32: 54 us with
+// it, 47 without; see look_back).
 // With one chunk, or chunks of whole sequences, only step 3 runs.
 //
 // Bound by issue slots, not memory: a row, channel and state costs the product
 // s A, its exponential (two slots), u B, the recurrence and C h, six slots, five
 // in step 1, and a row and channel about forty more (step size, gate,
-// conversions, sums over the quad).  8192 x 2048 x 16 bf16 takes 149 us: 56 in
-// step 1, 6 in step 2, 77 in step 3, with 86 to 88% of the slots of steps 1 and
-// 3 taken and 1.0 TB/s of traffic.
+// conversions, sums over the quad).  8192 x 2048 x 16 bf16 takes 147 us; under
+// the profiler 62 in step 1, 11 in step 2 and 84 in step 3, with 87% of the
+// slots of steps 1 and 3 taken and 1.7 TB/s of traffic.
 #include <algorithm>
 
 #include "seq_scan.h"
@@ -359,12 +359,16 @@ struct ScanPlan {
 
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
-// The chunk: as long as leaves the waves that fit each of the chip's 1024 SIMDs
-// at once, four (8192 x 2048 x 16: 167 us with two, 154 with three, 149 with
-// four, 151 with six) or, for pairs of channels of more than 16 states, three
-// (4001 x 2111 x 24 fp32: 151 us with two, 157 with three, 180 with four), but
-// no shorter than 16 rows (160 x 512 x 16: 42 us with 64 rows, 28 with 32, 22
-// with 16); up to 64 rows one chunk is as fast as three kernels.  Equal
+// The chunk: as long as leaves four waves for each of the chip's 1024 SIMDs
+// (8192 x 2048 x 16: 167 us with two, 154 with three, 149 with four, 151 with
+// six) or, for pairs of channels of more than 16 states, three, which lies
+// between the others both where sequences are ragged (4001 x 2111 x 24 fp32:
+// 151 us with two, 157 with three, 180 with four) and where there is one (138,
+// 128, 119).  Kernels of more than 32 states hold two waves a SIMD, of more than
+// 64 one; with chunks for as many 2001 x 500 rows take 55 us instead of 63 (64
+// states) and 108 instead of 132 (128), 8192 x 2048 x 64 512 instead of 476.
+// No chunk is shorter than 16 rows (160 x 512 x 16: 42 us with 64 rows, 28 with
+// 32, 22 with 16); up to 64 rows one chunk is as fast as three kernels.  Equal
 // sequences are cut into equal parts, or taken whole where they are shorter.
 ScanPlan plan_scan(const im2win_scan_desc* d) {
     ScanPlan p;

@@ -22,9 +22,9 @@
 //
 // Bound by issue slots: per row, channel and state kernel 1 takes eight, the
 // walk forwards of kernel 3 five, the states again five, the row backwards
-// twelve and the folds two.  8 x 2048 rows of 2048 x 16 bf16 take 770 us: 165 in
-// kernel 1, 45 in 2, 535 in 3 (89% of its slots taken), 27 in 4; chunks of 64
-// rows write and read 0.3 GB of states, shorter ones more.
+// twelve and the folds two.  8 x 2048 rows of 2048 x 16 bf16 take 770 us; under
+// the profiler 173 in kernel 1, 46 in 2, 557 in 3 (90% of its slots taken), 28 in
+// 4; chunks of 64 rows write and read 0.3 GB of states, shorter ones more.
 #include <algorithm>
 
 #include "seq_scan.h"
@@ -765,7 +765,9 @@ BwdPlan plan_bwd(const im2win_scan_desc* d) {
 // States of a lane up to which chunks may look for themselves instead of a
 // carry kernel, in three walks each: 16 chunks a sequence 130 us with the kernel
 // and 126 without, 32 chunks 214 and 229; of 64 states, 63 chunks in 9 ragged
-// sequences 104 and 134.
+// sequences 104 and 134.  One ragged sequence that holds nearly all of 63 chunks
+// costs more (4000 x 2048 x 16: 213 us with the kernel, 258 without; 1000 x 420 x
+// 32: 68 and 111), many gain (2003 x 2048 x 16 in 17 sequences: 140 and 133).
 constexpr int kLookStates = 8;
 
 constexpr int kEmptyBlocks = 32;
