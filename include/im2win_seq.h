@@ -2,7 +2,10 @@
  * im2win_seq.h -- operators over sequences of tokens: the short causal
  * convolution of state space layers (a depthwise convolution along time),
  * the selective state space scan that reads its output, and the
- * root-mean-square norm with the residual's addition in front of both.
+ * root-mean-square norm with the residual's addition in front of both; and
+ * those of the layers that stand between such layers in hybrid stacks: the
+ * gated linear recurrence, and the norm of queries and keys with the position
+ * rotation.
  * Exported by libim2win beside the im2win entry points of im2win.h (same
  * error codes, error messages and conventions about streams and ownership;
  * see there).  Where this header differs:
@@ -239,6 +242,124 @@ int im2win_selective_scan_backward(const im2win_scan_desc* d, const void* dy, co
                                    void* ddt, float* dA, void* dB, void* dC, float* dD, void* dz,
                                    float* ddt_bias, float* d_initial_state, void* workspace,
                                    size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Gated linear recurrence                                                   */
+/* ------------------------------------------------------------------------ */
+
+typedef struct {
+    int64_t tokens;      /* T (requests, for the step) */
+    int64_t channels;    /* D */
+    int64_t sequences;   /* B >= 1 (not used by the step) */
+    int64_t ld_x, ld_r, ld_i;    /* row strides of x, r and i */
+    int32_t dtype;       /* of x, r, i, y and their gradients */
+    float c;             /* > 0, the gate's exponent */
+} im2win_recurrence_desc;
+
+/*
+ * For each channel, along each sequence, with s the logistic function,
+ *   L[t] = -c softplus(lam) s(r[t]),  a[t] = exp(L[t]),
+ *   h[t] = a[t] h[t-1] + sqrt(1 - a[t]^2) s(i[t]) x[t],   y[t] = h[t],
+ * where the state before a sequence is its initial state, or zero.
+ *   x, r, i  device, T x D
+ *   lam      device, D, fp32
+ *   initial_state  device, B x D, fp32, or NULL (zeros)
+ *   y        device, T x D
+ *   final_state    device, B x D, fp32, or NULL
+ *   chunk_states   device, chunks x D, fp32, or NULL: the states that enter the
+ *                  chunks of rows which the kernels work on, kept for the
+ *                  gradients; im2win_gated_recurrence_chunks gives their number.
+ *                  Where a sequence begins a chunk its row has no meaning.
+ *   workspace      device, 16-byte aligned, at least the bytes that
+ *                  im2win_gated_recurrence_workspace_bytes gives (NULL when 0)
+ * Errors: EINVAL, ENULL, EALIGN, EWORKSPACE, EOVERFLOW, EHIP.
+ */
+int im2win_gated_recurrence_chunks(const im2win_recurrence_desc* d, int64_t* chunks);
+int im2win_gated_recurrence_workspace_bytes(const im2win_recurrence_desc* d, size_t* bytes);
+int im2win_gated_recurrence(const im2win_recurrence_desc* d, const void* x, const void* r, const void* i,
+                            const float* lam, const int32_t* seq_starts, const float* initial_state,
+                            void* y, float* final_state, float* chunk_states, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace that im2win_gated_recurrence_backward takes.  Host only. */
+int im2win_gated_recurrence_backward_workspace_bytes(const im2win_recurrence_desc* d, size_t* bytes);
+
+/*
+ * Gradients of im2win_gated_recurrence for the gradient dy of y (T x D, dense)
+ * and, where d_final_state (B x D, fp32) is given, of the final states.
+ * chunk_states is what the forward call wrote for the same inputs, or NULL:
+ * then it is computed again.
+ *   dx, dr, di       device, T x D
+ *   dlam             device, D, fp32
+ *   d_initial_state  device, B x D, fp32, or NULL
+ *   workspace        device, 16-byte aligned, at least the bytes above
+ * Errors: EINVAL, ENULL, EALIGN, EWORKSPACE, EOVERFLOW, EHIP.
+ */
+int im2win_gated_recurrence_backward(const im2win_recurrence_desc* d, const void* dy, const void* x,
+                                     const void* r, const void* i, const float* lam,
+                                     const int32_t* seq_starts, const float* initial_state,
+                                     const float* d_final_state, const float* chunk_states, void* dx,
+                                     void* dr, void* di, float* dlam, float* d_initial_state,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * One token for each of d->tokens requests: the state of request i is
+ * state[slots[i]] of a pool of state_slots states (D each, fp32), moved on in
+ * place; slots as for im2win_causal_conv1d_step.
+ * Errors: EINVAL, ENULL, EALIGN, EOVERFLOW, EHIP.
+ */
+int im2win_gated_recurrence_step(const im2win_recurrence_desc* d, const void* x, const void* r,
+                                 const void* i, const float* lam, const int32_t* slots, float* state,
+                                 int64_t state_slots, void* y, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Norm of queries and keys for each head, with the position rotation        */
+/* ------------------------------------------------------------------------ */
+
+typedef struct {
+    int64_t tokens;            /* T */
+    int64_t q_heads, k_heads;  /* H and K heads a row, either may be 0 */
+    int64_t head_dim;          /* channels of a head, even, 2 to 512 */
+    int64_t rot_dim;           /* the first of them that are rotated, even, 0 to head_dim */
+    int64_t ld_q, ld_k;        /* row strides of q and k */
+    int32_t dtype;             /* of q, k, the outputs and their gradients */
+    int32_t interleaved;       /* pairs (2p, 2p+1) where nonzero, (p, p + rot_dim/2) otherwise */
+    float eps;                 /* >= 0 */
+} im2win_qk_desc;
+
+/*
+ * For every head's channels x of a row t (w = wq or wk),
+ *   u = x * rsqrt(mean(x^2) + eps) * w,
+ *   (y[p], y[p']) = (u[p] cos - u[p'] sin, u[p'] cos + u[p] sin)
+ * for the rotated pairs p, p' with the angle positions[t] * freqs[p] (radians);
+ * y = u for the other channels.
+ *   q, k       device, T x H x head_dim and T x K x head_dim, a row's heads
+ *              one behind the other (a side without heads may be NULL)
+ *   wq, wk     device, head_dim, fp32
+ *   positions  device, T int32;  freqs  device, rot_dim/2, fp32 (both may be
+ *              NULL where rot_dim is 0)
+ *   yq, yk     device, dense; yq may be q itself where q is dense, yk likewise
+ * Errors: EINVAL, ENULL, EALIGN, EOVERFLOW, EHIP.
+ */
+int im2win_qk_norm_rope(const im2win_qk_desc* d, const void* q, const void* k, const float* wq,
+                        const float* wk, const int32_t* positions, const float* freqs, void* yq,
+                        void* yk, void* stream);
+
+/* Bytes of workspace that im2win_qk_norm_rope_backward takes.  Host only. */
+int im2win_qk_norm_rope_backward_workspace_bytes(const im2win_qk_desc* d, size_t* bytes);
+
+/*
+ * Gradients for dyq and dyk (dense), with the q and k that the forward call read.
+ *   dq, dk    device, dense; dq may be dyq itself, dk likewise
+ *   dwq, dwk  device, head_dim, fp32 (zeros for a side without heads)
+ *   workspace device, 16-byte aligned, at least the bytes above
+ * Errors: EINVAL, ENULL, EALIGN, EWORKSPACE, EOVERFLOW, EHIP.
+ */
+int im2win_qk_norm_rope_backward(const im2win_qk_desc* d, const void* dyq, const void* dyk, const void* q,
+                                 const void* k, const float* wq, const float* wk,
+                                 const int32_t* positions, const float* freqs, void* dq, void* dk,
+                                 float* dwq, float* dwk, void* workspace, size_t workspace_bytes,
+                                 void* stream);
 
 #ifdef __cplusplus
 }

@@ -8,7 +8,7 @@ The tensor helpers below them (``desc_for``, ``transform``, ``conv2d``,
 only to allocate device memory (window tensor, filter scratch, output) on the
 call's HIP stream.  The operators over sequences of tokens
 (``include/im2win_seq.h``) are bound the same way in ``sequence.py`` and
-exported here.
+``hybrid.py`` and exported here.
 
 There is no fallback: if the library is missing or was built for another
 target, loading fails with an error.  Build it with
@@ -91,6 +91,7 @@ def load_library():
         "im2win_check_plan": [D],
     }
     sigs.update(sequence.SIGNATURES)
+    sigs.update(hybrid.SIGNATURES)
     for name, args in sigs.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -353,3 +354,5 @@ def direct_conv2d(x: torch.Tensor, w: torch.Tensor, desc: im2win_desc, y: torch.
 
 from . import sequence  # noqa: E402  (needs the names above)
 from .sequence import *  # noqa: E402,F401,F403
+from . import hybrid  # noqa: E402  (needs sequence)
+from .hybrid import *  # noqa: E402,F401,F403

@@ -41,6 +41,28 @@ struct SeqMap {
         const int s = uniform(starts[b]);
         return s < 0 ? 0 : s > tokens ? tokens : s;
     }
+    // first(b) for a b of the lane's own
+    __device__ int clamped(int b) const {
+        const int s = starts[b];
+        return s < 0 ? 0 : s > tokens ? tokens : s;
+    }
+    // How many of the sequences begin in front of row t, where starts are
+    // given; the wave's lanes, all of them active, look at 64 at a time.
+    __device__ int before(int t) const {
+        const int lane = threadIdx.x % kWave;
+        int lo = 0, n = count;         // starts[i] < t for i < lo, the number lies in [lo, lo + n]
+        while (n > kWave - 1) {
+            const int step = (n + kWave - 2) / (kWave - 1);
+            const int i = lo + lane * step;
+            const uint64_t in = __ballot(i < count && clamped(i < count ? i : count) < t);
+            const int k = __builtin_popcountll(in);
+            if (k == 0) return uniform(lo);
+            lo += (k - 1) * step;
+            n = count - lo < step ? count - lo : step;
+        }
+        const int i = lo + lane;
+        return uniform(lo + __builtin_popcountll(__ballot(lane < n && clamped(i < count ? i : count) < t)));
+    }
     // The sequence that holds row t, for first(0) <= t < first(count), and its
     // rows.  The wave's lanes, all of them active, look at 64 starts at a time,
     // so that up to 63 sequences take one load's latency and 4000 two.

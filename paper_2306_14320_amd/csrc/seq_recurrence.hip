@@ -1,0 +1,899 @@
+// Gated linear recurrence over packed rows of tokens, its gradients and its
+// form for single tokens.  For each channel, along each sequence, with s the
+// logistic function,
+//   L_t = -c softplus(lam) s(r_t),  a_t = exp(L_t),  m_t = sqrt(1 - a_t^2),
+//   h_t = a_t h_{t-1} + m_t s(i_t) x_t,   y = h.
+// Gradients, with G_t = dy_t + a_{t+1} G_{t+1}:
+//   dx = G m s(i),  di = G m x s(i) (1 - s(i)),
+//   dL = G (a h_{t-1} - (a^2 / m) s(i) x),  dr = dL L (1 - s(r)),
+//   dlam = sum_t dL L s(lam) / softplus(lam).
+//
+// A step h -> a h + b is a pair (a, b), and pairs compose, so time is cut into
+// chunks of 128 rows, whatever sequences lie in them.  A workgroup takes one
+// chunk of 64 or 128 channels, reads its rows once into registers (16 rows a
+// wave), composes them, leaves the chunk's pair for the workgroups behind it,
+// composes the pairs of the chunks in front, and applies the state that enters
+// to its registers: every input is read once and every output written once.
+// Bound by memory.
+//
+// The first row of a sequence does not look back: its pair is marked by a
+// negative a (the decays are positive), and composing selects instead of
+// multiplying, so that an infinity or a NaN stays in its own sequence.
+#include "seq_common.h"
+
+#include <type_traits>
+
+namespace im2win {
+namespace {
+
+constexpr int kRows = 16;                 // rows a wave holds in registers
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kChunk = kRows * kWaves;    // rows of a workgroup
+constexpr int kGroup = 32;                // chunks whose pairs are looked at one by one
+constexpr int kLook = kGroup / kWaves;    // of those, the ones a wave looks at
+constexpr float kReset = -1.0f;           // the a of a pair that does not look back
+constexpr float kLog2e = 1.44269504088896f;
+
+struct Pair {
+    float a, b;
+};
+
+// first `p`, then `q`
+__device__ __forceinline__ Pair then(Pair p, Pair q) {
+    if (q.a < 0.0f) return q;
+    return {p.a < 0.0f ? kReset : p.a * q.a, fmaf(q.a, p.b, q.b)};
+}
+__device__ __forceinline__ float apply(Pair q, float h) { return q.a < 0.0f ? q.b : fmaf(q.a, h, q.b); }
+
+// ---------------------------------------------------------------------------
+// Words that workgroups leave for each other: 64 bits in one access, so a word
+// is whole or still the pattern that the fill kernel wrote.  No data beside
+// the word is read, so relaxed accesses of the device's scope suffice.
+// ---------------------------------------------------------------------------
+constexpr uint64_t kEmpty = ~0ull;
+
+__device__ __forceinline__ void leave(uint64_t* w, Pair p) {
+    uint32_t a = __float_as_uint(p.a);
+    if (a == 0xffffffffu) a = 0x7fc00000u;      // a NaN that would look like an empty word
+    __hip_atomic_store(w, (uint64_t)__float_as_uint(p.b) << 32 | a, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t look(const uint64_t* w) {
+    return __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ Pair pair_of(uint64_t w) { return {__uint_as_float((uint32_t)w), __uint_as_float((uint32_t)(w >> 32))}; }
+
+// 128-row chunks of a call, in the order of their tickets: a workgroup waits
+// for chunks of smaller tickets only, and a ticket is drawn by a workgroup that
+// runs, so every wait ends whatever order the workgroups start in.
+struct Look {
+    uint64_t* pairs;      // chunk x channel: the pair of a chunk's rows
+    uint64_t* states;     // group x channel: the state behind a whole group (b of a pair)
+    uint32_t* ticket;     // one less than the number of tickets drawn
+    int chunks;
+};
+
+__global__ __launch_bounds__(256) void fill_kernel(uint64_t* p, int64_t n) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) p[i] = kEmpty;
+}
+
+// ---------------------------------------------------------------------------
+// The sequences' first and last rows inside of a chunk
+// ---------------------------------------------------------------------------
+struct Marks {
+    int first[kChunk];    // the sequence that begins at a row, or -1
+    int last[kChunk];     // the sequence that ends with a row, or -1
+};
+
+// Fills the marks of the chunk of rows [row0, row0 + kChunk) and calls
+// empty(b), with all lanes of a wave, for each sequence without rows that
+// lies there (the last chunk: there or behind it).
+template <typename F>
+__device__ __forceinline__ void mark(const SeqMap& seq, int row0, bool last_chunk, Marks& m, F empty) {
+    const int tid = threadIdx.x, lane = tid % kWave;
+    if (!seq.starts) {
+        if (tid < kChunk) {
+            const int t = row0 + tid;
+            const bool in = t < seq.tokens;
+            const int b = in ? t / seq.len : 0;
+            m.first[tid] = in && t == b * seq.len ? b : -1;
+            m.last[tid] = in && t + 1 == (b + 1) * seq.len ? b : -1;
+        }
+        __syncthreads();
+        return;
+    }
+    if (tid < kChunk) m.first[tid] = m.last[tid] = -1;
+    __syncthreads();
+    // sequences that begin in front of the chunk: all but the last of them end there
+    const int skip = seq.before(row0);
+    const int end = row0 + kChunk;
+    for (int base = (skip ? skip - 1 : 0) + tid / kWave * kWave; base < seq.count; base += kThreads) {
+        const int b = base + lane;
+        int f = 0, n = 0;
+        bool mine = false;
+        if (b < seq.count) {
+            f = seq.clamped(b), n = seq.clamped(b + 1);
+            mine = f < end || last_chunk;
+            if (mine && n > f) {
+                if (f >= row0 && f < end) m.first[f - row0] = b;
+                if (n > row0 && n <= end) m.last[n - 1 - row0] = b;
+            }
+        }
+        uint64_t none = __ballot(mine && n <= f && f >= row0);
+        while (none) {
+            const int k = __builtin_ctzll(none);
+            none &= none - 1;
+            empty(uniform(base + k));
+        }
+        if (!__ballot(mine)) break;
+    }
+    __syncthreads();
+}
+
+// The rows [t0, t0 + kRows) that lie in [lo, hi), a bit each
+__device__ __forceinline__ uint32_t rows_inside(int t0, int lo, int hi) {
+    const int from = lo - t0, to = hi - t0;
+    const uint32_t upto = to <= 0 ? 0u : to >= kRows ? 0xffffu : (1u << to) - 1;
+    return from <= 0 ? upto : from >= kRows ? 0u : upto & ~((1u << from) - 1);
+}
+// The rows of a wave that marks name, a bit each; the sequence itself is read where a bit is set.
+__device__ __forceinline__ uint32_t marked(const int* m) {
+    const int lane = threadIdx.x % kWave;
+    return (uint32_t)__ballot(lane < kRows && m[lane % kRows] >= 0);
+}
+
+// ---------------------------------------------------------------------------
+// V neighbouring channels of a row in a register: one element, or two bfloat16
+// (4 bytes at any alignment).  Nothing beside the row is read: the lane with
+// the odd last channel reads the one before it too, and takes the upper half;
+// lanes behind the row read what its last lane reads and store nothing.
+// ---------------------------------------------------------------------------
+template <typename T, int V>
+struct Lane {
+    int c, n;        // first channel, channels that are the lane's own (0 and less: none)
+    int at, shift;   // where it reads, and by how much the word moves down
+    __device__ __forceinline__ Lane(int first, int channels) {
+        c = first;
+        n = channels - first;
+        at = n >= V ? c : channels - V;
+        shift = V == 2 && n == 1 ? 16 : 0;
+    }
+    __device__ __forceinline__ uint32_t load(const T* row) const {
+        if constexpr (V * sizeof(T) == 4) {
+            uint32_t u;
+            __builtin_memcpy(&u, row + at, 4);
+            return u;
+        } else {
+            return __builtin_bit_cast(uint16_t, row[at]);
+        }
+    }
+    __device__ __forceinline__ float get(uint32_t u, int v) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(u);
+        else if constexpr (V == 1) return __uint_as_float(u << 16);
+        else return __uint_as_float(v ? u & 0xffff0000u : (u >> shift) << 16);
+    }
+    __device__ __forceinline__ void store(T* row, const float (&v)[V]) const {
+        if constexpr (V == 1) {
+            if (n > 0) row[c] = (T)v[0];
+        } else {
+            if (n > 1) {
+                const uint32_t u = pack_bf16(v[0], v[1]);
+                __builtin_memcpy(row + c, &u, 4);
+            } else if (n == 1) {
+                row[c] = (bf16)v[0];
+            }
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------
+// The gates of one element
+// ---------------------------------------------------------------------------
+struct Gate {
+    float a, m;      // exp(L) and sqrt(1 - exp(2 L)); g = -L / ln 2 >= 0
+};
+
+// 1 - exp(2 L) loses all digits near L = 0, so below 0.25 it is the series
+// u (1 - u/2 (1 - u/3 (1 - u/4 (1 - u/5 (1 - u/6))))) of u = -2 L (its rest is
+// under u^6 / 5040 = 5e-8); above, the subtraction is off by 3e-7 relative and
+// the root halves that.
+__device__ __forceinline__ Gate gate_of(float g) {
+    Gate o;
+    o.a = __builtin_amdgcn_exp2f(-g);
+    const float u = g * (2.0f / kLog2e);
+    const float s = u * fmaf(-0.5f * u, fmaf(u * (-1.0f / 3.0f), fmaf(u * -0.25f, fmaf(u * -0.2f, fmaf(u, -1.0f / 6.0f, 1.0f), 1.0f), 1.0f), 1.0f), 1.0f);
+    const float d = fmaf(-o.a, o.a, 1.0f);
+    o.m = __builtin_amdgcn_sqrtf(u < 0.25f ? s : d);
+    return o;
+}
+
+// c softplus(lam) log2(e): what s(r) is multiplied with
+__device__ __forceinline__ float rate_of(float lam, float c) {
+    const float sp = lam > 20.0f ? lam : log1pf(expf(lam));
+    return c * sp * kLog2e;
+}
+
+struct RecArgs {
+    const void *x, *r, *i;
+    const float* lam;
+    SeqMap seq;
+    const float* init;
+    void* y;              // NULL: only the states
+    float* final_state;
+    float* chunk_states;  // chunk x channel, or NULL
+    Look look;
+    int64_t ld_x, ld_r, ld_i;
+    int channels, tiles;
+    float c;
+};
+
+// The state that enters a chunk: the state behind the group in front, then
+// the pairs of the group's chunks in order, each wave composing kLook of them.
+// `step` is +1 (time runs forwards) or -1; order counts chunks in that
+// direction.  All threads of the workgroup take part; p holds V channels from c.
+template <int V>
+__device__ __forceinline__ void look_back(const Look& k, int order, int c, int channels, Pair (*pre)[kWave * V], float* enter, float (&h)[V]) {
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int group = order / kGroup, base = group * kGroup;
+    Pair p[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) p[v] = {1.0f, 0.0f};
+    const int from = base + wave * kLook;
+    if (from < order) {
+        uint64_t w[kLook][V];
+        while (true) {
+            bool ready = true;
+#pragma unroll
+            for (int j = 0; j < kLook; ++j) {
+                const int q = from + j < order ? from + j : from;
+#pragma unroll
+                for (int v = 0; v < V; ++v) w[j][v] = c + v < channels ? look(k.pairs + (int64_t)q * channels + c + v) : 0;
+            }
+#pragma unroll
+            for (int j = 0; j < kLook; ++j)
+#pragma unroll
+                for (int v = 0; v < V; ++v) ready &= w[j][v] != kEmpty;
+            if (!__ballot(!ready)) break;
+            __builtin_amdgcn_s_sleep(2);
+        }
+#pragma unroll
+        for (int j = 0; j < kLook; ++j)
+            if (from + j < order)
+#pragma unroll
+                for (int v = 0; v < V; ++v) p[v] = then(p[v], pair_of(w[j][v]));
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) pre[wave][lane * V + v] = p[v];
+    if (wave == 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            uint64_t w = 0;
+            if (group && c + v < channels)
+                while ((w = look(k.states + (int64_t)(group - 1) * channels + c + v)) == kEmpty) __builtin_amdgcn_s_sleep(2);
+            enter[lane * V + v] = pair_of(w).b;
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        h[v] = enter[lane * V + v];
+        for (int w = 0; w < kWaves; ++w) h[v] = apply(pre[w][lane * V + v], h[v]);
+    }
+}
+
+template <typename T, int V>
+__global__ __launch_bounds__(kThreads, 2) void recurrence_kernel(RecArgs a) {
+    __shared__ Marks marks;
+    __shared__ Pair agg[kWaves][kWave * V];
+    __shared__ Pair pre[kWaves][kWave * V];
+    __shared__ float enter[kWave * V];
+    __shared__ int drawn;
+    const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const bool many = a.look.chunks > 1;
+    int ticket = blockIdx.x;
+    if (many) {
+        if (threadIdx.x == 0) drawn = (int)(atomicAdd(a.look.ticket, 1u) + 1u);
+        __syncthreads();
+        ticket = uniform(drawn);
+    }
+    const int chunk = ticket / a.tiles, tile = ticket - chunk * a.tiles;
+    const int row0 = chunk * kChunk;
+    const Lane<T, V> own((tile * kWave + lane) * V, a.channels);
+    const int c = own.c, n = own.n;
+    mark(a.seq, row0, chunk == a.look.chunks - 1, marks, [&](int b) {
+        if (!a.final_state) return;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < n) a.final_state[(int64_t)b * a.channels + c + v] = a.init ? a.init[(int64_t)b * a.channels + c + v] : 0.0f;
+    });
+    const int lo = a.seq.first(0), hi = a.seq.first(a.seq.count);
+    if (lo >= hi) return;      // of every workgroup: none waits
+
+    const int t0 = row0 + wave * kRows;
+    uint32_t xw[kRows], rw[kRows], iw[kRows];
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+        const int t = t0 + j < lo ? lo : t0 + j >= hi ? hi - 1 : t0 + j;
+        xw[j] = own.load(static_cast<const T*>(a.x) + t * a.ld_x);
+        rw[j] = own.load(static_cast<const T*>(a.r) + t * a.ld_r);
+        iw[j] = own.load(static_cast<const T*>(a.i) + t * a.ld_i);
+    }
+    float rate[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) rate[v] = v < n ? rate_of(a.lam[c + v], a.c) : 0.0f;
+
+    float da[kRows][V], db[kRows][V];
+    Pair p[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) p[v] = {1.0f, 0.0f};
+    const uint32_t begin = marked(marks.first + wave * kRows), end = marked(marks.last + wave * kRows);
+    const uint32_t inside = rows_inside(t0, lo, hi);
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+        const bool in = inside >> j & 1;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const Gate g = gate_of(rate[v] * sigmoid(own.get(rw[j], v)));
+            da[j][v] = in ? g.a : 1.0f;
+            db[j][v] = in ? g.m * sigmoid(own.get(iw[j], v)) * own.get(xw[j], v) : 0.0f;
+        }
+        if (begin >> j & 1) {
+            const int b = uniform(marks.first[wave * kRows + j]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (a.init && v < n) db[j][v] = fmaf(da[j][v], a.init[(int64_t)b * a.channels + c + v], db[j][v]);
+                p[v].b = db[j][v];
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                p[v].a *= da[j][v];
+                p[v].b = fmaf(da[j][v], p[v].b, db[j][v]);
+            }
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        if (begin) p[v].a = kReset;
+        agg[wave][lane * V + v] = p[v];
+    }
+    __syncthreads();
+    if (many && wave == 0 && chunk + 1 < a.look.chunks) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            Pair q = agg[0][lane * V + v];
+            for (int w = 1; w < kWaves; ++w) q = then(q, agg[w][lane * V + v]);
+            if (v < n) leave(a.look.pairs + (int64_t)chunk * a.channels + c + v, q);
+        }
+    }
+    float h[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) h[v] = 0.0f;
+    if (chunk) look_back<V>(a.look, chunk, c, a.channels, pre, enter, h);
+    if (a.chunk_states && wave == 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < n) a.chunk_states[(int64_t)chunk * a.channels + c + v] = h[v];
+    }
+    for (int w = 0; w < wave; ++w) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = apply(agg[w][lane * V + v], h[v]);
+    }
+    if (wave == kWaves - 1 && chunk % kGroup == kGroup - 1 && chunk + 1 < a.look.chunks) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < n) leave(a.look.states + (int64_t)(chunk / kGroup) * a.channels + c + v, {0.0f, apply(p[v], h[v])});
+    }
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = begin >> j & 1 ? db[j][v] : fmaf(da[j][v], h[v], db[j][v]);
+        if ((inside >> j & 1) && a.y) own.store(static_cast<T*>(a.y) + (int64_t)(t0 + j) * a.channels, h);
+        if ((end >> j & 1) && a.final_state) {
+            const int e = uniform(marks.last[wave * kRows + j]);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v < n) a.final_state[(int64_t)e * a.channels + c + v] = h[v];
+        }
+    }
+}
+
+// Final states (or gradients of initial ones) of sequences without rows when
+// there are no rows at all: from[b], or zero.
+__global__ __launch_bounds__(256) void copy_states_kernel(const float* from, float* to, int64_t n) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) to[i] = from ? from[i] : 0.0f;
+}
+
+// ---------------------------------------------------------------------------
+// Gradients: one pass too.  The state that enters a chunk comes from the
+// forward call (chunk_states), the gradient that enters it from behind by the
+// same look at the chunks behind it, e_t = a_t G_t in the place of h.
+// ---------------------------------------------------------------------------
+struct RecBwdArgs {
+    const void *dy, *x, *r, *i;
+    const float* lam;
+    SeqMap seq;
+    const float *init, *d_final, *chunk_states;
+    void *dx, *dr, *di;
+    float *d_init, *part;     // part: chunk x channel, the chunk's sum of dL L
+    Look look;
+    int64_t ld_x, ld_r, ld_i;
+    int channels, tiles;
+    float c;
+};
+
+template <typename T, int V>
+__global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs a) {
+    __shared__ Marks marks;
+    __shared__ Pair agg[kWaves][kWave * V];
+    __shared__ Pair back[kWaves][kWave * V];
+    __shared__ Pair pre[kWaves][kWave * V];
+    __shared__ float enter[kWave * V];
+    __shared__ int drawn;
+    const int wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+    const bool many = a.look.chunks > 1;
+    int ticket = blockIdx.x;
+    if (many) {
+        if (threadIdx.x == 0) drawn = (int)(atomicAdd(a.look.ticket, 1u) + 1u);
+        __syncthreads();
+        ticket = uniform(drawn);
+    }
+    const int order = ticket / a.tiles, tile = ticket - order * a.tiles;
+    const int chunk = a.look.chunks - 1 - order;
+    const int row0 = chunk * kChunk;
+    const Lane<T, V> own((tile * kWave + lane) * V, a.channels);
+    const int c = own.c, n = own.n;
+    mark(a.seq, row0, order == 0, marks, [&](int b) {
+        if (!a.d_init) return;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < n) a.d_init[(int64_t)b * a.channels + c + v] = a.d_final ? a.d_final[(int64_t)b * a.channels + c + v] : 0.0f;
+    });
+    const int lo = a.seq.first(0), hi = a.seq.first(a.seq.count);
+    if (lo >= hi) {            // of every workgroup: none waits
+        if (wave == 0) {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v < n) a.part[(int64_t)chunk * a.channels + c + v] = 0.0f;
+        }
+        return;
+    }
+
+    const int t0 = row0 + wave * kRows;
+    uint32_t xw[kRows], rw[kRows], iw[kRows], gw[kRows];
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+        const int t = t0 + j < lo ? lo : t0 + j >= hi ? hi - 1 : t0 + j;
+        xw[j] = own.load(static_cast<const T*>(a.x) + t * a.ld_x);
+        rw[j] = own.load(static_cast<const T*>(a.r) + t * a.ld_r);
+        iw[j] = own.load(static_cast<const T*>(a.i) + t * a.ld_i);
+        gw[j] = own.load(static_cast<const T*>(a.dy) + (int64_t)t * a.channels);
+    }
+    float rate[V], h[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        rate[v] = v < n ? rate_of(a.lam[c + v], a.c) : 0.0f;
+        h[v] = v < n && chunk ? a.chunk_states[(int64_t)chunk * a.channels + c + v] : 0.0f;
+    }
+
+    // hb: first the row's b, then the state in front of the row
+    float da[kRows][V], hb[kRows][V];
+    Pair p[V], q[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) p[v] = q[v] = {1.0f, 0.0f};
+    const uint32_t begin = marked(marks.first + wave * kRows), end = marked(marks.last + wave * kRows);
+    const uint32_t inside = rows_inside(t0, lo, hi);
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+        const bool in = inside >> j & 1;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const Gate g = gate_of(rate[v] * sigmoid(own.get(rw[j], v)));
+            da[j][v] = in ? g.a : 1.0f;
+            hb[j][v] = in ? g.m * sigmoid(own.get(iw[j], v)) * own.get(xw[j], v) : 0.0f;
+        }
+        if (begin >> j & 1) {
+            const int b = uniform(marks.first[wave * kRows + j]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const float h0 = a.init && v < n ? a.init[(int64_t)b * a.channels + c + v] : 0.0f;
+                p[v].b = fmaf(da[j][v], h0, hb[j][v]);
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                p[v].a *= da[j][v];
+                p[v].b = fmaf(da[j][v], p[v].b, hb[j][v]);
+            }
+        }
+    }
+#pragma unroll
+    for (int j = kRows - 1; j >= 0; --j) {
+        const bool in = inside >> j & 1;
+        if (end >> j & 1) {
+            const int e = uniform(marks.last[wave * kRows + j]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) q[v].b = a.d_final && v < n ? a.d_final[(int64_t)e * a.channels + c + v] : 0.0f;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            q[v].b = da[j][v] * (q[v].b + (in ? own.get(gw[j], v) : 0.0f));
+            q[v].a *= da[j][v];
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        if (begin) p[v].a = kReset;
+        if (end) q[v].a = kReset;
+        agg[wave][lane * V + v] = p[v];
+        back[wave][lane * V + v] = q[v];
+    }
+    __syncthreads();
+    if (many && wave == 0 && chunk) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            Pair s = back[kWaves - 1][lane * V + v];
+            for (int w = kWaves - 2; w >= 0; --w) s = then(s, back[w][lane * V + v]);
+            if (v < n) leave(a.look.pairs + (int64_t)order * a.channels + c + v, s);
+        }
+    }
+    float g[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) g[v] = 0.0f;
+    if (order) look_back<V>(a.look, order, c, a.channels, pre, enter, g);
+    for (int w = 0; w < wave; ++w) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[v] = apply(agg[w][lane * V + v], h[v]);
+    }
+    for (int w = kWaves - 1; w > wave; --w) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) g[v] = apply(back[w][lane * V + v], g[v]);
+    }
+    if (wave == 0 && order % kGroup == kGroup - 1 && chunk) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < n) leave(a.look.states + (int64_t)(order / kGroup) * a.channels + c + v, {0.0f, apply(q[v], g[v])});
+    }
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+        if (begin >> j & 1) {
+            const int b = uniform(marks.first[wave * kRows + j]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[v] = a.init && v < n ? a.init[(int64_t)b * a.channels + c + v] : 0.0f;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float before = h[v];
+            h[v] = fmaf(da[j][v], h[v], hb[j][v]);
+            hb[j][v] = before;
+        }
+    }
+    float sum[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) sum[v] = 0.0f;
+#pragma unroll
+    for (int j = kRows - 1; j >= 0; --j) {
+        const bool in = inside >> j & 1;
+        if (end >> j & 1) {
+            const int e = uniform(marks.last[wave * kRows + j]);
+#pragma unroll
+            for (int v = 0; v < V; ++v) g[v] = a.d_final && v < n ? a.d_final[(int64_t)e * a.channels + c + v] : 0.0f;
+        }
+        float ox[V], orr[V], oi[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const float x = own.get(xw[j], v), sr = sigmoid(own.get(rw[j], v)), si = sigmoid(own.get(iw[j], v));
+            const float gg = g[v] + (in ? own.get(gw[j], v) : 0.0f);
+            const float l2 = rate[v] * sr;                   // -L / ln 2
+            const Gate gt = gate_of(l2);
+            const float l = l2 * (-1.0f / kLog2e), gm = gg * gt.m;
+            // L / m stays finite: it goes to zero with L
+            const float lm = gt.m > 0.0f ? l * __builtin_amdgcn_rcpf(gt.m) : 0.0f;
+            const float dl = gg * gt.a * fmaf(-gt.a * lm, si * x, l * hb[j][v]);      // dL L
+            ox[v] = gm * si;
+            oi[v] = ox[v] * x * (1.0f - si);
+            orr[v] = dl * (1.0f - sr);
+            sum[v] += in ? dl : 0.0f;
+            g[v] = in ? gt.a * gg : g[v];
+        }
+        __builtin_amdgcn_sched_barrier(0);      // a row at a time: mixed, the rows' temporaries spill
+        if (in) {
+            const int64_t at = (int64_t)(t0 + j) * a.channels;
+            own.store(static_cast<T*>(a.dx) + at, ox);
+            own.store(static_cast<T*>(a.dr) + at, orr);
+            own.store(static_cast<T*>(a.di) + at, oi);
+        }
+        if ((begin >> j & 1) && a.d_init) {
+            const int b = uniform(marks.first[wave * kRows + j]);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (v < n) a.d_init[(int64_t)b * a.channels + c + v] = g[v];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int v = 0; v < V; ++v) pre[wave][lane * V + v].b = sum[v];
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            for (int w = 1; w < kWaves; ++w) sum[v] += pre[w][lane * V + v].b;
+            if (v < n) a.part[(int64_t)chunk * a.channels + c + v] = sum[v];
+        }
+    }
+}
+
+// dlam from the chunks' sums: 64 channels a workgroup, every 16th chunk a wave
+constexpr int kSumWaves = 16;
+__global__ __launch_bounds__(kSumWaves * kWave) void recurrence_bwd_sum_kernel(const float* part, const float* lam, float* dlam, int chunks, int channels) {
+    __shared__ float sum[kSumWaves][kWave];
+    const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+    const int c = (int)blockIdx.x * kWave + lane;
+    float s = 0.0f;
+    if (c < channels) {
+#pragma unroll 8
+        for (int i = wave; i < chunks; i += kSumWaves) s += part[(int64_t)i * channels + c];
+    }
+    sum[wave][lane] = s;
+    __syncthreads();
+    if (wave == 0 && c < channels) {
+        for (int i = 1; i < kSumWaves; ++i) s += sum[i][lane];
+        // s(lam) / softplus(lam): with e = exp(lam), e / ((1 + e) log1p(e)), which goes to 1 with e
+        const float l = lam[c], e = expf(l);
+        const float ratio = l > 20.0f ? 1.0f / l : e > 0.0f ? e / ((1.0f + e) * log1pf(e)) : 1.0f;
+        dlam[c] = s * ratio;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// One token of each request
+// ---------------------------------------------------------------------------
+struct RecStepArgs {
+    const void *x, *r, *i;
+    const float* lam;
+    const int32_t* slots;
+    float* state;
+    void* y;
+    int64_t ld_x, ld_r, ld_i, state_slots;
+    int channels;
+    float c;
+};
+
+template <typename T, int V>
+__global__ __launch_bounds__(256) void recurrence_step_kernel(RecStepArgs a) {
+    const Lane<T, V> own(((int)blockIdx.y * 256 + (int)threadIdx.x) * V, a.channels);
+    const int c = own.c, n = own.n;
+    if (n <= 0) return;
+    const int64_t t = blockIdx.x;
+    const int64_t slot = a.slots ? a.slots[t] : t;
+    const bool live = slot >= 0 && slot < a.state_slots;
+    float* st = a.state + (live ? slot : 0) * a.channels + c;
+    const uint32_t xw = own.load(static_cast<const T*>(a.x) + t * a.ld_x);
+    const uint32_t rw = own.load(static_cast<const T*>(a.r) + t * a.ld_r);
+    const uint32_t iw = own.load(static_cast<const T*>(a.i) + t * a.ld_i);
+    float h[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        h[v] = 0.0f;
+        if (!live || v >= n) continue;
+        const Gate g = gate_of(rate_of(a.lam[c + v], a.c) * sigmoid(own.get(rw, v)));
+        h[v] = fmaf(g.a, st[v], g.m * sigmoid(own.get(iw, v)) * own.get(xw, v));
+    }
+    own.store(static_cast<T*>(a.y) + t * a.channels, h);
+    if (live) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (v < n) st[v] = h[v];
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+int check_desc(const im2win_recurrence_desc* d) {
+    if (!d) return fail(IM2WIN_ENULL, "descriptor is NULL");
+    int rc = check_rows(d->tokens, d->channels, d->dtype);
+    if (rc) return rc;
+    if (!(d->c > 0.0f) || d->c > 1e30f) return fail(IM2WIN_EINVAL, "c must be positive (got %g)", (double)d->c);
+    if ((rc = check_ld(d->ld_x, d->channels, "ld_x")) || (rc = check_ld(d->ld_r, d->channels, "ld_r")) || (rc = check_ld(d->ld_i, d->channels, "ld_i"))) return rc;
+    return IM2WIN_OK;
+}
+
+size_t size_of(int32_t dtype) { return dtype == IM2WIN_F32 ? 4 : 2; }
+
+// Channels of a lane: 4 bytes of a row, or a row of one bfloat16
+int lane_channels(const im2win_recurrence_desc* d) { return d->dtype == IM2WIN_F32 || d->channels == 1 ? 1 : 2; }
+
+struct Plan {
+    int64_t chunks, tiles;
+    size_t words, look_bytes, states_bytes, total;
+};
+
+Plan plan_of(const im2win_recurrence_desc* d) {
+    Plan p{};
+    p.chunks = (d->tokens + kChunk - 1) / kChunk;
+    const int64_t per = kWave * lane_channels(d);
+    p.tiles = (d->channels + per - 1) / per;
+    if (p.chunks > 1) p.words = (size_t)((p.chunks + p.chunks / kGroup) * d->channels + 2);      // pairs, states, ticket, to 16 bytes
+    p.look_bytes = (p.words * 8 + 15) / 16 * 16;
+    p.states_bytes = ((size_t)(p.chunks * d->channels) * 4 + 15) / 16 * 16;
+    return p;
+}
+
+int check_plan(const im2win_recurrence_desc* d, const Plan& p) {
+    int rc = check_launch(p.chunks * p.tiles, kThreads, "gated_recurrence");
+    if (!rc) rc = check_launch(((int64_t)p.words + 255) / 256, 256, "gated_recurrence's workspace");
+    if (!rc && d->tokens == 0) rc = check_launch((d->sequences * d->channels + 255) / 256, 256, "gated_recurrence's states");
+    return rc;
+}
+
+Look look_of(const Plan& p, int64_t channels, void* ws) {
+    Look k{};
+    k.chunks = (int)p.chunks;
+    if (p.chunks > 1) {
+        k.ticket = static_cast<uint32_t*>(ws);
+        k.pairs = static_cast<uint64_t*>(ws) + 2;
+        k.states = k.pairs + p.chunks * channels;
+    }
+    return k;
+}
+
+void fill(const Plan& p, void* ws, hipStream_t s) {
+    if (p.words)
+        hipLaunchKernelGGL(fill_kernel, dim3((unsigned)((p.words + 255) / 256)), dim3(256), 0, s, static_cast<uint64_t*>(ws), (int64_t)p.words);
+}
+
+template <typename F>
+void with_type(const im2win_recurrence_desc* d, F f) {
+    using std::integral_constant;
+    if (d->dtype == IM2WIN_F32) f(float{}, integral_constant<int, 1>{});
+    else if (lane_channels(d) == 1) f(bf16{}, integral_constant<int, 1>{});
+    else f(bf16{}, integral_constant<int, 2>{});
+}
+
+int launch_forward(const im2win_recurrence_desc* d, const Plan& p, RecArgs& a, void* ws, hipStream_t s) {
+    a.look = look_of(p, d->channels, ws);
+    a.ld_x = d->ld_x; a.ld_r = d->ld_r; a.ld_i = d->ld_i;
+    a.channels = (int)d->channels; a.tiles = (int)p.tiles; a.c = d->c;
+    fill(p, ws, s);
+    with_type(d, [&](auto t, auto v) {
+        hipLaunchKernelGGL((recurrence_kernel<decltype(t), decltype(v)::value>), dim3((unsigned)(p.chunks * p.tiles)), dim3(kThreads), 0, s, a);
+    });
+    return launched("gated_recurrence");
+}
+
+int copy_states(const float* from, float* to, int64_t n, hipStream_t s) {
+    if (to && n) hipLaunchKernelGGL(copy_states_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, from, to, n);
+    return launched("gated_recurrence's states");
+}
+
+}  // namespace
+}  // namespace im2win
+
+using namespace im2win;
+
+extern "C" {
+
+int im2win_gated_recurrence_chunks(const im2win_recurrence_desc* d, int64_t* chunks) {
+    int rc = check_desc(d);
+    if (rc) return rc;
+    if (!chunks) return fail(IM2WIN_ENULL, "chunks is NULL");
+    *chunks = plan_of(d).chunks;
+    return ok();
+}
+
+int im2win_gated_recurrence_workspace_bytes(const im2win_recurrence_desc* d, size_t* bytes) {
+    int rc = check_desc(d);
+    if (rc) return rc;
+    if (!bytes) return fail(IM2WIN_ENULL, "bytes is NULL");
+    *bytes = plan_of(d).look_bytes;
+    return ok();
+}
+
+int im2win_gated_recurrence(const im2win_recurrence_desc* d, const void* x, const void* r, const void* i, const float* lam,
+                            const int32_t* seq_starts, const float* initial_state, void* y, float* final_state,
+                            float* chunk_states, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_desc(d);
+    if (rc || (rc = check_sequences(d->tokens, d->sequences, seq_starts, true)) || (rc = need_ptr(lam, 4, "lam")) ||
+        (rc = may_ptr(initial_state, 4, "initial_state")) || (rc = may_ptr(final_state, 4, "final_state")) ||
+        (rc = may_ptr(chunk_states, 4, "chunk_states")))
+        return rc;
+    const Plan p = plan_of(d);
+    const size_t e = size_of(d->dtype);
+    if (d->tokens && ((rc = need_ptr(x, e, "x")) || (rc = need_ptr(r, e, "r")) || (rc = need_ptr(i, e, "i")) || (rc = need_ptr(y, e, "y")))) return rc;
+    if (p.look_bytes && (rc = need_ptr(workspace, 16, "workspace"))) return rc;
+    if (workspace_bytes < p.look_bytes)
+        return fail(IM2WIN_EWORKSPACE, "workspace holds %zu bytes, the recurrence needs %zu", workspace_bytes, p.look_bytes);
+    if ((rc = check_plan(d, p))) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    if (d->tokens == 0) return copy_states(initial_state, final_state, d->sequences * d->channels, s);
+    RecArgs a{};
+    a.x = x; a.r = r; a.i = i; a.lam = lam; a.seq = make_seq_map(d->tokens, d->sequences, seq_starts);
+    a.init = initial_state; a.y = y; a.final_state = final_state; a.chunk_states = chunk_states;
+    return launch_forward(d, p, a, workspace, s);
+}
+
+int im2win_gated_recurrence_backward_workspace_bytes(const im2win_recurrence_desc* d, size_t* bytes) {
+    int rc = check_desc(d);
+    if (rc) return rc;
+    if (!bytes) return fail(IM2WIN_ENULL, "bytes is NULL");
+    const Plan p = plan_of(d);
+    *bytes = p.look_bytes + 2 * p.states_bytes;     // the look, the chunks' sums, the chunks' states
+    return ok();
+}
+
+int im2win_gated_recurrence_backward(const im2win_recurrence_desc* d, const void* dy, const void* x, const void* r, const void* i,
+                                     const float* lam, const int32_t* seq_starts, const float* initial_state,
+                                     const float* d_final_state, const float* chunk_states, void* dx, void* dr, void* di,
+                                     float* dlam, float* d_initial_state, void* workspace, size_t workspace_bytes, void* stream) {
+    int rc = check_desc(d);
+    if (rc || (rc = check_sequences(d->tokens, d->sequences, seq_starts, true)) || (rc = need_ptr(lam, 4, "lam")) ||
+        (rc = need_ptr(dlam, 4, "dlam")) || (rc = may_ptr(initial_state, 4, "initial_state")) ||
+        (rc = may_ptr(d_final_state, 4, "d_final_state")) || (rc = may_ptr(d_initial_state, 4, "d_initial_state")) ||
+        (rc = may_ptr(chunk_states, 4, "chunk_states")))
+        return rc;
+    const Plan p = plan_of(d);
+    const size_t e = size_of(d->dtype), need = p.look_bytes + 2 * p.states_bytes;
+    if (d->tokens && ((rc = need_ptr(dy, e, "dy")) || (rc = need_ptr(x, e, "x")) || (rc = need_ptr(r, e, "r")) || (rc = need_ptr(i, e, "i")) ||
+                      (rc = need_ptr(dx, e, "dx")) || (rc = need_ptr(dr, e, "dr")) || (rc = need_ptr(di, e, "di")) ||
+                      (rc = need_ptr(workspace, 16, "workspace"))))
+        return rc;
+    if (workspace_bytes < need)
+        return fail(IM2WIN_EWORKSPACE, "workspace holds %zu bytes, the gradients need %zu", workspace_bytes, need);
+    if ((rc = check_plan(d, p))) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    char* ws = static_cast<char*>(workspace);
+    float* part = reinterpret_cast<float*>(ws + p.look_bytes);
+    if (d->tokens) {
+        const SeqMap seq = make_seq_map(d->tokens, d->sequences, seq_starts);
+        if (!chunk_states && p.chunks > 1) {
+            RecArgs f{};
+            f.x = x; f.r = r; f.i = i; f.lam = lam; f.seq = seq; f.init = initial_state;
+            f.chunk_states = reinterpret_cast<float*>(ws + p.look_bytes + p.states_bytes);
+            chunk_states = f.chunk_states;
+            if ((rc = launch_forward(d, p, f, ws, s))) return rc;
+        }
+        RecBwdArgs a{};
+        a.dy = dy; a.x = x; a.r = r; a.i = i; a.lam = lam; a.seq = seq;
+        a.init = initial_state; a.d_final = d_final_state; a.chunk_states = chunk_states;
+        a.dx = dx; a.dr = dr; a.di = di; a.d_init = d_initial_state; a.part = part;
+        a.look = look_of(p, d->channels, ws);
+        a.ld_x = d->ld_x; a.ld_r = d->ld_r; a.ld_i = d->ld_i;
+        a.channels = (int)d->channels; a.tiles = (int)p.tiles; a.c = d->c;
+        fill(p, ws, s);
+        with_type(d, [&](auto t, auto v) {
+            hipLaunchKernelGGL((recurrence_bwd_kernel<decltype(t), decltype(v)::value>), dim3((unsigned)(p.chunks * p.tiles)), dim3(kThreads), 0, s, a);
+        });
+    } else if ((rc = copy_states(d_final_state, d_initial_state, d->sequences * d->channels, s))) {
+        return rc;
+    }
+    hipLaunchKernelGGL(recurrence_bwd_sum_kernel, dim3((unsigned)((d->channels + kWave - 1) / kWave)), dim3(kSumWaves * kWave), 0, s,
+                       part, lam, dlam, (int)p.chunks, (int)d->channels);
+    return launched("gated_recurrence_backward");
+}
+
+int im2win_gated_recurrence_step(const im2win_recurrence_desc* d, const void* x, const void* r, const void* i, const float* lam,
+                                 const int32_t* slots, float* state, int64_t state_slots, void* y, void* stream) {
+    int rc = check_desc(d);
+    if (rc || (rc = need_ptr(lam, 4, "lam"))) return rc;
+    if (state_slots < 0) return fail(IM2WIN_EINVAL, "state_slots must be >= 0 (got %lld)", (long long)state_slots);
+    if (d->tokens == 0) return ok();
+    const size_t e = size_of(d->dtype);
+    if ((rc = need_ptr(x, e, "x")) || (rc = need_ptr(r, e, "r")) || (rc = need_ptr(i, e, "i")) || (rc = need_ptr(y, e, "y")) ||
+        (rc = may_ptr(slots, 4, "slots")) || (rc = need_ptr(state, 4, "state")))
+        return rc;
+    const int64_t per = 256 * lane_channels(d), tiles = (d->channels + per - 1) / per;
+    if ((rc = check_launch(d->tokens * tiles, 256, "gated_recurrence_step"))) return rc;
+    RecStepArgs a{};
+    a.x = x; a.r = r; a.i = i; a.lam = lam; a.slots = slots; a.state = state; a.y = y;
+    a.ld_x = d->ld_x; a.ld_r = d->ld_r; a.ld_i = d->ld_i; a.state_slots = state_slots;
+    a.channels = (int)d->channels; a.c = d->c;
+    with_type(d, [&](auto t, auto v) {
+        hipLaunchKernelGGL((recurrence_step_kernel<decltype(t), decltype(v)::value>), dim3((unsigned)d->tokens, (unsigned)tiles), dim3(256), 0, static_cast<hipStream_t>(stream), a);
+    });
+    return launched("gated_recurrence_step");
+}
+
+}  // extern "C"
