@@ -4,8 +4,8 @@
  * the selective state space scan that reads its output, and the
  * root-mean-square norm with the residual's addition in front of both; and
  * those of the layers that stand between such layers in hybrid stacks: the
- * gated linear recurrence, and the norm of queries and keys with the position
- * rotation.
+ * gated linear recurrence, the norm of queries and keys with the position
+ * rotation, and attention with a sliding window.
  * Exported by libim2win beside the im2win entry points of im2win.h (same
  * error codes, error messages and conventions about streams and ownership;
  * see there).  Where this header differs:
@@ -360,6 +360,64 @@ int im2win_qk_norm_rope_backward(const im2win_qk_desc* d, const void* dyq, const
                                  const int32_t* positions, const float* freqs, void* dq, void* dk,
                                  float* dwq, float* dwk, void* workspace, size_t workspace_bytes,
                                  void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Attention with a sliding window and first tokens that stay visible        */
+/* ------------------------------------------------------------------------ */
+
+typedef struct {
+    int64_t tokens;            /* T, at most 2^30 (requests, for the step) */
+    int64_t sequences;         /* B >= 1 (not used by the step) */
+    int64_t q_heads, kv_heads; /* H and K; query head h reads key head h / (H / K) */
+    int64_t head_dim;          /* a multiple of 8 up to 256 */
+    int64_t window;            /* W >= 1: a token sees itself and the W-1 before it */
+    int64_t sinks;             /* S, 0 to 32: and the first S of its sequence */
+    int64_t ld_q, ld_k, ld_v;  /* row strides of q, k and v */
+    int32_t dtype;             /* of q, k, v, the caches, y and the gradients */
+    float scale;               /* > 0 */
+} im2win_window_desc;
+
+/*
+ * y[t][h] = sum_j w[j] v[j], w = softmax over j of scale * q[t][h] . k[j], for
+ * the positions j <= p of t's sequence with j > p - W or j < S, where p is
+ * t's position: past[b] + its row in the sequence.  Positions below past[b]
+ * are read from the request's cache, the others are the call's own rows.  A
+ * masked position does not enter, whatever its key and value hold.
+ *   q, k, v  device, T x H x head_dim and T x K x head_dim (k, v)
+ *   k_cache, v_cache  device, cache_slots x (S + W) x K x head_dim, or both
+ *            NULL: position j lies in row j where j < S, else in row
+ *            S + (j - S) mod W.  The call reads what lies before past[b] and
+ *            leaves the new tokens' keys and values there.
+ *   past     device, B int32, or NULL (zeros): tokens that the request had
+ *            before the call; values outside of [0, 2^30] are taken as the nearest
+ *   slots    device, B int32, or NULL (b): the request's slot of the cache.  No
+ *            two requests may name the same slot.  A request whose slot is
+ *            outside of [0, cache_slots) gets y = 0 and leaves the cache as it is.
+ *   y        device, T x H x head_dim
+ *   lse      device, T x H, fp32, or NULL: log of the sum of exp(scale q . k) (-inf
+ *            without visible keys), for the gradients
+ * Errors: EINVAL, ENULL, EALIGN, EOVERFLOW, EHIP.
+ */
+int im2win_window_attention(const im2win_window_desc* d, const void* q, const void* k, const void* v,
+                            const int32_t* seq_starts, void* k_cache, void* v_cache,
+                            int64_t cache_slots, const int32_t* past, const int32_t* slots, void* y,
+                            float* lse, void* stream);
+
+/* Bytes of workspace that im2win_window_attention_step takes.  Host only. */
+int im2win_window_attention_step_workspace_bytes(const im2win_window_desc* d, size_t* bytes);
+
+/*
+ * One token for each of d->tokens requests, at position past[i]: its key and
+ * value (rows of k and v) go to the request's cache, and y is the attention
+ * over what the cache then holds of the request.  past is needed and is not
+ * moved on; cache and slots as above.
+ *   workspace  device, 16-byte aligned, at least the bytes above (NULL when 0)
+ * Errors: EINVAL, ENULL, EALIGN, EWORKSPACE, EOVERFLOW, EHIP.
+ */
+int im2win_window_attention_step(const im2win_window_desc* d, const void* q, const void* k,
+                                 const void* v, void* k_cache, void* v_cache, int64_t cache_slots,
+                                 const int32_t* past, const int32_t* slots, void* y, void* workspace,
+                                 size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

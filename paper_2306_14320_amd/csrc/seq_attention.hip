@@ -1,0 +1,583 @@
+// Attention with a sliding window and a few first tokens that stay visible,
+// over packed sequences, and its form for single tokens.  For a query at
+// position p of its sequence,
+//   y = sum_j w_j v_j,  w = softmax_j(scale q k_j),
+// over the keys j <= p with j > p - window or j < sinks.
+//
+// One pass over the visible keys with the running maximum m and sum l of the
+// softmax; scores and weights never leave the registers.  Keys of positions
+// the request had before the call come from its cache, a ring of sinks +
+// window rows, in which the call leaves the new tokens' keys and values.
+#include "seq_attention.h"
+
+#include <algorithm>
+
+namespace im2win {
+namespace {
+
+struct AttnArgs {
+    const void *q, *k, *v;
+    void *k_cache, *v_cache;
+    const int32_t *past, *slots;
+    void* y;
+    float* lse;
+    SeqMap seq;
+    int64_t ld_q, ld_k, ld_v, cache_slots;
+    int64_t places, items;
+    int q_heads, kv_heads, dim, window, sinks;
+    int pack, tile;          // heads of a workgroup, its queries
+    float c;                 // scale log2(e)
+    // single tokens
+    int requests, splits, split_rows, stage;
+    float *part_ml, *part_o;
+};
+
+constexpr int kMaxPast = 1 << 30;
+
+__device__ __forceinline__ int past_of(const int32_t* past, int b) {
+    const int p = past ? uniform(past[b]) : 0;
+    return p < 0 ? 0 : p > kMaxPast ? kMaxPast : p;
+}
+// The row of position p in a request's cache
+__device__ __forceinline__ int ring(int p, int window, int sinks) { return p < sinks ? p : sinks + (p - sinks) % window; }
+
+template <typename T>
+__device__ __forceinline__ bool finite(T x) {
+    return (__float_as_uint((float)x) & 0x7f800000u) != 0x7f800000u;
+}
+
+// Running softmax of a lane's column and its output
+template <int DP>
+struct Running {
+    float m = -INFINITY, l = 0.0f;
+    f32x16 o[DP / 32];
+    __device__ __forceinline__ Running() {
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) o[t] = f32x16{};
+    }
+};
+
+// Takes NB blocks of 32 masked scores (raw products) into the running softmax
+// and leaves the weights in their place.
+template <int DP, int NB>
+__device__ __forceinline__ void soften(Running<DP>& r, f32x16 (&s)[NB], float c) {
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float m = fmaxf(r.m, top * c);
+    const float base = m == -INFINITY ? 0.0f : m;        // a column that has seen no key yet
+    if (__ballot(m > r.m)) {
+        const float a = __builtin_amdgcn_exp2f(r.m - base);
+        r.l *= a;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) r.o[t] *= a;
+    }
+    r.m = m;
+    float sum = 0.0f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -base));
+            sum += s[b][i];
+        }
+    r.l += sum;       // of the lane's half; the halves are added at the end
+}
+
+// The weights of 16 keys as a right operand: rounded to bf16 where the values
+// are, as their products' operand (2^-9 of a weight, against 2^-9 of a value).
+template <typename T>
+__device__ __forceinline__ Frag<T> weights(const f32x16& s, int part) {
+    Frag<T> f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f.set(j, s[8 * part + j]);
+    return f;
+}
+
+// Writes four neighbouring channels
+__device__ __forceinline__ void put4(float* p, float a, float b, float c, float d) {
+    const float v[4] = {a, b, c, d};
+    __builtin_memcpy(p, v, 16);
+}
+__device__ __forceinline__ void put4(bf16* p, float a, float b, float c, float d) {
+    const uint32_t v[2] = {pack_bf16(a, b), pack_bf16(c, d)};
+    __builtin_memcpy(p, v, 8);
+}
+
+template <typename T, int DP> constexpr int kTileKeys = sizeof(T) == 2 && DP <= 128 ? 64 : 32;
+// Waves a SIMD: two, of 256 registers, up to 384 bytes of a head's row but for
+// 192 bf16 channels, whose accumulators do not fit beside the queries; else one.
+template <typename T, int DP> constexpr int kFwdWaves = DP * sizeof(T) > 384 || DP >= 192 ? 1 : 2;
+// Whether the next tile's rows wait in registers while one is worked on.  Beside
+// 1 KB of queries and outputs a lane they would spill.
+template <typename T, int DP> constexpr bool kFwdAhead = DP * sizeof(T) <= 512;
+template <typename T, int DP> constexpr bool kStepAhead = DP * sizeof(T) <= 256;
+
+// ---------------------------------------------------------------------------
+// Prompts and training: a workgroup takes up to 128 columns, the queries of
+// `tile` rows for `pack` heads that share keys and values.  Their tiles pass
+// through LDS, the next one's loads in flight while one is worked on.
+// ---------------------------------------------------------------------------
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_attention_kernel(AttnArgs a) {
+    constexpr int BK = kTileKeys<T, DP>, NB = BK / 32;
+    using KV = Tile<T, DP, BK>;
+    static_assert(BK * KV::kChunks % kAttnThreads == 0, "whole rounds");
+    __shared__ __align__(16) char kt[KV::kBytes], vt[KV::kBytes];
+    __shared__ uint32_t flags[2];      // rows of the tile whose values are not all finite
+    const int64_t item = die_order(blockIdx.x, a.items);
+    if (item >= a.items) return;
+    const int hb = (int)(item / a.places);
+    const SeqTile st = seq_tile(a.seq, (int)(item % a.places), a.tile);
+    if (st.row >= st.len) return;
+    const int tid = threadIdx.x, wave = uniform(tid / kWave), lane = tid % kWave, half = lane / 32;
+    const int h0 = hb * a.pack, kvh = h0 / (a.q_heads / a.kv_heads);
+    const int rows = a.sinks + a.window;
+    const int64_t slot = !a.k_cache ? 0 : a.slots ? uniform(a.slots[st.b]) : st.b;
+    const bool served = !a.k_cache || (slot >= 0 && slot < a.cache_slots);
+    const int past = a.k_cache ? past_of(a.past, st.b) : 0;
+
+    // the lane's column
+    const int col = wave * kCols + lane % kCols, qi = col / a.pack;
+    const int row = st.row + qi;                        // of the sequence
+    const bool live = qi < a.tile && row < st.len;
+    const int last = st.row + a.tile < st.len ? st.row + a.tile - 1 : st.len - 1;
+    const int pos = past + (row < last ? row : last);
+    const int head = h0 + col % a.pack;
+    Frag<T> q[DP / 16];
+    {
+        const T* p = static_cast<const T*>(a.q) + (st.first + (row < last ? row : last)) * a.ld_q + (int64_t)head * a.dim;
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+            if (16 * s + 8 * half < a.dim) q[s].load(p + 16 * s + 8 * half);
+            else q[s].zero();
+        }
+    }
+
+    // the keys: where sinks lie in front of the first query's window a tile of them, then the window's
+    const int qfirst = past + st.row, qlast = past + last;
+    const int begin = qfirst - a.window + 1 > 0 ? qfirst - a.window + 1 : 0;
+    const int first_end = a.sinks < begin ? a.sinks : begin;      // keys of the sinks' tile
+    const int end = qlast + 1;
+    // queries of this wave, for tiles that all of them see
+    const int wq0 = past + st.row + wave * kCols / a.pack;
+    int wq1 = past + st.row + (wave * kCols + kCols - 1) / a.pack;
+    wq1 = wq1 < qlast ? wq1 : qlast;
+
+    Chunk kr[KV::kPerThread], vr[KV::kPerThread];
+    auto address = [&](int p, const void* in, const void* cache, int64_t ld) {
+        if (p < past) return static_cast<const T*>(cache) + ((slot * rows + ring(p, a.window, a.sinks)) * a.kv_heads + kvh) * a.dim;
+        return static_cast<const T*>(in) + (st.first + (p - past)) * ld + (int64_t)kvh * a.dim;
+    };
+    auto fetch = [&](int base, int stop) {
+#pragma unroll
+        for (int i = 0; i < KV::kPerThread; ++i) {
+            const int n = tid + i * kAttnThreads, p = base + n / KV::kChunks, e = n % KV::kChunks * KV::kElems;
+            if (p < stop && e < a.dim) {
+                kr[i].load(address(p, a.k, a.k_cache, a.ld_k) + e);
+                vr[i].load(address(p, a.v, a.v_cache, a.ld_v) + e);
+            } else {
+                kr[i].zero();
+                vr[i].zero();
+            }
+        }
+    };
+
+    Running<DP> r;
+    bool sink_tile = first_end > 0;
+    int base = sink_tile ? 0 : begin, stop = sink_tile ? first_end : end;
+    if (!served) base = stop = end;
+    if (kFwdAhead<T, DP> && base < stop) fetch(base, stop);
+    while (base < stop) {
+        if (!kFwdAhead<T, DP>) fetch(base, stop);
+        // a tile that some column does not see all of: its values' infinities and NaN stay out of the product
+        const bool partial = base + BK > stop || base + BK - 1 > qfirst || base <= qlast - a.window;
+        __syncthreads();
+        if (tid < 2) flags[tid] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < KV::kPerThread; ++i) {
+            const int n = tid + i * kAttnThreads, rw = n / KV::kChunks, at = KV::at(rw, n % KV::kChunks);
+            kr[i].store(kt + at);
+            if (partial && drop_nonfinite<T>(vr[i])) atomicOr(&flags[rw / 32], 1u << rw % 32);
+            vr[i].store(vt + at);
+        }
+        __syncthreads();
+        const int now = base, now_stop = stop;
+        if (sink_tile) sink_tile = false, base = begin, stop = end;
+        else base += BK;
+        if (kFwdAhead<T, DP> && base < stop) fetch(base, stop);
+        // keys in front of the wave's first window (but for sinks) or behind its last query
+        if (now > wq1 || (now + BK <= wq0 - a.window + 1 && now >= a.sinks)) continue;
+
+        f32x16 s[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[b] = f32x16{};
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) mma(s[b], KV::row_frag(kt, 32 * b + lane % 32, d, half), q[d]);
+        const bool whole = now + BK <= now_stop && now + BK - 1 <= wq0 && now > wq1 - a.window;
+        if (!whole) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int p = now + 32 * b + acc_row(i, half);
+                    const bool seen = p < now_stop && p <= pos && (p > pos - a.window || p < a.sinks);
+                    s[b][i] = seen ? s[b][i] : -INFINITY;
+                }
+        }
+        soften<DP, NB>(r, s, a.c);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                const Frag<T> w = weights<T>(s[b], part);
+#pragma unroll
+                for (int t = 0; t < DP / 32; ++t) mma(r.o[t], KV::col_frag(vt, t, 2 * b + part, lane), w);
+            }
+        // what was kept out of the product: a column that sees such a value has it
+        for (int f = 0; f < NB; ++f)
+            for (uint32_t rest = uniform(flags[f]); rest; rest &= rest - 1) {
+                const int p = now + 32 * f + __builtin_ctz(rest);
+                const bool seen = p <= pos && (p > pos - a.window || p < a.sinks);
+                const T* v = address(p, a.v, a.v_cache, a.ld_v);
+#pragma unroll
+                for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int d = 32 * t + acc_row(i, half);
+                        if (d < a.dim && seen && !finite(v[d])) r.o[t][i] += (float)v[d];
+                    }
+            }
+    }
+    const float l = r.l + __shfl_xor(r.l, 32);
+    if (!live) return;
+    const float scale = l == 0.0f ? 0.0f : 1.0f / l;      // without a visible key: zeros
+    const int64_t t = st.first + row;
+    T* y = static_cast<T*>(a.y) + (t * a.q_heads + head) * a.dim;
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int d = 32 * b + acc_row(i, half);
+            if (d < a.dim) put4(y + d, r.o[b][i] * scale, r.o[b][i + 1] * scale, r.o[b][i + 2] * scale, r.o[b][i + 3] * scale);
+        }
+    if (a.lse && half == 0) a.lse[t * a.q_heads + head] = l == 0.0f ? -INFINITY : (r.m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// The cache behind a prompt: a wave takes a new token, and copies its keys and
+// values where they are among the first tokens or the last window.
+template <typename T>
+__global__ __launch_bounds__(kAttnThreads) void window_cache_kernel(AttnArgs a) {
+    const int t = uniform((int)(blockIdx.x * 4 + threadIdx.x / kWave)), lane = threadIdx.x % kWave;
+    if (t < a.seq.first(0) || t >= a.seq.first(a.seq.count)) return;
+    const SeqMap::Found f = a.seq.at(t);
+    const int64_t slot = a.slots ? uniform(a.slots[f.b]) : f.b;
+    if (slot < 0 || slot >= a.cache_slots) return;
+    const int past = past_of(a.past, f.b), p = past + t - f.first, end = past + f.end - f.first;
+    if (p >= a.sinks && p < end - a.window) return;
+    const int n = a.kv_heads * a.dim;
+    const int64_t to = (slot * (a.sinks + a.window) + ring(p, a.window, a.sinks)) * n;
+    constexpr int E = 16 / sizeof(T);
+    for (int e = lane * E; e < n; e += kWave * E) {
+        Chunk k, v;
+        k.load(static_cast<const T*>(a.k) + t * a.ld_k + e);
+        v.load(static_cast<const T*>(a.v) + t * a.ld_v + e);
+        k.store(static_cast<T*>(a.k_cache) + to + e);
+        v.store(static_cast<T*>(a.v_cache) + to + e);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Single tokens: the columns are the heads of a request that share keys and
+// values; a workgroup takes a share of its cache's rows, each wave 32 of them at
+// a time.  Keys go straight to the operand's registers, values through the
+// wave's own part of LDS, which turns them.  The new token's row is read from
+// the inputs and written to the cache by the lanes that hold it.  Bound by memory.
+// ---------------------------------------------------------------------------
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void window_step_kernel(AttnArgs a) {
+    using V = Tile<T, DP, 32>;
+    constexpr int kRound = 32 * V::kChunks / kWave;      // chunks of a lane
+    extern __shared__ __align__(16) char stage[];        // a.stage bytes of each wave
+    __shared__ float ml[4][2][kCols];
+    const int tid = threadIdx.x, wave = uniform(tid / kWave), lane = tid % kWave, half = lane / 32;
+    const int blocks = a.q_heads / a.pack;
+    const int split = blockIdx.x % a.splits, hb = blockIdx.x / a.splits % blocks, b = blockIdx.x / a.splits / blocks;
+    const int h0 = hb * a.pack, kvh = h0 / (a.q_heads / a.kv_heads);
+    const int64_t rows = a.sinks + a.window, slot = a.slots ? uniform(a.slots[b]) : b;
+    const bool served = slot >= 0 && slot < a.cache_slots;
+    const int past = past_of(a.past, b), fresh = ring(past, a.window, a.sinks);
+    const int filled = !served ? 0 : past + 1 < rows ? past + 1 : (int)rows;
+    const int from = split * a.split_rows, to = from + a.split_rows < filled ? from + a.split_rows : filled;
+    const int col = lane % kCols, head = h0 + (col < a.pack ? col : 0);
+    const int64_t cached = (slot * rows * a.kv_heads + kvh) * a.dim, step = (int64_t)a.kv_heads * a.dim;
+    T* kc = static_cast<T*>(a.k_cache) + (served ? cached : 0);
+    T* vc = static_cast<T*>(a.v_cache) + (served ? cached : 0);
+    const T* kn = static_cast<const T*>(a.k) + b * a.ld_k + (int64_t)kvh * a.dim;
+    const T* vn = static_cast<const T*>(a.v) + b * a.ld_v + (int64_t)kvh * a.dim;
+    char* mine = stage + wave * a.stage;
+
+    Frag<T> q[DP / 16];
+    const T* qp = static_cast<const T*>(a.q) + b * a.ld_q + (int64_t)head * a.dim;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+        if (16 * s + 8 * half < a.dim) q[s].load(qp + 16 * s + 8 * half);
+        else q[s].zero();
+    }
+    Frag<T> k[DP / 16];
+    Chunk v[kRound];
+    auto fetch_k = [&](int base) {
+        const int row = base + lane % 32;
+        const T* p = row == fresh ? kn : kc + row * step;
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+            if (row < to && 16 * s + 8 * half < a.dim) k[s].load(p + 16 * s + 8 * half);
+            else k[s].zero();
+        }
+    };
+    auto fetch_v = [&](int base) {
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) {
+            const int n = lane + i * kWave, rw = base + n / V::kChunks, e = n % V::kChunks * V::kElems;
+            if (rw < to && e < a.dim) v[i].load((rw == fresh ? vn : vc + rw * step) + e);
+            else v[i].zero();
+        }
+    };
+    constexpr bool kAhead = kStepAhead<T, DP>;
+    Running<DP> r;
+    const int first = from + wave * 32;
+    if (kAhead && first < to) fetch_k(first), fetch_v(first);
+    for (int base = first; base < to; base += 128) {
+        if (!kAhead) fetch_k(base);
+        const bool has_fresh = fresh >= base && fresh < base + 32;      // the new token's row goes to the cache
+        if (has_fresh && base + lane % 32 == fresh) {
+#pragma unroll
+            for (int s = 0; s < DP / 16; ++s)
+                if (16 * s + 8 * half < a.dim) __builtin_memcpy(kc + fresh * step + 16 * s + 8 * half, &k[s].v, 8 * sizeof(T));
+        }
+        f32x16 s[1] = {f32x16{}};
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d) mma(s[0], k[d], q[d]);
+        if (!kAhead) fetch_v(base);
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) {
+            const int n = lane + i * kWave, e = n % V::kChunks * V::kElems;
+            if (has_fresh && base + n / V::kChunks == fresh && e < a.dim) v[i].store(vc + fresh * step + e);
+            v[i].store(mine + V::at(n / V::kChunks, n % V::kChunks));
+        }
+        if (kAhead && base + 128 < to) fetch_k(base + 128), fetch_v(base + 128);
+        if (base + 32 > to) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[0][i] = base + acc_row(i, half) < to ? s[0][i] : -INFINITY;
+        }
+        soften<DP, 1>(r, s, a.c);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const Frag<T> w = weights<T>(s[0], part);
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t) mma(r.o[t], V::col_frag(mine, t, part, lane), w);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
+    // the four waves' shares: a channel's row of columns each, and their statistics
+    r.l += __shfl_xor(r.l, 32);
+    float* o = reinterpret_cast<float*>(mine);
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            if (col < a.pack) o[(32 * t + acc_row(i, half)) * a.pack + col] = r.o[t][i];
+    if (half == 0) ml[wave][0][col] = r.m, ml[wave][1][col] = r.l;
+    __syncthreads();
+    for (int n = tid; n < a.dim * a.pack; n += kAttnThreads) {
+        const int c = n % a.pack, d = n / a.pack;
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w][0][c]);
+        const float base = m == -INFINITY ? 0.0f : m;
+        float sum = 0.0f, l = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = __builtin_amdgcn_exp2f(ml[w][0][c] - base);
+            l = fmaf(ml[w][1][c], f, l);
+            sum = fmaf(reinterpret_cast<const float*>(stage + w * a.stage)[d * a.pack + c], f, sum);
+        }
+        const int64_t at = (int64_t)b * a.q_heads + h0 + c;
+        if (a.splits == 1) {
+            static_cast<T*>(a.y)[at * a.dim + d] = (T)(l == 0.0f ? 0.0f : sum / l);
+        } else {
+            a.part_o[(at * a.splits + split) * a.dim + d] = sum;
+            if (d == 0) a.part_ml[(at * a.splits + split) * 2] = m, a.part_ml[(at * a.splits + split) * 2 + 1] = l;
+        }
+    }
+}
+
+// The shares of a request's head: a wave, four channels a lane
+template <typename T>
+__global__ __launch_bounds__(kAttnThreads) void window_step_join_kernel(AttnArgs a) {
+    const int64_t at = (int64_t)blockIdx.x * 4 + threadIdx.x / kWave;
+    const int lane = threadIdx.x % kWave;
+    if (at >= (int64_t)a.requests * a.q_heads) return;
+    const float* ml = a.part_ml + at * a.splits * 2;
+    float m = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[2 * s]);
+    const float base = m == -INFINITY ? 0.0f : m;
+    float l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    const int d = 4 * lane;
+    for (int s = 0; s < a.splits; ++s) {
+        const float f = __builtin_amdgcn_exp2f(ml[2 * s] - base);
+        l = fmaf(ml[2 * s + 1], f, l);
+        if (d < a.dim) {
+            float v[4];
+            __builtin_memcpy(v, a.part_o + (at * a.splits + s) * a.dim + d, 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], f, o[i]);
+        }
+    }
+    const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+    if (d < a.dim) put4(static_cast<T*>(a.y) + at * a.dim + d, o[0] * scale, o[1] * scale, o[2] * scale, o[3] * scale);
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+template <typename F>
+void with_type(int32_t dtype, F f) {
+    if (dtype == IM2WIN_F32) f(float{});
+    else f(bf16{});
+}
+
+AttnArgs args_of(const im2win_window_desc* d, const void* q, const void* k, const void* v) {
+    AttnArgs a{};
+    a.q = q; a.k = k; a.v = v;
+    a.ld_q = d->ld_q; a.ld_k = d->ld_k; a.ld_v = d->ld_v;
+    a.q_heads = (int)d->q_heads; a.kv_heads = (int)d->kv_heads; a.dim = (int)d->head_dim;
+    a.window = (int)d->window; a.sinks = (int)d->sinks;
+    a.c = d->scale * kLog2e;
+    a.pack = heads_packed(d->q_heads, d->kv_heads);
+    a.tile = kGroupCols / a.pack;
+    return a;
+}
+
+int check_cache(const im2win_window_desc* d, const void* k_cache, const void* v_cache, int64_t cache_slots, const int32_t* past, const int32_t* slots) {
+    const size_t e = attn_size_of(d->dtype);
+    int rc;
+    if (cache_slots < 0) return fail(IM2WIN_EINVAL, "cache_slots must be >= 0 (got %lld)", (long long)cache_slots);
+    if ((rc = need_ptr(k_cache, e, "k_cache")) || (rc = need_ptr(v_cache, e, "v_cache")) || (rc = may_ptr(slots, 4, "slots"))) return rc;
+    return may_ptr(past, 4, "past");
+}
+
+// Shares of a request's rows: none where requests and heads fill the chip
+// twice over; else as many as do, of 128 rows (one round of the workgroup) at least.
+struct Split {
+    int splits, rows;
+};
+Split split_of(const im2win_window_desc* d) {
+    const int64_t blocks = d->tokens * (d->q_heads / heads_packed(d->q_heads, d->kv_heads)), rows = d->sinks + d->window;
+    int64_t n = blocks ? (512 + blocks - 1) / blocks : 1;
+    n = std::max<int64_t>(1, std::min(n, (rows + 127) / 128));
+    Split s{};
+    s.rows = (int)(((rows + n - 1) / n + 127) / 128 * 128);
+    s.splits = (int)((rows + s.rows - 1) / s.rows);
+    return s;
+}
+size_t step_bytes(const im2win_window_desc* d) {
+    const Split s = split_of(d);
+    if (s.splits == 1) return 0;
+    return (size_t)(d->tokens * d->q_heads * s.splits) * (size_t)(d->head_dim + 2) * 4;
+}
+
+}  // namespace
+}  // namespace im2win
+
+using namespace im2win;
+
+extern "C" {
+
+int im2win_window_attention(const im2win_window_desc* d, const void* q, const void* k, const void* v, const int32_t* seq_starts,
+                            void* k_cache, void* v_cache, int64_t cache_slots, const int32_t* past, const int32_t* slots, void* y, float* lse,
+                            void* stream) {
+    int rc = check_attention(d);
+    if (rc || (rc = check_sequences(d->tokens, d->sequences, seq_starts, true))) return rc;
+    const bool cached = k_cache || v_cache;
+    if (cached && (rc = check_cache(d, k_cache, v_cache, cache_slots, past, slots))) return rc;
+    if (!cached && (past || slots)) return fail(IM2WIN_EINVAL, "past and slots belong to a cache (k_cache is NULL)");
+    if (d->tokens == 0) return ok();
+    const size_t e = attn_size_of(d->dtype);
+    if ((rc = need_ptr(q, e, "q")) || (rc = need_ptr(k, e, "k")) || (rc = need_ptr(v, e, "v")) || (rc = need_ptr(y, e, "y")) || (rc = may_ptr(lse, 4, "lse"))) return rc;
+    AttnArgs a = args_of(d, q, k, v);
+    a.k_cache = k_cache; a.v_cache = v_cache; a.cache_slots = cache_slots; a.past = past; a.slots = slots;
+    a.y = y; a.lse = lse;
+    a.seq = make_seq_map(d->tokens, d->sequences, seq_starts);
+    a.places = seq_places(d->tokens, d->sequences, seq_starts, a.tile);
+    a.items = a.places * (d->q_heads / a.pack);
+    const int64_t groups = (a.items + 7) / 8 * 8, copies = (d->tokens + 3) / 4;
+    if ((rc = check_launch(groups, kAttnThreads, "window_attention")) || (rc = check_launch(copies, kAttnThreads, "window_attention's cache"))) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    with_type(d->dtype, [&](auto t) {
+        using T = decltype(t);
+        with_head(d->head_dim, [&](auto dp) {
+            hipLaunchKernelGGL((window_attention_kernel<T, decltype(dp)::value>), dim3((unsigned)groups), dim3(kAttnThreads), 0, s, a);
+        });
+        if (cached) hipLaunchKernelGGL((window_cache_kernel<T>), dim3((unsigned)copies), dim3(kAttnThreads), 0, s, a);
+    });
+    return launched("window_attention");
+}
+
+int im2win_window_attention_step_workspace_bytes(const im2win_window_desc* d, size_t* bytes) {
+    int rc = check_attention(d);
+    if (rc) return rc;
+    if (!bytes) return fail(IM2WIN_ENULL, "bytes is NULL");
+    *bytes = step_bytes(d);
+    return ok();
+}
+
+int im2win_window_attention_step(const im2win_window_desc* d, const void* q, const void* k, const void* v, void* k_cache, void* v_cache,
+                                 int64_t cache_slots, const int32_t* past, const int32_t* slots, void* y, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+    int rc = check_attention(d);
+    if (rc) return rc;
+    if (d->tokens == 0) return ok();
+    const size_t e = attn_size_of(d->dtype), need = step_bytes(d);
+    if ((rc = need_ptr(q, e, "q")) || (rc = need_ptr(k, e, "k")) || (rc = need_ptr(v, e, "v")) || (rc = need_ptr(y, e, "y")) ||
+        (rc = check_cache(d, k_cache, v_cache, cache_slots, past, slots)) || (rc = need_ptr(past, 4, "past")) ||
+        (need && (rc = need_ptr(workspace, 16, "workspace"))))
+        return rc;
+    if (workspace_bytes < need) return fail(IM2WIN_EWORKSPACE, "workspace holds %zu bytes, the step needs %zu", workspace_bytes, need);
+    AttnArgs a = args_of(d, q, k, v);
+    a.k_cache = k_cache; a.v_cache = v_cache; a.cache_slots = cache_slots; a.past = past; a.slots = slots;
+    a.y = y;
+    const Split sp = split_of(d);
+    a.requests = (int)d->tokens; a.splits = sp.splits; a.split_rows = sp.rows;
+    a.part_o = static_cast<float*>(workspace);
+    a.part_ml = a.part_o + d->tokens * d->q_heads * sp.splits * d->head_dim;
+    const int64_t groups = d->tokens * (d->q_heads / a.pack) * sp.splits, joins = (d->tokens * d->q_heads + 3) / 4;
+    if ((rc = check_launch(groups, kAttnThreads, "window_attention_step")) || (rc = check_launch(joins, kAttnThreads, "window_attention_step's shares"))) return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t attribute = hipSuccess;
+    with_type(d->dtype, [&](auto t) {
+        using T = decltype(t);
+        with_head(d->head_dim, [&](auto dp) {
+            constexpr int DP = decltype(dp)::value;
+            // a wave's values of 32 rows, and behind them its share of the outputs
+            a.stage = std::max(Tile<T, DP, 32>::kBytes, a.pack * DP * 4);
+            if (4 * a.stage > 65536)
+                attribute = hipFuncSetAttribute(reinterpret_cast<const void*>(&window_step_kernel<T, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, 4 * a.stage);
+            if (attribute == hipSuccess)
+                hipLaunchKernelGGL((window_step_kernel<T, DP>), dim3((unsigned)groups), dim3(kAttnThreads), 4 * a.stage, s, a);
+        });
+        if (sp.splits > 1 && attribute == hipSuccess)
+            hipLaunchKernelGGL((window_step_join_kernel<T>), dim3((unsigned)joins), dim3(kAttnThreads), 0, s, a);
+    });
+    if (attribute != hipSuccess) return fail(IM2WIN_EHIP, "window_attention_step's LDS: %s", hipGetErrorString(attribute));
+    return launched("window_attention_step");
+}
+
+}  // extern "C"

@@ -27,6 +27,9 @@ __all__ = [
     "im2win_qk_desc", "im2win_qk_norm_rope", "im2win_qk_norm_rope_backward_workspace_bytes",
     "im2win_qk_norm_rope_backward",
     "qk_norm_rope_desc_for", "qk_norm_rope", "qk_norm_rope_backward", "QkGradients",
+    "im2win_window_desc", "im2win_window_attention", "im2win_window_attention_step_workspace_bytes",
+    "im2win_window_attention_step",
+    "window_attention_desc_for", "window_attention", "window_attention_step",
 ]
 
 
@@ -43,8 +46,16 @@ class im2win_qk_desc(_Desc):
                 ("eps", ctypes.c_float)]
 
 
+class im2win_window_desc(_Desc):
+    """Mirror of the C ``im2win_window_desc``."""
+    _fields_ = [("tokens", _I64), ("sequences", _I64), ("q_heads", _I64), ("kv_heads", _I64), ("head_dim", _I64),
+                ("window", _I64), ("sinks", _I64), ("ld_q", _I64), ("ld_k", _I64), ("ld_v", _I64),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 _REC = ctypes.POINTER(im2win_recurrence_desc)
 _QK = ctypes.POINTER(im2win_qk_desc)
+_WIN = ctypes.POINTER(im2win_window_desc)
 
 SIGNATURES = {
     "im2win_gated_recurrence_chunks": [_REC, ctypes.POINTER(_I64)],
@@ -56,6 +67,9 @@ SIGNATURES = {
     "im2win_qk_norm_rope": [_QK] + [_P] * 9,
     "im2win_qk_norm_rope_backward_workspace_bytes": [_QK, ctypes.POINTER(_SZ)],
     "im2win_qk_norm_rope_backward": [_QK] + [_P] * 13 + [_SZ, _P],
+    "im2win_window_attention": [_WIN] + [_P] * 6 + [_I64] + [_P] * 5,
+    "im2win_window_attention_step_workspace_bytes": [_WIN, ctypes.POINTER(_SZ)],
+    "im2win_window_attention_step": [_WIN] + [_P] * 5 + [_I64] + [_P] * 4 + [_SZ, _P],
 }
 
 
@@ -107,6 +121,21 @@ def im2win_qk_norm_rope_backward(desc, dyq, dyk, q, k, wq, wk, positions, freqs,
                                  workspace_bytes, stream) -> None:
     _check(load_library().im2win_qk_norm_rope_backward(ctypes.byref(desc), dyq, dyk, q, k, wq, wk, positions, freqs, dq,
                                                        dk, dwq, dwk, workspace, workspace_bytes, stream))
+
+
+def im2win_window_attention(desc, q, k, v, seq_starts, k_cache, v_cache, cache_slots, past, slots, y, lse, stream) -> None:
+    _check(load_library().im2win_window_attention(ctypes.byref(desc), q, k, v, seq_starts, k_cache, v_cache,
+                                                  cache_slots, past, slots, y, lse, stream))
+
+
+def im2win_window_attention_step_workspace_bytes(desc) -> int:
+    return _bytes("im2win_window_attention_step_workspace_bytes", desc)
+
+
+def im2win_window_attention_step(desc, q, k, v, k_cache, v_cache, cache_slots, past, slots, y, workspace,
+                                 workspace_bytes, stream) -> None:
+    _check(load_library().im2win_window_attention_step(ctypes.byref(desc), q, k, v, k_cache, v_cache, cache_slots, past,
+                                                       slots, y, workspace, workspace_bytes, stream))
 
 
 # ---------------------------------------------------------------------------
@@ -261,3 +290,75 @@ def qk_norm_rope_backward(dyq, dyk, q, k, wq, wk, desc, positions=None, freqs=No
     im2win_qk_norm_rope_backward(desc, dyqp, dykp, qp, kp, wqp, wkp, pp, fp, dqp, dkp, dwq.data_ptr(), dwk.data_ptr(),
                                  wsp, wsb, _stream_on(stream, dev))
     return QkGradients(dq, dk, dwq, dwk)
+
+
+# ---------------------------------------------------------------------------
+# Attention with a sliding window
+# ---------------------------------------------------------------------------
+
+def window_attention_desc_for(q, k, v, window, sinks=0, sequences=1, scale=None) -> im2win_window_desc:
+    """Descriptor of the attention of q (T x H x head size) over k and v (T x K
+    x head size), rows of any stride, in `sequences` packed sequences: a token
+    sees itself, the window - 1 tokens before it, and the first `sinks` of its
+    sequence; scale is head size ** -0.5 when None."""
+    ld = [_row_stride(t, n) for t, n in ((q, "q"), (k, "k"), (v, "v"))]
+    if q.dim() != 3 or k.dim() != 3 or k.shape != v.shape or q.shape[::2] != k.shape[::2] or not q.dtype == k.dtype == v.dtype:
+        raise ValueError("q must be T x H x D, k and v T x K x D, of one dtype (got %s, %s and %s)"
+                         % (tuple(q.shape), tuple(k.shape), tuple(v.shape)))
+    t, h, dim = q.shape
+    return im2win_window_desc(t, sequences, h, k.shape[1], dim, window, sinks, *ld, _dtype_code(q.dtype),
+                              dim ** -0.5 if scale is None else scale)
+
+
+def _att_inputs(q, k, v, d):
+    ty, dev, rows = _torch_dtype(d), _device_of(q, "q"), (d.tokens, d.q_heads, d.head_dim)
+    keys = (d.tokens, d.kv_heads, d.head_dim)
+    return dev, ty, rows, (_rows(q, "q", rows, ty, d.ld_q, dev), _rows(k, "k", keys, ty, d.ld_k, dev),
+                           _rows(v, "v", keys, ty, d.ld_v, dev))
+
+
+def _caches(k_cache, v_cache, d, ty, dev):
+    """The pointers of both caches and their slots."""
+    if not isinstance(k_cache, torch.Tensor) or not isinstance(v_cache, torch.Tensor):
+        raise ValueError("k_cache and v_cache must be tensors")
+    shape = (k_cache.shape[0], d.sinks + d.window, d.kv_heads, d.head_dim)
+    return _dense(k_cache, "k_cache", shape, ty, dev), _dense(v_cache, "v_cache", shape, ty, dev), shape[0]
+
+
+def window_attention(q, k, v, desc, seq_starts=None, k_cache=None, v_cache=None, past=None, slots=None, y=None,
+                     lse=None, stream=None):
+    """y = softmax(scale q k) v over the visible keys, T x H x head size in q's
+    dtype.  With k_cache and v_cache (slots x (sinks + window) x K x head size)
+    the sequences go on from requests that have had past (int32, zeros when
+    None) tokens, in the slots named (int32, sequence b's is b when None;
+    outside of the cache: y = 0, nothing is kept), and their caches are moved
+    on.  lse (T x H, fp32), if given, receives what the gradients need."""
+    d = desc
+    dev, ty, rows, (qp, kp, vp) = _att_inputs(q, k, v, d)
+    sp = _dense(seq_starts, "seq_starts", (d.sequences + 1,), torch.int32, dev)
+    kcp = vcp = None
+    pool = 0
+    if k_cache is not None or v_cache is not None:
+        kcp, vcp, pool = _caches(k_cache, v_cache, d, ty, dev)
+    pp = _dense(past, "past", (d.sequences,), torch.int32, dev)
+    slp = _dense(slots, "slots", (d.sequences,), torch.int32, dev)
+    lp = _dense(lse, "lse", (d.tokens, d.q_heads), _F32, dev)
+    y, yp = _out(y, "y", rows, ty, q, dev, stream)
+    im2win_window_attention(d, qp, kp, vp, sp, kcp, vcp, pool, pp, slp, yp, lp, _stream_on(stream, dev))
+    return y
+
+
+def window_attention_step(q, k, v, k_cache, v_cache, past, desc, slots=None, y=None, workspace=None, stream=None):
+    """One token of each request, at position past[i] (int32; not moved on):
+    its key and value go to the request's cache, y is the attention over what
+    the cache then holds of the request.  slots (int32) as for the other
+    single-token calls."""
+    d = desc
+    dev, ty, rows, (qp, kp, vp) = _att_inputs(q, k, v, d)
+    kcp, vcp, pool = _caches(k_cache, v_cache, d, ty, dev)
+    pp = _dense(past, "past", (d.tokens,), torch.int32, dev)
+    slp = _dense(slots, "slots", (d.tokens,), torch.int32, dev)
+    y, yp = _out(y, "y", rows, ty, q, dev, stream)
+    workspace, wsp, wsb = _workspace(workspace, im2win_window_attention_step_workspace_bytes(d), q, stream)
+    im2win_window_attention_step(d, qp, kp, vp, kcp, vcp, pool, pp, slp, yp, wsp, wsb, _stream_on(stream, dev))
+    return y

@@ -115,3 +115,27 @@ def rotated(u, angle, rot, near, back=False):
 
 def qk(x, w, angle, rot, near, eps):
     return rotated(x / (x.square().mean(-1, keepdim=True) + eps).sqrt() * w, angle, rot, near)
+
+
+def visible(n, m, past, window, sinks):
+    """Which of the keys 0 .. m-1 the queries past .. past+n-1 see: n x m."""
+    i, j = torch.arange(past, past + n)[:, None], torch.arange(m)[None]
+    return (j <= i) & ((j > i - window) | (j < sinks))
+
+
+def attend(q, k, v, past, window, sinks, scale):
+    """One head of one sequence, keys from position 0: y, the log of the sums
+    of the exponentials, and the bound of y's fp32 error for weights that are
+    rounded to a type of unit roundoff u: a function of u."""
+    seen = visible(q.shape[0], k.shape[0], past, window, sinks)
+    s = (q @ k.t() * scale).masked_fill(~seen, -float("inf"))
+    w = torch.softmax(s, 1)
+    # a score is a sum of D products; weights carry its error twice (their own and the sum's)
+    size = torch.where(seen, q.abs() @ k.abs().t() * scale, 0.0).amax(1, keepdim=True)
+    rel = 2 * (q.shape[1] + 8) * U32 * size + (seen.sum(1, keepdim=True) + 24) * U32
+    wv = w @ v.abs()
+    return w @ v, torch.logsumexp(s, 1), (lambda u: (rel + u) * wv), (rel + 8 * U32 * (1 + s.amax(1, keepdim=True).abs())).flatten()
+
+
+def ring_row(p, window, sinks):
+    return p if p < sinks else sinks + (p - sinks) % window
