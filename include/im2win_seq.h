@@ -419,6 +419,23 @@ int im2win_window_attention_step(const im2win_window_desc* d, const void* q, con
                                  const int32_t* past, const int32_t* slots, void* y, void* workspace,
                                  size_t workspace_bytes, void* stream);
 
+/* Bytes of workspace that im2win_window_attention_backward takes.  Host only. */
+int im2win_window_attention_backward_workspace_bytes(const im2win_window_desc* d, size_t* bytes);
+
+/*
+ * Gradients of im2win_window_attention without a cache, for dy (dense), with
+ * the y and lse that the forward call wrote.  An infinity or a NaN reaches
+ * gradients of its own sequence only (there, of masked places too).
+ *   dq          device, T x H x head_dim, dense
+ *   dk, dv      device, T x K x head_dim, dense
+ *   workspace   device, 16-byte aligned, at least the bytes above
+ * Errors: EINVAL, ENULL, EALIGN, EWORKSPACE, EOVERFLOW, EHIP.
+ */
+int im2win_window_attention_backward(const im2win_window_desc* d, const void* dy, const void* q,
+                                     const void* k, const void* v, const void* y, const float* lse,
+                                     const int32_t* seq_starts, void* dq, void* dk, void* dv,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,524 @@
+// Gradients of window attention.  With the weights w = exp(scale q k - lse) of
+// the forward call, dp = dy v and delta = dy y (over the channels),
+//   ds = w (dp - delta),  dq = scale sum_j ds k_j,
+//   dk = scale sum_t ds q_t,  dv = sum_t w dy_t.
+// A query that sees one key alone has w = 1 whatever its score: its ds is zero,
+// and taken as such.
+//
+// Three kernels, none of which stores scores or adds atomically:
+//  - queries' tiles walk their visible keys (dq, and delta for the others);
+//  - keys' tiles walk the queries of all their heads that see them by the
+//    window (dk, dv);
+//  - the first tokens' keys are seen by all queries behind: those pairs, cut
+//    into pieces of 512 queries, leave partial sums, which the tile of the
+//    sequence's first keys adds (launched before it).
+// Scores are computed twice: seven products of queries and keys where five
+// would do, against a sum of dq over the keys' tiles in memory.
+#include "seq_attention.h"
+
+#include <algorithm>
+
+namespace im2win {
+namespace {
+
+constexpr int kPiece = 512;        // queries whose sums for the first tokens' keys go together
+
+struct AttnBwdArgs {
+    const void *dy, *q, *k, *v, *y;
+    const float* lse;
+    void *dq, *dk, *dv;
+    float *delta, *part;           // part: place x key head x (dk, dv) x sinks x channels
+    SeqMap seq;
+    int64_t ld_q, ld_k, ld_v;
+    int64_t q_places, q_items, k_places, k_items, pieces;
+    int q_heads, kv_heads, dim, window, sinks;
+    int pack, tile;
+    float c, scale;
+};
+
+__device__ __forceinline__ void put4(float* p, float a, float b, float c, float d) {
+    const float v[4] = {a, b, c, d};
+    __builtin_memcpy(p, v, 16);
+}
+__device__ __forceinline__ void put4(bf16* p, float a, float b, float c, float d) {
+    const uint32_t v[2] = {pack_bf16(a, b), pack_bf16(c, d)};
+    __builtin_memcpy(p, v, 8);
+}
+
+// Sixteen values of an accumulator as a right operand (the weights and ds:
+// rounded to bf16 where the other operand is).
+template <typename T>
+__device__ __forceinline__ Frag<T> operand(const f32x16& s, int part) {
+    Frag<T> f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f.set(j, s[8 * part + j]);
+    return f;
+}
+
+template <typename T>
+__device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int dim) {
+    Frag<T> f;
+    if (16 * s + 8 * half < dim) f.load(row + 16 * s + 8 * half);
+    else f.zero();
+    return f;
+}
+
+template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 128 ? 64 : 32;
+template <typename T, int DP> constexpr int kDqWaves = DP * sizeof(T) > 256 ? 1 : 2;
+template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 192 ? 1 : 2;
+template <typename T, int DP> constexpr bool kBwdAhead = DP * sizeof(T) <= 256;
+
+// ---------------------------------------------------------------------------
+// dq and delta: workgroups and columns as in the forward kernel
+// ---------------------------------------------------------------------------
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_kernel(AttnBwdArgs a) {
+    constexpr int BK = kTileRows<T, DP>, NB = BK / 32;
+    using KV = Tile<T, DP, BK>;
+    static_assert(BK * KV::kChunks % kAttnThreads == 0, "whole rounds");
+    __shared__ __align__(16) char kt[KV::kBytes], vt[KV::kBytes];
+    const int64_t item = die_order(blockIdx.x, a.q_items);
+    if (item >= a.q_items) return;
+    const int hb = (int)(item / a.q_places);
+    const SeqTile st = seq_tile(a.seq, (int)(item % a.q_places), a.tile);
+    if (st.row >= st.len) return;
+    const int tid = threadIdx.x, wave = uniform(tid / kWave), lane = tid % kWave, half = lane / 32;
+    const int h0 = hb * a.pack, kvh = h0 / (a.q_heads / a.kv_heads);
+    const int col = wave * kCols + lane % kCols, qi = col / a.pack, row = st.row + qi;
+    const bool live = qi < a.tile && row < st.len;
+    const int last = st.row + a.tile < st.len ? st.row + a.tile - 1 : st.len - 1;
+    const int pos = row < last ? row : last, head = h0 + col % a.pack;
+    const int64_t t = st.first + pos, at = t * a.q_heads + head;
+    Frag<T> q[DP / 16], g[DP / 16];
+    float delta = 0.0f;
+    const T* qp = static_cast<const T*>(a.q) + t * a.ld_q + (int64_t)head * a.dim;
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) {
+        q[s] = load_frag(qp, s, half, a.dim);
+        g[s] = load_frag(static_cast<const T*>(a.dy) + at * a.dim, s, half, a.dim);
+        const Frag<T> y = load_frag(static_cast<const T*>(a.y) + at * a.dim, s, half, a.dim);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) delta = fmaf(g[s].get(i), y.get(i), delta);
+    }
+    delta += __shfl_xor(delta, 32);
+    if (live && half == 0) a.delta[at] = delta;
+    const float lse = a.lse[at] * kLog2e;
+    const bool single = pos == 0 || (a.window == 1 && a.sinks == 0);
+
+    const int begin = st.row - a.window + 1 > 0 ? st.row - a.window + 1 : 0;
+    const int first_end = a.sinks < begin ? a.sinks : begin, end = last + 1;
+    const int wq0 = st.row + wave * kCols / a.pack;
+    int wq1 = st.row + (wave * kCols + kCols - 1) / a.pack;
+    wq1 = wq1 < last ? wq1 : last;
+    Chunk kr[KV::kPerThread], vr[KV::kPerThread];
+    auto fetch = [&](int base, int stop) {
+#pragma unroll
+        for (int i = 0; i < KV::kPerThread; ++i) {
+            const int n = tid + i * kAttnThreads, p = base + n / KV::kChunks, e = n % KV::kChunks * KV::kElems;
+            if (p < stop && e < a.dim) {
+                kr[i].load(static_cast<const T*>(a.k) + (int64_t)(st.first + p) * a.ld_k + (int64_t)kvh * a.dim + e);
+                vr[i].load(static_cast<const T*>(a.v) + (int64_t)(st.first + p) * a.ld_v + (int64_t)kvh * a.dim + e);
+            } else {
+                kr[i].zero();
+                vr[i].zero();
+            }
+        }
+    };
+    f32x16 o[DP / 32];
+#pragma unroll
+    for (int i = 0; i < DP / 32; ++i) o[i] = f32x16{};
+    bool sink_tile = first_end > 0;
+    int base = sink_tile ? 0 : begin, stop = sink_tile ? first_end : end;
+    if (kBwdAhead<T, DP>) fetch(base, stop);
+    while (base < stop) {
+        if (!kBwdAhead<T, DP>) fetch(base, stop);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < KV::kPerThread; ++i) {
+            const int n = tid + i * kAttnThreads, to = KV::at(n / KV::kChunks, n % KV::kChunks);
+            kr[i].store(kt + to);
+            vr[i].store(vt + to);
+        }
+        __syncthreads();
+        const int now = base, now_stop = stop;
+        if (sink_tile) sink_tile = false, base = begin, stop = end;
+        else base += BK;
+        if (kBwdAhead<T, DP> && base < stop) fetch(base, stop);
+        if (now > wq1 || (now + BK <= wq0 - a.window + 1 && now >= a.sinks)) continue;
+        const bool whole = now + BK <= now_stop && now + BK - 1 <= wq0 && now > wq1 - a.window;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int d = 0; d < DP / 16; ++d) {
+                mma(s, KV::row_frag(kt, 32 * b + lane % 32, d, half), q[d]);
+                mma(dp, KV::row_frag(vt, 32 * b + lane % 32, d, half), g[d]);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -lse)) * (dp[i] - delta);
+            if (!whole) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int p = now + 32 * b + acc_row(i, half);
+                    const bool seen = p < now_stop && p <= pos && (p > pos - a.window || p < a.sinks) && !single;
+                    s[i] = seen ? s[i] : 0.0f;
+                }
+            }
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                const Frag<T> w = operand<T>(s, part);
+#pragma unroll
+                for (int d = 0; d < DP / 32; ++d) mma(o[d], KV::col_frag(kt, d, 2 * b + part, lane), w);
+            }
+        }
+    }
+    if (!live) return;
+    T* dq = static_cast<T*>(a.dq) + at * a.dim;
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int d = 32 * b + acc_row(i, half);
+            if (d < a.dim) put4(dq + d, o[b][i] * a.scale, o[b][i + 1] * a.scale, o[b][i + 2] * a.scale, o[b][i + 3] * a.scale);
+        }
+}
+
+// ---------------------------------------------------------------------------
+// A block of 32 queries in LDS against the wave's 32 keys, one a lane's
+// column: w and ds stay in the accumulators and are the right operands of
+// dv^T += dy^T w and dk^T += q^T ds.
+// ---------------------------------------------------------------------------
+template <typename T, int DP>
+struct Keys {
+    Frag<T> k[DP / 16], v[DP / 16];
+    f32x16 dk[DP / 32], dv[DP / 32];
+
+    __device__ __forceinline__ void load(const T* kp, const T* vp, int half, int dim, bool live) {
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+            if (live) {
+                k[s] = load_frag(kp, s, half, dim);
+                v[s] = load_frag(vp, s, half, dim);
+            } else {
+                k[s].zero();
+                v[s].zero();
+            }
+        }
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = f32x16{};
+    }
+    // seen(position) for the lane's key, and single(position), where the block
+    // is not seen as a whole; lse and delta are the block's rows' in LDS.
+    template <int R, typename F, typename G>
+    __device__ __forceinline__ void take(const char* qt, const char* gt, const float* lse, const float* delta, int b, int base, bool whole, float c, F seen, G single) {
+        using Q = Tile<T, DP, R>;
+        const int lane = threadIdx.x % kWave, half = lane / 32;
+        f32x16 s = {}, dp = {};
+#pragma unroll
+        for (int d = 0; d < DP / 16; ++d) {
+            mma(s, Q::row_frag(qt, 32 * b + lane % 32, d, half), k[d]);
+            mma(dp, Q::row_frag(gt, 32 * b + lane % 32, d, half), v[d]);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            float l[4], e[4];
+            __builtin_memcpy(l, lse + 32 * b + acc_row(i, half), 16);
+            __builtin_memcpy(e, delta + 32 * b + acc_row(i, half), 16);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                s[i + j] = __builtin_amdgcn_exp2f(fmaf(s[i + j], c, -l[j]));
+                dp[i + j] = s[i + j] * (dp[i + j] - e[j]);
+            }
+        }
+        if (!whole) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int p = base + 32 * b + acc_row(i, half);
+                const bool in = seen(p);
+                s[i] = in ? s[i] : 0.0f;
+                dp[i] = in && !single(p) ? dp[i] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            const Frag<T> w = operand<T>(s, part), ds = operand<T>(dp, part);
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d) {
+                mma(dv[d], Q::col_frag(gt, d, 2 * b + part, lane), w);
+                mma(dk[d], Q::col_frag(qt, d, 2 * b + part, lane), ds);
+            }
+        }
+    }
+};
+
+template <typename T, int DP>
+__global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_kernel(AttnBwdArgs a) {
+    constexpr int BQ = kTileRows<T, DP>, NB = BQ / 32;
+    using Q = Tile<T, DP, BQ>;
+    static_assert(BQ * Q::kChunks % kAttnThreads == 0, "whole rounds");
+    __shared__ __align__(16) char qt[Q::kBytes], gt[Q::kBytes];
+    __shared__ __align__(16) float lse[BQ], delta[BQ];
+    const int64_t item = die_order(blockIdx.x, a.k_items);
+    if (item >= a.k_items) return;
+    const int kvh = (int)(item / a.k_places);
+    const SeqTile st = seq_tile(a.seq, (int)(item % a.k_places), kGroupCols);
+    if (st.row >= st.len) return;
+    const int tid = threadIdx.x, wave = uniform(tid / kWave), lane = tid % kWave, half = lane / 32;
+    const int group = a.q_heads / a.kv_heads;
+    const int key = st.row + wave * kCols + lane % kCols;      // the lane's column
+    const bool live = key < st.len;
+    const int k0 = st.row + wave * kCols, k1 = k0 + kCols - 1;
+    Keys<T, DP> keys;
+    keys.load(static_cast<const T*>(a.k) + (int64_t)(st.first + key) * a.ld_k + (int64_t)kvh * a.dim,
+              static_cast<const T*>(a.v) + (int64_t)(st.first + key) * a.ld_v + (int64_t)kvh * a.dim, half, a.dim, live);
+
+    // queries that see some key of the tile by the window
+    const int begin = st.row, far = st.row + kGroupCols - 1 + a.window;
+    const int end = far < st.len ? far : st.len;
+    const int tiles = (end - begin + BQ - 1) / BQ;
+    Chunk qr[Q::kPerThread], gr[Q::kPerThread];
+    float lr = 0.0f, er = 0.0f;
+    auto fetch = [&](int n) {
+        const int head = kvh * group + n / tiles, base = begin + n % tiles * BQ;
+#pragma unroll
+        for (int i = 0; i < Q::kPerThread; ++i) {
+            const int m = tid + i * kAttnThreads, p = base + m / Q::kChunks, e = m % Q::kChunks * Q::kElems;
+            if (p < end && e < a.dim) {
+                qr[i].load(static_cast<const T*>(a.q) + (int64_t)(st.first + p) * a.ld_q + (int64_t)head * a.dim + e);
+                gr[i].load(static_cast<const T*>(a.dy) + ((int64_t)(st.first + p) * a.q_heads + head) * a.dim + e);
+            } else {
+                qr[i].zero();
+                gr[i].zero();
+            }
+        }
+        if (tid < BQ) {
+            const int64_t at = (int64_t)(st.first + base + tid) * a.q_heads + head;
+            lr = base + tid < end ? a.lse[at] * kLog2e : 0.0f;
+            er = base + tid < end ? a.delta[at] : 0.0f;
+        }
+    };
+    const int count = tiles * group;
+    if (kBwdAhead<T, DP>) fetch(0);
+    for (int n = 0; n < count; ++n) {
+        if (!kBwdAhead<T, DP>) fetch(n);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < Q::kPerThread; ++i) {
+            const int m = tid + i * kAttnThreads, to = Q::at(m / Q::kChunks, m % Q::kChunks);
+            qr[i].store(qt + to);
+            gr[i].store(gt + to);
+        }
+        if (tid < BQ) lse[tid] = lr, delta[tid] = er;
+        __syncthreads();
+        if (kBwdAhead<T, DP> && n + 1 < count) fetch(n + 1);
+        const int base = begin + n % tiles * BQ;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int p0 = base + 32 * b, p1 = p0 + 31;
+            if (p0 >= end || p1 < k0 || p0 - k1 >= a.window) continue;
+            const bool whole = p1 < end && k1 <= p0 && p1 - k0 < a.window;
+            keys.template take<BQ>(
+                qt, gt, lse, delta, b, base, whole, a.c, [&](int p) { return p < end && p >= key && p - key < a.window; },
+                [&](int p) { return p == 0 || (a.window == 1 && a.sinks == 0); });
+        }
+    }
+    // queries behind the window that see the first tokens
+    if (a.sinks && st.row == 0 && wave == 0 && key < a.sinks && st.len > a.window) {
+        const int from = a.window / kPiece, to = (st.len + kPiece - 1) / kPiece, place = st.first / kPiece + st.b;
+        for (int z = from; z < to; ++z) {
+            const float* p = a.part + (((int64_t)(a.seq.starts ? place : st.b * ((a.seq.len + kPiece - 1) / kPiece)) + z) * a.kv_heads + kvh) * 2 * a.sinks * a.dim + (int64_t)key * a.dim;
+#pragma unroll
+            for (int d = 0; d < DP / 32; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int e = 32 * d + acc_row(i, half);
+                    if (e < a.dim) {
+                        keys.dk[d][i] += p[e];
+                        keys.dv[d][i] += p[(int64_t)a.sinks * a.dim + e];
+                    }
+                }
+        }
+    }
+    if (!live) return;
+    const int64_t to = ((int64_t)(st.first + key) * a.kv_heads + kvh) * a.dim;
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+            const int d = 32 * b + acc_row(i, half);
+            if (d >= a.dim) continue;
+            put4(static_cast<T*>(a.dk) + to + d, keys.dk[b][i] * a.scale, keys.dk[b][i + 1] * a.scale, keys.dk[b][i + 2] * a.scale, keys.dk[b][i + 3] * a.scale);
+            put4(static_cast<T*>(a.dv) + to + d, keys.dv[b][i], keys.dv[b][i + 1], keys.dv[b][i + 2], keys.dv[b][i + 3]);
+        }
+}
+
+// ---------------------------------------------------------------------------
+// The first tokens' keys and the queries that have left them behind their
+// window: a workgroup takes a piece of 512 queries for all heads of a key head,
+// each wave 32 queries at a time in its own part of LDS.
+// ---------------------------------------------------------------------------
+template <typename T, int DP> constexpr int kSinkOwn = 2 * Tile<T, DP, 32>::kBytes + 256;      // a wave's queries, gradients, lse and delta
+template <typename T, int DP> constexpr int kSinkWaves = 4 * kSinkOwn<T, DP> > 160 * 1024 ? 2 : 4;
+template <typename T, int DP>
+constexpr int kSinkLds = kSinkWaves<T, DP> * (kSinkOwn<T, DP> > 32 * 33 * 4 ? kSinkOwn<T, DP> : 32 * 33 * 4);
+
+template <typename T, int DP>
+__global__ __launch_bounds__((kSinkWaves<T, DP> * kWave), (kDkvWaves<T, DP>)) void window_sink_kernel(AttnBwdArgs a) {
+    using Q = Tile<T, DP, 32>;
+    constexpr int kRound = 32 * Q::kChunks / kWave, kOwn = kSinkOwn<T, DP>, NW = kSinkWaves<T, DP>;
+    extern __shared__ __align__(16) char stage[];
+    const int64_t item = die_order(blockIdx.x, a.pieces * a.kv_heads);
+    if (item >= a.pieces * a.kv_heads) return;
+    const int kvh = (int)(item % a.kv_heads);
+    const int place = (int)(item / a.kv_heads);
+    const SeqTile st = seq_tile(a.seq, place, kPiece);
+    const int tid = threadIdx.x, wave = uniform(tid / kWave), lane = tid % kWave, half = lane / 32;
+    const int end = st.row + kPiece < st.len ? st.row + kPiece : st.len;
+    if (st.row >= st.len || end <= a.window) return;
+    const int group = a.q_heads / a.kv_heads, key = lane % kCols;
+    char *qt = stage + wave * kOwn, *gt = qt + Q::kBytes;
+    float *lse = reinterpret_cast<float*>(gt + Q::kBytes), *delta = lse + 32;
+    Keys<T, DP> keys;
+    keys.load(static_cast<const T*>(a.k) + (int64_t)(st.first + key) * a.ld_k + (int64_t)kvh * a.dim,
+              static_cast<const T*>(a.v) + (int64_t)(st.first + key) * a.ld_v + (int64_t)kvh * a.dim, half, a.dim, key < a.sinks && key < st.len);
+    const int blocks = (end - st.row + 31) / 32;
+    for (int n = wave; n < blocks * group; n += NW) {
+        const int head = kvh * group + n / blocks, base = st.row + n % blocks * 32;
+        if (base + 31 < a.window) continue;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) {
+            const int m = lane + i * kWave, p = base + m / Q::kChunks, e = m % Q::kChunks * Q::kElems;
+            Chunk x, g;
+            if (p < end && e < a.dim) {
+                x.load(static_cast<const T*>(a.q) + (int64_t)(st.first + p) * a.ld_q + (int64_t)head * a.dim + e);
+                g.load(static_cast<const T*>(a.dy) + ((int64_t)(st.first + p) * a.q_heads + head) * a.dim + e);
+            } else {
+                x.zero();
+                g.zero();
+            }
+            const int to = Q::at(m / Q::kChunks, m % Q::kChunks);
+            x.store(qt + to);
+            g.store(gt + to);
+        }
+        if (lane < 32) {
+            const int64_t at = (int64_t)(st.first + base + lane) * a.q_heads + head;
+            lse[lane] = base + lane < end ? a.lse[at] * kLog2e : 0.0f;
+            delta[lane] = base + lane < end ? a.delta[at] : 0.0f;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        keys.template take<32>(qt, gt, lse, delta, 0, base, false, a.c,
+                               [&](int p) { return p < end && key < a.sinks && p - key >= a.window; }, [](int) { return false; });
+    }
+    // the waves' sums, in their order: 32 channels of all keys at a time
+    float* out = a.part + ((int64_t)place * a.kv_heads + kvh) * 2 * a.sinks * a.dim;
+    float(*sum)[32][33] = reinterpret_cast<float(*)[32][33]>(stage);      // wave, channel, key
+    __syncthreads();
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int d = 0; d < DP / 32; ++d) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[wave][acc_row(i, half)][key] = which ? keys.dv[d][i] : keys.dk[d][i];
+            __syncthreads();
+            for (int n = tid; n < 32 * a.sinks; n += NW * kWave) {
+                const int e = n % 32, s = n / 32;
+                float v = sum[0][e][s];
+#pragma unroll
+                for (int w = 1; w < NW; ++w) v += sum[w][e][s];
+                if (32 * d + e < a.dim) out[((int64_t)which * a.sinks + s) * a.dim + 32 * d + e] = v;
+            }
+            __syncthreads();
+        }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+template <typename F>
+void with_type(int32_t dtype, F f) {
+    if (dtype == IM2WIN_F32) f(float{});
+    else f(bf16{});
+}
+
+// Pieces of queries that may see first tokens outside of their window: none
+// where no sequence can be longer than the window.
+int64_t pieces_of(const im2win_window_desc* d, const int32_t* starts) {
+    if (!d->sinks || d->tokens <= d->window) return 0;
+    if (!starts && d->tokens / d->sequences <= d->window) return 0;
+    return seq_places(d->tokens, d->sequences, starts, kPiece);
+}
+// With and without seq_starts (whose places are never fewer): the query does not know.
+size_t bwd_bytes(const im2win_window_desc* d) {
+    const size_t delta = ((size_t)(d->tokens * d->q_heads) * 4 + 15) / 16 * 16;
+    const int64_t pieces = d->sinks && d->tokens > d->window ? d->tokens / kPiece + d->sequences : 0;
+    return delta + (size_t)(pieces * d->kv_heads * 2 * d->sinks * d->head_dim) * 4;
+}
+
+}  // namespace
+}  // namespace im2win
+
+using namespace im2win;
+
+extern "C" {
+
+int im2win_window_attention_backward_workspace_bytes(const im2win_window_desc* d, size_t* bytes) {
+    int rc = check_attention(d);
+    if (rc) return rc;
+    if (d->sequences < 1 || d->sequences > kMaxTokens) return fail(IM2WIN_EINVAL, "sequences must be 1 to %lld (got %lld)", (long long)kMaxTokens, (long long)d->sequences);
+    if (!bytes) return fail(IM2WIN_ENULL, "bytes is NULL");
+    *bytes = bwd_bytes(d);
+    return ok();
+}
+
+int im2win_window_attention_backward(const im2win_window_desc* d, const void* dy, const void* q, const void* k, const void* v, const void* y,
+                                     const float* lse, const int32_t* seq_starts, void* dq, void* dk, void* dv, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+    int rc = check_attention(d);
+    if (rc || (rc = check_sequences(d->tokens, d->sequences, seq_starts, true))) return rc;
+    if (d->tokens == 0) return ok();
+    const size_t e = attn_size_of(d->dtype), need = bwd_bytes(d);
+    if ((rc = need_ptr(dy, e, "dy")) || (rc = need_ptr(q, e, "q")) || (rc = need_ptr(k, e, "k")) || (rc = need_ptr(v, e, "v")) ||
+        (rc = need_ptr(y, e, "y")) || (rc = need_ptr(lse, 4, "lse")) || (rc = need_ptr(dq, e, "dq")) || (rc = need_ptr(dk, e, "dk")) ||
+        (rc = need_ptr(dv, e, "dv")) || (rc = need_ptr(workspace, 16, "workspace")))
+        return rc;
+    if (workspace_bytes < need) return fail(IM2WIN_EWORKSPACE, "workspace holds %zu bytes, the gradients need %zu", workspace_bytes, need);
+    AttnBwdArgs a{};
+    a.dy = dy; a.q = q; a.k = k; a.v = v; a.y = y; a.lse = lse; a.dq = dq; a.dk = dk; a.dv = dv;
+    a.ld_q = d->ld_q; a.ld_k = d->ld_k; a.ld_v = d->ld_v;
+    a.q_heads = (int)d->q_heads; a.kv_heads = (int)d->kv_heads; a.dim = (int)d->head_dim; a.window = (int)d->window; a.sinks = (int)d->sinks;
+    a.pack = heads_packed(d->q_heads, d->kv_heads);
+    a.tile = kGroupCols / a.pack;
+    a.c = d->scale * kLog2e; a.scale = d->scale;
+    a.seq = make_seq_map(d->tokens, d->sequences, seq_starts);
+    a.q_places = seq_places(d->tokens, d->sequences, seq_starts, a.tile);
+    a.q_items = a.q_places * (d->q_heads / a.pack);
+    a.k_places = seq_places(d->tokens, d->sequences, seq_starts, kGroupCols);
+    a.k_items = a.k_places * d->kv_heads;
+    a.pieces = pieces_of(d, seq_starts);
+    a.delta = static_cast<float*>(workspace);
+    a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + ((size_t)(d->tokens * d->q_heads) * 4 + 15) / 16 * 16);
+    const int64_t gq = (a.q_items + 7) / 8 * 8, gk = (a.k_items + 7) / 8 * 8, gs = (a.pieces * d->kv_heads + 7) / 8 * 8;
+    if ((rc = check_launch(gq, kAttnThreads, "window_attention_backward's queries")) || (rc = check_launch(gk, kAttnThreads, "window_attention_backward's keys")) ||
+        (rc = check_launch(gs, kAttnThreads, "window_attention_backward's first tokens")))
+        return rc;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t attribute = hipSuccess;
+    with_type(d->dtype, [&](auto ty) {
+        using T = decltype(ty);
+        with_head(d->head_dim, [&](auto dp) {
+            constexpr int DP = decltype(dp)::value;
+            constexpr int kLds = kSinkLds<T, DP>;
+            if (a.pieces && kLds > 65536)
+                attribute = hipFuncSetAttribute(reinterpret_cast<const void*>(&window_sink_kernel<T, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+            if (attribute != hipSuccess) return;
+            hipLaunchKernelGGL((window_dq_kernel<T, DP>), dim3((unsigned)gq), dim3(kAttnThreads), 0, s, a);
+            if (a.pieces) hipLaunchKernelGGL((window_sink_kernel<T, DP>), dim3((unsigned)gs), dim3(kSinkWaves<T, DP> * kWave), kLds, s, a);
+            hipLaunchKernelGGL((window_dkv_kernel<T, DP>), dim3((unsigned)gk), dim3(kAttnThreads), 0, s, a);
+        });
+    });
+    if (attribute != hipSuccess) return fail(IM2WIN_EHIP, "window_attention_backward's LDS: %s", hipGetErrorString(attribute));
+    return launched("window_attention_backward");
+}
+
+}  // extern "C"

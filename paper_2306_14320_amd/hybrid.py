@@ -28,8 +28,10 @@ __all__ = [
     "im2win_qk_norm_rope_backward",
     "qk_norm_rope_desc_for", "qk_norm_rope", "qk_norm_rope_backward", "QkGradients",
     "im2win_window_desc", "im2win_window_attention", "im2win_window_attention_step_workspace_bytes",
-    "im2win_window_attention_step",
-    "window_attention_desc_for", "window_attention", "window_attention_step",
+    "im2win_window_attention_step", "im2win_window_attention_backward_workspace_bytes",
+    "im2win_window_attention_backward",
+    "window_attention_desc_for", "window_attention", "window_attention_backward", "window_attention_step",
+    "AttentionGradients",
 ]
 
 
@@ -69,6 +71,8 @@ SIGNATURES = {
     "im2win_qk_norm_rope_backward": [_QK] + [_P] * 13 + [_SZ, _P],
     "im2win_window_attention": [_WIN] + [_P] * 6 + [_I64] + [_P] * 5,
     "im2win_window_attention_step_workspace_bytes": [_WIN, ctypes.POINTER(_SZ)],
+    "im2win_window_attention_backward_workspace_bytes": [_WIN, ctypes.POINTER(_SZ)],
+    "im2win_window_attention_backward": [_WIN] + [_P] * 11 + [_SZ, _P],
     "im2win_window_attention_step": [_WIN] + [_P] * 5 + [_I64] + [_P] * 4 + [_SZ, _P],
 }
 
@@ -136,6 +140,16 @@ def im2win_window_attention_step(desc, q, k, v, k_cache, v_cache, cache_slots, p
                                  workspace_bytes, stream) -> None:
     _check(load_library().im2win_window_attention_step(ctypes.byref(desc), q, k, v, k_cache, v_cache, cache_slots, past,
                                                        slots, y, workspace, workspace_bytes, stream))
+
+
+def im2win_window_attention_backward_workspace_bytes(desc) -> int:
+    return _bytes("im2win_window_attention_backward_workspace_bytes", desc)
+
+
+def im2win_window_attention_backward(desc, dy, q, k, v, y, lse, seq_starts, dq, dk, dv, workspace, workspace_bytes,
+                                     stream) -> None:
+    _check(load_library().im2win_window_attention_backward(ctypes.byref(desc), dy, q, k, v, y, lse, seq_starts, dq, dk,
+                                                           dv, workspace, workspace_bytes, stream))
 
 
 # ---------------------------------------------------------------------------
@@ -346,6 +360,30 @@ def window_attention(q, k, v, desc, seq_starts=None, k_cache=None, v_cache=None,
     y, yp = _out(y, "y", rows, ty, q, dev, stream)
     im2win_window_attention(d, qp, kp, vp, sp, kcp, vcp, pool, pp, slp, yp, lp, _stream_on(stream, dev))
     return y
+
+
+class AttentionGradients(NamedTuple):
+    dq: torch.Tensor     # T x H x head size, q's dtype
+    dk: torch.Tensor     # T x K x head size, q's dtype
+    dv: torch.Tensor     # T x K x head size, q's dtype
+
+
+def window_attention_backward(dy, q, k, v, y, lse, desc, seq_starts=None, workspace=None, stream=None) -> AttentionGradients:
+    """Gradients of window_attention without a cache for dy (dense), with the y
+    and lse that it wrote."""
+    d = desc
+    dev, ty, rows, (qp, kp, vp) = _att_inputs(q, k, v, d)
+    keys = (d.tokens, d.kv_heads, d.head_dim)
+    for t, name in ((dy, "dy"), (y, "y"), (lse, "lse")):
+        if not isinstance(t, torch.Tensor):
+            raise ValueError(f"{name} must be a tensor")
+    dyp, yp = _dense(dy, "dy", rows, ty, dev), _dense(y, "y", rows, ty, dev)
+    lp = _dense(lse, "lse", (d.tokens, d.q_heads), _F32, dev)
+    sp = _dense(seq_starts, "seq_starts", (d.sequences + 1,), torch.int32, dev)
+    g = AttentionGradients(_new(rows, ty, q, stream), _new(keys, ty, q, stream), _new(keys, ty, q, stream))
+    workspace, wsp, wsb = _workspace(workspace, im2win_window_attention_backward_workspace_bytes(d), q, stream)
+    im2win_window_attention_backward(d, dyp, qp, kp, vp, yp, lp, sp, *[t.data_ptr() for t in g], wsp, wsb, _stream_on(stream, dev))
+    return g
 
 
 def window_attention_step(q, k, v, k_cache, v_cache, past, desc, slots=None, y=None, workspace=None, stream=None):

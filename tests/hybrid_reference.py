@@ -139,3 +139,25 @@ def attend(q, k, v, past, window, sinks, scale):
 
 def ring_row(p, window, sinks):
     return p if p < sinks else sinks + (p - sinks) % window
+
+
+def attend_gradients(q, k, v, dy, window, sinks, scale, u):
+    """Gradients of one head of one sequence and the bounds of the kernels'
+    errors, for operands (weights, ds, the kept y) rounded to unit roundoff u:
+    [(dq, bound), (dk, bound), (dv, bound)]."""
+    n, d = q.shape
+    seen = visible(n, n, 0, window, sinks)
+    w = torch.softmax((q @ k.t() * scale).masked_fill(~seen, -float("inf")), 1)
+    y, dp = w @ v, dy @ v.t()
+    delta = (dy * y).sum(1, keepdim=True)
+    ds = torch.where(seen.sum(1, keepdim=True) == 1, torch.zeros_like(w), w * (dp - delta))
+    size = torch.where(seen, q.abs() @ k.abs().t() * scale, 0.0).amax(1, keepdim=True)
+    rel = 3 * (d + 8) * U32 * size + (seen.sum(1, keepdim=True) + 32) * U32      # of a weight: its score's, and lse's
+    edp = (d + 8) * U32 * (dy.abs() @ v.abs().t())
+    ey = (rel + u) * (w @ v.abs()) + (u + U32) * y.abs()
+    edelta = (dy.abs() * ey).sum(1, keepdim=True) + (d + 8) * U32 * (dy * y).abs().sum(1, keepdim=True)
+    eds = w * (rel * (dp - delta).abs() + edp + edelta)
+    eds = torch.where(seen.sum(1, keepdim=True) == 1, torch.zeros_like(w), eds + u * (ds.abs() + eds))
+    more = (n + 16) * U32
+    return [(scale * ds @ k, scale * (eds + more * ds.abs()) @ k.abs()), (scale * ds.t() @ q, scale * (eds + more * ds.abs()).t() @ q.abs()),
+            (w.t() @ dy, ((rel + u + more) * w).t() @ dy.abs())]
