@@ -30,6 +30,7 @@ constexpr int kRows = 16;                 // rows a wave holds in registers
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kChunk = kRows * kWaves;    // rows of a workgroup
+constexpr uint32_t kAllRows = (1u << kRows) - 1;
 constexpr int kGroup = 32;                // chunks whose pairs are looked at one by one
 constexpr int kLook = kGroup / kWaves;    // of those, the ones a wave looks at
 constexpr float kReset = -1.0f;           // the a of a pair that does not look back
@@ -73,10 +74,6 @@ struct Look {
     int chunks;
 };
 
-__global__ __launch_bounds__(256) void fill_kernel(uint64_t* p, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) p[i] = kEmpty;
-}
 
 // ---------------------------------------------------------------------------
 // The sequences' first and last rows inside of a chunk
@@ -134,7 +131,7 @@ __device__ __forceinline__ void mark(const SeqMap& seq, int row0, bool last_chun
 // The rows [t0, t0 + kRows) that lie in [lo, hi), a bit each
 __device__ __forceinline__ uint32_t rows_inside(int t0, int lo, int hi) {
     const int from = lo - t0, to = hi - t0;
-    const uint32_t upto = to <= 0 ? 0u : to >= kRows ? 0xffffu : (1u << to) - 1;
+    const uint32_t upto = to <= 0 ? 0u : to >= kRows ? kAllRows : (1u << to) - 1;
     return from <= 0 ? upto : from >= kRows ? 0u : upto & ~((1u << from) - 1);
 }
 // The rows of a wave that marks name, a bit each; the sequence itself is read where a bit is set.
@@ -145,45 +142,44 @@ __device__ __forceinline__ uint32_t marked(const int* m) {
 
 // ---------------------------------------------------------------------------
 // V neighbouring channels of a row in a register: one element, or two bfloat16
-// (4 bytes at any alignment).  Nothing beside the row is read: the lane with
-// the odd last channel reads the one before it too, and takes the upper half;
-// lanes behind the row read what its last lane reads and store nothing.
+// (4 bytes at any alignment).  Nothing beside the row is touched: the lane that
+// would have an odd last channel takes the one before it too, and both lanes
+// compute and write the same values there; lanes behind the row read what its
+// last lane reads and write nothing.
 // ---------------------------------------------------------------------------
 template <typename T, int V>
 struct Lane {
-    int c, n;        // first channel, channels that are the lane's own (0 and less: none)
-    int at, shift;   // where it reads, and by how much the word moves down
+    int c;           // first channel
+    bool on;
     __device__ __forceinline__ Lane(int first, int channels) {
-        c = first;
-        n = channels - first;
-        at = n >= V ? c : channels - V;
-        shift = V == 2 && n == 1 ? 16 : 0;
+        on = first < channels;
+        c = first + V <= channels ? first : channels - V;
     }
     __device__ __forceinline__ uint32_t load(const T* row) const {
         if constexpr (V * sizeof(T) == 4) {
             uint32_t u;
-            __builtin_memcpy(&u, row + at, 4);
+            __builtin_memcpy(&u, row + c, 4);
             return u;
         } else {
-            return __builtin_bit_cast(uint16_t, row[at]);
+            return __builtin_bit_cast(uint16_t, row[c]);
         }
     }
-    __device__ __forceinline__ float get(uint32_t u, int v) const {
+    static __device__ __forceinline__ float get(uint32_t u, int v) {
         if constexpr (sizeof(T) == 4) return __uint_as_float(u);
-        else if constexpr (V == 1) return __uint_as_float(u << 16);
-        else return __uint_as_float(v ? u & 0xffff0000u : (u >> shift) << 16);
+        else return __uint_as_float(v ? u & 0xffff0000u : u << 16);
     }
     __device__ __forceinline__ void store(T* row, const float (&v)[V]) const {
+        if (!on) return;
         if constexpr (V == 1) {
-            if (n > 0) row[c] = (T)v[0];
+            row[c] = (T)v[0];
         } else {
-            if (n > 1) {
-                const uint32_t u = pack_bf16(v[0], v[1]);
-                __builtin_memcpy(row + c, &u, 4);
-            } else if (n == 1) {
-                row[c] = (bf16)v[0];
-            }
+            const uint32_t u = pack_bf16(v[0], v[1]);
+            __builtin_memcpy(row + c, &u, 4);
         }
+    }
+    __device__ __forceinline__ void load(const float* row, float (&v)[V]) const { __builtin_memcpy(v, row + c, 4 * V); }
+    __device__ __forceinline__ void store_f32(float* row, const float (&v)[V]) const {
+        if (on) __builtin_memcpy(row + c, v, 4 * V);
     }
 };
 
@@ -191,20 +187,20 @@ struct Lane {
 // The gates of one element
 // ---------------------------------------------------------------------------
 struct Gate {
-    float a, m;      // exp(L) and sqrt(1 - exp(2 L)); g = -L / ln 2 >= 0
+    float a, d;      // exp(L) and 1 - exp(2 L), for g = -L / ln 2 >= 0
 };
 
-// 1 - exp(2 L) loses all digits near L = 0, so below 0.25 it is the series
-// u (1 - u/2 (1 - u/3 (1 - u/4 (1 - u/5 (1 - u/6))))) of u = -2 L (its rest is
-// under u^6 / 5040 = 5e-8); above, the subtraction is off by 3e-7 relative and
-// the root halves that.
+// 1 - exp(2 L) loses all digits near L = 0, so where u = -2 L is below 0.25 it
+// is the series u (1 - u/2! + u^2/3! - .. - u^5/6!), in powers of g = u / (2 ln
+// 2) (its rest is under u^6 / 5040 = 5e-8); above, the subtraction is off by
+// 9e-7 relative, and the root that is taken of it halves that.
 __device__ __forceinline__ Gate gate_of(float g) {
+    constexpr float k = 2.0f / kLog2e;
+    constexpr float k1 = k, k2 = -k * k / 2, k3 = k * k * k / 6, k4 = -k * k * k * k / 24, k5 = k * k * k * k * k / 120, k6 = -k * k * k * k * k * k / 720;
     Gate o;
     o.a = __builtin_amdgcn_exp2f(-g);
-    const float u = g * (2.0f / kLog2e);
-    const float s = u * fmaf(-0.5f * u, fmaf(u * (-1.0f / 3.0f), fmaf(u * -0.25f, fmaf(u * -0.2f, fmaf(u, -1.0f / 6.0f, 1.0f), 1.0f), 1.0f), 1.0f), 1.0f);
-    const float d = fmaf(-o.a, o.a, 1.0f);
-    o.m = __builtin_amdgcn_sqrtf(u < 0.25f ? s : d);
+    const float s = g * fmaf(g, fmaf(g, fmaf(g, fmaf(g, fmaf(g, k6, k5), k4), k3), k2), k1);
+    o.d = g < 0.25f / k ? s : fmaf(-o.a, o.a, 1.0f);
     return o;
 }
 
@@ -214,9 +210,28 @@ __device__ __forceinline__ float rate_of(float lam, float c) {
     return c * sp * kLog2e;
 }
 
+// Empties the words that workgroups leave for each other, and works out the
+// rates once (each workgroup on its own would add five instructions an element).
+__global__ __launch_bounds__(256) void prepare_kernel(uint64_t* p, int64_t n, const float* lam, float* rates, int channels, float c) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (i < n) p[i] = kEmpty;
+    if (i < channels) rates[i] = rate_of(lam[i], c);
+}
+
+template <typename T, int V>
+__device__ __forceinline__ void load_rates(const Lane<T, V>& own, const float* rates, const float* lam, float c, float (&r)[V]) {
+    if (rates) {
+        own.load(rates, r);
+    } else {
+        own.load(lam, r);
+#pragma unroll
+        for (int v = 0; v < V; ++v) r[v] = rate_of(r[v], c);
+    }
+}
+
 struct RecArgs {
     const void *x, *r, *i;
-    const float* lam;
+    const float *lam, *rates;      // rates: NULL where one chunk holds all rows
     SeqMap seq;
     const float* init;
     void* y;              // NULL: only the states
@@ -248,7 +263,7 @@ __device__ __forceinline__ void look_back(const Look& k, int order, int c, int c
             for (int j = 0; j < kLook; ++j) {
                 const int q = from + j < order ? from + j : from;
 #pragma unroll
-                for (int v = 0; v < V; ++v) w[j][v] = c + v < channels ? look(k.pairs + (int64_t)q * channels + c + v) : 0;
+                for (int v = 0; v < V; ++v) w[j][v] = look(k.pairs + (int64_t)q * channels + c + v);
             }
 #pragma unroll
             for (int j = 0; j < kLook; ++j)
@@ -269,7 +284,7 @@ __device__ __forceinline__ void look_back(const Look& k, int order, int c, int c
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             uint64_t w = 0;
-            if (group && c + v < channels)
+            if (group)
                 while ((w = look(k.states + (int64_t)(group - 1) * channels + c + v)) == kEmpty) __builtin_amdgcn_s_sleep(2);
             enter[lane * V + v] = pair_of(w).b;
         }
@@ -300,51 +315,70 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_kernel(RecArgs a) {
     const int chunk = ticket / a.tiles, tile = ticket - chunk * a.tiles;
     const int row0 = chunk * kChunk;
     const Lane<T, V> own((tile * kWave + lane) * V, a.channels);
-    const int c = own.c, n = own.n;
+    const int c = own.c;
     mark(a.seq, row0, chunk == a.look.chunks - 1, marks, [&](int b) {
         if (!a.final_state) return;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v < n) a.final_state[(int64_t)b * a.channels + c + v] = a.init ? a.init[(int64_t)b * a.channels + c + v] : 0.0f;
+        float h[V] = {};
+        if (a.init) own.load(a.init + (int64_t)b * a.channels, h);
+        own.store_f32(a.final_state + (int64_t)b * a.channels, h);
     });
     const int lo = a.seq.first(0), hi = a.seq.first(a.seq.count);
     if (lo >= hi) return;      // of every workgroup: none waits
 
     const int t0 = row0 + wave * kRows;
     uint32_t xw[kRows], rw[kRows], iw[kRows];
+    const int ts = t0 < lo ? lo : t0 >= hi ? hi - 1 : t0;
+    const T* xp = static_cast<const T*>(a.x) + ts * a.ld_x;
+    const T* rp = static_cast<const T*>(a.r) + ts * a.ld_r;
+    const T* ip = static_cast<const T*>(a.i) + ts * a.ld_i;
 #pragma unroll
     for (int j = 0; j < kRows; ++j) {
-        const int t = t0 + j < lo ? lo : t0 + j >= hi ? hi - 1 : t0 + j;
-        xw[j] = own.load(static_cast<const T*>(a.x) + t * a.ld_x);
-        rw[j] = own.load(static_cast<const T*>(a.r) + t * a.ld_r);
-        iw[j] = own.load(static_cast<const T*>(a.i) + t * a.ld_i);
+        xw[j] = own.load(xp);
+        rw[j] = own.load(rp);
+        iw[j] = own.load(ip);
+        const bool on = t0 + j >= lo && t0 + j + 1 < hi;      // rows outside of the sequences are not read
+        xp += on ? a.ld_x : 0;
+        rp += on ? a.ld_r : 0;
+        ip += on ? a.ld_i : 0;
     }
     float rate[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) rate[v] = v < n ? rate_of(a.lam[c + v], a.c) : 0.0f;
+    load_rates(own, a.rates, a.lam, a.c, rate);
 
     float da[kRows][V], db[kRows][V];
-    Pair p[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) p[v] = {1.0f, 0.0f};
     const uint32_t begin = marked(marks.first + wave * kRows), end = marked(marks.last + wave * kRows);
     const uint32_t inside = rows_inside(t0, lo, hi);
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-        const bool in = inside >> j & 1;
+    for (int j = 0; j < kRows; ++j)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Gate g = gate_of(rate[v] * sigmoid(own.get(rw[j], v)));
-            da[j][v] = in ? g.a : 1.0f;
-            db[j][v] = in ? g.m * sigmoid(own.get(iw[j], v)) * own.get(xw[j], v) : 0.0f;
+            da[j][v] = g.a;
+            db[j][v] = __builtin_amdgcn_sqrtf(g.d) * sigmoid(own.get(iw[j], v)) * own.get(xw[j], v);
         }
-        if (begin >> j & 1) {
-            const int b = uniform(marks.first[wave * kRows + j]);
+    if (inside != kAllRows) {
+#pragma unroll
+        for (int j = 0; j < kRows; ++j)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                if (a.init && v < n) db[j][v] = fmaf(da[j][v], a.init[(int64_t)b * a.channels + c + v], db[j][v]);
-                p[v].b = db[j][v];
+                da[j][v] = inside >> j & 1 ? da[j][v] : 1.0f;
+                db[j][v] = inside >> j & 1 ? db[j][v] : 0.0f;
             }
+    }
+    // the wave's rows as one pair; where a sequence begins, its state from before is in b
+    Pair p[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) p[v] = {1.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+        if (begin >> j & 1) {
+            if (a.init) {
+                float h0[V];
+                own.load(a.init + (int64_t)uniform(marks.first[wave * kRows + j]) * a.channels, h0);
+#pragma unroll
+                for (int v = 0; v < V; ++v) db[j][v] = fmaf(da[j][v], h0[v], db[j][v]);
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) p[v] = {kReset, db[j][v]};
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -364,18 +398,12 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_kernel(RecArgs a) {
         for (int v = 0; v < V; ++v) {
             Pair q = agg[0][lane * V + v];
             for (int w = 1; w < kWaves; ++w) q = then(q, agg[w][lane * V + v]);
-            if (v < n) leave(a.look.pairs + (int64_t)chunk * a.channels + c + v, q);
+            if (own.on) leave(a.look.pairs + (int64_t)chunk * a.channels + c + v, q);
         }
     }
-    float h[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) h[v] = 0.0f;
+    float h[V] = {};
     if (chunk) look_back<V>(a.look, chunk, c, a.channels, pre, enter, h);
-    if (a.chunk_states && wave == 0) {
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v < n) a.chunk_states[(int64_t)chunk * a.channels + c + v] = h[v];
-    }
+    if (a.chunk_states && wave == 0) own.store_f32(a.chunk_states + (int64_t)chunk * a.channels, h);
     for (int w = 0; w < wave; ++w) {
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = apply(agg[w][lane * V + v], h[v]);
@@ -383,19 +411,21 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_kernel(RecArgs a) {
     if (wave == kWaves - 1 && chunk % kGroup == kGroup - 1 && chunk + 1 < a.look.chunks) {
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (v < n) leave(a.look.states + (int64_t)(chunk / kGroup) * a.channels + c + v, {0.0f, apply(p[v], h[v])});
+            if (own.on) leave(a.look.states + (int64_t)(chunk / kGroup) * a.channels + c + v, {0.0f, apply(p[v], h[v])});
     }
+    T* yp = static_cast<T*>(a.y) + (int64_t)t0 * a.channels;
 #pragma unroll
     for (int j = 0; j < kRows; ++j) {
+        if (begin >> j & 1) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) h[v] = begin >> j & 1 ? db[j][v] : fmaf(da[j][v], h[v], db[j][v]);
-        if ((inside >> j & 1) && a.y) own.store(static_cast<T*>(a.y) + (int64_t)(t0 + j) * a.channels, h);
-        if ((end >> j & 1) && a.final_state) {
-            const int e = uniform(marks.last[wave * kRows + j]);
+            for (int v = 0; v < V; ++v) h[v] = db[j][v];
+        } else {
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (v < n) a.final_state[(int64_t)e * a.channels + c + v] = h[v];
+            for (int v = 0; v < V; ++v) h[v] = fmaf(da[j][v], h[v], db[j][v]);
         }
+        if ((inside >> j & 1) && a.y) own.store(yp, h);
+        yp += a.channels;
+        if ((end >> j & 1) && a.final_state) own.store_f32(a.final_state + (int64_t)uniform(marks.last[wave * kRows + j]) * a.channels, h);
     }
 }
 
@@ -413,7 +443,7 @@ __global__ __launch_bounds__(256) void copy_states_kernel(const float* from, flo
 // ---------------------------------------------------------------------------
 struct RecBwdArgs {
     const void *dy, *x, *r, *i;
-    const float* lam;
+    const float *lam, *rates;
     SeqMap seq;
     const float *init, *d_final, *chunk_states;
     void *dx, *dr, *di;
@@ -444,82 +474,104 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
     const int chunk = a.look.chunks - 1 - order;
     const int row0 = chunk * kChunk;
     const Lane<T, V> own((tile * kWave + lane) * V, a.channels);
-    const int c = own.c, n = own.n;
+    const int c = own.c;
     mark(a.seq, row0, order == 0, marks, [&](int b) {
         if (!a.d_init) return;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v < n) a.d_init[(int64_t)b * a.channels + c + v] = a.d_final ? a.d_final[(int64_t)b * a.channels + c + v] : 0.0f;
+        float h[V] = {};
+        if (a.d_final) own.load(a.d_final + (int64_t)b * a.channels, h);
+        own.store_f32(a.d_init + (int64_t)b * a.channels, h);
     });
     const int lo = a.seq.first(0), hi = a.seq.first(a.seq.count);
     if (lo >= hi) {            // of every workgroup: none waits
-        if (wave == 0) {
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (v < n) a.part[(int64_t)chunk * a.channels + c + v] = 0.0f;
-        }
+        const float zero[V] = {};
+        if (wave == 0) own.store_f32(a.part + (int64_t)chunk * a.channels, zero);
         return;
     }
 
     const int t0 = row0 + wave * kRows;
     uint32_t xw[kRows], rw[kRows], iw[kRows], gw[kRows];
+    const int ts = t0 < lo ? lo : t0 >= hi ? hi - 1 : t0;
+    const T* xp = static_cast<const T*>(a.x) + ts * a.ld_x;
+    const T* rp = static_cast<const T*>(a.r) + ts * a.ld_r;
+    const T* dp = static_cast<const T*>(a.dy) + (int64_t)ts * a.channels;
+    const T* ip = static_cast<const T*>(a.i) + ts * a.ld_i;
 #pragma unroll
     for (int j = 0; j < kRows; ++j) {
-        const int t = t0 + j < lo ? lo : t0 + j >= hi ? hi - 1 : t0 + j;
-        xw[j] = own.load(static_cast<const T*>(a.x) + t * a.ld_x);
-        rw[j] = own.load(static_cast<const T*>(a.r) + t * a.ld_r);
-        iw[j] = own.load(static_cast<const T*>(a.i) + t * a.ld_i);
-        gw[j] = own.load(static_cast<const T*>(a.dy) + (int64_t)t * a.channels);
+        xw[j] = own.load(xp);
+        rw[j] = own.load(rp);
+        iw[j] = own.load(ip);
+        gw[j] = own.load(dp);
+        const bool on = t0 + j >= lo && t0 + j + 1 < hi;      // rows outside of the sequences are not read
+        xp += on ? a.ld_x : 0;
+        rp += on ? a.ld_r : 0;
+        ip += on ? a.ld_i : 0;
+        dp += on ? a.channels : 0;
     }
-    float rate[V], h[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        rate[v] = v < n ? rate_of(a.lam[c + v], a.c) : 0.0f;
-        h[v] = v < n && chunk ? a.chunk_states[(int64_t)chunk * a.channels + c + v] : 0.0f;
-    }
+    float rate[V], h[V] = {};
+    load_rates(own, a.rates, a.lam, a.c, rate);
+    if (chunk) own.load(a.chunk_states + (int64_t)chunk * a.channels, h);
 
     // hb: first the row's b, then the state in front of the row
     float da[kRows][V], hb[kRows][V];
-    Pair p[V], q[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) p[v] = q[v] = {1.0f, 0.0f};
     const uint32_t begin = marked(marks.first + wave * kRows), end = marked(marks.last + wave * kRows);
     const uint32_t inside = rows_inside(t0, lo, hi);
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-        const bool in = inside >> j & 1;
+    for (int j = 0; j < kRows; ++j)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Gate g = gate_of(rate[v] * sigmoid(own.get(rw[j], v)));
-            da[j][v] = in ? g.a : 1.0f;
-            hb[j][v] = in ? g.m * sigmoid(own.get(iw[j], v)) * own.get(xw[j], v) : 0.0f;
+            da[j][v] = g.a;
+            hb[j][v] = __builtin_amdgcn_sqrtf(g.d) * sigmoid(own.get(iw[j], v)) * own.get(xw[j], v);
         }
+    if (inside != kAllRows) {
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {
+            if (!(inside >> j & 1)) gw[j] = 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                da[j][v] = inside >> j & 1 ? da[j][v] : 1.0f;
+                hb[j][v] = inside >> j & 1 ? hb[j][v] : 0.0f;
+            }
+        }
+    }
+    auto initial = [&](int j, float (&h0)[V]) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) h0[v] = 0.0f;
+        if (a.init) own.load(a.init + (int64_t)uniform(marks.first[wave * kRows + j]) * a.channels, h0);
+    };
+    auto after = [&](int j, float (&g0)[V]) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) g0[v] = 0.0f;
+        if (a.d_final) own.load(a.d_final + (int64_t)uniform(marks.last[wave * kRows + j]) * a.channels, g0);
+    };
+    Pair p[V], q[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) p[v] = q[v] = {1.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
         if (begin >> j & 1) {
-            const int b = uniform(marks.first[wave * kRows + j]);
+            float h0[V];
+            initial(j, h0);
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const float h0 = a.init && v < n ? a.init[(int64_t)b * a.channels + c + v] : 0.0f;
-                p[v].b = fmaf(da[j][v], h0, hb[j][v]);
-            }
-        } else {
+            for (int v = 0; v < V; ++v) p[v].b = h0[v];
+        }
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                p[v].a *= da[j][v];
-                p[v].b = fmaf(da[j][v], p[v].b, hb[j][v]);
-            }
+        for (int v = 0; v < V; ++v) {
+            p[v].a *= da[j][v];
+            p[v].b = fmaf(da[j][v], p[v].b, hb[j][v]);
         }
     }
 #pragma unroll
     for (int j = kRows - 1; j >= 0; --j) {
-        const bool in = inside >> j & 1;
         if (end >> j & 1) {
-            const int e = uniform(marks.last[wave * kRows + j]);
+            float g0[V];
+            after(j, g0);
 #pragma unroll
-            for (int v = 0; v < V; ++v) q[v].b = a.d_final && v < n ? a.d_final[(int64_t)e * a.channels + c + v] : 0.0f;
+            for (int v = 0; v < V; ++v) q[v].b = g0[v];
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            q[v].b = da[j][v] * (q[v].b + (in ? own.get(gw[j], v) : 0.0f));
+            q[v].b = da[j][v] * (q[v].b + own.get(gw[j], v));
             q[v].a *= da[j][v];
         }
     }
@@ -536,33 +588,16 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
         for (int v = 0; v < V; ++v) {
             Pair s = back[kWaves - 1][lane * V + v];
             for (int w = kWaves - 2; w >= 0; --w) s = then(s, back[w][lane * V + v]);
-            if (v < n) leave(a.look.pairs + (int64_t)order * a.channels + c + v, s);
+            if (own.on) leave(a.look.pairs + (int64_t)order * a.channels + c + v, s);
         }
     }
-    float g[V];
-#pragma unroll
-    for (int v = 0; v < V; ++v) g[v] = 0.0f;
-    if (order) look_back<V>(a.look, order, c, a.channels, pre, enter, g);
     for (int w = 0; w < wave; ++w) {
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = apply(agg[w][lane * V + v], h[v]);
     }
-    for (int w = kWaves - 1; w > wave; --w) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) g[v] = apply(back[w][lane * V + v], g[v]);
-    }
-    if (wave == 0 && order % kGroup == kGroup - 1 && chunk) {
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v < n) leave(a.look.states + (int64_t)(order / kGroup) * a.channels + c + v, {0.0f, apply(q[v], g[v])});
-    }
 #pragma unroll
     for (int j = 0; j < kRows; ++j) {
-        if (begin >> j & 1) {
-            const int b = uniform(marks.first[wave * kRows + j]);
-#pragma unroll
-            for (int v = 0; v < V; ++v) h[v] = a.init && v < n ? a.init[(int64_t)b * a.channels + c + v] : 0.0f;
-        }
+        if (begin >> j & 1) initial(j, h);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float before = h[v];
@@ -570,47 +605,52 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
             hb[j][v] = before;
         }
     }
-    float sum[V];
+    float g[V] = {};
+    if (order) look_back<V>(a.look, order, c, a.channels, pre, enter, g);
+    for (int w = kWaves - 1; w > wave; --w) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) sum[v] = 0.0f;
+        for (int v = 0; v < V; ++v) g[v] = apply(back[w][lane * V + v], g[v]);
+    }
+    if (wave == 0 && order % kGroup == kGroup - 1 && chunk) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (own.on) leave(a.look.states + (int64_t)(order / kGroup) * a.channels + c + v, {0.0f, apply(q[v], g[v])});
+    }
+    float sum[V] = {};
+    const int64_t behind = (int64_t)(t0 + kRows) * a.channels;
+    T *dx = static_cast<T*>(a.dx) + behind, *dr = static_cast<T*>(a.dr) + behind, *di = static_cast<T*>(a.di) + behind;
 #pragma unroll
     for (int j = kRows - 1; j >= 0; --j) {
-        const bool in = inside >> j & 1;
-        if (end >> j & 1) {
-            const int e = uniform(marks.last[wave * kRows + j]);
-#pragma unroll
-            for (int v = 0; v < V; ++v) g[v] = a.d_final && v < n ? a.d_final[(int64_t)e * a.channels + c + v] : 0.0f;
-        }
+        dx -= a.channels;
+        dr -= a.channels;
+        di -= a.channels;
+        if (!(inside >> j & 1)) continue;
+        if (end >> j & 1) after(j, g);
+        // the gates again: kept from above, they would take four registers an element
+        arrive(rw[j]);
+        arrive(iw[j]);
         float ox[V], orr[V], oi[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const float x = own.get(xw[j], v), sr = sigmoid(own.get(rw[j], v)), si = sigmoid(own.get(iw[j], v));
-            const float gg = g[v] + (in ? own.get(gw[j], v) : 0.0f);
+            const float gg = g[v] + own.get(gw[j], v);
             const float l2 = rate[v] * sr;                   // -L / ln 2
             const Gate gt = gate_of(l2);
-            const float l = l2 * (-1.0f / kLog2e), gm = gg * gt.m;
-            // L / m stays finite: it goes to zero with L
-            const float lm = gt.m > 0.0f ? l * __builtin_amdgcn_rcpf(gt.m) : 0.0f;
-            const float dl = gg * gt.a * fmaf(-gt.a * lm, si * x, l * hb[j][v]);      // dL L
+            // 1 / m; L / m goes to zero with L, and is zero where both are
+            const float d = fmaxf(gt.d, 0x1p-125f), im = __builtin_amdgcn_rsqf(d);
+            const float l = l2 * (-1.0f / kLog2e), gm = gg * (d * im);
+            const float dl = gg * gt.a * fmaf(-gt.a * (l * im), si * x, l * hb[j][v]);      // dL L
             ox[v] = gm * si;
-            oi[v] = ox[v] * x * (1.0f - si);
-            orr[v] = dl * (1.0f - sr);
-            sum[v] += in ? dl : 0.0f;
-            g[v] = in ? gt.a * gg : g[v];
+            oi[v] = ox[v] * fmaf(-si, x, x);
+            orr[v] = fmaf(-sr, dl, dl);
+            sum[v] += dl;
+            g[v] = gt.a * gg;
         }
+        own.store(dx, ox);
+        own.store(dr, orr);
+        own.store(di, oi);
+        if ((begin >> j & 1) && a.d_init) own.store_f32(a.d_init + (int64_t)uniform(marks.first[wave * kRows + j]) * a.channels, g);
         __builtin_amdgcn_sched_barrier(0);      // a row at a time: mixed, the rows' temporaries spill
-        if (in) {
-            const int64_t at = (int64_t)(t0 + j) * a.channels;
-            own.store(static_cast<T*>(a.dx) + at, ox);
-            own.store(static_cast<T*>(a.dr) + at, orr);
-            own.store(static_cast<T*>(a.di) + at, oi);
-        }
-        if ((begin >> j & 1) && a.d_init) {
-            const int b = uniform(marks.first[wave * kRows + j]);
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (v < n) a.d_init[(int64_t)b * a.channels + c + v] = g[v];
-        }
     }
     __syncthreads();
 #pragma unroll
@@ -618,10 +658,9 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
     __syncthreads();
     if (wave == 0) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
+        for (int v = 0; v < V; ++v)
             for (int w = 1; w < kWaves; ++w) sum[v] += pre[w][lane * V + v].b;
-            if (v < n) a.part[(int64_t)chunk * a.channels + c + v] = sum[v];
-        }
+        own.store_f32(a.part + (int64_t)chunk * a.channels, sum);
     }
 }
 
@@ -663,29 +702,28 @@ struct RecStepArgs {
 
 template <typename T, int V>
 __global__ __launch_bounds__(256) void recurrence_step_kernel(RecStepArgs a) {
-    const Lane<T, V> own(((int)blockIdx.y * 256 + (int)threadIdx.x) * V, a.channels);
-    const int c = own.c, n = own.n;
+    const int c = ((int)blockIdx.y * 256 + (int)threadIdx.x) * V, n = a.channels - c;
     if (n <= 0) return;
     const int64_t t = blockIdx.x;
     const int64_t slot = a.slots ? a.slots[t] : t;
     const bool live = slot >= 0 && slot < a.state_slots;
     float* st = a.state + (live ? slot : 0) * a.channels + c;
-    const uint32_t xw = own.load(static_cast<const T*>(a.x) + t * a.ld_x);
-    const uint32_t rw = own.load(static_cast<const T*>(a.r) + t * a.ld_r);
-    const uint32_t iw = own.load(static_cast<const T*>(a.i) + t * a.ld_i);
-    float h[V];
+    const T* x = static_cast<const T*>(a.x) + t * a.ld_x + c;
+    const T* r = static_cast<const T*>(a.r) + t * a.ld_r + c;
+    const T* i = static_cast<const T*>(a.i) + t * a.ld_i + c;
+    T* y = static_cast<T*>(a.y) + t * a.channels + c;
+    // (the scans' lanes share an odd last channel; here each has its own, since the state moves in place)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        h[v] = 0.0f;
-        if (!live || v >= n) continue;
-        const Gate g = gate_of(rate_of(a.lam[c + v], a.c) * sigmoid(own.get(rw, v)));
-        h[v] = fmaf(g.a, st[v], g.m * sigmoid(own.get(iw, v)) * own.get(xw, v));
-    }
-    own.store(static_cast<T*>(a.y) + t * a.channels, h);
-    if (live) {
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (v < n) st[v] = h[v];
+        if (v >= n) continue;
+        if (!live) {
+            y[v] = (T)0.0f;
+            continue;
+        }
+        const Gate g = gate_of(rate_of(a.lam[c + v], a.c) * sigmoid((float)r[v]));
+        const float h = fmaf(g.a, st[v], __builtin_amdgcn_sqrtf(g.d) * sigmoid((float)i[v]) * (float)x[v]);
+        y[v] = (T)h;
+        st[v] = h;
     }
 }
 
@@ -717,7 +755,7 @@ Plan plan_of(const im2win_recurrence_desc* d) {
     const int64_t per = kWave * lane_channels(d);
     p.tiles = (d->channels + per - 1) / per;
     if (p.chunks > 1) p.words = (size_t)((p.chunks + p.chunks / kGroup) * d->channels + 2);      // pairs, states, ticket, to 16 bytes
-    p.look_bytes = (p.words * 8 + 15) / 16 * 16;
+    p.look_bytes = p.words ? (p.words * 8 + 15) / 16 * 16 + ((size_t)d->channels * 4 + 15) / 16 * 16 : 0;      // the rates behind the words
     p.states_bytes = ((size_t)(p.chunks * d->channels) * 4 + 15) / 16 * 16;
     return p;
 }
@@ -740,9 +778,14 @@ Look look_of(const Plan& p, int64_t channels, void* ws) {
     return k;
 }
 
-void fill(const Plan& p, void* ws, hipStream_t s) {
-    if (p.words)
-        hipLaunchKernelGGL(fill_kernel, dim3((unsigned)((p.words + 255) / 256)), dim3(256), 0, s, static_cast<uint64_t*>(ws), (int64_t)p.words);
+// Empties the words and works out the rates; where they lie, or NULL.
+const float* prepare(const im2win_recurrence_desc* d, const Plan& p, const float* lam, void* ws, hipStream_t s) {
+    if (!p.words) return nullptr;
+    float* rates = reinterpret_cast<float*>(static_cast<char*>(ws) + (p.words * 8 + 15) / 16 * 16);
+    // there are at least as many words as channels
+    hipLaunchKernelGGL(prepare_kernel, dim3((unsigned)((p.words + 255) / 256)), dim3(256), 0, s, static_cast<uint64_t*>(ws), (int64_t)p.words, lam, rates,
+                       (int)d->channels, d->c);
+    return rates;
 }
 
 template <typename F>
@@ -757,7 +800,7 @@ int launch_forward(const im2win_recurrence_desc* d, const Plan& p, RecArgs& a, v
     a.look = look_of(p, d->channels, ws);
     a.ld_x = d->ld_x; a.ld_r = d->ld_r; a.ld_i = d->ld_i;
     a.channels = (int)d->channels; a.tiles = (int)p.tiles; a.c = d->c;
-    fill(p, ws, s);
+    a.rates = prepare(d, p, a.lam, ws, s);
     with_type(d, [&](auto t, auto v) {
         hipLaunchKernelGGL((recurrence_kernel<decltype(t), decltype(v)::value>), dim3((unsigned)(p.chunks * p.tiles)), dim3(kThreads), 0, s, a);
     });
@@ -862,7 +905,7 @@ int im2win_gated_recurrence_backward(const im2win_recurrence_desc* d, const void
         a.look = look_of(p, d->channels, ws);
         a.ld_x = d->ld_x; a.ld_r = d->ld_r; a.ld_i = d->ld_i;
         a.channels = (int)d->channels; a.tiles = (int)p.tiles; a.c = d->c;
-        fill(p, ws, s);
+        a.rates = prepare(d, p, lam, ws, s);
         with_type(d, [&](auto t, auto v) {
             hipLaunchKernelGGL((recurrence_bwd_kernel<decltype(t), decltype(v)::value>), dim3((unsigned)(p.chunks * p.tiles)), dim3(kThreads), 0, s, a);
         });
