@@ -149,19 +149,24 @@ __device__ __forceinline__ uint32_t marked(const int* m) {
 // ---------------------------------------------------------------------------
 template <typename T, int V>
 struct Lane {
-    int c;           // first channel
+    int c;                    // first channel
+    uint32_t offset, wide;    // its bytes in a row of T and of floats: 32 bits beside the row's scalar address
     bool on;
     __device__ __forceinline__ Lane(int first, int channels) {
         on = first < channels;
         c = first + V <= channels ? first : channels - V;
+        offset = (uint32_t)c * (uint32_t)sizeof(T);
+        wide = (uint32_t)c * 4u;
     }
     __device__ __forceinline__ uint32_t load(const T* row) const {
         if constexpr (V * sizeof(T) == 4) {
             uint32_t u;
-            __builtin_memcpy(&u, row + c, 4);
+            __builtin_memcpy(&u, reinterpret_cast<const char*>(row) + offset, 4);
             return u;
         } else {
-            return __builtin_bit_cast(uint16_t, row[c]);
+            uint16_t u;
+            __builtin_memcpy(&u, reinterpret_cast<const char*>(row) + offset, 2);
+            return u;
         }
     }
     static __device__ __forceinline__ float get(uint32_t u, int v) {
@@ -170,16 +175,18 @@ struct Lane {
     }
     __device__ __forceinline__ void store(T* row, const float (&v)[V]) const {
         if (!on) return;
+        char* p = reinterpret_cast<char*>(row) + offset;
         if constexpr (V == 1) {
-            row[c] = (T)v[0];
+            const T u = (T)v[0];
+            __builtin_memcpy(p, &u, sizeof(T));
         } else {
             const uint32_t u = pack_bf16(v[0], v[1]);
-            __builtin_memcpy(row + c, &u, 4);
+            __builtin_memcpy(p, &u, 4);
         }
     }
-    __device__ __forceinline__ void load(const float* row, float (&v)[V]) const { __builtin_memcpy(v, row + c, 4 * V); }
+    __device__ __forceinline__ void load(const float* row, float (&v)[V]) const { __builtin_memcpy(v, reinterpret_cast<const char*>(row) + wide, 4 * V); }
     __device__ __forceinline__ void store_f32(float* row, const float (&v)[V]) const {
-        if (on) __builtin_memcpy(row + c, v, 4 * V);
+        if (on) __builtin_memcpy(reinterpret_cast<char*>(row) + wide, v, 4 * V);
     }
 };
 
@@ -364,29 +371,34 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_kernel(RecArgs a) {
                 db[j][v] = inside >> j & 1 ? db[j][v] : 0.0f;
             }
     }
-    // the wave's rows as one pair; where a sequence begins, its state from before is in b
+    // where sequences begin, their states from before are in b
+    if (begin && a.init) {
+#pragma unroll
+        for (int j = 0; j < kRows; ++j) {
+            if (!(begin >> j & 1)) continue;
+            float h0[V];
+            own.load(a.init + (int64_t)uniform(marks.first[wave * kRows + j]) * a.channels, h0);
+#pragma unroll
+            for (int v = 0; v < V; ++v) db[j][v] = fmaf(da[j][v], h0[v], db[j][v]);
+        }
+    }
+    // the wave's rows as one pair; most waves hold no row that a sequence begins with
     Pair p[V];
+    auto compose = [&](auto plain) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) p[v] = {1.0f, 0.0f};
+        for (int v = 0; v < V; ++v) p[v] = {1.0f, 0.0f};
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-        if (begin >> j & 1) {
-            if (a.init) {
-                float h0[V];
-                own.load(a.init + (int64_t)uniform(marks.first[wave * kRows + j]) * a.channels, h0);
-#pragma unroll
-                for (int v = 0; v < V; ++v) db[j][v] = fmaf(da[j][v], h0[v], db[j][v]);
-            }
-#pragma unroll
-            for (int v = 0; v < V; ++v) p[v] = {kReset, db[j][v]};
-        } else {
+        for (int j = 0; j < kRows; ++j) {
+            const bool first = !plain && (begin >> j & 1);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 p[v].a *= da[j][v];
-                p[v].b = fmaf(da[j][v], p[v].b, db[j][v]);
+                p[v].b = first ? db[j][v] : fmaf(da[j][v], p[v].b, db[j][v]);
             }
         }
-    }
+    };
+    if (begin) compose(std::false_type{});
+    else compose(std::true_type{});
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         if (begin) p[v].a = kReset;
@@ -413,20 +425,21 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_kernel(RecArgs a) {
         for (int v = 0; v < V; ++v)
             if (own.on) leave(a.look.states + (int64_t)(chunk / kGroup) * a.channels + c + v, {0.0f, apply(p[v], h[v])});
     }
+    if (!a.y && !a.final_state) return;
     T* yp = static_cast<T*>(a.y) + (int64_t)t0 * a.channels;
+    auto write = [&](auto plain) {
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-        if (begin >> j & 1) {
+        for (int j = 0; j < kRows; ++j) {
+            const bool first = !plain && (begin >> j & 1);
 #pragma unroll
-            for (int v = 0; v < V; ++v) h[v] = db[j][v];
-        } else {
-#pragma unroll
-            for (int v = 0; v < V; ++v) h[v] = fmaf(da[j][v], h[v], db[j][v]);
+            for (int v = 0; v < V; ++v) h[v] = first ? db[j][v] : fmaf(da[j][v], h[v], db[j][v]);
+            if (plain || ((inside >> j & 1) && a.y)) own.store(yp, h);
+            yp += a.channels;
+            if (!plain && (end >> j & 1) && a.final_state) own.store_f32(a.final_state + (int64_t)uniform(marks.last[wave * kRows + j]) * a.channels, h);
         }
-        if ((inside >> j & 1) && a.y) own.store(yp, h);
-        yp += a.channels;
-        if ((end >> j & 1) && a.final_state) own.store_f32(a.final_state + (int64_t)uniform(marks.last[wave * kRows + j]) * a.channels, h);
-    }
+    };
+    if ((begin | end) || inside != kAllRows || !a.y) write(std::false_type{});
+    else write(std::true_type{});
 }
 
 // Final states (or gradients of initial ones) of sequences without rows when
@@ -545,36 +558,39 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
         if (a.d_final) own.load(a.d_final + (int64_t)uniform(marks.last[wave * kRows + j]) * a.channels, g0);
     };
     Pair p[V], q[V];
+    auto compose = [&](auto plain) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) p[v] = q[v] = {1.0f, 0.0f};
+        for (int v = 0; v < V; ++v) p[v] = q[v] = {1.0f, 0.0f};
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-        if (begin >> j & 1) {
-            float h0[V];
-            initial(j, h0);
+        for (int j = 0; j < kRows; ++j) {
+            if (!plain && (begin >> j & 1)) {
+                float h0[V];
+                initial(j, h0);
 #pragma unroll
-            for (int v = 0; v < V; ++v) p[v].b = h0[v];
+                for (int v = 0; v < V; ++v) p[v].b = h0[v];
+            }
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                p[v].a *= da[j][v];
+                p[v].b = fmaf(da[j][v], p[v].b, hb[j][v]);
+            }
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            p[v].a *= da[j][v];
-            p[v].b = fmaf(da[j][v], p[v].b, hb[j][v]);
-        }
-    }
+        for (int j = kRows - 1; j >= 0; --j) {
+            if (!plain && (end >> j & 1)) {
+                float g0[V];
+                after(j, g0);
 #pragma unroll
-    for (int j = kRows - 1; j >= 0; --j) {
-        if (end >> j & 1) {
-            float g0[V];
-            after(j, g0);
+                for (int v = 0; v < V; ++v) q[v].b = g0[v];
+            }
 #pragma unroll
-            for (int v = 0; v < V; ++v) q[v].b = g0[v];
+            for (int v = 0; v < V; ++v) q[v].b = da[j][v] * (q[v].b + own.get(gw[j], v));
         }
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            q[v].b = da[j][v] * (q[v].b + own.get(gw[j], v));
-            q[v].a *= da[j][v];
-        }
-    }
+        for (int v = 0; v < V; ++v) q[v].a = p[v].a;      // the same product
+    };
+    if (begin | end) compose(std::false_type{});
+    else compose(std::true_type{});
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         if (begin) p[v].a = kReset;
@@ -595,16 +611,20 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = apply(agg[w][lane * V + v], h[v]);
     }
+    auto states = [&](auto plain) {
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
-        if (begin >> j & 1) initial(j, h);
+        for (int j = 0; j < kRows; ++j) {
+            if (!plain && (begin >> j & 1)) initial(j, h);
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float before = h[v];
-            h[v] = fmaf(da[j][v], h[v], hb[j][v]);
-            hb[j][v] = before;
+            for (int v = 0; v < V; ++v) {
+                const float before = h[v];
+                h[v] = fmaf(da[j][v], h[v], hb[j][v]);
+                hb[j][v] = before;
+            }
         }
-    }
+    };
+    if (begin) states(std::false_type{});
+    else states(std::true_type{});
     float g[V] = {};
     if (order) look_back<V>(a.look, order, c, a.channels, pre, enter, g);
     for (int w = kWaves - 1; w > wave; --w) {
@@ -619,39 +639,43 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
     float sum[V] = {};
     const int64_t behind = (int64_t)(t0 + kRows) * a.channels;
     T *dx = static_cast<T*>(a.dx) + behind, *dr = static_cast<T*>(a.dr) + behind, *di = static_cast<T*>(a.di) + behind;
+    auto write = [&](auto plain) {
 #pragma unroll
-    for (int j = kRows - 1; j >= 0; --j) {
-        dx -= a.channels;
-        dr -= a.channels;
-        di -= a.channels;
-        if (!(inside >> j & 1)) continue;
-        if (end >> j & 1) after(j, g);
-        // the gates again: kept from above, they would take four registers an element
-        arrive(rw[j]);
-        arrive(iw[j]);
-        float ox[V], orr[V], oi[V];
+        for (int j = kRows - 1; j >= 0; --j) {
+            dx -= a.channels;
+            dr -= a.channels;
+            di -= a.channels;
+            if (!plain && !(inside >> j & 1)) continue;
+            if (!plain && (end >> j & 1)) after(j, g);
+            // the gates again: kept from above, they would take four registers an element
+            arrive(rw[j]);
+            arrive(iw[j]);
+            float ox[V], orr[V], oi[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const float x = own.get(xw[j], v), sr = sigmoid(own.get(rw[j], v)), si = sigmoid(own.get(iw[j], v));
-            const float gg = g[v] + own.get(gw[j], v);
-            const float l2 = rate[v] * sr;                   // -L / ln 2
-            const Gate gt = gate_of(l2);
-            // 1 / m; L / m goes to zero with L, and is zero where both are
-            const float d = fmaxf(gt.d, 0x1p-125f), im = __builtin_amdgcn_rsqf(d);
-            const float l = l2 * (-1.0f / kLog2e), gm = gg * (d * im);
-            const float dl = gg * gt.a * fmaf(-gt.a * (l * im), si * x, l * hb[j][v]);      // dL L
-            ox[v] = gm * si;
-            oi[v] = ox[v] * fmaf(-si, x, x);
-            orr[v] = fmaf(-sr, dl, dl);
-            sum[v] += dl;
-            g[v] = gt.a * gg;
+            for (int v = 0; v < V; ++v) {
+                const float x = own.get(xw[j], v), sr = sigmoid(own.get(rw[j], v)), si = sigmoid(own.get(iw[j], v));
+                const float gg = g[v] + own.get(gw[j], v);
+                const float l2 = rate[v] * sr;                   // -L / ln 2
+                const Gate gt = gate_of(l2);
+                // 1 / m; L / m goes to zero with L, and is zero where both are
+                const float d = fmaxf(gt.d, 0x1p-125f), im = __builtin_amdgcn_rsqf(d);
+                const float l = l2 * (-1.0f / kLog2e), gm = gg * (d * im);
+                const float dl = gg * gt.a * fmaf(-gt.a * (l * im), si * x, l * hb[j][v]);      // dL L
+                ox[v] = gm * si;
+                oi[v] = ox[v] * fmaf(-si, x, x);
+                orr[v] = fmaf(-sr, dl, dl);
+                sum[v] += dl;
+                g[v] = gt.a * gg;
+            }
+            own.store(dx, ox);
+            own.store(dr, orr);
+            own.store(di, oi);
+            if (!plain && (begin >> j & 1) && a.d_init) own.store_f32(a.d_init + (int64_t)uniform(marks.first[wave * kRows + j]) * a.channels, g);
+            __builtin_amdgcn_sched_barrier(0);      // a row at a time: mixed, the rows' temporaries spill
         }
-        own.store(dx, ox);
-        own.store(dr, orr);
-        own.store(di, oi);
-        if ((begin >> j & 1) && a.d_init) own.store_f32(a.d_init + (int64_t)uniform(marks.first[wave * kRows + j]) * a.channels, g);
-        __builtin_amdgcn_sched_barrier(0);      // a row at a time: mixed, the rows' temporaries spill
-    }
+    };
+    if ((begin | end) || inside != kAllRows) write(std::false_type{});
+    else write(std::true_type{});
     __syncthreads();
 #pragma unroll
     for (int v = 0; v < V; ++v) pre[wave][lane * V + v].b = sum[v];
