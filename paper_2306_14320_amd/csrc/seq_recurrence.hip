@@ -27,10 +27,12 @@ namespace im2win {
 namespace {
 
 constexpr int kRows = 16;                 // rows a wave holds in registers
+constexpr int kBwdRows = 8;               // in the gradients, which hold twice as much of each
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kChunk = kRows * kWaves;    // rows of a workgroup
-constexpr uint32_t kAllRows = (1u << kRows) - 1;
+constexpr int kBwdChunk = kBwdRows * kWaves;
+template <int R> constexpr uint32_t kAllRows = (1u << R) - 1;
 constexpr int kGroup = 32;                // chunks whose pairs are looked at one by one
 constexpr int kLook = kGroup / kWaves;    // of those, the ones a wave looks at
 constexpr float kReset = -1.0f;           // the a of a pair that does not look back
@@ -78,19 +80,20 @@ struct Look {
 // ---------------------------------------------------------------------------
 // The sequences' first and last rows inside of a chunk
 // ---------------------------------------------------------------------------
+template <int N>
 struct Marks {
-    int first[kChunk];    // the sequence that begins at a row, or -1
-    int last[kChunk];     // the sequence that ends with a row, or -1
+    int first[N];    // the sequence that begins at a row, or -1
+    int last[N];     // the sequence that ends with a row, or -1
 };
 
-// Fills the marks of the chunk of rows [row0, row0 + kChunk) and calls
+// Fills the marks of the chunk of rows [row0, row0 + N) and calls
 // empty(b), with all lanes of a wave, for each sequence without rows that
 // lies there (the last chunk: there or behind it).
-template <typename F>
-__device__ __forceinline__ void mark(const SeqMap& seq, int row0, bool last_chunk, Marks& m, F empty) {
+template <int N, typename F>
+__device__ __forceinline__ void mark(const SeqMap& seq, int row0, bool last_chunk, Marks<N>& m, F empty) {
     const int tid = threadIdx.x, lane = tid % kWave;
     if (!seq.starts) {
-        if (tid < kChunk) {
+        if (tid < N) {
             const int t = row0 + tid;
             const bool in = t < seq.tokens;
             const int b = in ? t / seq.len : 0;
@@ -100,11 +103,11 @@ __device__ __forceinline__ void mark(const SeqMap& seq, int row0, bool last_chun
         __syncthreads();
         return;
     }
-    if (tid < kChunk) m.first[tid] = m.last[tid] = -1;
+    if (tid < N) m.first[tid] = m.last[tid] = -1;
     __syncthreads();
     // sequences that begin in front of the chunk: all but the last of them end there
     const int skip = seq.before(row0);
-    const int end = row0 + kChunk;
+    const int end = row0 + N;
     for (int base = (skip ? skip - 1 : 0) + tid / kWave * kWave; base < seq.count; base += kThreads) {
         const int b = base + lane;
         int f = 0, n = 0;
@@ -128,16 +131,18 @@ __device__ __forceinline__ void mark(const SeqMap& seq, int row0, bool last_chun
     __syncthreads();
 }
 
-// The rows [t0, t0 + kRows) that lie in [lo, hi), a bit each
+// The rows [t0, t0 + R) that lie in [lo, hi), a bit each
+template <int R>
 __device__ __forceinline__ uint32_t rows_inside(int t0, int lo, int hi) {
     const int from = lo - t0, to = hi - t0;
-    const uint32_t upto = to <= 0 ? 0u : to >= kRows ? kAllRows : (1u << to) - 1;
-    return from <= 0 ? upto : from >= kRows ? 0u : upto & ~((1u << from) - 1);
+    const uint32_t upto = to <= 0 ? 0u : to >= R ? kAllRows<R> : (1u << to) - 1;
+    return from <= 0 ? upto : from >= R ? 0u : upto & ~((1u << from) - 1);
 }
 // The rows of a wave that marks name, a bit each; the sequence itself is read where a bit is set.
+template <int R>
 __device__ __forceinline__ uint32_t marked(const int* m) {
     const int lane = threadIdx.x % kWave;
-    return (uint32_t)__ballot(lane < kRows && m[lane % kRows] >= 0);
+    return (uint32_t)__ballot(lane < R && m[lane % R] >= 0);
 }
 
 // ---------------------------------------------------------------------------
@@ -243,7 +248,7 @@ struct RecArgs {
     const float* init;
     void* y;              // NULL: only the states
     float* final_state;
-    float* chunk_states;  // chunk x channel, or NULL
+    float* chunk_states;  // chunk of the gradients x channel, or NULL
     Look look;
     int64_t ld_x, ld_r, ld_i;
     int channels, tiles;
@@ -306,7 +311,7 @@ __device__ __forceinline__ void look_back(const Look& k, int order, int c, int c
 
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads, 2) void recurrence_kernel(RecArgs a) {
-    __shared__ Marks marks;
+    __shared__ Marks<kChunk> marks;
     __shared__ Pair agg[kWaves][kWave * V];
     __shared__ Pair pre[kWaves][kWave * V];
     __shared__ float enter[kWave * V];
@@ -352,8 +357,8 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_kernel(RecArgs a) {
     load_rates(own, a.rates, a.lam, a.c, rate);
 
     float da[kRows][V], db[kRows][V];
-    const uint32_t begin = marked(marks.first + wave * kRows), end = marked(marks.last + wave * kRows);
-    const uint32_t inside = rows_inside(t0, lo, hi);
+    const uint32_t begin = marked<kRows>(marks.first + wave * kRows), end = marked<kRows>(marks.last + wave * kRows);
+    const uint32_t inside = rows_inside<kRows>(t0, lo, hi);
 #pragma unroll
     for (int j = 0; j < kRows; ++j)
 #pragma unroll
@@ -362,7 +367,7 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_kernel(RecArgs a) {
             da[j][v] = g.a;
             db[j][v] = __builtin_amdgcn_sqrtf(g.d) * sigmoid(own.get(iw[j], v)) * own.get(xw[j], v);
         }
-    if (inside != kAllRows) {
+    if (inside != kAllRows<kRows>) {
 #pragma unroll
         for (int j = 0; j < kRows; ++j)
 #pragma unroll
@@ -415,11 +420,11 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_kernel(RecArgs a) {
     }
     float h[V] = {};
     if (chunk) look_back<V>(a.look, chunk, c, a.channels, pre, enter, h);
-    if (a.chunk_states && wave == 0) own.store_f32(a.chunk_states + (int64_t)chunk * a.channels, h);
     for (int w = 0; w < wave; ++w) {
 #pragma unroll
         for (int v = 0; v < V; ++v) h[v] = apply(agg[w][lane * V + v], h[v]);
     }
+    if (a.chunk_states && wave * kRows % kBwdChunk == 0 && t0 < a.seq.tokens) own.store_f32(a.chunk_states + (int64_t)(t0 / kBwdChunk) * a.channels, h);
     if (wave == kWaves - 1 && chunk % kGroup == kGroup - 1 && chunk + 1 < a.look.chunks) {
 #pragma unroll
         for (int v = 0; v < V; ++v)
@@ -438,7 +443,7 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_kernel(RecArgs a) {
             if (!plain && (end >> j & 1) && a.final_state) own.store_f32(a.final_state + (int64_t)uniform(marks.last[wave * kRows + j]) * a.channels, h);
         }
     };
-    if ((begin | end) || inside != kAllRows || !a.y) write(std::false_type{});
+    if ((begin | end) || inside != kAllRows<kRows> || !a.y) write(std::false_type{});
     else write(std::true_type{});
 }
 
@@ -469,7 +474,7 @@ struct RecBwdArgs {
 
 template <typename T, int V>
 __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs a) {
-    __shared__ Marks marks;
+    __shared__ Marks<kBwdChunk> marks;
     __shared__ Pair agg[kWaves][kWave * V];
     __shared__ Pair back[kWaves][kWave * V];
     __shared__ Pair pre[kWaves][kWave * V];
@@ -485,7 +490,7 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
     }
     const int order = ticket / a.tiles, tile = ticket - order * a.tiles;
     const int chunk = a.look.chunks - 1 - order;
-    const int row0 = chunk * kChunk;
+    const int row0 = chunk * kBwdChunk;
     const Lane<T, V> own((tile * kWave + lane) * V, a.channels);
     const int c = own.c;
     mark(a.seq, row0, order == 0, marks, [&](int b) {
@@ -501,15 +506,15 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
         return;
     }
 
-    const int t0 = row0 + wave * kRows;
-    uint32_t xw[kRows], rw[kRows], iw[kRows], gw[kRows];
+    const int t0 = row0 + wave * kBwdRows;
+    uint32_t xw[kBwdRows], rw[kBwdRows], iw[kBwdRows], gw[kBwdRows];
     const int ts = t0 < lo ? lo : t0 >= hi ? hi - 1 : t0;
     const T* xp = static_cast<const T*>(a.x) + ts * a.ld_x;
     const T* rp = static_cast<const T*>(a.r) + ts * a.ld_r;
     const T* dp = static_cast<const T*>(a.dy) + (int64_t)ts * a.channels;
     const T* ip = static_cast<const T*>(a.i) + ts * a.ld_i;
 #pragma unroll
-    for (int j = 0; j < kRows; ++j) {
+    for (int j = 0; j < kBwdRows; ++j) {
         xw[j] = own.load(xp);
         rw[j] = own.load(rp);
         iw[j] = own.load(ip);
@@ -525,20 +530,20 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
     if (chunk) own.load(a.chunk_states + (int64_t)chunk * a.channels, h);
 
     // hb: first the row's b, then the state in front of the row
-    float da[kRows][V], hb[kRows][V];
-    const uint32_t begin = marked(marks.first + wave * kRows), end = marked(marks.last + wave * kRows);
-    const uint32_t inside = rows_inside(t0, lo, hi);
+    float da[kBwdRows][V], hb[kBwdRows][V];
+    const uint32_t begin = marked<kBwdRows>(marks.first + wave * kBwdRows), end = marked<kBwdRows>(marks.last + wave * kBwdRows);
+    const uint32_t inside = rows_inside<kBwdRows>(t0, lo, hi);
 #pragma unroll
-    for (int j = 0; j < kRows; ++j)
+    for (int j = 0; j < kBwdRows; ++j)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Gate g = gate_of(rate[v] * sigmoid(own.get(rw[j], v)));
             da[j][v] = g.a;
             hb[j][v] = __builtin_amdgcn_sqrtf(g.d) * sigmoid(own.get(iw[j], v)) * own.get(xw[j], v);
         }
-    if (inside != kAllRows) {
+    if (inside != kAllRows<kBwdRows>) {
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) {
+        for (int j = 0; j < kBwdRows; ++j) {
             if (!(inside >> j & 1)) gw[j] = 0;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -550,19 +555,19 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
     auto initial = [&](int j, float (&h0)[V]) {
 #pragma unroll
         for (int v = 0; v < V; ++v) h0[v] = 0.0f;
-        if (a.init) own.load(a.init + (int64_t)uniform(marks.first[wave * kRows + j]) * a.channels, h0);
+        if (a.init) own.load(a.init + (int64_t)uniform(marks.first[wave * kBwdRows + j]) * a.channels, h0);
     };
     auto after = [&](int j, float (&g0)[V]) {
 #pragma unroll
         for (int v = 0; v < V; ++v) g0[v] = 0.0f;
-        if (a.d_final) own.load(a.d_final + (int64_t)uniform(marks.last[wave * kRows + j]) * a.channels, g0);
+        if (a.d_final) own.load(a.d_final + (int64_t)uniform(marks.last[wave * kBwdRows + j]) * a.channels, g0);
     };
     Pair p[V], q[V];
     auto compose = [&](auto plain) {
 #pragma unroll
         for (int v = 0; v < V; ++v) p[v] = q[v] = {1.0f, 0.0f};
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) {
+        for (int j = 0; j < kBwdRows; ++j) {
             if (!plain && (begin >> j & 1)) {
                 float h0[V];
                 initial(j, h0);
@@ -576,7 +581,7 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
             }
         }
 #pragma unroll
-        for (int j = kRows - 1; j >= 0; --j) {
+        for (int j = kBwdRows - 1; j >= 0; --j) {
             if (!plain && (end >> j & 1)) {
                 float g0[V];
                 after(j, g0);
@@ -613,7 +618,7 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
     }
     auto states = [&](auto plain) {
 #pragma unroll
-        for (int j = 0; j < kRows; ++j) {
+        for (int j = 0; j < kBwdRows; ++j) {
             if (!plain && (begin >> j & 1)) initial(j, h);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
@@ -637,11 +642,11 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
             if (own.on) leave(a.look.states + (int64_t)(order / kGroup) * a.channels + c + v, {0.0f, apply(q[v], g[v])});
     }
     float sum[V] = {};
-    const int64_t behind = (int64_t)(t0 + kRows) * a.channels;
+    const int64_t behind = (int64_t)(t0 + kBwdRows) * a.channels;
     T *dx = static_cast<T*>(a.dx) + behind, *dr = static_cast<T*>(a.dr) + behind, *di = static_cast<T*>(a.di) + behind;
     auto write = [&](auto plain) {
 #pragma unroll
-        for (int j = kRows - 1; j >= 0; --j) {
+        for (int j = kBwdRows - 1; j >= 0; --j) {
             dx -= a.channels;
             dr -= a.channels;
             di -= a.channels;
@@ -670,11 +675,11 @@ __global__ __launch_bounds__(kThreads, 2) void recurrence_bwd_kernel(RecBwdArgs 
             own.store(dx, ox);
             own.store(dr, orr);
             own.store(di, oi);
-            if (!plain && (begin >> j & 1) && a.d_init) own.store_f32(a.d_init + (int64_t)uniform(marks.first[wave * kRows + j]) * a.channels, g);
+            if (!plain && (begin >> j & 1) && a.d_init) own.store_f32(a.d_init + (int64_t)uniform(marks.first[wave * kBwdRows + j]) * a.channels, g);
             __builtin_amdgcn_sched_barrier(0);      // a row at a time: mixed, the rows' temporaries spill
         }
     };
-    if ((begin | end) || inside != kAllRows) write(std::false_type{});
+    if ((begin | end) || inside != kAllRows<kBwdRows>) write(std::false_type{});
     else write(std::true_type{});
     __syncthreads();
 #pragma unroll
@@ -773,9 +778,9 @@ struct Plan {
     size_t words, look_bytes, states_bytes, total;
 };
 
-Plan plan_of(const im2win_recurrence_desc* d) {
+Plan plan_of(const im2win_recurrence_desc* d, int chunk) {
     Plan p{};
-    p.chunks = (d->tokens + kChunk - 1) / kChunk;
+    p.chunks = (d->tokens + chunk - 1) / chunk;
     const int64_t per = kWave * lane_channels(d);
     p.tiles = (d->channels + per - 1) / per;
     if (p.chunks > 1) p.words = (size_t)((p.chunks + p.chunks / kGroup) * d->channels + 2);      // pairs, states, ticket, to 16 bytes
@@ -847,7 +852,7 @@ int im2win_gated_recurrence_chunks(const im2win_recurrence_desc* d, int64_t* chu
     int rc = check_desc(d);
     if (rc) return rc;
     if (!chunks) return fail(IM2WIN_ENULL, "chunks is NULL");
-    *chunks = plan_of(d).chunks;
+    *chunks = plan_of(d, kBwdChunk).chunks;
     return ok();
 }
 
@@ -855,7 +860,7 @@ int im2win_gated_recurrence_workspace_bytes(const im2win_recurrence_desc* d, siz
     int rc = check_desc(d);
     if (rc) return rc;
     if (!bytes) return fail(IM2WIN_ENULL, "bytes is NULL");
-    *bytes = plan_of(d).look_bytes;
+    *bytes = plan_of(d, kChunk).look_bytes;
     return ok();
 }
 
@@ -867,7 +872,7 @@ int im2win_gated_recurrence(const im2win_recurrence_desc* d, const void* x, cons
         (rc = may_ptr(initial_state, 4, "initial_state")) || (rc = may_ptr(final_state, 4, "final_state")) ||
         (rc = may_ptr(chunk_states, 4, "chunk_states")))
         return rc;
-    const Plan p = plan_of(d);
+    const Plan p = plan_of(d, kChunk);
     const size_t e = size_of(d->dtype);
     if (d->tokens && ((rc = need_ptr(x, e, "x")) || (rc = need_ptr(r, e, "r")) || (rc = need_ptr(i, e, "i")) || (rc = need_ptr(y, e, "y")))) return rc;
     if (p.look_bytes && (rc = need_ptr(workspace, 16, "workspace"))) return rc;
@@ -886,7 +891,7 @@ int im2win_gated_recurrence_backward_workspace_bytes(const im2win_recurrence_des
     int rc = check_desc(d);
     if (rc) return rc;
     if (!bytes) return fail(IM2WIN_ENULL, "bytes is NULL");
-    const Plan p = plan_of(d);
+    const Plan p = plan_of(d, kBwdChunk);
     *bytes = p.look_bytes + 2 * p.states_bytes;     // the look, the chunks' sums, the chunks' states
     return ok();
 }
@@ -901,7 +906,7 @@ int im2win_gated_recurrence_backward(const im2win_recurrence_desc* d, const void
         (rc = may_ptr(d_final_state, 4, "d_final_state")) || (rc = may_ptr(d_initial_state, 4, "d_initial_state")) ||
         (rc = may_ptr(chunk_states, 4, "chunk_states")))
         return rc;
-    const Plan p = plan_of(d);
+    const Plan p = plan_of(d, kBwdChunk);
     const size_t e = size_of(d->dtype), need = p.look_bytes + 2 * p.states_bytes;
     if (d->tokens && ((rc = need_ptr(dy, e, "dy")) || (rc = need_ptr(x, e, "x")) || (rc = need_ptr(r, e, "r")) || (rc = need_ptr(i, e, "i")) ||
                       (rc = need_ptr(dx, e, "dx")) || (rc = need_ptr(dr, e, "dr")) || (rc = need_ptr(di, e, "di")) ||
@@ -920,7 +925,7 @@ int im2win_gated_recurrence_backward(const im2win_recurrence_desc* d, const void
             f.x = x; f.r = r; f.i = i; f.lam = lam; f.seq = seq; f.init = initial_state;
             f.chunk_states = reinterpret_cast<float*>(ws + p.look_bytes + p.states_bytes);
             chunk_states = f.chunk_states;
-            if ((rc = launch_forward(d, p, f, ws, s))) return rc;
+            if ((rc = launch_forward(d, plan_of(d, kChunk), f, ws, s))) return rc;      // of fewer chunks: its words fit where the gradients' lie
         }
         RecBwdArgs a{};
         a.dy = dy; a.x = x; a.r = r; a.i = i; a.lam = lam; a.seq = seq;
