@@ -372,7 +372,7 @@ typedef struct {
     int64_t head_dim;          /* a multiple of 8 up to 256 */
     int64_t window;            /* W >= 1: a token sees itself and the W-1 before it */
     int64_t sinks;             /* S, 0 to 32: and the first S of its sequence */
-    int64_t ld_q, ld_k, ld_v;  /* row strides of q, k and v */
+    int64_t ld_q, ld_k, ld_v;  /* row strides of q, k and v, below 2^24 */
     int32_t dtype;             /* of q, k, v, the caches, y and the gradients */
     float scale;               /* > 0 */
 } im2win_window_desc;

@@ -12,6 +12,7 @@
 
 #include "seq_common.h"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace im2win {
@@ -71,7 +72,6 @@ struct Tile {
     static constexpr int kElems = 16 / sizeof(T);
     static constexpr int kChunks = DP / kElems;             // of a row
     static constexpr int kBytes = R * DP * (int)sizeof(T);
-    static constexpr int kPerThread = R * kChunks / kAttnThreads;      // where a workgroup holds it
 
     static __device__ __forceinline__ int turn(int row) {
         if constexpr (kChunks % 8 == 0) return (row & 3) << 1 | (row >> 2 & 1);
@@ -127,10 +127,59 @@ private:
 
 // 16 bytes in flight
 struct Chunk {
-    uint32_t u[4];
-    __device__ __forceinline__ void zero() { u[0] = u[1] = u[2] = u[3] = 0; }
-    __device__ __forceinline__ void load(const void* p) { __builtin_memcpy(u, p, 16); }
-    __device__ __forceinline__ void store(void* p) const { __builtin_memcpy(p, u, 16); }
+    uint32_t __attribute__((ext_vector_type(4))) u;
+    __device__ __forceinline__ void zero() { u = 0; }
+    __device__ __forceinline__ void load(const void* p) { __builtin_memcpy(&u, p, 16); }
+    __device__ __forceinline__ void store(void* p) const { __builtin_memcpy(p, &u, 16); }
+};
+
+// ---------------------------------------------------------------------------
+// A tile's way from rows in memory to LDS, 16 bytes a thread and pass, through
+// registers in which the loads stay in flight.  Threads side by side take a
+// row's chunks (their number rounded up to a power of two, so that a thread's
+// place in its row is the same in every pass and its address one 32-bit offset
+// beside a scalar one).
+// ---------------------------------------------------------------------------
+constexpr int64_t kMaxAttnStride = int64_t(1) << 24;      // 64 rows of bf16 or 32 of fp32 within 32 bits of bytes
+
+template <typename T, int DP, int R>
+struct Stage {
+    using Lds = Tile<T, DP, R>;
+    static constexpr int up(int n) { return n <= 4 ? 4 : n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64; }
+    static constexpr int kLanes = up(Lds::kChunks), kPassRows = kAttnThreads / kLanes, kPasses = R / kPassRows;
+    static_assert(kPasses >= 1 && R % kPassRows == 0, "whole passes");
+    Chunk c[kPasses];
+
+    static __device__ __forceinline__ int row() { return (int)threadIdx.x / kLanes; }
+    static __device__ __forceinline__ int chunk() { return (int)threadIdx.x % kLanes; }
+    static __device__ __forceinline__ bool inside(int dim) { return chunk() * Lds::kElems < dim; }      // the chunk holds channels
+    // Bytes from the tile's first row to the thread's first chunk, for rows `stride` bytes apart
+    static __device__ __forceinline__ uint32_t offset(uint32_t stride) { return (uint32_t)row() * stride + (uint32_t)chunk() * 16; }
+
+    // `valid` of the tile's rows exist (all where at least R), the first at p; the others, and channels behind dim, are zeros
+    __device__ __forceinline__ void fetch(const char* p, uint32_t offset, uint32_t stride, int valid, int dim) {
+        if (valid >= R && (Lds::kChunks * Lds::kElems == dim && Lds::kChunks == kLanes)) {
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i) {
+                c[i].load(p + offset);
+                p += (int64_t)kPassRows * stride;
+            }
+        } else {
+            const bool in = inside(dim);
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i) {
+                if (in && row() + i * kPassRows < valid) c[i].load(p + offset);
+                else c[i].zero();
+                p += (int64_t)kPassRows * stride;
+            }
+        }
+    }
+    __device__ __forceinline__ void put(char* lds) const {
+        if (Lds::kChunks == kLanes || chunk() < Lds::kChunks) {
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i) c[i].store(lds + Lds::at(row() + i * kPassRows, chunk()));
+        }
+    }
 };
 
 // Zeroes the infinities and NaN among a chunk's elements; whether there were any.
@@ -242,6 +291,8 @@ inline int check_attention(const im2win_window_desc* d) {
     if ((rc = check_ld(d->ld_q, d->q_heads * d->head_dim, "ld_q")) || (rc = check_ld(d->ld_k, d->kv_heads * d->head_dim, "ld_k")) ||
         (rc = check_ld(d->ld_v, d->kv_heads * d->head_dim, "ld_v")))
         return rc;
+    if (std::max({d->ld_q, d->ld_k, d->ld_v}) >= kMaxAttnStride)
+        return fail(IM2WIN_EOVERFLOW, "row strides stay below 2^24 (got %lld, %lld, %lld)", (long long)d->ld_q, (long long)d->ld_k, (long long)d->ld_v);
     return IM2WIN_OK;
 }
 

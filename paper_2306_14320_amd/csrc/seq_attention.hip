@@ -125,7 +125,7 @@ template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_attention_kernel(AttnArgs a) {
     constexpr int BK = kTileKeys<T, DP>, NB = BK / 32;
     using KV = Tile<T, DP, BK>;
-    static_assert(BK * KV::kChunks % kAttnThreads == 0, "whole rounds");
+    using St = Stage<T, DP, BK>;
     __shared__ __align__(16) char kt[KV::kBytes], vt[KV::kBytes];
     __shared__ uint32_t flags[2];      // rows of the tile whose values are not all finite
     const int64_t item = die_order(blockIdx.x, a.items);
@@ -167,21 +167,33 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
     int wq1 = past + st.row + (wave * kCols + kCols - 1) / a.pack;
     wq1 = wq1 < qlast ? wq1 : qlast;
 
-    Chunk kr[KV::kPerThread], vr[KV::kPerThread];
-    auto address = [&](int p, const void* in, const void* cache, int64_t ld) {
-        if (p < past) return static_cast<const T*>(cache) + ((slot * rows + ring(p, a.window, a.sinks)) * a.kv_heads + kvh) * a.dim;
-        return static_cast<const T*>(in) + (st.first + (p - past)) * ld + (int64_t)kvh * a.dim;
+    // the value or key rows of the call, from position `past` on, and those of the cache
+    auto cached = [&](int p) { return ((slot * rows + ring(p, a.window, a.sinks)) * a.kv_heads + kvh) * a.dim; };
+    const uint32_t sk = (uint32_t)a.ld_k * (uint32_t)sizeof(T), sv = (uint32_t)a.ld_v * (uint32_t)sizeof(T);
+    const uint32_t ok = St::offset(sk), ov = St::offset(sv);
+    const char* kn = reinterpret_cast<const char*>(static_cast<const T*>(a.k) + st.first * a.ld_k + (int64_t)kvh * a.dim);
+    const char* vn = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + st.first * a.ld_v + (int64_t)kvh * a.dim);
+    auto value = [&](int p) {
+        return p < past ? static_cast<const T*>(a.v_cache) + cached(p) : reinterpret_cast<const T*>(vn + (int64_t)(p - past) * sv);
     };
+    St kr, vr;
     auto fetch = [&](int base, int stop) {
+        if (base >= past) {
+            kr.fetch(kn + (int64_t)(base - past) * sk, ok, sk, stop - base, a.dim);
+            vr.fetch(vn + (int64_t)(base - past) * sv, ov, sv, stop - base, a.dim);
+            return;
+        }
+        const int e = St::chunk() * KV::kElems;
 #pragma unroll
-        for (int i = 0; i < KV::kPerThread; ++i) {
-            const int n = tid + i * kAttnThreads, p = base + n / KV::kChunks, e = n % KV::kChunks * KV::kElems;
+        for (int i = 0; i < St::kPasses; ++i) {
+            const int p = base + St::row() + i * St::kPassRows;
             if (p < stop && e < a.dim) {
-                kr[i].load(address(p, a.k, a.k_cache, a.ld_k) + e);
-                vr[i].load(address(p, a.v, a.v_cache, a.ld_v) + e);
+                const T* k = p < past ? static_cast<const T*>(a.k_cache) + cached(p) : reinterpret_cast<const T*>(kn + (int64_t)(p - past) * sk);
+                kr.c[i].load(k + e);
+                vr.c[i].load(value(p) + e);
             } else {
-                kr[i].zero();
-                vr[i].zero();
+                kr.c[i].zero();
+                vr.c[i].zero();
             }
         }
     };
@@ -198,13 +210,15 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
         __syncthreads();
         if (tid < 2) flags[tid] = 0;
         __syncthreads();
+        if (partial) {
 #pragma unroll
-        for (int i = 0; i < KV::kPerThread; ++i) {
-            const int n = tid + i * kAttnThreads, rw = n / KV::kChunks, at = KV::at(rw, n % KV::kChunks);
-            kr[i].store(kt + at);
-            if (partial && drop_nonfinite<T>(vr[i])) atomicOr(&flags[rw / 32], 1u << rw % 32);
-            vr[i].store(vt + at);
+            for (int i = 0; i < St::kPasses; ++i) {
+                const int rw = St::row() + i * St::kPassRows;
+                if (drop_nonfinite<T>(vr.c[i])) atomicOr(&flags[rw / 32], 1u << rw % 32);
+            }
         }
+        kr.put(kt);
+        vr.put(vt);
         __syncthreads();
         const int now = base, now_stop = stop;
         if (sink_tile) sink_tile = false, base = begin, stop = end;
@@ -245,7 +259,7 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
             for (uint32_t rest = uniform(flags[f]); rest; rest &= rest - 1) {
                 const int p = now + 32 * f + __builtin_ctz(rest);
                 const bool seen = p <= pos && (p > pos - a.window || p < a.sinks);
-                const T* v = address(p, a.v, a.v_cache, a.ld_v);
+                const T* v = value(p);
 #pragma unroll
                 for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
@@ -426,23 +440,32 @@ __global__ __launch_bounds__(kAttnThreads) void window_step_join_kernel(AttnArgs
     const int lane = threadIdx.x % kWave;
     if (at >= (int64_t)a.requests * a.q_heads) return;
     const float* ml = a.part_ml + at * a.splits * 2;
+    const float* part = a.part_o + at * a.splits * a.dim;
+    // the largest of all shares, a share a lane
     float m = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, ml[2 * s]);
+    for (int s = lane; s < a.splits; s += kWave) m = fmaxf(m, ml[2 * s]);
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) m = fmaxf(m, __shfl_xor(m, x));
     const float base = m == -INFINITY ? 0.0f : m;
     float l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    const int d = 4 * lane;
-    for (int s = 0; s < a.splits; ++s) {
-        const float f = __builtin_amdgcn_exp2f(ml[2 * s] - base);
-        l = fmaf(ml[2 * s + 1], f, l);
-        if (d < a.dim) {
+    const int d = 4 * lane < a.dim ? 4 * lane : 0;
+    for (int s0 = 0; s0 < a.splits; s0 += kWave) {
+        const int n = a.splits - s0 < kWave ? a.splits - s0 : kWave;
+        const float f = lane < n ? __builtin_amdgcn_exp2f(ml[2 * (s0 + lane)] - base) : 0.0f;
+        l += lane < n ? f * ml[2 * (s0 + lane) + 1] : 0.0f;
+#pragma unroll 8
+        for (int s = 0; s < n; ++s) {
+            const float fs = __shfl(f, s);
             float v[4];
-            __builtin_memcpy(v, a.part_o + (at * a.splits + s) * a.dim + d, 16);
+            __builtin_memcpy(v, part + (int64_t)(s0 + s) * a.dim + d, 16);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], f, o[i]);
+            for (int i = 0; i < 4; ++i) o[i] = fmaf(v[i], fs, o[i]);
         }
     }
+#pragma unroll
+    for (int x = 1; x < kWave; x *= 2) l += __shfl_xor(l, x);
     const float scale = l == 0.0f ? 0.0f : 1.0f / l;
-    if (d < a.dim) put4(static_cast<T*>(a.y) + at * a.dim + d, o[0] * scale, o[1] * scale, o[2] * scale, o[3] * scale);
+    if (4 * lane < a.dim) put4(static_cast<T*>(a.y) + at * a.dim + d, o[0] * scale, o[1] * scale, o[2] * scale, o[3] * scale);
 }
 
 // ---------------------------------------------------------------------------

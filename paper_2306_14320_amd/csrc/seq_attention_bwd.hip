@@ -21,8 +21,6 @@
 namespace im2win {
 namespace {
 
-constexpr int kPiece = 512;        // queries whose sums for the first tokens' keys go together
-
 struct AttnBwdArgs {
     const void *dy, *q, *k, *v, *y;
     const float* lse;
@@ -32,7 +30,7 @@ struct AttnBwdArgs {
     int64_t ld_q, ld_k, ld_v;
     int64_t q_places, q_items, k_places, k_items, pieces;
     int q_heads, kv_heads, dim, window, sinks;
-    int pack, tile;
+    int pack, tile, piece;         // piece: queries whose sums for the first tokens' keys go together
     float c, scale;
 };
 
@@ -65,7 +63,7 @@ __device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int 
 
 template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 128 ? 64 : 32;
 template <typename T, int DP> constexpr int kDqWaves = DP * sizeof(T) > 256 ? 1 : 2;
-template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 192 ? 1 : 2;
+template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 128 ? 1 : 2;
 template <typename T, int DP> constexpr bool kBwdAhead = DP * sizeof(T) <= 256;
 
 // ---------------------------------------------------------------------------
@@ -75,7 +73,7 @@ template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_kernel(AttnBwdArgs a) {
     constexpr int BK = kTileRows<T, DP>, NB = BK / 32;
     using KV = Tile<T, DP, BK>;
-    static_assert(BK * KV::kChunks % kAttnThreads == 0, "whole rounds");
+    using St = Stage<T, DP, BK>;
     __shared__ __align__(16) char kt[KV::kBytes], vt[KV::kBytes];
     const int64_t item = die_order(blockIdx.x, a.q_items);
     if (item >= a.q_items) return;
@@ -110,19 +108,14 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
     const int wq0 = st.row + wave * kCols / a.pack;
     int wq1 = st.row + (wave * kCols + kCols - 1) / a.pack;
     wq1 = wq1 < last ? wq1 : last;
-    Chunk kr[KV::kPerThread], vr[KV::kPerThread];
+    const uint32_t sk = (uint32_t)a.ld_k * (uint32_t)sizeof(T), sv = (uint32_t)a.ld_v * (uint32_t)sizeof(T);
+    const uint32_t ok = St::offset(sk), ov = St::offset(sv);
+    const char* kp = reinterpret_cast<const char*>(static_cast<const T*>(a.k) + st.first * a.ld_k + (int64_t)kvh * a.dim);
+    const char* vp = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + st.first * a.ld_v + (int64_t)kvh * a.dim);
+    St kr, vr;
     auto fetch = [&](int base, int stop) {
-#pragma unroll
-        for (int i = 0; i < KV::kPerThread; ++i) {
-            const int n = tid + i * kAttnThreads, p = base + n / KV::kChunks, e = n % KV::kChunks * KV::kElems;
-            if (p < stop && e < a.dim) {
-                kr[i].load(static_cast<const T*>(a.k) + (int64_t)(st.first + p) * a.ld_k + (int64_t)kvh * a.dim + e);
-                vr[i].load(static_cast<const T*>(a.v) + (int64_t)(st.first + p) * a.ld_v + (int64_t)kvh * a.dim + e);
-            } else {
-                kr[i].zero();
-                vr[i].zero();
-            }
-        }
+        kr.fetch(kp + (int64_t)base * sk, ok, sk, stop - base, a.dim);
+        vr.fetch(vp + (int64_t)base * sv, ov, sv, stop - base, a.dim);
     };
     f32x16 o[DP / 32];
 #pragma unroll
@@ -133,12 +126,8 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
     while (base < stop) {
         if (!kBwdAhead<T, DP>) fetch(base, stop);
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < KV::kPerThread; ++i) {
-            const int n = tid + i * kAttnThreads, to = KV::at(n / KV::kChunks, n % KV::kChunks);
-            kr[i].store(kt + to);
-            vr[i].store(vt + to);
-        }
+        kr.put(kt);
+        vr.put(vt);
         __syncthreads();
         const int now = base, now_stop = stop;
         if (sink_tile) sink_tile = false, base = begin, stop = end;
@@ -255,7 +244,7 @@ template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_kernel(AttnBwdArgs a) {
     constexpr int BQ = kTileRows<T, DP>, NB = BQ / 32;
     using Q = Tile<T, DP, BQ>;
-    static_assert(BQ * Q::kChunks % kAttnThreads == 0, "whole rounds");
+    using St = Stage<T, DP, BQ>;
     __shared__ __align__(16) char qt[Q::kBytes], gt[Q::kBytes];
     __shared__ __align__(16) float lse[BQ], delta[BQ];
     const int64_t item = die_order(blockIdx.x, a.k_items);
@@ -275,69 +264,78 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
     // queries that see some key of the tile by the window
     const int begin = st.row, far = st.row + kGroupCols - 1 + a.window;
     const int end = far < st.len ? far : st.len;
-    const int tiles = (end - begin + BQ - 1) / BQ;
-    Chunk qr[Q::kPerThread], gr[Q::kPerThread];
+    const uint32_t sq = (uint32_t)a.ld_q * (uint32_t)sizeof(T), sg = (uint32_t)(a.q_heads * a.dim) * (uint32_t)sizeof(T);
+    const uint32_t oq = St::offset(sq), og = St::offset(sg);
+    const char* qp = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + st.first * a.ld_q + (int64_t)kvh * group * a.dim);
+    const char* gp = reinterpret_cast<const char*>(static_cast<const T*>(a.dy) + ((int64_t)st.first * a.q_heads + kvh * group) * a.dim);
+    St qr, gr;
     float lr = 0.0f, er = 0.0f;
-    auto fetch = [&](int n) {
-        const int head = kvh * group + n / tiles, base = begin + n % tiles * BQ;
-#pragma unroll
-        for (int i = 0; i < Q::kPerThread; ++i) {
-            const int m = tid + i * kAttnThreads, p = base + m / Q::kChunks, e = m % Q::kChunks * Q::kElems;
-            if (p < end && e < a.dim) {
-                qr[i].load(static_cast<const T*>(a.q) + (int64_t)(st.first + p) * a.ld_q + (int64_t)head * a.dim + e);
-                gr[i].load(static_cast<const T*>(a.dy) + ((int64_t)(st.first + p) * a.q_heads + head) * a.dim + e);
-            } else {
-                qr[i].zero();
-                gr[i].zero();
-            }
-        }
+    auto fetch = [&](int g, int base) {
+        const int64_t head = (int64_t)g * a.dim * (int)sizeof(T);
+        qr.fetch(qp + head + (int64_t)base * sq, oq, sq, end - base, a.dim);
+        gr.fetch(gp + head + (int64_t)base * sg, og, sg, end - base, a.dim);
         if (tid < BQ) {
-            const int64_t at = (int64_t)(st.first + base + tid) * a.q_heads + head;
+            const int64_t at = (int64_t)(st.first + base + tid) * a.q_heads + kvh * group + g;
             lr = base + tid < end ? a.lse[at] * kLog2e : 0.0f;
             er = base + tid < end ? a.delta[at] : 0.0f;
         }
     };
-    const int count = tiles * group;
-    if (kBwdAhead<T, DP>) fetch(0);
-    for (int n = 0; n < count; ++n) {
-        if (!kBwdAhead<T, DP>) fetch(n);
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < Q::kPerThread; ++i) {
-            const int m = tid + i * kAttnThreads, to = Q::at(m / Q::kChunks, m % Q::kChunks);
-            qr[i].store(qt + to);
-            gr[i].store(gt + to);
+    // the sums that the first tokens' pieces left: those of the sequence, added into the first of them
+    const int pieces_from = a.window / a.piece, pieces_to = (st.len + a.piece - 1) / a.piece;
+    const bool first_keys = a.sinks && st.row == 0 && st.len > a.window;
+    const int place = a.seq.starts ? st.first / a.piece + st.b : st.b * ((a.seq.len + a.piece - 1) / a.piece);
+    const int64_t sums = 2 * (int64_t)a.sinks * a.dim;
+    float* part = a.part + ((int64_t)(place + pieces_from) * a.kv_heads + kvh) * sums;
+    if (first_keys && pieces_to - pieces_from > 1) {
+        for (int n = tid; n < sums; n += kAttnThreads) {
+            float v = 0.0f;
+#pragma unroll 8
+            for (int z = 0; z < pieces_to - pieces_from; ++z) v += part[z * a.kv_heads * sums + n];
+            part[n] = v;
         }
+    }
+    // tiles of queries, one head after the other
+    int g = 0, base = begin;
+    if (kBwdAhead<T, DP>) fetch(g, base);
+    while (g < group) {
+        if (!kBwdAhead<T, DP>) fetch(g, base);
+        __syncthreads();
+        qr.put(qt);
+        gr.put(gt);
         if (tid < BQ) lse[tid] = lr, delta[tid] = er;
         __syncthreads();
-        if (kBwdAhead<T, DP> && n + 1 < count) fetch(n + 1);
-        const int base = begin + n % tiles * BQ;
+        const int now = base;
+        base += BQ;
+        if (base >= end) base = begin, ++g;
+        if (kBwdAhead<T, DP> && g < group) fetch(g, base);
+        auto seen = [&](int p) { return p < end && p >= key && p - key < a.window; };
+        auto single = [&](int p) { return p == 0 || (a.window == 1 && a.sinks == 0); };
+        // seen as a whole: the tile's blocks without a branch between them, one's products beside the other's exponentials, where registers suffice
+        const bool whole = now + BQ <= end && k1 <= now && now + BQ - 1 - k0 < a.window;
+        if (kDkvWaves<T, DP> == 1 && whole) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            const int p0 = base + 32 * b, p1 = p0 + 31;
-            if (p0 >= end || p1 < k0 || p0 - k1 >= a.window) continue;
-            const bool whole = p1 < end && k1 <= p0 && p1 - k0 < a.window;
-            keys.template take<BQ>(
-                qt, gt, lse, delta, b, base, whole, a.c, [&](int p) { return p < end && p >= key && p - key < a.window; },
-                [&](int p) { return p == 0 || (a.window == 1 && a.sinks == 0); });
+            for (int b = 0; b < NB; ++b) keys.template take<BQ>(qt, gt, lse, delta, b, now, true, a.c, seen, single);
+        } else {
+            for (int b = 0; b < NB; ++b) {
+                const int p0 = now + 32 * b, p1 = p0 + 31;
+                if (p0 >= end || p1 < k0 || p0 - k1 >= a.window) continue;
+                keys.template take<BQ>(qt, gt, lse, delta, b, now, whole, a.c, seen, single);
+            }
         }
     }
     // queries behind the window that see the first tokens
-    if (a.sinks && st.row == 0 && wave == 0 && key < a.sinks && st.len > a.window) {
-        const int from = a.window / kPiece, to = (st.len + kPiece - 1) / kPiece, place = st.first / kPiece + st.b;
-        for (int z = from; z < to; ++z) {
-            const float* p = a.part + (((int64_t)(a.seq.starts ? place : st.b * ((a.seq.len + kPiece - 1) / kPiece)) + z) * a.kv_heads + kvh) * 2 * a.sinks * a.dim + (int64_t)key * a.dim;
+    if (first_keys && wave == 0 && key < a.sinks) {
+        const float* p = part + (int64_t)key * a.dim;
 #pragma unroll
-            for (int d = 0; d < DP / 32; ++d)
+        for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int e = 32 * d + acc_row(i, half);
-                    if (e < a.dim) {
-                        keys.dk[d][i] += p[e];
-                        keys.dv[d][i] += p[(int64_t)a.sinks * a.dim + e];
-                    }
+            for (int i = 0; i < 16; ++i) {
+                const int e = 32 * d + acc_row(i, half);
+                if (e < a.dim) {
+                    keys.dk[d][i] += p[e];
+                    keys.dv[d][i] += p[(int64_t)a.sinks * a.dim + e];
                 }
-        }
+            }
     }
     if (!live) return;
     const int64_t to = ((int64_t)(st.first + key) * a.kv_heads + kvh) * a.dim;
@@ -354,7 +352,7 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
 
 // ---------------------------------------------------------------------------
 // The first tokens' keys and the queries that have left them behind their
-// window: a workgroup takes a piece of 512 queries for all heads of a key head,
+// window: a workgroup takes a piece of the queries for all heads of a key head,
 // each wave 32 queries at a time in its own part of LDS.
 // ---------------------------------------------------------------------------
 template <typename T, int DP> constexpr int kSinkOwn = 2 * Tile<T, DP, 32>::kBytes + 256;      // a wave's queries, gradients, lse and delta
@@ -371,9 +369,9 @@ __global__ __launch_bounds__((kSinkWaves<T, DP> * kWave), (kDkvWaves<T, DP>)) vo
     if (item >= a.pieces * a.kv_heads) return;
     const int kvh = (int)(item % a.kv_heads);
     const int place = (int)(item / a.kv_heads);
-    const SeqTile st = seq_tile(a.seq, place, kPiece);
+    const SeqTile st = seq_tile(a.seq, place, a.piece);
     const int tid = threadIdx.x, wave = uniform(tid / kWave), lane = tid % kWave, half = lane / 32;
-    const int end = st.row + kPiece < st.len ? st.row + kPiece : st.len;
+    const int end = st.row + a.piece < st.len ? st.row + a.piece : st.len;
     if (st.row >= st.len || end <= a.window) return;
     const int group = a.q_heads / a.kv_heads, key = lane % kCols;
     char *qt = stage + wave * kOwn, *gt = qt + Q::kBytes;
@@ -443,15 +441,19 @@ void with_type(int32_t dtype, F f) {
 
 // Pieces of queries that may see first tokens outside of their window: none
 // where no sequence can be longer than the window.
+int64_t piece_rows(const im2win_window_desc* d) {
+    const int64_t rows = (d->tokens * d->kv_heads / 1024 + 127) / 128 * 128;      // some 1024 workgroups, of whole rounds of their waves
+    return std::max<int64_t>(128, std::min<int64_t>(rows, 4096));
+}
 int64_t pieces_of(const im2win_window_desc* d, const int32_t* starts) {
     if (!d->sinks || d->tokens <= d->window) return 0;
     if (!starts && d->tokens / d->sequences <= d->window) return 0;
-    return seq_places(d->tokens, d->sequences, starts, kPiece);
+    return seq_places(d->tokens, d->sequences, starts, piece_rows(d));
 }
 // With and without seq_starts (whose places are never fewer): the query does not know.
 size_t bwd_bytes(const im2win_window_desc* d) {
     const size_t delta = ((size_t)(d->tokens * d->q_heads) * 4 + 15) / 16 * 16;
-    const int64_t pieces = d->sinks && d->tokens > d->window ? d->tokens / kPiece + d->sequences : 0;
+    const int64_t pieces = d->sinks && d->tokens > d->window ? d->tokens / piece_rows(d) + d->sequences : 0;
     return delta + (size_t)(pieces * d->kv_heads * 2 * d->sinks * d->head_dim) * 4;
 }
 
@@ -496,6 +498,7 @@ int im2win_window_attention_backward(const im2win_window_desc* d, const void* dy
     a.k_places = seq_places(d->tokens, d->sequences, seq_starts, kGroupCols);
     a.k_items = a.k_places * d->kv_heads;
     a.pieces = pieces_of(d, seq_starts);
+    a.piece = (int)piece_rows(d);
     a.delta = static_cast<float*>(workspace);
     a.part = reinterpret_cast<float*>(static_cast<char*>(workspace) + ((size_t)(d->tokens * d->q_heads) * 4 + 15) / 16 * 16);
     const int64_t gq = (a.q_items + 7) / 8 * 8, gk = (a.k_items + 7) / 8 * 8, gs = (a.pieces * d->kv_heads + 7) / 8 * 8;
