@@ -62,58 +62,73 @@ __device__ __forceinline__ void mma(f32x16& acc, const Frag<float>& a, const Fra
 __device__ __forceinline__ int acc_row(int i, int half) { return 8 * (i / 4) + 4 * half + i % 4; }
 
 // ---------------------------------------------------------------------------
-// A tile of R rows of DP elements in LDS, in 16-byte chunks whose place in the
-// row is changed by the row's number: eight neighbouring rows then lie in
-// different banks where a wave reads one chunk of each (scores), and four
-// neighbouring rows where it reads two chunks of each (transposed).
+// A tile of R rows of DP elements in LDS, in 16-byte chunks whose place among
+// eight (four, where the row's chunks are no multiple of eight) is changed by
+// the row's number: eight neighbouring rows then lie in different banks where a
+// wave reads one chunk of each (scores), and four neighbouring rows where it
+// reads two chunks of each (transposed).  A chunk's number splits into a part
+// of the lane's and a constant, so an address is the lane's base, one exclusive
+// or, and an immediate.
 // ---------------------------------------------------------------------------
 template <typename T, int DP, int R>
 struct Tile {
     static constexpr int kElems = 16 / sizeof(T);
     static constexpr int kChunks = DP / kElems;             // of a row
-    static constexpr int kBytes = R * DP * (int)sizeof(T);
+    static constexpr int kRow = DP * (int)sizeof(T);        // bytes
+    static constexpr int kBytes = R * kRow;
+    static constexpr int kMask = kChunks % 8 == 0 ? 7 : 3;
+    static_assert(kChunks % 4 == 0, "whole groups of chunks");
 
     static __device__ __forceinline__ int turn(int row) {
-        if constexpr (kChunks % 8 == 0) return (row & 3) << 1 | (row >> 2 & 1);
+        if constexpr (kMask == 7) return (row & 3) << 1 | (row >> 2 & 1);
         else return (row >> 1 & 1) << 1 | (row >> 2 & 1);
     }
-    static __device__ __forceinline__ int at(int row, int chunk) { return (row * kChunks + (chunk ^ turn(row))) * 16; }
+    static __device__ __forceinline__ int at(int row, int chunk) { return row * kRow + (chunk ^ turn(row)) * 16; }
 
-    // The left operand for products over the row's elements: row `row`, elements 16 s + 8 half ..
-    static __device__ __forceinline__ Frag<T> row_frag(const char* lds, int row, int s, int half) {
+    // The left operand for products over the row's elements: row lane % 32 of
+    // block `block`, elements 16 s + 8 (lane / 32) ..
+    static __device__ __forceinline__ int row_base(int lane) {
+        const int row = lane % 32, half = lane / 32;
+        return row * kRow + (turn(row) ^ (sizeof(T) == 2 ? half : 2 * half)) * 16;
+    }
+    static __device__ __forceinline__ Frag<T> row_frag(const char* lds, int base, int block, int s) {
         Frag<T> f;
         if constexpr (sizeof(T) == 2) {
-            f.load(lds + at(row, 2 * s + half));
+            f.load(lds + (base ^ (2 * s & kMask) * 16) + (2 * s & ~kMask) * 16 + block * 32 * kRow);
         } else {
-            __builtin_memcpy(f.v, lds + at(row, 4 * s + 2 * half), 16);
-            __builtin_memcpy(f.v + 4, lds + at(row, 4 * s + 2 * half + 1), 16);
+            __builtin_memcpy(f.v, lds + (base ^ (4 * s & kMask) * 16) + (4 * s & ~kMask) * 16 + block * 32 * kRow, 16);
+            __builtin_memcpy(f.v + 4, lds + (base ^ ((4 * s + 1) & kMask) * 16) + (4 * s & ~kMask) * 16 + block * 32 * kRow, 16);
         }
         return f;
     }
     // The left operand for products over rows: element 32 dt + lane % 32 of the
-    // rows 16 s + 8 (j / 4) + 4 half + j % 4.  In bf16 the LDS turns blocks of
-    // four rows by 16 elements for 16 lanes: lane l of them names row l / 4,
+    // rows 16 s + 8 (j / 4) + 4 (lane / 32) + j % 4.  In bf16 the LDS turns blocks
+    // of four rows by 16 elements for 16 lanes: lane l of them names row l / 4,
     // elements 4 (l % 4) .., and receives element l of the four rows.
-    static __device__ __forceinline__ Frag<T> col_frag(const char* lds, int dt, int s, int lane) {
-        Frag<T> f;
+    static __device__ __forceinline__ int col_base(int lane) {
         const int half = lane / 32;
         if constexpr (sizeof(T) == 2) {
-            const int l = lane % 16, row = 16 * s + 4 * half + l / 4;
-            const int e = 32 * dt + lane / 16 % 2 * 16 + 4 * (l % 4);
+            const int l = lane % 16, row = 4 * half + l / 4;
+            return row * kRow + (turn(row) ^ (lane / 16 % 2 * 2 + l % 4 / 2)) * 16 + l % 2 * 8;
+        } else {
+            return 4 * half * kRow + (turn(4 * half) ^ (lane % 32 / 4)) * 16 + lane % 4 * 4;
+        }
+    }
+    static __device__ __forceinline__ Frag<T> col_frag(const char* lds, int base, int dt, int s) {
+        Frag<T> f;
+        if constexpr (sizeof(T) == 2) {
+            const char* p = lds + (base ^ (4 * dt & kMask) * 16) + (4 * dt & ~kMask) * 16 + 16 * s * kRow;
             union {
                 s16x4 h[2];
                 bf16x8 v;
             } u;
-            u.h[0] = turned(lds + at(row, e / 8) + e % 8 * 2);
-            u.h[1] = turned(lds + at(row + 8, e / 8) + e % 8 * 2);
+            u.h[0] = turned(p);
+            u.h[1] = turned(p + 8 * kRow);
             f.v = u.v;
         } else {
-            const int e = 32 * dt + lane % 32;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int row = 16 * s + 8 * (j / 4) + 4 * half + j % 4;
-                f.v[j] = *reinterpret_cast<const float*>(lds + at(row, e / 4) + e % 4 * 4);
-            }
+            for (int j = 0; j < 8; ++j)      // turn(4 half + j % 4) = turn(4 half) ^ 2 (j % 4)
+                f.v[j] = *reinterpret_cast<const float*>(lds + (base ^ (j % 4) * 32) + 8 * dt * 16 + (16 * s + 8 * (j / 4) + j % 4) * kRow);
         }
         return f;
     }
@@ -134,68 +149,97 @@ struct Chunk {
 };
 
 // ---------------------------------------------------------------------------
-// A tile's way from rows in memory to LDS, 16 bytes a thread and pass, through
-// registers in which the loads stay in flight.  Threads side by side take a
-// row's chunks (their number rounded up to a power of two, so that a thread's
-// place in its row is the same in every pass and its address one 32-bit offset
-// beside a scalar one).
+// A tile's way from rows in memory to LDS: copied by the memory pipeline
+// itself, 16 bytes a lane, without registers.  A lane's place in LDS is fixed
+// (64 lanes side by side), so it fetches the chunk that belongs there.
 // ---------------------------------------------------------------------------
-constexpr int64_t kMaxAttnStride = int64_t(1) << 24;      // 64 rows of bf16 or 32 of fp32 within 32 bits of bytes
+constexpr int64_t kMaxAttnStride = int64_t(1) << 24;      // a tile's 64 rows of bf16 or 32 of fp32 within 32 bits of bytes
+
+// The wave's own copies have arrived, and then everyone's.
+__device__ __forceinline__ void arrived() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
 
 template <typename T, int DP, int R>
-struct Stage {
+struct Feed {
     using Lds = Tile<T, DP, R>;
-    static constexpr int up(int n) { return n <= 4 ? 4 : n <= 8 ? 8 : n <= 16 ? 16 : n <= 32 ? 32 : 64; }
-    static constexpr int kLanes = up(Lds::kChunks), kPassRows = kAttnThreads / kLanes, kPasses = R / kPassRows;
-    static_assert(kPasses >= 1 && R % kPassRows == 0, "whole passes");
-    Chunk c[kPasses];
+    static constexpr int kPasses = R * Lds::kChunks / kAttnThreads;
+    static_assert(R * Lds::kChunks % kAttnThreads == 0, "whole passes");
+    // where a pass is a multiple of eight rows, a lane's chunk is the same in all of them
+    static constexpr bool kSame = kAttnThreads % (8 * Lds::kChunks) == 0;
+    static constexpr int kPassRows = kAttnThreads / Lds::kChunks;
 
-    static __device__ __forceinline__ int row() { return (int)threadIdx.x / kLanes; }
-    static __device__ __forceinline__ int chunk() { return (int)threadIdx.x % kLanes; }
-    static __device__ __forceinline__ bool inside(int dim) { return chunk() * Lds::kElems < dim; }      // the chunk holds channels
-    // Bytes from the tile's first row to the thread's first chunk, for rows `stride` bytes apart
-    static __device__ __forceinline__ uint32_t offset(uint32_t stride) { return (uint32_t)row() * stride + (uint32_t)chunk() * 16; }
+    static __device__ __forceinline__ int row(int i) { return ((int)threadIdx.x + i * kAttnThreads) / Lds::kChunks; }
+    static __device__ __forceinline__ int chunk(int i) { return ((int)threadIdx.x + i * kAttnThreads) % Lds::kChunks ^ Lds::turn(row(i)); }
 
-    // `valid` of the tile's rows exist (all where at least R), the first at p; the others, and channels behind dim, are zeros
-    __device__ __forceinline__ void fetch(const char* p, uint32_t offset, uint32_t stride, int valid, int dim) {
-        if (valid >= R && (Lds::kChunks * Lds::kElems == dim && Lds::kChunks == kLanes)) {
+    uint32_t offset[kSame ? 1 : kPasses], stride;
+    __device__ __forceinline__ explicit Feed(int64_t elements) {
+        stride = (uint32_t)elements * (uint32_t)sizeof(T);
 #pragma unroll
-            for (int i = 0; i < kPasses; ++i) {
-                c[i].load(p + offset);
-                p += (int64_t)kPassRows * stride;
-            }
-        } else {
-            const bool in = inside(dim);
-#pragma unroll
-            for (int i = 0; i < kPasses; ++i) {
-                if (in && row() + i * kPassRows < valid) c[i].load(p + offset);
-                else c[i].zero();
-                p += (int64_t)kPassRows * stride;
-            }
-        }
+        for (int i = 0; i < (kSame ? 1 : kPasses); ++i) offset[i] = (uint32_t)row(i) * stride + (uint32_t)chunk(i) * 16;
     }
-    __device__ __forceinline__ void put(char* lds) const {
-        if (Lds::kChunks == kLanes || chunk() < Lds::kChunks) {
+    static __device__ __forceinline__ void copy(const void* from, char* lds, int i) {
+        typedef __attribute__((address_space(3))) void lds_void;
+        char* to = lds + (uniform((int)threadIdx.x / kWave) * kWave + i * kAttnThreads) * 16;
+        __builtin_amdgcn_global_load_lds(from, (lds_void*)(to), 16, 0, 0);
+    }
+    // The tile's first row is at p and `valid` rows exist (1 at least): behind
+    // them the last one is repeated.  Channels behind dim are left alone.
+    __device__ __forceinline__ void issue(char* lds, const char* p, int valid, int dim) const {
+        if (valid >= R && dim == DP) {
 #pragma unroll
-            for (int i = 0; i < kPasses; ++i) c[i].store(lds + Lds::at(row() + i * kPassRows, chunk()));
+            for (int i = 0; i < kPasses; ++i) copy(p + (kSame ? (int64_t)(i * kPassRows) * stride : 0) + offset[kSame ? 0 : i], lds, i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPasses; ++i) {
+                const int r = row(i) < valid ? row(i) : valid - 1;
+                if (chunk(i) * Lds::kElems < dim) copy(p + (int64_t)r * stride + chunk(i) * 16, lds, i);
+            }
         }
     }
 };
 
-// Zeroes the infinities and NaN among a chunk's elements; whether there were any.
+// Zeroes LDS whose channels behind dim no copy writes
+__device__ __forceinline__ void clear(char* lds, int bytes) {
+    Chunk z;
+    z.zero();
+    for (int i = threadIdx.x * 16; i < bytes; i += kAttnThreads * 16) z.store(lds + i);
+    __syncthreads();
+}
+
+// The sum, or the largest, of both halves' values
+__device__ __forceinline__ float half_sum(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float half_max(float v) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Whether a chunk holds an infinity or a NaN (an exponent of ones carries over when one is added)
 template <typename T>
-__device__ __forceinline__ bool drop_nonfinite(Chunk& c) {
-    bool any = false;
+__device__ __forceinline__ bool nonfinite(const Chunk& c) {
+    uint32_t any = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        any |= sizeof(T) == 4 ? (c.u[i] & 0x7f800000u) + 0x00800000u : (c.u[i] & 0x7f807f80u) + 0x00800080u;
+    return any & (sizeof(T) == 4 ? 0x80000000u : 0x80008000u);
+}
+
+// Zeroes the infinities and NaN among a chunk's elements
+template <typename T>
+__device__ __forceinline__ void drop_nonfinite(Chunk& c) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if constexpr (sizeof(T) == 4) {
-            if ((c.u[i] & 0x7f800000u) == 0x7f800000u) c.u[i] = 0, any = true;
+            if ((c.u[i] & 0x7f800000u) == 0x7f800000u) c.u[i] = 0;
         } else {
-            if ((c.u[i] & 0x7f80u) == 0x7f80u) c.u[i] &= 0xffff0000u, any = true;
-            if ((c.u[i] & 0x7f800000u) == 0x7f800000u) c.u[i] &= 0x0000ffffu, any = true;
+            if ((c.u[i] & 0x7f80u) == 0x7f80u) c.u[i] &= 0xffff0000u;
+            if ((c.u[i] & 0x7f800000u) == 0x7f800000u) c.u[i] &= 0x0000ffffu;
         }
     }
-    return any;
 }
 
 // ---------------------------------------------------------------------------

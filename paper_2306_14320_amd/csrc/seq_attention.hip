@@ -58,7 +58,9 @@ struct Running {
 };
 
 // Takes NB blocks of 32 masked scores (raw products) into the running softmax
-// and leaves the weights in their place.
+// and leaves the weights in their place.  The base of the exponentials, m, need
+// not be the largest score: it is moved where a score passes it by more than
+// 2^8, so that most tiles leave the sums as they are.
 template <int DP, int NB>
 __device__ __forceinline__ void soften(Running<DP>& r, f32x16 (&s)[NB], float c) {
     float top = s[0][0];
@@ -66,16 +68,16 @@ __device__ __forceinline__ void soften(Running<DP>& r, f32x16 (&s)[NB], float c)
     for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float m = fmaxf(r.m, top * c);
-    const float base = m == -INFINITY ? 0.0f : m;        // a column that has seen no key yet
-    if (__ballot(m > r.m)) {
-        const float a = __builtin_amdgcn_exp2f(r.m - base);
+    top = half_max(top) * c;
+    if (__ballot(top > r.m + 8.0f)) {
+        const float m = top > r.m + 8.0f ? top : r.m;
+        const float a = __builtin_amdgcn_exp2f(r.m - (m == -INFINITY ? 0.0f : m));      // 0 in a column that has seen no key yet
+        r.m = m;
         r.l *= a;
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t) r.o[t] *= a;
     }
-    r.m = m;
+    const float base = r.m == -INFINITY ? 0.0f : r.m;
     float sum = 0.0f;
 #pragma unroll
     for (int b = 0; b < NB; ++b)
@@ -108,26 +110,23 @@ __device__ __forceinline__ void put4(bf16* p, float a, float b, float c, float d
 }
 
 template <typename T, int DP> constexpr int kTileKeys = sizeof(T) == 2 && DP <= 128 ? 64 : 32;
-// Waves a SIMD: two, of 256 registers, up to 384 bytes of a head's row but for
-// 192 bf16 channels, whose accumulators do not fit beside the queries; else one.
+// Waves a SIMD: two, of 256 registers, where the queries' and outputs' fit; else one.
 template <typename T, int DP> constexpr int kFwdWaves = DP * sizeof(T) > 384 || DP >= 192 ? 1 : 2;
-// Whether the next tile's rows wait in registers while one is worked on.  Beside
-// 1 KB of queries and outputs a lane they would spill.
-template <typename T, int DP> constexpr bool kFwdAhead = DP * sizeof(T) <= 512;
+// Whether the step's next rows wait in registers while some are worked on
 template <typename T, int DP> constexpr bool kStepAhead = DP * sizeof(T) <= 256;
 
 // ---------------------------------------------------------------------------
 // Prompts and training: a workgroup takes up to 128 columns, the queries of
 // `tile` rows for `pack` heads that share keys and values.  Their tiles pass
-// through LDS, the next one's loads in flight while one is worked on.
+// through LDS, the next one's copies under way while one is worked on.
 // ---------------------------------------------------------------------------
 template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_attention_kernel(AttnArgs a) {
     constexpr int BK = kTileKeys<T, DP>, NB = BK / 32;
     using KV = Tile<T, DP, BK>;
-    using St = Stage<T, DP, BK>;
-    __shared__ __align__(16) char kt[KV::kBytes], vt[KV::kBytes];
-    __shared__ uint32_t flags[2];      // rows of the tile whose values are not all finite
+    using Copy = Feed<T, DP, BK>;
+    __shared__ __align__(128) char lds[4 * KV::kBytes];      // two buffers of keys, then two of values
+    __shared__ uint32_t flags[2][2];      // rows of a buffer whose values are not all finite
     const int64_t item = die_order(blockIdx.x, a.items);
     if (item >= a.items) return;
     const int hb = (int)(item / a.places);
@@ -169,61 +168,71 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
 
     // the value or key rows of the call, from position `past` on, and those of the cache
     auto cached = [&](int p) { return ((slot * rows + ring(p, a.window, a.sinks)) * a.kv_heads + kvh) * a.dim; };
-    const uint32_t sk = (uint32_t)a.ld_k * (uint32_t)sizeof(T), sv = (uint32_t)a.ld_v * (uint32_t)sizeof(T);
-    const uint32_t ok = St::offset(sk), ov = St::offset(sv);
+    const Copy ck(a.ld_k), cv(a.ld_v);
     const char* kn = reinterpret_cast<const char*>(static_cast<const T*>(a.k) + st.first * a.ld_k + (int64_t)kvh * a.dim);
     const char* vn = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + st.first * a.ld_v + (int64_t)kvh * a.dim);
     auto value = [&](int p) {
-        return p < past ? static_cast<const T*>(a.v_cache) + cached(p) : reinterpret_cast<const T*>(vn + (int64_t)(p - past) * sv);
+        return p < past ? static_cast<const T*>(a.v_cache) + cached(p) : reinterpret_cast<const T*>(vn + (int64_t)(p - past) * cv.stride);
     };
-    St kr, vr;
-    auto fetch = [&](int base, int stop) {
+    auto issue = [&](int buffer, int base, int stop) {
+        char *kt = lds + buffer * KV::kBytes, *vt = lds + (2 + buffer) * KV::kBytes;
         if (base >= past) {
-            kr.fetch(kn + (int64_t)(base - past) * sk, ok, sk, stop - base, a.dim);
-            vr.fetch(vn + (int64_t)(base - past) * sv, ov, sv, stop - base, a.dim);
+            ck.issue(kt, kn + (int64_t)(base - past) * ck.stride, stop - base, a.dim);
+            cv.issue(vt, vn + (int64_t)(base - past) * cv.stride, stop - base, a.dim);
             return;
         }
-        const int e = St::chunk() * KV::kElems;
 #pragma unroll
-        for (int i = 0; i < St::kPasses; ++i) {
-            const int p = base + St::row() + i * St::kPassRows;
-            if (p < stop && e < a.dim) {
-                const T* k = p < past ? static_cast<const T*>(a.k_cache) + cached(p) : reinterpret_cast<const T*>(kn + (int64_t)(p - past) * sk);
-                kr.c[i].load(k + e);
-                vr.c[i].load(value(p) + e);
-            } else {
-                kr.c[i].zero();
-                vr.c[i].zero();
-            }
+        for (int i = 0; i < Copy::kPasses; ++i) {
+            const int n = base + Copy::row(i), p = n < stop ? n : stop - 1, e = Copy::chunk(i) * KV::kElems;
+            if (e >= a.dim) continue;
+            const T* k = p < past ? static_cast<const T*>(a.k_cache) + cached(p) : reinterpret_cast<const T*>(kn + (int64_t)(p - past) * ck.stride);
+            Copy::copy(k + e, kt, i);
+            Copy::copy(value(p) + e, vt, i);
         }
     };
 
+    const int rb = KV::row_base(lane), cb = KV::col_base(lane);
     Running<DP> r;
-    bool sink_tile = first_end > 0;
-    int base = sink_tile ? 0 : begin, stop = sink_tile ? first_end : end;
+    if (a.dim != DP) clear(lds, 4 * KV::kBytes);
+    if (tid < 4) flags[tid / 2][tid % 2] = 0;
+    bool sinks_now = first_end > 0;
+    int base = sinks_now ? 0 : begin, stop = sinks_now ? first_end : end, buffer = 0;
     if (!served) base = stop = end;
-    if (kFwdAhead<T, DP> && base < stop) fetch(base, stop);
+    if (base < stop) issue(0, base, stop);
     while (base < stop) {
-        if (!kFwdAhead<T, DP>) fetch(base, stop);
-        // a tile that some column does not see all of: its values' infinities and NaN stay out of the product
-        const bool partial = base + BK > stop || base + BK - 1 > qfirst || base <= qlast - a.window;
-        __syncthreads();
-        if (tid < 2) flags[tid] = 0;
-        __syncthreads();
-        if (partial) {
-#pragma unroll
-            for (int i = 0; i < St::kPasses; ++i) {
-                const int rw = St::row() + i * St::kPassRows;
-                if (drop_nonfinite<T>(vr.c[i])) atomicOr(&flags[rw / 32], 1u << rw % 32);
-            }
-        }
-        kr.put(kt);
-        vr.put(vt);
-        __syncthreads();
+        arrived();
         const int now = base, now_stop = stop;
-        if (sink_tile) sink_tile = false, base = begin, stop = end;
+        const bool sink_tile = sinks_now;
+        if (sinks_now) sinks_now = false, base = begin, stop = end;
         else base += BK;
-        if (kFwdAhead<T, DP> && base < stop) fetch(base, stop);
+        // a tile that some column does not see all of: its values' infinities and NaN stay out of the product
+        if (now + BK > now_stop || now + BK - 1 > qfirst || now <= qlast - a.window) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < Copy::kPasses; ++i) {
+                Chunk c;
+                c.load(lds + (2 + buffer) * KV::kBytes + (tid + i * kAttnThreads) * 16);
+                bad |= nonfinite<T>(c);
+            }
+            if (bad) {
+#pragma unroll
+                for (int i = 0; i < Copy::kPasses; ++i) {
+                    char* to = lds + (2 + buffer) * KV::kBytes + (tid + i * kAttnThreads) * 16;
+                    Chunk c;
+                    c.load(to);
+                    if (!nonfinite<T>(c)) continue;
+                    drop_nonfinite<T>(c);
+                    c.store(to);
+                    atomicOr(&flags[buffer][Copy::row(i) / 32], 1u << Copy::row(i) % 32);
+                }
+            }
+            __syncthreads();
+        }
+        if (tid < 2) flags[buffer ^ 1][tid] = 0;      // read before the last barrier
+        if (base < stop) issue(buffer ^ 1, base, stop);
+        const int kb = rb + buffer * KV::kBytes, vb = cb + (2 + buffer) * KV::kBytes;
+        const int current = buffer;
+        buffer ^= 1;
         // keys in front of the wave's first window (but for sinks) or behind its last query
         if (now > wq1 || (now + BK <= wq0 - a.window + 1 && now >= a.sinks)) continue;
 
@@ -233,17 +242,27 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d)
 #pragma unroll
-            for (int b = 0; b < NB; ++b) mma(s[b], KV::row_frag(kt, 32 * b + lane % 32, d, half), q[d]);
-        const bool whole = now + BK <= now_stop && now + BK - 1 <= wq0 && now > wq1 - a.window;
-        if (!whole) {
+            for (int b = 0; b < NB; ++b) mma(s[b], KV::row_frag(lds, kb, b, d), q[d]);
+        if (sink_tile) {                // all of them seen, by all
+            const int n = now_stop - 4 * half;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = 32 * b + acc_row(i, 0) < n ? s[b][i] : -INFINITY;
+        } else if (now < a.sinks) {     // the sequence's first keys
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int p = now + 32 * b + acc_row(i, half);
-                    const bool seen = p < now_stop && p <= pos && (p > pos - a.window || p < a.sinks);
-                    s[b][i] = seen ? s[b][i] : -INFINITY;
+                    s[b][i] = p <= pos && (p > pos - a.window || p < a.sinks) ? s[b][i] : -INFINITY;
                 }
+        } else if (!(now + BK - 1 <= wq0 && now > wq1 - a.window)) {      // pos - window < p <= pos
+            const int low = pos - a.window + 1 - now - 4 * half;
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = (uint32_t)(32 * b + acc_row(i, 0) - low) < (uint32_t)a.window ? s[b][i] : -INFINITY;
         }
         soften<DP, NB>(r, s, a.c);
 #pragma unroll
@@ -252,12 +271,13 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
             for (int part = 0; part < 2; ++part) {
                 const Frag<T> w = weights<T>(s[b], part);
 #pragma unroll
-                for (int t = 0; t < DP / 32; ++t) mma(r.o[t], KV::col_frag(vt, t, 2 * b + part, lane), w);
+                for (int t = 0; t < DP / 32; ++t) mma(r.o[t], KV::col_frag(lds, vb, t, 2 * b + part), w);
             }
         // what was kept out of the product: a column that sees such a value has it
         for (int f = 0; f < NB; ++f)
-            for (uint32_t rest = uniform(flags[f]); rest; rest &= rest - 1) {
+            for (uint32_t rest = uniform(flags[current][f]); rest; rest &= rest - 1) {
                 const int p = now + 32 * f + __builtin_ctz(rest);
+                if (p >= now_stop) continue;      // the last row again
                 const bool seen = p <= pos && (p > pos - a.window || p < a.sinks);
                 const T* v = value(p);
 #pragma unroll
@@ -269,7 +289,7 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
                     }
             }
     }
-    const float l = r.l + __shfl_xor(r.l, 32);
+    const float l = half_sum(r.l);
     if (!live) return;
     const float scale = l == 0.0f ? 0.0f : 1.0f / l;      // without a visible key: zeros
     const int64_t t = st.first + row;
@@ -336,6 +356,7 @@ __global__ __launch_bounds__(kAttnThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void 
     const T* kn = static_cast<const T*>(a.k) + b * a.ld_k + (int64_t)kvh * a.dim;
     const T* vn = static_cast<const T*>(a.v) + b * a.ld_v + (int64_t)kvh * a.dim;
     char* mine = stage + wave * a.stage;
+    const int cb = V::col_base(lane);
 
     Frag<T> q[DP / 16];
     const T* qp = static_cast<const T*>(a.q) + b * a.ld_q + (int64_t)head * a.dim;
@@ -396,12 +417,12 @@ __global__ __launch_bounds__(kAttnThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void 
         for (int part = 0; part < 2; ++part) {
             const Frag<T> w = weights<T>(s[0], part);
 #pragma unroll
-            for (int t = 0; t < DP / 32; ++t) mma(r.o[t], V::col_frag(mine, t, part, lane), w);
+            for (int t = 0; t < DP / 32; ++t) mma(r.o[t], V::col_frag(mine, cb, t, part), w);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     // the four waves' shares: a channel's row of columns each, and their statistics
-    r.l += __shfl_xor(r.l, 32);
+    r.l = half_sum(r.l);
     float* o = reinterpret_cast<float*>(mine);
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)

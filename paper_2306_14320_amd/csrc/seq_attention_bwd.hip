@@ -64,7 +64,6 @@ __device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int 
 template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 128 ? 64 : 32;
 template <typename T, int DP> constexpr int kDqWaves = DP * sizeof(T) > 256 ? 1 : 2;
 template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 128 ? 1 : 2;
-template <typename T, int DP> constexpr bool kBwdAhead = DP * sizeof(T) <= 256;
 
 // ---------------------------------------------------------------------------
 // dq and delta: workgroups and columns as in the forward kernel
@@ -73,8 +72,8 @@ template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_kernel(AttnBwdArgs a) {
     constexpr int BK = kTileRows<T, DP>, NB = BK / 32;
     using KV = Tile<T, DP, BK>;
-    using St = Stage<T, DP, BK>;
-    __shared__ __align__(16) char kt[KV::kBytes], vt[KV::kBytes];
+    using Copy = Feed<T, DP, BK>;
+    __shared__ __align__(128) char lds[4 * KV::kBytes];      // two buffers of keys, then two of values
     const int64_t item = die_order(blockIdx.x, a.q_items);
     if (item >= a.q_items) return;
     const int hb = (int)(item / a.q_places);
@@ -98,8 +97,7 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
 #pragma unroll
         for (int i = 0; i < 8; ++i) delta = fmaf(g[s].get(i), y.get(i), delta);
     }
-    delta += __shfl_xor(delta, 32);
-    if (live && half == 0) a.delta[at] = delta;
+    delta = half_sum(delta);
     const float lse = a.lse[at] * kLog2e;
     const bool single = pos == 0 || (a.window == 1 && a.sinks == 0);
 
@@ -108,59 +106,72 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
     const int wq0 = st.row + wave * kCols / a.pack;
     int wq1 = st.row + (wave * kCols + kCols - 1) / a.pack;
     wq1 = wq1 < last ? wq1 : last;
-    const uint32_t sk = (uint32_t)a.ld_k * (uint32_t)sizeof(T), sv = (uint32_t)a.ld_v * (uint32_t)sizeof(T);
-    const uint32_t ok = St::offset(sk), ov = St::offset(sv);
+    const Copy ck(a.ld_k), cv(a.ld_v);
     const char* kp = reinterpret_cast<const char*>(static_cast<const T*>(a.k) + st.first * a.ld_k + (int64_t)kvh * a.dim);
     const char* vp = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + st.first * a.ld_v + (int64_t)kvh * a.dim);
-    St kr, vr;
-    auto fetch = [&](int base, int stop) {
-        kr.fetch(kp + (int64_t)base * sk, ok, sk, stop - base, a.dim);
-        vr.fetch(vp + (int64_t)base * sv, ov, sv, stop - base, a.dim);
+    auto issue = [&](int buffer, int base, int stop) {
+        ck.issue(lds + buffer * KV::kBytes, kp + (int64_t)base * ck.stride, stop - base, a.dim);
+        cv.issue(lds + (2 + buffer) * KV::kBytes, vp + (int64_t)base * cv.stride, stop - base, a.dim);
     };
+    const int rb = KV::row_base(lane), cb = KV::col_base(lane);
     f32x16 o[DP / 32];
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) o[i] = f32x16{};
-    bool sink_tile = first_end > 0;
-    int base = sink_tile ? 0 : begin, stop = sink_tile ? first_end : end;
-    if (kBwdAhead<T, DP>) fetch(base, stop);
+    if (a.dim != DP) clear(lds, 4 * KV::kBytes);
+    bool sinks_now = first_end > 0;
+    int base = sinks_now ? 0 : begin, stop = sinks_now ? first_end : end, buffer = 0;
+    float rest = 0.0f;
+    issue(0, base, stop);
     while (base < stop) {
-        if (!kBwdAhead<T, DP>) fetch(base, stop);
-        __syncthreads();
-        kr.put(kt);
-        vr.put(vt);
-        __syncthreads();
+        arrived();
         const int now = base, now_stop = stop;
-        if (sink_tile) sink_tile = false, base = begin, stop = end;
+        const bool sink_tile = sinks_now;
+        if (sinks_now) sinks_now = false, base = begin, stop = end;
         else base += BK;
-        if (kBwdAhead<T, DP> && base < stop) fetch(base, stop);
+        if (base < stop) issue(buffer ^ 1, base, stop);
+        const int kb = rb + buffer * KV::kBytes, kc = cb + buffer * KV::kBytes, vb = rb + (2 + buffer) * KV::kBytes;
+        buffer ^= 1;
         if (now > wq1 || (now + BK <= wq0 - a.window + 1 && now >= a.sinks)) continue;
-        const bool whole = now + BK <= now_stop && now + BK - 1 <= wq0 && now > wq1 - a.window;
+        const bool whole = !sink_tile && now >= a.sinks && now + BK - 1 <= wq0 && now > wq1 - a.window;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             f32x16 s = {}, dp = {};
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) {
-                mma(s, KV::row_frag(kt, 32 * b + lane % 32, d, half), q[d]);
-                mma(dp, KV::row_frag(vt, 32 * b + lane % 32, d, half), g[d]);
+                mma(s, KV::row_frag(lds, kb, b, d), q[d]);
+                mma(dp, KV::row_frag(lds, vb, b, d), g[d]);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -lse)) * (dp[i] - delta);
             if (!whole) {
+                const int low = pos - a.window + 1 - now - 4 * half, high = now_stop - now - 4 * half;
+                if (sink_tile) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int p = now + 32 * b + acc_row(i, half);
-                    const bool seen = p < now_stop && p <= pos && (p > pos - a.window || p < a.sinks) && !single;
-                    s[i] = seen ? s[i] : 0.0f;
+                    for (int i = 0; i < 16; ++i) s[i] = 32 * b + acc_row(i, 0) < high ? s[i] : 0.0f;
+                } else if (now >= a.sinks) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) s[i] = (uint32_t)(32 * b + acc_row(i, 0) - low) < (uint32_t)a.window && !single ? s[i] : 0.0f;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int p = now + 32 * b + acc_row(i, half);
+                        s[i] = p <= pos && (p > pos - a.window || p < a.sinks) && !single ? s[i] : 0.0f;
+                    }
                 }
             }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) rest += s[i];
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
                 const Frag<T> w = operand<T>(s, part);
 #pragma unroll
-                for (int d = 0; d < DP / 32; ++d) mma(o[d], KV::col_frag(kt, d, 2 * b + part, lane), w);
+                for (int d = 0; d < DP / 32; ++d) mma(o[d], KV::col_frag(lds, kc, d, 2 * b + part), w);
             }
         }
     }
+    // ds sums to zero over the keys: what it sums to is what delta is off by, from the rounded y
+    rest = half_sum(rest);
+    if (live && half == 0) a.delta[at] = delta + rest;
     if (!live) return;
     T* dq = static_cast<T*>(a.dq) + at * a.dim;
 #pragma unroll
@@ -181,6 +192,7 @@ template <typename T, int DP>
 struct Keys {
     Frag<T> k[DP / 16], v[DP / 16];
     f32x16 dk[DP / 32], dv[DP / 32];
+    int rb, cb;                  // the lane's places in a tile
 
     __device__ __forceinline__ void load(const T* kp, const T* vp, int half, int dim, bool live) {
 #pragma unroll
@@ -195,18 +207,21 @@ struct Keys {
         }
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d) dk[d] = dv[d] = f32x16{};
+        rb = Tile<T, DP, 32>::row_base(threadIdx.x % kWave);
+        cb = Tile<T, DP, 32>::col_base(threadIdx.x % kWave);
     }
     // seen(position) for the lane's key, and single(position), where the block
-    // is not seen as a whole; lse and delta are the block's rows' in LDS.
+    // is not seen as a whole; qt and gt are the tiles' places in LDS, lse and delta
+    // their rows' there.
     template <int R, typename F, typename G>
-    __device__ __forceinline__ void take(const char* qt, const char* gt, const float* lse, const float* delta, int b, int base, bool whole, float c, F seen, G single) {
+    __device__ __forceinline__ void take(const char* lds, int qt, int gt, const float* lse, const float* delta, int b, int base, bool whole, float c, F seen, G single) {
         using Q = Tile<T, DP, R>;
         const int lane = threadIdx.x % kWave, half = lane / 32;
         f32x16 s = {}, dp = {};
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d) {
-            mma(s, Q::row_frag(qt, 32 * b + lane % 32, d, half), k[d]);
-            mma(dp, Q::row_frag(gt, 32 * b + lane % 32, d, half), v[d]);
+            mma(s, Q::row_frag(lds, rb + qt, b, d), k[d]);
+            mma(dp, Q::row_frag(lds, rb + gt, b, d), v[d]);
         }
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
@@ -233,8 +248,8 @@ struct Keys {
             const Frag<T> w = operand<T>(s, part), ds = operand<T>(dp, part);
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {
-                mma(dv[d], Q::col_frag(gt, d, 2 * b + part, lane), w);
-                mma(dk[d], Q::col_frag(qt, d, 2 * b + part, lane), ds);
+                mma(dv[d], Q::col_frag(lds, cb + gt, d, 2 * b + part), w);
+                mma(dk[d], Q::col_frag(lds, cb + qt, d, 2 * b + part), ds);
             }
         }
     }
@@ -244,9 +259,9 @@ template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_kernel(AttnBwdArgs a) {
     constexpr int BQ = kTileRows<T, DP>, NB = BQ / 32;
     using Q = Tile<T, DP, BQ>;
-    using St = Stage<T, DP, BQ>;
-    __shared__ __align__(16) char qt[Q::kBytes], gt[Q::kBytes];
-    __shared__ __align__(16) float lse[BQ], delta[BQ];
+    using Copy = Feed<T, DP, BQ>;
+    __shared__ __align__(128) char lds[4 * Q::kBytes];      // two buffers of queries, then two of gradients
+    __shared__ __align__(16) float lse[2][BQ], delta[2][BQ];
     const int64_t item = die_order(blockIdx.x, a.k_items);
     if (item >= a.k_items) return;
     const int kvh = (int)(item / a.k_places);
@@ -264,21 +279,19 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
     // queries that see some key of the tile by the window
     const int begin = st.row, far = st.row + kGroupCols - 1 + a.window;
     const int end = far < st.len ? far : st.len;
-    const uint32_t sq = (uint32_t)a.ld_q * (uint32_t)sizeof(T), sg = (uint32_t)(a.q_heads * a.dim) * (uint32_t)sizeof(T);
-    const uint32_t oq = St::offset(sq), og = St::offset(sg);
+    const Copy cq(a.ld_q), cg((int64_t)a.q_heads * a.dim);
     const char* qp = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + st.first * a.ld_q + (int64_t)kvh * group * a.dim);
     const char* gp = reinterpret_cast<const char*>(static_cast<const T*>(a.dy) + ((int64_t)st.first * a.q_heads + kvh * group) * a.dim);
-    St qr, gr;
     float lr = 0.0f, er = 0.0f;
-    auto fetch = [&](int g, int base) {
-        const int64_t head = (int64_t)g * a.dim * (int)sizeof(T);
-        qr.fetch(qp + head + (int64_t)base * sq, oq, sq, end - base, a.dim);
-        gr.fetch(gp + head + (int64_t)base * sg, og, sg, end - base, a.dim);
+    auto issue = [&](int buffer, int g, int base) {
         if (tid < BQ) {
             const int64_t at = (int64_t)(st.first + base + tid) * a.q_heads + kvh * group + g;
             lr = base + tid < end ? a.lse[at] * kLog2e : 0.0f;
             er = base + tid < end ? a.delta[at] : 0.0f;
         }
+        const int64_t head = (int64_t)g * a.dim * (int)sizeof(T);
+        cq.issue(lds + buffer * Q::kBytes, qp + head + (int64_t)base * cq.stride, end - base, a.dim);
+        cg.issue(lds + (2 + buffer) * Q::kBytes, gp + head + (int64_t)base * cg.stride, end - base, a.dim);
     };
     // the sums that the first tokens' pieces left: those of the sequence, added into the first of them
     const int pieces_from = a.window / a.piece, pieces_to = (st.len + a.piece - 1) / a.piece;
@@ -295,32 +308,25 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
         }
     }
     // tiles of queries, one head after the other
-    int g = 0, base = begin;
-    if (kBwdAhead<T, DP>) fetch(g, base);
+    if (a.dim != DP) clear(lds, 4 * Q::kBytes);
+    int g = 0, base = begin, buffer = 0;
+    issue(0, g, base);
     while (g < group) {
-        if (!kBwdAhead<T, DP>) fetch(g, base);
-        __syncthreads();
-        qr.put(qt);
-        gr.put(gt);
-        if (tid < BQ) lse[tid] = lr, delta[tid] = er;
-        __syncthreads();
-        const int now = base;
+        if (tid < BQ) lse[buffer][tid] = lr, delta[buffer][tid] = er;
+        arrived();
+        const int now = base, current = buffer;
         base += BQ;
+        buffer ^= 1;
         if (base >= end) base = begin, ++g;
-        if (kBwdAhead<T, DP> && g < group) fetch(g, base);
-        auto seen = [&](int p) { return p < end && p >= key && p - key < a.window; };
-        auto single = [&](int p) { return p == 0 || (a.window == 1 && a.sinks == 0); };
-        // seen as a whole: the tile's blocks without a branch between them, one's products beside the other's exponentials, where registers suffice
+        if (g < group) issue(buffer, g, base);
+        const int qt = current * Q::kBytes, gt = (2 + current) * Q::kBytes;
         const bool whole = now + BQ <= end && k1 <= now && now + BQ - 1 - k0 < a.window;
-        if (kDkvWaves<T, DP> == 1 && whole) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) keys.template take<BQ>(qt, gt, lse, delta, b, now, true, a.c, seen, single);
-        } else {
-            for (int b = 0; b < NB; ++b) {
-                const int p0 = now + 32 * b, p1 = p0 + 31;
-                if (p0 >= end || p1 < k0 || p0 - k1 >= a.window) continue;
-                keys.template take<BQ>(qt, gt, lse, delta, b, now, whole, a.c, seen, single);
-            }
+        for (int b = 0; b < NB; ++b) {
+            const int p0 = now + 32 * b, p1 = p0 + 31;
+            if (p0 >= end || p1 < k0 || p0 - k1 >= a.window) continue;
+            keys.template take<BQ>(
+                lds, qt, gt, lse[current], delta[current], b, now, whole, a.c, [&](int p) { return p < end && p >= key && p - key < a.window; },
+                [&](int p) { return p == 0 || (a.window == 1 && a.sinks == 0); });
         }
     }
     // queries behind the window that see the first tokens
@@ -374,8 +380,8 @@ __global__ __launch_bounds__((kSinkWaves<T, DP> * kWave), (kDkvWaves<T, DP>)) vo
     const int end = st.row + a.piece < st.len ? st.row + a.piece : st.len;
     if (st.row >= st.len || end <= a.window) return;
     const int group = a.q_heads / a.kv_heads, key = lane % kCols;
-    char *qt = stage + wave * kOwn, *gt = qt + Q::kBytes;
-    float *lse = reinterpret_cast<float*>(gt + Q::kBytes), *delta = lse + 32;
+    char* own = stage + wave * kOwn;
+    float *lse = reinterpret_cast<float*>(own + 2 * Q::kBytes), *delta = lse + 32;
     Keys<T, DP> keys;
     keys.load(static_cast<const T*>(a.k) + (int64_t)(st.first + key) * a.ld_k + (int64_t)kvh * a.dim,
               static_cast<const T*>(a.v) + (int64_t)(st.first + key) * a.ld_v + (int64_t)kvh * a.dim, half, a.dim, key < a.sinks && key < st.len);
@@ -396,8 +402,8 @@ __global__ __launch_bounds__((kSinkWaves<T, DP> * kWave), (kDkvWaves<T, DP>)) vo
                 g.zero();
             }
             const int to = Q::at(m / Q::kChunks, m % Q::kChunks);
-            x.store(qt + to);
-            g.store(gt + to);
+            x.store(own + to);
+            g.store(own + Q::kBytes + to);
         }
         if (lane < 32) {
             const int64_t at = (int64_t)(st.first + base + lane) * a.q_heads + head;
@@ -405,7 +411,7 @@ __global__ __launch_bounds__((kSinkWaves<T, DP> * kWave), (kDkvWaves<T, DP>)) vo
             delta[lane] = base + lane < end ? a.delta[at] : 0.0f;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        keys.template take<32>(qt, gt, lse, delta, 0, base, false, a.c,
+        keys.template take<32>(own, 0, Q::kBytes, lse, delta, 0, base, false, a.c,
                                [&](int p) { return p < end && key < a.sinks && p - key >= a.window; }, [](int) { return false; });
     }
     // the waves' sums, in their order: 32 channels of all keys at a time
