@@ -63,7 +63,7 @@ __device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int 
 
 template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 128 ? 64 : 32;
 template <typename T, int DP> constexpr int kDqWaves = DP * sizeof(T) > 256 ? 1 : 2;
-template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 128 ? 1 : 2;
+template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 256 ? 1 : 2;
 
 // ---------------------------------------------------------------------------
 // dq and delta: workgroups and columns as in the forward kernel
