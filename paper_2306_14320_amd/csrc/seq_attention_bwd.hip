@@ -255,6 +255,32 @@ struct Keys {
     }
 };
 
+// The sums that the first tokens' pieces of a sequence left, for the tile of its first keys
+struct FirstSums {
+    bool any;
+    int pieces;
+    int64_t count, step;      // values of a piece, from one piece to the next
+    float* part;
+    __device__ __forceinline__ FirstSums(const AttnBwdArgs& a, const SeqTile& st, int kvh) {
+        any = a.sinks && st.len > a.window;
+        const int from = a.window / a.piece, place = a.seq.starts ? st.first / a.piece + st.b : st.b * ((a.seq.len + a.piece - 1) / a.piece);
+        pieces = (st.len + a.piece - 1) / a.piece - from;
+        count = 2 * (int64_t)a.sinks * a.dim;
+        step = a.kv_heads * count;
+        part = a.part + ((int64_t)(place + from) * a.kv_heads + kvh) * count;
+    }
+    // All of them into the first piece's: by all threads of the workgroup, in front of a barrier
+    __device__ __forceinline__ void add(int tid, int threads) const {
+        if (pieces < 2) return;
+        for (int n = tid; n < count; n += threads) {
+            float v = 0.0f;
+#pragma unroll 8
+            for (int z = 0; z < pieces; ++z) v += part[z * step + n];
+            part[n] = v;
+        }
+    }
+};
+
 template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_kernel(AttnBwdArgs a) {
     constexpr int BQ = kTileRows<T, DP>, NB = BQ / 32;
@@ -293,20 +319,9 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
         cq.issue(lds + buffer * Q::kBytes, qp + head + (int64_t)base * cq.stride, end - base, a.dim);
         cg.issue(lds + (2 + buffer) * Q::kBytes, gp + head + (int64_t)base * cg.stride, end - base, a.dim);
     };
-    // the sums that the first tokens' pieces left: those of the sequence, added into the first of them
-    const int pieces_from = a.window / a.piece, pieces_to = (st.len + a.piece - 1) / a.piece;
-    const bool first_keys = a.sinks && st.row == 0 && st.len > a.window;
-    const int place = a.seq.starts ? st.first / a.piece + st.b : st.b * ((a.seq.len + a.piece - 1) / a.piece);
-    const int64_t sums = 2 * (int64_t)a.sinks * a.dim;
-    float* part = a.part + ((int64_t)(place + pieces_from) * a.kv_heads + kvh) * sums;
-    if (first_keys && pieces_to - pieces_from > 1) {
-        for (int n = tid; n < sums; n += kAttnThreads) {
-            float v = 0.0f;
-#pragma unroll 8
-            for (int z = 0; z < pieces_to - pieces_from; ++z) v += part[z * a.kv_heads * sums + n];
-            part[n] = v;
-        }
-    }
+    const FirstSums first(a, st, kvh);
+    const bool first_keys = st.row == 0 && first.any;
+    if (first_keys) first.add(tid, kAttnThreads);
     // tiles of queries, one head after the other
     if (a.dim != DP) clear(lds, 4 * Q::kBytes);
     int g = 0, base = begin, buffer = 0;
@@ -331,7 +346,7 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
     }
     // queries behind the window that see the first tokens
     if (first_keys && wave == 0 && key < a.sinks) {
-        const float* p = part + (int64_t)key * a.dim;
+        const float* p = first.part + (int64_t)key * a.dim;
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d)
 #pragma unroll
@@ -357,38 +372,47 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
 }
 
 // ---------------------------------------------------------------------------
-// The first tokens' keys and the queries that have left them behind their
-// window: a workgroup takes a piece of the queries for all heads of a key head,
-// each wave 32 queries at a time in its own part of LDS.
+// 32 keys a workgroup, each wave 32 queries of a head at a time in its own part
+// of LDS, without barriers; the waves' sums are added at the end.  Two uses:
+//  - FIRST: the first tokens' keys and the queries that have left them behind
+//    their window, a piece of the queries a workgroup; leaves sums for the tile
+//    of the sequence's first keys;
+//  - otherwise dk and dv of small problems, whose tiles of 128 keys would leave
+//    the chip idle: four times the workgroups, and the queries' walk is shared
+//    by four waves.
 // ---------------------------------------------------------------------------
-template <typename T, int DP> constexpr int kSinkOwn = 2 * Tile<T, DP, 32>::kBytes + 256;      // a wave's queries, gradients, lse and delta
-template <typename T, int DP> constexpr int kSinkWaves = 4 * kSinkOwn<T, DP> > 160 * 1024 ? 2 : 4;
+template <typename T, int DP> constexpr int kNarrowOwn = 2 * Tile<T, DP, 32>::kBytes + 256;      // a wave's queries, gradients, lse and delta
+template <typename T, int DP> constexpr int kNarrowWaves = 4 * kNarrowOwn<T, DP> > 160 * 1024 ? 2 : 4;
 template <typename T, int DP>
-constexpr int kSinkLds = kSinkWaves<T, DP> * (kSinkOwn<T, DP> > 32 * 33 * 4 ? kSinkOwn<T, DP> : 32 * 33 * 4);
+constexpr int kNarrowLds = kNarrowWaves<T, DP> * (kNarrowOwn<T, DP> > 32 * 33 * 4 ? kNarrowOwn<T, DP> : 32 * 33 * 4);
 
-template <typename T, int DP>
-__global__ __launch_bounds__((kSinkWaves<T, DP> * kWave), (kDkvWaves<T, DP>)) void window_sink_kernel(AttnBwdArgs a) {
+template <typename T, int DP, bool FIRST>
+__global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 128 ? 1 : 2)) void window_narrow_kernel(AttnBwdArgs a) {
     using Q = Tile<T, DP, 32>;
-    constexpr int kRound = 32 * Q::kChunks / kWave, kOwn = kSinkOwn<T, DP>, NW = kSinkWaves<T, DP>;
+    constexpr int kRound = 32 * Q::kChunks / kWave, kOwn = kNarrowOwn<T, DP>, NW = kNarrowWaves<T, DP>;
     extern __shared__ __align__(16) char stage[];
-    const int64_t item = die_order(blockIdx.x, a.pieces * a.kv_heads);
-    if (item >= a.pieces * a.kv_heads) return;
+    const int64_t items = (FIRST ? a.pieces : a.k_places) * a.kv_heads, item = die_order(blockIdx.x, items);
+    if (item >= items) return;
     const int kvh = (int)(item % a.kv_heads);
     const int place = (int)(item / a.kv_heads);
-    const SeqTile st = seq_tile(a.seq, place, a.piece);
-    const int tid = threadIdx.x, wave = uniform(tid / kWave), lane = tid % kWave, half = lane / 32;
-    const int end = st.row + a.piece < st.len ? st.row + a.piece : st.len;
-    if (st.row >= st.len || end <= a.window) return;
-    const int group = a.q_heads / a.kv_heads, key = lane % kCols;
+    const SeqTile st = seq_tile(a.seq, place, FIRST ? a.piece : kCols);
+    if (st.row >= st.len) return;
+    // the queries' rows
+    const int64_t far = FIRST ? (int64_t)st.row + a.piece : (int64_t)st.row + kCols - 1 + a.window;
+    const int end = far < st.len ? (int)far : st.len;
+    if (FIRST && end <= a.window) return;
+    const int from = FIRST && st.row < a.window ? a.window : st.row;
+    const int tid = threadIdx.x, wave = uniform(tid / kWave), lane = tid % kWave, half = lane / 32, col = lane % kCols;
+    const int group = a.q_heads / a.kv_heads, k0 = FIRST ? 0 : st.row, key = k0 + col;
+    const bool live = key < st.len && (!FIRST || key < a.sinks);
     char* own = stage + wave * kOwn;
     float *lse = reinterpret_cast<float*>(own + 2 * Q::kBytes), *delta = lse + 32;
     Keys<T, DP> keys;
     keys.load(static_cast<const T*>(a.k) + (int64_t)(st.first + key) * a.ld_k + (int64_t)kvh * a.dim,
-              static_cast<const T*>(a.v) + (int64_t)(st.first + key) * a.ld_v + (int64_t)kvh * a.dim, half, a.dim, key < a.sinks && key < st.len);
-    const int blocks = (end - st.row + 31) / 32;
-    for (int n = wave; n < blocks * group; n += NW) {
-        const int head = kvh * group + n / blocks, base = st.row + n % blocks * 32;
-        if (base + 31 < a.window) continue;
+              static_cast<const T*>(a.v) + (int64_t)(st.first + key) * a.ld_v + (int64_t)kvh * a.dim, half, a.dim, live);
+    const int blocks = (end - from + 31) / 32;
+    for (int64_t n = wave; n < (int64_t)blocks * group; n += NW) {
+        const int head = kvh * group + (int)(n / blocks), base = from + (int)(n % blocks) * 32;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int i = 0; i < kRound; ++i) {
@@ -411,11 +435,19 @@ __global__ __launch_bounds__((kSinkWaves<T, DP> * kWave), (kDkvWaves<T, DP>)) vo
             delta[lane] = base + lane < end ? a.delta[at] : 0.0f;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        keys.template take<32>(own, 0, Q::kBytes, lse, delta, 0, base, false, a.c,
-                               [&](int p) { return p < end && key < a.sinks && p - key >= a.window; }, [](int) { return false; });
+        if constexpr (FIRST) {
+            keys.template take<32>(own, 0, Q::kBytes, lse, delta, 0, base, false, a.c,
+                                   [&](int p) { return p < end && key < a.sinks && p - key >= a.window; }, [](int) { return false; });
+        } else {
+            const bool whole = base + 32 <= end && k0 + kCols - 1 <= base && base + 31 - k0 < a.window;
+            keys.template take<32>(own, 0, Q::kBytes, lse, delta, 0, base, whole, a.c, [&](int p) { return p < end && p >= key && p - key < a.window; },
+                                   [&](int p) { return p == 0 || (a.window == 1 && a.sinks == 0); });
+        }
     }
     // the waves' sums, in their order: 32 channels of all keys at a time
-    float* out = a.part + ((int64_t)place * a.kv_heads + kvh) * 2 * a.sinks * a.dim;
+    const FirstSums first(a, st, kvh);
+    const bool first_keys = !FIRST && st.row == 0 && first.any;
+    if (first_keys) first.add(tid, NW * kWave);
     float(*sum)[32][33] = reinterpret_cast<float(*)[32][33]>(stage);      // wave, channel, key
     __syncthreads();
 #pragma unroll
@@ -423,14 +455,22 @@ __global__ __launch_bounds__((kSinkWaves<T, DP> * kWave), (kDkvWaves<T, DP>)) vo
 #pragma unroll
         for (int d = 0; d < DP / 32; ++d) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum[wave][acc_row(i, half)][key] = which ? keys.dv[d][i] : keys.dk[d][i];
+            for (int i = 0; i < 16; ++i) sum[wave][acc_row(i, half)][col] = which ? keys.dv[d][i] : keys.dk[d][i];
             __syncthreads();
-            for (int n = tid; n < 32 * a.sinks; n += NW * kWave) {
-                const int e = n % 32, s = n / 32;
-                float v = sum[0][e][s];
+            for (int n = tid; n < 32 * 32; n += NW * kWave) {
+                const int e = 32 * d + n % 32, s = n / 32;
+                float v = sum[0][n % 32][s];
 #pragma unroll
-                for (int w = 1; w < NW; ++w) v += sum[w][e][s];
-                if (32 * d + e < a.dim) out[((int64_t)which * a.sinks + s) * a.dim + 32 * d + e] = v;
+                for (int w = 1; w < NW; ++w) v += sum[w][n % 32][s];
+                if (e >= a.dim) continue;
+                if constexpr (FIRST) {
+                    if (s < a.sinks) a.part[((((int64_t)place * a.kv_heads + kvh) * 2 + which) * a.sinks + s) * a.dim + e] = v;
+                } else if (k0 + s < st.len) {
+                    if (first_keys && s < a.sinks) v += first.part[(int64_t)(which * a.sinks + s) * a.dim + e];
+                    const int64_t to = ((int64_t)(st.first + k0 + s) * a.kv_heads + kvh) * a.dim + e;
+                    if (which) static_cast<T*>(a.dv)[to] = (T)v;
+                    else static_cast<T*>(a.dk)[to] = (T)(v * a.scale);
+                }
             }
             __syncthreads();
         }
@@ -444,6 +484,8 @@ void with_type(int32_t dtype, F f) {
     if (dtype == IM2WIN_F32) f(float{});
     else f(bf16{});
 }
+
+constexpr int64_t kNarrowBelow = 256;
 
 // Pieces of queries that may see first tokens outside of their window: none
 // where no sequence can be longer than the window.
@@ -501,7 +543,9 @@ int im2win_window_attention_backward(const im2win_window_desc* d, const void* dy
     a.seq = make_seq_map(d->tokens, d->sequences, seq_starts);
     a.q_places = seq_places(d->tokens, d->sequences, seq_starts, a.tile);
     a.q_items = a.q_places * (d->q_heads / a.pack);
-    a.k_places = seq_places(d->tokens, d->sequences, seq_starts, kGroupCols);
+    // where tiles of 128 keys would not give every CU a workgroup, tiles of 32
+    const bool narrow = seq_places(d->tokens, d->sequences, seq_starts, kGroupCols) * d->kv_heads < kNarrowBelow;
+    a.k_places = seq_places(d->tokens, d->sequences, seq_starts, narrow ? kCols : kGroupCols);
     a.k_items = a.k_places * d->kv_heads;
     a.pieces = pieces_of(d, seq_starts);
     a.piece = (int)piece_rows(d);
@@ -517,13 +561,18 @@ int im2win_window_attention_backward(const im2win_window_desc* d, const void* dy
         using T = decltype(ty);
         with_head(d->head_dim, [&](auto dp) {
             constexpr int DP = decltype(dp)::value;
-            constexpr int kLds = kSinkLds<T, DP>;
-            if (a.pieces && kLds > 65536)
-                attribute = hipFuncSetAttribute(reinterpret_cast<const void*>(&window_sink_kernel<T, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+            constexpr int kLds = kNarrowLds<T, DP>;
+            auto allow = [&](const void* kernel) {
+                if (kLds > 65536 && attribute == hipSuccess) attribute = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+            };
+            if (a.pieces) allow(reinterpret_cast<const void*>(&window_narrow_kernel<T, DP, true>));
+            if (narrow) allow(reinterpret_cast<const void*>(&window_narrow_kernel<T, DP, false>));
             if (attribute != hipSuccess) return;
             hipLaunchKernelGGL((window_dq_kernel<T, DP>), dim3((unsigned)gq), dim3(kAttnThreads), 0, s, a);
-            if (a.pieces) hipLaunchKernelGGL((window_sink_kernel<T, DP>), dim3((unsigned)gs), dim3(kSinkWaves<T, DP> * kWave), kLds, s, a);
-            hipLaunchKernelGGL((window_dkv_kernel<T, DP>), dim3((unsigned)gk), dim3(kAttnThreads), 0, s, a);
+            constexpr int kThreads = kNarrowWaves<T, DP> * kWave;
+            if (a.pieces) hipLaunchKernelGGL((window_narrow_kernel<T, DP, true>), dim3((unsigned)gs), dim3(kThreads), kLds, s, a);
+            if (narrow) hipLaunchKernelGGL((window_narrow_kernel<T, DP, false>), dim3((unsigned)gk), dim3(kThreads), kLds, s, a);
+            else hipLaunchKernelGGL((window_dkv_kernel<T, DP>), dim3((unsigned)gk), dim3(kAttnThreads), 0, s, a);
         });
     });
     if (attribute != hipSuccess) return fail(IM2WIN_EHIP, "window_attention_backward's LDS: %s", hipGetErrorString(attribute));
