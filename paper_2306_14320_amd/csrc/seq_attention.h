@@ -155,9 +155,19 @@ struct Chunk {
 // ---------------------------------------------------------------------------
 constexpr int64_t kMaxAttnStride = int64_t(1) << 24;      // a tile's 64 rows of bf16 or 32 of fp32 within 32 bits of bytes
 
-// The wave's own copies have arrived, and then everyone's.
-__device__ __forceinline__ void arrived() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+// Tiles are copied this many ahead of the one that is worked on, two where LDS
+// holds three pairs of them: a copy takes longer than a tile's work, and where
+// few workgroups share a CU nothing else covers it (1000 tokens of 16 x 128
+// bf16: 30 us with one tile ahead).
+template <int BYTES> constexpr int kAheadTiles = 3 * 2 * BYTES <= 156 * 1024 ? 2 : 1;
+
+// The wave's copies but for the newest N have arrived, and then everyone's.
+// N may only count copies that each wave has issued whatever its lanes hold.
+template <int N>
+__device__ __forceinline__ void arrived(bool all_but_newest) {
+    static_assert(N < 64, "the counter's range");
+    if (all_but_newest) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
 }
 

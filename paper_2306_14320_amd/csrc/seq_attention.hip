@@ -125,8 +125,9 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
     constexpr int BK = kTileKeys<T, DP>, NB = BK / 32;
     using KV = Tile<T, DP, BK>;
     using Copy = Feed<T, DP, BK>;
-    __shared__ __align__(128) char lds[4 * KV::kBytes];      // two buffers of keys, then two of values
-    __shared__ uint32_t flags[2][2];      // rows of a buffer whose values are not all finite
+    constexpr int kAhead = kAheadTiles<KV::kBytes>, kBuffers = kAhead + 1;
+    __shared__ __align__(128) char lds[2 * kBuffers * KV::kBytes];      // buffers of keys, then of values
+    __shared__ uint32_t flags[kBuffers][2];      // rows of a buffer whose values are not all finite
     const int64_t item = die_order(blockIdx.x, a.items);
     if (item >= a.items) return;
     const int hb = (int)(item / a.places);
@@ -175,7 +176,7 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
         return p < past ? static_cast<const T*>(a.v_cache) + cached(p) : reinterpret_cast<const T*>(vn + (int64_t)(p - past) * cv.stride);
     };
     auto issue = [&](int buffer, int base, int stop) {
-        char *kt = lds + buffer * KV::kBytes, *vt = lds + (2 + buffer) * KV::kBytes;
+        char *kt = lds + buffer * KV::kBytes, *vt = lds + (kBuffers + buffer) * KV::kBytes;
         if (base >= past) {
             ck.issue(kt, kn + (int64_t)(base - past) * ck.stride, stop - base, a.dim);
             cv.issue(vt, vn + (int64_t)(base - past) * cv.stride, stop - base, a.dim);
@@ -193,31 +194,32 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
 
     const int rb = KV::row_base(lane), cb = KV::col_base(lane);
     Running<DP> r;
-    if (a.dim != DP) clear(lds, 4 * KV::kBytes);
-    if (tid < 4) flags[tid / 2][tid % 2] = 0;
-    bool sinks_now = first_end > 0;
-    int base = sinks_now ? 0 : begin, stop = sinks_now ? first_end : end, buffer = 0;
-    if (!served) base = stop = end;
-    if (base < stop) issue(0, base, stop);
-    while (base < stop) {
-        arrived();
-        const int now = base, now_stop = stop;
-        const bool sink_tile = sinks_now;
-        if (sinks_now) sinks_now = false, base = begin, stop = end;
-        else base += BK;
+    if (a.dim != DP) clear(lds, 2 * kBuffers * KV::kBytes);
+    if (tid < 2 * kBuffers) flags[tid / 2][tid % 2] = 0;
+    // tile i: the sinks', where there is one, and those of the windows
+    const int lead = first_end > 0 ? 1 : 0, count = served ? lead + (end - begin + BK - 1) / BK : 0;
+    auto base_of = [&](int i) { return i < lead ? 0 : begin + (i - lead) * BK; };
+    auto stop_of = [&](int i) { return i < lead ? first_end : end; };
+    for (int i = 0; i < kAhead && i < count; ++i) issue(i, base_of(i), stop_of(i));
+    int buffer = 0;
+    for (int n = 0; n < count; ++n) {
+        const bool sink_tile = n < lead;
+        const int now = base_of(n), now_stop = stop_of(n), newest = n + kAhead - 1;
+        // the newest tile under way, if it is another: whole, and not of the cache, it is as many copies in every wave
+        arrived<2 * Copy::kPasses>(kAhead == 2 && newest < count && a.dim == DP && base_of(newest) >= past && base_of(newest) + BK <= stop_of(newest));
         // a tile that some column does not see all of: its values' infinities and NaN stay out of the product
         if (now + BK > now_stop || now + BK - 1 > qfirst || now <= qlast - a.window) {
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < Copy::kPasses; ++i) {
                 Chunk c;
-                c.load(lds + (2 + buffer) * KV::kBytes + (tid + i * kAttnThreads) * 16);
+                c.load(lds + (kBuffers + buffer) * KV::kBytes + (tid + i * kAttnThreads) * 16);
                 bad |= nonfinite<T>(c);
             }
             if (bad) {
 #pragma unroll
                 for (int i = 0; i < Copy::kPasses; ++i) {
-                    char* to = lds + (2 + buffer) * KV::kBytes + (tid + i * kAttnThreads) * 16;
+                    char* to = lds + (kBuffers + buffer) * KV::kBytes + (tid + i * kAttnThreads) * 16;
                     Chunk c;
                     c.load(to);
                     if (!nonfinite<T>(c)) continue;
@@ -228,11 +230,11 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
             }
             __syncthreads();
         }
-        if (tid < 2) flags[buffer ^ 1][tid] = 0;      // read before the last barrier
-        if (base < stop) issue(buffer ^ 1, base, stop);
-        const int kb = rb + buffer * KV::kBytes, vb = cb + (2 + buffer) * KV::kBytes;
-        const int current = buffer;
-        buffer ^= 1;
+        const int current = buffer, before = buffer ? buffer - 1 : kBuffers - 1;      // the tile before was read in front of the last barrier
+        if (tid < 2) flags[before][tid] = 0;
+        if (n + kAhead < count) issue(before, base_of(n + kAhead), stop_of(n + kAhead));
+        const int kb = rb + buffer * KV::kBytes, vb = cb + (kBuffers + buffer) * KV::kBytes;
+        buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
         // keys in front of the wave's first window (but for sinks) or behind its last query
         if (now > wq1 || (now + BK <= wq0 - a.window + 1 && now >= a.sinks)) continue;
 

@@ -61,7 +61,7 @@ __device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int 
     return f;
 }
 
-template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 128 ? 64 : 32;
+template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 96 ? 64 : 32;
 template <typename T, int DP> constexpr int kDqWaves = DP * sizeof(T) > 256 ? 1 : 2;
 template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 256 ? 1 : 2;
 
@@ -73,7 +73,8 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
     constexpr int BK = kTileRows<T, DP>, NB = BK / 32;
     using KV = Tile<T, DP, BK>;
     using Copy = Feed<T, DP, BK>;
-    __shared__ __align__(128) char lds[4 * KV::kBytes];      // two buffers of keys, then two of values
+    constexpr int kAhead = kAheadTiles<KV::kBytes>, kBuffers = kAhead + 1;
+    __shared__ __align__(128) char lds[2 * kBuffers * KV::kBytes];      // buffers of keys, then of values
     const int64_t item = die_order(blockIdx.x, a.q_items);
     if (item >= a.q_items) return;
     const int hb = (int)(item / a.q_places);
@@ -111,26 +112,28 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
     const char* vp = reinterpret_cast<const char*>(static_cast<const T*>(a.v) + st.first * a.ld_v + (int64_t)kvh * a.dim);
     auto issue = [&](int buffer, int base, int stop) {
         ck.issue(lds + buffer * KV::kBytes, kp + (int64_t)base * ck.stride, stop - base, a.dim);
-        cv.issue(lds + (2 + buffer) * KV::kBytes, vp + (int64_t)base * cv.stride, stop - base, a.dim);
+        cv.issue(lds + (kBuffers + buffer) * KV::kBytes, vp + (int64_t)base * cv.stride, stop - base, a.dim);
     };
     const int rb = KV::row_base(lane), cb = KV::col_base(lane);
     f32x16 o[DP / 32];
 #pragma unroll
     for (int i = 0; i < DP / 32; ++i) o[i] = f32x16{};
-    if (a.dim != DP) clear(lds, 4 * KV::kBytes);
-    bool sinks_now = first_end > 0;
-    int base = sinks_now ? 0 : begin, stop = sinks_now ? first_end : end, buffer = 0;
+    if (a.dim != DP) clear(lds, 2 * kBuffers * KV::kBytes);
+    // tile i: the sinks', where there is one, and those of the windows
+    const int lead = first_end > 0 ? 1 : 0, count = lead + (end - begin + BK - 1) / BK;
+    auto base_of = [&](int i) { return i < lead ? 0 : begin + (i - lead) * BK; };
+    auto stop_of = [&](int i) { return i < lead ? first_end : end; };
+    for (int i = 0; i < kAhead && i < count; ++i) issue(i, base_of(i), stop_of(i));
+    int buffer = 0;
     float rest = 0.0f;
-    issue(0, base, stop);
-    while (base < stop) {
-        arrived();
-        const int now = base, now_stop = stop;
-        const bool sink_tile = sinks_now;
-        if (sinks_now) sinks_now = false, base = begin, stop = end;
-        else base += BK;
-        if (base < stop) issue(buffer ^ 1, base, stop);
-        const int kb = rb + buffer * KV::kBytes, kc = cb + buffer * KV::kBytes, vb = rb + (2 + buffer) * KV::kBytes;
-        buffer ^= 1;
+    for (int n = 0; n < count; ++n) {
+        const bool sink_tile = n < lead;
+        const int now = base_of(n), now_stop = stop_of(n), newest = n + kAhead - 1;
+        arrived<2 * Copy::kPasses>(kAhead == 2 && newest < count && a.dim == DP && base_of(newest) + BK <= stop_of(newest));
+        const int before = buffer ? buffer - 1 : kBuffers - 1;
+        if (n + kAhead < count) issue(before, base_of(n + kAhead), stop_of(n + kAhead));
+        const int kb = rb + buffer * KV::kBytes, kc = cb + buffer * KV::kBytes, vb = rb + (kBuffers + buffer) * KV::kBytes;
+        buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
         if (now > wq1 || (now + BK <= wq0 - a.window + 1 && now >= a.sinks)) continue;
         const bool whole = !sink_tile && now >= a.sinks && now + BK - 1 <= wq0 && now > wq1 - a.window;
 #pragma unroll
@@ -286,8 +289,9 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
     constexpr int BQ = kTileRows<T, DP>, NB = BQ / 32;
     using Q = Tile<T, DP, BQ>;
     using Copy = Feed<T, DP, BQ>;
-    __shared__ __align__(128) char lds[4 * Q::kBytes];      // two buffers of queries, then two of gradients
-    __shared__ __align__(16) float lse[2][BQ], delta[2][BQ];
+    constexpr int kAhead = kAheadTiles<Q::kBytes>, kBuffers = kAhead + 1;
+    __shared__ __align__(128) char lds[2 * kBuffers * Q::kBytes];      // buffers of queries, then of gradients
+    __shared__ __align__(16) float lse[kBuffers][BQ], delta[kBuffers][BQ];
     const int64_t item = die_order(blockIdx.x, a.k_items);
     if (item >= a.k_items) return;
     const int kvh = (int)(item / a.k_places);
@@ -317,30 +321,52 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
         }
         const int64_t head = (int64_t)g * a.dim * (int)sizeof(T);
         cq.issue(lds + buffer * Q::kBytes, qp + head + (int64_t)base * cq.stride, end - base, a.dim);
-        cg.issue(lds + (2 + buffer) * Q::kBytes, gp + head + (int64_t)base * cg.stride, end - base, a.dim);
+        cg.issue(lds + (kBuffers + buffer) * Q::kBytes, gp + head + (int64_t)base * cg.stride, end - base, a.dim);
     };
     const FirstSums first(a, st, kvh);
     const bool first_keys = st.row == 0 && first.any;
     if (first_keys) first.add(tid, kAttnThreads);
-    // tiles of queries, one head after the other
-    if (a.dim != DP) clear(lds, 4 * Q::kBytes);
-    int g = 0, base = begin, buffer = 0;
-    issue(0, g, base);
-    while (g < group) {
-        if (tid < BQ) lse[buffer][tid] = lr, delta[buffer][tid] = er;
-        arrived();
-        const int now = base, current = buffer;
-        base += BQ;
-        buffer ^= 1;
-        if (base >= end) base = begin, ++g;
-        if (g < group) issue(buffer, g, base);
-        const int qt = current * Q::kBytes, gt = (2 + current) * Q::kBytes;
-        const bool whole = now + BQ <= end && k1 <= now && now + BQ - 1 - k0 < a.window;
+    // tiles of queries, one head after the other; lse and delta of a tile wait
+    // in registers from its issue to the next iteration
+    if (a.dim != DP) clear(lds, 2 * kBuffers * Q::kBytes);
+    const int count = group * ((end - begin + BQ - 1) / BQ);
+    int ahead_g = 0, ahead_base = begin, ahead = 0, held = -1, buffer = 0, now = begin;
+    bool newest_whole = false;
+    auto advance = [&](int& g, int& b) {
+        b += BQ;
+        if (b >= end) b = begin, ++g;
+    };
+    auto keep = [&] {
+        if (held >= 0 && tid < BQ) lse[held][tid] = lr, delta[held][tid] = er;
+    };
+    auto next = [&](int into) {
+        issue(into, ahead_g, ahead_base);
+        newest_whole = a.dim == DP && ahead_base + BQ <= end;
+        held = into;
+        ++ahead;
+        advance(ahead_g, ahead_base);
+    };
+    for (int i = 0; i < kAhead && i < count; ++i) {
+        keep();
+        next(i);
+    }
+    int g = 0;
+    for (int n = 0; n < count; ++n) {
+        keep();
+        held = -1;
+        arrived<2 * Copy::kPasses>(kAhead == 2 && ahead == n + 2 && newest_whole);
+        const int at = now, before = buffer ? buffer - 1 : kBuffers - 1;
+        advance(g, now);
+        if (ahead < count) next(before);
+        const int qt = buffer * Q::kBytes, gt = (kBuffers + buffer) * Q::kBytes;
+        const float *ls = lse[buffer], *de = delta[buffer];
+        buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
+        const bool whole = at + BQ <= end && k1 <= at && at + BQ - 1 - k0 < a.window;
         for (int b = 0; b < NB; ++b) {
-            const int p0 = now + 32 * b, p1 = p0 + 31;
+            const int p0 = at + 32 * b, p1 = p0 + 31;
             if (p0 >= end || p1 < k0 || p0 - k1 >= a.window) continue;
             keys.template take<BQ>(
-                lds, qt, gt, lse[current], delta[current], b, now, whole, a.c, [&](int p) { return p < end && p >= key && p - key < a.window; },
+                lds, qt, gt, ls, de, b, at, whole, a.c, [&](int p) { return p < end && p >= key && p - key < a.window; },
                 [&](int p) { return p == 0 || (a.window == 1 && a.sinks == 0); });
         }
     }
@@ -386,6 +412,8 @@ template <typename T, int DP> constexpr int kNarrowWaves = 4 * kNarrowOwn<T, DP>
 template <typename T, int DP>
 constexpr int kNarrowLds = kNarrowWaves<T, DP> * (kNarrowOwn<T, DP> > 32 * 33 * 4 ? kNarrowOwn<T, DP> : 32 * 33 * 4);
 
+template <typename T, int DP> constexpr bool kNarrowAhead = DP * sizeof(T) <= 256;
+
 template <typename T, int DP, bool FIRST>
 __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 128 ? 1 : 2)) void window_narrow_kernel(AttnBwdArgs a) {
     using Q = Tile<T, DP, 32>;
@@ -411,30 +439,42 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
     keys.load(static_cast<const T*>(a.k) + (int64_t)(st.first + key) * a.ld_k + (int64_t)kvh * a.dim,
               static_cast<const T*>(a.v) + (int64_t)(st.first + key) * a.ld_v + (int64_t)kvh * a.dim, half, a.dim, live);
     const int blocks = (end - from + 31) / 32;
-    for (int64_t n = wave; n < (int64_t)blocks * group; n += NW) {
+    const int64_t count = (int64_t)blocks * group;
+    // a block's rows wait in registers while the one before it is worked on
+    Chunk x[kRound], g[kRound];
+    float lr = 0.0f, er = 0.0f;
+    auto fetch = [&](int64_t n) {
         const int head = kvh * group + (int)(n / blocks), base = from + (int)(n % blocks) * 32;
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int i = 0; i < kRound; ++i) {
             const int m = lane + i * kWave, p = base + m / Q::kChunks, e = m % Q::kChunks * Q::kElems;
-            Chunk x, g;
             if (p < end && e < a.dim) {
-                x.load(static_cast<const T*>(a.q) + (int64_t)(st.first + p) * a.ld_q + (int64_t)head * a.dim + e);
-                g.load(static_cast<const T*>(a.dy) + ((int64_t)(st.first + p) * a.q_heads + head) * a.dim + e);
+                x[i].load(static_cast<const T*>(a.q) + (int64_t)(st.first + p) * a.ld_q + (int64_t)head * a.dim + e);
+                g[i].load(static_cast<const T*>(a.dy) + ((int64_t)(st.first + p) * a.q_heads + head) * a.dim + e);
             } else {
-                x.zero();
-                g.zero();
+                x[i].zero();
+                g[i].zero();
             }
-            const int to = Q::at(m / Q::kChunks, m % Q::kChunks);
-            x.store(own + to);
-            g.store(own + Q::kBytes + to);
         }
-        if (lane < 32) {
-            const int64_t at = (int64_t)(st.first + base + lane) * a.q_heads + head;
-            lse[lane] = base + lane < end ? a.lse[at] * kLog2e : 0.0f;
-            delta[lane] = base + lane < end ? a.delta[at] : 0.0f;
-        }
+        const int p = base + col;
+        const int64_t at = (int64_t)(st.first + (p < end ? p : end - 1)) * a.q_heads + head;
+        lr = a.lse[at] * kLog2e;
+        er = a.delta[at];
+    };
+    if (kNarrowAhead<T, DP> && wave < count) fetch(wave);
+    for (int64_t n = wave; n < count; n += NW) {
+        const int base = from + (int)(n % blocks) * 32;
+        if (!kNarrowAhead<T, DP>) fetch(n);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) {
+            const int m = lane + i * kWave, to = Q::at(m / Q::kChunks, m % Q::kChunks);
+            x[i].store(own + to);
+            g[i].store(own + Q::kBytes + to);
+        }
+        if (lane < 32) lse[lane] = lr, delta[lane] = er;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (kNarrowAhead<T, DP> && n + NW < count) fetch(n + NW);
         if constexpr (FIRST) {
             keys.template take<32>(own, 0, Q::kBytes, lse, delta, 0, base, false, a.c,
                                    [&](int p) { return p < end && key < a.sinks && p - key >= a.window; }, [](int) { return false; });
