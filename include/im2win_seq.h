@@ -366,11 +366,11 @@ int im2win_qk_norm_rope_backward(const im2win_qk_desc* d, const void* dyq, const
 /* ------------------------------------------------------------------------ */
 
 typedef struct {
-    int64_t tokens;            /* T, at most 2^30 (requests, for the step) */
+    int64_t tokens;            /* T, at most 2^29 (requests, for the step) */
     int64_t sequences;         /* B >= 1 (not used by the step) */
     int64_t q_heads, kv_heads; /* H and K; query head h reads key head h / (H / K) */
     int64_t head_dim;          /* a multiple of 8 up to 256 */
-    int64_t window;            /* W >= 1: a token sees itself and the W-1 before it */
+    int64_t window;            /* W, 1 to 2^30: a token sees itself and the W-1 before it */
     int64_t sinks;             /* S, 0 to 32: and the first S of its sequence */
     int64_t ld_q, ld_k, ld_v;  /* row strides of q, k and v, below 2^24 */
     int32_t dtype;             /* of q, k, v, the caches, y and the gradients */

@@ -155,11 +155,11 @@ struct Chunk {
 // ---------------------------------------------------------------------------
 constexpr int64_t kMaxAttnStride = int64_t(1) << 24;      // a tile's 64 rows of bf16 or 32 of fp32 within 32 bits of bytes
 
-// Tiles are copied this many ahead of the one that is worked on, two where LDS
-// holds three pairs of them: a copy takes longer than a tile's work, and where
-// few workgroups share a CU nothing else covers it (1000 tokens of 16 x 128
-// bf16: 30 us with one tile ahead).
-template <int BYTES> constexpr int kAheadTiles = 3 * 2 * BYTES <= 156 * 1024 ? 2 : 1;
+// Tiles are copied this many ahead of the one that is worked on: two where one
+// workgroup a CU has LDS for three pairs of them, since no other covers the
+// copies' way then (2503 tokens fp32: 209 -> 189 us); with more workgroups one
+// (two take 238 us where one takes 195, by the registers that they cost).
+template <int BYTES, int WAVES> constexpr int kAheadTiles = WAVES == 1 && 3 * 2 * BYTES <= 156 * 1024 ? 2 : 1;
 
 // The wave's copies but for the newest N have arrived, and then everyone's.
 // N may only count copies that each wave has issued whatever its lanes hold.
@@ -333,7 +333,8 @@ inline int check_attention(const im2win_window_desc* d) {
     if (!d) return fail(IM2WIN_ENULL, "descriptor is NULL");
     int rc = check_rows(d->tokens, 1, d->dtype);
     if (rc) return rc;
-    if (d->tokens > (int64_t(1) << 30)) return fail(IM2WIN_EOVERFLOW, "at most 2^30 tokens (got %lld)", (long long)d->tokens);
+    // positions, with up to 2^30 tokens before the call and a tile behind the last, stay in 32 bits
+    if (d->tokens > (int64_t(1) << 29)) return fail(IM2WIN_EOVERFLOW, "at most 2^29 tokens (got %lld)", (long long)d->tokens);
     if (d->kv_heads < 1 || d->q_heads < 1 || d->q_heads > 65536 || d->q_heads % d->kv_heads)
         return fail(IM2WIN_EINVAL, "q_heads must be 1 to 65536 and a multiple of kv_heads (got %lld, %lld)", (long long)d->q_heads, (long long)d->kv_heads);
     if (d->head_dim < 8 || d->head_dim > 256 || d->head_dim % 8)

@@ -110,7 +110,10 @@ __device__ __forceinline__ void put4(bf16* p, float a, float b, float c, float d
 }
 
 template <typename T, int DP> constexpr int kTileKeys = sizeof(T) == 2 && DP <= 96 ? 64 : 32;
-// Waves a SIMD: two, of 256 registers, where the queries' and outputs' fit; else one.
+// Waves a SIMD.  Up to 128 channels of bf16 three hide the waits for LDS best
+// (16384 tokens of 16 x 128, window 1024: 195 us, 214 with two waves, and 217 with
+// two that read each operand a step ahead); 96 channels, whose tiles are of 64
+// rows, and wider rows have registers for two, or one.
 template <typename T, int DP> constexpr int kFwdWaves = DP * sizeof(T) > 384 || DP >= 192 ? 1 : sizeof(T) == 2 && DP != 96 ? 3 : 2;
 // Whether the step's next rows wait in registers while some are worked on
 template <typename T, int DP> constexpr bool kStepAhead = DP * sizeof(T) <= 256;
@@ -125,7 +128,7 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
     constexpr int BK = kTileKeys<T, DP>, NB = BK / 32;
     using KV = Tile<T, DP, BK>;
     using Copy = Feed<T, DP, BK>;
-    constexpr int kAhead = kAheadTiles<KV::kBytes>, kBuffers = kAhead + 1;
+    constexpr int kAhead = kAheadTiles<KV::kBytes, kFwdWaves<T, DP>>, kBuffers = kAhead + 1;
     __shared__ __align__(128) char lds[2 * kBuffers * KV::kBytes];      // buffers of keys, then of values
     __shared__ uint32_t flags[kBuffers][2];      // rows of a buffer whose values are not all finite
     const int64_t item = die_order(blockIdx.x, a.items);
@@ -238,45 +241,36 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
         // keys in front of the wave's first window (but for sinks) or behind its last query
         if (now > wq1 || (now + BK <= wq0 - a.window + 1 && now >= a.sinks)) continue;
 
-        f32x16 s[NB];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) s[b] = f32x16{};
+        for (int b = 0; b < NB; ++b) {      // 32 keys at a time
+            f32x16 s[1] = {f32x16{}};
 #pragma unroll
-        for (int d = 0; d < DP / 16; ++d)
+            for (int d = 0; d < DP / 16; ++d) mma(s[0], KV::row_frag(lds, kb, b, d), q[d]);
+            if (sink_tile) {                // all of them seen, by all
+                const int n = now_stop - 4 * half;
 #pragma unroll
-            for (int b = 0; b < NB; ++b) mma(s[b], KV::row_frag(lds, kb, b, d), q[d]);
-        if (sink_tile) {                // all of them seen, by all
-            const int n = now_stop - 4 * half;
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[b][i] = 32 * b + acc_row(i, 0) < n ? s[b][i] : -INFINITY;
-        } else if (now < a.sinks) {     // the sequence's first keys
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
+                for (int i = 0; i < 16; ++i) s[0][i] = 32 * b + acc_row(i, 0) < n ? s[0][i] : -INFINITY;
+            } else if (now < a.sinks) {     // the sequence's first keys
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const int p = now + 32 * b + acc_row(i, half);
-                    s[b][i] = p <= pos && (p > pos - a.window || p < a.sinks) ? s[b][i] : -INFINITY;
+                    s[0][i] = p <= pos && (p > pos - a.window || p < a.sinks) ? s[0][i] : -INFINITY;
                 }
-        } else if (!(now + BK - 1 <= wq0 && now > wq1 - a.window)) {      // pos - window < p <= pos
-            const int low = pos - a.window + 1 - now - 4 * half;
+            } else if (!(now + BK - 1 <= wq0 && now > wq1 - a.window)) {      // pos - window < p <= pos
+                const int low = pos - a.window + 1 - now - 4 * half;
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) s[b][i] = (uint32_t)(32 * b + acc_row(i, 0) - low) < (uint32_t)a.window ? s[b][i] : -INFINITY;
-        }
-        soften<DP, NB>(r, s, a.c);
-        __builtin_amdgcn_s_setprio(1);      // a wave with products to issue goes first (206 -> 201 us)
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
+                for (int i = 0; i < 16; ++i) s[0][i] = (uint32_t)(32 * b + acc_row(i, 0) - low) < (uint32_t)a.window ? s[0][i] : -INFINITY;
+            }
+            soften<DP, 1>(r, s, a.c);
+            __builtin_amdgcn_s_setprio(1);      // a wave with products to issue goes first
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
-                const Frag<T> w = weights<T>(s[b], part);
+                const Frag<T> w = weights<T>(s[0], part);
 #pragma unroll
                 for (int t = 0; t < DP / 32; ++t) mma(r.o[t], KV::col_frag(lds, vb, t, 2 * b + part), w);
             }
-        __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_s_setprio(0);
+        }
         // what was kept out of the product: a column that sees such a value has it
         for (int f = 0; f < NB; ++f)
             for (uint32_t rest = uniform(flags[current][f]); rest; rest &= rest - 1) {

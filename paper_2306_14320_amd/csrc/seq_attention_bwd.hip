@@ -73,7 +73,7 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
     constexpr int BK = kTileRows<T, DP>, NB = BK / 32;
     using KV = Tile<T, DP, BK>;
     using Copy = Feed<T, DP, BK>;
-    constexpr int kAhead = kAheadTiles<KV::kBytes>, kBuffers = kAhead + 1;
+    constexpr int kAhead = kAheadTiles<KV::kBytes, kDqWaves<T, DP>>, kBuffers = kAhead + 1;
     __shared__ __align__(128) char lds[2 * kBuffers * KV::kBytes];      // buffers of keys, then of values
     const int64_t item = die_order(blockIdx.x, a.q_items);
     if (item >= a.q_items) return;
@@ -289,7 +289,7 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
     constexpr int BQ = kTileRows<T, DP>, NB = BQ / 32;
     using Q = Tile<T, DP, BQ>;
     using Copy = Feed<T, DP, BQ>;
-    constexpr int kAhead = kAheadTiles<Q::kBytes>, kBuffers = kAhead + 1;
+    constexpr int kAhead = kAheadTiles<Q::kBytes, kDkvWaves<T, DP>>, kBuffers = kAhead + 1;
     __shared__ __align__(128) char lds[2 * kBuffers * Q::kBytes];      // buffers of queries, then of gradients
     __shared__ __align__(16) float lse[kBuffers][BQ], delta[kBuffers][BQ];
     const int64_t item = die_order(blockIdx.x, a.k_items);
