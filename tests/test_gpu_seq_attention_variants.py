@@ -13,7 +13,7 @@ F32, BF16 = torch.float32, torch.bfloat16
 
 # tiles of 128 keys x key heads: at least 256
 MANY = [
-    (BF16, 128, 128, 64, 100, 3, (130, 1), None, 0), (F32, 86, 86, 32, 50, 2, [0, 100, 101, 300], None, 1), (BF16, 128, 64, 128, 150, 4, (256, 2), None, 0),
+    (BF16, 128, 128, 64, 100, 3, (130, 1), None, 0), (F32, 86, 86, 32, 50, 2, [0, 100, 101, 300], None, 1), (BF16, 128, 64, 128, 150, 4, (512, 2), None, 0),
     (BF16, 128, 128, 80, 1000, 0, (256, 1), None, 0), (F32, 64, 64, 104, 33, 1, (512, 1), None, 0), (BF16, 64, 64, 184, 90, 5, (385, 1), None, 0),
     (F32, 64, 64, 160, 20, 0, (400, 1), None, 0), (BF16, 64, 64, 256, 129, 2, (400, 1), None, 0), (F32, 64, 64, 256, 64, 1, (390, 1), None, 0), (BF16, 130, 130, 32, 1, 0, (200, 1), None, 0),
 ]
