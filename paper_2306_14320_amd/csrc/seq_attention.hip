@@ -115,8 +115,12 @@ template <typename T, int DP> constexpr int kTileKeys = sizeof(T) == 2 && DP <= 
 // two that read each operand a step ahead); 96 channels, whose tiles are of 64
 // rows, and wider rows have registers for two, or one.
 template <typename T, int DP> constexpr int kFwdWaves = DP * sizeof(T) > 384 || DP >= 192 ? 1 : sizeof(T) == 2 && DP != 96 ? 3 : 2;
-// Whether the step's next rows wait in registers while some are worked on
-template <typename T, int DP> constexpr bool kStepAhead = DP * sizeof(T) <= 256;
+// The step: waves a SIMD, and whether the next rows wait in registers while
+// some are worked on (beside 1 KB of queries and outputs a lane they would spill).
+constexpr int step_waves(int row_bytes) { return row_bytes <= 128 ? 4 : row_bytes <= 256 ? 2 : 1; }
+template <typename T, int DP> constexpr bool kStepAhead = DP * sizeof(T) <= 512 && DP <= 192;
+// A wave's LDS for 32 rows: keys and values, or values in the place of keys
+template <typename T, int DP> constexpr int kStepStage = (kStepAhead<T, DP> ? 2 : 1) * Tile<T, DP, 32>::kBytes;
 
 // ---------------------------------------------------------------------------
 // Prompts and training: a workgroup takes up to 128 columns, the queries of
@@ -330,16 +334,16 @@ __global__ __launch_bounds__(kAttnThreads) void window_cache_kernel(AttnArgs a) 
 // ---------------------------------------------------------------------------
 // Single tokens: the columns are the heads of a request that share keys and
 // values; a workgroup takes a share of its cache's rows, each wave 32 of them at
-// a time.  Keys go straight to the operand's registers, values through the
-// wave's own part of LDS, which turns them.  The new token's row is read from
-// the inputs and written to the cache by the lanes that hold it.  Bound by memory.
+// a time, whole rows by neighbouring lanes, through its own part of LDS.  The
+// new token's row is read from the inputs and written to the cache by the lanes
+// that hold it.  Bound by memory.
 // ---------------------------------------------------------------------------
 template <typename T, int DP>
-__global__ __launch_bounds__(kAttnThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void window_step_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kAttnThreads, (step_waves(DP * sizeof(T)))) void window_step_kernel(AttnArgs a) {
     using V = Tile<T, DP, 32>;
-    constexpr int kRound = 32 * V::kChunks / kWave;      // chunks of a lane
+    constexpr int kRound = 32 * V::kChunks / kWave, NW = kAttnThreads / kWave;      // chunks of a lane; waves
     extern __shared__ __align__(16) char stage[];        // a.stage bytes of each wave
-    __shared__ float ml[4][2][kCols];
+    __shared__ float ml[NW][2][kCols];
     const int tid = threadIdx.x, wave = uniform(tid / kWave), lane = tid % kWave, half = lane / 32;
     const int blocks = a.q_heads / a.pack;
     const int split = blockIdx.x % a.splits, hb = blockIdx.x / a.splits % blocks, b = blockIdx.x / a.splits / blocks;
@@ -365,61 +369,64 @@ __global__ __launch_bounds__(kAttnThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void 
         if (16 * s + 8 * half < a.dim) q[s].load(qp + 16 * s + 8 * half);
         else q[s].zero();
     }
-    Frag<T> k[DP / 16];
-    Chunk v[kRound];
-    auto fetch_k = [&](int base) {
-        const int row = base + lane % 32;
-        const T* p = row == fresh ? kn : kc + row * step;
-#pragma unroll
-        for (int s = 0; s < DP / 16; ++s) {
-            if (row < to && 16 * s + 8 * half < a.dim) k[s].load(p + 16 * s + 8 * half);
-            else k[s].zero();
-        }
-    };
-    auto fetch_v = [&](int base) {
+    Chunk k[kRound], v[kRound];
+    auto fetch = [&](Chunk (&c)[kRound], int base, const T* cache, const T* now) {
 #pragma unroll
         for (int i = 0; i < kRound; ++i) {
             const int n = lane + i * kWave, rw = base + n / V::kChunks, e = n % V::kChunks * V::kElems;
-            if (rw < to && e < a.dim) v[i].load((rw == fresh ? vn : vc + rw * step) + e);
-            else v[i].zero();
+            if (rw < to && e < a.dim) c[i].load((rw == fresh ? now : cache + rw * step) + e);
+            else c[i].zero();
+        }
+    };
+    // to the wave's LDS; the new token's row to the cache too
+    auto put = [&](const Chunk (&c)[kRound], int base, char* lds, T* cache) {
+        const bool has_fresh = fresh >= base && fresh < base + 32;
+#pragma unroll
+        for (int i = 0; i < kRound; ++i) {
+            const int n = lane + i * kWave, rw = n / V::kChunks, e = n % V::kChunks * V::kElems;
+            if (has_fresh && base + rw == fresh && e < a.dim) c[i].store(cache + fresh * step + e);
+            c[i].store(lds + V::at(rw, n % V::kChunks));
         }
     };
     constexpr bool kAhead = kStepAhead<T, DP>;
+    const int rb = V::row_base(lane);
+    char* values = mine + kStepStage<T, DP> - V::kBytes;
     Running<DP> r;
     const int first = from + wave * 32;
-    if (kAhead && first < to) fetch_k(first), fetch_v(first);
-    for (int base = first; base < to; base += 128) {
-        if (!kAhead) fetch_k(base);
-        const bool has_fresh = fresh >= base && fresh < base + 32;      // the new token's row goes to the cache
-        if (has_fresh && base + lane % 32 == fresh) {
-#pragma unroll
-            for (int s = 0; s < DP / 16; ++s)
-                if (16 * s + 8 * half < a.dim) __builtin_memcpy(kc + fresh * step + 16 * s + 8 * half, &k[s].v, 8 * sizeof(T));
+    if (kAhead && first < to) {
+        fetch(k, first, kc, kn);
+        fetch(v, first, vc, vn);
+    }
+    for (int base = first; base < to; base += 32 * NW) {
+        if (!kAhead) fetch(k, base, kc, kn);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        put(k, base, mine, kc);
+        if (kAhead) put(v, base, values, vc);
+        else fetch(v, base, vc, vn);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (kAhead && base + 32 * NW < to) {
+            fetch(k, base + 32 * NW, kc, kn);
+            fetch(v, base + 32 * NW, vc, vn);
         }
         f32x16 s[1] = {f32x16{}};
 #pragma unroll
-        for (int d = 0; d < DP / 16; ++d) mma(s[0], k[d], q[d]);
-        if (!kAhead) fetch_v(base);
-#pragma unroll
-        for (int i = 0; i < kRound; ++i) {
-            const int n = lane + i * kWave, e = n % V::kChunks * V::kElems;
-            if (has_fresh && base + n / V::kChunks == fresh && e < a.dim) v[i].store(vc + fresh * step + e);
-            v[i].store(mine + V::at(n / V::kChunks, n % V::kChunks));
+        for (int d = 0; d < DP / 16; ++d) mma(s[0], V::row_frag(mine, rb, 0, d), q[d]);
+        if (!kAhead) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            put(v, base, values, vc);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
-        if (kAhead && base + 128 < to) fetch_k(base + 128), fetch_v(base + 128);
         if (base + 32 > to) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[0][i] = base + acc_row(i, half) < to ? s[0][i] : -INFINITY;
         }
         soften<DP, 1>(r, s, a.c);
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
             const Frag<T> w = weights<T>(s[0], part);
 #pragma unroll
-            for (int t = 0; t < DP / 32; ++t) mma(r.o[t], V::col_frag(mine, cb, t, part), w);
+            for (int t = 0; t < DP / 32; ++t) mma(r.o[t], V::col_frag(values, cb, t, part), w);
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
     // the four waves' shares: a channel's row of columns each, and their statistics
     r.l = half_sum(r.l);
@@ -435,11 +442,11 @@ __global__ __launch_bounds__(kAttnThreads, (DP * sizeof(T) > 256 ? 1 : 2)) void 
         const int c = n % a.pack, d = n / a.pack;
         float m = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w][0][c]);
+        for (int w = 0; w < NW; ++w) m = fmaxf(m, ml[w][0][c]);
         const float base = m == -INFINITY ? 0.0f : m;
         float sum = 0.0f, l = 0.0f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const float f = __builtin_amdgcn_exp2f(ml[w][0][c] - base);
             l = fmaf(ml[w][1][c], f, l);
             sum = fmaf(reinterpret_cast<const float*>(stage + w * a.stage)[d * a.pack + c], f, sum);
@@ -518,17 +525,18 @@ int check_cache(const im2win_window_desc* d, const void* k_cache, const void* v_
     return may_ptr(past, 4, "past");
 }
 
-// Shares of a request's rows: none where requests and heads fill the chip
-// twice over; else as many as do, of 128 rows (one round of the workgroup) at least.
+// Shares of a request's rows: as many as let requests and heads fill the
+// chip, of 128 rows (one round of the workgroup) at least.
 struct Split {
     int splits, rows;
 };
 Split split_of(const im2win_window_desc* d) {
     const int64_t blocks = d->tokens * (d->q_heads / heads_packed(d->q_heads, d->kv_heads)), rows = d->sinks + d->window;
-    int64_t n = blocks ? (512 + blocks - 1) / blocks : 1;
-    n = std::max<int64_t>(1, std::min(n, (rows + 127) / 128));
+    int64_t room = 256;
+    with_head(d->head_dim, [&](auto dp) { room = 256 * step_waves((int)(decltype(dp)::value * attn_size_of(d->dtype))); });
+    const int64_t n = std::max<int64_t>(1, std::min(blocks ? room / blocks : 1, (rows + 127) / 128));
     Split s{};
-    s.rows = (int)(((rows + n - 1) / n + 127) / 128 * 128);
+    s.rows = (int)(((rows + n - 1) / n + 31) / 32 * 32);
     s.splits = (int)((rows + s.rows - 1) / s.rows);
     return s;
 }
@@ -610,8 +618,8 @@ int im2win_window_attention_step(const im2win_window_desc* d, const void* q, con
         using T = decltype(t);
         with_head(d->head_dim, [&](auto dp) {
             constexpr int DP = decltype(dp)::value;
-            // a wave's values of 32 rows, and behind them its share of the outputs
-            a.stage = std::max(Tile<T, DP, 32>::kBytes, a.pack * DP * 4);
+            // a wave's keys and values of 32 rows, and behind them its share of the outputs
+            a.stage = std::max(kStepStage<T, DP>, a.pack * DP * 4);
             if (4 * a.stage > 65536)
                 attribute = hipFuncSetAttribute(reinterpret_cast<const void*>(&window_step_kernel<T, DP>), hipFuncAttributeMaxDynamicSharedMemorySize, 4 * a.stage);
             if (attribute == hipSuccess)
