@@ -425,8 +425,11 @@ Shape shape_of(const im2win_qk_desc* d) {
     return s;
 }
 
-// Workgroups of the gradients, whose waves walk the rows
-int64_t bwd_blocks(const Shape& s) { return std::min<int64_t>(s.blocks, 1024); }
+// Workgroups of the gradients, whose waves walk the rows: as many as run at
+// once (runs of eight pairs have registers for three waves a SIMD: 16384 rows of
+// 20 x 128 bf16 take 59 us with 768 workgroups, 73 with 1024, whose last quarter
+// runs alone; 4001 rows of 15 x 80 fp32 take 27 with 768 and 24 with 1024).
+int64_t bwd_blocks(const Shape& s) { return std::min<int64_t>(s.blocks, s.v == 8 ? 768 : 1024); }
 
 template <typename F>
 void with_shape(const im2win_qk_desc* d, const Shape& s, F f) {
