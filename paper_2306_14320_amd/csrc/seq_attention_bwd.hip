@@ -61,6 +61,8 @@ __device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int 
     return f;
 }
 
+// Rows of the keys' kernel's tiles of queries (of 128 bf16 channels 32: 863 us a
+// training step against 875 with 64; the queries' kernel's tiles of keys: 875 and 863)
 template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 96 ? 64 : 32;
 template <typename T, int DP> constexpr int kDqWaves = DP * sizeof(T) > 256 ? 1 : 2;
 template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 256 ? 1 : 2;
@@ -70,7 +72,7 @@ template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 256 ? 1
 // ---------------------------------------------------------------------------
 template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_kernel(AttnBwdArgs a) {
-    constexpr int BK = kTileRows<T, DP>, NB = BK / 32;
+    constexpr int BK = sizeof(T) == 2 && DP <= 128 ? 64 : 32, NB = BK / 32;
     using KV = Tile<T, DP, BK>;
     using Copy = Feed<T, DP, BK>;
     constexpr int kAhead = kAheadTiles<KV::kBytes, kDqWaves<T, DP>>, kBuffers = kAhead + 1;
@@ -249,11 +251,13 @@ struct Keys {
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
             const Frag<T> w = operand<T>(s, part), ds = operand<T>(dp, part);
+            __builtin_amdgcn_s_setprio(1);      // products first; keeps the exponentials in front of them (1000 tokens of 16 x 128: 168 -> 141 us)
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {
                 mma(dv[d], Q::col_frag(lds, cb + gt, d, 2 * b + part), w);
                 mma(dk[d], Q::col_frag(lds, cb + qt, d, 2 * b + part), ds);
             }
+            __builtin_amdgcn_s_setprio(0);
         }
     }
 };
