@@ -64,6 +64,7 @@ __device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int 
 // Rows of the keys' kernel's tiles of queries (of 128 bf16 channels 32: 863 us a
 // training step against 875 with 64; the queries' kernel's tiles of keys: 875 and 863)
 template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 96 ? 64 : 32;
+constexpr int kWalkTwice = 2;      // tiles of keys
 template <typename T, int DP> constexpr int kDqWaves = DP * sizeof(T) > 256 ? 1 : 2;
 template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 256 ? 1 : 2;
 
@@ -125,53 +126,75 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
     const int lead = first_end > 0 ? 1 : 0, count = lead + (end - begin + BK - 1) / BK;
     auto base_of = [&](int i) { return i < lead ? 0 : begin + (i - lead) * BK; };
     auto stop_of = [&](int i) { return i < lead ? first_end : end; };
-    for (int i = 0; i < kAhead && i < count; ++i) issue(i, base_of(i), stop_of(i));
-    int buffer = 0;
+    // delta comes from the y that was rounded, which shows where few keys are
+    // seen: there a first walk finds what ds sums to over the keys, zero but for
+    // delta's error, and corrects it
     float rest = 0.0f;
-    for (int n = 0; n < count; ++n) {
-        const bool sink_tile = n < lead;
-        const int now = base_of(n), now_stop = stop_of(n), newest = n + kAhead - 1;
-        arrived<2 * Copy::kPasses>(kAhead == 2 && newest < count && a.dim == DP && base_of(newest) + BK <= stop_of(newest));
-        const int before = buffer ? buffer - 1 : kBuffers - 1;
-        if (n + kAhead < count) issue(before, base_of(n + kAhead), stop_of(n + kAhead));
-        const int kb = rb + buffer * KV::kBytes, kc = cb + buffer * KV::kBytes, vb = rb + (kBuffers + buffer) * KV::kBytes;
-        buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
-        if (now > wq1 || (now + BK <= wq0 - a.window + 1 && now >= a.sinks)) continue;
-        const bool whole = !sink_tile && now >= a.sinks && now + BK - 1 <= wq0 && now > wq1 - a.window;
+    for (int walk = sizeof(T) == 2 && count <= kWalkTwice ? 0 : 1; walk < 2; ++walk) {
+        for (int i = 0; i < kAhead && i < count; ++i) issue(i, base_of(i), stop_of(i));
+        int buffer = 0;
+        for (int n = 0; n < count; ++n) {
+            const bool sink_tile = n < lead;
+            const int now = base_of(n), now_stop = stop_of(n), newest = n + kAhead - 1;
+            arrived<2 * Copy::kPasses>(kAhead == 2 && newest < count && a.dim == DP && base_of(newest) + BK <= stop_of(newest));
+            const int before = buffer ? buffer - 1 : kBuffers - 1;
+            if (n + kAhead < count) issue(before, base_of(n + kAhead), stop_of(n + kAhead));
+            const int kb = rb + buffer * KV::kBytes, kc = cb + buffer * KV::kBytes, vb = rb + (kBuffers + buffer) * KV::kBytes;
+            buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
+            if (now > wq1 || (now + BK <= wq0 - a.window + 1 && now >= a.sinks)) continue;
+            const bool whole = !sink_tile && now >= a.sinks && now + BK - 1 <= wq0 && now > wq1 - a.window;
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            f32x16 s = {}, dp = {};
+            for (int b = 0; b < NB; ++b) {
+                f32x16 s = {}, dp = {};
 #pragma unroll
-            for (int d = 0; d < DP / 16; ++d) {
-                mma(s, KV::row_frag(lds, kb, b, d), q[d]);
-                mma(dp, KV::row_frag(lds, vb, b, d), g[d]);
-            }
+                for (int d = 0; d < DP / 16; ++d) {
+                    mma(s, KV::row_frag(lds, kb, b, d), q[d]);
+                    mma(dp, KV::row_frag(lds, vb, b, d), g[d]);
+                }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -lse)) * (dp[i] - delta);
-            if (!whole) {
-                const int low = pos - a.window + 1 - now - 4 * half, high = now_stop - now - 4 * half;
-                if (sink_tile) {
+                for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], a.c, -lse)) * (dp[i] - delta);
+                if (!whole) {
+                    const int low = pos - a.window + 1 - now - 4 * half, high = now_stop - now - 4 * half;
+                    if (sink_tile) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = 32 * b + acc_row(i, 0) < high ? s[i] : 0.0f;
-                } else if (now >= a.sinks) {
+                        for (int i = 0; i < 16; ++i) s[i] = 32 * b + acc_row(i, 0) < high ? s[i] : 0.0f;
+                    } else if (now >= a.sinks) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) s[i] = (uint32_t)(32 * b + acc_row(i, 0) - low) < (uint32_t)a.window && !single ? s[i] : 0.0f;
-                } else {
+                        for (int i = 0; i < 16; ++i) s[i] = (uint32_t)(32 * b + acc_row(i, 0) - low) < (uint32_t)a.window && !single ? s[i] : 0.0f;
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int p = now + 32 * b + acc_row(i, half);
-                        s[i] = p <= pos && (p > pos - a.window || p < a.sinks) && !single ? s[i] : 0.0f;
+                        for (int i = 0; i < 16; ++i) {
+                            const int p = now + 32 * b + acc_row(i, half);
+                            s[i] = p <= pos && (p > pos - a.window || p < a.sinks) && !single ? s[i] : 0.0f;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) rest += s[i];
+                if (walk == 0) continue;
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    const Frag<T> w = operand<T>(s, part);
+                    // what the rounding of ds to bf16 leaves goes the same way: dq then
+                    // keeps its own rounding's error alone (half as much again before)
+                    Frag<T> low;
+                    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) low.set(i, s[8 * part + i] - w.get(i));
+                    }
+#pragma unroll
+                    for (int d = 0; d < DP / 32; ++d) {
+                        const Frag<T> f = KV::col_frag(lds, kc, d, 2 * b + part);
+                        mma(o[d], f, w);
+                        if constexpr (sizeof(T) == 2) mma(o[d], f, low);
                     }
                 }
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) rest += s[i];
-#pragma unroll
-            for (int part = 0; part < 2; ++part) {
-                const Frag<T> w = operand<T>(s, part);
-#pragma unroll
-                for (int d = 0; d < DP / 32; ++d) mma(o[d], KV::col_frag(lds, kc, d, 2 * b + part), w);
-            }
+        }
+        if (walk == 0) {
+            delta += half_sum(rest);
+            rest = 0.0f;
+            __syncthreads();
         }
     }
     // ds sums to zero over the keys: what it sums to is what delta is off by, from the rounded y
