@@ -10,10 +10,20 @@
 //  - keys' tiles walk the queries of all their heads that see them by the
 //    window (dk, dv);
 //  - the first tokens' keys are seen by all queries behind: those pairs, cut
-//    into pieces of 512 queries, leave partial sums, which the tile of the
+//    into pieces of queries, leave partial sums, which the tile of the
 //    sequence's first keys adds (launched before it).
 // Scores are computed twice: seven products of queries and keys where five
-// would do, against a sum of dq over the keys' tiles in memory.
+// would do (eight in bf16, where dq takes ds in two parts), against a sum of dq
+// over the keys' tiles in memory.
+//
+// 16384 tokens of 16 heads over 4, 128 bf16 channels, window 1024, 4 first
+// tokens: 325 us for dq, 46 for the first tokens' keys, 406 for dk and dv; the
+// products of all pairs in sight, at the rate of a large one, would take 215, 1
+// and 215.  The
+// operands' way out of LDS and the exponentials bound them: matrix cores are
+// busy for a third of the time, and waves wait for LDS for half of theirs.
+// 2503 tokens of 6 heads over 2, 96 fp32 channels, window 201: 56, 31 and 59 us, latency of
+// few workgroups.
 #include "seq_attention.h"
 
 #include <algorithm>
@@ -61,10 +71,16 @@ __device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int 
     return f;
 }
 
-// Rows of the keys' kernel's tiles of queries (of 128 bf16 channels 32: 863 us a
-// training step against 875 with 64; the queries' kernel's tiles of keys: 875 and 863)
+// Rows of the keys' kernel's tiles of queries: of 128 bf16 channels 32 (a training
+// step of 16384 tokens: 863 us, 875 with 64).  The queries' kernel's tiles of
+// keys are of 64 rows there (863 us, 875 with 32).
 template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 96 ? 64 : 32;
-constexpr int kWalkTwice = 2;      // tiles of keys
+// Up to this many tiles of keys the queries walk them twice.  The correction
+// matters where a row sees some ten keys, and costs the walk again: 128 tokens of
+// 16 x 128 52 -> 59 us; more than two tiles, and so all long sequences, pay none.
+constexpr int kWalkTwice = 2;
+// Waves a SIMD: two where the operands leave registers for two (dk and dv of 16384
+// tokens of 16 x 128 bf16: a training step 881 us, 921 with one)
 template <typename T, int DP> constexpr int kDqWaves = DP * sizeof(T) > 256 ? 1 : 2;
 template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 256 ? 1 : 2;
 
@@ -176,7 +192,8 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
                 for (int part = 0; part < 2; ++part) {
                     const Frag<T> w = operand<T>(s, part);
                     // what the rounding of ds to bf16 leaves goes the same way: dq then
-                    // keeps its own rounding's error alone (half as much again before)
+                    // keeps its own rounding's error alone (half as much again before;
+                    // 40 us of a training step's 905)
                     Frag<T> low;
                     if constexpr (sizeof(T) == 2) {
 #pragma unroll
@@ -433,13 +450,13 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
 //  - otherwise dk and dv of small problems, whose tiles of 128 keys would leave
 //    the chip idle: four times the workgroups, and the queries' walk is shared
 //    by four waves.
+// A block's rows come from memory as it begins: with the next one's in registers
+// meanwhile 1000 tokens of 16 x 128 take 149 us, not 144, of 8 x 256 bf16 315, not 257.
 // ---------------------------------------------------------------------------
 template <typename T, int DP> constexpr int kNarrowOwn = 2 * Tile<T, DP, 32>::kBytes + 256;      // a wave's queries, gradients, lse and delta
 template <typename T, int DP> constexpr int kNarrowWaves = 4 * kNarrowOwn<T, DP> > 160 * 1024 ? 2 : 4;
 template <typename T, int DP>
 constexpr int kNarrowLds = kNarrowWaves<T, DP> * (kNarrowOwn<T, DP> > 32 * 33 * 4 ? kNarrowOwn<T, DP> : 32 * 33 * 4);
-
-template <typename T, int DP> constexpr bool kNarrowAhead = DP * sizeof(T) <= 256;
 
 template <typename T, int DP, bool FIRST>
 __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 128 ? 1 : 2)) void window_narrow_kernel(AttnBwdArgs a) {
@@ -467,7 +484,6 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
               static_cast<const T*>(a.v) + (int64_t)(st.first + key) * a.ld_v + (int64_t)kvh * a.dim, half, a.dim, live);
     const int blocks = (end - from + 31) / 32;
     const int64_t count = (int64_t)blocks * group;
-    // a block's rows wait in registers while the one before it is worked on
     Chunk x[kRound], g[kRound];
     float lr = 0.0f, er = 0.0f;
     auto fetch = [&](int64_t n) {
@@ -488,10 +504,9 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
         lr = a.lse[at] * kLog2e;
         er = a.delta[at];
     };
-    if (kNarrowAhead<T, DP> && wave < count) fetch(wave);
     for (int64_t n = wave; n < count; n += NW) {
         const int base = from + (int)(n % blocks) * 32;
-        if (!kNarrowAhead<T, DP>) fetch(n);
+        fetch(n);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int i = 0; i < kRound; ++i) {
@@ -501,7 +516,6 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
         }
         if (lane < 32) lse[lane] = lr, delta[lane] = er;
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        if (kNarrowAhead<T, DP> && n + NW < count) fetch(n + NW);
         if constexpr (FIRST) {
             keys.template take<32>(own, 0, Q::kBytes, lse, delta, 0, base, false, a.c,
                                    [&](int p) { return p < end && key < a.sinks && p - key >= a.window; }, [](int) { return false; });
@@ -552,12 +566,19 @@ void with_type(int32_t dtype, F f) {
     else f(bf16{});
 }
 
+// Tiles of 128 keys that would leave CUs idle go to the narrow kernel: 2503 tokens
+// of 2 heads fp32 (40 tiles) 368 -> 209 us, 1000 tokens of 4 heads bf16 (32) 261 ->
+// 176.  Where they fill the chip they are faster: 16096 tokens of 4 heads (504) 376
+// us, 513 in the narrow kernel.
 constexpr int64_t kNarrowBelow = 256;
 
 // Pieces of queries that may see first tokens outside of their window: none
 // where no sequence can be longer than the window.
 int64_t piece_rows(const im2win_window_desc* d) {
-    const int64_t rows = (d->tokens * d->kv_heads / 1024 + 127) / 128 * 128;      // some 1024 workgroups, of whole rounds of their waves
+    // some 1024 workgroups, of whole rounds of their waves (512 rows whatever the
+    // problem: 1000 tokens 181 us, not 144, 2503 of 2 heads fp32 261, not 188,
+    // 16384 of 4 heads 921, not 906)
+    const int64_t rows = (d->tokens * d->kv_heads / 1024 + 127) / 128 * 128;
     return std::max<int64_t>(128, std::min<int64_t>(rows, 4096));
 }
 int64_t pieces_of(const im2win_window_desc* d, const int32_t* starts) {

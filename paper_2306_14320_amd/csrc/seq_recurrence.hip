@@ -14,7 +14,12 @@
 // wave), composes them, leaves the chunk's pair for the workgroups behind it,
 // composes the pairs of the chunks in front, and applies the state that enters
 // to its registers: every input is read once and every output written once.
-// Bound by memory.
+//
+// Forward, 8192 rows of 2048 bf16 channels in one sequence: 48.7 us with the kernel
+// that prepares the words, 2.8 TB/s over what has to move (a copy: 5.1); the vector
+// units are busy for 58%, and the wait for the chunks in front takes the rest.
+// Gradients, 16384 rows of 4096 in 8 sequences: 283 us, 3.7 TB/s, vector units 73%
+// busy; the forward call that leaves their states 142 us, 4.2 TB/s.
 //
 // The first row of a sequence does not look back: its pair is marked by a
 // negative a (the decays are positive), and composing selects instead of
@@ -26,14 +31,20 @@
 namespace im2win {
 namespace {
 
-constexpr int kRows = 16;                 // rows a wave holds in registers
-constexpr int kBwdRows = 8;               // in the gradients, which hold twice as much of each
+// Rows a wave holds in registers, by waves a workgroup: 16 x 8 rows take 59 us on the
+// long prompt (before the gates took fewer instructions), 8 x 8 65, 8 x 16 and 16 x 4 67.
+constexpr int kRows = 16;
+// In the gradients, which hold twice as much of each: a training step 410 us, 444
+// with 16 rows.
+constexpr int kBwdRows = 8;
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kWave;
 constexpr int kChunk = kRows * kWaves;    // rows of a workgroup
 constexpr int kBwdChunk = kBwdRows * kWaves;
 template <int R> constexpr uint32_t kAllRows = (1u << R) - 1;
-constexpr int kGroup = 32;                // chunks whose pairs are looked at one by one
+// Chunks whose pairs are looked at one by one, behind the last whole group's state:
+// the long prompt takes 50 us and a training step 410; with groups of 64 54 and 517.
+constexpr int kGroup = 32;
 constexpr int kLook = kGroup / kWaves;    // of those, the ones a wave looks at
 constexpr float kReset = -1.0f;           // the a of a pair that does not look back
 constexpr float kLog2e = 1.44269504088896f;
