@@ -1,7 +1,9 @@
 """Binding of the operators of hybrid sequence layers of ``libim2win.so``
 (``include/im2win_seq.h``): the gated linear recurrence, its gradients and its
-form for single tokens, and the norm of queries and keys for each head with
-the position rotation and its gradients.
+form for single tokens; the norm of queries and keys for each head with the
+position rotation and its gradients; and window attention with first tokens
+that stay visible, its gradients and its form for single tokens out of a ring
+cache.
 
 Conventions are those of ``sequence.py``: the ``im2win_*`` functions mirror
 the C entry points and take device pointers, the tensor helpers check every
