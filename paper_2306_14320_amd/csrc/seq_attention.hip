@@ -98,7 +98,7 @@ __device__ __forceinline__ void soften(Running<DP>& r, f32x16 (&s)[NB], float c)
 }
 
 // The weights of 16 keys as a right operand: rounded to bf16 where the values
-// are, as their products' operand (2^-9 of a weight, against 2^-9 of a value).
+// are, as their products' operand (off by 2^-8 at most, as a value that was rounded is).
 template <typename T>
 __device__ __forceinline__ Frag<T> weights(const f32x16& s, int part) {
     Frag<T> f;
@@ -254,11 +254,11 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
         if (n + kAhead < count) issue(before, base_of(n + kAhead), stop_of(n + kAhead));
         const int kb = rb + buffer * KV::kBytes, vb = cb + (kBuffers + buffer) * KV::kBytes;
         buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
-        // keys in front of the wave's first window (but for sinks) or behind its last query
-        if (now > wq1 || (now + BK <= wq0 - a.window + 1 && now >= a.sinks)) continue;
-
 #pragma unroll
         for (int b = 0; b < NB; ++b) {      // 32 keys at a time
+            // those in front of the wave's first window (but for sinks) or behind its last query
+            const int from = now + 32 * b;
+            if (from > wq1 || (from + 32 <= wq0 - a.window + 1 && from >= a.sinks) || (b && sink_tile)) continue;
             f32x16 s[1] = {f32x16{}};
 #pragma unroll
             for (int d = 0; d < DP / 16; ++d) mma(s[0], KV::row_frag(lds, kb, b, d), q[d]);
@@ -272,7 +272,7 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
                     const int p = now + 32 * b + acc_row(i, half);
                     s[0][i] = p <= pos && (p > pos - a.window || p < a.sinks) ? s[0][i] : -INFINITY;
                 }
-            } else if (!(now + BK - 1 <= wq0 && now > wq1 - a.window)) {      // pos - window < p <= pos
+            } else if (!(from + 31 <= wq0 && from > wq1 - a.window)) {      // pos - window < p <= pos
                 const int low = pos - a.window + 1 - now - 4 * half;
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[0][i] = (uint32_t)(32 * b + acc_row(i, 0) - low) < (uint32_t)a.window ? s[0][i] : -INFINITY;

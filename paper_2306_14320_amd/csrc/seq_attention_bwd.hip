@@ -157,10 +157,12 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
             if (n + kAhead < count) issue(before, base_of(n + kAhead), stop_of(n + kAhead));
             const int kb = rb + buffer * KV::kBytes, kc = cb + buffer * KV::kBytes, vb = rb + (kBuffers + buffer) * KV::kBytes;
             buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
-            if (now > wq1 || (now + BK <= wq0 - a.window + 1 && now >= a.sinks)) continue;
-            const bool whole = !sink_tile && now >= a.sinks && now + BK - 1 <= wq0 && now > wq1 - a.window;
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
+                // 32 keys that all of the wave's queries see, or none
+                const int from = now + 32 * b;
+                if (from > wq1 || (from + 32 <= wq0 - a.window + 1 && from >= a.sinks) || (b && sink_tile)) continue;
+                const bool whole = !sink_tile && from >= a.sinks && from + 31 <= wq0 && from > wq1 - a.window;
                 f32x16 s = {}, dp = {};
 #pragma unroll
                 for (int d = 0; d < DP / 16; ++d) {
