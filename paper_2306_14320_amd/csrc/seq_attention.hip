@@ -9,11 +9,10 @@
 // the request had before the call come from its cache, a ring of sinks +
 // window rows, in which the call leaves the new tokens' keys and values.
 //
-// 16384 tokens of 16 heads over 4, 128 bf16 channels, window 1024: 195 us, whose two
-// products would take 107 at the rate of a large one; 225 where lse is left too
-// and each set of inputs is new to the caches.  9001 tokens of 12 heads over 4, 64
-// channels, window 500, 13 ragged prompts: 51 us (11 for the products), and 6 for
-// the caches.  Waves wait for LDS for half of their time, the vector units are busy
+// 16384 tokens of 16 heads over 4, 128 bf16 channels, window 1024: 199 us, 206 in
+// front of the gradients, whose two products would take 107 at the rate of a large one.
+// 9001 tokens of 12 heads over 4, 64 channels, window 500, 13 ragged prompts: 41 us
+// (11 for the products) with the 6 for the caches.  Waves wait for LDS for half of their time, the vector units are busy
 // for half of it and the matrix cores for 30%: exponentials, maximum and sum of
 // 64 channels' scores take longer than their products.
 #include "seq_attention.h"
@@ -117,16 +116,17 @@ __device__ __forceinline__ void put4(bf16* p, float a, float b, float c, float d
     __builtin_memcpy(p, v, 8);
 }
 
-// Keys of a tile.  9001 tokens of 12 heads of 64 channels take 55 us with 64 keys, 57 with
-// 32, but 16384 of 16 heads of 128 channels 388 and 207: two buffers of 64 such rows
+// Keys of a tile.  9001 tokens of 12 heads of 64 channels took 55 us with 64 keys, 57 with
+// 32, at three waves, but 16384 of 16 heads of 128 channels 388 and 207: two buffers of 64 such rows
 // leave LDS for two workgroups.  (32 rows of 32 or 96 channels are no whole number of
 // copies by all threads.)
 template <typename T, int DP> constexpr int kTileKeys = sizeof(T) == 2 && DP <= 96 ? 64 : 32;
-// Waves a SIMD.  Up to 128 channels of bf16 three hide the waits for LDS best
-// (16384 tokens of 16 x 128, window 1024: 195 us, 214 with two waves, and 217 with
-// two that read each operand a step ahead); 96 channels, whose tiles are of 64
-// rows, and wider rows have registers for two, or one.
-template <typename T, int DP> constexpr int kFwdWaves = DP * sizeof(T) > 384 || DP >= 192 ? 1 : sizeof(T) == 2 && DP != 96 ? 3 : 2;
+// Waves a SIMD.  Of 128 channels of bf16 three hide the waits for LDS best (16384 tokens
+// of 16 heads, window 1024, before blocks were left out: 195 us, 214 with two waves, 217
+// with two that read each operand a step ahead), of 64 and fewer four (9001 tokens of
+// 12 heads: 45 us, 52 with three); of 96 three gain nothing over two, and wider rows
+// have registers for two, or one.
+template <typename T, int DP> constexpr int kFwdWaves = DP * sizeof(T) > 384 || DP >= 192 ? 1 : sizeof(T) == 2 && DP != 96 ? (DP > 64 ? 3 : 4) : 2;
 // The step: waves a SIMD, and whether the next rows wait in registers while
 // some are worked on (beside 1 KB of queries and outputs a lane they would spill).
 constexpr int step_waves(int row_bytes) { return row_bytes <= 128 ? 4 : row_bytes <= 256 ? 2 : 1; }

@@ -17,12 +17,12 @@
 // over the keys' tiles in memory.
 //
 // 16384 tokens of 16 heads over 4, 128 bf16 channels, window 1024, 4 first
-// tokens: 325 us for dq, 46 for the first tokens' keys, 406 for dk and dv; the
+// tokens: 315 us for dq, 45 for the first tokens' keys, 413 for dk and dv; the
 // products of all pairs in sight, at the rate of a large one, would take 215, 1
 // and 215.  The
 // operands' way out of LDS and the exponentials bound them: matrix cores are
 // busy for a third of the time, and waves wait for LDS for half of theirs.
-// 2503 tokens of 6 heads over 2, 96 fp32 channels, window 201: 56, 31 and 59 us, latency of
+// 2503 tokens of 6 heads over 2, 96 fp32 channels, window 201: 54, 32 and 60 us, latency of
 // few workgroups.
 #include "seq_attention.h"
 
@@ -79,9 +79,13 @@ template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 
 // matters where a row sees some ten keys, and costs the walk again: 128 tokens of
 // 16 x 128 52 -> 59 us; more than two tiles, and so all long sequences, pay none.
 constexpr int kWalkTwice = 2;
-// Waves a SIMD: two where the operands leave registers for two (dk and dv of 16384
-// tokens of 16 x 128 bf16: a training step 881 us, 921 with one)
-template <typename T, int DP> constexpr int kDqWaves = DP * sizeof(T) > 256 ? 1 : 2;
+// Waves a SIMD, of dq by its registers (training steps: 16384 tokens of 16 x 64 bf16
+// 304 us with three waves, 313 with two; 8192 tokens of 16 heads of 32 fp32 498 with two,
+// 517 with three, of 96 fp32 1187 with two, 1246 with one, of 128 fp32 1605 and 1655,
+// of 192 bf16 605 and 590), of dk and dv fewer, which hold the sums of both (16 x 128
+// bf16 881 with two, 921 with one; 16 x 64 bf16 297 with two, 326 with three; 96 fp32
+// 1190 with one, 1403 with two; 192 bf16 605 and 1235).
+template <typename T, int DP> constexpr int kDqWaves = DP > 128 ? 1 : sizeof(T) == 2 && DP <= 64 ? 3 : 2;
 template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 256 ? 1 : 2;
 
 // ---------------------------------------------------------------------------
@@ -159,7 +163,8 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
             buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                // 32 keys that all of the wave's queries see, or none
+                // 32 keys that all of the wave's queries see, or none (taken tile by
+                // tile instead, a training step of 16384 tokens took 937 us, not 908)
                 const int from = now + 32 * b;
                 if (from > wq1 || (from + 32 <= wq0 - a.window + 1 && from >= a.sinks) || (b && sink_tile)) continue;
                 const bool whole = !sink_tile && from >= a.sinks && from + 31 <= wq0 && from > wq1 - a.window;
@@ -407,10 +412,10 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
         const int qt = buffer * Q::kBytes, gt = (kBuffers + buffer) * Q::kBytes;
         const float *ls = lse[buffer], *de = delta[buffer];
         buffer = buffer + 1 < kBuffers ? buffer + 1 : 0;
-        const bool whole = at + BQ <= end && k1 <= at && at + BQ - 1 - k0 < a.window;
         for (int b = 0; b < NB; ++b) {
             const int p0 = at + 32 * b, p1 = p0 + 31;
             if (p0 >= end || p1 < k0 || p0 - k1 >= a.window) continue;
+            const bool whole = p1 < end && k1 <= p0 && p1 - k0 < a.window;
             keys.template take<BQ>(
                 lds, qt, gt, ls, de, b, at, whole, a.c, [&](int p) { return p < end && p >= key && p - key < a.window; },
                 [&](int p) { return p == 0 || (a.window == 1 && a.sinks == 0); });
