@@ -395,7 +395,8 @@ typedef struct {
  *            outside of [0, cache_slots) gets y = 0 and leaves the cache as it is.
  *   y        device, T x H x head_dim
  *   lse      device, T x H, fp32, or NULL: log of the sum of exp(scale q . k) (-inf
- *            without visible keys), for the gradients
+ *            for a request without a slot), for the gradients
+ * Where all of a query's scores are -inf, y is NaN and lse -inf, as the formula has it.
  * Errors: EINVAL, ENULL, EALIGN, EOVERFLOW, EHIP.
  */
 int im2win_window_attention(const im2win_window_desc* d, const void* q, const void* k, const void* v,

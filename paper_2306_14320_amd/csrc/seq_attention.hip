@@ -307,7 +307,9 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
     }
     const float l = half_sum(r.l);
     if (!live) return;
-    const float scale = l == 0.0f ? 0.0f : 1.0f / l;      // without a visible key: zeros
+    // A query sees itself, so a served one's l is zero only where all of its scores are
+    // -inf: 0 / 0 then, as the softmax has it.
+    const float scale = served ? 1.0f / l : 0.0f;
     const int64_t t = st.first + row;
     T* y = static_cast<T*>(a.y) + (t * a.q_heads + head) * a.dim;
 #pragma unroll
@@ -468,7 +470,7 @@ __global__ __launch_bounds__(kAttnThreads, (step_waves(DP * sizeof(T)))) void wi
         }
         const int64_t at = (int64_t)b * a.q_heads + h0 + c;
         if (a.splits == 1) {
-            static_cast<T*>(a.y)[at * a.dim + d] = (T)(l == 0.0f ? 0.0f : sum / l);
+            static_cast<T*>(a.y)[at * a.dim + d] = (T)(served ? sum / l : 0.0f);
         } else {
             a.part_o[(at * a.splits + split) * a.dim + d] = sum;
             if (d == 0) a.part_ml[(at * a.splits + split) * 2] = m, a.part_ml[(at * a.splits + split) * 2 + 1] = l;
@@ -507,7 +509,9 @@ __global__ __launch_bounds__(kAttnThreads) void window_step_join_kernel(AttnArgs
     }
 #pragma unroll
     for (int x = 1; x < kWave; x *= 2) l += __shfl_xor(l, x);
-    const float scale = l == 0.0f ? 0.0f : 1.0f / l;
+    const int b = uniform((int)(at / a.q_heads));
+    const int64_t slot = a.slots ? uniform(a.slots[b]) : b;
+    const float scale = slot >= 0 && slot < a.cache_slots ? 1.0f / l : 0.0f;
     if (4 * lane < a.dim) put4(static_cast<T*>(a.y) + at * a.dim + d, o[0] * scale, o[1] * scale, o[2] * scale, o[3] * scale);
 }
 
