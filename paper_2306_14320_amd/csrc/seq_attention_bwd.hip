@@ -75,10 +75,11 @@ __device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int 
 // step of 16384 tokens: 863 us, 875 with 64).  The queries' kernel's tiles of
 // keys are of 64 rows there (863 us, 875 with 32).
 template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 96 ? 64 : 32;
-// Up to this many tiles of keys the queries walk them twice.  The correction
-// matters where a row sees some ten keys, and costs the walk again: 128 tokens of
-// 16 x 128 52 -> 59 us; more than two tiles, and so all long sequences, pay none.
-constexpr int kWalkTwice = 2;
+// Queries that see fewer keys than this walk them twice: all of them with windows
+// below it, otherwise the first workgroups of each sequence.  Without the
+// correction, the error of dq is 1.95 times its own rounding's where two keys are
+// seen, 1.25 where eight are, 1.10 where 24 are and under 1.06 from 64 on.
+constexpr int kFewKeys = 64;
 // Waves a SIMD, of dq by its registers (training steps: 16384 tokens of 16 x 64 bf16
 // 304 us with three waves, 313 with two; 8192 tokens of 16 heads of 32 fp32 498 with two,
 // 517 with three, of 96 fp32 1187 with two, 1246 with one, of 128 fp32 1605 and 1655,
@@ -150,7 +151,8 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
     // seen: there a first walk finds what ds sums to over the keys, zero but for
     // delta's error, and corrects it
     float rest = 0.0f;
-    for (int walk = sizeof(T) == 2 && count <= kWalkTwice ? 0 : 1; walk < 2; ++walk) {
+    const bool few = st.row + 1 < kFewKeys || a.window + a.sinks < kFewKeys;      // keys of the tile's first query
+    for (int walk = sizeof(T) == 2 && few ? 0 : 1; walk < 2; ++walk) {
         for (int i = 0; i < kAhead && i < count; ++i) issue(i, base_of(i), stop_of(i));
         int buffer = 0;
         for (int n = 0; n < count; ++n) {
