@@ -425,8 +425,8 @@ int im2win_window_attention_backward_workspace_bytes(const im2win_window_desc* d
 
 /*
  * Gradients of im2win_window_attention without a cache, for dy (dense), with
- * the y and lse that the forward call wrote.  An infinity or a NaN reaches
- * gradients of its own sequence only (there, of masked places too).
+ * the y and lse that the forward call wrote.  A masked pair does not enter:
+ * an infinity or a NaN reaches what the formulas over the pairs in sight give it.
  *   dq          device, T x H x head_dim, dense
  *   dk, dv      device, T x K x head_dim, dense
  *   workspace   device, 16-byte aligned, at least the bytes above

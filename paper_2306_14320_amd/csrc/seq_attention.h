@@ -252,6 +252,21 @@ __device__ __forceinline__ void drop_nonfinite(Chunk& c) {
     }
 }
 
+template <typename T>
+__device__ __forceinline__ bool finite(T x) {
+    return (__float_as_uint((float)x) & 0x7f800000u) != 0x7f800000u;
+}
+// Whether one of a lane's sums is not finite
+template <int N>
+__device__ __forceinline__ bool nonfinite(const f32x16 (&o)[N]) {
+    float z = 0.0f;      // zero times a finite value is zero
+#pragma unroll
+    for (int t = 0; t < N; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) z = fmaf(o[t][i], 0.0f, z);
+    return !(z == 0.0f);
+}
+
 // ---------------------------------------------------------------------------
 // Tiles of `rows` rows of the sequences.  The host does not know the
 // sequences' lengths, so sequence b owns the places first(b) / rows + b and

@@ -48,11 +48,6 @@ __device__ __forceinline__ int past_of(const int32_t* past, int b) {
 // The row of position p in a request's cache
 __device__ __forceinline__ int ring(int p, int window, int sinks) { return p < sinks ? p : sinks + (p - sinks) % window; }
 
-template <typename T>
-__device__ __forceinline__ bool finite(T x) {
-    return (__float_as_uint((float)x) & 0x7f800000u) != 0x7f800000u;
-}
-
 // Running softmax of a lane's column and its output
 template <int DP>
 struct Running {

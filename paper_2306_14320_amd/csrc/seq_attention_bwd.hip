@@ -3,7 +3,7 @@
 //   ds = w (dp - delta),  dq = scale sum_j ds k_j,
 //   dk = scale sum_t ds q_t,  dv = sum_t w dy_t.
 // A query that sees one key alone has w = 1 whatever its score: its ds is zero,
-// and taken as such.
+// and taken as such where it is finite.
 //
 // Three kernels, none of which stores scores or adds atomically:
 //  - queries' tiles walk their visible keys (dq, and delta for the others);
@@ -12,6 +12,9 @@
 //  - the first tokens' keys are seen by all queries behind: those pairs, cut
 //    into pieces of queries, leave partial sums, which the tile of the
 //    sequence's first keys adds (launched before it).
+// The matrix products multiply an infinity or a NaN in a masked place by zero:
+// where results are not finite, a wave computes them again from the pairs in
+// sight alone.
 // Scores are computed twice: seven products of queries and keys where five
 // would do (eight in bf16, where dq takes ds in two parts), against a sum of dq
 // over the keys' tiles in memory.
@@ -90,6 +93,132 @@ template <typename T, int DP> constexpr int kDqWaves = DP > 128 ? 1 : sizeof(T) 
 template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 256 ? 1 : 2;
 
 // ---------------------------------------------------------------------------
+// Results that are not finite, from the formulas over the pairs in sight: a wave
+// takes a query, or a key, and its lanes the channels, a pair after the other.
+// Slow, for the few places that stand in a block with an infinity or a NaN that
+// they do not see; where lse or delta is not finite itself, the results are what
+// they should be.
+// ---------------------------------------------------------------------------
+constexpr int kLaneChannels = 4;       // 256 channels
+
+template <typename T>
+struct Row {
+    float v[kLaneChannels] = {};
+    __device__ __forceinline__ Row() {}
+    __device__ __forceinline__ Row(const T* p, int lane, int dim) {
+#pragma unroll
+        for (int i = 0; i < kLaneChannels; ++i) v[i] = lane + i * kWave < dim ? (float)p[lane + i * kWave] : 0.0f;
+    }
+    __device__ __forceinline__ float dot(const Row& o) const {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kLaneChannels; ++i) s = fmaf(v[i], o.v[i], s);
+#pragma unroll
+        for (int m = 1; m < kWave; m *= 2) s += __shfl_xor(s, m);
+        return s;
+    }
+    __device__ __forceinline__ void add(float w, const Row& o) {
+#pragma unroll
+        for (int i = 0; i < kLaneChannels; ++i) v[i] = fmaf(w, o.v[i], v[i]);
+    }
+    __device__ __forceinline__ void put(T* p, int lane, int dim, float scale) const {
+#pragma unroll
+        for (int i = 0; i < kLaneChannels; ++i)
+            if (lane + i * kWave < dim) p[lane + i * kWave] = (T)(v[i] * scale);
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ void repair_query(const AttnBwdArgs& a, const SeqTile& st, int pos, int head, float delta) {
+    const int lane = threadIdx.x % kWave, kvh = head / (a.q_heads / a.kv_heads);
+    const int64_t t = st.first + pos, at = t * a.q_heads + head;
+    T* dq = static_cast<T*>(a.dq) + at * a.dim;
+    const float lse = a.lse[at] * kLog2e;
+    if (!__ballot(finite(lse) && finite(delta))) return;
+    const Row<T> q(static_cast<const T*>(a.q) + t * a.ld_q + (int64_t)head * a.dim, lane, a.dim), g(static_cast<const T*>(a.dy) + at * a.dim, lane, a.dim);
+    Row<T> sum;
+    const int low = pos - a.window + 1 > 0 ? pos - a.window + 1 : 0, first = a.sinks < low ? a.sinks : low;
+    const bool single = pos == 0 || (a.window == 1 && a.sinks == 0);
+    for (int n = 0; n < first + pos + 1 - low; ++n) {
+        const int64_t p = st.first + (n < first ? n : low + n - first);
+        const Row<T> k(static_cast<const T*>(a.k) + p * a.ld_k + (int64_t)kvh * a.dim, lane, a.dim), v(static_cast<const T*>(a.v) + p * a.ld_v + (int64_t)kvh * a.dim, lane, a.dim);
+        const float ds = __builtin_amdgcn_exp2f(fmaf(q.dot(k), a.c, -lse)) * (g.dot(v) - delta);
+        sum.add(single ? 0.0f * ds : ds, k);
+    }
+    sum.put(dq, lane, a.dim, a.scale);
+}
+
+template <typename T>
+__device__ __forceinline__ void repair_key(const AttnBwdArgs& a, const SeqTile& st, int key, int kvh, bool need_k, bool need_v) {
+    const int lane = threadIdx.x % kWave, group = a.q_heads / a.kv_heads;
+    const int64_t t = st.first + key, to = (t * a.kv_heads + kvh) * a.dim;
+    T *dk = static_cast<T*>(a.dk) + to, *dv = static_cast<T*>(a.dv) + to;
+    const int end = key < a.sinks || st.len - key < a.window ? st.len : key + a.window;
+    bool bad_lse = false, bad_delta = false;
+    for (int p = key + lane; p < end; p += kWave)
+        for (int h = kvh * group; h < kvh * group + group; ++h) {
+            bad_lse |= !finite(a.lse[(int64_t)(st.first + p) * a.q_heads + h]);
+            bad_delta |= !finite(a.delta[(int64_t)(st.first + p) * a.q_heads + h]);
+        }
+    need_v = need_v && !__ballot(bad_lse);
+    need_k = need_k && !__ballot(bad_lse || bad_delta);
+    const Row<T> k(static_cast<const T*>(a.k) + t * a.ld_k + (int64_t)kvh * a.dim, lane, a.dim), v(static_cast<const T*>(a.v) + t * a.ld_v + (int64_t)kvh * a.dim, lane, a.dim);
+    Row<T> sum_k, sum_v;
+    for (int h = kvh * group; h < kvh * group + group; ++h)
+        for (int p = key; p < end && (need_k || need_v); ++p) {
+            const int64_t row = st.first + p, at = row * a.q_heads + h;
+            const Row<T> q(static_cast<const T*>(a.q) + row * a.ld_q + (int64_t)h * a.dim, lane, a.dim), g(static_cast<const T*>(a.dy) + at * a.dim, lane, a.dim);
+            const float w = __builtin_amdgcn_exp2f(fmaf(q.dot(k), a.c, -a.lse[at] * kLog2e));
+            sum_v.add(w, g);
+            const float ds = w * (g.dot(v) - a.delta[at]);
+            sum_k.add(p == 0 || (a.window == 1 && a.sinks == 0) ? 0.0f * ds : ds, q);
+        }
+    if (need_k) sum_k.put(dk, lane, a.dim, a.scale);
+    if (need_v) sum_v.put(dv, lane, a.dim, 1.0f);
+}
+
+// The kernel's arguments, loaded again, and its block: what the results' second
+// computation needs is worked out anew, since held over the walk it would take
+// the walk's registers (a training step of 16384 tokens 925 us, 903 so).
+struct Again : AttnBwdArgs {
+    int block;
+};
+__device__ __forceinline__ Again arguments() {
+    typedef const __attribute__((address_space(4))) uint64_t* Words;
+    Words p = (Words)__builtin_amdgcn_kernarg_segment_ptr();
+    int block = blockIdx.x;
+    asm volatile("" : "+s"(p), "+s"(block));
+    constexpr int N = sizeof(AttnBwdArgs) / 8;
+    static_assert(sizeof(AttnBwdArgs) % 8 == 0, "whole words");
+    uint64_t w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = p[i];
+    Again a;
+    __builtin_memcpy(static_cast<AttnBwdArgs*>(&a), w, sizeof(AttnBwdArgs));
+    a.block = block;
+    return a;
+}
+
+// The queries (columns of the wave) of a tile, and keys (from `from` on), with a bit each
+template <typename T>
+__device__ __forceinline__ void repair_queries(uint32_t bad, float delta) {
+    const Again a = arguments();
+    const int64_t item = die_order(a.block, a.q_items);
+    const SeqTile st = seq_tile(a.seq, (int)(item % a.q_places), a.tile);
+    for (; bad; bad &= bad - 1) {
+        const int c = __builtin_ctz(bad), n = uniform(threadIdx.x / kWave) * kCols + c;
+        repair_query<T>(a, st, st.row + n / a.pack, (int)(item / a.q_places) * a.pack + n % a.pack, __shfl(delta, c));
+    }
+}
+template <typename T>
+__device__ __forceinline__ void repair_keys(const Again& a, const SeqTile& st, int kvh, int from, uint32_t bad_k, uint32_t bad_v) {
+    for (uint32_t bad = uniform(bad_k | bad_v); bad; bad &= bad - 1) {
+        const int c = __builtin_ctz(bad);
+        repair_key<T>(a, st, st.row + uniform(from) + c, kvh, bad_k >> c & 1, bad_v >> c & 1);
+    }
+}
+
+// ---------------------------------------------------------------------------
 // dq and delta: workgroups and columns as in the forward kernel
 // ---------------------------------------------------------------------------
 template <typename T, int DP>
@@ -124,7 +253,7 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
     }
     delta = half_sum(delta);
     const float lse = a.lse[at] * kLog2e;
-    const bool single = pos == 0 || (a.window == 1 && a.sinks == 0);
+    const float several = pos == 0 || (a.window == 1 && a.sinks == 0) ? 0.0f : 1.0f;      // keys seen
 
     const int begin = st.row - a.window + 1 > 0 ? st.row - a.window + 1 : 0;
     const int first_end = a.sinks < begin ? a.sinks : begin, end = last + 1;
@@ -185,12 +314,12 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
                         for (int i = 0; i < 16; ++i) s[i] = 32 * b + acc_row(i, 0) < high ? s[i] : 0.0f;
                     } else if (now >= a.sinks) {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) s[i] = (uint32_t)(32 * b + acc_row(i, 0) - low) < (uint32_t)a.window && !single ? s[i] : 0.0f;
+                        for (int i = 0; i < 16; ++i) s[i] = (uint32_t)(32 * b + acc_row(i, 0) - low) < (uint32_t)a.window ? s[i] * several : 0.0f;
                     } else {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
                             const int p = now + 32 * b + acc_row(i, half);
-                            s[i] = p <= pos && (p > pos - a.window || p < a.sinks) && !single ? s[i] : 0.0f;
+                            s[i] = p <= pos && (p > pos - a.window || p < a.sinks) ? s[i] * several : 0.0f;
                         }
                     }
                 }
@@ -225,16 +354,18 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
     }
     // ds sums to zero over the keys: what it sums to is what delta is off by, from the rounded y
     rest = half_sum(rest);
-    if (live && half == 0) a.delta[at] = delta + rest;
-    if (!live) return;
+    delta += rest;
+    if (live && half == 0) a.delta[at] = delta;
     T* dq = static_cast<T*>(a.dq) + at * a.dim;
+    const uint64_t bad = __ballot(live && nonfinite(o));
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const int d = 32 * b + acc_row(i, half);
-            if (d < a.dim) put4(dq + d, o[b][i] * a.scale, o[b][i + 1] * a.scale, o[b][i + 2] * a.scale, o[b][i + 3] * a.scale);
+            if (live && d < a.dim) put4(dq + d, o[b][i] * a.scale, o[b][i + 1] * a.scale, o[b][i + 2] * a.scale, o[b][i + 3] * a.scale);
         }
+    if (bad) repair_queries<T>((uint32_t)bad | (uint32_t)(bad >> 32), delta);
 }
 
 // ---------------------------------------------------------------------------
@@ -294,7 +425,7 @@ struct Keys {
                 const int p = base + 32 * b + acc_row(i, half);
                 const bool in = seen(p);
                 s[i] = in ? s[i] : 0.0f;
-                dp[i] = in && !single(p) ? dp[i] : 0.0f;
+                dp[i] = in ? dp[i] * (single(p) ? 0.0f : 1.0f) : 0.0f;
             }
         }
 #pragma unroll
@@ -437,17 +568,23 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
                 }
             }
     }
-    if (!live) return;
+    const uint64_t bad_k = __ballot(live && nonfinite(keys.dk)), bad_v = __ballot(live && nonfinite(keys.dv));
     const int64_t to = ((int64_t)(st.first + key) * a.kv_heads + kvh) * a.dim;
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const int d = 32 * b + acc_row(i, half);
-            if (d >= a.dim) continue;
+            if (!live || d >= a.dim) continue;
             put4(static_cast<T*>(a.dk) + to + d, keys.dk[b][i] * a.scale, keys.dk[b][i + 1] * a.scale, keys.dk[b][i + 2] * a.scale, keys.dk[b][i + 3] * a.scale);
             put4(static_cast<T*>(a.dv) + to + d, keys.dv[b][i], keys.dv[b][i + 1], keys.dv[b][i + 2], keys.dv[b][i + 3]);
         }
+    if (bad_k | bad_v) {
+        const Again b = arguments();
+        const int64_t n = die_order(b.block, b.k_items);
+        repair_keys<T>(b, seq_tile(b.seq, (int)(n % b.k_places), kGroupCols), (int)(n / b.k_places), threadIdx.x / kWave * kCols,
+                       (uint32_t)bad_k | (uint32_t)(bad_k >> 32), (uint32_t)bad_v | (uint32_t)(bad_v >> 32));
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -472,6 +609,7 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
     using Q = Tile<T, DP, 32>;
     constexpr int kRound = 32 * Q::kChunks / kWave, kOwn = kNarrowOwn<T, DP>, NW = kNarrowWaves<T, DP>;
     extern __shared__ __align__(16) char stage[];
+    __shared__ uint32_t again[2];      // keys whose dk or dv is not finite
     const int64_t items = (FIRST ? a.pieces : a.k_places) * a.kv_heads, item = die_order(blockIdx.x, items);
     if (item >= items) return;
     const int kvh = (int)(item % a.kv_heads);
@@ -539,6 +677,7 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
     const bool first_keys = !FIRST && st.row == 0 && first.any;
     if (first_keys) first.add(tid, NW * kWave);
     float(*sum)[32][33] = reinterpret_cast<float(*)[32][33]>(stage);      // wave, channel, key
+    if (tid < 2) again[tid] = 0;
     __syncthreads();
 #pragma unroll
     for (int which = 0; which < 2; ++which)
@@ -557,12 +696,20 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
                     if (s < a.sinks) a.part[((((int64_t)place * a.kv_heads + kvh) * 2 + which) * a.sinks + s) * a.dim + e] = v;
                 } else if (k0 + s < st.len) {
                     if (first_keys && s < a.sinks) v += first.part[(int64_t)(which * a.sinks + s) * a.dim + e];
+                    if (!finite(v)) atomicOr(&again[which], 1u << s);
                     const int64_t to = ((int64_t)(st.first + k0 + s) * a.kv_heads + kvh) * a.dim + e;
                     if (which) static_cast<T*>(a.dv)[to] = (T)v;
                     else static_cast<T*>(a.dk)[to] = (T)(v * a.scale);
                 }
             }
             __syncthreads();
+        }
+    if constexpr (!FIRST)
+        if (again[0] | again[1]) {
+            const Again b = arguments();
+            const int64_t n = die_order(b.block, b.k_items);
+            const uint32_t mine = (NW == 4 ? 0x11111111u : 0x55555555u) << threadIdx.x / kWave;
+            repair_keys<T>(b, seq_tile(b.seq, (int)(n / b.kv_heads), kCols), (int)(n % b.kv_heads), 0, again[0] & mine, again[1] & mine);
         }
 }
 
