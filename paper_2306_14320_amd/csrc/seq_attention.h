@@ -58,6 +58,47 @@ __device__ __forceinline__ void mma(f32x16& acc, const Frag<float>& a, const Fra
     for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[j], b.v[j], acc, 0, 0, 0);
 }
 
+// Sixteen values of an accumulator as a product's right operand.  In bf16 they
+// go in two parts, the rounding to bf16 and what it leaves (together off by
+// 2^-17): weights and ds of one part would add an error as large as an output's
+// own rounding.
+template <typename T> struct Parts;
+template <> struct Parts<float> {
+    Frag<float> high;
+    __device__ __forceinline__ Parts(const f32x16& s, int part) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) high.v[j] = s[8 * part + j];
+    }
+};
+template <> struct Parts<bf16> {
+    Frag<bf16> high, low;
+    __device__ __forceinline__ Parts(const f32x16& s, int part) {
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {      // from the pair's word: from its elements, each would be rounded once more
+            const float x = s[8 * part + 2 * j], y = s[8 * part + 2 * j + 1];
+            h[j] = pair(x, y);
+            l[j] = pair(x - __uint_as_float(h[j] << 16), y - __uint_as_float(h[j] & 0xffff0000u));
+        }
+        __builtin_memcpy(&high, h, 16);
+        __builtin_memcpy(&low, l, 16);
+    }
+
+private:
+    static __device__ __forceinline__ uint32_t pair(float x, float y) {
+        const __bf16 __attribute__((ext_vector_type(2))) v = {(bf16)x, (bf16)y};
+        uint32_t u;
+        __builtin_memcpy(&u, &v, 4);
+        arrive(u);
+        return u;
+    }
+};
+template <typename T>
+__device__ __forceinline__ void mma(f32x16& acc, const Frag<T>& a, const Parts<T>& b) {
+    mma(acc, a, b.high);
+    if constexpr (sizeof(T) == 2) mma(acc, a, b.low);
+}
+
 // Row of accumulator register i
 __device__ __forceinline__ int acc_row(int i, int half) { return 8 * (i / 4) + 4 * half + i % 4; }
 
@@ -265,6 +306,30 @@ __device__ __forceinline__ bool nonfinite(const f32x16 (&o)[N]) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) z = fmaf(o[t][i], 0.0f, z);
     return !(z == 0.0f);
+}
+
+// A kernel's arguments (all of them, A), loaded again, and its block: what the
+// rare work behind a walk needs is worked out anew, since held over the walk it
+// would take the walk's registers (a training step of 16384 tokens 925 us, 903 so).
+template <typename A>
+struct Again : A {
+    int block;
+};
+template <typename A>
+__device__ __forceinline__ Again<A> arguments() {
+    typedef const __attribute__((address_space(4))) uint64_t* Words;
+    Words p = (Words)__builtin_amdgcn_kernarg_segment_ptr();
+    int block = blockIdx.x;
+    asm volatile("" : "+s"(p), "+s"(block));
+    constexpr int N = sizeof(A) / 8;
+    static_assert(sizeof(A) % 8 == 0, "whole words");
+    uint64_t w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = p[i];
+    Again<A> a;
+    __builtin_memcpy(static_cast<A*>(&a), w, sizeof(A));
+    a.block = block;
+    return a;
 }
 
 // ---------------------------------------------------------------------------

@@ -56,16 +56,6 @@ __device__ __forceinline__ void put4(bf16* p, float a, float b, float c, float d
     __builtin_memcpy(p, v, 8);
 }
 
-// Sixteen values of an accumulator as a right operand (the weights and ds:
-// rounded to bf16 where the other operand is).
-template <typename T>
-__device__ __forceinline__ Frag<T> operand(const f32x16& s, int part) {
-    Frag<T> f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) f.set(j, s[8 * part + j]);
-    return f;
-}
-
 template <typename T>
 __device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int dim) {
     Frag<T> f;
@@ -177,32 +167,10 @@ __device__ __forceinline__ void repair_key(const AttnBwdArgs& a, const SeqTile& 
     if (need_v) sum_v.put(dv, lane, a.dim, 1.0f);
 }
 
-// The kernel's arguments, loaded again, and its block: what the results' second
-// computation needs is worked out anew, since held over the walk it would take
-// the walk's registers (a training step of 16384 tokens 925 us, 903 so).
-struct Again : AttnBwdArgs {
-    int block;
-};
-__device__ __forceinline__ Again arguments() {
-    typedef const __attribute__((address_space(4))) uint64_t* Words;
-    Words p = (Words)__builtin_amdgcn_kernarg_segment_ptr();
-    int block = blockIdx.x;
-    asm volatile("" : "+s"(p), "+s"(block));
-    constexpr int N = sizeof(AttnBwdArgs) / 8;
-    static_assert(sizeof(AttnBwdArgs) % 8 == 0, "whole words");
-    uint64_t w[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = p[i];
-    Again a;
-    __builtin_memcpy(static_cast<AttnBwdArgs*>(&a), w, sizeof(AttnBwdArgs));
-    a.block = block;
-    return a;
-}
-
 // The queries (columns of the wave) of a tile, and keys (from `from` on), with a bit each
 template <typename T>
 __device__ __forceinline__ void repair_queries(uint32_t bad, float delta) {
-    const Again a = arguments();
+    const Again<AttnBwdArgs> a = arguments<AttnBwdArgs>();
     const int64_t item = die_order(a.block, a.q_items);
     const SeqTile st = seq_tile(a.seq, (int)(item % a.q_places), a.tile);
     for (; bad; bad &= bad - 1) {
@@ -211,7 +179,7 @@ __device__ __forceinline__ void repair_queries(uint32_t bad, float delta) {
     }
 }
 template <typename T>
-__device__ __forceinline__ void repair_keys(const Again& a, const SeqTile& st, int kvh, int from, uint32_t bad_k, uint32_t bad_v) {
+__device__ __forceinline__ void repair_keys(const AttnBwdArgs& a, const SeqTile& st, int kvh, int from, uint32_t bad_k, uint32_t bad_v) {
     for (uint32_t bad = uniform(bad_k | bad_v); bad; bad &= bad - 1) {
         const int c = __builtin_ctz(bad);
         repair_key<T>(a, st, st.row + uniform(from) + c, kvh, bad_k >> c & 1, bad_v >> c & 1);
@@ -328,21 +296,9 @@ __global__ __launch_bounds__(kAttnThreads, (kDqWaves<T, DP>)) void window_dq_ker
                 if (walk == 0) continue;
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
-                    const Frag<T> w = operand<T>(s, part);
-                    // what the rounding of ds to bf16 leaves goes the same way: dq then
-                    // keeps its own rounding's error alone (half as much again before;
-                    // 40 us of a training step's 905)
-                    Frag<T> low;
-                    if constexpr (sizeof(T) == 2) {
+                    const Parts<T> w(s, part);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) low.set(i, s[8 * part + i] - w.get(i));
-                    }
-#pragma unroll
-                    for (int d = 0; d < DP / 32; ++d) {
-                        const Frag<T> f = KV::col_frag(lds, kc, d, 2 * b + part);
-                        mma(o[d], f, w);
-                        if constexpr (sizeof(T) == 2) mma(o[d], f, low);
-                    }
+                    for (int d = 0; d < DP / 32; ++d) mma(o[d], KV::col_frag(lds, kc, d, 2 * b + part), w);
                 }
             }
         }
@@ -430,7 +386,7 @@ struct Keys {
         }
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
-            const Frag<T> w = operand<T>(s, part), ds = operand<T>(dp, part);
+            const Parts<T> w(s, part), ds(dp, part);
             __builtin_amdgcn_s_setprio(1);      // products first; keeps the exponentials in front of them (1000 tokens of 16 x 128: 168 -> 141 us)
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {
@@ -580,7 +536,7 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
             put4(static_cast<T*>(a.dv) + to + d, keys.dv[b][i], keys.dv[b][i + 1], keys.dv[b][i + 2], keys.dv[b][i + 3]);
         }
     if (bad_k | bad_v) {
-        const Again b = arguments();
+        const Again<AttnBwdArgs> b = arguments<AttnBwdArgs>();
         const int64_t n = die_order(b.block, b.k_items);
         repair_keys<T>(b, seq_tile(b.seq, (int)(n % b.k_places), kGroupCols), (int)(n / b.k_places), threadIdx.x / kWave * kCols,
                        (uint32_t)bad_k | (uint32_t)(bad_k >> 32), (uint32_t)bad_v | (uint32_t)(bad_v >> 32));
@@ -706,7 +662,7 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
         }
     if constexpr (!FIRST)
         if (again[0] | again[1]) {
-            const Again b = arguments();
+            const Again<AttnBwdArgs> b = arguments<AttnBwdArgs>();
             const int64_t n = die_order(b.block, b.k_items);
             const uint32_t mine = (NW == 4 ? 0x11111111u : 0x55555555u) << threadIdx.x / kWave;
             repair_keys<T>(b, seq_tile(b.seq, (int)(n / b.kv_heads), kCols), (int)(n % b.kv_heads), 0, again[0] & mine, again[1] & mine);

@@ -87,3 +87,44 @@ def test_gradients_of_what_sees_it(shape, lo, hi, dtype):
             assert ((g[same].double() - before[same].double()).abs() <= 8 * u * size.expand_as(p)[same]).all(), (name, row, value, what, "places that do not see it")
             if what == "y":
                 assert torch.equal(g[same], before[same]), (name, row, value, what)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+def test_infinite_values_that_all_columns_see(dtype):
+    """Blocks of keys that every query of a workgroup sees: an infinity among the
+    values is one in the outputs, of its sign, and NaN where both signs meet."""
+    c = Case(dtype, 2, 1, 64, 500, 0, [0, 900], None, 0)
+    clean = c.run()
+    c.v[200, 0, 3], c.v[230, 0, 3], c.v[210, 0, 7], c.v[220, 0, 7], c.v[250, 0, 40] = INF, INF, -INF, INF, NAN
+    y = c.run()
+    assert (y[200:730, :, 3] == INF).all() and (y[210:220, :, 7] == -INF).all() and torch.isnan(y[220:710, :, 7]).all()
+    assert (y[710:720, :, 7] == INF).all() and torch.isnan(y[250:750, :, 40]).all()
+    rest = [d for d in range(64) if d not in (3, 7, 40)]
+    assert torch.equal(y[:900, :, rest], clean[:900, :, rest]) and torch.equal(y[:200], clean[:200]) and torch.equal(y[750:900], clean[750:900])
+    # a prompt that goes on from a cache which holds them
+    c = Case(dtype, 2, 1, 64, 300, 2, [0, 90], [400], 0)
+    clean = c.run()
+    for t, b in zip(c.caches, c.before):
+        t.copy_(b)
+    s = int(c.slots[0])
+    c.caches[1][s, 1, 0, 5], c.caches[1][s, 2 + (390 - 2) % 300, 0, 6] = -INF, INF
+    y = c.run()
+    assert (y[:90, :, 5] == -INF).all() and (y[:90, :, 6] == INF).all()
+    rest = [d for d in range(64) if d not in (5, 6)]
+    assert torch.equal(y[:90, :, rest], clean[:90, :, rest])
+
+
+@pytest.mark.parametrize("window", [90, 3000], ids=["one share", "shares"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+def test_step_infinite_values(dtype, window):
+    g = torch.Generator().manual_seed(window)
+    q, k, v = (torch.randn(3, n, 64, generator=g).to(dtype).to(DEV) for n in (4, 2, 2))
+    caches = [torch.randn(3, window, 2, 64, generator=g).to(dtype).to(DEV) for _ in range(2)]
+    past = torch.tensor([window + 5, 30, window - 1], dtype=torch.int32, device=DEV)
+    desc = P.window_attention_desc_for(q, k, v, window)
+    clean = P.window_attention_step(q, k, v, *[t.clone() for t in caches], past, desc)
+    caches[1][0, 60, 1, 9], caches[1][1, 40, 0, 2], v[2, 0, 63], caches[1][2, 3, 0, 62], caches[1][2, 50, 0, 62] = INF, NAN, -INF, INF, -INF
+    y = P.window_attention_step(q, k, v, *caches, past, desc)
+    want = clean.clone()
+    want[0, 2:, 9], want[2, :2, 63], want[2, :2, 62] = INF, -INF, NAN
+    assert torch.equal(torch.nan_to_num(y, nan=77.0), torch.nan_to_num(want, nan=77.0))
