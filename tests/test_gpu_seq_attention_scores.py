@@ -1,9 +1,16 @@
 """Window attention on the GPU where the scores are out of the ordinary: all of
-a query's scores minus infinity."""
+a query's scores minus infinity; scores that climb and fall by more and by less
+from one block of keys to the next than the base of the exponentials is left
+behind for (2^8), up to magnitudes of 100, with the bounds of the ordinary ones,
+which carry the scores' size."""
 import pytest
 import torch
 
 import paper_2306_14320_amd as P
+import test_gpu_seq_attention as forward
+import test_gpu_seq_attention_bwd as backward
+from hybrid_reference import attend, ring_row
+from seq_reference import U16, out_round
 from test_gpu_seq_attention import Case
 
 pytestmark = pytest.mark.gpu
@@ -48,3 +55,78 @@ def test_step_scores_of_minus_infinity(dtype, window):
     y = P.window_attention_step(q, k, v, *caches, past, desc, slots=slots)
     assert torch.isnan(y[0, 0]).all() and torch.isnan(y[3, 2]).all()
     assert torch.equal(y[1], clean[1]) and (y[2] == 0).all() and torch.equal(y[0, 2:], clean[0, 2:]) and torch.equal(y[3, :2], clean[3, :2])
+
+
+# what a key's position adds to its scores (natural units; a block has 32 keys)
+PROFILES = {
+    "climb": lambda p, sinks: 0.25 * (p % 400), "climb slowly": lambda p, sinks: 0.1 * (p % 400), "fall": lambda p, sinks: -0.25 * (p % 400),
+    "jump": lambda p, sinks: (0.0, 60.0, -40.0, 95.0, 20.0)[p // 37 % 5], "first tokens": lambda p, sinks: 80.0 if p < sinks else 0.02 * (p % 400),
+}
+SHAPES = [
+    (F32, 4, 2, 64, 200, 2, (420, 1), None, 0), (BF16, 3, 1, 128, 150, 4, [0, 100, 101, 420], [0, 64, 700], 0), (BF16, 2, 2, 64, 300, 3, (450, 1), None, 0),
+    (F32, 2, 1, 256, 120, 1, (300, 1), None, 0), (BF16, 4, 1, 256, 130, 0, [0, 290, 330], [90, 500], 0), (BF16, 8, 2, 96, 90, 32, (300, 1), None, 0),
+    (F32, 3, 1, 32, 70, 5, [0, 40, 300], [300, 2], 1), (BF16, 64, 64, 64, 200, 2, (520, 1), None, 0),
+]
+SHAPE_IDS = ["%s-%dq%dk%d-w%d-s%d" % ((str(c[0])[6:],) + c[1:6]) for c in SHAPES]
+
+
+def _shaped(profile):
+    """Case, with a channel of the queries and keys that adds the profile to the scores."""
+    def build(*args):
+        c = Case(*args)
+
+        def key(p):
+            return profile(p, c.sinks) / (4 * c.scale)
+
+        c.q[:, :, 0] = 4
+        for b, (lo, hi) in enumerate(zip(c.starts, c.starts[1:])):
+            past = c.past_list[b]
+            c.k[lo:hi, :, 0] = torch.tensor([key(past + t) for t in range(hi - lo)], device=DEV, dtype=torch.float64).to(c.dtype)[:, None]
+            for p in range(past) if c.before else ():
+                if p < c.sinks or p >= past - c.window:
+                    c.caches[0][c.slots[b], ring_row(p, c.window, c.sinks), :, 0] = key(p)
+        c.before = [t.clone() for t in getattr(c, "caches", [])]
+        return c
+    return build
+
+
+@pytest.mark.parametrize("profile", PROFILES)
+@pytest.mark.parametrize("shape", SHAPES, ids=SHAPE_IDS)
+def test_far_apart(shape, profile, monkeypatch):
+    monkeypatch.setattr(forward, "Case", _shaped(PROFILES[profile]))
+    forward.test_forward(shape)
+
+
+@pytest.mark.parametrize("profile", PROFILES)
+@pytest.mark.parametrize("shape", [s for s in SHAPES if s[7] is None], ids=[i for i, s in zip(SHAPE_IDS, SHAPES) if s[7] is None])
+def test_far_apart_gradients(shape, profile, monkeypatch):
+    monkeypatch.setattr(backward, "Case", _shaped(PROFILES[profile]))
+    backward.test_backward(shape)
+
+
+@pytest.mark.parametrize("profile", PROFILES)
+@pytest.mark.parametrize("dtype, h, kv, dim, window, sinks", [(F32, 4, 1, 64, 3000, 4), (BF16, 8, 2, 128, 2000, 2), (BF16, 4, 4, 256, 600, 0), (F32, 6, 2, 96, 100, 3)])
+def test_far_apart_step(dtype, h, kv, dim, window, sinks, profile):
+    """Shares of a request's rows, and waves of a share, whose largest scores are far apart."""
+    g = torch.Generator().manual_seed(dim)
+    n, scale, past = 3, dim ** -0.5, [window + 700, window - 1, 40]
+    q, k, v = (torch.randn(n, m, dim, generator=g).to(dtype) for m in (h, kv, kv))
+    caches = [torch.randn(n, sinks + window, kv, dim, generator=g).to(dtype) for _ in range(2)]
+    q[:, :, 0] = 4
+    for b, p in enumerate(past):
+        k[b, :, 0] = PROFILES[profile](p, sinks) / (4 * scale)
+        for r in range(sinks + window):
+            caches[0][b, r, :, 0] = PROFILES[profile](r, sinks) / (4 * scale)      # rows, in the ring's order
+    on = [t.to(DEV) for t in (q, k, v, *caches)]
+    desc = P.window_attention_desc_for(*on[:3], window, sinks, scale=scale)
+    y = P.window_attention_step(*on, torch.tensor(past, dtype=torch.int32, device=DEV), desc)
+    u = U16 if dtype == BF16 else 0.0
+    for b, p in enumerate(past):
+        for c, new in zip(caches, (k, v)):
+            c[b, ring_row(p, window, sinks)] = new[b]
+        rows = min(p + 1, sinks + window)
+        for head in range(h):
+            kk, vv = (c[b, :rows, head // (h // kv)].double() for c in caches)
+            ref, _, bound, _ = attend(q[b:b + 1, head].double(), kk, vv, rows - 1, rows, 0, scale)
+            e = bound(u)
+            forward._within(y[b:b + 1, head], ref, e + out_round(dtype) * (ref.abs() + e), ("y", b, head))
