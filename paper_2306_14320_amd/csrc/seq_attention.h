@@ -342,18 +342,12 @@ struct SeqTile {
     int b, first, len, row;      // the sequence, its first row and length, the tile's first row in it (len and more: nothing to do)
 };
 
-__device__ __forceinline__ SeqTile seq_tile(const SeqMap& seq, int place, int rows) {
+// The tile at a place, where seq_starts is given and sequence b's places begin at
+// first_place(b), which does not decrease.
+template <typename F>
+__device__ __forceinline__ SeqTile find_tile(const SeqMap& seq, int place, int rows, F first_place) {
     SeqTile t;
-    if (!seq.starts) {
-        const int per = (seq.len + rows - 1) / rows;
-        t.b = uniform(place / per);
-        t.first = t.b * seq.len;
-        t.len = seq.len;
-        t.row = (place - t.b * per) * rows;
-        return t;
-    }
     const int lane = threadIdx.x % kWave;
-    auto first_place = [&](int b) { return seq.clamped(b) / rows + b; };     // strictly increasing
     int lo = 0, n = seq.count;
     while (n > kWave - 1) {
         const int step = (n + kWave - 2) / (kWave - 1), i = lo + lane * step;
@@ -366,8 +360,18 @@ __device__ __forceinline__ SeqTile seq_tile(const SeqMap& seq, int place, int ro
     t.b = uniform(lo + 63 - __builtin_clzll(in));
     t.first = seq.first(t.b);
     t.len = seq.first(t.b + 1) - t.first;
-    t.row = (place - (t.first / rows + t.b)) * rows;
-    if (t.row < 0) t.row = t.len > 0 ? t.len : 0;      // only where seq_starts decreases
+    const int64_t row = (int64_t)(place - uniform(first_place(t.b))) * rows;
+    t.row = row < 0 || row > t.len ? (t.len > 0 ? t.len : 0) : (int)row;      // (below zero only where seq_starts decreases)
+    return t;
+}
+__device__ __forceinline__ SeqTile seq_tile(const SeqMap& seq, int place, int rows) {
+    if (seq.starts) return find_tile(seq, place, rows, [&](int b) { return seq.clamped(b) / rows + b; });
+    SeqTile t;
+    const int per = (seq.len + rows - 1) / rows;
+    t.b = uniform(place / per);
+    t.first = t.b * seq.len;
+    t.len = seq.len;
+    t.row = (place - t.b * per) * rows;
     return t;
 }
 inline int64_t seq_places(int64_t tokens, int64_t sequences, const int32_t* starts, int64_t rows) {

@@ -398,6 +398,20 @@ struct Keys {
     }
 };
 
+// Pieces of the sequences that are longer than the window, of which tokens / (window
+// + 1) can exist, whatever the number of sequences: where seq_starts is given,
+// sequence b, from row f on, owns the places from f / piece + min(b, f / (window + 1))
+// on.  Behind a sequence that is longer that is larger by its pieces at least;
+// behind others it may not be, and the last of those that begin at a place has it.
+__device__ __forceinline__ int first_piece(const AttnBwdArgs& a, int b, int first) {
+    const int longer = first / (a.window + 1);
+    return first / a.piece + (b < longer ? b : longer);
+}
+__device__ __forceinline__ SeqTile piece_tile(const AttnBwdArgs& a, int place) {
+    if (!a.seq.starts) return seq_tile(a.seq, place, a.piece);
+    return find_tile(a.seq, place, a.piece, [&](int b) { return first_piece(a, b, a.seq.clamped(b)); });
+}
+
 // The sums that the first tokens' pieces of a sequence left, for the tile of its first keys
 struct FirstSums {
     bool any;
@@ -406,7 +420,7 @@ struct FirstSums {
     float* part;
     __device__ __forceinline__ FirstSums(const AttnBwdArgs& a, const SeqTile& st, int kvh) {
         any = a.sinks && st.len > a.window;
-        const int from = a.window / a.piece, place = a.seq.starts ? st.first / a.piece + st.b : st.b * ((a.seq.len + a.piece - 1) / a.piece);
+        const int from = a.window / a.piece, place = a.seq.starts ? first_piece(a, st.b, st.first) : st.b * ((a.seq.len + a.piece - 1) / a.piece);
         pieces = (st.len + a.piece - 1) / a.piece - from;
         count = 2 * (int64_t)a.sinks * a.dim;
         step = a.kv_heads * count;
@@ -570,7 +584,7 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
     if (item >= items) return;
     const int kvh = (int)(item % a.kv_heads);
     const int place = (int)(item / a.kv_heads);
-    const SeqTile st = seq_tile(a.seq, place, FIRST ? a.piece : kCols);
+    const SeqTile st = FIRST ? piece_tile(a, place) : seq_tile(a.seq, place, kCols);
     if (st.row >= st.len) return;
     // the queries' rows
     const int64_t far = FIRST ? (int64_t)st.row + a.piece : (int64_t)st.row + kCols - 1 + a.window;
@@ -696,12 +710,13 @@ int64_t piece_rows(const im2win_window_desc* d) {
 int64_t pieces_of(const im2win_window_desc* d, const int32_t* starts) {
     if (!d->sinks || d->tokens <= d->window) return 0;
     if (!starts && d->tokens / d->sequences <= d->window) return 0;
-    return seq_places(d->tokens, d->sequences, starts, piece_rows(d));
+    if (!starts) return seq_places(d->tokens, d->sequences, starts, piece_rows(d));
+    return d->tokens / piece_rows(d) + std::min(d->sequences, d->tokens / (d->window + 1));
 }
 // With and without seq_starts (whose places are never fewer): the query does not know.
 size_t bwd_bytes(const im2win_window_desc* d) {
     const size_t delta = ((size_t)(d->tokens * d->q_heads) * 4 + 15) / 16 * 16;
-    const int64_t pieces = d->sinks && d->tokens > d->window ? d->tokens / piece_rows(d) + d->sequences : 0;
+    const int64_t pieces = d->sinks && d->tokens > d->window ? d->tokens / piece_rows(d) + std::min(d->sequences, d->tokens / (d->window + 1)) : 0;
     return delta + (size_t)(pieces * d->kv_heads * 2 * d->sinks * d->head_dim) * 4;
 }
 
