@@ -18,7 +18,7 @@
 //
 // The angle of a far position has more digits than fp32: the turns are taken
 // in fp64, and what is left behind the whole ones (at most half a turn) in
-// fp32, off by 2^-26 turns.
+// two parts of fp32, the second of which turns the first's cosine and sine on.
 #include "seq_common.h"
 
 #include <algorithm>
@@ -162,10 +162,11 @@ __device__ __forceinline__ void angles(const QkArgs& a, int t, float* cs, float*
     for (int p = lane; p < a.rot / 2; p += kWave) {
         double turns = at * ((double)a.freqs[p] * 0.15915494309189533577);
         turns -= __builtin_rint(turns);
+        const float near = (float)turns, rest = (float)(turns - (double)near) * 6.28318530717958648f;
         float s, c;
-        sincospif(2.0f * (float)turns, &s, &c);
-        cs[p] = c;
-        sn[p] = s;
+        sincospif(2.0f * near, &s, &c);
+        cs[p] = fmaf(-s, rest, c);
+        sn[p] = fmaf(c, rest, s);
     }
 }
 
@@ -361,23 +362,39 @@ __global__ __launch_bounds__(kWavesPer * kWave) void qk_norm_rope_bwd_kernel(QkA
     }
 }
 
-constexpr int kSumWaves = 16;
+constexpr int kSumWaves = 16, kSums = 8;
+
+// The sum of values by pairs, whose error grows with the logarithm of their number
+template <int N>
+__device__ __forceinline__ float added(const float (&v)[N]) {
+    float s[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) s[i] = v[i];
+#pragma unroll
+    for (int n = N / 2; n; n /= 2)
+#pragma unroll
+        for (int i = 0; i < n; ++i) s[i] += s[i + n];
+    return s[0];
+}
 
 // dwq and dwk from the workgroups' sums
 __global__ __launch_bounds__(kSumWaves * kWave) void qk_norm_rope_bwd_sum_kernel(const float* part, float* dwq, float* dwk, int blocks, int dim) {
     __shared__ float sum[kSumWaves][kWave];
     const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
     const int c = (int)blockIdx.x * kWave + lane;
-    float s = 0.0f;
+    float s[kSums] = {};
     if (c < 2 * dim) {
-#pragma unroll 8
-        for (int i = wave; i < blocks; i += kSumWaves) s += part[(int64_t)i * 2 * dim + c];
+        for (int i = wave; i < blocks; i += kSums * kSumWaves)
+#pragma unroll
+            for (int j = 0; j < kSums; ++j) s[j] += i + j * kSumWaves < blocks ? part[(int64_t)(i + j * kSumWaves) * 2 * dim + c] : 0.0f;
     }
-    sum[wave][lane] = s;
+    sum[wave][lane] = added(s);
     __syncthreads();
     if (wave == 0 && c < 2 * dim) {
-        for (int i = 1; i < kSumWaves; ++i) s += sum[i][lane];
-        (c < dim ? dwq + c : dwk + (c - dim))[0] = s;
+        float w[kSumWaves];
+#pragma unroll
+        for (int i = 0; i < kSumWaves; ++i) w[i] = sum[i][lane];
+        (c < dim ? dwq + c : dwk + (c - dim))[0] = added(w);
     }
 }
 
