@@ -444,11 +444,16 @@ Shape shape_of(const im2win_qk_desc* d) {
     return s;
 }
 
-// Workgroups of the gradients, whose waves walk the rows: as many as run at
-// once (runs of eight pairs have registers for three waves a SIMD: 16384 rows of
-// 20 x 128 bf16 take 59 us with 768 workgroups, 73 with 1024, whose last quarter
-// runs alone; 4001 rows of 15 x 80 fp32 take 27 with 768 and 24 with 1024).
-int64_t bwd_blocks(const Shape& s) { return std::min<int64_t>(s.blocks, s.v == 8 ? 768 : 1024); }
+// Workgroups of the gradients, whose waves walk the rows: as many as run at once,
+// by the registers of the variant, so that none waits for the others (bf16 rows of
+// 16384: 20 x 128, three a CU, 58 us with 768, 74 with 1024; 6 x 510 of single
+// pairs in fours 100 with 768, 126 with 1024; 20 x 80 in runs of four 51 with 1280,
+// 56 with 1024; 20 x 70 of single pairs 128 with 1536, 158 with 1024).  In fp32
+// four a CU take runs of four (20 x 128 106 with 1024, 118 with 1280).
+int64_t bwd_blocks(const Shape& s, int32_t dtype) {
+    const int64_t per_cu = s.v == 8 || s.j > 1 ? 3 : s.v == 1 ? 6 : dtype == IM2WIN_F32 ? 4 : 5;
+    return std::min<int64_t>(s.blocks, 256 * per_cu);
+}
 
 template <typename F>
 void with_shape(const im2win_qk_desc* d, const Shape& s, F f) {
@@ -524,7 +529,7 @@ int im2win_qk_norm_rope_backward_workspace_bytes(const im2win_qk_desc* d, size_t
     int rc = check_desc(d);
     if (rc) return rc;
     if (!bytes) return fail(IM2WIN_ENULL, "bytes is NULL");
-    *bytes = (size_t)(bwd_blocks(shape_of(d)) * 2 * d->head_dim * 4);
+    *bytes = (size_t)(bwd_blocks(shape_of(d), d->dtype) * 2 * d->head_dim * 4);
     return ok();
 }
 
@@ -539,7 +544,7 @@ int im2win_qk_norm_rope_backward(const im2win_qk_desc* d, const void* dyq, const
                       (rc = need_ptr(workspace, 16, "workspace"))))
         return rc;
     const Shape s = shape_of(d);
-    const int64_t blocks = bwd_blocks(s);
+    const int64_t blocks = bwd_blocks(s, d->dtype);
     const size_t need = (size_t)(blocks * 2 * d->head_dim * 4);
     if (workspace_bytes < need)
         return fail(IM2WIN_EWORKSPACE, "workspace holds %zu bytes, the gradients need %zu", workspace_bytes, need);
