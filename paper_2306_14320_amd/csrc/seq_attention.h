@@ -259,6 +259,16 @@ __device__ __forceinline__ void clear(char* lds, int bytes) {
     __syncthreads();
 }
 
+// Writes four neighbouring channels
+__device__ __forceinline__ void put4(float* p, float a, float b, float c, float d) {
+    const float v[4] = {a, b, c, d};
+    __builtin_memcpy(p, v, 16);
+}
+__device__ __forceinline__ void put4(bf16* p, float a, float b, float c, float d) {
+    const uint32_t v[2] = {pack_bf16(a, b), pack_bf16(c, d)};
+    __builtin_memcpy(p, v, 8);
+}
+
 // The sum, or the largest, of both halves' values
 __device__ __forceinline__ float half_sum(float v) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -410,8 +420,6 @@ inline int heads_packed(int64_t q_heads, int64_t kv_heads) {
         if (group % p == 0) best = p;
     return best;
 }
-
-inline size_t attn_size_of(int32_t dtype) { return dtype == IM2WIN_F32 ? 4 : 2; }
 
 inline int check_attention(const im2win_window_desc* d) {
     if (!d) return fail(IM2WIN_ENULL, "descriptor is NULL");

@@ -91,16 +91,6 @@ __device__ __forceinline__ void soften(Running<DP>& r, f32x16 (&s)[NB], float c)
     r.l += sum;       // of the lane's half; the halves are added at the end
 }
 
-// Writes four neighbouring channels
-__device__ __forceinline__ void put4(float* p, float a, float b, float c, float d) {
-    const float v[4] = {a, b, c, d};
-    __builtin_memcpy(p, v, 16);
-}
-__device__ __forceinline__ void put4(bf16* p, float a, float b, float c, float d) {
-    const uint32_t v[2] = {pack_bf16(a, b), pack_bf16(c, d)};
-    __builtin_memcpy(p, v, 8);
-}
-
 // Keys of a tile.  9001 tokens of 12 heads of 64 channels took 55 us with 64 keys, 57 with
 // 32, at three waves, but 16384 of 16 heads of 128 channels 388 and 207: two buffers of 64 such rows
 // leave LDS for two workgroups.  (32 rows of 32 or 96 channels are no whole number of
@@ -564,12 +554,6 @@ __global__ __launch_bounds__(kAttnThreads) void window_step_join_kernel(AttnArgs
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-template <typename F>
-void with_type(int32_t dtype, F f) {
-    if (dtype == IM2WIN_F32) f(float{});
-    else f(bf16{});
-}
-
 AttnArgs args_of(const im2win_window_desc* d, const void* q, const void* k, const void* v) {
     AttnArgs a{};
     a.q = q; a.k = k; a.v = v;
@@ -583,7 +567,7 @@ AttnArgs args_of(const im2win_window_desc* d, const void* q, const void* k, cons
 }
 
 int check_cache(const im2win_window_desc* d, const void* k_cache, const void* v_cache, int64_t cache_slots, const int32_t* past, const int32_t* slots) {
-    const size_t e = attn_size_of(d->dtype);
+    const size_t e = size_of(d->dtype);
     int rc;
     if (cache_slots < 0) return fail(IM2WIN_EINVAL, "cache_slots must be >= 0 (got %lld)", (long long)cache_slots);
     if ((rc = need_ptr(k_cache, e, "k_cache")) || (rc = need_ptr(v_cache, e, "v_cache")) || (rc = may_ptr(slots, 4, "slots"))) return rc;
@@ -600,7 +584,7 @@ struct Split {
 Split split_of(const im2win_window_desc* d) {
     const int64_t blocks = d->tokens * (d->q_heads / heads_packed(d->q_heads, d->kv_heads)), rows = d->sinks + d->window;
     int64_t room = 256;
-    with_head(d->head_dim, [&](auto dp) { room = 256 * step_waves((int)(decltype(dp)::value * attn_size_of(d->dtype))); });
+    with_head(d->head_dim, [&](auto dp) { room = 256 * step_waves((int)(decltype(dp)::value * size_of(d->dtype))); });
     const int64_t n = std::max<int64_t>(1, std::min(blocks ? room / blocks : 1, (rows + 127) / 128));
     Split s{};
     s.rows = (int)(((rows + n - 1) / n + 31) / 32 * 32);
@@ -629,7 +613,7 @@ int im2win_window_attention(const im2win_window_desc* d, const void* q, const vo
     if (cached && (rc = check_cache(d, k_cache, v_cache, cache_slots, past, slots))) return rc;
     if (!cached && (past || slots)) return fail(IM2WIN_EINVAL, "past and slots belong to a cache (k_cache is NULL)");
     if (d->tokens == 0) return ok();
-    const size_t e = attn_size_of(d->dtype);
+    const size_t e = size_of(d->dtype);
     if ((rc = need_ptr(q, e, "q")) || (rc = need_ptr(k, e, "k")) || (rc = need_ptr(v, e, "v")) || (rc = need_ptr(y, e, "y")) || (rc = may_ptr(lse, 4, "lse"))) return rc;
     AttnArgs a = args_of(d, q, k, v);
     a.k_cache = k_cache; a.v_cache = v_cache; a.cache_slots = cache_slots; a.past = past; a.slots = slots;
@@ -664,7 +648,7 @@ int im2win_window_attention_step(const im2win_window_desc* d, const void* q, con
     int rc = check_attention(d);
     if (rc) return rc;
     if (d->tokens == 0) return ok();
-    const size_t e = attn_size_of(d->dtype), need = step_bytes(d);
+    const size_t e = size_of(d->dtype), need = step_bytes(d);
     if ((rc = need_ptr(q, e, "q")) || (rc = need_ptr(k, e, "k")) || (rc = need_ptr(v, e, "v")) || (rc = need_ptr(y, e, "y")) ||
         (rc = check_cache(d, k_cache, v_cache, cache_slots, past, slots)) || (rc = need_ptr(past, 4, "past")) ||
         (need && (rc = need_ptr(workspace, 16, "workspace"))))

@@ -47,15 +47,6 @@ struct AttnBwdArgs {
     float c, scale;
 };
 
-__device__ __forceinline__ void put4(float* p, float a, float b, float c, float d) {
-    const float v[4] = {a, b, c, d};
-    __builtin_memcpy(p, v, 16);
-}
-__device__ __forceinline__ void put4(bf16* p, float a, float b, float c, float d) {
-    const uint32_t v[2] = {pack_bf16(a, b), pack_bf16(c, d)};
-    __builtin_memcpy(p, v, 8);
-}
-
 template <typename T>
 __device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int dim) {
     Frag<T> f;
@@ -686,12 +677,6 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-template <typename F>
-void with_type(int32_t dtype, F f) {
-    if (dtype == IM2WIN_F32) f(float{});
-    else f(bf16{});
-}
-
 // Tiles of 128 keys that would leave CUs idle go to the narrow kernel: 2503 tokens
 // of 2 heads fp32 (40 tiles) 368 -> 209 us, 1000 tokens of 4 heads bf16 (32) 261 ->
 // 176.  Where they fill the chip they are faster: 16096 tokens of 4 heads (504) 376
@@ -742,7 +727,7 @@ int im2win_window_attention_backward(const im2win_window_desc* d, const void* dy
     int rc = check_attention(d);
     if (rc || (rc = check_sequences(d->tokens, d->sequences, seq_starts, true))) return rc;
     if (d->tokens == 0) return ok();
-    const size_t e = attn_size_of(d->dtype), need = bwd_bytes(d);
+    const size_t e = size_of(d->dtype), need = bwd_bytes(d);
     if ((rc = need_ptr(dy, e, "dy")) || (rc = need_ptr(q, e, "q")) || (rc = need_ptr(k, e, "k")) || (rc = need_ptr(v, e, "v")) ||
         (rc = need_ptr(y, e, "y")) || (rc = need_ptr(lse, 4, "lse")) || (rc = need_ptr(dq, e, "dq")) || (rc = need_ptr(dk, e, "dk")) ||
         (rc = need_ptr(dv, e, "dv")) || (rc = need_ptr(workspace, 16, "workspace")))

@@ -193,6 +193,15 @@ __device__ __forceinline__ float sigmoid(float v) {
 // ---------------------------------------------------------------------------
 inline bool aligned_to(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+inline size_t size_of(int32_t dtype) { return dtype == IM2WIN_F32 ? 4 : 2; }
+
+// f(a value of the type)
+template <typename F>
+void with_type(int32_t dtype, F f) {
+    if (dtype == IM2WIN_F32) f(float{});
+    else f(bf16{});
+}
+
 // A pointer an entry point needs (or may have): not NULL, aligned to its element.
 inline int need_ptr(const void* p, size_t align, const char* name) {
     if (!p) return fail(IM2WIN_ENULL, "%s is NULL", name);

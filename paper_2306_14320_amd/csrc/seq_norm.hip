@@ -386,8 +386,6 @@ int check_desc(const im2win_norm_desc* d) {
     return check_ld(d->ld_x, d->channels, "ld_x");
 }
 
-size_t size_of(int32_t dtype) { return dtype == IM2WIN_F32 ? 4 : 2; }
-
 // f(threads, steps): the smallest workgroup that holds the row.  A wave per
 // row up to 512 channels, then 256 threads of one to four steps, then 1024
 // of two: 16384 channels, which their 128 registers just hold beside dw (the

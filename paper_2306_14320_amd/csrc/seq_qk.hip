@@ -401,8 +401,6 @@ __global__ __launch_bounds__(kSumWaves * kWave) void qk_norm_rope_bwd_sum_kernel
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
-size_t size_of(int32_t dtype) { return dtype == IM2WIN_F32 ? 4 : 2; }
-
 int check_desc(const im2win_qk_desc* d) {
     if (!d) return fail(IM2WIN_ENULL, "descriptor is NULL");
     if (d->q_heads < 0 || d->k_heads < 0 || d->q_heads + d->k_heads < 1 || d->q_heads > 65536 || d->k_heads > 65536)

@@ -779,8 +779,6 @@ int check_desc(const im2win_recurrence_desc* d) {
     return IM2WIN_OK;
 }
 
-size_t size_of(int32_t dtype) { return dtype == IM2WIN_F32 ? 4 : 2; }
-
 // Channels of a lane: 4 bytes of a row, or a row of one bfloat16
 int lane_channels(const im2win_recurrence_desc* d) { return d->dtype == IM2WIN_F32 || d->channels == 1 ? 1 : 2; }
 

@@ -407,12 +407,6 @@ ScanPlan plan_scan(const im2win_scan_desc* d) {
 
 constexpr int kEmptyBlocks = 32;     // workgroups that look for sequences without rows
 
-template <typename F>
-void with_type(int32_t dtype, F f) {
-    if (dtype == IM2WIN_F32) f(float{});
-    else f(bf16{});
-}
-
 }  // namespace
 
 int check_scan(const im2win_scan_desc* d, bool sequences, const int32_t* starts, bool have_starts) {

@@ -772,12 +772,6 @@ constexpr int kLookStates = 8;
 
 constexpr int kEmptyBlocks = 32;
 
-template <typename F>
-void with_type(int32_t dtype, F f) {
-    if (dtype == IM2WIN_F32) f(float{});
-    else f(bf16{});
-}
-
 }  // namespace
 }  // namespace im2win
 
