@@ -133,6 +133,12 @@ __device__ __forceinline__ void put_nonfinite(uint32_t bad) {
                 const T x = lane + e * kWave < a.dim ? v[lane + e * kWave] : (T)0.0f;
                 sum[e] += finite(x) ? 0.0f : (float)x;
             }
+            if (i % 16 == 0) {      // all channels NaN: whatever else they see
+                bool done = true;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) done &= lane + e * kWave >= a.dim || sum[e] != sum[e];
+                if (!__ballot(!done)) break;
+            }
         }
         T* y = static_cast<T*>(a.y) + ((int64_t)(st.first + row) * a.q_heads + h0 + n % a.pack) * a.dim;
 #pragma unroll

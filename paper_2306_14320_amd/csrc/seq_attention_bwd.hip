@@ -98,6 +98,12 @@ struct Row {
         for (int m = 1; m < kWave; m *= 2) s += __shfl_xor(s, m);
         return s;
     }
+    __device__ __forceinline__ bool any_finite(int lane, int dim) const {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < kLaneChannels; ++i) any |= lane + i * kWave < dim && finite(v[i]);
+        return __ballot(any);
+    }
     __device__ __forceinline__ void add(float w, const Row& o) {
 #pragma unroll
         for (int i = 0; i < kLaneChannels; ++i) v[i] = fmaf(w, o.v[i], v[i]);
@@ -153,6 +159,7 @@ __device__ __forceinline__ void repair_key(const AttnBwdArgs& a, const SeqTile& 
             sum_v.add(w, g);
             const float ds = w * (g.dot(v) - a.delta[at]);
             sum_k.add(p == 0 || (a.window == 1 && a.sinks == 0) ? 0.0f * ds : ds, q);
+            if (!need_k && p % 16 == 0) need_v = sum_v.any_finite(lane, a.dim);      // (of dy that is NaN throughout, nothing)
         }
     if (need_k) sum_k.put(dk, lane, a.dim, a.scale);
     if (need_v) sum_v.put(dv, lane, a.dim, 1.0f);
