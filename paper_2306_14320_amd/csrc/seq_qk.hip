@@ -510,7 +510,7 @@ int im2win_qk_norm_rope(const im2win_qk_desc* d, const void* q, const void* k, c
     int rc = check_desc(d);
     if (rc || (rc = check_inputs(d, q, k, wq, wk, positions, freqs))) return rc;
     const size_t e = size_of(d->dtype);
-    if (d->tokens && ((d->q_heads && (rc = need_ptr(yq, e, "q's output"))) || (d->k_heads && (rc = need_ptr(yk, e, "k's output"))))) return rc;
+    if (d->tokens && ((d->q_heads && (rc = need_ptr(yq, e, "yq"))) || (d->k_heads && (rc = need_ptr(yk, e, "yk"))))) return rc;
     if (d->tokens == 0) return ok();
     const Shape s = shape_of(d);
     if ((rc = check_launch(s.blocks, kWavesPer * kWave, "qk_norm_rope"))) return rc;
@@ -537,8 +537,8 @@ int im2win_qk_norm_rope_backward(const im2win_qk_desc* d, const void* dyq, const
     int rc = check_desc(d);
     if (rc || (rc = check_inputs(d, q, k, wq, wk, positions, freqs)) || (rc = need_ptr(dwq, 4, "dwq")) || (rc = need_ptr(dwk, 4, "dwk"))) return rc;
     const size_t e = size_of(d->dtype);
-    if (d->tokens && ((d->q_heads && ((rc = need_ptr(dyq, e, "dq's input")) || (rc = need_ptr(dq, e, "dq")))) ||
-                      (d->k_heads && ((rc = need_ptr(dyk, e, "dk's input")) || (rc = need_ptr(dk, e, "dk")))) ||
+    if (d->tokens && ((d->q_heads && ((rc = need_ptr(dyq, e, "dyq")) || (rc = need_ptr(dq, e, "dq")))) ||
+                      (d->k_heads && ((rc = need_ptr(dyk, e, "dyk")) || (rc = need_ptr(dk, e, "dk")))) ||
                       (rc = need_ptr(workspace, 16, "workspace"))))
         return rc;
     const Shape s = shape_of(d);
