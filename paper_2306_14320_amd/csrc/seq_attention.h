@@ -198,8 +198,8 @@ constexpr int64_t kMaxAttnStride = int64_t(1) << 24;      // a tile's 64 rows of
 
 // Tiles are copied this many ahead of the one that is worked on: two where one
 // workgroup a CU has LDS for three pairs of them, since no other covers the
-// copies' way then (2503 tokens fp32: 209 -> 189 us); with more workgroups one
-// (two take 238 us where one takes 195, by the registers that they cost).
+// copies' way then (2503 tokens fp32: 209 -> 189 us, as they first ran); with more
+// workgroups one (two took 238 us where one took 195, by the registers that they cost).
 template <int BYTES, int WAVES> constexpr int kAheadTiles = WAVES == 1 && 3 * 2 * BYTES <= 156 * 1024 ? 2 : 1;
 
 // The wave's copies but for the newest N have arrived, and then everyone's.

@@ -9,12 +9,13 @@
 // the request had before the call come from its cache, a ring of sinks +
 // window rows, in which the call leaves the new tokens' keys and values.
 //
-// 16384 tokens of 16 heads over 4, 128 bf16 channels, window 1024: 199 us, 206 in
-// front of the gradients, whose two products would take 107 at the rate of a large one.
-// 9001 tokens of 12 heads over 4, 64 channels, window 500, 13 ragged prompts: 41 us
-// (11 for the products) with the 6 for the caches.  Waves wait for LDS for half of their time, the vector units are busy
-// for half of it and the matrix cores for 30%: exponentials, maximum and sum of
-// 64 channels' scores take longer than their products.
+// 16384 tokens of 16 heads over 4, 128 bf16 channels, window 1024, in front of the
+// gradients: 235 us, where three products (the weights have two parts) would take
+// 161 at the rate of a large one; matrix cores are busy for 43%, vector units for
+// 51%, and waves wait for 37% of their cycles.  9001 tokens of 12 heads over 4, 64
+// channels, window 500, 13 ragged prompts: 47 us (17 for the products), and 5 for
+// the caches; vector units 61%, matrix cores 25%: exponentials, maximum, sum and
+// both parts of 64 channels' weights take longer than their products.
 #include "seq_attention.h"
 
 #include <algorithm>
@@ -91,15 +92,14 @@ __device__ __forceinline__ void soften(Running<DP>& r, f32x16 (&s)[NB], float c)
     r.l += sum;       // of the lane's half; the halves are added at the end
 }
 
-// Keys of a tile.  9001 tokens of 12 heads of 64 channels took 55 us with 64 keys, 57 with
-// 32, at three waves, but 16384 of 16 heads of 128 channels 388 and 207: two buffers of 64 such rows
-// leave LDS for two workgroups.  (32 rows of 32 or 96 channels are no whole number of
-// copies by all threads.)
+// Keys of a tile.  9001 tokens of 12 heads of 64 channels take 51.7 us with 64 keys,
+// 53.5 with 32, but 16384 of 16 heads of 128 channels 420 and 242: two buffers of 64
+// such rows leave LDS for two workgroups.  (32 rows of 32 or 96 channels are no whole
+// number of copies by all threads.)
 template <typename T, int DP> constexpr int kTileKeys = sizeof(T) == 2 && DP <= 96 ? 64 : 32;
 // Waves a SIMD.  Of 128 channels of bf16 three hide the waits for LDS best (16384 tokens
-// of 16 heads, window 1024, before blocks were left out: 195 us, 214 with two waves, 217
-// with two that read each operand a step ahead), of 64 and fewer four (9001 tokens of
-// 12 heads: 45 us, 52 with three); of 96 three gain nothing over two, and wider rows
+// of 16 heads, window 1024: 242 us, 254 with two), of 64 and fewer four (9001 tokens of
+// 12 heads: 52 us, 58 with three); of 96 three gain nothing over two, and wider rows
 // have registers for two, or one.
 template <typename T, int DP> constexpr int kFwdWaves = DP * sizeof(T) > 384 || DP >= 192 ? 1 : sizeof(T) == 2 && DP != 96 ? (DP > 64 ? 3 : 4) : 2;
 // The step: waves a SIMD, and whether the next rows wait in registers while
@@ -365,8 +365,8 @@ __global__ __launch_bounds__(kAttnThreads) void window_cache_kernel(AttnArgs a) 
 // a time, whole rows by neighbouring lanes, through its own part of LDS.  The
 // new token's row is read from the inputs and written to the cache by the lanes
 // that hold it.  Bound by memory: 128 requests of 1028 rows of 4 heads of 128 bf16
-// take 47 to 48.6 us, 4.6 TB/s (56 with each lane reading its own row; 64 channels
-// 57 us, not 67, 256 59, not 84).  In fp32 the matrix instructions bound it, of
+// take 49 us, 4.5 TB/s (with each lane reading its own row 56, when it took 47 to
+// 48.6 with weights of one part).  In fp32 the matrix instructions bound it, of
 // which a request's 4 heads use 4 columns of 32: 141 us, 87 at a copy's rate.
 // ---------------------------------------------------------------------------
 // An infinity among the values (as in put_nonfinite): the wave's rows, for all heads
@@ -583,7 +583,7 @@ int check_cache(const im2win_window_desc* d, const void* k_cache, const void* v_
 // Shares of a request's rows: as many as have room on the chip at once beside the
 // other requests' and heads', of 128 rows (one round of the workgroup) at least:
 // 100 requests of 260 rows take 16 us, 27 with one share more, which waits for the
-// others.  2 requests of 4100 rows have 33 shares: 7 us, and 10.6 for the join.
+// others.  2 requests of 4100 rows have 33 shares: 7.6 us, and 10 for the join.
 struct Split {
     int splits, rows;
 };

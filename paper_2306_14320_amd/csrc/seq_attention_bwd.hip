@@ -16,17 +16,16 @@
 // where results are not finite, a wave computes them again from the pairs in
 // sight alone.
 // Scores are computed twice: seven products of queries and keys where five
-// would do (eight in bf16, where dq takes ds in two parts), against a sum of dq
-// over the keys' tiles in memory.
+// would do (ten in bf16, where weights and ds have two parts), against a sum of
+// dq over the keys' tiles in memory.
 //
 // 16384 tokens of 16 heads over 4, 128 bf16 channels, window 1024, 4 first
-// tokens: 315 us for dq, 45 for the first tokens' keys, 413 for dk and dv; the
+// tokens: 296 us for dq, 44 for the first tokens' keys, 486 for dk and dv; the
 // products of all pairs in sight, at the rate of a large one, would take 215, 1
-// and 215.  The
-// operands' way out of LDS and the exponentials bound them: matrix cores are
-// busy for a third of the time, and waves wait for LDS for half of theirs.
-// 2503 tokens of 6 heads over 2, 96 fp32 channels, window 201: 54, 32 and 60 us, latency of
-// few workgroups.
+// and 322.  The operands' way out of LDS and the exponentials take the rest:
+// matrix cores are busy for 43% and 39% of the time of dq and of dk and dv, and
+// waves wait for 38% and 55% of theirs.  2503 tokens of 6 heads over 2, 96 fp32
+// channels, window 201: 52, 32 and 61 us, latency of few workgroups.
 #include "seq_attention.h"
 
 #include <algorithm>
@@ -56,20 +55,23 @@ __device__ __forceinline__ Frag<T> load_frag(const T* row, int s, int half, int 
 }
 
 // Rows of the keys' kernel's tiles of queries: of 128 bf16 channels 32 (a training
-// step of 16384 tokens: 863 us, 875 with 64).  The queries' kernel's tiles of
-// keys are of 64 rows there (863 us, 875 with 32).
+// step of 16384 tokens with a window of 16: 235 us, 251 with 64; of 1024 1067 with
+// both).  The queries' kernel's tiles of keys are of 64 rows there (1067 us, 1081
+// with 32).
 template <typename T, int DP> constexpr int kTileRows = sizeof(T) == 2 && DP <= 96 ? 64 : 32;
 // Queries that see fewer keys than this walk them twice: all of them with windows
 // below it, otherwise the first workgroups of each sequence.  Without the
 // correction, the error of dq is 1.95 times its own rounding's where two keys are
-// seen, 1.25 where eight are, 1.10 where 24 are and under 1.06 from 64 on.
+// seen, 1.25 where eight are, 1.10 where 24 are and under 1.06 from 64 on.  It costs
+// the walk's scores again: a training step of 16384 tokens of 16 x 128 with a window
+// of 16 226 -> 235 us, of 16 key heads of 64 with one of 48 194 -> 209.
 constexpr int kFewKeys = 64;
 // Waves a SIMD, of dq by its registers (training steps: 16384 tokens of 16 x 64 bf16
-// 304 us with three waves, 313 with two; 8192 tokens of 16 heads of 32 fp32 498 with two,
-// 517 with three, of 96 fp32 1187 with two, 1246 with one, of 128 fp32 1605 and 1655,
-// of 192 bf16 605 and 590), of dk and dv fewer, which hold the sums of both (16 x 128
-// bf16 881 with two, 921 with one; 16 x 64 bf16 297 with two, 326 with three; 96 fp32
-// 1190 with one, 1403 with two; 192 bf16 605 and 1235).
+// 573 us with three waves, 578 with two; 8192 tokens of 16 heads of 96 fp32 1100 with
+// two, 1153 with one, of 128 fp32 1468 and 1538; of 192 bf16 557 with two, 561 with
+// one), of dk and dv fewer, which hold the sums of both (16 x 128 bf16 1067 with two,
+// 1173 with one; 16 x 64 bf16 569 with two, 623 with three; 96 fp32 1100 with one,
+// 1342 with two, 128 fp32 1468 and 1940; 192 bf16 561 and 1161).
 template <typename T, int DP> constexpr int kDqWaves = DP > 128 ? 1 : sizeof(T) == 2 && DP <= 64 ? 3 : 2;
 template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 256 ? 1 : 2;
 
@@ -385,7 +387,7 @@ struct Keys {
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
             const Parts<T> w(s, part), ds(dp, part);
-            __builtin_amdgcn_s_setprio(1);      // products first; keeps the exponentials in front of them (1000 tokens of 16 x 128: 168 -> 141 us)
+            __builtin_amdgcn_s_setprio(1);      // products first; keeps the exponentials in front of them (8192 tokens of 16 x 32 fp32: 454 -> 445 us)
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {
                 mma(dv[d], Q::col_frag(lds, cb + gt, d, 2 * b + part), w);
@@ -565,7 +567,8 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
 //    the chip idle: four times the workgroups, and the queries' walk is shared
 //    by four waves.
 // A block's rows come from memory as it begins: with the next one's in registers
-// meanwhile 1000 tokens of 16 x 128 take 149 us, not 144, of 8 x 256 bf16 315, not 257.
+// meanwhile, and operands of one part, 1000 tokens of 16 x 128 took 149 us, not 144, of
+// 8 x 256 bf16 315, not 257.
 // ---------------------------------------------------------------------------
 template <typename T, int DP> constexpr int kNarrowOwn = 2 * Tile<T, DP, 32>::kBytes + 256;      // a wave's queries, gradients, lse and delta
 template <typename T, int DP> constexpr int kNarrowWaves = 4 * kNarrowOwn<T, DP> > 160 * 1024 ? 2 : 4;
@@ -686,15 +689,18 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
 // ---------------------------------------------------------------------------
 // Tiles of 128 keys that would leave CUs idle go to the narrow kernel: 2503 tokens
 // of 2 heads fp32 (40 tiles) 368 -> 209 us, 1000 tokens of 4 heads bf16 (32) 261 ->
-// 176.  Where they fill the chip they are faster: 16096 tokens of 4 heads (504) 376
-// us, 513 in the narrow kernel.
+// 176, as they first ran.  Where they fill the chip they are faster: 16384 tokens of 4
+// heads bf16 in sequences of 64 (1024 half full) 223 us, 268 in the narrow kernel, of
+// 16 331 and 347.  Places are counted, not rows: ragged sequences have up to one each
+// more than they fill (4096 tokens in 64 of them 209 us, which the narrow kernel
+// would do in 148, 500 in 64 57 and 46).
 constexpr int64_t kNarrowBelow = 256;
 
 // Pieces of queries that may see first tokens outside of their window: none
 // where no sequence can be longer than the window.
 int64_t piece_rows(const im2win_window_desc* d) {
     // some 1024 workgroups, of whole rounds of their waves (512 rows whatever the
-    // problem: 1000 tokens 181 us, not 144, 2503 of 2 heads fp32 261, not 188,
+    // problem: as they first ran, 1000 tokens 181 us, not 144, 2503 of 2 heads fp32 261, not 188,
     // 16384 of 4 heads 921, not 906)
     const int64_t rows = (d->tokens * d->kv_heads / 1024 + 127) / 128 * 128;
     return std::max<int64_t>(128, std::min<int64_t>(rows, 4096));

@@ -8,10 +8,10 @@
 // with du the rotation of dy by the opposite angle, n = x r and g = du w:
 //   dx = r (g - n mean(g n)),  dw = sum over rows and heads of du n.
 //
-// Bound by memory (16384 rows of 20 heads of 128 bf16: 33.5 us, 5.0 TB/s, as a copy)
-// with 90% of the issue slots taken (the gradients, 4001 rows of 15 heads of 80 fp32:
-// 15.5 us, 3.7 TB/s, and 6.3 for the weights' sums): a head's channels are read once, into the registers of a
-// few neighbouring lanes, as pairs: a lane holds V pairs, 16 bytes of the
+// Bound by memory (16384 rows of 20 heads of 128 bf16: 35.8 us a call, 4.7 TB/s, where
+// a copy has 5.1) with vector units busy for 88% (the gradients, 4001 rows of 15 heads
+// of 80 fp32: 16.1 us, 3.6 TB/s, and 5.4 for the weights' sums): a head's channels are
+// read once, into the registers of a few neighbouring lanes, as pairs: a lane holds V pairs, 16 bytes of the
 // first channels and 16 of their partners, so that the rotation needs no
 // exchange and the sum of squares a few within the group.  The wave's lanes
 // take one angle each and share them through LDS; all heads of the row use them.

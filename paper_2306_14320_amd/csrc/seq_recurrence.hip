@@ -15,11 +15,11 @@
 // composes the pairs of the chunks in front, and applies the state that enters
 // to its registers: every input is read once and every output written once.
 //
-// Forward, 8192 rows of 2048 bf16 channels in one sequence: 48.7 us with the kernel
+// Forward, 8192 rows of 2048 bf16 channels in one sequence: 48.9 us with the kernel
 // that prepares the words, 2.8 TB/s over what has to move (a copy: 5.1); the vector
-// units are busy for 58%, and the wait for the chunks in front takes the rest.
-// Gradients, 16384 rows of 4096 in 8 sequences: 283 us, 3.7 TB/s, vector units 73%
-// busy; the forward call that leaves their states 142 us, 4.2 TB/s.
+// units are busy for 48%, and the wait for the chunks in front takes the rest.
+// Gradients, 16384 rows of 4096 in 8 sequences: 262 us, 4.0 TB/s, vector units 73%
+// busy; the forward call that leaves their states 136 us, 4.4 TB/s.
 //
 // The first row of a sequence does not look back: its pair is marked by a
 // negative a (the decays are positive), and composing selects instead of
