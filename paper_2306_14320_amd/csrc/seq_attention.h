@@ -84,13 +84,35 @@ template <> struct Parts<bf16> {
         __builtin_memcpy(&low, l, 16);
     }
 
-private:
+protected:
+    __device__ __forceinline__ Parts() {}
     static __device__ __forceinline__ uint32_t pair(float x, float y) {
         const __bf16 __attribute__((ext_vector_type(2))) v = {(bf16)x, (bf16)y};
         uint32_t u;
         __builtin_memcpy(&u, &v, 4);
         arrive(u);
         return u;
+    }
+};
+
+// Weights, which are not negative: the first part is cut off, not rounded, and
+// 2^-18 of it is added to the second, which then is zero with the weight alone: an
+// infinity times both is one (together off by 2^-15).
+template <typename T> struct Weights : Parts<T> {
+    using Parts<T>::Parts;
+};
+template <> struct Weights<bf16> : Parts<bf16> {
+    __device__ __forceinline__ Weights(const f32x16& s, int part) {
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t x = __float_as_uint(s[8 * part + 2 * j]), y = __float_as_uint(s[8 * part + 2 * j + 1]);
+            const uint32_t xh = x & 0xffff0000u, yh = y & 0xffff0000u;
+            h[j] = xh >> 16 | yh;
+            l[j] = pair(fmaf(__uint_as_float(xh), 0x1p-18f - 1.0f, __uint_as_float(x)), fmaf(__uint_as_float(yh), 0x1p-18f - 1.0f, __uint_as_float(y)));
+        }
+        __builtin_memcpy(&high, h, 16);
+        __builtin_memcpy(&low, l, 16);
     }
 };
 template <typename T>

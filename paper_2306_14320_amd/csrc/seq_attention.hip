@@ -109,44 +109,6 @@ template <typename T, int DP> constexpr bool kStepAhead = DP * sizeof(T) <= 512 
 // A wave's LDS for 32 rows: keys and values, or values in the place of keys
 template <typename T, int DP> constexpr int kStepStage = (kStepAhead<T, DP> ? 2 : 1) * Tile<T, DP, 32>::kBytes;
 
-// An infinity among the values of a tile that all columns see is NaN times a
-// weight's two parts.  For the wave's columns `bad` such channels get the sum of
-// what they see that is not finite, as in tiles that some columns see in part.
-template <typename T>
-__device__ __forceinline__ void put_nonfinite(uint32_t bad) {
-    const Again<AttnArgs> a = arguments<AttnArgs>();
-    const int64_t item = die_order(a.block, a.items);
-    const SeqTile st = seq_tile(a.seq, (int)(item % a.places), a.tile);
-    const int lane = threadIdx.x % kWave, h0 = (int)(item / a.places) * a.pack, kvh = h0 / (a.q_heads / a.kv_heads);
-    const int64_t slot = !a.k_cache ? 0 : a.slots ? uniform(a.slots[st.b]) : st.b;
-    const int past = a.k_cache ? past_of(a.past, st.b) : 0;
-    for (; bad; bad &= bad - 1) {
-        const int n = uniform(threadIdx.x / kWave) * kCols + __builtin_ctz(bad), row = st.row + n / a.pack, pos = past + row;
-        const int low = pos - a.window + 1 > 0 ? pos - a.window + 1 : 0, first = a.sinks < low ? a.sinks : low;
-        float sum[4] = {};      // 256 channels
-        for (int i = 0; i < first + pos + 1 - low; ++i) {
-            const int p = i < first ? i : low + i - first;
-            const T* v = p < past ? static_cast<const T*>(a.v_cache) + ((slot * (a.sinks + a.window) + ring(p, a.window, a.sinks)) * a.kv_heads + kvh) * a.dim
-                                  : static_cast<const T*>(a.v) + (int64_t)(st.first + p - past) * a.ld_v + (int64_t)kvh * a.dim;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const T x = lane + e * kWave < a.dim ? v[lane + e * kWave] : (T)0.0f;
-                sum[e] += finite(x) ? 0.0f : (float)x;
-            }
-            if (i % 16 == 0) {      // all channels NaN: whatever else they see
-                bool done = true;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) done &= lane + e * kWave >= a.dim || sum[e] != sum[e];
-                if (!__ballot(!done)) break;
-            }
-        }
-        T* y = static_cast<T*>(a.y) + ((int64_t)(st.first + row) * a.q_heads + h0 + n % a.pack) * a.dim;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (!finite(sum[e])) y[lane + e * kWave] = (T)sum[e];
-    }
-}
-
 // ---------------------------------------------------------------------------
 // Prompts and training: a workgroup takes up to 128 columns, the queries of
 // `tile` rows for `pack` heads that share keys and values.  Their tiles pass
@@ -294,7 +256,7 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
             __builtin_amdgcn_s_setprio(1);      // a wave with products to issue goes first
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
-                const Parts<T> w(s[0], part);
+                const Weights<T> w(s[0], part);
 #pragma unroll
                 for (int t = 0; t < DP / 32; ++t) mma(r.o[t], KV::col_frag(lds, vb, t, 2 * b + part), w);
             }
@@ -319,7 +281,7 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
             }
     }
     const float l = half_sum(r.l);
-    const uint64_t bad = sizeof(T) == 2 ? __ballot(live && finite(l) && nonfinite(r.o)) : 0;
+    if (!live) return;
     // A query sees itself, so a served one's l is zero only where all of its scores are
     // -inf: 0 / 0 then, as the softmax has it.
     const float scale = served ? 1.0f / l : 0.0f;
@@ -330,10 +292,9 @@ __global__ __launch_bounds__(kAttnThreads, (kFwdWaves<T, DP>)) void window_atten
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
             const int d = 32 * b + acc_row(i, half);
-            if (live && d < a.dim) put4(y + d, r.o[b][i] * scale, r.o[b][i + 1] * scale, r.o[b][i + 2] * scale, r.o[b][i + 3] * scale);
+            if (d < a.dim) put4(y + d, r.o[b][i] * scale, r.o[b][i + 1] * scale, r.o[b][i + 2] * scale, r.o[b][i + 3] * scale);
         }
-    if (a.lse && live && half == 0) a.lse[t * a.q_heads + head] = l == 0.0f ? -INFINITY : (r.m + __builtin_amdgcn_logf(l)) * kLn2;
-    if (bad) put_nonfinite<T>((uint32_t)bad | (uint32_t)(bad >> 32));
+    if (a.lse && half == 0) a.lse[t * a.q_heads + head] = l == 0.0f ? -INFINITY : (r.m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // The cache behind a prompt: a wave takes a new token, and copies its keys and
@@ -369,32 +330,6 @@ __global__ __launch_bounds__(kAttnThreads) void window_cache_kernel(AttnArgs a) 
 // 48.6 with weights of one part).  In fp32 the matrix instructions bound it, of
 // which a request's 4 heads use 4 columns of 32: 141 us, 87 at a copy's rate.
 // ---------------------------------------------------------------------------
-// An infinity among the values (as in put_nonfinite): the wave's rows, for all heads
-template <typename T>
-__device__ __forceinline__ void put_nonfinite_shares(float* o) {
-    const Again<AttnArgs> a = arguments<AttnArgs>();
-    const int lane = threadIdx.x % kWave, blocks = a.q_heads / a.pack, split = a.block % a.splits, b = a.block / a.splits / blocks;
-    const int kvh = a.block / a.splits % blocks * a.pack / (a.q_heads / a.kv_heads), rows = a.sinks + a.window;
-    const int past = past_of(a.past, b), fresh = ring(past, a.window, a.sinks), filled = past + 1 < rows ? past + 1 : rows;
-    const int from = split * a.split_rows, to = from + a.split_rows < filled ? from + a.split_rows : filled;
-    const T* cache = static_cast<const T*>(a.v_cache) + ((int64_t)(a.slots ? uniform(a.slots[b]) : b) * rows * a.kv_heads + kvh) * a.dim;
-    const T* now = static_cast<const T*>(a.v) + b * a.ld_v + (int64_t)kvh * a.dim;
-    float sum[4] = {};      // 256 channels
-    for (int base = from + uniform(threadIdx.x / kWave) * 32; base < to; base += 32 * kAttnThreads / kWave)
-        for (int r = base; r < base + 32 && r < to; ++r) {
-            const T* v = r == fresh ? now : cache + (int64_t)r * a.kv_heads * a.dim;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const T x = lane + e * kWave < a.dim ? v[lane + e * kWave] : (T)0.0f;
-                sum[e] += finite(x) ? 0.0f : (float)x;
-            }
-        }
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (!finite(sum[e]))
-            for (int c = 0; c < a.pack; ++c) o[(lane + e * kWave) * a.pack + c] = sum[e];
-}
-
 template <typename T, int DP>
 __global__ __launch_bounds__(kAttnThreads, (step_waves(DP * sizeof(T)))) void window_step_kernel(AttnArgs a) {
     using V = Tile<T, DP, 32>;
@@ -480,21 +415,19 @@ __global__ __launch_bounds__(kAttnThreads, (step_waves(DP * sizeof(T)))) void wi
         soften<DP, 1>(r, s, a.c);
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
-            const Parts<T> w(s[0], part);
+            const Weights<T> w(s[0], part);
 #pragma unroll
             for (int t = 0; t < DP / 32; ++t) mma(r.o[t], V::col_frag(values, cb, t, part), w);
         }
     }
     // the four waves' shares: a channel's row of columns each, and their statistics
     r.l = half_sum(r.l);
-    const bool bad = sizeof(T) == 2 && __ballot(finite(r.l) && nonfinite(r.o));
     float* o = reinterpret_cast<float*>(mine);
 #pragma unroll
     for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             if (col < a.pack) o[(32 * t + acc_row(i, half)) * a.pack + col] = r.o[t][i];
-    if (bad) put_nonfinite_shares<T>(o);
     if (half == 0) ml[wave][0][col] = r.m, ml[wave][1][col] = r.l;
     __syncthreads();
     for (int n = tid; n < a.dim * a.pack; n += kAttnThreads) {

@@ -386,7 +386,8 @@ struct Keys {
         }
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
-            const Parts<T> w(s, part), ds(dp, part);
+            const Weights<T> w(s, part);
+            const Parts<T> ds(dp, part);
             __builtin_amdgcn_s_setprio(1);      // products first; keeps the exponentials in front of them (8192 tokens of 16 x 32 fp32: 454 -> 445 us)
 #pragma unroll
             for (int d = 0; d < DP / 32; ++d) {

@@ -128,3 +128,50 @@ def test_step_infinite_values(dtype, window):
     want = clean.clone()
     want[0, 2:, 9], want[2, :2, 63], want[2, :2, 62] = INF, -INF, NAN
     assert torch.equal(torch.nan_to_num(y, nan=77.0), torch.nan_to_num(want, nan=77.0))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+@pytest.mark.parametrize("shape, lo, hi", SHAPES[:1] + SHAPES[2:], ids=["small", "wide", "many", "long"])
+def test_lowest_values_in_masked_places(shape, lo, hi, dtype):
+    """The type's lowest and largest finite values: what does not see them keeps its bits."""
+    def run(change):
+        c = Case(dtype, *shape)
+        dy = torch.randn(c.tokens, c.h, c.dim, generator=torch.Generator().manual_seed(7)).to(dtype).to(DEV)
+        change(c, dy)
+        lse = torch.empty(c.tokens, c.h, device=DEV)
+        y = c.run(lse=lse)
+        return c, (y,) + tuple(P.window_attention_backward(dy, c.q, c.k, c.v, y, lse, c.desc, seq_starts=c.sp))
+
+    low, high = torch.finfo(dtype).min, torch.finfo(dtype).max
+    c, clean = run(lambda c, dy: None)
+    j = torch.arange(hi - lo)
+    see = (j[None] <= j[:, None]) & ((j[None] > j[:, None] - c.window) | (j[None] < c.sinks))      # query, key
+    key, query = 40, 60
+
+    def keys(c, dy):
+        c.k[lo + key], c.v[lo + key] = low, high
+
+    _, got = run(keys)
+    rows = [int(t) for t in j if not see[t, key]]                          # queries that do not see the key,
+    others = [int(t) for t in j if not (see[:, t] & see[:, key]).any()]    # keys that no query sees beside it
+    assert len(rows) > 20
+    assert all(torch.equal(a[lo:hi][rows], b[lo:hi][rows]) for a, b in zip(got[:2], clean[:2]))
+    assert all(torch.equal(a[lo:hi][others], b[lo:hi][others]) for a, b in zip(got[2:], clean[2:]))
+
+    def queries(c, dy):
+        c.q[lo + query], dy[lo + query] = high, low
+
+    _, got = run(queries)
+    rows, others = [int(t) for t in j if t != query], [int(t) for t in j if not see[query, t]]
+    assert all(torch.equal(a[lo:hi][rows], b[lo:hi][rows]) for a, b in zip(got[:2], clean[:2]))
+    assert len(others) > 20 and all(torch.equal(a[lo:hi][others], b[lo:hi][others]) for a, b in zip(got[2:], clean[2:]))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=str)
+def test_step_first_token_of_infinity(dtype):
+    """A weight of exactly one."""
+    q, k, v = (torch.ones(2, n, 32, device=DEV, dtype=dtype) for n in (2, 1, 1))
+    v[0, 0, 3], v[1, 0, 4] = INF, -INF
+    caches = [torch.full((2, 9, 1, 32), NAN, device=DEV, dtype=dtype) for _ in range(2)]
+    y = P.window_attention_step(q, k, v, *caches, torch.zeros(2, dtype=torch.int32, device=DEV), P.window_attention_desc_for(q, k, v, 9))
+    assert torch.equal(y, v.expand_as(y))
