@@ -76,35 +76,25 @@ template <typename T, int DP> constexpr int kDqWaves = DP > 128 ? 1 : sizeof(T) 
 template <typename T, int DP> constexpr int kDkvWaves = DP * sizeof(T) > 256 ? 1 : 2;
 
 // ---------------------------------------------------------------------------
-// Results that are not finite, from the formulas over the pairs in sight: a wave
-// takes a query, or a key, and its lanes the channels, a pair after the other.
-// Slow, for the few places that stand in a block with an infinity or a NaN that
-// they do not see; where lse or delta is not finite itself, the results are what
-// they should be.
+// Results that are not finite, from the formulas over the pairs in sight: for the
+// few places that stand in a block with an infinity or a NaN that they do not see.
+// A wave takes a query, or a key: its lanes compute 64 pairs' weights and ds, a
+// pair each, and then add the pairs' rows one after the other, a channel each.
+// Where lse or delta is not finite itself, all results are NaN already.
 // ---------------------------------------------------------------------------
 constexpr int kLaneChannels = 4;       // 256 channels
 
+// Channels lane, lane + 64, .. of a row
 template <typename T>
 struct Row {
     float v[kLaneChannels] = {};
     __device__ __forceinline__ Row() {}
     __device__ __forceinline__ Row(const T* p, int lane, int dim) {
 #pragma unroll
-        for (int i = 0; i < kLaneChannels; ++i) v[i] = lane + i * kWave < dim ? (float)p[lane + i * kWave] : 0.0f;
-    }
-    __device__ __forceinline__ float dot(const Row& o) const {
-        float s = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kLaneChannels; ++i) s = fmaf(v[i], o.v[i], s);
-#pragma unroll
-        for (int m = 1; m < kWave; m *= 2) s += __shfl_xor(s, m);
-        return s;
-    }
-    __device__ __forceinline__ bool any_finite(int lane, int dim) const {
-        bool any = false;
-#pragma unroll
-        for (int i = 0; i < kLaneChannels; ++i) any |= lane + i * kWave < dim && finite(v[i]);
-        return __ballot(any);
+        for (int i = 0; i < kLaneChannels; ++i) {      // (loads of all lanes, which can be under way together)
+            const T x = p[lane + i * kWave < dim ? lane + i * kWave : 0];
+            v[i] = lane + i * kWave < dim ? (float)x : 0.0f;
+        }
     }
     __device__ __forceinline__ void add(float w, const Row& o) {
 #pragma unroll
@@ -117,24 +107,40 @@ struct Row {
     }
 };
 
+// The product of a lane's rows
+template <typename T>
+__device__ __forceinline__ float dot(const T* a, const T* b, int dim) {
+    float s = 0.0f;
+    for (int c = 0; c < dim; c += 8) {
+        Frag<T> x, y;
+        x.load(a + c);
+        y.load(b + c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = fmaf(x.get(i), y.get(i), s);
+    }
+    return s;
+}
+
 template <typename T>
 __device__ __forceinline__ void repair_query(const AttnBwdArgs& a, const SeqTile& st, int pos, int head, float delta) {
     const int lane = threadIdx.x % kWave, kvh = head / (a.q_heads / a.kv_heads);
     const int64_t t = st.first + pos, at = t * a.q_heads + head;
-    T* dq = static_cast<T*>(a.dq) + at * a.dim;
     const float lse = a.lse[at] * kLog2e;
     if (!__ballot(finite(lse) && finite(delta))) return;
-    const Row<T> q(static_cast<const T*>(a.q) + t * a.ld_q + (int64_t)head * a.dim, lane, a.dim), g(static_cast<const T*>(a.dy) + at * a.dim, lane, a.dim);
+    const T *q = static_cast<const T*>(a.q) + t * a.ld_q + (int64_t)head * a.dim, *g = static_cast<const T*>(a.dy) + at * a.dim;
+    const int low = pos - a.window + 1 > 0 ? pos - a.window + 1 : 0, first = a.sinks < low ? a.sinks : low, count = first + pos + 1 - low;
+    const float several = pos == 0 || (a.window == 1 && a.sinks == 0) ? 0.0f : 1.0f;
+    auto key = [&](int n) { return (int64_t)st.first + (n < first ? n : low + n - first); };
     Row<T> sum;
-    const int low = pos - a.window + 1 > 0 ? pos - a.window + 1 : 0, first = a.sinks < low ? a.sinks : low;
-    const bool single = pos == 0 || (a.window == 1 && a.sinks == 0);
-    for (int n = 0; n < first + pos + 1 - low; ++n) {
-        const int64_t p = st.first + (n < first ? n : low + n - first);
-        const Row<T> k(static_cast<const T*>(a.k) + p * a.ld_k + (int64_t)kvh * a.dim, lane, a.dim), v(static_cast<const T*>(a.v) + p * a.ld_v + (int64_t)kvh * a.dim, lane, a.dim);
-        const float ds = __builtin_amdgcn_exp2f(fmaf(q.dot(k), a.c, -lse)) * (g.dot(v) - delta);
-        sum.add(single ? 0.0f * ds : ds, k);
+    for (int n0 = 0; n0 < count; n0 += kWave) {
+        const int here = count - n0 < kWave ? count - n0 : kWave;
+        const int64_t mine = key(n0 + (lane < here ? lane : 0));
+        const float s = dot(static_cast<const T*>(a.k) + mine * a.ld_k + (int64_t)kvh * a.dim, q, a.dim), dp = dot(static_cast<const T*>(a.v) + mine * a.ld_v + (int64_t)kvh * a.dim, g, a.dim);
+        const float ds = __builtin_amdgcn_exp2f(fmaf(s, a.c, -lse)) * (dp - delta) * several;
+#pragma unroll 8
+        for (int r = 0; r < here; ++r) sum.add(__shfl(ds, r), Row<T>(static_cast<const T*>(a.k) + key(n0 + r) * a.ld_k + (int64_t)kvh * a.dim, lane, a.dim));
     }
-    sum.put(dq, lane, a.dim, a.scale);
+    sum.put(static_cast<T*>(a.dq) + at * a.dim, lane, a.dim, a.scale);
 }
 
 template <typename T>
@@ -143,25 +149,42 @@ __device__ __forceinline__ void repair_key(const AttnBwdArgs& a, const SeqTile& 
     const int64_t t = st.first + key, to = (t * a.kv_heads + kvh) * a.dim;
     T *dk = static_cast<T*>(a.dk) + to, *dv = static_cast<T*>(a.dv) + to;
     const int end = key < a.sinks || st.len - key < a.window ? st.len : key + a.window;
-    bool bad_lse = false, bad_delta = false;
-    for (int p = key + lane; p < end; p += kWave)
-        for (int h = kvh * group; h < kvh * group + group; ++h) {
-            bad_lse |= !finite(a.lse[(int64_t)(st.first + p) * a.q_heads + h]);
-            bad_delta |= !finite(a.delta[(int64_t)(st.first + p) * a.q_heads + h]);
+    auto row = [&](int p, int h) { return (int64_t)(st.first + p) * a.q_heads + kvh * group + h; };
+    // What the rows in sight account for: dk where a delta is not finite, and the
+    // channels of dv where that row's dy (whose every infinity shows in delta) is not.
+    Row<T> open(dv, lane, a.dim);
+    for (int h = 0; h < group; ++h)
+        for (int p0 = key; p0 < end; p0 += kWave) {
+            const int64_t mine = row(p0 + lane < end ? p0 + lane : end - 1, h);
+            if (__ballot(!finite(a.lse[mine]))) return;
+            uint64_t bad = __ballot(p0 + lane < end && !finite(a.delta[mine]));
+            if (bad) need_k = false;
+            for (; bad && need_v; bad &= bad - 1) {
+                const Row<T> g(static_cast<const T*>(a.dy) + row(p0 + __builtin_ctzll(bad), h) * a.dim, lane, a.dim);
+                bool any = false;
+#pragma unroll
+                for (int i = 0; i < kLaneChannels; ++i) {
+                    open.v[i] = finite(g.v[i]) ? open.v[i] : 0.0f;
+                    any |= !finite(open.v[i]);
+                }
+                need_v = __ballot(any);
+            }
+            if (!need_k && !need_v) return;
         }
-    need_v = need_v && !__ballot(bad_lse);
-    need_k = need_k && !__ballot(bad_lse || bad_delta);
-    const Row<T> k(static_cast<const T*>(a.k) + t * a.ld_k + (int64_t)kvh * a.dim, lane, a.dim), v(static_cast<const T*>(a.v) + t * a.ld_v + (int64_t)kvh * a.dim, lane, a.dim);
+    const T *k = static_cast<const T*>(a.k) + t * a.ld_k + (int64_t)kvh * a.dim, *v = static_cast<const T*>(a.v) + t * a.ld_v + (int64_t)kvh * a.dim;
     Row<T> sum_k, sum_v;
-    for (int h = kvh * group; h < kvh * group + group; ++h)
-        for (int p = key; p < end && (need_k || need_v); ++p) {
-            const int64_t row = st.first + p, at = row * a.q_heads + h;
-            const Row<T> q(static_cast<const T*>(a.q) + row * a.ld_q + (int64_t)h * a.dim, lane, a.dim), g(static_cast<const T*>(a.dy) + at * a.dim, lane, a.dim);
-            const float w = __builtin_amdgcn_exp2f(fmaf(q.dot(k), a.c, -a.lse[at] * kLog2e));
-            sum_v.add(w, g);
-            const float ds = w * (g.dot(v) - a.delta[at]);
-            sum_k.add(p == 0 || (a.window == 1 && a.sinks == 0) ? 0.0f * ds : ds, q);
-            if (!need_k && p % 16 == 0) need_v = sum_v.any_finite(lane, a.dim);      // (of dy that is NaN throughout, nothing)
+    for (int h = 0; h < group; ++h)
+        for (int p0 = key; p0 < end; p0 += kWave) {
+            const int here = end - p0 < kWave ? end - p0 : kWave, mine = p0 + (lane < here ? lane : 0);
+            auto query = [&](int p) { return static_cast<const T*>(a.q) + (int64_t)(st.first + p) * a.ld_q + (int64_t)(kvh * group + h) * a.dim; };
+            auto grad = [&](int p) { return static_cast<const T*>(a.dy) + row(p, h) * a.dim; };
+            const float w = __builtin_amdgcn_exp2f(fmaf(dot(query(mine), k, a.dim), a.c, -a.lse[row(mine, h)] * kLog2e));
+            const float ds = w * (dot(grad(mine), v, a.dim) - a.delta[row(mine, h)]) * (mine == 0 || (a.window == 1 && a.sinks == 0) ? 0.0f : 1.0f);
+#pragma unroll 8
+            for (int r = 0; r < here; ++r) {
+                sum_v.add(__shfl(w, r), Row<T>(grad(p0 + r), lane, a.dim));
+                sum_k.add(__shfl(ds, r), Row<T>(query(p0 + r), lane, a.dim));
+            }
         }
     if (need_k) sum_k.put(dk, lane, a.dim, a.scale);
     if (need_v) sum_v.put(dv, lane, a.dim, 1.0f);
