@@ -96,8 +96,8 @@ protected:
 };
 
 // Weights, which are not negative: the first part is cut off, not rounded, and
-// 2^-18 of it is added to the second, which then is zero with the weight alone: an
-// infinity times both is one (together off by 2^-15).
+// 2^-24 of it is added to the second, which then is zero with the weight alone: an
+// infinity times both is one (together off by 2^-16).
 template <typename T> struct Weights : Parts<T> {
     using Parts<T>::Parts;
 };
@@ -109,7 +109,7 @@ template <> struct Weights<bf16> : Parts<bf16> {
             const uint32_t x = __float_as_uint(s[8 * part + 2 * j]), y = __float_as_uint(s[8 * part + 2 * j + 1]);
             const uint32_t xh = x & 0xffff0000u, yh = y & 0xffff0000u;
             h[j] = xh >> 16 | yh;
-            l[j] = pair(fmaf(__uint_as_float(xh), 0x1p-18f - 1.0f, __uint_as_float(x)), fmaf(__uint_as_float(yh), 0x1p-18f - 1.0f, __uint_as_float(y)));
+            l[j] = pair(fmaf(__uint_as_float(xh), 0x1p-24f - 1.0f, __uint_as_float(x)), fmaf(__uint_as_float(yh), 0x1p-24f - 1.0f, __uint_as_float(y)));
         }
         __builtin_memcpy(&high, h, 16);
         __builtin_memcpy(&low, l, 16);
@@ -338,30 +338,6 @@ __device__ __forceinline__ bool nonfinite(const f32x16 (&o)[N]) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) z = fmaf(o[t][i], 0.0f, z);
     return !(z == 0.0f);
-}
-
-// A kernel's arguments (all of them, A), loaded again, and its block: what the
-// rare work behind a walk needs is worked out anew, since held over the walk it
-// would take the walk's registers (a training step of 16384 tokens 925 us, 903 so).
-template <typename A>
-struct Again : A {
-    int block;
-};
-template <typename A>
-__device__ __forceinline__ Again<A> arguments() {
-    typedef const __attribute__((address_space(4))) uint64_t* Words;
-    Words p = (Words)__builtin_amdgcn_kernarg_segment_ptr();
-    int block = blockIdx.x;
-    asm volatile("" : "+s"(p), "+s"(block));
-    constexpr int N = sizeof(A) / 8;
-    static_assert(sizeof(A) % 8 == 0, "whole words");
-    uint64_t w[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = p[i];
-    Again<A> a;
-    __builtin_memcpy(static_cast<A*>(&a), w, sizeof(A));
-    a.block = block;
-    return a;
 }
 
 // ---------------------------------------------------------------------------

@@ -190,10 +190,32 @@ __device__ __forceinline__ void repair_key(const AttnBwdArgs& a, const SeqTile& 
     if (need_v) sum_v.put(dv, lane, a.dim, 1.0f);
 }
 
+// The kernel's arguments (it has no others), loaded again, and its block: what the
+// second computation needs is worked out anew, since held over the walk it would
+// take the walk's registers (a training step of 16384 tokens 925 us, 903 so).
+struct Again : AttnBwdArgs {
+    int block;
+};
+__device__ __forceinline__ Again arguments() {
+    typedef const __attribute__((address_space(4))) uint64_t* Words;
+    Words p = (Words)__builtin_amdgcn_kernarg_segment_ptr();
+    int block = blockIdx.x;
+    asm volatile("" : "+s"(p), "+s"(block));
+    constexpr int N = sizeof(AttnBwdArgs) / 8;
+    static_assert(sizeof(AttnBwdArgs) % 8 == 0, "whole words");
+    uint64_t w[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = p[i];
+    Again a;
+    __builtin_memcpy(static_cast<AttnBwdArgs*>(&a), w, sizeof(AttnBwdArgs));
+    a.block = block;
+    return a;
+}
+
 // The queries (columns of the wave) of a tile, and keys (from `from` on), with a bit each
 template <typename T>
 __device__ __forceinline__ void repair_queries(uint32_t bad, float delta) {
-    const Again<AttnBwdArgs> a = arguments<AttnBwdArgs>();
+    const Again a = arguments();
     const int64_t item = die_order(a.block, a.q_items);
     const SeqTile st = seq_tile(a.seq, (int)(item % a.q_places), a.tile);
     for (; bad; bad &= bad - 1) {
@@ -207,6 +229,17 @@ __device__ __forceinline__ void repair_keys(const AttnBwdArgs& a, const SeqTile&
         const int c = __builtin_ctz(bad);
         repair_key<T>(a, st, st.row + uniform(from) + c, kvh, bad_k >> c & 1, bad_v >> c & 1);
     }
+}
+// (Called where the walk spills by the hundreds: 4096 tokens of 8 x 256 fp32 1541 us
+// with it inlined, 1433 so; narrower walks have registers that a call would take.)
+template <typename T>
+__device__ __attribute__((noinline)) void call_repair_keys(const AttnBwdArgs& a, const SeqTile& st, int kvh, int from, uint32_t bad_k, uint32_t bad_v) {
+    repair_keys<T>(a, st, kvh, from, bad_k, bad_v);
+}
+template <typename T, int DP>
+__device__ __forceinline__ void repair_tile(const AttnBwdArgs& a, const SeqTile& st, int kvh, int from, uint32_t bad_k, uint32_t bad_v) {
+    if constexpr (DP * sizeof(T) > 768) call_repair_keys<T>(a, st, kvh, from, bad_k, bad_v);
+    else repair_keys<T>(a, st, kvh, from, bad_k, bad_v);
 }
 
 // ---------------------------------------------------------------------------
@@ -574,9 +607,9 @@ __global__ __launch_bounds__(kAttnThreads, (kDkvWaves<T, DP>)) void window_dkv_k
             put4(static_cast<T*>(a.dv) + to + d, keys.dv[b][i], keys.dv[b][i + 1], keys.dv[b][i + 2], keys.dv[b][i + 3]);
         }
     if (bad_k | bad_v) {
-        const Again<AttnBwdArgs> b = arguments<AttnBwdArgs>();
+        const Again b = arguments();
         const int64_t n = die_order(b.block, b.k_items);
-        repair_keys<T>(b, seq_tile(b.seq, (int)(n % b.k_places), kGroupCols), (int)(n / b.k_places), threadIdx.x / kWave * kCols,
+        repair_tile<T, DP>(b, seq_tile(b.seq, (int)(n % b.k_places), kGroupCols), (int)(n / b.k_places), threadIdx.x / kWave * kCols,
                        (uint32_t)bad_k | (uint32_t)(bad_k >> 32), (uint32_t)bad_v | (uint32_t)(bad_v >> 32));
     }
 }
@@ -701,10 +734,10 @@ __global__ __launch_bounds__((kNarrowWaves<T, DP> * kWave), (DP * sizeof(T) > 12
         }
     if constexpr (!FIRST)
         if (again[0] | again[1]) {
-            const Again<AttnBwdArgs> b = arguments<AttnBwdArgs>();
+            const Again b = arguments();
             const int64_t n = die_order(b.block, b.k_items);
             const uint32_t mine = (NW == 4 ? 0x11111111u : 0x55555555u) << threadIdx.x / kWave;
-            repair_keys<T>(b, seq_tile(b.seq, (int)(n / b.kv_heads), kCols), (int)(n % b.kv_heads), 0, again[0] & mine, again[1] & mine);
+            repair_tile<T, DP>(b, seq_tile(b.seq, (int)(n / b.kv_heads), kCols), (int)(n % b.kv_heads), 0, again[0] & mine, again[1] & mine);
         }
 }
 
