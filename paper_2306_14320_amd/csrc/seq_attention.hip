@@ -10,9 +10,9 @@
 // window rows, in which the call leaves the new tokens' keys and values.
 //
 // 16384 tokens of 16 heads over 4, 128 bf16 channels, window 1024, in front of the
-// gradients: 235 us, where three products (the weights have two parts) would take
-// 161 at the rate of a large one; matrix cores are busy for 43%, vector units for
-// 51%, and waves wait for 37% of their cycles.  9001 tokens of 12 heads over 4, 64
+// gradients: 227 us, where three products (the weights have two parts) would take
+// 161 at the rate of a large one; matrix cores are busy for 44%, vector units for
+// 51%, and waves wait for 36% of their cycles.  9001 tokens of 12 heads over 4, 64
 // channels, window 500, 13 ragged prompts: 47 us (17 for the products), and 5 for
 // the caches; vector units 61%, matrix cores 25%: exponentials, maximum, sum and
 // both parts of 64 channels' weights take longer than their products.

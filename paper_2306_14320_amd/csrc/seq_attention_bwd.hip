@@ -20,12 +20,12 @@
 // dq over the keys' tiles in memory.
 //
 // 16384 tokens of 16 heads over 4, 128 bf16 channels, window 1024, 4 first
-// tokens: 296 us for dq, 44 for the first tokens' keys, 486 for dk and dv; the
+// tokens: 291 us for dq, 45 for the first tokens' keys, 480 for dk and dv; the
 // products of all pairs in sight, at the rate of a large one, would take 215, 1
 // and 322.  The operands' way out of LDS and the exponentials take the rest:
-// matrix cores are busy for 43% and 39% of the time of dq and of dk and dv, and
-// waves wait for 38% and 55% of theirs.  2503 tokens of 6 heads over 2, 96 fp32
-// channels, window 201: 52, 32 and 61 us, latency of few workgroups.
+// matrix cores are busy for 43% and 38% of the time of dq and of dk and dv, and
+// waves wait for 38% and 56% of theirs.  2503 tokens of 6 heads over 2, 96 fp32
+// channels, window 201: 52, 31 and 60 us, latency of few workgroups.
 #include "seq_attention.h"
 
 #include <algorithm>
